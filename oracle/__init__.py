@@ -191,6 +191,77 @@ def rmsnorm_bwd(dy, x, gamma, rstd, bf=False):
     return dx, dg
 
 
+def layernorm_fwd(x, gamma, beta, eps=1e-6, bf=False):
+    x, gamma, beta = _io(x, bf), _io(gamma, bf), _io(beta, bf)
+    rows, D = x.shape
+    y = np.empty_like(x)
+    mean, rstd = np.empty(rows, np.float32), np.empty(rows, np.float32)
+    lib().orc_layernorm_fwd(C.c_int(int(bf)), _p(x), _p(gamma), _p(beta), C.c_int(rows), C.c_int(D), C.c_float(eps), _p(y), _p(mean), _p(rstd))
+    return y, mean, rstd
+
+
+def layernorm_bwd(dy, x, gamma, mean, rstd, res=None, bf=False):
+    """res: the gradient that bypasses the norm, added before dx is rounded."""
+    dy, x, gamma, res = _io(dy, bf), _io(x, bf), _io(gamma, bf), _io(res, bf)
+    mean, rstd = _c(mean, np.float32), _c(rstd, np.float32)
+    rows, D = x.shape
+    dx = np.empty_like(x)
+    dg, db = np.empty(D, np.float32), np.empty(D, np.float32)
+    lib().orc_layernorm_bwd(C.c_int(int(bf)), _p(dy), _p(x), _p(gamma), _p(mean), _p(rstd), C.c_int(rows), C.c_int(D), _p(res), _p(dx),
+                            _p(dg), _p(db))
+    return dx, dg, db
+
+
+# ---- 8-bit activation checkpoints -------------------------------------------
+def act8_pack(x, bf=True):
+    """Codes int8 [rows, D] and exponent fields uint8 [rows, ceil(D / 32)]."""
+    x = _io(x, bf)
+    rows, D = x.shape
+    q, e = np.empty((rows, D), np.int8), np.empty((rows, (D + 31) // 32), np.uint8)
+    lib().orc_act8_pack(C.c_int(int(bf)), _p(x), C.c_int(rows), C.c_int(D), _p(q), _p(e))
+    return q, e
+
+
+def act8_unpack(q, e, bf=True):
+    q, e = _c(q, np.int8), _c(e, np.uint8)
+    rows, D = q.shape
+    y = np.empty((rows, D), np.uint16 if bf else np.float32)
+    lib().orc_act8_unpack(C.c_int(int(bf)), _p(q), _p(e), C.c_int(rows), C.c_int(D), _p(y))
+    return y
+
+
+# ---- gated linear recurrence --------------------------------------------------
+LINREC_BLOCK = 64
+
+
+def linrec_fwd(gv, B, S, flags=None, h0=None):
+    """gv: uint16 [B*S, 2D] (gate | value).  Returns y [B*S, D], hT [B, D] and the states at the starts of the blocks."""
+    gv = _c(gv, np.uint16)
+    D = gv.shape[1] // 2
+    assert gv.shape[0] == B * S
+    flags = _c(flags, np.uint8) if flags is not None else None
+    h0 = _c(h0, np.float32) if h0 is not None else None
+    y, hT = np.empty((B * S, D), np.uint16), np.empty((B, D), np.float32)
+    states = np.empty((B, (S + LINREC_BLOCK - 1) // LINREC_BLOCK, D), np.float32)
+    base = gv.ctypes.data
+    lib().orc_linrec_fwd(C.c_void_p(base), C.c_void_p(base + 2 * D), C.c_int(2 * D), C.c_int(B), C.c_int(S), C.c_int(D), _p(flags), _p(h0),
+                         _p(y), C.c_int(D), _p(hT), _p(states))
+    return y, hT, states
+
+
+def linrec_bwd(dy, gv, states, B, S, flags=None, dhT=None):
+    """Returns dgv [B*S, 2D] and dh0 [B, D]."""
+    dy, gv, states = _c(dy, np.uint16), _c(gv, np.uint16), _c(states, np.float32)
+    D = gv.shape[1] // 2
+    flags = _c(flags, np.uint8) if flags is not None else None
+    dhT = _c(dhT, np.float32) if dhT is not None else None
+    dgv, dh0 = np.empty_like(gv), np.empty((B, D), np.float32)
+    base, dbase = gv.ctypes.data, dgv.ctypes.data
+    lib().orc_linrec_bwd(_p(dy), C.c_int(D), C.c_void_p(base), C.c_void_p(base + 2 * D), C.c_int(2 * D), C.c_int(B), C.c_int(S), C.c_int(D),
+                         _p(flags), _p(states), _p(dhT), C.c_void_p(dbase), C.c_void_p(dbase + 2 * D), C.c_int(2 * D), _p(dh0))
+    return dgv, dh0
+
+
 def rope(x, S, cos, sin, inverse=False):
     """x: bf16 bits [T, nh, 128]; cos, sin: f32 [S, 64]; position = t mod S."""
     x = _c(x, np.uint16)

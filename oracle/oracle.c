@@ -982,3 +982,210 @@ void orc_rope(const bf16_t *x, int T, int nh, int S, const float *cs, const floa
     }
   }
 }
+
+/* ------------------------------------------------------------------ */
+/* layer norm: mean and variance of a row by the fixed tree, the       */
+/* variance from the differences to the mean                           */
+/* ------------------------------------------------------------------ */
+void orc_layernorm_fwd(int bf, const void *x, const void *gamma, const void *beta, int rows, int D, float eps, void *y,
+                       float *mean, float *rstd) {
+  float invD = (float)(1.0 / (double)D);
+#pragma omp parallel for
+  for (int r = 0; r < rows; ++r) {
+    float *t = (float *)malloc((size_t)D * sizeof(float));
+    for (int j = 0; j < D; ++j) t[j] = ld(bf, x, (size_t)r * D + j);
+    float mu = fmul(det_sum(t, D), invD);
+    for (int j = 0; j < D; ++j) { float d = fsub(ld(bf, x, (size_t)r * D + j), mu); t[j] = fmul(d, d); }
+    float rs = fdiv(1.0f, fsqrt(fadd(fmul(det_sum(t, D), invD), eps)));
+    mean[r] = mu;
+    rstd[r] = rs;
+    for (int j = 0; j < D; ++j) {
+      float v = fmul(fsub(ld(bf, x, (size_t)r * D + j), mu), rs);
+      if (gamma) v = fmul(v, ld(bf, gamma, j));
+      if (beta) v = fadd(v, ld(bf, beta, j));
+      st(bf, y, (size_t)r * D + j, v);
+    }
+    free(t);
+  }
+}
+
+/* dx = rstd * ((w - c1) - xhat * c2), w = dy * gamma; with res the gradient that bypasses the norm is added before the one
+ * rounding; dgamma and dbeta are trees over the rows */
+void orc_layernorm_bwd(int bf, const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                       int rows, int D, const void *res, void *dx, float *dgamma, float *dbeta) {
+  float invD = (float)(1.0 / (double)D);
+#pragma omp parallel for
+  for (int r = 0; r < rows; ++r) {
+    float *w = (float *)malloc((size_t)D * sizeof(float)), *xh = (float *)malloc((size_t)D * sizeof(float));
+    float *t = (float *)malloc((size_t)D * sizeof(float));
+    for (int j = 0; j < D; ++j) {
+      w[j] = ld(bf, dy, (size_t)r * D + j);
+      if (gamma) w[j] = fmul(w[j], ld(bf, gamma, j));
+      xh[j] = fmul(fsub(ld(bf, x, (size_t)r * D + j), mean[r]), rstd[r]);
+      t[j] = fmul(w[j], xh[j]);
+    }
+    float c1 = fmul(det_sum(w, D), invD), c2 = fmul(det_sum(t, D), invD);
+    for (int j = 0; j < D; ++j) {
+      float v = fmul(rstd[r], fsub(fsub(w[j], c1), fmul(xh[j], c2)));
+      if (res) v = fadd(ld(bf, res, (size_t)r * D + j), v);
+      st(bf, dx, (size_t)r * D + j, v);
+    }
+    free(w); free(xh); free(t);
+  }
+#pragma omp parallel for
+  for (int j = 0; j < D; ++j) {
+    float *t = (float *)malloc((size_t)(rows ? rows : 1) * sizeof(float));
+    if (dgamma) {
+      for (int r = 0; r < rows; ++r)
+        t[r] = fmul(ld(bf, dy, (size_t)r * D + j), fmul(fsub(ld(bf, x, (size_t)r * D + j), mean[r]), rstd[r]));
+      dgamma[j] = det_sum(t, rows);
+    }
+    if (dbeta) {
+      for (int r = 0; r < rows; ++r) t[r] = ld(bf, dy, (size_t)r * D + j);
+      dbeta[j] = det_sum(t, rows);
+    }
+    free(t);
+  }
+}
+
+/* ------------------------------------------------------------------ */
+/* 8-bit activation checkpoints: 32 adjacent values of a row share a   */
+/* power-of-two step, kept as its binary32 exponent field              */
+/* ------------------------------------------------------------------ */
+void orc_act8_pack(int bf, const void *x, int rows, int D, int8_t *q, uint8_t *e) {
+  int ng = (D + 31) / 32;
+  for (int r = 0; r < rows; ++r)
+    for (int g = 0; g < ng; ++g) {
+      int lo = 32 * g, hi = lo + 32 < D ? lo + 32 : D;
+      float m = 0.0f;
+      int finite = 1;
+      for (int j = lo; j < hi; ++j) {
+        float v = ld(bf, x, (size_t)r * D + j);
+        if (isnan(v) || isinf(v)) finite = 0;
+        else if (fabsf(v) > m) m = fabsf(v);
+      }
+      int E = -126;                                     /* the smallest step 2^E >= 2^-126 with m <= 127 * 2^E */
+      while (ldexp(127.0, E) < (double)m) ++E;
+      e[(size_t)r * ng + g] = finite ? (uint8_t)(E + 127) : 255;
+      for (int j = lo; j < hi; ++j) {
+        float v = ld(bf, x, (size_t)r * D + j);
+        if (finite) q[(size_t)r * D + j] = (int8_t)rint(ldexp((double)v, -E));
+        else q[(size_t)r * D + j] = isinf(v) ? (v > 0 ? 127 : -127) : 0;
+      }
+    }
+}
+void orc_act8_unpack(int bf, const int8_t *q, const uint8_t *e, int rows, int D, void *y) {
+  int ng = (D + 31) / 32;
+  for (int r = 0; r < rows; ++r)
+    for (int j = 0; j < D; ++j)     /* field 255 is an infinite step: code 0 becomes a NaN, the others infinities */
+      st(bf, y, (size_t)r * D + j, fmul((float)q[(size_t)r * D + j], u2f((uint32_t)e[(size_t)r * ng + j / 32] << 23)));
+}
+
+/* ------------------------------------------------------------------ */
+/* gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) v_t           */
+/* ------------------------------------------------------------------ */
+#define LR_CHUNK 8   /* rows of a span that is walked row by row */
+#define LR_BLOCK 64  /* rows of a block of chunks */
+
+/* the smaller of f and 1 - f is e / (1 + e), e = exp(-|g|); the larger its difference to 1 */
+static void lr_gate(float g, float *f, float *z) {
+  float e = det_exp(fneg(fabs1(g)));
+  float m = fdiv(e, fadd(1.0f, e)), M = fsub(1.0f, m);
+  if (g != g) { *f = *z = NAN; return; }
+  *f = f2u(g) >> 31 ? m : M;
+  *z = f2u(g) >> 31 ? M : m;
+}
+/* the span (A, H) applied to what comes in; a span that forgets everything lets nothing in, not even a NaN */
+static float lr_apply(float A, float H, float s) { return A == 0.0f ? H : fadd(fmul(A, s), H); }
+
+/* One channel.  With chunk-wise composites (A, H) from zero, prefixes of them within a block and the states at the starts of
+ * the blocks: h[t] is walked from the state at the start of its chunk. */
+static void lr_forward(const float *f, const float *z, const float *v, const uint8_t *flags, int S, float h0, float *hprev,
+                       float *h, float *states, float *hT) {
+  float s = h0;
+  for (int b0 = 0, b = 0; b0 < S; b0 += LR_BLOCK, ++b) {
+    int b1 = b0 + LR_BLOCK < S ? b0 + LR_BLOCK : S;
+    if (states) states[b] = s;
+    float PA = 1.0f, PH = 0.0f;
+    for (int c0 = b0; c0 < b1; c0 += LR_CHUNK) {
+      int c1 = c0 + LR_CHUNK < b1 ? c0 + LR_CHUNK : b1;
+      float x = c0 == b0 ? s : lr_apply(PA, PH, s), A = 1.0f, H = 0.0f;
+      for (int t = c0; t < c1; ++t) {
+        float u = fmul(z[t], v[t]);
+        int cut = flags && flags[t];
+        hprev[t] = cut ? 0.0f : x;
+        x = cut ? u : fadd(fmul(f[t], x), u);
+        h[t] = x;
+        if (t == c0) { A = cut ? 0.0f : f[t]; H = u; }
+        else { A = cut ? 0.0f : fmul(A, f[t]); H = cut ? u : fadd(fmul(f[t], H), u); }
+      }
+      if (c0 == b0) { PA = A; PH = H; }
+      else { PH = lr_apply(A, H, PH); PA = A == 0.0f ? 0.0f : fmul(PA, A); }
+    }
+    s = lr_apply(PA, PH, s);
+  }
+  if (hT) *hT = s;
+}
+void orc_linrec_fwd(const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int D, const uint8_t *flags, const float *h0,
+                    bf16_t *y, int ldy, float *hT, float *states) {
+  int nb = (S + LR_BLOCK - 1) / LR_BLOCK;
+#pragma omp parallel for
+  for (int i = 0; i < B * D; ++i) {
+    int b = i / D, j = i % D;
+    float *w = (float *)malloc((size_t)(5 * (size_t)S + nb + 1) * sizeof(float));
+    float *f = w, *z = w + S, *vv = w + 2 * (size_t)S, *hp = w + 3 * (size_t)S, *h = w + 4 * (size_t)S, *stt = w + 5 * (size_t)S;
+    for (int t = 0; t < S; ++t) {
+      lr_gate(bf2f(g[((size_t)b * S + t) * ldi + j]), f + t, z + t);
+      vv[t] = bf2f(v[((size_t)b * S + t) * ldi + j]);
+    }
+    lr_forward(f, z, vv, flags ? flags + (size_t)b * S : NULL, S, h0 ? h0[i] : 0.0f, hp, h, stt, hT ? hT + i : NULL);
+    for (int t = 0; t < S; ++t) y[((size_t)b * S + t) * ldy + j] = f2bf(h[t]);
+    if (states) for (int k = 0; k < nb; ++k) states[((size_t)b * nb + k) * D + j] = stt[k];
+    free(w);
+  }
+}
+/* dh_t = dy_t + f_{t+1} dh_{t+1}: the same composition from the end; carry = f_t dh_t is what row t hands to row t - 1 */
+void orc_linrec_bwd(const bf16_t *dy, int ldy, const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int D,
+                    const uint8_t *flags, const float *states, const float *dhT, bf16_t *dg, bf16_t *dv, int ldd, float *dh0) {
+  int nb = (S + LR_BLOCK - 1) / LR_BLOCK;
+#pragma omp parallel for
+  for (int i = 0; i < B * D; ++i) {
+    int b = i / D, j = i % D;
+    const uint8_t *fl = flags ? flags + (size_t)b * S : NULL;
+    float *w = (float *)malloc((6 * (size_t)S + 1) * sizeof(float));
+    float *f = w, *z = w + S, *vv = w + 2 * (size_t)S, *hp = w + 3 * (size_t)S, *h = w + 4 * (size_t)S, *d = w + 5 * (size_t)S;
+    for (int t = 0; t < S; ++t) {
+      lr_gate(bf2f(g[((size_t)b * S + t) * ldi + j]), f + t, z + t);
+      vv[t] = bf2f(v[((size_t)b * S + t) * ldi + j]);
+    }
+    float carry = dhT ? dhT[i] : 0.0f;
+    for (int b0 = (nb - 1) * LR_BLOCK; b0 >= 0; b0 -= LR_BLOCK) {
+      int b1 = b0 + LR_BLOCK < S ? b0 + LR_BLOCK : S, nc = (b1 - b0 + LR_CHUNK - 1) / LR_CHUNK;
+      /* the block again from its state, as in the forward pass */
+      lr_forward(f + b0, z + b0, vv + b0, fl ? fl + b0 : NULL, b1 - b0, states[((size_t)b * nb + b0 / LR_BLOCK) * D + j], hp + b0, h + b0,
+                 NULL, NULL);
+      float SA = 1.0f, SK = 0.0f;
+      for (int c = nc - 1; c >= 0; --c) {
+        int c0 = b0 + c * LR_CHUNK, c1 = c0 + LR_CHUNK < b1 ? c0 + LR_CHUNK : b1;
+        float x = c == nc - 1 ? carry : lr_apply(SA, SK, carry), A = 1.0f, K = 0.0f;
+        for (int t = c1 - 1; t >= c0; --t) {
+          int cut = fl && fl[t];
+          float dyt = bf2f(dy[((size_t)b * S + t) * ldy + j]);
+          d[t] = fadd(dyt, x);
+          x = cut ? 0.0f : fmul(f[t], d[t]);
+          if (t == c1 - 1) { A = cut ? 0.0f : f[t]; K = cut ? 0.0f : fmul(f[t], dyt); }
+          else { A = cut ? 0.0f : fmul(f[t], A); K = cut ? 0.0f : fmul(f[t], fadd(dyt, K)); }
+        }
+        if (c == nc - 1) { SA = A; SK = K; }
+        else { SK = lr_apply(A, K, SK); SA = A == 0.0f ? 0.0f : fmul(SA, A); }
+      }
+      carry = lr_apply(SA, SK, carry);
+    }
+    for (int t = 0; t < S; ++t) {
+      dv[((size_t)b * S + t) * ldd + j] = f2bf(fmul(d[t], z[t]));
+      dg[((size_t)b * S + t) * ldd + j] = f2bf(fmul(fmul(d[t], fsub(hp[t], vv[t])), fmul(f[t], z[t])));
+    }
+    if (dh0) dh0[i] = carry;
+    free(w);
+  }
+}
