@@ -166,6 +166,70 @@ int det_residual_rmsnorm_fwd(const det_bf16* a, const det_bf16* b, const det_bf1
 int det_rmsnorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf16* gamma, const float* rstd, int rows, int D,
                              const det_bf16* res, det_bf16* dx, float* dgamma, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- layer norm -------------------------------------------------------------------------------------------
+ * The norm that subtracts the mean; not in the paper's block, for replays of models that use it.  Any rows and 1 <= D <= 8192;
+ * pointers 16-byte aligned where D % 8 == 0, aligned to their element otherwise; io: dtype of x, y, gamma, beta, dy, dx.
+ *   mean = det_sum(x) * (1/D), d = x - mean, rstd = 1 / sqrt(det_sum(d^2) * (1/D) + eps), y = (d * rstd) * gamma + beta;
+ * gamma or beta NULL: without that step.  mean, rstd f32 [rows]. */
+int det_layernorm_fwd(int io, const void* x, const void* gamma, const void* beta, int rows, int D, float eps, void* y, float* mean,
+                      float* rstd, void* stream);
+/* The same of the residual sum, bf16: sum = bf16(a + b) is stored and normalised (b NULL: of a, sum unused).  With qy the int8 codes of y for
+ * the next linear (see det_linear_fwd_q), with q8 and e8 the 8-bit checkpoint of what is normalised (det_act8_pack); both want
+ * D % 8 == 0 and 8-byte aligned codes.  sum and y overlap neither a nor b. */
+int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, const det_bf16* gamma, const det_bf16* beta, int rows, int D, float eps,
+                               det_bf16* sum, det_bf16* y, float* mean, float* rstd, const float* s_q, int8_t* qy, int8_t* q8,
+                               uint8_t* e8, void* stream);
+/* xhat = (x - mean) * rstd, w = dy * gamma, c1 = det_sum(w) * (1/D), c2 = det_sum(w * xhat) * (1/D): dx = rstd * ((w - c1) - xhat * c2);
+ * dgamma[j] = det_sum over rows of dy * xhat, dbeta[j] = det_sum over rows of dy (f32 [D], each may be NULL; ws is needed for either). */
+size_t det_layernorm_bwd_ws_bytes(int rows, int D);
+int det_layernorm_bwd(int io, const void* dy, const void* x, const void* gamma, const float* mean, const float* rstd, int rows, int D,
+                      void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream);
+/* bf16, and the gradient res that bypasses the norm is added before dx is rounded (once).  dx may be res. */
+int det_layernorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf16* gamma, const float* mean, const float* rstd, int rows,
+                               int D, const det_bf16* res, det_bf16* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                               void* stream);
+/* The same from the 8-bit checkpoint of x: bit for bit det_layernorm_bwd_residual of det_act8_unpack's values (res may be NULL). */
+int det_layernorm_bwd_act8(const det_bf16* dy, const int8_t* q8, const uint8_t* e8, const det_bf16* gamma, const float* mean,
+                           const float* rstd, int rows, int D, const det_bf16* res, det_bf16* dx, float* dgamma, float* dbeta, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* ---- activations in 8 bits between the forward and the backward pass ------------------------------------------
+ * The replay runs every virtual rank on one GPU, so what a micro-batch keeps for its backward pass bounds its size.  32 adjacent values of
+ * a row (the last group of a row may be shorter) share a step 2^E, the smallest power of two with max|v| <= 127 * 2^E, at least
+ * 2^-126: code = rne(v * 2^-E) in [-127, 127], value = code * 2^E.  Every product is exact, so a value is off by at most half a step and comes
+ * back exactly in bf16 as in f32.  q8 int8 [rows, D], e8 uint8 [rows, ceil(D/32)] = E + 127; a group with an infinity or a NaN has
+ * e8 = 255 and comes back as infinities (code +-127) and NaNs (code 0).
+ * io: dtype of x and y; their rows are ld elements apart (ld >= D); any D, any alignment to the element. */
+size_t det_act8_exp_bytes(int rows, int D); /* bytes of e8 */
+int det_act8_pack(int io, const void* x, int ld, int rows, int D, int8_t* q8, uint8_t* e8, void* stream);
+int det_act8_unpack(int io, const int8_t* q8, const uint8_t* e8, int rows, int D, void* y, int ld, void* stream);
+/* SwiGLU (see det_swiglu_fwd) with gu kept in 8 bits: det_swiglu_fwd_act8 is the forward pass that also packs gu; det_swiglu_act8 and
+ * det_swiglu_bwd_act8 are det_swiglu_fwd and det_swiglu_bwd of the unpacked gu, bit for bit.  With qh also det_swiglu_fwd_q's codes of the h
+ * they write (qh, s_q may be NULL).  q8 int8 [rows, 2F], e8 [rows, 2F/32]; F % 32 == 0; q8, qh 8-byte aligned. */
+int det_swiglu_fwd_act8(const det_bf16* gu, int rows, int F, det_bf16* h, int8_t* q8, uint8_t* e8, const float* s_q, int8_t* qh, void* stream);
+int det_swiglu_act8(const int8_t* q8, const uint8_t* e8, int rows, int F, det_bf16* h, const float* s_q, int8_t* qh, void* stream);
+int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8, int rows, int F, det_bf16* dgu, void* stream);
+
+/* ---- gated linear recurrence -----------------------------------------------------------------------------------
+ * A mixer of the tokens of a sequence beside attention, linear in its length.  Per channel, over the S rows of each of B sequences:
+ *   e = det_exp(-|g|), m = e / (1 + e): f = (g >= 0 ? 1 - m : m) is the forget gate, z = (g >= 0 ? m : 1 - m) its complement;
+ *   h_t = f_t h_{t-1} + z_t v_t, y = bf16(h).
+ * h_{-1} = h0 f32 [B, D] (NULL: zero), hT = the state behind the last row (may be NULL, may be h0: the next call's h0, one row at
+ * a time included).  flags uint8 [B, S] (may be NULL): a row whose flag is set starts from zero instead of h_{t-1}; nothing before it, a NaN
+ * included, reaches it, and no gradient goes back across it.  g, v bf16 (row b*S + t at ld*(b*S + t); gate and value may be the two halves of one
+ * projection), y with ld_y.  Rows are composed in chunks of 8 and blocks of 64: s -> A s + H row by row within a chunk, chunk by chunk
+ * within a block, block by block along the sequence; h is walked from the state at the start of its chunk; A = 0 lets nothing in.
+ * states f32 [B, ceil(S/64), D] (det_linrec_state_floats; NULL: not kept) are the states in front of the blocks, for the backward pass.
+ * D, ld, ld_y, ld_d even, S <= 2^30; bf16 pointers 4-byte, f32 pointers 8-byte aligned.  S = 0: hT = h0, dh0 = dhT.  Outputs overlap no
+ * input but as said. */
+size_t det_linrec_state_floats(int B, int S, int D);
+int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, det_bf16* y, int ld_y, const uint8_t* flags,
+                   const float* h0, float* hT, float* states, void* stream);
+/* dh_t = dy_t + f_{t+1} dh_{t+1}, behind the last row dhT f32 [B, D] (NULL: zero): dv = dh z, dg = dh (h_{t-1} - v) (f z) (bf16, row stride ld_d),
+ * dh0 f32 [B, D] (may be NULL, may be dhT); composed as in the forward pass, from the last row to the first. */
+int det_linrec_bwd(const det_bf16* dy, int ld_y, const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, const float* states,
+                   det_bf16* dg, det_bf16* dv, int ld_d, const uint8_t* flags, const float* dhT, float* dh0, void* stream);
+
 /* ---- per-head operations of the attention block (Sec. 3.1 "QK-norm", "RoPE") --------------------------
  * Rows of 128 values (one head of one token) inside wider token rows: element (t, h, i) of x sits at
  * x[t*ld + h*128 + i]; ld, ld_y, ... are row strides in elements (multiples of 4, >= nh*128); pointers 8-byte

@@ -69,6 +69,11 @@ _SIGNATURES = {
     "det_residual_rmsnorm_fwd": "ipppiifpppppp", "det_rmsnorm_bwd_residual": "ippppiippppzp", "det_test_igemm_tn": "ippiiipipp", "det_test_lmhead_tile": "iiippiiipip",
     "det_test_wait_timeout": "iplp", "det_test_wait_warp": "iplp", "det_test_attn_fwd": "iipppiiiiiipipppp",
     "det_test_attn_rows": "iiii", "det_test_lmhead_pick": "iiii",
+    "det_layernorm_fwd": "iipppiifpppp", "det_residual_layernorm_fwd": "ippppiifppppppppp", "det_layernorm_bwd_ws_bytes": "zii",
+    "det_layernorm_bwd": "iipppppiippppzp", "det_layernorm_bwd_residual": "ipppppiipppppzp", "det_layernorm_bwd_act8": "ippppppiipppppzp",
+    "det_act8_exp_bytes": "zii", "det_act8_pack": "iipiiippp", "det_act8_unpack": "iippiipip",
+    "det_swiglu_fwd_act8": "ipiipppppp", "det_swiglu_act8": "ippiipppp", "det_swiglu_bwd_act8": "ipppiipp",
+    "det_linrec_state_floats": "ziii", "det_linrec_fwd": "ippiiiipippppp", "det_linrec_bwd": "ipippiiiipppipppp",
 }
 
 # The entry points that csrc/binding.cpp calls directly: what it makes of each Python argument (letters as above; w: a workspace tensor or None,
@@ -85,6 +90,10 @@ _PATTERNS = {
     "det_residual_add": "ppzps", "det_embed_fwd": "pipiips", "det_embed_bwd": "pipiips", "det_lmhead_fwd": "ppiiips",
     "det_lmhead_fwd_v2": "ppiiipwsp", "det_lmhead_bwd": "pppiiippis", "det_lmhead_bwd_v2": "pppiiippwsp",
     "det_attn_fwd_v2": "pppiiiipipwsp", "det_tensor_hash_async": "pzpws",
+    "det_layernorm_fwd": "ipppiifppps", "det_residual_layernorm_fwd": "ppppiifpppppppps", "det_layernorm_bwd": "ipppppiipppws",
+    "det_layernorm_bwd_residual": "pppppiippppws", "det_layernorm_bwd_act8": "ppppppiippppws", "det_act8_pack": "ipiiipps",
+    "det_act8_unpack": "ippiipis", "det_swiglu_fwd_act8": "piippppps", "det_swiglu_act8": "ppiippps",
+    "det_swiglu_bwd_act8": "pppiips", "det_linrec_fwd": "ppiiiipipppps", "det_linrec_bwd": "pippiiiipppippps",
 }
 
 
@@ -294,6 +303,67 @@ def det_xent_fwd(logits, target, rows, V, z_weight, loss_row, lse, loss_mean, z_
 
 def det_xent_bwd(logits_inout, target, lse, rows, V, z_weight, scale):
     _c.det_xent_bwd(logits_inout, target, lse, rows, V, z_weight, scale)
+
+
+# ---- layer norm, 8-bit checkpoints, gated linear recurrence ---------------------------------------------------
+def det_layernorm_fwd(io, x, gamma, beta, rows, D, eps, y, mean, rstd):
+    _c.det_layernorm_fwd(io, x, gamma, beta, rows, D, eps, y, mean, rstd)
+
+
+def det_residual_layernorm_fwd(a, b, gamma, beta, rows, D, eps, sum_out, y, mean, rstd, s_q=None, qy=None, q8=None, e8=None):
+    _c.det_residual_layernorm_fwd(a, b, gamma, beta, rows, D, eps, sum_out, y, mean, rstd, s_q, qy, q8, e8)
+
+
+def det_layernorm_bwd_ws_bytes(rows, D):
+    return load().det_layernorm_bwd_ws_bytes(rows, D)
+
+
+def det_layernorm_bwd(io, dy, x, gamma, mean, rstd, rows, D, dx, dgamma, dbeta, ws):
+    _c.det_layernorm_bwd(io, dy, x, gamma, mean, rstd, rows, D, dx, dgamma, dbeta, ws)
+
+
+def det_layernorm_bwd_residual(dy, x, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws):
+    _c.det_layernorm_bwd_residual(dy, x, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws)
+
+
+def det_layernorm_bwd_act8(dy, q8, e8, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws):
+    _c.det_layernorm_bwd_act8(dy, q8, e8, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws)
+
+
+def det_act8_exp_bytes(rows, D):
+    return load().det_act8_exp_bytes(rows, D)
+
+
+def det_act8_pack(io, x, ld, rows, D, q8, e8):
+    _c.det_act8_pack(io, x, ld, rows, D, q8, e8)
+
+
+def det_act8_unpack(io, q8, e8, rows, D, y, ld):
+    _c.det_act8_unpack(io, q8, e8, rows, D, y, ld)
+
+
+def det_swiglu_fwd_act8(gu, rows, F, h, q8, e8, s_q=None, qh=None):
+    _c.det_swiglu_fwd_act8(gu, rows, F, h, q8, e8, s_q, qh)
+
+
+def det_swiglu_act8(q8, e8, rows, F, h, s_q=None, qh=None):
+    _c.det_swiglu_act8(q8, e8, rows, F, h, s_q, qh)
+
+
+def det_swiglu_bwd_act8(dh, q8, e8, rows, F, dgu):
+    _c.det_swiglu_bwd_act8(dh, q8, e8, rows, F, dgu)
+
+
+def det_linrec_state_floats(B, S, D):
+    return load().det_linrec_state_floats(B, S, D)
+
+
+def det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags=None, h0=None, hT=None, states=None):
+    _c.det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags, h0, hT, states)
+
+
+def det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags=None, dhT=None, dh0=None):
+    _c.det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags, dhT, dh0)
 
 
 # ---- attention ------------------------------------------------------------------------------------------------

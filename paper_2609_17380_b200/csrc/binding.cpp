@@ -111,7 +111,9 @@ static Entry entries[] = {
     DET_ENTRY(det_attn_fwd_q), DET_ENTRY(det_attn_fwd_int8pv), DET_ENTRY(det_attn_bwd), DET_ENTRY(det_attn_bwd_fixq), DET_ENTRY(det_swiglu_fwd),
     DET_ENTRY(det_swiglu_fwd_q), DET_ENTRY(det_swiglu_bwd), DET_ENTRY(det_residual_add), DET_ENTRY(det_embed_fwd), DET_ENTRY(det_embed_bwd),
     DET_ENTRY(det_lmhead_fwd), DET_ENTRY(det_lmhead_fwd_v2), DET_ENTRY(det_lmhead_bwd), DET_ENTRY(det_lmhead_bwd_v2), DET_ENTRY(det_attn_fwd_v2),
-    DET_ENTRY(det_tensor_hash_async)};
+    DET_ENTRY(det_tensor_hash_async), DET_ENTRY(det_layernorm_fwd), DET_ENTRY(det_residual_layernorm_fwd), DET_ENTRY(det_layernorm_bwd),
+    DET_ENTRY(det_layernorm_bwd_residual), DET_ENTRY(det_layernorm_bwd_act8), DET_ENTRY(det_act8_pack), DET_ENTRY(det_act8_unpack),
+    DET_ENTRY(det_swiglu_fwd_act8), DET_ENTRY(det_swiglu_act8), DET_ENTRY(det_swiglu_bwd_act8), DET_ENTRY(det_linrec_fwd), DET_ENTRY(det_linrec_bwd)};
 
 // One callable that bind returns, owned by the capsule that is its self: nothing is shared between two results of bind.
 struct Callable {

@@ -1,0 +1,468 @@
+// Layer norm, forward and backward: the norm that subtracts the mean, with gain and shift.
+//   forward   mean = sum(x) / D, d = x - mean, rstd = 1 / sqrt(sum(d^2) / D + eps), y = (d * rstd) * gamma + beta
+//   backward  xhat = (x - mean) * rstd, w = dy * gamma, c1 = sum(w) / D, c2 = sum(w * xhat) / D,
+//             dx = rstd * ((w - c1) - xhat * c2), dgamma = sum over rows of dy * xhat, dbeta = sum over rows of dy
+// Every sum is the fixed tree; the variance comes from the differences to the mean, so a mean far from zero costs no digits.  What bounds
+// them is memory: a row is read once and stays in registers between the two sums of the forward pass and between sums and output
+// of the backward one.
+#include <type_traits>
+
+#include "common.cuh"
+#include "internal.h"
+#include "rows.cuh"
+
+namespace det {
+
+// A row is held by WPR warps, a leaf of 256 columns each, eight adjacent columns a lane.  WPR < 8: a CTA of eight warps has 8 / WPR such groups,
+// with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are in flight at a time.
+template <int WPR, bool BF>
+struct LnShape {
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS;
+  static constexpr int ROWS = WPR == 32 ? 1 : (WPR == 16 || !BF ? 2 : 4);
+  static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : 4);
+};
+template <int WPR>
+using LnBwd = LnShape<WPR, false>;   // backward: two rows in flight (one where 32 warps hold a row): two tensors, and dx beside them
+
+// The row's tree over its WPR leaf sums (in shared memory, one barrier back); a leaf beyond D does not exist.
+template <int WPR>
+__device__ __forceinline__ float row_tree(const float* leaf, int D) {
+  if (WPR <= 8) {
+    float L[WPR];
+#pragma unroll
+    for (int j = 0; j < WPR; ++j) L[j] = leaf[j];
+    return reg_tree<WPR>(L, 0, 256, D);
+  }
+  const int lane = threadIdx.x & 31;
+  float v = leaf[lane % WPR];
+#pragma unroll
+  for (int w = 1; w < WPR; w <<= 1) {
+    const float o = __shfl_xor_sync(0xffffffffu, v, w);
+    const int right = ((lane % WPR) | w) & ~(w - 1);
+    v = right * 256 < D ? fadd(v, o) : ((lane & w) ? o : v);
+  }
+  return v;
+}
+template <bool VEC>
+__device__ __forceinline__ float leaf_tree(const float v[8], int warp, int e0, int D, bool full) {
+  if (full) return warp_tree_full(tree8_full(v));
+  return warp_tree(VEC ? tree8_full(v) : tree8(v, e0, D), (long long)warp * 256, 8, D);
+}
+
+template <bool BF, int WPR, bool VEC>
+__global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::CTAS)
+    k_ln_fwd(const void* __restrict__ x, const void* __restrict__ res, const void* __restrict__ gamma, const void* __restrict__ beta,
+             int rows, int D, float eps, float invD, void* __restrict__ sum, void* __restrict__ y, float* __restrict__ mean,
+             float* __restrict__ rstd, const float* __restrict__ s_q, int8_t* __restrict__ qy, int8_t* __restrict__ q8,
+             uint8_t* __restrict__ e8) {
+  grid_dep();
+  using S = LnShape<WPR, BF>;
+  constexpr int R = S::ROWS;
+  __shared__ float leaf_s[S::GROUPS][2][R][WPR];
+  const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
+  const int e0 = warp * 256 + lane * 8, n = D - e0;
+  const bool full = (D & 255) == 0;
+  const long long first = ((long long)blockIdx.x * S::GROUPS + grp) * R;
+  float v[R][8];
+#pragma unroll
+  for (int a = 0; a < R; ++a) load8n<BF, VEC>(x, (size_t)(first + a) * D + e0, first + a < rows ? n : 0, v[a]);
+  if (res) {   // the residual sum in front of the norm: rounded and stored, and the rounded one is what is normalised
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      const int m = first + a < rows ? n : 0;
+      float b[8];
+      load8n<BF, VEC>(res, (size_t)(first + a) * D + e0, m, b);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], b[t]);
+      store8n<BF, VEC>(sum, (size_t)(first + a) * D + e0, m, v[a]);
+      if (BF) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[a][t] = bf2f(f2bf(v[a][t]));
+      }
+    }
+  }
+  if (BF && VEC && q8) {   // the checkpoint of what is normalised
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      const uint32_t field = a8_field(a8_quad_max(a8_amax8(v[a])));
+      if (first + a < rows && n > 0) {
+        *reinterpret_cast<uint2*>(q8 + (size_t)(first + a) * D + e0) = a8_codes8(v[a], field);
+        if ((lane & 3) == 0) e8[(size_t)(first + a) * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP] = (uint8_t)field;
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < R; ++a) {
+    const float s = leaf_tree<VEC>(v[a], warp, e0, D, full);
+    if (lane == 0) leaf_s[grp][0][a][warp] = s;
+  }
+  __syncthreads();
+  float mu[R];
+#pragma unroll
+  for (int a = 0; a < R; ++a) {
+    mu[a] = fmul(row_tree<WPR>(leaf_s[grp][0][a], D), invD);
+    float sq[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      v[a][t] = fsub(v[a][t], mu[a]);
+      sq[t] = fmul(v[a][t], v[a][t]);
+    }
+    const float s = leaf_tree<VEC>(sq, warp, e0, D, full);
+    if (lane == 0) leaf_s[grp][1][a][warp] = s;
+  }
+  float g[8], b[8];
+  if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
+  if (beta) load8n<BF, VEC>(beta, e0, n, b);
+  const float inv_q = (BF && VEC && qy) ? fdiv(1.0f, s_q[0]) : 0.0f;
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < R; ++a) {
+    const float rs = fdiv(1.0f, fsqrt(fadd(fmul(row_tree<WPR>(leaf_s[grp][1][a], D), invD), eps)));
+    if (first + a >= rows) continue;
+    if (warp == 0 && lane == 0) {
+      mean[first + a] = mu[a];
+      rstd[first + a] = rs;
+    }
+    float o[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[t] = fmul(v[a][t], rs);
+    if (gamma) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = fmul(o[t], g[t]);
+    }
+    if (beta) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
+    }
+    const size_t at = (size_t)(first + a) * D + e0;
+    store8n<BF, VEC>(y, at, n, o);
+    if (BF && VEC && qy && n > 0) {   // the next linear's quantiser, applied to the bf16 values just stored
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = bf2f(f2bf(o[t]));
+      *reinterpret_cast<uint2*>(qy + at) = quant8(o, inv_q);
+    }
+  }
+}
+
+// Backward.  Each group of warps takes `passes` x ROWS adjacent rows (passes a power of two), ROWS at a time; a lane sees the same eight columns of
+// all of them, so the trees of dgamma and dbeta over the group's rows run in its own registers, the nodes of finished passes waiting
+// in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
+enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is: as dy, or the 8-bit checkpoint (dy bf16)
+template <int KIND, int WPR, bool VEC>
+__global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16 ? 2 : 1))
+    k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
+             const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int passes, const void* res,
+             void* dx, float* __restrict__ partial, int* __restrict__ tickets) {
+  grid_dep();
+  constexpr bool BF = KIND != LN_F32;
+  using S = LnBwd<WPR>;
+  constexpr int R = S::ROWS, T = S::THREADS;
+  extern __shared__ float waiting[];                      // [levels][16][T]
+  __shared__ float leaf_s[2][S::GROUPS][R][2][WPR];
+  const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
+  const int e0 = warp * 256 + lane * 8, n = D - e0;
+  const bool full = (D & 255) == 0;
+  const long long r0 = ((long long)blockIdx.x * S::GROUPS + grp) * R * passes;
+  if (partial && blockIdx.x == 0 && (int)threadIdx.x < 2 * ((D + 255) / 256)) tickets[threadIdx.x] = 0;   // for the kernel that follows
+  float g[8];
+  if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
+  float node[16];                                         // of this group's rows so far: 8 columns of dgamma, 8 of dbeta
+#pragma unroll 1
+  for (int p = 0; p < passes; ++p) {
+    const long long first = r0 + (long long)p * R;
+    float w[R][8], xh[R][8], rs[R];
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      const long long row = first + a;
+      const int m = row < rows ? n : 0;
+      load8n<BF, VEC>(dy, (size_t)row * D + e0, m, w[a]);
+      if (KIND == LN_ACT8) {
+        const int8_t* q = reinterpret_cast<const int8_t*>(x) + (size_t)row * D + e0;
+        const float step = m > 0 ? a8_step(e8[(size_t)row * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP]) : 0.0f;
+        uint2 c = make_uint2(0, 0);
+        if (VEC) {
+          if (m > 0) c = *reinterpret_cast<const uint2*>(q);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            if (t < m) (t < 4 ? c.x : c.y) |= (uint32_t)(uint8_t)q[t] << (8 * (t & 3));
+        }
+        a8_values8(c, step, xh[a]);
+      } else {
+        load8n<BF, VEC>(x, (size_t)row * D + e0, m, xh[a]);
+      }
+      rs[a] = row < rows ? rstd[row] : 0.0f;
+      const float mu = row < rows ? mean[row] : 0.0f;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu), rs[a]);
+    }
+    if (partial) {   // rows in pairs, pairs in pairs; a right node exists iff its first row does, else the left one is carried up unchanged
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        float c[R], d[R];
+#pragma unroll
+        for (int a = 0; a < R; ++a) { c[a] = fmul(w[a][t], xh[a][t]); d[a] = w[a][t]; }
+        node[t] = reg_tree<R>(c, first, 1, rows);
+        node[8 + t] = reg_tree<R>(d, first, 1, rows);
+      }
+      int level = 0;
+      for (; (p >> level) & 1; ++level) {
+        const bool have = r0 + (long long)((p >> level) << level) * R < rows;
+        float* l = waiting + (size_t)level * 16 * T + threadIdx.x;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) node[t] = have ? fadd(l[t * T], node[t]) : l[t * T];
+      }
+      if (p + 1 < passes) {
+        float* l = waiting + (size_t)level * 16 * T + threadIdx.x;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) l[t * T] = node[t];
+      }
+    }
+    if (gamma) {
+#pragma unroll
+      for (int a = 0; a < R; ++a)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) w[a][t] = fmul(w[a][t], g[t]);
+    }
+    float (*leaf)[2][WPR] = leaf_s[p & 1][grp];
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      float pr[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) pr[t] = fmul(w[a][t], xh[a][t]);
+      const float s1 = leaf_tree<VEC>(w[a], warp, e0, D, full), s2 = leaf_tree<VEC>(pr, warp, e0, D, full);
+      if (lane == 0) { leaf[a][0][warp] = s1; leaf[a][1][warp] = s2; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      const float c1 = fmul(row_tree<WPR>(leaf[a][0], D), invD), c2 = fmul(row_tree<WPR>(leaf[a][1], D), invD);
+      const int m = first + a < rows ? n : 0;
+      const size_t at = (size_t)(first + a) * D + e0;
+      float o[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
+      if (res) {   // the gradient that bypasses the norm (res may be dx)
+        float b[8];
+        load8n<BF, VEC>(res, at, m, b);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[t] = fadd(b[t], o[t]);
+      }
+      store8n<BF, VEC>(dx, at, m, o);
+    }
+  }
+  if (!partial) return;
+  if (S::GROUPS > 1) {   // the tree over the groups' nodes
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 16; ++t) waiting[t * T + threadIdx.x] = node[t];
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      float c[S::GROUPS];
+#pragma unroll
+      for (int k = 0; k < S::GROUPS; ++k) c[k] = waiting[t * T + k * WPR * 32 + threadIdx.x];
+      node[t] = reg_tree<S::GROUPS>(c, r0, (long long)R * passes, rows);
+    }
+  }
+  float* dst = partial + (size_t)blockIdx.x * D + e0;
+  store8n<false, VEC>(dst, 0, n, node);
+  store8n<false, VEC>(dst + (size_t)gridDim.x * D, 0, n, node + 8);
+}
+
+// The trees over the row blocks (`stride` rows each) of every column of dgamma (z = 0) and dbeta (z = 1), 32 nodes a thread; the CTA
+// that completes a block of 256 columns goes on to the levels above for those columns, as in the RMSNorm's gain gradient.
+__global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ partial, int nb, int stride, int rows, int D, float* __restrict__ upper,
+                                                 int nu, int* __restrict__ tickets, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ int last_s;
+  const int col = blockIdx.x * 256 + threadIdx.x, z = blockIdx.z;
+  float* out = z ? dbeta : dgamma;
+  grid_dep();
+  if (!out) return;
+  partial += (size_t)z * nb * D;
+  upper += (size_t)z * nu * D;
+  if (col < D) {
+    float s[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int b = blockIdx.y * 32 + i;
+      s[i] = b < nb ? partial[(size_t)b * D + col] : 0.0f;
+    }
+    upper[(size_t)blockIdx.y * D + col] = reg_tree<32>(s, (long long)blockIdx.y * 32 * stride, stride, rows);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last_s = atomicAdd(&tickets[2 * blockIdx.x + z], 1) == nu - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!last_s || col >= D) return;
+  int n = nu;
+  long long st = 32ll * stride;
+  while (n > 1) {
+    const int groups = (n + 31) / 32;
+    for (int gg = 0; gg < groups; ++gg) {
+      float s[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i] = gg * 32 + i < n ? __ldcg(&upper[(size_t)(gg * 32 + i) * D + col]) : 0.0f;
+      upper[(size_t)gg * D + col] = reg_tree<32>(s, (long long)gg * 32 * st, st, rows);
+    }
+    n = groups;
+    st *= 32;
+  }
+  // the sum of one row is that row, carried up without an addition: flushed like every value that enters or leaves an operation
+  const float r = __ldcg(&upper[col]);
+  out[col] = (__float_as_uint(r) & 0x7f800000u) ? r : __uint_as_float(__float_as_uint(r) & 0x80000000u);
+}
+
+// ---- host side -------------------------------------------------------------------------------------------
+template <class F>
+static void with_wpr(int D, F f) {
+  if (D <= 256) f(std::integral_constant<int, 1>());
+  else if (D <= 512) f(std::integral_constant<int, 2>());
+  else if (D <= 1024) f(std::integral_constant<int, 4>());
+  else if (D <= 2048) f(std::integral_constant<int, 8>());
+  else if (D <= 4096) f(std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 32>());
+}
+template <class F>
+static void with_bool(bool b, F f) { if (b) f(std::true_type()); else f(std::false_type()); }
+
+static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, const void* beta, int rows, int D, float eps, void* sum,
+                  void* y, float* mean, float* rstd, const float* s_q, int8_t* qy, int8_t* q8, uint8_t* e8, cudaStream_t st) {
+  with_wpr(D, [&](auto wpr) {
+    with_bool(bf, [&](auto is_bf) {
+      with_bool(D % 8 == 0, [&](auto is_vec) {
+        constexpr int W = decltype(wpr)::value;
+        using S = LnShape<W, decltype(is_bf)::value>;
+        const int per = S::GROUPS * S::ROWS;
+        launch_after(k_ln_fwd<decltype(is_bf)::value, W, decltype(is_vec)::value>, dim3((unsigned)(((long long)rows + per - 1) / per)), S::THREADS, 0, st, x,
+                     res, gamma, beta, rows, D, eps, (float)(1.0 / (double)D), sum, y, mean, rstd, s_q, qy, q8, e8);
+      });
+    });
+  });
+  DET_CHECK_LAUNCH();
+  return DET_OK;
+}
+
+// Rows a CTA of the backward pass takes: a multiple of what it has in flight, more of it while the grid still covers the GPU (each halving of
+// the nodes saves the second kernel half its reading), at most 8 passes (three levels of waiting nodes, 48 KiB).
+static int ln_passes(int rows, int per) {
+  int passes = 1;
+  while (passes < 8 && (long long)rows > (long long)passes * 2 * per * 444) passes *= 2;
+  return passes;
+}
+static int ln_rows_in_flight(int D) {
+  int per = 0;
+  with_wpr(D, [&](auto wpr) { using S = LnBwd<decltype(wpr)::value>; per = S::GROUPS * S::ROWS; });
+  return per;
+}
+template <int KIND>
+static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
+                  const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
+  const bool cols = dgamma || dbeta;
+  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, per), stride = per * passes;
+  const int nb = (int)(((long long)rows + stride - 1) / stride), nu = (nb + 31) / 32;
+  float* partial = cols ? (float*)ws : nullptr;
+  float* upper = cols ? partial + 2 * (size_t)nb * D : nullptr;
+  int* tickets = cols ? reinterpret_cast<int*>(upper + 2 * (size_t)nu * D) : nullptr;
+  int rc = DET_OK;
+  with_wpr(D, [&](auto wpr) {
+    with_bool(D % 8 == 0, [&](auto is_vec) {
+      constexpr int W = decltype(wpr)::value;
+      using S = LnBwd<W>;
+      int levels = 0;
+      while ((1 << levels) < passes) ++levels;
+      if (S::GROUPS > 1 && levels == 0) levels = 1;
+      const size_t smem = cols ? (size_t)levels * 16 * S::THREADS * sizeof(float) : 0;
+      auto kern = k_ln_bwd<KIND, W, decltype(is_vec)::value>;
+      if (smem > 40 * 1024) {
+        static DevOnce once;
+        rc = dev_ensure_smem(once, (const void*)kern, (size_t)3 * 16 * S::THREADS * sizeof(float));
+        if (rc != DET_OK) return;
+      }
+      launch_after(kern, dim3(nb), S::THREADS, smem, st, dy, x, e8, gamma, mean, rstd, rows, D, (float)(1.0 / (double)D), passes, res, dx, partial, tickets);
+    });
+  });
+  if (rc != DET_OK) return rc;
+  if (cols)
+    launch_after(k_ln_cols, dim3((D + 255) / 256, nu, 2), 256, 0, st, (const float*)partial, nb, stride, rows, D, upper, nu, tickets, dgamma, dbeta);
+  DET_CHECK_LAUNCH();
+  return DET_OK;
+}
+static bool elem_aligned(const void* p, int D, size_t elem) { return (uintptr_t)p % (D % 8 == 0 ? 16 : elem) == 0; }
+
+}  // namespace det
+
+using namespace det;
+
+extern "C" int det_layernorm_fwd(int io, const void* x, const void* gamma, const void* beta, int rows, int D, float eps, void* y, float* mean,
+                                 float* rstd, void* stream) {
+  if (!x || !y || !mean || !rstd || rows < 0 || D <= 0 || (io != DET_F32 && io != DET_BF16)) return DET_ERR_ARG;
+  if (D > 8192) return DET_ERR_SHAPE;
+  const size_t el = io == DET_BF16 ? 2 : 4;
+  if (!elem_aligned(x, D, el) || !elem_aligned(y, D, el) || !elem_aligned(gamma, D, el) || !elem_aligned(beta, D, el)) return DET_ERR_ALIGN;
+  if (rows == 0) return DET_OK;
+  return ln_fwd(io == DET_BF16, x, nullptr, gamma, beta, rows, D, eps, nullptr, y, mean, rstd, nullptr, nullptr, nullptr, nullptr, (cudaStream_t)stream);
+}
+
+extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, const det_bf16* gamma, const det_bf16* beta, int rows, int D,
+                                          float eps, det_bf16* sum, det_bf16* y, float* mean, float* rstd, const float* s_q, int8_t* qy,
+                                          int8_t* q8, uint8_t* e8, void* stream) {
+  if (!a || (b && !sum) || !y || !mean || !rstd || (qy && !s_q) || (!q8 != !e8) || rows < 0 || D <= 0) return DET_ERR_ARG;
+  if (D > 8192 || (D % 8 && (qy || q8))) return DET_ERR_SHAPE;
+  if (!elem_aligned(a, D, 2) || !elem_aligned(b, D, 2) || !elem_aligned(gamma, D, 2) || !elem_aligned(beta, D, 2) ||
+      (b && !elem_aligned(sum, D, 2)) || !elem_aligned(y, D, 2) || (((uintptr_t)qy | (uintptr_t)q8) & 7u))
+    return DET_ERR_ALIGN;
+  if (rows == 0) return DET_OK;
+  return ln_fwd(true, a, b, gamma, beta, rows, D, eps, sum, y, mean, rstd, s_q, qy, q8, e8, (cudaStream_t)stream);
+}
+
+extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
+  if (rows <= 0 || D <= 0 || D > 8192) return 256;
+  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, per);
+  const size_t nb = ((size_t)rows + stride - 1) / stride, nu = (nb + 31) / 32;
+  return align_up(2 * (nb + nu) * (size_t)D * sizeof(float), 256) + 256;
+}
+
+// what the three backward calls have in common: checks, nothing to do, launch
+template <int KIND>
+static int ln_bwd_entry(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
+                        const void* res, void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, cudaStream_t st) {
+  if (!dy || !x || !mean || !rstd || !dx || rows < 0 || D <= 0) return DET_ERR_ARG;
+  if (D > 8192) return DET_ERR_SHAPE;
+  const size_t el = KIND == LN_F32 ? 4 : 2;
+  if (!elem_aligned(dy, D, el) || !elem_aligned(dx, D, el) || !elem_aligned(gamma, D, el) || !elem_aligned(res, D, el)) return DET_ERR_ALIGN;
+  if (KIND == LN_ACT8 ? (D % 8 == 0 && ((uintptr_t)x & 7u)) : !elem_aligned(x, D, el)) return DET_ERR_ALIGN;
+  if ((dgamma || dbeta) && rows > 0 && (!ws || !aligned16(ws) || ws_bytes < det_layernorm_bwd_ws_bytes(rows, D))) return DET_ERR_WORKSPACE;
+  if (rows == 0) {
+    if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)D * sizeof(float), st) != cudaSuccess) return DET_ERR_CUDA;
+    if (dbeta && cudaMemsetAsync(dbeta, 0, (size_t)D * sizeof(float), st) != cudaSuccess) return DET_ERR_CUDA;
+    return DET_OK;
+  }
+  return ln_bwd<KIND>(dy, x, e8, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws, st);
+}
+
+extern "C" int det_layernorm_bwd(int io, const void* dy, const void* x, const void* gamma, const float* mean, const float* rstd, int rows,
+                                 int D, void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  if (io == DET_BF16)
+    return ln_bwd_entry<LN_BF16>(dy, x, nullptr, gamma, mean, rstd, rows, D, nullptr, dx, dgamma, dbeta, ws, ws_bytes, (cudaStream_t)stream);
+  if (io != DET_F32) return DET_ERR_ARG;
+  return ln_bwd_entry<LN_F32>(dy, x, nullptr, gamma, mean, rstd, rows, D, nullptr, dx, dgamma, dbeta, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+extern "C" int det_layernorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf16* gamma, const float* mean, const float* rstd,
+                                          int rows, int D, const det_bf16* res, det_bf16* dx, float* dgamma, float* dbeta, void* ws,
+                                          size_t ws_bytes, void* stream) {
+  if (!res) return DET_ERR_ARG;
+  return ln_bwd_entry<LN_BF16>(dy, x, nullptr, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+extern "C" int det_layernorm_bwd_act8(const det_bf16* dy, const int8_t* q8, const uint8_t* e8, const det_bf16* gamma, const float* mean,
+                                      const float* rstd, int rows, int D, const det_bf16* res, det_bf16* dx, float* dgamma, float* dbeta,
+                                      void* ws, size_t ws_bytes, void* stream) {
+  if (!e8) return DET_ERR_ARG;
+  return ln_bwd_entry<LN_ACT8>(dy, q8, e8, gamma, mean, rstd, rows, D, res, dx, dgamma, dbeta, ws, ws_bytes, (cudaStream_t)stream);
+}

@@ -3,33 +3,9 @@
 // a warp owns a leaf).
 #include "common.cuh"
 #include "internal.h"
+#include "rows.cuh"
 
 namespace det {
-
-template <bool BF>
-__device__ __forceinline__ void load8(const void* p, size_t idx, float v[8]) {
-  if (BF) {
-    uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + idx);
-    v[0] = bflo(u.x); v[1] = bfhi(u.x); v[2] = bflo(u.y); v[3] = bfhi(u.y);
-    v[4] = bflo(u.z); v[5] = bfhi(u.z); v[6] = bflo(u.w); v[7] = bfhi(u.w);
-  } else {
-    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + idx);
-    float4 a = q[0], b = q[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
-}
-template <bool BF>
-__device__ __forceinline__ void store8(void* p, size_t idx, const float v[8]) {
-  if (BF) {
-    uint4 u;
-    u.x = pack_bf2(v[0], v[1]); u.y = pack_bf2(v[2], v[3]); u.z = pack_bf2(v[4], v[5]); u.w = pack_bf2(v[6], v[7]);
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p) + idx) = u;
-  } else {
-    float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + idx);
-    q[0] = make_float4(v[0], v[1], v[2], v[3]);
-    q[1] = make_float4(v[4], v[5], v[6], v[7]);
-  }
-}
 
 // ------------------------------------------------------------------------------------------------
 // RMSNorm.  Rows of at most 2048 elements (8 leaves) are held in registers between the sum of squares and

@@ -1,0 +1,115 @@
+// Eight adjacent values of a row, bf16 or f32, in registers; the 8-bit checkpoint of 32 adjacent values (four lanes of eight).
+#pragma once
+#include "common.cuh"
+
+namespace det {
+
+template <bool BF>
+__device__ __forceinline__ void load8(const void* p, size_t idx, float v[8]) {
+  if (BF) {
+    uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + idx);
+    v[0] = bflo(u.x); v[1] = bfhi(u.x); v[2] = bflo(u.y); v[3] = bfhi(u.y);
+    v[4] = bflo(u.z); v[5] = bfhi(u.z); v[6] = bflo(u.w); v[7] = bfhi(u.w);
+  } else {
+    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + idx);
+    float4 a = q[0], b = q[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+template <bool BF>
+__device__ __forceinline__ void store8(void* p, size_t idx, const float v[8]) {
+  if (BF) {
+    uint4 u;
+    u.x = pack_bf2(v[0], v[1]); u.y = pack_bf2(v[2], v[3]); u.z = pack_bf2(v[4], v[5]); u.w = pack_bf2(v[6], v[7]);
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p) + idx) = u;
+  } else {
+    float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + idx);
+    q[0] = make_float4(v[0], v[1], v[2], v[3]);
+    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+// The same for rows of any length and address (VEC false: element by element): the first n of them, n may be beyond 8 or negative.
+template <bool BF, bool VEC>
+__device__ __forceinline__ void load8n(const void* p, size_t idx, int n, float v[8]) {
+  if (VEC) {
+    if (n > 0) { load8<BF>(p, idx, v); return; }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = 0.0f;
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      v[t] = t < n ? (BF ? bf2f(reinterpret_cast<const uint16_t*>(p)[idx + t]) : reinterpret_cast<const float*>(p)[idx + t]) : 0.0f;
+  }
+}
+template <bool BF, bool VEC>
+__device__ __forceinline__ void store8n(void* p, size_t idx, int n, const float v[8]) {
+  if (VEC) {
+    if (n > 0) store8<BF>(p, idx, v);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (t < n) {
+        if (BF) reinterpret_cast<uint16_t*>(p)[idx + t] = f2bf(v[t]);
+        else reinterpret_cast<float*>(p)[idx + t] = v[t];
+      }
+  }
+}
+
+// ---- 8-bit checkpoints -----------------------------------------------------------------------------------
+// A group is 32 adjacent values of a row.  Its step is the smallest power of two 2^E, at least 2^-126, with max|v| <= 127 * 2^E, kept as
+// its binary32 exponent field E + 127 (1 .. 249); code = rne(v / 2^E) in -127 .. 127.  With a power of two every product here is exact:
+// the code is the nearest one, and code * 2^E has at most 7 significant bits, so it is exact in bf16 too.  Field 255 marks a group
+// that holds an infinity or a NaN: codes +-127 for the infinities and 0 for the rest, which come back as infinities and NaNs.
+constexpr int A8_GROUP = 32;
+// the field from the largest magnitude's bits (of the whole group): its own exponent field less 6, one more past 127/64 of its power of two
+__device__ __forceinline__ uint32_t a8_field(uint32_t amax) {
+  const int f = (int)(amax >> 23) - 6 + ((amax & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+  return amax >= 0x7f800000u ? 255u : (uint32_t)max(f, 1);
+}
+__device__ __forceinline__ float a8_step(uint32_t field) { return __uint_as_float(field << 23); }
+__device__ __forceinline__ float a8_inv(uint32_t field) { return __uint_as_float((254u - field) << 23); }    // of a finite group
+__device__ __forceinline__ uint32_t a8_code_nonfinite(float v) {
+  return fabsf(v) != __int_as_float(0x7f800000) ? 0u : (v > 0.0f ? 127u : 0x81u);
+}
+// codes of eight values, low byte first; |v * inv| <= 127, and adding 1.5 * 2^23 rounds it to the nearest even integer, left in the low byte
+__device__ __forceinline__ uint2 a8_codes8(const float v[8], uint32_t field) {
+  uint32_t c[8];
+  if (field != 255u) {
+    const float inv = a8_inv(field);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) c[t] = __float_as_uint(fadd(fmul(v[t], inv), 12582912.0f));
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) c[t] = a8_code_nonfinite(v[t]);
+  }
+  uint2 o;
+  o.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+  o.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+  return o;
+}
+// one byte of four codes as a number: the byte, its sign flipped, in the low bits of 2^23 is 2^23 + 128 + code
+__device__ __forceinline__ float a8_value(uint32_t codes, int byte, float step) {
+  const uint32_t u = __byte_perm(codes ^ 0x80808080u, 0x4b000000u, 0x7540 + byte);
+  return fmul(fsub(__uint_as_float(u), 8388736.0f), step);
+}
+__device__ __forceinline__ void a8_values8(uint2 q, float step, float v[8]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    v[t] = a8_value(q.x, t, step);
+    v[4 + t] = a8_value(q.y, t, step);
+  }
+}
+// the largest magnitude of eight values as bits: an order of unsigned integers, NaNs above infinity
+__device__ __forceinline__ uint32_t a8_amax8(const float v[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) m = max(m, __float_as_uint(v[t]) & 0x7fffffffu);
+  return m;
+}
+// over the four lanes that hold a group; all lanes of the warp take part
+__device__ __forceinline__ uint32_t a8_quad_max(uint32_t m) {
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+}
+
+}  // namespace det
