@@ -11,10 +11,10 @@
 // a NaN.  The backward pass is the same from the last row to the first.  None of it depends on how blocks are dealt out.
 //
 // A chunk is walked by a half or a whole warp, two channels a lane, so a CTA of eight warps has a strip of 64 channels and one block, or 32 channels
-// and two blocks, a round.  The CTAs of a cluster take adjacent blocks, hand each other their block maps through distributed shared memory, one
-// cluster barrier per round, and every CTA applies the maps of the blocks before its own.  So every value is read once and written
-// once however long a sequence is and however few there are, with no workspace.  The raw values of the next round come in by asynchronous copies,
-// each thread its own, while this round is handed over.
+// and two blocks, a round.  One warp composes the chunk maps of a round.  The CTAs of a cluster take adjacent blocks and hand each other their
+// block maps through distributed shared memory, one cluster barrier per round; every CTA applies the maps of the blocks before its own.
+// So every value is read once and written once however long a sequence is and however few there are, with no workspace.  The raw
+// values of the next round come in by asynchronous copies while this one is worked on.
 #include "common.cuh"
 #include "internal.h"
 
@@ -22,26 +22,56 @@ namespace det {
 
 constexpr int LR_CHUNK = 8, LR_CHUNKS = 8, LR_BLOCK = LR_CHUNK * LR_CHUNKS, LR_T = 256, LR_MAXC = 16;
 
-// The gate of a bf16 has few arguments: the magnitudes from 2^-26 (e rounds to 1 below it) to 128 (e flushes to 0 long before), 33 exponents of
-// 128 fractions.  A CTA with many rows evaluates them all once into shared memory: a lookup instead of an exponential and a
-// division for every value.
-constexpr int LR_LOW = 0x3280, LR_TOP = 0x4300, LR_TAB = LR_TOP - LR_LOW + 1;
-
 __device__ __forceinline__ float lr_minor(float g) {
   const float e = det_exp_le0(-fabsf(g));
   return fdiv(e, fadd(1.0f, e));
 }
+// The gate of a bf16 has few arguments: the magnitudes from 2^-26 (e rounds to 1 below it) to 128 (e flushes to 0 long before), 33 exponents of
+// 128 fractions.  Their values of lr_minor, evaluated by the compiler with the same steps, are part of the library; a CTA copies them into shared
+// memory: a lookup instead of an exponential and a division for every value (some 30 of 50 instructions).
+constexpr int LR_LOW = 0x3280, LR_TOP = 0x4300, LR_TAB = (LR_TOP - LR_LOW + 1 + 3) / 4 * 4;
+struct __align__(16) LrTable { float m[LR_TAB]; };
+constexpr float lr_minor_at(int bits) {
+  float x = -(1.0f + (bits & 127) / 128.0f);
+  for (int e = bits >> 7; e > 127; --e) x *= 2.0f;
+  for (int e = bits >> 7; e < 127; ++e) x *= 0.5f;
+  if (x < -0x1.5d58a0p+6f) return 0.0f;
+  float t = x * 0x1.715476p+0f;
+  t = t + 12582912.0f;
+  const float kf = t - 12582912.0f;
+  t = kf * 0x1.62e400p-1f;
+  float r = x - t;
+  t = kf * 0x1.7f7d1cp-20f;
+  r = r - t;
+  const float c[7] = {0x1.6c16c2p-10f, 0x1.111112p-7f, 0x1.555556p-5f, 0x1.555556p-3f, 0.5f, 1.0f, 1.0f};
+  float q = 0x1.a01a02p-13f;
+  for (int i = 0; i < 7; ++i) {
+    t = q * r;
+    q = t + c[i];
+  }
+  for (int k = (int)kf; k < 0; ++k) q *= 0.5f;
+  const float d = 1.0f + q;
+  return q / d;
+}
+constexpr LrTable lr_make_table() {
+  LrTable t{};
+  for (int i = 0; i < LR_TAB; ++i) t.m[i] = lr_minor_at(LR_LOW + i);
+  return t;
+}
+__device__ constexpr LrTable lr_table_image = lr_make_table();
+
 __device__ __forceinline__ void lr_gate(float m, bool negative, float& f, float& z) {
   const float M = fsub(1.0f, m);
   f = negative ? m : M;
   z = negative ? M : m;
 }
-// gates of the two channels in one word; a NaN is looked up as an infinity: lr_gates puts it right
+// gates of the two channels in one word; by table a NaN is looked up as an infinity: lr_gates puts it right
 template <bool TAB>
 __device__ __forceinline__ void lr_gate2(uint32_t w, const float* tab, float f[2], float z[2]) {
   const char* t = reinterpret_cast<const char*>(tab);
-  const float m0 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w << 2) & 0x1fffcu) - 4 * LR_LOW, 4 * (LR_TAB - 1))) : lr_minor(bflo(w));
-  const float m1 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w >> 14) & 0x1fffcu) - 4 * LR_LOW, 4 * (LR_TAB - 1))) : lr_minor(bfhi(w));
+  constexpr int last = 4 * (LR_TOP - LR_LOW);
+  const float m0 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w << 2) & 0x1fffcu) - 4 * LR_LOW, last)) : lr_minor(bflo(w));
+  const float m1 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w >> 14) & 0x1fffcu) - 4 * LR_LOW, last)) : lr_minor(bfhi(w));
   lr_gate(m0, w & 0x8000u, f[0], z[0]);
   lr_gate(m1, (int)w < 0, f[1], z[1]);
 }
@@ -68,35 +98,39 @@ __device__ __forceinline__ void lr_extend(LrMap& m, int i, int n, const float f[
   m.a = cut ? make_float2(0.0f, 0.0f) : a;
 }
 
-// NS: tensors that come in by asynchronous copies
-template <int NS>
-struct LrShared {
-  uint32_t raw[2][NS][LR_CHUNK][LR_T];                   // two rounds
-  float4 chunk[LR_T];                                    // [chunk of the CTA][lane of it]: the chunk maps of this round
-  float4 block[2][LR_MAXC * 32];                         // [block of the round][lane]: block maps of the cluster; two rounds
-  float4 ahead[NS == 3 ? LR_T : 1];                      // backward: the chunk maps of the recurrence itself
-  float tab[LR_TAB];
+// CH channels a CTA: LANES lanes a chunk, BLOCKS blocks a round.
+template <int CH>
+struct LrDim {
+  static constexpr int LANES = CH / 2, BLOCKS = 64 / CH, PAD = CH == 64 ? 0 : 16;     // PAD: so that the two halves of a warp read different banks
+  static constexpr int STRIDE = LR_CHUNK * LANES + PAD, RAW = BLOCKS * LR_CHUNKS * STRIDE;
 };
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// NS: tensors that come in by asynchronous copies.  The block maps of the cluster, two rounds of them, lie behind this.
+template <int CH, int NS>
+struct __align__(16) LrShared {
+  uint32_t raw[2][NS][LrDim<CH>::RAW];                   // two rounds; [chunk of the CTA][row][lane]
+  float tab[LR_TAB];
+  float4 chunk[LR_T];                                    // [block of the CTA][chunk][lane]: the chunk maps of this round, then the maps of those before
+  float4 ahead[NS == 3 ? LR_T : 1];                      // backward: the same of the recurrence itself
+  float2 start[32];                                      // [block of the CTA][lane]: what comes into the blocks
+  float2 state[NS == 3 ? 32 : 1];                        // backward: the states in front of the blocks
+  __device__ __forceinline__ float4* slots(int round, int cl) { return reinterpret_cast<float4*>(this + 1) + (round & 1) * 32 * cl; }
+  static size_t bytes(int cl) { return sizeof(LrShared) + (size_t)2 * cl * 32 * sizeof(float4); }
+};
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void store_in_cluster(const void* local, int rank, float4 v) {
   uint32_t a;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-// four bytes, or zero where there is nothing
-__device__ __forceinline__ void copy4(uint32_t* dst, const void* src, bool there) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 4 : 0) : "memory");
+// 16 or 4 bytes, zeros where there is nothing (the address is not followed then)
+template <int WORDS>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
+  if (WORDS == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
-template <int NS>
-__device__ __forceinline__ void lr_table(LrShared<NS>& sh) {
-  for (int i = threadIdx.x; i < LR_TAB; i += LR_T) sh.tab[i] = lr_minor(__uint_as_float((uint32_t)(LR_LOW + i) << 16));
-  __syncthreads();
-}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 struct LrArgs {
   const uint16_t *g, *v, *dy;
@@ -108,29 +142,38 @@ struct LrArgs {
   int S, D, strips, nb, cl;                              // cl: CTAs of a cluster
 };
 
-// Where a thread is.  CH channels a CTA: CH / 2 lanes a chunk, BLOCKS blocks a round.
+// Where a thread is
 template <int CH>
 struct LrPlace {
-  static constexpr int LANES = CH / 2, BLOCKS = 64 / CH;
-  int b, c0, rank, blk, k, lane;                         // sequence, first channel; block of the CTA's, chunk of the block, lane of the chunk
+  int b, c0, rank, blk, k, lane;                         // sequence, first channel of the strip; block of the CTA's, chunk of the block, lane of the chunk
   bool have;                                             // the lane's channels exist
   __device__ __forceinline__ LrPlace(const LrArgs& p) {
     rank = blockIdx.x % p.cl;
     const int q = blockIdx.x / p.cl;
     b = q / p.strips;
-    lane = threadIdx.x % LANES;
-    const int chunk = threadIdx.x / LANES;
+    lane = threadIdx.x % LrDim<CH>::LANES;
+    const int chunk = threadIdx.x / LrDim<CH>::LANES;
     blk = chunk / LR_CHUNKS;
     k = chunk % LR_CHUNKS;
-    c0 = (q % p.strips) * CH + 2 * lane;
-    have = c0 < p.D;
+    c0 = (q % p.strips) * CH;
+    have = c0 + 2 * lane < p.D;
   }
 };
-// this thread's rows of a tensor on their way: `there` of them (0: none, its address is not followed)
-__device__ __forceinline__ void lr_fetch(uint32_t (*raw)[LR_T], const uint16_t* x, size_t ld, size_t row, int c0, int there) {
-  const uint16_t* q = there > 0 ? x + row * ld + c0 : x;
+// The rows of the CTA's blocks of one tensor on their way, in pieces of WORDS words: block j starts at row first + j * step (64 or -64), rows
+// outside the sequence and channels outside the tensor are zeros.
+template <int CH, int WORDS>
+__device__ __forceinline__ void lr_fetch(uint32_t* raw, const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace<CH>& at, int first, int step) {
+  constexpr int LANES = LrDim<CH>::LANES, PER = LANES / WORDS, COUNT = LrDim<CH>::BLOCKS * LR_BLOCK * PER / LR_T;
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(raw);
+  const int word = (threadIdx.x % PER) * WORDS, r0 = threadIdx.x / PER;
+  const bool have = at.c0 + 2 * word < p.D;
+  const uint16_t* base = x + (size_t)at.b * p.S * ld + at.c0 + 2 * word;
 #pragma unroll
-  for (int i = 0; i < LR_CHUNK; ++i) copy4(&raw[i][threadIdx.x], i < there ? q + i * ld : x, i < there);
+  for (int j = 0; j < COUNT; ++j) {
+    const int row = r0 + j * (LR_T / PER), t = first + (row / LR_BLOCK) * step + row % LR_BLOCK;
+    const bool there = have && (unsigned)t < (unsigned)p.S;
+    copy_async<WORDS>(dst + 4 * ((row / LR_CHUNK) * LrDim<CH>::STRIDE + (row % LR_CHUNK) * LANES + word), there ? base + (size_t)t * ld : x, there);
+  }
 }
 // the flag of row (lane of the chunk) of a chunk of n rows, and from the flags of the warp the cuts of this thread's chunk
 template <int CH, bool FLAGS>
@@ -142,64 +185,61 @@ __device__ __forceinline__ uint32_t lr_cuts(bool flag) {
   if (!FLAGS) return 0;
   return __ballot_sync(0xffffffffu, flag) >> ((threadIdx.x & 31) & ~(CH / 2 - 1));
 }
-// The gates of a chunk.  By table a NaN gate comes out as one of an infinity: it makes its gate a NaN here.
-template <bool TAB>
-__device__ __forceinline__ void lr_gates(const uint32_t w[LR_CHUNK], const float* tab, float f[LR_CHUNK][2], float z[LR_CHUNK][2]) {
+// The gates of a chunk.  A NaN gate comes out of the table as one of an infinity: it makes its gate a NaN here.
+__device__ __forceinline__ void lr_gates(const uint32_t* raw, int lanes, const float* tab, float f[LR_CHUNK][2], float z[LR_CHUNK][2]) {
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < LR_CHUNK; ++i) {
-    lr_gate2<TAB>(w[i], tab, f[i], z[i]);
-    if (TAB) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+    const uint32_t w = raw[i * lanes];
+    lr_gate2<true>(w, tab, f[i], z[i]);
+    top = __vmaxu2(top, w & 0x7fff7fffu);
   }
-  if (TAB && ((top & 0xffffu) > 0x7f80u || (top >> 16) > 0x7f80u)) {
+  if ((top & 0xffffu) > 0x7f80u || (top >> 16) > 0x7f80u) {
 #pragma unroll
     for (int i = 0; i < LR_CHUNK; ++i) {
-      if ((w[i] & 0x7fffu) > 0x7f80u) f[i][0] = z[i][0] = __int_as_float(0x7fffffff);
-      if (((w[i] >> 16) & 0x7fffu) > 0x7f80u) f[i][1] = z[i][1] = __int_as_float(0x7fffffff);
+      const uint32_t w = raw[i * lanes];
+      if ((w & 0x7fffu) > 0x7f80u) f[i][0] = z[i][0] = __int_as_float(0x7fffffff);
+      if (((w >> 16) & 0x7fffu) > 0x7f80u) f[i][1] = z[i][1] = __int_as_float(0x7fffffff);
     }
   }
 }
-// the maps of the chunks of a block before chunk k, one after the other; k > 0, at most `chunks` exist
+// The maps of the `chunks` chunks of a block, one after the other, by one thread: the map of those before chunk k takes chunk k's place, the map
+// of all comes back.
 template <int LANES>
-__device__ __forceinline__ LrMap lr_before(const float4* chunk, int k, int chunks) {
+__device__ __forceinline__ LrMap lr_scan(float4* chunk, int chunks) {
   LrMap m = lr_unpack(chunk[0]);
+  float4 next = chunk[LANES];
 #pragma unroll
-  for (int i = 1; i < LR_CHUNKS - 1; ++i) {
-    const LrMap next = lr_unpack(chunk[i * LANES]);
-    if (i < min(k, chunks)) m = lr_compose(m, next);
+  for (int i = 1; i < LR_CHUNKS; ++i) {
+    if (i >= chunks) break;
+    const LrMap here = lr_unpack(next);
+    if (i + 1 < chunks) next = chunk[(i + 1) * LANES];
+    chunk[i * LANES] = lr_pack(m);
+    m = lr_compose(m, here);
   }
   return m;
 }
-// The round's hand-over: this thread's chunk map in, the map of the chunks of its block before it out; `s`, the state at the start of the
-// round, becomes the one at the start of the next round, and the state at the start of this thread's block is returned.  `chunks` of the
-// block exist, `blocks` of the round; k is the chunk's place in the block in the order of the pass.
+// The round's hand-over, by the first warp, a thread per block of the CTA and lane: block maps to the CTAs of the cluster, what comes into each block
+// of this CTA back.  `s`, what comes into the round, becomes what comes into the next one.  `chunks` of the thread's block exist, in the places from
+// `first` on; `blocks` of the round.
 template <int CH, int NS>
-__device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p, const LrPlace<CH>& at, int round, int k, int chunks, int blocks,
-                                               const LrMap& mine, LrMap& before, float2& s) {
-  constexpr int LANES = LrPlace<CH>::LANES, BLOCKS = LrPlace<CH>::BLOCKS;
-  float4* chunk = sh.chunk + at.blk * LR_CHUNKS * LANES + at.lane;
-  chunk[k * LANES] = lr_pack(mine);
-  __syncthreads();
-  float4* slots = sh.block[round & 1];
-  before = mine;
-  if (k > 0 && chunks > 0) before = lr_before<LANES>(chunk, k, chunks);
-  if (k == LR_CHUNKS - 1 && chunks > 0) {
-    const float4 whole = lr_pack(chunks == LR_CHUNKS ? lr_compose(before, mine) : before);
-    float4* slot = slots + (at.rank * BLOCKS + at.blk) * LANES + at.lane;
-    if (p.cl == 1) *slot = whole;
-    else
-      for (int r = 0; r < p.cl; ++r) store_in_cluster(slot, r, whole);
-  }
+__device__ __forceinline__ float2 lr_hand_over(LrShared<CH, NS>& sh, const LrArgs& p, const LrPlace<CH>& at, int round, int first, int chunks, int blocks,
+                                               float2& s) {
+  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
+  const int blk = threadIdx.x / LANES, own = at.rank * BLOCKS + blk;
+  float4* slots = sh.slots(round, p.cl);
+  const float4 whole = lr_pack(lr_scan<LANES>(sh.chunk + (blk * LR_CHUNKS + first) * LANES + at.lane, chunks));
   if (p.cl == 1) {
-    __syncthreads();
+    slots[own * LANES + at.lane] = whole;
+    __syncwarp();
   } else {
-    // the barrier itself orders nothing: a release by every thread would wait for its stores of the round before
-    if (__any_sync(0xffffffffu, k == LR_CHUNKS - 1)) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    for (int r = 0; r < p.cl; ++r) store_in_cluster(&slots[own * LANES + at.lane], r, whole);
+    // the barrier orders nothing by itself: a release by every thread would wait for its stores of the round before
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
     cluster_arrive();
     cluster_wait();
   }
   float2 start = s;
-  const int own = at.rank * BLOCKS + at.blk;
 #pragma unroll 4
   for (int r = 0; r < blocks; ++r) {
     if (r == own) start = s;
@@ -207,160 +247,187 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p
   }
   return start;
 }
+// for the other warps: they arrive at once and wait with the rest
+__device__ __forceinline__ void lr_stand_by(const LrArgs& p) {
+  if (p.cl == 1) return;
+  cluster_arrive();
+  cluster_wait();
+}
+template <int CH, int NS>
+__device__ __forceinline__ void lr_copy_table(LrShared<CH, NS>& sh) {
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(sh.tab);
+  for (int i = threadIdx.x; i < LR_TAB / 4; i += LR_T) copy_async<4>(dst + 16 * i, lr_table_image.m + 4 * i, true);
+}
 
-template <int CH, bool TAB, bool FLAGS>
+template <int CH, int WORDS, bool FLAGS>
 __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<2>& sh = *reinterpret_cast<LrShared<2>*>(smem);
+  LrShared<CH, 2>& sh = *reinterpret_cast<LrShared<CH, 2>*>(smem);
   const LrPlace<CH> at(p);
-  constexpr int BLOCKS = LrPlace<CH>::BLOCKS;
+  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
   if (p.cl > 1) cluster_arrive();                        // every CTA has started before another one writes to its shared memory
-  if (TAB) lr_table(sh);
+  lr_copy_table(sh);
   grid_dep();
   const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per, step = per * LR_BLOCK;
-  int t0 = ((at.rank * BLOCKS + at.blk) * LR_CHUNKS + at.k) * LR_CHUNK;
+  int b0 = at.rank * BLOCKS * LR_BLOCK;                  // the CTA's first row of the round
+  const int ch = at.c0 + 2 * at.lane;
+  const bool lead = threadIdx.x < 32;
   bool flag = false;
-  auto fetch = [&](int round, int t) {
-    const int n = at.have ? p.S - t : 0;
-    const size_t row = (size_t)at.b * p.S + t;
-    lr_fetch(sh.raw[round & 1][0], p.g, p.ld, row, at.c0, n);
-    lr_fetch(sh.raw[round & 1][1], p.v, p.ld, row, at.c0, n);
-    copies_close();
+  auto fetch = [&](int round, int row) {
+    lr_fetch<CH, WORDS>(sh.raw[round & 1][0], p.g, p.ld, p, at, row, LR_BLOCK);
+    lr_fetch<CH, WORDS>(sh.raw[round & 1][1], p.v, p.ld, p, at, row, LR_BLOCK);
+    const int t = row + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK;
     flag = lr_flag<CH, FLAGS>(p, at, t, p.S - t);
   };
-  fetch(0, t0);
+  fetch(0, b0);
   float2 s = make_float2(0.0f, 0.0f);
-  if (p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + at.c0);
-  __syncwarp();
+  if (lead && p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + ch);
+  copies_done();
+  __syncthreads();
   if (p.cl > 1) cluster_wait();
-  for (int k = 0; k < rounds; ++k, t0 += step) {
-    const int blk = k * per + at.rank * BLOCKS + at.blk, n = p.S - t0;                 // n rows of the chunk exist
-    const int chunks = max(0, min(LR_CHUNKS, (p.S - blk * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK));
+  for (int k = 0; k < rounds; ++k, b0 += step) {
+    const int t0 = b0 + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK, n = p.S - t0;          // n rows of the chunk exist
     const uint32_t cuts = lr_cuts<CH, FLAGS>(flag);
-    if (k + 1 < rounds) fetch(k + 1, t0 + step);
-    else copies_close();
-    copies_wait<1>();
-    uint32_t wg[LR_CHUNK];
-#pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) wg[i] = sh.raw[k & 1][0][i][threadIdx.x];
+    if (k + 1 < rounds) fetch(k + 1, b0 + step);
+    const uint32_t* raw = sh.raw[k & 1][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
     float f[LR_CHUNK][2], u[LR_CHUNK][2];
-    lr_gates<TAB>(wg, sh.tab, f, u);
+    lr_gates(raw, LANES, sh.tab, f, u);
+    raw += LrDim<CH>::RAW;
     LrMap mine;
 #pragma unroll
     for (int i = 0; i < LR_CHUNK; ++i) {
-      const uint32_t w = sh.raw[k & 1][1][i][threadIdx.x];
+      const uint32_t w = raw[i * LANES];
       u[i][0] = fmul(u[i][0], bflo(w));
       u[i][1] = fmul(u[i][1], bfhi(w));
       lr_extend(mine, i, n, f[i], make_float2(u[i][0], u[i][1]), (cuts >> i) & 1);
     }
-    LrMap before;
-    const float2 start = lr_hand_over(sh, p, at, k, at.k, chunks, min(per, p.nb - k * per), mine, before, s);
-    if (p.save && at.k == 0 && n > 0 && at.have) *reinterpret_cast<float2*>(p.save + ((size_t)at.b * p.nb + blk) * p.D + at.c0) = start;
-    float2 h = at.k ? lr_apply(before, start) : start;
-    uint16_t* out = p.y + ((size_t)at.b * p.S + t0) * p.ld_y + at.c0;
+    sh.chunk[threadIdx.x] = lr_pack(mine);               // [block][chunk][lane] is the thread's number
+    __syncthreads();
+    if (lead) {
+      const int row = b0 + (threadIdx.x / LANES) * LR_BLOCK, blk = row / LR_BLOCK;
+      const int chunks = max(0, min(LR_CHUNKS, (p.S - row + LR_CHUNK - 1) / LR_CHUNK));
+      const float2 start = lr_hand_over(sh, p, at, k, 0, chunks, min(per, p.nb - k * per), s);
+      sh.start[threadIdx.x] = start;
+      if (p.save && chunks > 0 && at.have) *reinterpret_cast<float2*>(p.save + ((size_t)at.b * p.nb + blk) * p.D + ch) = start;
+    } else {
+      lr_stand_by(p);
+    }
+    copies_done();
+    __syncthreads();
+    float2 h = sh.start[at.blk * LANES + at.lane];
+    if (at.k) h = lr_apply(lr_unpack(sh.chunk[threadIdx.x]), h);
+    uint16_t* out = p.y + ((size_t)at.b * p.S + t0) * p.ld_y + ch;
 #pragma unroll
     for (int i = 0; i < LR_CHUNK; ++i) {
       h = lr_step(f[i], make_float2(u[i][0], u[i][1]), h, (cuts >> i) & 1);
-      if (i < n && at.have) *reinterpret_cast<uint32_t*>(out + i * p.ld_y) = pack_bf2(h.x, h.y);
+      if (i < n && at.have) *reinterpret_cast<uint32_t*>(out) = pack_bf2(h.x, h.y);
+      out += p.ld_y;
     }
     __syncwarp();
   }
-  if (p.last && at.have && threadIdx.x < CH / 2 && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + at.c0) = s;
+  if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
-template <int CH, bool TAB, bool FLAGS>
+template <int CH, int WORDS, bool FLAGS>
 __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<3>& sh = *reinterpret_cast<LrShared<3>*>(smem);
+  LrShared<CH, 3>& sh = *reinterpret_cast<LrShared<CH, 3>*>(smem);
   const LrPlace<CH> at(p);
-  constexpr int LANES = LrPlace<CH>::LANES, BLOCKS = LrPlace<CH>::BLOCKS;
+  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
   if (p.cl > 1) cluster_arrive();
-  if (TAB) lr_table(sh);
+  lr_copy_table(sh);
   grid_dep();
   const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per;
+  const int ch = at.c0 + 2 * at.lane, warp = threadIdx.x >> 5, own = (threadIdx.x & 31) / LANES;
+  int top = p.nb - 1 - at.rank * BLOCKS;                 // the CTA's blocks of the round are top, top - 1; below 0: none
   bool flag = false;
-  float2 state_next = make_float2(0.0f, 0.0f);
-  auto fetch = [&](int round, int blk) {                 // blk below 0: there is none
-    const int t = blk * LR_BLOCK + at.k * LR_CHUNK, n = blk >= 0 && at.have ? p.S - t : 0;
-    const size_t row = blk >= 0 ? (size_t)at.b * p.S + t : 0;
-    lr_fetch(sh.raw[round & 1][0], p.g, p.ld, row, at.c0, n);
-    lr_fetch(sh.raw[round & 1][1], p.v, p.ld, row, at.c0, n);
-    lr_fetch(sh.raw[round & 1][2], p.dy, p.ld_y, row, at.c0, n);
-    copies_close();
-    flag = lr_flag<CH, FLAGS>(p, at, t, blk >= 0 ? p.S - t : 0);
-    if (blk >= 0 && at.have) state_next = *reinterpret_cast<const float2*>(p.states + ((size_t)at.b * p.nb + blk) * p.D + at.c0);
+  float2 state = make_float2(0.0f, 0.0f);
+  auto fetch = [&](int round, int first) {
+    const int row = first * LR_BLOCK;
+    lr_fetch<CH, WORDS>(sh.raw[round & 1][0], p.g, p.ld, p, at, row, -LR_BLOCK);
+    lr_fetch<CH, WORDS>(sh.raw[round & 1][1], p.v, p.ld, p, at, row, -LR_BLOCK);
+    lr_fetch<CH, WORDS>(sh.raw[round & 1][2], p.dy, p.ld_y, p, at, row, -LR_BLOCK);
+    const int t = (first - at.blk) * LR_BLOCK + at.k * LR_CHUNK;
+    flag = lr_flag<CH, FLAGS>(p, at, t, first - at.blk < 0 ? 0 : p.S - t);
+    if (warp == 1 && first - own >= 0 && at.have) state = *reinterpret_cast<const float2*>(p.states + ((size_t)at.b * p.nb + first - own) * p.D + ch);
   };
-  int blk = p.nb - 1 - (at.rank * BLOCKS + at.blk);       // from the last block to the first
-  fetch(0, blk);
+  fetch(0, top);
   float2 s = make_float2(0.0f, 0.0f);
-  if (p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + at.c0);
-  __syncwarp();
+  if (warp == 0 && p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + ch);
+  copies_done();
+  __syncthreads();
   if (p.cl > 1) cluster_wait();
-  for (int r = 0; r < rounds; ++r, blk -= per) {
+  for (int r = 0; r < rounds; ++r, top -= per) {
+    const int blk = top - at.blk, t0 = blk * LR_BLOCK + at.k * LR_CHUNK, n = blk < 0 ? 0 : p.S - t0;
     const int chunks = blk < 0 ? 0 : min(LR_CHUNKS, (p.S - blk * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK);
-    const int t0 = blk * LR_BLOCK + at.k * LR_CHUNK, n = blk < 0 ? 0 : p.S - t0;
     const uint32_t cuts = lr_cuts<CH, FLAGS>(flag);
-    const float2 state = state_next;
-    if (r + 1 < rounds) fetch(r + 1, blk - per);
-    else copies_close();
-    copies_wait<1>();
-    const uint32_t (*raw)[LR_CHUNK][LR_T] = sh.raw[r & 1];
-    uint32_t wg[LR_CHUNK];
-#pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) wg[i] = raw[0][i][threadIdx.x];
+    const float2 front = state;
+    if (r + 1 < rounds) fetch(r + 1, top - per);
+    const uint32_t* raw = sh.raw[r & 1][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
     float f[LR_CHUNK][2], z[LR_CHUNK][2];
-    lr_gates<TAB>(wg, sh.tab, f, z);
+    uint32_t wv[LR_CHUNK], wd[LR_CHUNK];
+    lr_gates(raw, LANES, sh.tab, f, z);
     LrMap mine, fore;                                    // of the gradient, of the state
 #pragma unroll
     for (int i = 0; i < LR_CHUNK; ++i) {
-      const uint32_t w = raw[1][i][threadIdx.x];
-      lr_extend(fore, i, n, f[i], make_float2(fmul(z[i][0], bflo(w)), fmul(z[i][1], bfhi(w))), (cuts >> i) & 1);
+      wv[i] = raw[LrDim<CH>::RAW + i * LANES];
+      wd[i] = raw[2 * LrDim<CH>::RAW + i * LANES];
+      lr_extend(fore, i, n, f[i], make_float2(fmul(z[i][0], bflo(wv[i])), fmul(z[i][1], bfhi(wv[i]))), (cuts >> i) & 1);
     }
     bool any = false;
     mine.a = mine.h = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int i = LR_CHUNK - 1; i >= 0; --i) {
       if (i >= n) continue;
-      const uint32_t w = raw[2][i][threadIdx.x];
-      const float2 d = make_float2(bflo(w), bfhi(w));
+      const float2 d = make_float2(bflo(wd[i]), bfhi(wd[i]));
       mine.h = any ? make_float2(fmul(f[i][0], fadd(d.x, mine.h.x)), fmul(f[i][1], fadd(d.y, mine.h.y))) : make_float2(fmul(f[i][0], d.x), fmul(f[i][1], d.y));
       mine.a = any ? make_float2(fmul(f[i][0], mine.a.x), fmul(f[i][1], mine.a.y)) : make_float2(f[i][0], f[i][1]);
       if ((cuts >> i) & 1) mine.a = mine.h = make_float2(0.0f, 0.0f);
       any = true;
     }
+    // in the order of the backward pass: the block's last chunk, which may not exist, has the first place
+    float4* place = sh.chunk + (at.blk * LR_CHUNKS + LR_CHUNKS - 1 - at.k) * LANES + at.lane;
+    *place = lr_pack(mine);
     sh.ahead[threadIdx.x] = lr_pack(fore);
-    // the order of the backward pass: chunk 0 is the block's last one that exists; those beyond the end stay behind it
-    const int order = at.k < chunks ? chunks - 1 - at.k : at.k;
-    LrMap behind;
-    const float2 start = lr_hand_over(sh, p, at, r, order, chunks, min(per, p.nb - r * per), mine, behind, s);
-    if (n > 0 && at.have) {
-      float2 h = state;
-      if (at.k) h = lr_apply(lr_before<LANES>(sh.ahead + at.blk * LR_CHUNKS * LANES + at.lane, at.k, LR_CHUNKS), state);
-      float2 prev[LR_CHUNK];
-#pragma unroll
-      for (int i = 0; i < LR_CHUNK; ++i) {
-        const uint32_t w = raw[1][i][threadIdx.x];
-        const bool cut = (cuts >> i) & 1;
-        prev[i] = cut ? make_float2(0.0f, 0.0f) : h;
-        h = lr_step(f[i], make_float2(fmul(z[i][0], bflo(w)), fmul(z[i][1], bfhi(w))), h, cut);
-        prev[i] = make_float2(fsub(prev[i].x, bflo(w)), fsub(prev[i].y, bfhi(w)));
+    __syncthreads();
+    if (warp == 0) {
+      const int b = top - own, have = b < 0 ? 0 : min(LR_CHUNKS, (p.S - b * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK);
+      sh.start[threadIdx.x] = lr_hand_over(sh, p, at, r, have ? LR_CHUNKS - have : 0, have, min(per, p.nb - r * per), s);
+    } else {
+      if (warp == 1) {
+        lr_scan<LANES>(sh.ahead + own * LR_CHUNKS * LANES + at.lane, LR_CHUNKS);
+        sh.state[threadIdx.x & 31] = front;
       }
-      float2 c = order ? lr_apply(behind, start) : start;
-      const size_t o = ((size_t)at.b * p.S + t0) * p.ld_d + at.c0;
-#pragma unroll
-      for (int i = LR_CHUNK - 1; i >= 0; --i) {
-        if (i >= n) continue;
-        const uint32_t w = raw[2][i][threadIdx.x];
-        const float2 d = make_float2(fadd(bflo(w), c.x), fadd(bfhi(w), c.y));
-        c = (cuts >> i) & 1 ? make_float2(0.0f, 0.0f) : make_float2(fmul(f[i][0], d.x), fmul(f[i][1], d.y));
-        *reinterpret_cast<uint32_t*>(p.dv + o + i * p.ld_d) = pack_bf2(fmul(d.x, z[i][0]), fmul(d.y, z[i][1]));
-        *reinterpret_cast<uint32_t*>(p.dg + o + i * p.ld_d) =
-            pack_bf2(fmul(fmul(d.x, prev[i].x), fmul(f[i][0], z[i][0])), fmul(fmul(d.y, prev[i].y), fmul(f[i][1], z[i][1])));
-      }
+      lr_stand_by(p);
     }
-    __syncthreads();                                     // `ahead` is read by then
+    copies_done();
+    __syncthreads();
+    float2 h = sh.state[at.blk * LANES + at.lane], c = sh.start[at.blk * LANES + at.lane];
+    if (at.k) h = lr_apply(lr_unpack(sh.ahead[threadIdx.x]), h);
+    if (at.k + 1 < chunks) c = lr_apply(lr_unpack(*place), c);
+    float2 diff[LR_CHUNK];                               // h_{t-1} - v
+#pragma unroll
+    for (int i = 0; i < LR_CHUNK; ++i) {
+      const bool cut = (cuts >> i) & 1;
+      const float2 v = make_float2(bflo(wv[i]), bfhi(wv[i]));
+      diff[i] = cut ? make_float2(fsub(0.0f, v.x), fsub(0.0f, v.y)) : make_float2(fsub(h.x, v.x), fsub(h.y, v.y));
+      h = lr_step(f[i], make_float2(fmul(z[i][0], v.x), fmul(z[i][1], v.y)), h, cut);
+    }
+    const size_t o = ((size_t)at.b * p.S + t0 + LR_CHUNK - 1) * p.ld_d + ch;           // only followed where the row exists
+    uint16_t *dv = p.dv + o, *dg = p.dg + o;
+#pragma unroll
+    for (int i = LR_CHUNK - 1; i >= 0; --i, dv -= p.ld_d, dg -= p.ld_d) {
+      if (i >= n) continue;
+      const float2 d = make_float2(fadd(bflo(wd[i]), c.x), fadd(bfhi(wd[i]), c.y));
+      c = (cuts >> i) & 1 ? make_float2(0.0f, 0.0f) : make_float2(fmul(f[i][0], d.x), fmul(f[i][1], d.y));
+      if (!at.have) continue;
+      *reinterpret_cast<uint32_t*>(dv) = pack_bf2(fmul(d.x, z[i][0]), fmul(d.y, z[i][1]));
+      *reinterpret_cast<uint32_t*>(dg) =
+          pack_bf2(fmul(fmul(d.x, diff[i].x), fmul(f[i][0], z[i][0])), fmul(fmul(d.y, diff[i].y), fmul(f[i][1], z[i][1])));
+    }
+    __syncwarp();
   }
-  if (p.last && at.have && threadIdx.x < CH / 2 && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + at.c0) = s;
+  if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
 // Sequences of one chunk (a token at a time among them): a thread walks two channels alone, with nothing to hand over.
@@ -427,13 +494,13 @@ static LrPlan lr_plan(int B, int D, int nb, int waves) {
   while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= room) q.cl *= 2;
   return q;
 }
-template <int NS>
-static int lr_launch(void (*kern)(const LrArgs), LrArgs& p, LrPlan q, int B, DevOnce& once, cudaStream_t st) {
-  p.cl = q.cl;
-  p.strips = (p.D + q.ch - 1) / q.ch;
-  int rc = dev_ensure_smem(once, (const void*)kern, sizeof(LrShared<NS>));
+static int lr_launch(void (*kern)(const LrArgs), const LrArgs& p, int B, size_t smem, size_t most, DevOnce& once, cudaStream_t st) {
+  int rc = dev_ensure_smem(once, (const void*)kern, most);
   if (rc != DET_OK) return rc;
-  if (q.cl > 8 && cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return DET_ERR_CUDA;
+  if (p.cl > 8 && cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    cudaGetLastError();
+    return DET_ERR_CUDA;
+  }
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -443,7 +510,7 @@ static int lr_launch(void (*kern)(const LrArgs), LrArgs& p, LrPlan q, int B, Dev
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((long long)B * p.strips * p.cl));
   cfg.blockDim = dim3(LR_T);
-  cfg.dynamicSmemBytes = sizeof(LrShared<NS>);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = p.cl > 1 ? 2 : 1;
@@ -452,10 +519,18 @@ static int lr_launch(void (*kern)(const LrArgs), LrArgs& p, LrPlan q, int B, Dev
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
-template <int CH, bool TAB, bool FLAGS>
-static int lr_run(bool bwd, LrArgs& p, LrPlan q, int B, cudaStream_t st) {
+template <int CH, int WORDS, bool FLAGS>
+static int lr_run(bool bwd, const LrArgs& p, int B, cudaStream_t st) {
   static DevOnce fwd_once, bwd_once;
-  return bwd ? lr_launch<3>(k_linrec_bwd<CH, TAB, FLAGS>, p, q, B, bwd_once, st) : lr_launch<2>(k_linrec_fwd<CH, TAB, FLAGS>, p, q, B, fwd_once, st);
+  using Sf = LrShared<CH, 2>;
+  using Sb = LrShared<CH, 3>;
+  return bwd ? lr_launch(k_linrec_bwd<CH, WORDS, FLAGS>, p, B, Sb::bytes(p.cl), Sb::bytes(LR_MAXC), bwd_once, st)
+             : lr_launch(k_linrec_fwd<CH, WORDS, FLAGS>, p, B, Sf::bytes(p.cl), Sf::bytes(LR_MAXC), fwd_once, st);
+}
+template <int CH>
+static int lr_pick(bool bwd, const LrArgs& p, int B, bool wide, cudaStream_t st) {
+  return wide ? (p.flags ? lr_run<CH, 4, true>(bwd, p, B, st) : lr_run<CH, 4, false>(bwd, p, B, st))
+              : (p.flags ? lr_run<CH, 1, true>(bwd, p, B, st) : lr_run<CH, 1, false>(bwd, p, B, st));
 }
 static int lr_any(bool bwd, LrArgs& p, int B, cudaStream_t st) {
   p.nb = (p.S + LR_BLOCK - 1) / LR_BLOCK;
@@ -466,12 +541,11 @@ static int lr_any(bool bwd, LrArgs& p, int B, cudaStream_t st) {
     return DET_OK;
   }
   const LrPlan q = lr_plan(B, p.D, p.nb, bwd ? 2 : 3);
-  const bool tab = p.nb * 64 / q.ch / q.cl >= 4;
-  if (q.ch == 64)
-    return tab ? (p.flags ? lr_run<64, true, true>(bwd, p, q, B, st) : lr_run<64, true, false>(bwd, p, q, B, st))
-               : (p.flags ? lr_run<64, false, true>(bwd, p, q, B, st) : lr_run<64, false, false>(bwd, p, q, B, st));
-  return tab ? (p.flags ? lr_run<32, true, true>(bwd, p, q, B, st) : lr_run<32, true, false>(bwd, p, q, B, st))
-             : (p.flags ? lr_run<32, false, true>(bwd, p, q, B, st) : lr_run<32, false, false>(bwd, p, q, B, st));
+  p.cl = q.cl;
+  p.strips = (p.D + q.ch - 1) / q.ch;
+  // whole pieces of 16 bytes where the tensors allow it
+  const bool wide = p.D % 8 == 0 && p.ld % 8 == 0 && aligned16(p.g) && aligned16(p.v) && (!bwd || (p.ld_y % 8 == 0 && aligned16(p.dy)));
+  return q.ch == 64 ? lr_pick<64>(bwd, p, B, wide, st) : lr_pick<32>(bwd, p, B, wide, st);
 }
 static int lr_check(const void* a, const void* b, int ld, int B, int S, int D) {
   if (!a || !b || B < 0 || S < 0 || D <= 0 || ld < D) return DET_ERR_ARG;
