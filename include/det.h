@@ -221,14 +221,15 @@ int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8,
  * within a block, block by block along the sequence; h is walked from the state at the start of its chunk; A = 0 lets nothing in.
  * states f32 [B, ceil(S/64), D] (det_linrec_state_floats; NULL: not kept) are the states in front of the blocks, for the backward pass.
  * D, ld, ld_y, ld_d even, S <= 2^30; bf16 pointers 4-byte, f32 pointers 8-byte aligned.  S = 0: hT = h0, dh0 = dhT.  Outputs overlap no
- * input but as said. */
+ * input but as said.  status_dev (may be NULL) receives DET_DEV_TIMEOUT if a bounded wait of one CTA for another runs out. */
 size_t det_linrec_state_floats(int B, int S, int D);
 int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, det_bf16* y, int ld_y, const uint8_t* flags,
-                   const float* h0, float* hT, float* states, void* stream);
+                   const float* h0, float* hT, float* states, void* stream, int* status_dev);
 /* dh_t = dy_t + f_{t+1} dh_{t+1}, behind the last row dhT f32 [B, D] (NULL: zero): dv = dh z, dg = dh (h_{t-1} - v) (f z) (bf16, row stride ld_d),
  * dh0 f32 [B, D] (may be NULL, may be dhT); composed as in the forward pass, from the last row to the first. */
 int det_linrec_bwd(const det_bf16* dy, int ld_y, const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, const float* states,
-                   det_bf16* dg, det_bf16* dv, int ld_d, const uint8_t* flags, const float* dhT, float* dh0, void* stream);
+                   det_bf16* dg, det_bf16* dv, int ld_d, const uint8_t* flags, const float* dhT, float* dh0, void* stream,
+                   int* status_dev);
 
 /* ---- per-head operations of the attention block (Sec. 3.1 "QK-norm", "RoPE") --------------------------
  * Rows of 128 values (one head of one token) inside wider token rows: element (t, h, i) of x sits at

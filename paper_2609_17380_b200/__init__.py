@@ -73,7 +73,7 @@ _SIGNATURES = {
     "det_layernorm_bwd": "iipppppiippppzp", "det_layernorm_bwd_residual": "ipppppiipppppzp", "det_layernorm_bwd_act8": "ippppppiipppppzp",
     "det_act8_exp_bytes": "zii", "det_act8_pack": "iipiiippp", "det_act8_unpack": "iippiipip",
     "det_swiglu_fwd_act8": "ipiipppppp", "det_swiglu_act8": "ippiipppp", "det_swiglu_bwd_act8": "ipppiipp",
-    "det_linrec_state_floats": "ziii", "det_linrec_fwd": "ippiiiipippppp", "det_linrec_bwd": "ipippiiiipppipppp",
+    "det_linrec_state_floats": "ziii", "det_linrec_fwd": "ippiiiipipppppp", "det_linrec_bwd": "ipippiiiipppippppp",
 }
 
 # The entry points that csrc/binding.cpp calls directly: what it makes of each Python argument (letters as above; w: a workspace tensor or None,
@@ -93,7 +93,7 @@ _PATTERNS = {
     "det_layernorm_fwd": "ipppiifppps", "det_residual_layernorm_fwd": "ppppiifpppppppps", "det_layernorm_bwd": "ipppppiipppws",
     "det_layernorm_bwd_residual": "pppppiippppws", "det_layernorm_bwd_act8": "ppppppiippppws", "det_act8_pack": "ipiiipps",
     "det_act8_unpack": "ippiipis", "det_swiglu_fwd_act8": "piippppps", "det_swiglu_act8": "ppiippps",
-    "det_swiglu_bwd_act8": "pppiips", "det_linrec_fwd": "ppiiiipipppps", "det_linrec_bwd": "pippiiiipppippps",
+    "det_swiglu_bwd_act8": "pppiips", "det_linrec_fwd": "ppiiiipippppsp", "det_linrec_bwd": "pippiiiipppipppsp",
 }
 
 
@@ -358,12 +358,12 @@ def det_linrec_state_floats(B, S, D):
     return load().det_linrec_state_floats(B, S, D)
 
 
-def det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags=None, h0=None, hT=None, states=None):
-    _c.det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags, h0, hT, states)
+def det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags=None, h0=None, hT=None, states=None, status_dev=None):
+    _c.det_linrec_fwd(g, v, ld, B, S, D, y, ld_y, flags, h0, hT, states, status_dev)
 
 
-def det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags=None, dhT=None, dh0=None):
-    _c.det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags, dhT, dh0)
+def det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags=None, dhT=None, dh0=None, status_dev=None):
+    _c.det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags, dhT, dh0, status_dev)
 
 
 # ---- attention ------------------------------------------------------------------------------------------------

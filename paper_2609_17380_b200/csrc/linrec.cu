@@ -12,11 +12,13 @@
 //
 // A chunk is walked by a half or a whole warp, two channels a lane, so a CTA of eight warps has a strip of 64 channels and one block, or 32 channels
 // and two blocks, a round.  One warp composes the chunk maps of a round.  The CTAs of a cluster take adjacent blocks and hand each other their
-// block maps through distributed shared memory, one cluster barrier per round; every CTA applies the maps of the blocks before its own.
+// block maps through distributed shared memory, by stores that complete a transaction barrier of the receiver (a fence and a cluster barrier a round
+// took 1300 cycles of 4800); every CTA applies the maps of the blocks before its own.
 // So every value is read once and written once however long a sequence is and however few there are, with no workspace.  The raw
 // values of the next round come in by asynchronous copies while this one is worked on.
 #include "common.cuh"
 #include "internal.h"
+#include "tc05.cuh"
 
 namespace det {
 
@@ -113,15 +115,21 @@ struct __align__(16) LrShared {
   float4 ahead[NS == 3 ? LR_T : 1];                      // backward: the same of the recurrence itself
   float2 start[32];                                      // [block of the CTA][lane]: what comes into the blocks
   float2 state[NS == 3 ? 32 : 1];                        // backward: the states in front of the blocks
+  unsigned long long arrived[2];                         // transaction barriers of the block maps, two rounds
+  int gone;                                              // a wait ran out
   __device__ __forceinline__ float4* slots(int round, int cl) { return reinterpret_cast<float4*>(this + 1) + (round & 1) * 32 * cl; }
   static size_t bytes(int cl) { return sizeof(LrShared) + (size_t)2 * cl * 32 * sizeof(float4); }
 };
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ void store_in_cluster(const void* local, int rank, float4 v) {
-  uint32_t a;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
-  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+// a float4 into the place of `local` in the CTA `rank` of the cluster, counted by its barrier in the place of `bar`
+__device__ __forceinline__ void store_in_cluster(const void* local, const void* bar, int rank, float4 v) {
+  uint32_t a, b;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(local)), "r"(rank));
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_u32(bar)), "r"(rank));
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(a), "f"(v.x), "f"(v.y),
+               "f"(v.z), "f"(v.w), "r"(b)
+               : "memory");
 }
 // 16 or 4 bytes, zeros where there is nothing (the address is not followed then)
 template <int WORDS>
@@ -140,6 +148,7 @@ struct LrArgs {
   float *last, *save;                                    // what comes out at the other end; states at the starts of the blocks
   size_t ld, ld_y, ld_d;
   int S, D, strips, nb, cl;                              // cl: CTAs of a cluster
+  int* status;
 };
 
 // Where a thread is
@@ -208,47 +217,74 @@ __device__ __forceinline__ void lr_gates(const uint32_t* raw, int lanes, const f
 template <int LANES>
 __device__ __forceinline__ LrMap lr_scan(float4* chunk, int chunks) {
   LrMap m = lr_unpack(chunk[0]);
-  float4 next = chunk[LANES];
+  if (chunks == LR_CHUNKS) {
+    float4 next[LR_CHUNKS];
 #pragma unroll
-  for (int i = 1; i < LR_CHUNKS; ++i) {
-    if (i >= chunks) break;
-    const LrMap here = lr_unpack(next);
-    if (i + 1 < chunks) next = chunk[(i + 1) * LANES];
-    chunk[i * LANES] = lr_pack(m);
-    m = lr_compose(m, here);
+    for (int i = 1; i < LR_CHUNKS; ++i) next[i] = chunk[i * LANES];
+#pragma unroll
+    for (int i = 1; i < LR_CHUNKS; ++i) {
+      chunk[i * LANES] = lr_pack(m);
+      m = lr_compose(m, lr_unpack(next[i]));
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 1; i < chunks; ++i) {
+      const LrMap here = lr_unpack(chunk[i * LANES]);
+      chunk[i * LANES] = lr_pack(m);
+      m = lr_compose(m, here);
+    }
   }
   return m;
 }
 // The round's hand-over, by the first warp, a thread per block of the CTA and lane: block maps to the CTAs of the cluster, what comes into each block
 // of this CTA back.  `s`, what comes into the round, becomes what comes into the next one.  `chunks` of the thread's block exist, in the places from
 // `first` on; `blocks` of the round.
+// The maps of two rounds have places of their own: a CTA sends those of round r + 2 when it has all of round r + 1, this CTA's among them, which this CTA
+// sent after it had read round r's.
 template <int CH, int NS>
 __device__ __forceinline__ float2 lr_hand_over(LrShared<CH, NS>& sh, const LrArgs& p, const LrPlace<CH>& at, int round, int first, int chunks, int blocks,
                                                float2& s) {
-  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
+  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS, BATCH = 8;
   const int blk = threadIdx.x / LANES, own = at.rank * BLOCKS + blk;
   float4* slots = sh.slots(round, p.cl);
+  uint64_t* bar = reinterpret_cast<uint64_t*>(&sh.arrived[round & 1]);
+  if (p.cl > 1 && threadIdx.x == 0) mbar_expect_tx(bar, p.cl * 32 * sizeof(float4));
   const float4 whole = lr_pack(lr_scan<LANES>(sh.chunk + (blk * LR_CHUNKS + first) * LANES + at.lane, chunks));
   if (p.cl == 1) {
     slots[own * LANES + at.lane] = whole;
     __syncwarp();
   } else {
-    for (int r = 0; r < p.cl; ++r) store_in_cluster(&slots[own * LANES + at.lane], r, whole);
-    // the barrier orders nothing by itself: a release by every thread would wait for its stores of the round before
-    asm volatile("fence.acq_rel.cluster;" ::: "memory");
-    cluster_arrive();
-    cluster_wait();
+#pragma unroll 4
+    for (int r = 0; r < p.cl; ++r) store_in_cluster(&slots[own * LANES + at.lane], bar, r, whole);
+    mbar_wait_warp(bar, (round >> 1) & 1, &sh.gone, p.status);
   }
   float2 start = s;
-#pragma unroll 4
-  for (int r = 0; r < blocks; ++r) {
-    if (r == own) start = s;
-    s = lr_apply(lr_unpack(slots[r * LANES + at.lane]), s);
+  for (int r0 = 0; r0 < blocks; r0 += BATCH) {
+    float4 m[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) m[i] = slots[min(r0 + i, blocks - 1) * LANES + at.lane];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      if (r0 + i == own) start = s;
+      if (r0 + i < blocks) s = lr_apply(lr_unpack(m[i]), s);
+    }
   }
   return start;
 }
-// for the other warps: they arrive at once and wait with the rest
-__device__ __forceinline__ void lr_stand_by(const LrArgs& p) {
+// before the first round: the barriers, known to the cluster before anyone sends
+template <int CH, int NS>
+__device__ __forceinline__ void lr_open(LrShared<CH, NS>& sh, const LrArgs& p) {
+  if (threadIdx.x == 0) {
+    sh.gone = 0;
+    mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[0]), 1);
+    mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[1]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (p.cl > 1) cluster_arrive();
+}
+// no CTA leaves while another one may still send to it (after a wait that ran out)
+__device__ __forceinline__ void lr_close(const LrArgs& p) {
   if (p.cl == 1) return;
   cluster_arrive();
   cluster_wait();
@@ -265,7 +301,7 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
   LrShared<CH, 2>& sh = *reinterpret_cast<LrShared<CH, 2>*>(smem);
   const LrPlace<CH> at(p);
   constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
-  if (p.cl > 1) cluster_arrive();                        // every CTA has started before another one writes to its shared memory
+  lr_open(sh, p);
   lr_copy_table(sh);
   grid_dep();
   const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per, step = per * LR_BLOCK;
@@ -309,11 +345,10 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
       const float2 start = lr_hand_over(sh, p, at, k, 0, chunks, min(per, p.nb - k * per), s);
       sh.start[threadIdx.x] = start;
       if (p.save && chunks > 0 && at.have) *reinterpret_cast<float2*>(p.save + ((size_t)at.b * p.nb + blk) * p.D + ch) = start;
-    } else {
-      lr_stand_by(p);
     }
     copies_done();
     __syncthreads();
+    if (sh.gone) break;
     float2 h = sh.start[at.blk * LANES + at.lane];
     if (at.k) h = lr_apply(lr_unpack(sh.chunk[threadIdx.x]), h);
     uint16_t* out = p.y + ((size_t)at.b * p.S + t0) * p.ld_y + ch;
@@ -325,6 +360,8 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
     }
     __syncwarp();
   }
+  copies_done();
+  lr_close(p);
   if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
@@ -334,7 +371,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
   LrShared<CH, 3>& sh = *reinterpret_cast<LrShared<CH, 3>*>(smem);
   const LrPlace<CH> at(p);
   constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
-  if (p.cl > 1) cluster_arrive();
+  lr_open(sh, p);
   lr_copy_table(sh);
   grid_dep();
   const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per;
@@ -393,15 +430,13 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
     if (warp == 0) {
       const int b = top - own, have = b < 0 ? 0 : min(LR_CHUNKS, (p.S - b * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK);
       sh.start[threadIdx.x] = lr_hand_over(sh, p, at, r, have ? LR_CHUNKS - have : 0, have, min(per, p.nb - r * per), s);
-    } else {
-      if (warp == 1) {
-        lr_scan<LANES>(sh.ahead + own * LR_CHUNKS * LANES + at.lane, LR_CHUNKS);
-        sh.state[threadIdx.x & 31] = front;
-      }
-      lr_stand_by(p);
+    } else if (warp == 1) {
+      lr_scan<LANES>(sh.ahead + own * LR_CHUNKS * LANES + at.lane, LR_CHUNKS);
+      sh.state[threadIdx.x & 31] = front;
     }
     copies_done();
     __syncthreads();
+    if (sh.gone) break;
     float2 h = sh.state[at.blk * LANES + at.lane], c = sh.start[at.blk * LANES + at.lane];
     if (at.k) h = lr_apply(lr_unpack(sh.ahead[threadIdx.x]), h);
     if (at.k + 1 < chunks) c = lr_apply(lr_unpack(*place), c);
@@ -427,6 +462,8 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
     }
     __syncwarp();
   }
+  copies_done();
+  lr_close(p);
   if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
@@ -484,14 +521,16 @@ __global__ void __launch_bounds__(128) k_linrec_chunk(const __grid_constant__ Lr
   if (p.last) *reinterpret_cast<float2*>(p.last + at) = lr_apply(m, s);
 }
 
-// The strip and the cluster: narrower strips and larger clusters until CTAs cover the GPU `waves` times, no more CTAs than there are blocks.
+// The strip and the cluster: narrow strips, then larger clusters, while their CTAs are all on the GPU at once (`per_sm` of them on an SM), no more CTAs
+// than there are blocks.  Clusters do not fill the GPU: of 444 CTAs, three on an SM, 416 fit in clusters of 4, 384 in clusters of 8, 336 in
+// clusters of 16, and a round of 65536 x 512 that needed 256 of 224 took twice as long.
 struct LrPlan { int ch, cl; };
-static LrPlan lr_plan(int B, int D, int nb, int waves) {
-  const long long room = (long long)waves * dev_sm_count();
+static LrPlan lr_plan(int B, int D, int nb, int per_sm) {
+  const long long slots = (long long)per_sm * dev_sm_count();
   LrPlan q = {64, 1};
   auto chains = [&](int ch) { return (long long)B * ((D + ch - 1) / ch); };
-  if (nb > 1 && chains(32) <= room) q.ch = 32;
-  while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= room) q.cl *= 2;
+  if (nb > 1 && chains(32) <= slots) q.ch = 32;
+  while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= (q.cl == 8 ? slots * 3 / 4 : slots * 6 / 7)) q.cl *= 2;
   return q;
 }
 static int lr_launch(void (*kern)(const LrArgs), const LrArgs& p, int B, size_t smem, size_t most, DevOnce& once, cudaStream_t st) {
@@ -570,7 +609,7 @@ extern "C" size_t det_linrec_state_floats(int B, int S, int D) {
 }
 
 extern "C" int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, det_bf16* y, int ld_y, const uint8_t* flags,
-                              const float* h0, float* hT, float* states, void* stream) {
+                              const float* h0, float* hT, float* states, void* stream, int* status_dev) {
   const int rc = lr_check(g, v, ld, B, S, D);
   if (rc != DET_OK) return rc;
   if (!y || ld_y < D) return DET_ERR_ARG;
@@ -579,14 +618,14 @@ extern "C" int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int 
   cudaStream_t st = (cudaStream_t)stream;
   if (B == 0 || S == 0) return lr_empty(h0, hT, (size_t)B * D, st);
   LrArgs p = {};
-  p.g = g; p.v = v; p.flags = flags; p.first = h0; p.y = y; p.last = hT; p.save = states;
+  p.g = g; p.v = v; p.flags = flags; p.first = h0; p.y = y; p.last = hT; p.save = states; p.status = status_dev;
   p.ld = ld; p.ld_y = ld_y; p.S = S; p.D = D;
   return lr_any(false, p, B, st);
 }
 
 extern "C" int det_linrec_bwd(const det_bf16* dy, int ld_y, const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D,
                               const float* states, det_bf16* dg, det_bf16* dv, int ld_d, const uint8_t* flags, const float* dhT, float* dh0,
-                              void* stream) {
+                              void* stream, int* status_dev) {
   const int rc = lr_check(g, v, ld, B, S, D);
   if (rc != DET_OK) return rc;
   if (!dy || ld_y < D || !dg || !dv || ld_d < D || (!states && B > 0 && S > 0)) return DET_ERR_ARG;
@@ -595,7 +634,7 @@ extern "C" int det_linrec_bwd(const det_bf16* dy, int ld_y, const det_bf16* g, c
   cudaStream_t st = (cudaStream_t)stream;
   if (B == 0 || S == 0) return lr_empty(dhT, dh0, (size_t)B * D, st);
   LrArgs p = {};
-  p.g = g; p.v = v; p.dy = dy; p.flags = flags; p.first = dhT; p.states = states; p.dg = dg; p.dv = dv; p.last = dh0;
+  p.g = g; p.v = v; p.dy = dy; p.flags = flags; p.first = dhT; p.states = states; p.dg = dg; p.dv = dv; p.last = dh0; p.status = status_dev;
   p.ld = ld; p.ld_y = ld_y; p.ld_d = ld_d; p.S = S; p.D = D;
   return lr_any(true, p, B, st);
 }

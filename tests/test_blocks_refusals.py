@@ -82,14 +82,14 @@ def test_swiglu_act8_refusals():
 
 
 def test_linrec_refusals():
-    f = _with(dict(g=A, v=A, ld=128, B=2, S=9, D=64, y=A, ldy=64, fl=None, h0=None, hT=None, st=None, s=None))
+    f = _with(dict(g=A, v=A, ld=128, B=2, S=9, D=64, y=A, ldy=64, fl=None, h0=None, hT=None, st=None, s=None, status=None))
     for bad in (dict(g=None), dict(v=None), dict(y=None), dict(B=-1), dict(S=-1), dict(D=0), dict(ld=62), dict(ldy=62)):
         refused(ARG, "det_linrec_fwd", f(**bad))
     for bad in (dict(D=63), dict(ld=129), dict(ldy=65), dict(S=2 ** 30 + 1), dict(B=2 ** 30)):
         refused(SHAPE, "det_linrec_fwd", f(**bad))
     for bad in (dict(g=A + 2), dict(v=A + 2), dict(y=A + 2), dict(h0=A + 4), dict(hT=A + 4), dict(st=A + 4)):
         refused(ALIGN, "det_linrec_fwd", f(**bad))
-    b = _with(dict(dy=A, ldy=64, g=A, v=A, ld=128, B=2, S=9, D=64, st=A, dg=A, dv=A, ldd=128, fl=None, dhT=None, dh0=None, s=None))
+    b = _with(dict(dy=A, ldy=64, g=A, v=A, ld=128, B=2, S=9, D=64, st=A, dg=A, dv=A, ldd=128, fl=None, dhT=None, dh0=None, s=None, status=None))
     for bad in (dict(dy=None), dict(g=None), dict(dg=None), dict(dv=None), dict(st=None), dict(ldy=62), dict(ldd=62), dict(ld=62)):
         refused(ARG, "det_linrec_bwd", b(**bad))
     for bad in (dict(D=63), dict(ldd=129), dict(ldy=65)):
