@@ -109,7 +109,7 @@ struct LrDim {
 // NS: tensors that come in by asynchronous copies.  The block maps of the cluster, two rounds of them, lie behind this.
 template <int CH, int NS>
 struct __align__(16) LrShared {
-  uint32_t raw[2][NS][LrDim<CH>::RAW];                   // two rounds; [chunk of the CTA][row][lane]
+  uint32_t raw[NS == 3 ? 2 : 1][NS][LrDim<CH>::RAW];     // backward two rounds; [chunk of the CTA][row][lane]
   float tab[LR_TAB];
   float4 chunk[LR_T];                                    // [block of the CTA][chunk][lane]: the chunk maps of this round, then the maps of those before
   float4 ahead[NS == 3 ? LR_T : 1];                      // backward: the same of the recurrence itself
@@ -259,6 +259,13 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<CH, NS>& sh, const LrArg
     mbar_wait_warp(bar, (round >> 1) & 1, &sh.gone, p.status);
   }
   float2 start = s;
+  if (p.cl == 1) {
+    for (int r = 0; r < blocks; ++r) {
+      if (r == own) start = s;
+      s = lr_apply(lr_unpack(slots[r * LANES + at.lane]), s);
+    }
+    return start;
+  }
   for (int r0 = 0; r0 < blocks; r0 += BATCH) {
     float4 m[BATCH];
 #pragma unroll
@@ -296,7 +303,7 @@ __device__ __forceinline__ void lr_copy_table(LrShared<CH, NS>& sh) {
 }
 
 template <int CH, int WORDS, bool FLAGS>
-__global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
+__global__ void __launch_bounds__(LR_T, 4) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
   LrShared<CH, 2>& sh = *reinterpret_cast<LrShared<CH, 2>*>(smem);
   const LrPlace<CH> at(p);
@@ -309,13 +316,13 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
   const int ch = at.c0 + 2 * at.lane;
   const bool lead = threadIdx.x < 32;
   bool flag = false;
-  auto fetch = [&](int round, int row) {
-    lr_fetch<CH, WORDS>(sh.raw[round & 1][0], p.g, p.ld, p, at, row, LR_BLOCK);
-    lr_fetch<CH, WORDS>(sh.raw[round & 1][1], p.v, p.ld, p, at, row, LR_BLOCK);
+  auto fetch = [&](int row) {
+    lr_fetch<CH, WORDS>(sh.raw[0][0], p.g, p.ld, p, at, row, LR_BLOCK);
+    lr_fetch<CH, WORDS>(sh.raw[0][1], p.v, p.ld, p, at, row, LR_BLOCK);
     const int t = row + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK;
     flag = lr_flag<CH, FLAGS>(p, at, t, p.S - t);
   };
-  fetch(0, b0);
+  fetch(b0);
   float2 s = make_float2(0.0f, 0.0f);
   if (lead && p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + ch);
   copies_done();
@@ -324,8 +331,7 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
   for (int k = 0; k < rounds; ++k, b0 += step) {
     const int t0 = b0 + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK, n = p.S - t0;          // n rows of the chunk exist
     const uint32_t cuts = lr_cuts<CH, FLAGS>(flag);
-    if (k + 1 < rounds) fetch(k + 1, b0 + step);
-    const uint32_t* raw = sh.raw[k & 1][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
+    const uint32_t* raw = sh.raw[0][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
     float f[LR_CHUNK][2], u[LR_CHUNK][2];
     lr_gates(raw, LANES, sh.tab, f, u);
     raw += LrDim<CH>::RAW;
@@ -339,6 +345,7 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
     }
     sh.chunk[threadIdx.x] = lr_pack(mine);               // [block][chunk][lane] is the thread's number
     __syncthreads();
+    if (k + 1 < rounds) fetch(b0 + step);                // the raw values of this round are read
     if (lead) {
       const int row = b0 + (threadIdx.x / LANES) * LR_BLOCK, blk = row / LR_BLOCK;
       const int chunks = max(0, min(LR_CHUNKS, (p.S - row + LR_CHUNK - 1) / LR_CHUNK));
@@ -530,7 +537,7 @@ static LrPlan lr_plan(int B, int D, int nb, int per_sm) {
   LrPlan q = {64, 1};
   auto chains = [&](int ch) { return (long long)B * ((D + ch - 1) / ch); };
   if (nb > 1 && chains(32) <= slots) q.ch = 32;
-  while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= (q.cl == 8 ? slots * 3 / 4 : slots * 6 / 7)) q.cl *= 2;
+  while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= (q.cl == 8 ? slots * 3 / 4 : (q.cl > 1 ? slots * 6 / 7 : slots))) q.cl *= 2;
   return q;
 }
 static int lr_launch(void (*kern)(const LrArgs), const LrArgs& p, int B, size_t smem, size_t most, DevOnce& once, cudaStream_t st) {
@@ -579,7 +586,7 @@ static int lr_any(bool bwd, LrArgs& p, int B, cudaStream_t st) {
     DET_CHECK_LAUNCH();
     return DET_OK;
   }
-  const LrPlan q = lr_plan(B, p.D, p.nb, bwd ? 2 : 3);
+  const LrPlan q = lr_plan(B, p.D, p.nb, bwd ? 2 : 4);
   p.cl = q.cl;
   p.strips = (p.D + q.ch - 1) / q.ch;
   // whole pieces of 16 bytes where the tensors allow it
