@@ -148,7 +148,15 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
 // all of them, so the trees of dgamma and dbeta over the group's rows run in its own registers, the nodes of finished passes waiting
 // in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
 enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is: as dy, or the 8-bit checkpoint (dy bf16)
-template <int KIND, int WPR, bool VEC>
+// What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, LN_AHEAD passes of them.
+constexpr int LN_AHEAD = 2;
+template <int KIND, int WPR>
+struct LnFetch {
+  static constexpr int DY = KIND == LN_F32 ? 32 : 16, X = KIND == LN_F32 ? 32 : (KIND == LN_BF16 ? 16 : 8);
+  static constexpr int T = LnBwd<WPR>::THREADS, R = LnBwd<WPR>::ROWS;
+  static constexpr int ROW = T * (DY + X), ROW_RES = ROW + T * DY;                 // bytes of a row
+};
+template <int KIND, int WPR, bool VEC, bool RES>
 __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16 ? 2 : 1))
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
              const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int passes, const void* res,
@@ -156,45 +164,84 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
   grid_dep();
   constexpr bool BF = KIND != LN_F32;
   using S = LnBwd<WPR>;
-  constexpr int R = S::ROWS, T = S::THREADS;
-  extern __shared__ float waiting[];                      // [levels][16][T]
+  using Fx = LnFetch<KIND, WPR>;
+  constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW;
+  extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][16][T]
+  float* waiting = reinterpret_cast<float*>(smem + (VEC ? LN_AHEAD * R * BYTES : 0));
   __shared__ float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = (D & 255) == 0;
+  const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const long long r0 = ((long long)blockIdx.x * S::GROUPS + grp) * R * passes;
   if (partial && blockIdx.x == 0 && (int)threadIdx.x < 2 * ((D + 255) / 256)) tickets[threadIdx.x] = 0;   // for the kernel that follows
+  // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
+  float mu_next[R], rs_next[R], step_next[R];
+  auto fetch = [&](int p) {
+    if (VEC && p < passes) {
+      char* place = smem + (p % LN_AHEAD) * R * BYTES;
+#pragma unroll
+      for (int a = 0; a < R; ++a, place += BYTES) {
+        const long long row = r0 + (long long)p * R + a;
+        const bool there = row < rows && n > 0;
+        const size_t at = there ? (size_t)row * D + e0 : 0;
+        row_fetch<Fx::DY, T>(place, static_cast<const char*>(dy) + at * (BF ? 2 : 4), there);
+        row_fetch<Fx::X, T>(place + T * Fx::DY, static_cast<const char*>(x) + at * (KIND == LN_ACT8 ? 1 : (BF ? 2 : 4)), there);
+        if (RES) row_fetch<Fx::DY, T>(place + T * (Fx::DY + Fx::X), static_cast<const char*>(res) + at * (BF ? 2 : 4), there);
+      }
+    }
+    if (VEC) fetch_close();
+  };
+  auto statistics = [&](int p) {
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+      const long long row = r0 + (long long)p * R + a;
+      const bool there = p < passes && row < rows;
+      mu_next[a] = there ? mean[row] : 0.0f;
+      rs_next[a] = there ? rstd[row] : 0.0f;
+      if (KIND == LN_ACT8) step_next[a] = there && n > 0 ? a8_step(e8[(size_t)row * groups8 + e0 / A8_GROUP]) : 0.0f;
+    }
+  };
+#pragma unroll
+  for (int p = 0; p < LN_AHEAD - 1; ++p) fetch(p);
+  statistics(0);
   float g[8];
   if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
   float node[16];                                         // of this group's rows so far: 8 columns of dgamma, 8 of dbeta
 #pragma unroll 1
   for (int p = 0; p < passes; ++p) {
     const long long first = r0 + (long long)p * R;
-    float w[R][8], xh[R][8], rs[R];
+    float w[R][8], xh[R][8], rs[R], mu[R], step[R];
+#pragma unroll
+    for (int a = 0; a < R; ++a) { mu[a] = mu_next[a]; rs[a] = rs_next[a]; step[a] = KIND == LN_ACT8 ? step_next[a] : 0.0f; }
+    fetch(p + LN_AHEAD - 1);
+    statistics(p + 1);
+    if (VEC) fetch_wait<LN_AHEAD - 1>();
+    const char* place = smem + (p % LN_AHEAD) * R * BYTES;
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const long long row = first + a;
       const int m = row < rows ? n : 0;
-      load8n<BF, VEC>(dy, (size_t)row * D + e0, m, w[a]);
+      if (VEC) row_take<BF, T>(place + a * BYTES, w[a]);
+      else load8n<BF, false>(dy, (size_t)row * D + e0, m, w[a]);
       if (KIND == LN_ACT8) {
-        const int8_t* q = reinterpret_cast<const int8_t*>(x) + (size_t)row * D + e0;
-        const float step = m > 0 ? a8_step(e8[(size_t)row * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP]) : 0.0f;
         uint2 c = make_uint2(0, 0);
         if (VEC) {
-          if (m > 0) c = *reinterpret_cast<const uint2*>(q);
+          c = reinterpret_cast<const uint2*>(place + a * BYTES + T * Fx::DY)[threadIdx.x];
         } else {
+          const int8_t* q = reinterpret_cast<const int8_t*>(x) + (size_t)row * D + e0;
 #pragma unroll
           for (int t = 0; t < 8; ++t)
             if (t < m) (t < 4 ? c.x : c.y) |= (uint32_t)(uint8_t)q[t] << (8 * (t & 3));
         }
-        a8_values8(c, step, xh[a]);
+        a8_values8(c, step[a], xh[a]);
+      } else if (VEC) {
+        row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
       } else {
-        load8n<BF, VEC>(x, (size_t)row * D + e0, m, xh[a]);
+        load8n<BF, false>(x, (size_t)row * D + e0, m, xh[a]);
       }
-      rs[a] = row < rows ? rstd[row] : 0.0f;
-      const float mu = row < rows ? mean[row] : 0.0f;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu), rs[a]);
+      for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu[a]), rs[a]);
     }
     if (partial) {   // rows in pairs, pairs in pairs; a right node exists iff its first row does, else the left one is carried up unchanged
 #pragma unroll
@@ -242,9 +289,10 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
       float o[8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
-      if (res) {   // the gradient that bypasses the norm (res may be dx)
+      if (RES) {   // the gradient that bypasses the norm (res may be dx)
         float b[8];
-        load8n<BF, VEC>(res, at, m, b);
+        if (VEC) row_take<BF, T>(place + a * BYTES + T * (Fx::DY + Fx::X), b);
+        else load8n<BF, false>(res, at, m, b);
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = fadd(b[t], o[t]);
       }
@@ -348,10 +396,11 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
 }
 
 // Rows a CTA of the backward pass takes: a multiple of what it has in flight, more of it while the grid still covers the GPU (each halving of
-// the nodes saves the second kernel half its reading), at most 8 passes (three levels of waiting nodes, 48 KiB).
-static int ln_passes(int rows, int per) {
+// the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
+constexpr int ln_levels(int threads) { return threads <= 512 ? 2 : 1; }
+static int ln_passes(int rows, int D, int per) {
   int passes = 1;
-  while (passes < 8 && (long long)rows > (long long)passes * 2 * per * 444) passes *= 2;
+  while (passes < (1 << ln_levels(D <= 4096 ? 512 : 1024)) && (long long)rows > (long long)passes * 2 * per * 444) passes *= 2;
   return passes;
 }
 static int ln_rows_in_flight(int D) {
@@ -363,7 +412,7 @@ template <int KIND>
 static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
                   const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
   const bool cols = dgamma || dbeta;
-  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, per), stride = per * passes;
+  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, D, per), stride = per * passes;
   const int nb = (int)(((long long)rows + stride - 1) / stride), nu = (nb + 31) / 32;
   float* partial = cols ? (float*)ws : nullptr;
   float* upper = cols ? partial + 2 * (size_t)nb * D : nullptr;
@@ -371,19 +420,24 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
   int rc = DET_OK;
   with_wpr(D, [&](auto wpr) {
     with_bool(D % 8 == 0, [&](auto is_vec) {
-      constexpr int W = decltype(wpr)::value;
-      using S = LnBwd<W>;
-      int levels = 0;
-      while ((1 << levels) < passes) ++levels;
-      if (S::GROUPS > 1 && levels == 0) levels = 1;
-      const size_t smem = cols ? (size_t)levels * 16 * S::THREADS * sizeof(float) : 0;
-      auto kern = k_ln_bwd<KIND, W, decltype(is_vec)::value>;
-      if (smem > 40 * 1024) {
-        static DevOnce once;
-        rc = dev_ensure_smem(once, (const void*)kern, (size_t)3 * 16 * S::THREADS * sizeof(float));
-        if (rc != DET_OK) return;
-      }
-      launch_after(kern, dim3(nb), S::THREADS, smem, st, dy, x, e8, gamma, mean, rstd, rows, D, (float)(1.0 / (double)D), passes, res, dx, partial, tickets);
+      with_bool(res != nullptr, [&](auto is_res) {
+        constexpr int W = decltype(wpr)::value;
+        constexpr bool VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
+        if constexpr (!(RES && KIND == LN_F32)) {
+          using S = LnBwd<W>;
+          int levels = 0;
+          while ((1 << levels) < passes) ++levels;
+          if (S::GROUPS > 1 && levels == 0) levels = 1;
+          const size_t ahead = VEC ? (size_t)LN_AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
+          const size_t level = (size_t)16 * S::THREADS * sizeof(float);
+          auto kern = k_ln_bwd<KIND, W, VEC, RES>;
+          static DevOnce once;
+          rc = dev_ensure_smem(once, (const void*)kern, ahead + ln_levels(S::THREADS) * level);
+          if (rc != DET_OK) return;
+          launch_after(kern, dim3(nb), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D, (float)(1.0 / (double)D),
+                       passes, res, dx, partial, tickets);
+        }
+      });
     });
   });
   if (rc != DET_OK) return rc;
@@ -422,7 +476,7 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
 
 extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
   if (rows <= 0 || D <= 0 || D > 8192) return 256;
-  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, per);
+  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, D, per);
   const size_t nb = ((size_t)rows + stride - 1) / stride, nu = (nb + 31) / 32;
   return align_up(2 * (nb + nu) * (size_t)D * sizeof(float), 256) + 256;
 }

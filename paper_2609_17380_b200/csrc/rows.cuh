@@ -55,6 +55,39 @@ __device__ __forceinline__ void store8n(void* p, size_t idx, int n, const float 
   }
 }
 
+// ---- values on their way: asynchronous copies into a place of the thread's own, so that nothing but the thread waits for them -----------
+// BYTES of eight adjacent values: 16 (bf16), 32 (f32), 8 (codes); `there` false: zeros, the address is not followed.  A CTA of T threads has
+// T * BYTES bytes a row.
+template <int BYTES, int T>
+__device__ __forceinline__ void row_fetch(char* place, const void* src, bool there) {
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(place);
+  if (BYTES == 8) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + threadIdx.x * 8), "l"(src), "r"(there ? 8 : 0) : "memory");
+  } else {
+#pragma unroll
+    for (int h = 0; h < BYTES / 16; ++h)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (h * T + threadIdx.x) * 16), "l"(static_cast<const char*>(src) + h * 16),
+                   "r"(there ? 16 : 0)
+                   : "memory");
+  }
+}
+__device__ __forceinline__ void fetch_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void fetch_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+template <bool BF, int T>
+__device__ __forceinline__ void row_take(const char* place, float v[8]) {
+  const uint4* q = reinterpret_cast<const uint4*>(place) + threadIdx.x;
+  const uint4 a = q[0];
+  if (BF) {
+    v[0] = bflo(a.x); v[1] = bfhi(a.x); v[2] = bflo(a.y); v[3] = bfhi(a.y);
+    v[4] = bflo(a.z); v[5] = bfhi(a.z); v[6] = bflo(a.w); v[7] = bfhi(a.w);
+  } else {
+    const uint4 b = q[T];
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  }
+}
+
 // ---- 8-bit checkpoints -----------------------------------------------------------------------------------
 // A group is 32 adjacent values of a row.  Its step is the smallest power of two 2^E, at least 2^-126, with max|v| <= 127 * 2^E, kept as
 // its binary32 exponent field E + 127 (1 .. 249); code = rne(v / 2^E) in -127 .. 127.  With a power of two every product here is exact:
