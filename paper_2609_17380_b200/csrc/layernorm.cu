@@ -14,24 +14,50 @@
 namespace det {
 
 // A row is held by WPR warps, a leaf of 256 columns each, eight adjacent columns a lane.  WPR < 8: a CTA of eight warps has 8 / WPR such groups,
-// with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are in flight at a time.
-template <int WPR, bool BF>
+// with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are worked on at a time (backward one where 32 warps hold a row: there
+// are 64 registers a thread).
+template <int WPR>
 struct LnShape {
-  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS;
-  static constexpr int ROWS = WPR == 32 ? 1 : (WPR == 16 || !BF ? 2 : 4);
-  static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : 4);
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = 2, CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : 4);
 };
 template <int WPR>
-using LnBwd = LnShape<WPR, false>;   // backward: two rows in flight (one where 32 warps hold a row): two tensors, and dx beside them
+struct LnBwd {
+  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
+};
 
-// The row's tree over its WPR leaf sums (in shared memory, one barrier back); a leaf beyond D does not exist.
+// The tree over N nodes of which the first `have` exist (at least one); all of them in the usual case, without a test.
+template <int N>
+__device__ __forceinline__ float node_tree(float (&v)[N], int have) {
+  if (have >= N) {
+#pragma unroll
+    for (int w = 1; w < N; w <<= 1)
+#pragma unroll
+      for (int j = 0; j < N; j += 2 * w) v[j] = fadd(v[j], v[j + w]);
+  } else {
+#pragma unroll
+    for (int w = 1; w < N; w <<= 1)
+#pragma unroll
+      for (int j = 0; j < N; j += 2 * w) v[j] = j + w < have ? fadd(v[j], v[j + w]) : v[j];
+  }
+  return v[0];
+}
+// The row's tree over its WPR leaf sums (in shared memory, one barrier back); a leaf beyond D does not exist.  (The tests for existence in 64 bits and
+// in every place cost as many instructions as the rest of the kernels.)
 template <int WPR>
-__device__ __forceinline__ float row_tree(const float* leaf, int D) {
+__device__ __forceinline__ float row_tree(const float* leaf, int leaves) {
   if (WPR <= 8) {
     float L[WPR];
+    if (WPR >= 4) {
 #pragma unroll
-    for (int j = 0; j < WPR; ++j) L[j] = leaf[j];
-    return reg_tree<WPR>(L, 0, 256, D);
+      for (int j = 0; j < WPR / 4; ++j) {
+        const float4 q = reinterpret_cast<const float4*>(leaf)[j];
+        L[4 * j] = q.x; L[4 * j + 1] = q.y; L[4 * j + 2] = q.z; L[4 * j + 3] = q.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < WPR; ++j) L[j] = leaf[j];
+    }
+    return node_tree<WPR>(L, leaves);
   }
   const int lane = threadIdx.x & 31;
   float v = leaf[lane % WPR];
@@ -39,7 +65,7 @@ __device__ __forceinline__ float row_tree(const float* leaf, int D) {
   for (int w = 1; w < WPR; w <<= 1) {
     const float o = __shfl_xor_sync(0xffffffffu, v, w);
     const int right = ((lane % WPR) | w) & ~(w - 1);
-    v = right * 256 < D ? fadd(v, o) : ((lane & w) ? o : v);
+    v = right < leaves ? fadd(v, o) : ((lane & w) ? o : v);
   }
   return v;
 }
@@ -49,97 +75,127 @@ __device__ __forceinline__ float leaf_tree(const float v[8], int warp, int e0, i
   return warp_tree(VEC ? tree8_full(v) : tree8(v, e0, D), (long long)warp * 256, 8, D);
 }
 
-template <bool BF, int WPR, bool VEC>
-__global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::CTAS)
+// Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (LN_FWD_AHEAD passes, each thread its own
+// columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
+// stream).
+constexpr int LN_FWD_AHEAD = 3;
+template <bool BF, int WPR, bool VEC, bool RES>
+__global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
     k_ln_fwd(const void* __restrict__ x, const void* __restrict__ res, const void* __restrict__ gamma, const void* __restrict__ beta,
              int rows, int D, float eps, float invD, void* __restrict__ sum, void* __restrict__ y, float* __restrict__ mean,
              float* __restrict__ rstd, const float* __restrict__ s_q, int8_t* __restrict__ qy, int8_t* __restrict__ q8,
              uint8_t* __restrict__ e8) {
   grid_dep();
-  using S = LnShape<WPR, BF>;
-  constexpr int R = S::ROWS;
-  __shared__ float leaf_s[S::GROUPS][2][R][WPR];
+  using S = LnShape<WPR>;
+  constexpr int R = S::ROWS, T = S::THREADS, EL = BF ? 2 : 4, BYTES = T * 8 * EL * (RES ? 2 : 1);      // BYTES: a row on its way
+  extern __shared__ __align__(16) char smem[];
+  __shared__ __align__(16) float leaf_s[S::GROUPS][2][R][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = (D & 255) == 0;
-  const long long first = ((long long)blockIdx.x * S::GROUPS + grp) * R;
-  float v[R][8];
+  const int leaves = (D + 255) >> 8;
+  const int stride = gridDim.x * S::GROUPS * R;
+  auto fetch = [&](int first, int slot) {
+    if (VEC) {
+      if (first < rows) {
+        char* place = smem + slot * R * BYTES;
 #pragma unroll
-  for (int a = 0; a < R; ++a) load8n<BF, VEC>(x, (size_t)(first + a) * D + e0, first + a < rows ? n : 0, v[a]);
-  if (res) {   // the residual sum in front of the norm: rounded and stored, and the rounded one is what is normalised
-#pragma unroll
-    for (int a = 0; a < R; ++a) {
-      const int m = first + a < rows ? n : 0;
-      float b[8];
-      load8n<BF, VEC>(res, (size_t)(first + a) * D + e0, m, b);
-#pragma unroll
-      for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], b[t]);
-      store8n<BF, VEC>(sum, (size_t)(first + a) * D + e0, m, v[a]);
-      if (BF) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v[a][t] = bf2f(f2bf(v[a][t]));
+        for (int a = 0; a < R; ++a, place += BYTES) {
+          const bool there = first + a < rows && n > 0;
+          const size_t at = there ? ((size_t)(first + a) * D + e0) * EL : 0;
+          row_fetch<8 * EL, T>(place, static_cast<const char*>(x) + at, there);
+          if (RES) row_fetch<8 * EL, T>(place + T * 8 * EL, static_cast<const char*>(res) + at, there);
+        }
       }
+      fetch_close();
     }
-  }
-  if (BF && VEC && q8) {   // the checkpoint of what is normalised
+  };
+  int first = (blockIdx.x * S::GROUPS + grp) * R;
 #pragma unroll
-    for (int a = 0; a < R; ++a) {
-      const uint32_t field = a8_field(a8_quad_max(a8_amax8(v[a])));
-      if (first + a < rows && n > 0) {
-        *reinterpret_cast<uint2*>(q8 + (size_t)(first + a) * D + e0) = a8_codes8(v[a], field);
-        if ((lane & 3) == 0) e8[(size_t)(first + a) * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP] = (uint8_t)field;
-      }
-    }
-  }
-#pragma unroll
-  for (int a = 0; a < R; ++a) {
-    const float s = leaf_tree<VEC>(v[a], warp, e0, D, full);
-    if (lane == 0) leaf_s[grp][0][a][warp] = s;
-  }
-  __syncthreads();
-  float mu[R];
-#pragma unroll
-  for (int a = 0; a < R; ++a) {
-    mu[a] = fmul(row_tree<WPR>(leaf_s[grp][0][a], D), invD);
-    float sq[8];
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      v[a][t] = fsub(v[a][t], mu[a]);
-      sq[t] = fmul(v[a][t], v[a][t]);
-    }
-    const float s = leaf_tree<VEC>(sq, warp, e0, D, full);
-    if (lane == 0) leaf_s[grp][1][a][warp] = s;
-  }
+  for (int k = 0; k < LN_FWD_AHEAD - 1; ++k) fetch(first + k * stride, k);
   float g[8], b[8];
   if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
   if (beta) load8n<BF, VEC>(beta, e0, n, b);
   const float inv_q = (BF && VEC && qy) ? fdiv(1.0f, s_q[0]) : 0.0f;
-  __syncthreads();
-#pragma unroll
-  for (int a = 0; a < R; ++a) {
-    const float rs = fdiv(1.0f, fsqrt(fadd(fmul(row_tree<WPR>(leaf_s[grp][1][a], D), invD), eps)));
-    if (first + a >= rows) continue;
-    if (warp == 0 && lane == 0) {
-      mean[first + a] = mu[a];
-      rstd[first + a] = rs;
+  // all groups of the CTA make the same passes
+  for (int base = blockIdx.x * S::GROUPS * R, slot = 0; base < rows; base += stride, first += stride) {
+    float v[R][8];
+    if (VEC) {
+      const int next = slot == 0 ? LN_FWD_AHEAD - 1 : slot - 1;
+      fetch(first + (LN_FWD_AHEAD - 1) * stride, next);
+      fetch_wait<LN_FWD_AHEAD - 1>();
     }
-    float o[8];
+    const char* place = smem + slot * R * BYTES;
+    slot = slot + 1 == LN_FWD_AHEAD ? 0 : slot + 1;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) o[t] = fmul(v[a][t], rs);
-    if (gamma) {
+    for (int a = 0; a < R; ++a) {
+      const int m = first + a < rows ? n : 0;
+      const size_t at = (size_t)(first + a) * D + e0;
+      if (VEC) row_take<BF, T>(place + a * BYTES, v[a]);
+      else load8n<BF, false>(x, at, m, v[a]);
+      if (RES) {   // the residual sum in front of the norm: rounded and stored, and the rounded one is what is normalised
+        float c[8];
+        if (VEC) row_take<BF, T>(place + a * BYTES + T * 8 * EL, c);
+        else load8n<BF, false>(res, at, m, c);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = fmul(o[t], g[t]);
+        for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], c[t]);
+        store8n<BF, VEC>(sum, at, m, v[a]);
+        if (BF) {
+#pragma unroll
+          for (int t = 0; t < 8; ++t) v[a][t] = bf2f(f2bf(v[a][t]));
+        }
+      }
+      if (BF && VEC && q8) {   // the checkpoint of what is normalised
+        const uint32_t field = a8_field(a8_quad_max(a8_amax8(v[a])));
+        if (m > 0) {
+          *reinterpret_cast<uint2*>(q8 + at) = a8_codes8(v[a], field);
+          if ((lane & 3) == 0) e8[(size_t)(first + a) * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP] = (uint8_t)field;
+        }
+      }
+      const float s = leaf_tree<VEC>(v[a], warp, e0, D, full);
+      if (lane == 0) leaf_s[grp][0][a][warp] = s;
     }
-    if (beta) {
+    __syncthreads();
+    float mu[R];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
+    for (int a = 0; a < R; ++a) {
+      mu[a] = fmul(row_tree<WPR>(leaf_s[grp][0][a], leaves), invD);
+      float sq[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        v[a][t] = fsub(v[a][t], mu[a]);
+        sq[t] = fmul(v[a][t], v[a][t]);
+      }
+      const float s = leaf_tree<VEC>(sq, warp, e0, D, full);
+      if (lane == 0) leaf_s[grp][1][a][warp] = s;
     }
-    const size_t at = (size_t)(first + a) * D + e0;
-    store8n<BF, VEC>(y, at, n, o);
-    if (BF && VEC && qy && n > 0) {   // the next linear's quantiser, applied to the bf16 values just stored
+    __syncthreads();
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = bf2f(f2bf(o[t]));
-      *reinterpret_cast<uint2*>(qy + at) = quant8(o, inv_q);
+    for (int a = 0; a < R; ++a) {
+      const float rs = fdiv(1.0f, fsqrt(fadd(fmul(row_tree<WPR>(leaf_s[grp][1][a], leaves), invD), eps)));
+      if (first + a >= rows) continue;
+      if (warp == 0 && lane == 0) {
+        mean[first + a] = mu[a];
+        rstd[first + a] = rs;
+      }
+      float o[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = fmul(v[a][t], rs);
+      if (gamma) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[t] = fmul(o[t], g[t]);
+      }
+      if (beta) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
+      }
+      const size_t at = (size_t)(first + a) * D + e0;
+      store8n<BF, VEC>(y, at, n, o);
+      if (BF && VEC && qy && n > 0) {   // the next linear's quantiser, applied to the bf16 values just stored
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[t] = bf2f(f2bf(o[t]));
+        *reinterpret_cast<uint2*>(qy + at) = quant8(o, inv_q);
+      }
     }
   }
 }
@@ -148,80 +204,92 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
 // all of them, so the trees of dgamma and dbeta over the group's rows run in its own registers, the nodes of finished passes waiting
 // in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
 enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is: as dy, or the 8-bit checkpoint (dy bf16)
-// What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, LN_AHEAD passes of them.
-constexpr int LN_AHEAD = 2;
+// What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, AHEAD passes of them.  As many CTAs as the GPU holds walk
+// over the blocks of rows, so the loads go on across the blocks.
 template <int KIND, int WPR>
 struct LnFetch {
+  static constexpr int AHEAD = KIND == LN_F32 ? 2 : 3;
   static constexpr int DY = KIND == LN_F32 ? 32 : 16, X = KIND == LN_F32 ? 32 : (KIND == LN_BF16 ? 16 : 8);
   static constexpr int T = LnBwd<WPR>::THREADS, R = LnBwd<WPR>::ROWS;
   static constexpr int ROW = T * (DY + X), ROW_RES = ROW + T * DY;                 // bytes of a row
 };
 template <int KIND, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16 ? 2 : 1))
+__global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
-             const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int passes, const void* res,
+             const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int nb, int passes, const void* res,
              void* dx, float* __restrict__ partial, int* __restrict__ tickets) {
   grid_dep();
   constexpr bool BF = KIND != LN_F32;
   using S = LnBwd<WPR>;
   using Fx = LnFetch<KIND, WPR>;
-  constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW;
+  constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW, AHEAD = Fx::AHEAD;
   extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][16][T]
-  float* waiting = reinterpret_cast<float*>(smem + (VEC ? LN_AHEAD * R * BYTES : 0));
-  __shared__ float leaf_s[2][S::GROUPS][R][2][WPR];
+  float* waiting = reinterpret_cast<float*>(smem + (VEC ? AHEAD * R * BYTES : 0));
+  __shared__ __align__(16) float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = (D & 255) == 0;
+  const int leaves = (D + 255) >> 8;
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
-  const long long r0 = ((long long)blockIdx.x * S::GROUPS + grp) * R * passes;
+  const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
   if (partial && blockIdx.x == 0 && (int)threadIdx.x < 2 * ((D + 255) / 256)) tickets[threadIdx.x] = 0;   // for the kernel that follows
   // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
   float mu_next[R], rs_next[R], step_next[R];
-  auto fetch = [&](int p) {
-    if (VEC && p < passes) {
-      char* place = smem + (p % LN_AHEAD) * R * BYTES;
+  struct { int base, p, slot; } ahead = {(int)blockIdx.x * block, 0, 0};        // the pass to fetch next
+  auto fetch = [&]() {
+    if (VEC) {
+      if (ahead.base < rows) {
+        char* place = smem + ahead.slot * R * BYTES;
 #pragma unroll
-      for (int a = 0; a < R; ++a, place += BYTES) {
-        const long long row = r0 + (long long)p * R + a;
-        const bool there = row < rows && n > 0;
-        const size_t at = there ? (size_t)row * D + e0 : 0;
-        row_fetch<Fx::DY, T>(place, static_cast<const char*>(dy) + at * (BF ? 2 : 4), there);
-        row_fetch<Fx::X, T>(place + T * Fx::DY, static_cast<const char*>(x) + at * (KIND == LN_ACT8 ? 1 : (BF ? 2 : 4)), there);
-        if (RES) row_fetch<Fx::DY, T>(place + T * (Fx::DY + Fx::X), static_cast<const char*>(res) + at * (BF ? 2 : 4), there);
+        for (int a = 0; a < R; ++a, place += BYTES) {
+          const int row = ahead.base + mine + ahead.p * R + a;
+          const bool there = row < rows && n > 0;
+          const size_t at = there ? (size_t)row * D + e0 : 0;
+          row_fetch<Fx::DY, T>(place, static_cast<const char*>(dy) + at * (BF ? 2 : 4), there);
+          row_fetch<Fx::X, T>(place + T * Fx::DY, static_cast<const char*>(x) + at * (KIND == LN_ACT8 ? 1 : (BF ? 2 : 4)), there);
+          if (RES) row_fetch<Fx::DY, T>(place + T * (Fx::DY + Fx::X), static_cast<const char*>(res) + at * (BF ? 2 : 4), there);
+        }
       }
+      fetch_close();
+      ahead.slot = ahead.slot + 1 == AHEAD ? 0 : ahead.slot + 1;
+      if (++ahead.p == passes) { ahead.p = 0; ahead.base += stride; }
     }
-    if (VEC) fetch_close();
   };
-  auto statistics = [&](int p) {
+  auto statistics = [&](int first) {
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      const long long row = r0 + (long long)p * R + a;
-      const bool there = p < passes && row < rows;
+      const int row = first + a;
+      const bool there = row < rows;
       mu_next[a] = there ? mean[row] : 0.0f;
       rs_next[a] = there ? rstd[row] : 0.0f;
       if (KIND == LN_ACT8) step_next[a] = there && n > 0 ? a8_step(e8[(size_t)row * groups8 + e0 / A8_GROUP]) : 0.0f;
     }
   };
 #pragma unroll
-  for (int p = 0; p < LN_AHEAD - 1; ++p) fetch(p);
-  statistics(0);
+  for (int k = 0; k < AHEAD - 1; ++k) fetch();
+  statistics(blockIdx.x * block + mine);
   float g[8];
   if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
   float node[16];                                         // of this group's rows so far: 8 columns of dgamma, 8 of dbeta
+  int slot = 0;
+  bool odd = false;                                       // which half of leaf_s the pass uses
+#pragma unroll 1
+  for (int blk = blockIdx.x; blk < nb; blk += gridDim.x) {
+  const int r0 = blk * block + mine;
 #pragma unroll 1
   for (int p = 0; p < passes; ++p) {
-    const long long first = r0 + (long long)p * R;
+    const int first = r0 + p * R;
     float w[R][8], xh[R][8], rs[R], mu[R], step[R];
 #pragma unroll
     for (int a = 0; a < R; ++a) { mu[a] = mu_next[a]; rs[a] = rs_next[a]; step[a] = KIND == LN_ACT8 ? step_next[a] : 0.0f; }
-    fetch(p + LN_AHEAD - 1);
-    statistics(p + 1);
-    if (VEC) fetch_wait<LN_AHEAD - 1>();
-    const char* place = smem + (p % LN_AHEAD) * R * BYTES;
+    fetch();
+    statistics(p + 1 < passes ? first + R : r0 + stride);
+    if (VEC) fetch_wait<AHEAD - 1>();
+    const char* place = smem + slot * R * BYTES;
+    slot = slot + 1 == AHEAD ? 0 : slot + 1;
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      const long long row = first + a;
-      const int m = row < rows ? n : 0;
+      const int row = first + a, m = row < rows ? n : 0;
       if (VEC) row_take<BF, T>(place + a * BYTES, w[a]);
       else load8n<BF, false>(dy, (size_t)row * D + e0, m, w[a]);
       if (KIND == LN_ACT8) {
@@ -249,12 +317,12 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
         float c[R], d[R];
 #pragma unroll
         for (int a = 0; a < R; ++a) { c[a] = fmul(w[a][t], xh[a][t]); d[a] = w[a][t]; }
-        node[t] = reg_tree<R>(c, first, 1, rows);
-        node[8 + t] = reg_tree<R>(d, first, 1, rows);
+        node[t] = node_tree<R>(c, rows - first);
+        node[8 + t] = node_tree<R>(d, rows - first);
       }
       int level = 0;
       for (; (p >> level) & 1; ++level) {
-        const bool have = r0 + (long long)((p >> level) << level) * R < rows;
+        const bool have = r0 + ((p >> level) << level) * R < rows;
         float* l = waiting + (size_t)level * 16 * T + threadIdx.x;
 #pragma unroll
         for (int t = 0; t < 16; ++t) node[t] = have ? fadd(l[t * T], node[t]) : l[t * T];
@@ -271,7 +339,8 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
 #pragma unroll
         for (int t = 0; t < 8; ++t) w[a][t] = fmul(w[a][t], g[t]);
     }
-    float (*leaf)[2][WPR] = leaf_s[p & 1][grp];
+    float (*leaf)[2][WPR] = leaf_s[odd][grp];
+    odd = !odd;
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       float pr[8];
@@ -283,7 +352,7 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
     __syncthreads();
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      const float c1 = fmul(row_tree<WPR>(leaf[a][0], D), invD), c2 = fmul(row_tree<WPR>(leaf[a][1], D), invD);
+      const float c1 = fmul(row_tree<WPR>(leaf[a][0], leaves), invD), c2 = fmul(row_tree<WPR>(leaf[a][1], leaves), invD);
       const int m = first + a < rows ? n : 0;
       const size_t at = (size_t)(first + a) * D + e0;
       float o[8];
@@ -299,29 +368,34 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, WPR <= 8 ? 3 : (WPR == 16
       store8n<BF, VEC>(dx, at, m, o);
     }
   }
-  if (!partial) return;
+  if (!partial) continue;
   if (S::GROUPS > 1) {   // the tree over the groups' nodes
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 16; ++t) waiting[t * T + threadIdx.x] = node[t];
     __syncthreads();
-    if (grp) return;
+    if (grp == 0) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      float c[S::GROUPS];
+      for (int t = 0; t < 16; ++t) {
+        float c[S::GROUPS];
 #pragma unroll
-      for (int k = 0; k < S::GROUPS; ++k) c[k] = waiting[t * T + k * WPR * 32 + threadIdx.x];
-      node[t] = reg_tree<S::GROUPS>(c, r0, (long long)R * passes, rows);
+        for (int k = 0; k < S::GROUPS; ++k) c[k] = waiting[t * T + k * WPR * 32 + threadIdx.x];
+        node[t] = node_tree<S::GROUPS>(c, (rows - r0 + R * passes - 1) / (R * passes));
+      }
     }
+    __syncthreads();
   }
-  float* dst = partial + (size_t)blockIdx.x * D + e0;
-  store8n<false, VEC>(dst, 0, n, node);
-  store8n<false, VEC>(dst + (size_t)gridDim.x * D, 0, n, node + 8);
+  if (grp == 0) {
+    float* dst = partial + (size_t)blk * D + e0;
+    store8n<false, VEC>(dst, 0, n, node);
+    store8n<false, VEC>(dst + (size_t)nb * D, 0, n, node + 8);
+  }
+  }
 }
 
-// The trees over the row blocks (`stride` rows each) of every column of dgamma (z = 0) and dbeta (z = 1), 32 nodes a thread; the CTA
+// The trees over the nb row blocks of every column of dgamma (z = 0) and dbeta (z = 1), 32 nodes a thread; the CTA
 // that completes a block of 256 columns goes on to the levels above for those columns, as in the RMSNorm's gain gradient.
-__global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ partial, int nb, int stride, int rows, int D, float* __restrict__ upper,
+__global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ partial, int nb, int D, float* __restrict__ upper,
                                                  int nu, int* __restrict__ tickets, float* __restrict__ dgamma, float* __restrict__ dbeta) {
   __shared__ int last_s;
   const int col = blockIdx.x * 256 + threadIdx.x, z = blockIdx.z;
@@ -337,7 +411,7 @@ __global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ parti
       const int b = blockIdx.y * 32 + i;
       s[i] = b < nb ? partial[(size_t)b * D + col] : 0.0f;
     }
-    upper[(size_t)blockIdx.y * D + col] = reg_tree<32>(s, (long long)blockIdx.y * 32 * stride, stride, rows);
+    upper[(size_t)blockIdx.y * D + col] = node_tree<32>(s, nb - blockIdx.y * 32);
   }
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -348,17 +422,15 @@ __global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ parti
   __syncthreads();
   if (!last_s || col >= D) return;
   int n = nu;
-  long long st = 32ll * stride;
   while (n > 1) {
     const int groups = (n + 31) / 32;
     for (int gg = 0; gg < groups; ++gg) {
       float s[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) s[i] = gg * 32 + i < n ? __ldcg(&upper[(size_t)(gg * 32 + i) * D + col]) : 0.0f;
-      upper[(size_t)gg * D + col] = reg_tree<32>(s, (long long)gg * 32 * st, st, rows);
+      upper[(size_t)gg * D + col] = node_tree<32>(s, n - gg * 32);
     }
     n = groups;
-    st *= 32;
   }
   // the sum of one row is that row, carried up without an addition: flushed like every value that enters or leaves an operation
   const float r = __ldcg(&upper[col]);
@@ -378,29 +450,46 @@ static void with_wpr(int D, F f) {
 template <class F>
 static void with_bool(bool b, F f) { if (b) f(std::true_type()); else f(std::false_type()); }
 
+// CTAs for `blocks` pieces of work: all that are on the GPU at once, `per_sm` on an SM
+static dim3 ln_grid(long long blocks, int per_sm) {
+  const long long most = (long long)per_sm * dev_sm_count();
+  return dim3((unsigned)(blocks < most || most <= 0 ? blocks : most));
+}
 static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, const void* beta, int rows, int D, float eps, void* sum,
                   void* y, float* mean, float* rstd, const float* s_q, int8_t* qy, int8_t* q8, uint8_t* e8, cudaStream_t st) {
+  int rc = DET_OK;
   with_wpr(D, [&](auto wpr) {
     with_bool(bf, [&](auto is_bf) {
       with_bool(D % 8 == 0, [&](auto is_vec) {
-        constexpr int W = decltype(wpr)::value;
-        using S = LnShape<W, decltype(is_bf)::value>;
-        const int per = S::GROUPS * S::ROWS;
-        launch_after(k_ln_fwd<decltype(is_bf)::value, W, decltype(is_vec)::value>, dim3((unsigned)(((long long)rows + per - 1) / per)), S::THREADS, 0, st, x,
-                     res, gamma, beta, rows, D, eps, (float)(1.0 / (double)D), sum, y, mean, rstd, s_q, qy, q8, e8);
+        with_bool(res != nullptr, [&](auto is_res) {
+          constexpr int W = decltype(wpr)::value;
+          constexpr bool BF = decltype(is_bf)::value, VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
+          if constexpr (BF || !RES) {
+            using S = LnShape<W>;
+            const int per = S::GROUPS * S::ROWS;
+            const size_t smem = VEC ? (size_t)LN_FWD_AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : 0;
+            auto kern = k_ln_fwd<BF, W, VEC, RES>;
+            static DevOnce once;
+            if (smem > 40 * 1024) rc = dev_ensure_smem(once, (const void*)kern, smem);
+            if (rc != DET_OK) return;
+            launch_after(kern, ln_grid(((long long)rows + per - 1) / per, S::CTAS), S::THREADS, smem, st, x, res, gamma, beta, rows, D, eps,
+                         (float)(1.0 / (double)D), sum, y, mean, rstd, s_q, qy, q8, e8);
+          }
+        });
       });
     });
   });
+  if (rc != DET_OK) return rc;
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
 
-// Rows a CTA of the backward pass takes: a multiple of what it has in flight, more of it while the grid still covers the GPU (each halving of
-// the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
+// Rows of a block of the backward pass, whose node goes to memory: a multiple of what a CTA works on at a time, more of it while there are two blocks for
+// every CTA on the GPU (each halving of the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
 constexpr int ln_levels(int threads) { return threads <= 512 ? 2 : 1; }
 static int ln_passes(int rows, int D, int per) {
   int passes = 1;
-  while (passes < (1 << ln_levels(D <= 4096 ? 512 : 1024)) && (long long)rows > (long long)passes * 2 * per * 444) passes *= 2;
+  while (passes < (1 << ln_levels(D <= 4096 ? 512 : 1024)) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
   return passes;
 }
 static int ln_rows_in_flight(int D) {
@@ -428,24 +517,25 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
           int levels = 0;
           while ((1 << levels) < passes) ++levels;
           if (S::GROUPS > 1 && levels == 0) levels = 1;
-          const size_t ahead = VEC ? (size_t)LN_AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
+          const size_t ahead = VEC ? (size_t)LnFetch<KIND, W>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
           const size_t level = (size_t)16 * S::THREADS * sizeof(float);
           auto kern = k_ln_bwd<KIND, W, VEC, RES>;
           static DevOnce once;
           rc = dev_ensure_smem(once, (const void*)kern, ahead + ln_levels(S::THREADS) * level);
           if (rc != DET_OK) return;
-          launch_after(kern, dim3(nb), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D, (float)(1.0 / (double)D),
-                       passes, res, dx, partial, tickets);
+          launch_after(kern, ln_grid(nb, S::CTAS), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
+                       (float)(1.0 / (double)D), nb, passes, res, dx, partial, tickets);
         }
       });
     });
   });
   if (rc != DET_OK) return rc;
   if (cols)
-    launch_after(k_ln_cols, dim3((D + 255) / 256, nu, 2), 256, 0, st, (const float*)partial, nb, stride, rows, D, upper, nu, tickets, dgamma, dbeta);
+    launch_after(k_ln_cols, dim3((D + 255) / 256, nu, 2), 256, 0, st, (const float*)partial, nb, D, upper, nu, tickets, dgamma, dbeta);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
+constexpr int LN_ROWS = 2000000000;         // so that the rows of the last CTA have numbers too
 static bool elem_aligned(const void* p, int D, size_t elem) { return (uintptr_t)p % (D % 8 == 0 ? 16 : elem) == 0; }
 
 }  // namespace det
@@ -455,7 +545,7 @@ using namespace det;
 extern "C" int det_layernorm_fwd(int io, const void* x, const void* gamma, const void* beta, int rows, int D, float eps, void* y, float* mean,
                                  float* rstd, void* stream) {
   if (!x || !y || !mean || !rstd || rows < 0 || D <= 0 || (io != DET_F32 && io != DET_BF16)) return DET_ERR_ARG;
-  if (D > 8192) return DET_ERR_SHAPE;
+  if (D > 8192 || rows > LN_ROWS) return DET_ERR_SHAPE;
   const size_t el = io == DET_BF16 ? 2 : 4;
   if (!elem_aligned(x, D, el) || !elem_aligned(y, D, el) || !elem_aligned(gamma, D, el) || !elem_aligned(beta, D, el)) return DET_ERR_ALIGN;
   if (rows == 0) return DET_OK;
@@ -466,7 +556,7 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
                                           float eps, det_bf16* sum, det_bf16* y, float* mean, float* rstd, const float* s_q, int8_t* qy,
                                           int8_t* q8, uint8_t* e8, void* stream) {
   if (!a || (b && !sum) || !y || !mean || !rstd || (qy && !s_q) || (!q8 != !e8) || rows < 0 || D <= 0) return DET_ERR_ARG;
-  if (D > 8192 || (D % 8 && (qy || q8))) return DET_ERR_SHAPE;
+  if (D > 8192 || rows > LN_ROWS || (D % 8 && (qy || q8))) return DET_ERR_SHAPE;
   if (!elem_aligned(a, D, 2) || !elem_aligned(b, D, 2) || !elem_aligned(gamma, D, 2) || !elem_aligned(beta, D, 2) ||
       (b && !elem_aligned(sum, D, 2)) || !elem_aligned(y, D, 2) || (((uintptr_t)qy | (uintptr_t)q8) & 7u))
     return DET_ERR_ALIGN;
@@ -486,7 +576,7 @@ template <int KIND>
 static int ln_bwd_entry(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
                         const void* res, void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, cudaStream_t st) {
   if (!dy || !x || !mean || !rstd || !dx || rows < 0 || D <= 0) return DET_ERR_ARG;
-  if (D > 8192) return DET_ERR_SHAPE;
+  if (D > 8192 || rows > LN_ROWS) return DET_ERR_SHAPE;
   const size_t el = KIND == LN_F32 ? 4 : 2;
   if (!elem_aligned(dy, D, el) || !elem_aligned(dx, D, el) || !elem_aligned(gamma, D, el) || !elem_aligned(res, D, el)) return DET_ERR_ALIGN;
   if (KIND == LN_ACT8 ? (D % 8 == 0 && ((uintptr_t)x & 7u)) : !elem_aligned(x, D, el)) return DET_ERR_ALIGN;
