@@ -16,13 +16,14 @@ namespace det {
 // A row is held by WPR warps, a leaf of 256 columns each, eight adjacent columns a lane.  WPR < 8: a CTA of eight warps has 8 / WPR such groups,
 // with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are worked on at a time (backward one where 32 warps hold a row: there
 // are 64 registers a thread).
-template <int WPR>
+template <int WPR, bool BF>
 struct LnShape {
-  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = 2, CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : 4);
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = BF && WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
+  static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
 };
 template <int WPR>
 struct LnBwd {
-  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
+  static constexpr int GROUPS = LnShape<WPR, false>::GROUPS, THREADS = LnShape<WPR, false>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
 };
 
 // The tree over N nodes of which the first `have` exist (at least one); all of them in the usual case, without a test.
@@ -69,24 +70,36 @@ __device__ __forceinline__ float row_tree(const float* leaf, int leaves) {
   }
   return v;
 }
+// The trees of N rows (or of two sums of rows) at `leaf`, N a power of two, dealt out over the lanes: lane l has row l mod N.  Every thread needs all of
+// them, and each is a dozen instructions, the root and the division behind the second one forty more.
+template <int N, int WPR>
+__device__ __forceinline__ float dealt_tree(const float* leaf, int leaves) {
+  if (WPR <= 8) return row_tree<WPR>(leaf + (threadIdx.x % N) * WPR, leaves);
+  float r = 0.0f;                                        // wide rows: the lanes share each tree
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float v = row_tree<WPR>(leaf + j * WPR, leaves);
+    if (threadIdx.x % N == j) r = v;
+  }
+  return r;
+}
 template <bool VEC>
 __device__ __forceinline__ float leaf_tree(const float v[8], int warp, int e0, int D, bool full) {
   if (full) return warp_tree_full(tree8_full(v));
   return warp_tree(VEC ? tree8_full(v) : tree8(v, e0, D), (long long)warp * 256, 8, D);
 }
 
-// Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (LN_FWD_AHEAD passes, each thread its own
+// Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (AHEAD passes, each thread its own
 // columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
 // stream).
-constexpr int LN_FWD_AHEAD = 3;
 template <bool BF, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
+__global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::CTAS)
     k_ln_fwd(const void* __restrict__ x, const void* __restrict__ res, const void* __restrict__ gamma, const void* __restrict__ beta,
              int rows, int D, float eps, float invD, void* __restrict__ sum, void* __restrict__ y, float* __restrict__ mean,
              float* __restrict__ rstd, const float* __restrict__ s_q, int8_t* __restrict__ qy, int8_t* __restrict__ q8,
              uint8_t* __restrict__ e8) {
   grid_dep();
-  using S = LnShape<WPR>;
+  using S = LnShape<WPR, BF>;
   constexpr int R = S::ROWS, T = S::THREADS, EL = BF ? 2 : 4, BYTES = T * 8 * EL * (RES ? 2 : 1);      // BYTES: a row on its way
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float leaf_s[S::GROUPS][2][R][WPR];
@@ -102,7 +115,7 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
 #pragma unroll
         for (int a = 0; a < R; ++a, place += BYTES) {
           const bool there = first + a < rows && n > 0;
-          const size_t at = there ? ((size_t)(first + a) * D + e0) * EL : 0;
+          const size_t at = there ? row_at(first + a, D, e0) * EL : 0;
           row_fetch<8 * EL, T>(place, static_cast<const char*>(x) + at, there);
           if (RES) row_fetch<8 * EL, T>(place + T * 8 * EL, static_cast<const char*>(res) + at, there);
         }
@@ -112,7 +125,7 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
   };
   int first = (blockIdx.x * S::GROUPS + grp) * R;
 #pragma unroll
-  for (int k = 0; k < LN_FWD_AHEAD - 1; ++k) fetch(first + k * stride, k);
+  for (int k = 0; k < S::AHEAD - 1; ++k) fetch(first + k * stride, k);
   float g[8], b[8];
   if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
   if (beta) load8n<BF, VEC>(beta, e0, n, b);
@@ -121,16 +134,16 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
   for (int base = blockIdx.x * S::GROUPS * R, slot = 0; base < rows; base += stride, first += stride) {
     float v[R][8];
     if (VEC) {
-      const int next = slot == 0 ? LN_FWD_AHEAD - 1 : slot - 1;
-      fetch(first + (LN_FWD_AHEAD - 1) * stride, next);
-      fetch_wait<LN_FWD_AHEAD - 1>();
+      const int next = slot == 0 ? S::AHEAD - 1 : slot - 1;
+      fetch(first + (S::AHEAD - 1) * stride, next);
+      fetch_wait<S::AHEAD - 1>();
     }
     const char* place = smem + slot * R * BYTES;
-    slot = slot + 1 == LN_FWD_AHEAD ? 0 : slot + 1;
+    slot = slot + 1 == S::AHEAD ? 0 : slot + 1;
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const int m = first + a < rows ? n : 0;
-      const size_t at = (size_t)(first + a) * D + e0;
+      const size_t at = row_at(first + a, D, e0);
       if (VEC) row_take<BF, T>(place + a * BYTES, v[a]);
       else load8n<BF, false>(x, at, m, v[a]);
       if (RES) {   // the residual sum in front of the norm: rounded and stored, and the rounded one is what is normalised
@@ -141,8 +154,7 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
         for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], c[t]);
         store8n<BF, VEC>(sum, at, m, v[a]);
         if (BF) {
-#pragma unroll
-          for (int t = 0; t < 8; ++t) v[a][t] = bf2f(f2bf(v[a][t]));
+          round8(v[a]);
         }
       }
       if (BF && VEC && q8) {   // the checkpoint of what is normalised
@@ -156,28 +168,29 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
       if (lane == 0) leaf_s[grp][0][a][warp] = s;
     }
     __syncthreads();
-    float mu[R];
+    const float mu_mine = fmul(dealt_tree<R, WPR>(leaf_s[grp][0][0], leaves), invD);
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      mu[a] = fmul(row_tree<WPR>(leaf_s[grp][0][a], leaves), invD);
+      const float mu = __shfl_sync(0xffffffffu, mu_mine, a);
       float sq[8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        v[a][t] = fsub(v[a][t], mu[a]);
+        v[a][t] = fsub(v[a][t], mu);
         sq[t] = fmul(v[a][t], v[a][t]);
       }
       const float s = leaf_tree<VEC>(sq, warp, e0, D, full);
       if (lane == 0) leaf_s[grp][1][a][warp] = s;
     }
     __syncthreads();
+    const float rs_mine = fdiv(1.0f, fsqrt(fadd(fmul(dealt_tree<R, WPR>(leaf_s[grp][1][0], leaves), invD), eps)));
+    if (warp == 0 && lane < R && first + lane < rows) {
+      mean[first + lane] = mu_mine;
+      rstd[first + lane] = rs_mine;
+    }
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      const float rs = fdiv(1.0f, fsqrt(fadd(fmul(row_tree<WPR>(leaf_s[grp][1][a], leaves), invD), eps)));
+      const float rs = __shfl_sync(0xffffffffu, rs_mine, a);
       if (first + a >= rows) continue;
-      if (warp == 0 && lane == 0) {
-        mean[first + a] = mu[a];
-        rstd[first + a] = rs;
-      }
       float o[8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) o[t] = fmul(v[a][t], rs);
@@ -189,11 +202,10 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
       }
-      const size_t at = (size_t)(first + a) * D + e0;
+      const size_t at = row_at(first + a, D, e0);
       store8n<BF, VEC>(y, at, n, o);
       if (BF && VEC && qy && n > 0) {   // the next linear's quantiser, applied to the bf16 values just stored
-#pragma unroll
-        for (int t = 0; t < 8; ++t) o[t] = bf2f(f2bf(o[t]));
+        round8(o);
         *reinterpret_cast<uint2*>(qy + at) = quant8(o, inv_q);
       }
     }
@@ -244,7 +256,7 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
         for (int a = 0; a < R; ++a, place += BYTES) {
           const int row = ahead.base + mine + ahead.p * R + a;
           const bool there = row < rows && n > 0;
-          const size_t at = there ? (size_t)row * D + e0 : 0;
+          const size_t at = there ? row_at(row, D, e0) : 0;
           row_fetch<Fx::DY, T>(place, static_cast<const char*>(dy) + at * (BF ? 2 : 4), there);
           row_fetch<Fx::X, T>(place + T * Fx::DY, static_cast<const char*>(x) + at * (KIND == LN_ACT8 ? 1 : (BF ? 2 : 4)), there);
           if (RES) row_fetch<Fx::DY, T>(place + T * (Fx::DY + Fx::X), static_cast<const char*>(res) + at * (BF ? 2 : 4), there);
@@ -291,13 +303,13 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
     for (int a = 0; a < R; ++a) {
       const int row = first + a, m = row < rows ? n : 0;
       if (VEC) row_take<BF, T>(place + a * BYTES, w[a]);
-      else load8n<BF, false>(dy, (size_t)row * D + e0, m, w[a]);
+      else load8n<BF, false>(dy, row_at(row, D, e0), m, w[a]);
       if (KIND == LN_ACT8) {
         uint2 c = make_uint2(0, 0);
         if (VEC) {
           c = reinterpret_cast<const uint2*>(place + a * BYTES + T * Fx::DY)[threadIdx.x];
         } else {
-          const int8_t* q = reinterpret_cast<const int8_t*>(x) + (size_t)row * D + e0;
+          const int8_t* q = reinterpret_cast<const int8_t*>(x) + row_at(row, D, e0);
 #pragma unroll
           for (int t = 0; t < 8; ++t)
             if (t < m) (t < 4 ? c.x : c.y) |= (uint32_t)(uint8_t)q[t] << (8 * (t & 3));
@@ -306,7 +318,7 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
       } else if (VEC) {
         row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
       } else {
-        load8n<BF, false>(x, (size_t)row * D + e0, m, xh[a]);
+        load8n<BF, false>(x, row_at(row, D, e0), m, xh[a]);
       }
 #pragma unroll
       for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu[a]), rs[a]);
@@ -350,11 +362,12 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
       if (lane == 0) { leaf[a][0][warp] = s1; leaf[a][1][warp] = s2; }
     }
     __syncthreads();
+    const float c_mine = fmul(dealt_tree<2 * R, WPR>(leaf[0][0], leaves), invD);
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-      const float c1 = fmul(row_tree<WPR>(leaf[a][0], leaves), invD), c2 = fmul(row_tree<WPR>(leaf[a][1], leaves), invD);
+      const float c1 = __shfl_sync(0xffffffffu, c_mine, 2 * a), c2 = __shfl_sync(0xffffffffu, c_mine, 2 * a + 1);
       const int m = first + a < rows ? n : 0;
-      const size_t at = (size_t)(first + a) * D + e0;
+      const size_t at = row_at(first + a, D, e0);
       float o[8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
@@ -465,9 +478,9 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
           constexpr int W = decltype(wpr)::value;
           constexpr bool BF = decltype(is_bf)::value, VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
           if constexpr (BF || !RES) {
-            using S = LnShape<W>;
+            using S = LnShape<W, BF>;
             const int per = S::GROUPS * S::ROWS;
-            const size_t smem = VEC ? (size_t)LN_FWD_AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : 0;
+            const size_t smem = VEC ? (size_t)S::AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : 0;
             auto kern = k_ln_fwd<BF, W, VEC, RES>;
             static DevOnce once;
             if (smem > 40 * 1024) rc = dev_ensure_smem(once, (const void*)kern, smem);

@@ -4,6 +4,23 @@
 
 namespace det {
 
+// two values rounded to bf16 in one instruction (one by one they go through the conversion pipe); same bits as two of f2bf
+__device__ __forceinline__ uint32_t bf_pair(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// eight values rounded to bf16 and back
+__device__ __forceinline__ void round8(float v[8]) {
+#pragma unroll
+  for (int t = 0; t < 8; t += 2) {
+    const uint32_t u = bf_pair(v[t], v[t + 1]);
+    v[t] = bflo(u);
+    v[t + 1] = bfhi(u);
+  }
+}
+// element `col` of row `row` of rows of D
+__device__ __forceinline__ size_t row_at(int row, int D, int col) { return (size_t)((unsigned long long)(unsigned)row * (unsigned)D) + col; }
 template <bool BF>
 __device__ __forceinline__ void load8(const void* p, size_t idx, float v[8]) {
   if (BF) {
@@ -20,7 +37,7 @@ template <bool BF>
 __device__ __forceinline__ void store8(void* p, size_t idx, const float v[8]) {
   if (BF) {
     uint4 u;
-    u.x = pack_bf2(v[0], v[1]); u.y = pack_bf2(v[2], v[3]); u.z = pack_bf2(v[4], v[5]); u.w = pack_bf2(v[6], v[7]);
+    u.x = bf_pair(v[0], v[1]); u.y = bf_pair(v[2], v[3]); u.z = bf_pair(v[4], v[5]); u.w = bf_pair(v[6], v[7]);
     *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p) + idx) = u;
   } else {
     float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + idx);
