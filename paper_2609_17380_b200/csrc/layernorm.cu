@@ -16,14 +16,14 @@ namespace det {
 // A row is held by WPR warps, a leaf of 256 columns each, eight adjacent columns a lane.  WPR < 8: a CTA of eight warps has 8 / WPR such groups,
 // with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are worked on at a time (backward one where 32 warps hold a row: there
 // are 64 registers a thread).
-template <int WPR, bool BF>
+template <int WPR>
 struct LnShape {
-  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = BF && WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
   static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
 };
 template <int WPR>
 struct LnBwd {
-  static constexpr int GROUPS = LnShape<WPR, false>::GROUPS, THREADS = LnShape<WPR, false>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
+  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
 };
 
 // The tree over N nodes of which the first `have` exist (at least one); all of them in the usual case, without a test.
@@ -83,23 +83,52 @@ __device__ __forceinline__ float dealt_tree(const float* leaf, int leaves) {
   }
   return r;
 }
-template <bool VEC>
-__device__ __forceinline__ float leaf_tree(const float v[8], int warp, int e0, int D, bool full) {
-  if (full) return warp_tree_full(tree8_full(v));
-  return warp_tree(VEC ? tree8_full(v) : tree8(v, e0, D), (long long)warp * 256, 8, D);
+// The leaves of N sums (N 2 or 4; each lane has its eight terms' sums in v), sum j's to out[j * WPR].  Each step of the butterfly over the lanes hands
+// half of the sums to the neighbour while there are several, so that four sums take 6 exchanges instead of 20; the tree of each is the same.
+template <int N, int WPR>
+__device__ __forceinline__ void leaf_sums(const float (&v)[N], float* out, int warp, int D, bool full) {
+  static_assert(N == 2 || N == 4, "two or four sums");
+  const int lane = threadIdx.x & 31;
+  if (full) {
+    const bool b0 = lane & 1, b1 = lane & 2;
+    float r;
+    int sum;
+    if constexpr (N == 4) {
+      const float p = fadd(b0 ? v[2] : v[0], __shfl_xor_sync(0xffffffffu, b0 ? v[0] : v[2], 1));
+      const float q = fadd(b0 ? v[3] : v[1], __shfl_xor_sync(0xffffffffu, b0 ? v[1] : v[3], 1));
+      r = fadd(b1 ? q : p, __shfl_xor_sync(0xffffffffu, b1 ? p : q, 2));
+      sum = (b0 ? 2 : 0) + (b1 ? 1 : 0);
+    } else {
+      r = fadd(b0 ? v[1] : v[0], __shfl_xor_sync(0xffffffffu, b0 ? v[0] : v[1], 1));
+      r = fadd(r, __shfl_xor_sync(0xffffffffu, r, 2));
+      sum = b0 ? 1 : 0;
+    }
+#pragma unroll
+    for (int w = 4; w < 32; w <<= 1) r = fadd(r, __shfl_xor_sync(0xffffffffu, r, w));
+    if (lane < N) out[sum * WPR + warp] = r;
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float r = warp_tree(v[j], (long long)warp * 256, 8, D);
+      if (lane == 0) out[j * WPR + warp] = r;
+    }
+  }
 }
+// the sum of a lane's eight terms
+template <bool VEC>
+__device__ __forceinline__ float lane_sum(const float v[8], int e0, int D) { return VEC ? tree8_full(v) : tree8(v, e0, D); }
 
 // Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (AHEAD passes, each thread its own
 // columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
 // stream).
 template <bool BF, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::CTAS)
+__global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
     k_ln_fwd(const void* __restrict__ x, const void* __restrict__ res, const void* __restrict__ gamma, const void* __restrict__ beta,
              int rows, int D, float eps, float invD, void* __restrict__ sum, void* __restrict__ y, float* __restrict__ mean,
              float* __restrict__ rstd, const float* __restrict__ s_q, int8_t* __restrict__ qy, int8_t* __restrict__ q8,
              uint8_t* __restrict__ e8) {
   grid_dep();
-  using S = LnShape<WPR, BF>;
+  using S = LnShape<WPR>;
   constexpr int R = S::ROWS, T = S::THREADS, EL = BF ? 2 : 4, BYTES = T * 8 * EL * (RES ? 2 : 1);      // BYTES: a row on its way
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float leaf_s[S::GROUPS][2][R][WPR];
@@ -112,10 +141,10 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
     if (VEC) {
       if (first < rows) {
         char* place = smem + slot * R * BYTES;
+        size_t at = row_at(first, D, e0) * EL;
 #pragma unroll
-        for (int a = 0; a < R; ++a, place += BYTES) {
+        for (int a = 0; a < R; ++a, place += BYTES, at += (size_t)D * EL) {
           const bool there = first + a < rows && n > 0;
-          const size_t at = there ? row_at(first + a, D, e0) * EL : 0;
           row_fetch<8 * EL, T>(place, static_cast<const char*>(x) + at, there);
           if (RES) row_fetch<8 * EL, T>(place + T * 8 * EL, static_cast<const char*>(res) + at, there);
         }
@@ -140,6 +169,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
     }
     const char* place = smem + slot * R * BYTES;
     slot = slot + 1 == S::AHEAD ? 0 : slot + 1;
+    float part[R];
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const int m = first + a < rows ? n : 0;
@@ -164,9 +194,9 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
           if ((lane & 3) == 0) e8[(size_t)(first + a) * ((D + A8_GROUP - 1) / A8_GROUP) + e0 / A8_GROUP] = (uint8_t)field;
         }
       }
-      const float s = leaf_tree<VEC>(v[a], warp, e0, D, full);
-      if (lane == 0) leaf_s[grp][0][a][warp] = s;
+      part[a] = lane_sum<VEC>(v[a], e0, D);
     }
+    leaf_sums<R, WPR>(part, leaf_s[grp][0][0], warp, D, full);
     __syncthreads();
     const float mu_mine = fmul(dealt_tree<R, WPR>(leaf_s[grp][0][0], leaves), invD);
 #pragma unroll
@@ -178,9 +208,9 @@ __global__ void __launch_bounds__(LnShape<WPR, BF>::THREADS, LnShape<WPR, BF>::C
         v[a][t] = fsub(v[a][t], mu);
         sq[t] = fmul(v[a][t], v[a][t]);
       }
-      const float s = leaf_tree<VEC>(sq, warp, e0, D, full);
-      if (lane == 0) leaf_s[grp][1][a][warp] = s;
+      part[a] = lane_sum<VEC>(sq, e0, D);
     }
+    leaf_sums<R, WPR>(part, leaf_s[grp][1][0], warp, D, full);
     __syncthreads();
     const float rs_mine = fdiv(1.0f, fsqrt(fadd(fmul(dealt_tree<R, WPR>(leaf_s[grp][1][0], leaves), invD), eps)));
     if (warp == 0 && lane < R && first + lane < rows) {
@@ -220,7 +250,7 @@ enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is: as dy, or the 8-b
 // over the blocks of rows, so the loads go on across the blocks.
 template <int KIND, int WPR>
 struct LnFetch {
-  static constexpr int AHEAD = KIND == LN_F32 ? 2 : 3;
+  static constexpr int AHEAD = KIND == LN_F32 || WPR == 32 ? 2 : 3;
   static constexpr int DY = KIND == LN_F32 ? 32 : 16, X = KIND == LN_F32 ? 32 : (KIND == LN_BF16 ? 16 : 8);
   static constexpr int T = LnBwd<WPR>::THREADS, R = LnBwd<WPR>::ROWS;
   static constexpr int ROW = T * (DY + X), ROW_RES = ROW + T * DY;                 // bytes of a row
@@ -235,8 +265,8 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
   using S = LnBwd<WPR>;
   using Fx = LnFetch<KIND, WPR>;
   constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW, AHEAD = Fx::AHEAD;
-  extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][16][T]
-  float* waiting = reinterpret_cast<float*>(smem + (VEC ? AHEAD * R * BYTES : 0));
+  extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][4][T]
+  float4* waiting = reinterpret_cast<float4*>(smem + (VEC ? AHEAD * R * BYTES : 0));
   __shared__ __align__(16) float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
@@ -252,11 +282,11 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
     if (VEC) {
       if (ahead.base < rows) {
         char* place = smem + ahead.slot * R * BYTES;
+        const int row = ahead.base + mine + ahead.p * R;
+        size_t at = row_at(row, D, e0);
 #pragma unroll
-        for (int a = 0; a < R; ++a, place += BYTES) {
-          const int row = ahead.base + mine + ahead.p * R + a;
-          const bool there = row < rows && n > 0;
-          const size_t at = there ? row_at(row, D, e0) : 0;
+        for (int a = 0; a < R; ++a, place += BYTES, at += D) {
+          const bool there = row + a < rows && n > 0;
           row_fetch<Fx::DY, T>(place, static_cast<const char*>(dy) + at * (BF ? 2 : 4), there);
           row_fetch<Fx::X, T>(place + T * Fx::DY, static_cast<const char*>(x) + at * (KIND == LN_ACT8 ? 1 : (BF ? 2 : 4)), there);
           if (RES) row_fetch<Fx::DY, T>(place + T * (Fx::DY + Fx::X), static_cast<const char*>(res) + at * (BF ? 2 : 4), there);
@@ -335,14 +365,20 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
       int level = 0;
       for (; (p >> level) & 1; ++level) {
         const bool have = r0 + ((p >> level) << level) * R < rows;
-        float* l = waiting + (size_t)level * 16 * T + threadIdx.x;
+        const float4* l = waiting + level * 4 * T + threadIdx.x;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) node[t] = have ? fadd(l[t * T], node[t]) : l[t * T];
+        for (int t = 0; t < 4; ++t) {
+          const float4 q = l[t * T];
+          node[4 * t] = have ? fadd(q.x, node[4 * t]) : q.x;
+          node[4 * t + 1] = have ? fadd(q.y, node[4 * t + 1]) : q.y;
+          node[4 * t + 2] = have ? fadd(q.z, node[4 * t + 2]) : q.z;
+          node[4 * t + 3] = have ? fadd(q.w, node[4 * t + 3]) : q.w;
+        }
       }
       if (p + 1 < passes) {
-        float* l = waiting + (size_t)level * 16 * T + threadIdx.x;
+        float4* l = waiting + level * 4 * T + threadIdx.x;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) l[t * T] = node[t];
+        for (int t = 0; t < 4; ++t) l[t * T] = make_float4(node[4 * t], node[4 * t + 1], node[4 * t + 2], node[4 * t + 3]);
       }
     }
     if (gamma) {
@@ -353,14 +389,16 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
     }
     float (*leaf)[2][WPR] = leaf_s[odd][grp];
     odd = !odd;
+    float part[2 * R];
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       float pr[8];
 #pragma unroll
       for (int t = 0; t < 8; ++t) pr[t] = fmul(w[a][t], xh[a][t]);
-      const float s1 = leaf_tree<VEC>(w[a], warp, e0, D, full), s2 = leaf_tree<VEC>(pr, warp, e0, D, full);
-      if (lane == 0) { leaf[a][0][warp] = s1; leaf[a][1][warp] = s2; }
+      part[2 * a] = lane_sum<VEC>(w[a], e0, D);
+      part[2 * a + 1] = lane_sum<VEC>(pr, e0, D);
     }
+    leaf_sums<2 * R, WPR>(part, leaf[0][0], warp, D, full);
     __syncthreads();
     const float c_mine = fmul(dealt_tree<2 * R, WPR>(leaf[0][0], leaves), invD);
 #pragma unroll
@@ -384,15 +422,16 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
   if (!partial) continue;
   if (S::GROUPS > 1) {   // the tree over the groups' nodes
     __syncthreads();
+    float* meet = reinterpret_cast<float*>(waiting) + threadIdx.x;
 #pragma unroll
-    for (int t = 0; t < 16; ++t) waiting[t * T + threadIdx.x] = node[t];
+    for (int t = 0; t < 16; ++t) meet[t * T] = node[t];
     __syncthreads();
     if (grp == 0) {
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
         float c[S::GROUPS];
 #pragma unroll
-        for (int k = 0; k < S::GROUPS; ++k) c[k] = waiting[t * T + k * WPR * 32 + threadIdx.x];
+        for (int k = 0; k < S::GROUPS; ++k) c[k] = meet[t * T + k * WPR * 32];
         node[t] = node_tree<S::GROUPS>(c, (rows - r0 + R * passes - 1) / (R * passes));
       }
     }
@@ -478,7 +517,7 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
           constexpr int W = decltype(wpr)::value;
           constexpr bool BF = decltype(is_bf)::value, VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
           if constexpr (BF || !RES) {
-            using S = LnShape<W, BF>;
+            using S = LnShape<W>;
             const int per = S::GROUPS * S::ROWS;
             const size_t smem = VEC ? (size_t)S::AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : 0;
             auto kern = k_ln_fwd<BF, W, VEC, RES>;
@@ -499,10 +538,10 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
 
 // Rows of a block of the backward pass, whose node goes to memory: a multiple of what a CTA works on at a time, more of it while there are two blocks for
 // every CTA on the GPU (each halving of the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
-constexpr int ln_levels(int threads) { return threads <= 512 ? 2 : 1; }
-static int ln_passes(int rows, int D, int per) {
+constexpr int ln_levels(bool f32, int threads) { return f32 && threads > 512 ? 1 : 2; }
+static int ln_passes(int rows, int per, int levels) {
   int passes = 1;
-  while (passes < (1 << ln_levels(D <= 4096 ? 512 : 1024)) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
+  while (passes < (1 << levels) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
   return passes;
 }
 static int ln_rows_in_flight(int D) {
@@ -514,7 +553,7 @@ template <int KIND>
 static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
                   const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
   const bool cols = dgamma || dbeta;
-  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, D, per), stride = per * passes;
+  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, per, ln_levels(KIND == LN_F32, D > 4096 ? 1024 : 512)), stride = per * passes;
   const int nb = (int)(((long long)rows + stride - 1) / stride), nu = (nb + 31) / 32;
   float* partial = cols ? (float*)ws : nullptr;
   float* upper = cols ? partial + 2 * (size_t)nb * D : nullptr;
@@ -534,7 +573,7 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
           const size_t level = (size_t)16 * S::THREADS * sizeof(float);
           auto kern = k_ln_bwd<KIND, W, VEC, RES>;
           static DevOnce once;
-          rc = dev_ensure_smem(once, (const void*)kern, ahead + ln_levels(S::THREADS) * level);
+          rc = dev_ensure_smem(once, (const void*)kern, ahead + ln_levels(KIND == LN_F32, S::THREADS) * level);
           if (rc != DET_OK) return;
           launch_after(kern, ln_grid(nb, S::CTAS), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
                        (float)(1.0 / (double)D), nb, passes, res, dx, partial, tickets);
@@ -579,7 +618,7 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
 
 extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
   if (rows <= 0 || D <= 0 || D > 8192) return 256;
-  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, D, per);
+  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, per, ln_levels(true, D > 4096 ? 1024 : 512));   // the more blocks of both types
   const size_t nb = ((size_t)rows + stride - 1) / stride, nu = (nb + 31) / 32;
   return align_up(2 * (nb + nu) * (size_t)D * sizeof(float), 256) + 256;
 }
