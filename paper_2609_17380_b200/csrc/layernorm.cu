@@ -21,9 +21,12 @@ struct LnShape {
   static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
   static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
 };
-template <int WPR>
+enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is backward: as dy, or the 8-bit checkpoint (dy bf16)
+template <int WPR, int KIND>
 struct LnBwd {
-  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : 2, CTAS = WPR <= 8 ? 2 : 1;
+  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : (WPR == 16 || KIND == LN_F32 ? 2 : 4);
+  static constexpr bool AHEAD_ROWS = KIND != LN_F32 || WPR > 8;          // f32: loads in place with a third CTA do better than 128 KiB on their way
+  static constexpr int CTAS = WPR > 8 ? 1 : (AHEAD_ROWS ? 2 : 3), LEVELS = WPR <= 8 && ROWS == 4 ? 1 : (KIND == LN_F32 && WPR == 32 ? 1 : 2);
 };
 
 // The tree over N nodes of which the first `have` exist (at least one); all of them in the usual case, without a test.
@@ -83,29 +86,33 @@ __device__ __forceinline__ float dealt_tree(const float* leaf, int leaves) {
   }
   return r;
 }
-// The leaves of N sums (N 2 or 4; each lane has its eight terms' sums in v), sum j's to out[j * WPR].  Each step of the butterfly over the lanes hands
-// half of the sums to the neighbour while there are several, so that four sums take 6 exchanges instead of 20; the tree of each is the same.
+// The leaves of N sums (a power of two; each lane has its eight terms' sums in v), sum j's to out[j * WPR].  Each step of the butterfly over the lanes
+// hands half of the sums to the neighbour while there are several, so that eight sums take 9 exchanges instead of 40; the tree of each is the same.
 template <int N, int WPR>
 __device__ __forceinline__ void leaf_sums(const float (&v)[N], float* out, int warp, int D, bool full) {
-  static_assert(N == 2 || N == 4, "two or four sums");
   const int lane = threadIdx.x & 31;
   if (full) {
-    const bool b0 = lane & 1, b1 = lane & 2;
-    float r;
-    int sum;
-    if constexpr (N == 4) {
-      const float p = fadd(b0 ? v[2] : v[0], __shfl_xor_sync(0xffffffffu, b0 ? v[0] : v[2], 1));
-      const float q = fadd(b0 ? v[3] : v[1], __shfl_xor_sync(0xffffffffu, b0 ? v[1] : v[3], 1));
-      r = fadd(b1 ? q : p, __shfl_xor_sync(0xffffffffu, b1 ? p : q, 2));
-      sum = (b0 ? 2 : 0) + (b1 ? 1 : 0);
-    } else {
-      r = fadd(b0 ? v[1] : v[0], __shfl_xor_sync(0xffffffffu, b0 ? v[0] : v[1], 1));
-      r = fadd(r, __shfl_xor_sync(0xffffffffu, r, 2));
-      sum = b0 ? 1 : 0;
-    }
+    float s[N];
 #pragma unroll
-    for (int w = 4; w < 32; w <<= 1) r = fadd(r, __shfl_xor_sync(0xffffffffu, r, w));
-    if (lane < N) out[sum * WPR + warp] = r;
+    for (int j = 0; j < N; ++j) s[j] = v[j];
+    int sum = 0;
+#pragma unroll
+    for (int w = 1, left = N; w < 32; w <<= 1) {
+      if (left > 1) {
+        left /= 2;
+        const bool up = lane & w;
+        sum += up ? left : 0;
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j)
+          if (j < left) {
+            const float away = up ? s[j] : s[j + left];
+            s[j] = fadd(up ? s[j + left] : s[j], __shfl_xor_sync(0xffffffffu, away, w));
+          }
+      } else {
+        s[0] = fadd(s[0], __shfl_xor_sync(0xffffffffu, s[0], w));
+      }
+    }
+    if (lane < N) out[sum * WPR + warp] = s[0];
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -245,28 +252,27 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
 // Backward.  Each group of warps takes `passes` x ROWS adjacent rows (passes a power of two), ROWS at a time; a lane sees the same eight columns of
 // all of them, so the trees of dgamma and dbeta over the group's rows run in its own registers, the nodes of finished passes waiting
 // in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
-enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is: as dy, or the 8-bit checkpoint (dy bf16)
 // What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, AHEAD passes of them.  As many CTAs as the GPU holds walk
 // over the blocks of rows, so the loads go on across the blocks.
 template <int KIND, int WPR>
 struct LnFetch {
-  static constexpr int AHEAD = KIND == LN_F32 || WPR == 32 ? 2 : 3;
+  static constexpr int AHEAD = WPR == 16 && KIND != LN_F32 ? 3 : 2;
   static constexpr int DY = KIND == LN_F32 ? 32 : 16, X = KIND == LN_F32 ? 32 : (KIND == LN_BF16 ? 16 : 8);
-  static constexpr int T = LnBwd<WPR>::THREADS, R = LnBwd<WPR>::ROWS;
+  static constexpr int T = LnBwd<WPR, KIND>::THREADS, R = LnBwd<WPR, KIND>::ROWS;
   static constexpr int ROW = T * (DY + X), ROW_RES = ROW + T * DY;                 // bytes of a row
 };
 template <int KIND, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
+__global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::CTAS)
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
              const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int nb, int passes, const void* res,
              void* dx, float* __restrict__ partial, int* __restrict__ tickets) {
   grid_dep();
-  constexpr bool BF = KIND != LN_F32;
-  using S = LnBwd<WPR>;
+  constexpr bool BF = KIND != LN_F32, STAGED = VEC && LnBwd<WPR, KIND>::AHEAD_ROWS;
+  using S = LnBwd<WPR, KIND>;
   using Fx = LnFetch<KIND, WPR>;
   constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW, AHEAD = Fx::AHEAD;
   extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][4][T]
-  float4* waiting = reinterpret_cast<float4*>(smem + (VEC ? AHEAD * R * BYTES : 0));
+  float4* waiting = reinterpret_cast<float4*>(smem + (STAGED ? AHEAD * R * BYTES : 0));
   __shared__ __align__(16) float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
@@ -279,7 +285,7 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
   float mu_next[R], rs_next[R], step_next[R];
   struct { int base, p, slot; } ahead = {(int)blockIdx.x * block, 0, 0};        // the pass to fetch next
   auto fetch = [&]() {
-    if (VEC) {
+    if (STAGED) {
       if (ahead.base < rows) {
         char* place = smem + ahead.slot * R * BYTES;
         const int row = ahead.base + mine + ahead.p * R;
@@ -326,17 +332,17 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
     for (int a = 0; a < R; ++a) { mu[a] = mu_next[a]; rs[a] = rs_next[a]; step[a] = KIND == LN_ACT8 ? step_next[a] : 0.0f; }
     fetch();
     statistics(p + 1 < passes ? first + R : r0 + stride);
-    if (VEC) fetch_wait<AHEAD - 1>();
+    if (STAGED) fetch_wait<AHEAD - 1>();
     const char* place = smem + slot * R * BYTES;
     slot = slot + 1 == AHEAD ? 0 : slot + 1;
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const int row = first + a, m = row < rows ? n : 0;
-      if (VEC) row_take<BF, T>(place + a * BYTES, w[a]);
-      else load8n<BF, false>(dy, row_at(row, D, e0), m, w[a]);
+      if (STAGED) row_take<BF, T>(place + a * BYTES, w[a]);
+      else load8n<BF, VEC>(dy, row_at(row, D, e0), m, w[a]);
       if (KIND == LN_ACT8) {
         uint2 c = make_uint2(0, 0);
-        if (VEC) {
+        if (STAGED) {
           c = reinterpret_cast<const uint2*>(place + a * BYTES + T * Fx::DY)[threadIdx.x];
         } else {
           const int8_t* q = reinterpret_cast<const int8_t*>(x) + row_at(row, D, e0);
@@ -345,10 +351,10 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
             if (t < m) (t < 4 ? c.x : c.y) |= (uint32_t)(uint8_t)q[t] << (8 * (t & 3));
         }
         a8_values8(c, step[a], xh[a]);
-      } else if (VEC) {
+      } else if (STAGED) {
         row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
       } else {
-        load8n<BF, false>(x, row_at(row, D, e0), m, xh[a]);
+        load8n<BF, VEC>(x, row_at(row, D, e0), m, xh[a]);
       }
 #pragma unroll
       for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu[a]), rs[a]);
@@ -411,8 +417,8 @@ __global__ void __launch_bounds__(LnBwd<WPR>::THREADS, LnBwd<WPR>::CTAS)
       for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
       if (RES) {   // the gradient that bypasses the norm (res may be dx)
         float b[8];
-        if (VEC) row_take<BF, T>(place + a * BYTES + T * (Fx::DY + Fx::X), b);
-        else load8n<BF, false>(res, at, m, b);
+        if (STAGED) row_take<BF, T>(place + a * BYTES + T * (Fx::DY + Fx::X), b);
+        else load8n<BF, VEC>(res, at, m, b);
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = fadd(b[t], o[t]);
       }
@@ -538,23 +544,21 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
 
 // Rows of a block of the backward pass, whose node goes to memory: a multiple of what a CTA works on at a time, more of it while there are two blocks for
 // every CTA on the GPU (each halving of the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
-constexpr int ln_levels(bool f32, int threads) { return f32 && threads > 512 ? 1 : 2; }
-static int ln_passes(int rows, int per, int levels) {
+struct LnBlock { int passes, rows; };
+template <int KIND>
+static LnBlock ln_block(int rows, int D) {
+  int per = 0, levels = 0;
+  with_wpr(D, [&](auto wpr) { using S = LnBwd<decltype(wpr)::value, KIND>; per = S::GROUPS * S::ROWS; levels = S::LEVELS; });
   int passes = 1;
   while (passes < (1 << levels) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
-  return passes;
-}
-static int ln_rows_in_flight(int D) {
-  int per = 0;
-  with_wpr(D, [&](auto wpr) { using S = LnBwd<decltype(wpr)::value>; per = S::GROUPS * S::ROWS; });
-  return per;
+  return {passes, passes * per};
 }
 template <int KIND>
 static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
                   const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
   const bool cols = dgamma || dbeta;
-  const int per = ln_rows_in_flight(D), passes = ln_passes(rows, per, ln_levels(KIND == LN_F32, D > 4096 ? 1024 : 512)), stride = per * passes;
-  const int nb = (int)(((long long)rows + stride - 1) / stride), nu = (nb + 31) / 32;
+  const LnBlock block = ln_block<KIND>(rows, D);
+  const int passes = block.passes, nb = (int)(((long long)rows + block.rows - 1) / block.rows), nu = (nb + 31) / 32;
   float* partial = cols ? (float*)ws : nullptr;
   float* upper = cols ? partial + 2 * (size_t)nb * D : nullptr;
   int* tickets = cols ? reinterpret_cast<int*>(upper + 2 * (size_t)nu * D) : nullptr;
@@ -565,15 +569,15 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
         constexpr int W = decltype(wpr)::value;
         constexpr bool VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
         if constexpr (!(RES && KIND == LN_F32)) {
-          using S = LnBwd<W>;
+          using S = LnBwd<W, KIND>;
           int levels = 0;
           while ((1 << levels) < passes) ++levels;
           if (S::GROUPS > 1 && levels == 0) levels = 1;
-          const size_t ahead = VEC ? (size_t)LnFetch<KIND, W>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
+          const size_t ahead = VEC && S::AHEAD_ROWS ? (size_t)LnFetch<KIND, W>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
           const size_t level = (size_t)16 * S::THREADS * sizeof(float);
           auto kern = k_ln_bwd<KIND, W, VEC, RES>;
           static DevOnce once;
-          rc = dev_ensure_smem(once, (const void*)kern, ahead + ln_levels(KIND == LN_F32, S::THREADS) * level);
+          rc = dev_ensure_smem(once, (const void*)kern, ahead + S::LEVELS * level);
           if (rc != DET_OK) return;
           launch_after(kern, ln_grid(nb, S::CTAS), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
                        (float)(1.0 / (double)D), nb, passes, res, dx, partial, tickets);
@@ -618,8 +622,8 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
 
 extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
   if (rows <= 0 || D <= 0 || D > 8192) return 256;
-  const int per = ln_rows_in_flight(D), stride = per * ln_passes(rows, per, ln_levels(true, D > 4096 ? 1024 : 512));   // the more blocks of both types
-  const size_t nb = ((size_t)rows + stride - 1) / stride, nu = (nb + 31) / 32;
+  const int least = min(ln_block<LN_F32>(rows, D).rows, min(ln_block<LN_BF16>(rows, D).rows, ln_block<LN_ACT8>(rows, D).rows));
+  const size_t nb = ((size_t)rows + least - 1) / least, nu = (nb + 31) / 32;
   return align_up(2 * (nb + nu) * (size_t)D * sizeof(float), 256) + 256;
 }
 
