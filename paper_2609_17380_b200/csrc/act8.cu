@@ -17,7 +17,7 @@ __global__ void __launch_bounds__(256) k_a8_pack(const void* __restrict__ x, siz
   const size_t r = i / lanes, c = (i % lanes) * 8;
   const bool have = r < (size_t)rows && c < (size_t)D;
   float v[8];
-  load8n<BF, true>(x, r * ld + c, have, v);
+  load8n<BF>(x, r * ld + c, have, v);
   const uint32_t field = a8_field(a8_quad_max(a8_amax8(v)));
   if (!have) return;
   *reinterpret_cast<uint2*>(q + r * D + c) = a8_codes8(v, field);
@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(256) k_swiglu_fwd_a8(const uint16_t* __restric
     a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
     a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
   } else {
-    load8n<true, true>(gu, at, have, g);
-    load8n<true, true>(gu, at + F, have, u);
+    load8n<true>(gu, at, have, g);
+    load8n<true>(gu, at + F, have, u);
     const uint32_t fg = a8_field(a8_quad_max(a8_amax8(g))), fu = a8_field(a8_quad_max(a8_amax8(u)));
     if (!have) return;
     *reinterpret_cast<uint2*>(q + at) = a8_codes8(g, fg);

@@ -16,17 +16,18 @@ namespace det {
 // A row is held by WPR warps, a leaf of 256 columns each, eight adjacent columns a lane.  WPR < 8: a CTA of eight warps has 8 / WPR such groups,
 // with rows of their own; WPR >= 8: the CTA is one group.  ROWS rows of a group are worked on at a time (backward one where 32 warps hold a row: there
 // are 64 registers a thread).
-template <int WPR>
+template <int WPR, bool BF, bool VEC>
 struct LnShape {
-  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = BF && VEC && WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
+  static constexpr bool AHEAD_ROWS = BF && VEC;          // binary32 rows: a CTA for every two rows and loads in place (27 us for 8192 x 2048, 36 ahead)
   static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
 };
 enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is backward: as dy, or the 8-bit checkpoint (dy bf16)
-template <int WPR, int KIND>
+template <int WPR, int KIND, bool VEC>
 struct LnBwd {
-  static constexpr int GROUPS = LnShape<WPR>::GROUPS, THREADS = LnShape<WPR>::THREADS, ROWS = WPR == 32 ? 1 : (WPR == 16 || KIND == LN_F32 ? 2 : 4);
-  static constexpr bool AHEAD_ROWS = KIND != LN_F32 || WPR > 8;          // f32: loads in place with a third CTA do better than 128 KiB on their way
-  static constexpr int CTAS = WPR > 8 ? 1 : (AHEAD_ROWS ? 2 : 3), LEVELS = WPR <= 8 && ROWS == 4 ? 1 : (KIND == LN_F32 && WPR == 32 ? 1 : 2);
+  static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = WPR == 32 ? 1 : (WPR == 16 || KIND == LN_F32 || !VEC ? 2 : 4);
+  static constexpr bool AHEAD_ROWS = VEC && (KIND != LN_F32 || WPR > 8);  // f32: loads in place with a third CTA do better than 128 KiB on their way
+  static constexpr int CTAS = WPR > 8 ? 1 : (AHEAD_ROWS || !VEC ? 2 : 3), LEVELS = WPR <= 8 && ROWS == 4 ? 1 : (KIND == LN_F32 && WPR == 32 ? 1 : 2);
 };
 
 // The tree over N nodes of which the first `have` exist (at least one); all of them in the usual case, without a test.
@@ -129,23 +130,25 @@ __device__ __forceinline__ float lane_sum(const float v[8], int e0, int D) { ret
 // columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
 // stream).
 template <bool BF, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
+__global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, BF, VEC>::CTAS)
     k_ln_fwd(const void* __restrict__ x, const void* __restrict__ res, const void* __restrict__ gamma, const void* __restrict__ beta,
              int rows, int D, float eps, float invD, void* __restrict__ sum, void* __restrict__ y, float* __restrict__ mean,
              float* __restrict__ rstd, const float* __restrict__ s_q, int8_t* __restrict__ qy, int8_t* __restrict__ q8,
              uint8_t* __restrict__ e8) {
   grid_dep();
-  using S = LnShape<WPR>;
+  using S = LnShape<WPR, BF, VEC>;
   constexpr int R = S::ROWS, T = S::THREADS, EL = BF ? 2 : 4, BYTES = T * 8 * EL * (RES ? 2 : 1);      // BYTES: a row on its way
+  static_assert(S::AHEAD_ROWS || !VEC || !RES, "the residual stream is bf16");
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float leaf_s[S::GROUPS][2][R][WPR];
+  float* room = reinterpret_cast<float*>(smem) + (threadIdx.x >> 5) * 256;            // VEC false: of the warp
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = (D & 255) == 0;
   const int leaves = (D + 255) >> 8;
   const int stride = gridDim.x * S::GROUPS * R;
   auto fetch = [&](int first, int slot) {
-    if (VEC) {
+    if (S::AHEAD_ROWS) {
       if (first < rows) {
         char* place = smem + slot * R * BYTES;
         size_t at = row_at(first, D, e0) * EL;
@@ -163,13 +166,23 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
 #pragma unroll
   for (int k = 0; k < S::AHEAD - 1; ++k) fetch(first + k * stride, k);
   float g[8], b[8];
-  if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
-  if (beta) load8n<BF, VEC>(beta, e0, n, b);
+  const int w0 = warp * 256, left = D - w0;              // the warp's first column, how many are left from there
+  auto take = [&](const void* p, float v[8]) {
+    if (VEC) {
+      load8n<BF>(p, e0, n, v);
+    } else {
+      uint32_t raw[8];
+      load_any<EL>(p, w0, left, raw);
+      deal_out(room, raw, v);
+    }
+  };
+  if (gamma) take(gamma, g);
+  if (beta) take(beta, b);
   const float inv_q = (BF && VEC && qy) ? fdiv(1.0f, s_q[0]) : 0.0f;
   // all groups of the CTA make the same passes
   for (int base = blockIdx.x * S::GROUPS * R, slot = 0; base < rows; base += stride, first += stride) {
     float v[R][8];
-    if (VEC) {
+    if (S::AHEAD_ROWS) {
       const int next = slot == 0 ? S::AHEAD - 1 : slot - 1;
       fetch(first + (S::AHEAD - 1) * stride, next);
       fetch_wait<S::AHEAD - 1>();
@@ -177,19 +190,31 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
     const char* place = smem + slot * R * BYTES;
     slot = slot + 1 == S::AHEAD ? 0 : slot + 1;
     float part[R];
+    uint32_t raw[R][8], raw_res[R][8];
+    if (!VEC) {
+#pragma unroll
+      for (int a = 0; a < R; ++a) {
+        load_any<EL>(x, row_at(first + a, D, w0), first + a < rows ? left : 0, raw[a]);
+        if (RES) load_any<EL>(res, row_at(first + a, D, w0), first + a < rows ? left : 0, raw_res[a]);
+      }
+    } else if (!S::AHEAD_ROWS) {
+#pragma unroll
+      for (int a = 0; a < R; ++a) load8n<BF>(x, row_at(first + a, D, e0), first + a < rows ? n : 0, v[a]);
+    }
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const int m = first + a < rows ? n : 0;
       const size_t at = row_at(first + a, D, e0);
-      if (VEC) row_take<BF, T>(place + a * BYTES, v[a]);
-      else load8n<BF, false>(x, at, m, v[a]);
+      if (S::AHEAD_ROWS) row_take<BF, T>(place + a * BYTES, v[a]);
+      else if (!VEC) deal_out(room, raw[a], v[a]);
       if (RES) {   // the residual sum in front of the norm: rounded and stored, and the rounded one is what is normalised
         float c[8];
-        if (VEC) row_take<BF, T>(place + a * BYTES + T * 8 * EL, c);
-        else load8n<BF, false>(res, at, m, c);
+        if (S::AHEAD_ROWS) row_take<BF, T>(place + a * BYTES + T * 8 * EL, c);
+        else deal_out(room, raw_res[a], c);
 #pragma unroll
         for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], c[t]);
-        store8n<BF, VEC>(sum, at, m, v[a]);
+        if (!VEC) store_any<BF>(sum, row_at(first + a, D, w0), first + a < rows ? left : 0, room, v[a]);
+        else if (m > 0) store8<BF>(sum, at, v[a]);
         if (BF) {
           round8(v[a]);
         }
@@ -240,7 +265,8 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
         for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
       }
       const size_t at = row_at(first + a, D, e0);
-      store8n<BF, VEC>(y, at, n, o);
+      if (!VEC) store_any<BF>(y, row_at(first + a, D, w0), left, room, o);
+      else if (n > 0) store8<BF>(y, at, o);
       if (BF && VEC && qy && n > 0) {   // the next linear's quantiser, applied to the bf16 values just stored
         round8(o);
         *reinterpret_cast<uint2*>(qy + at) = quant8(o, inv_q);
@@ -254,25 +280,27 @@ __global__ void __launch_bounds__(LnShape<WPR>::THREADS, LnShape<WPR>::CTAS)
 // in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
 // What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, AHEAD passes of them.  As many CTAs as the GPU holds walk
 // over the blocks of rows, so the loads go on across the blocks.
-template <int KIND, int WPR>
+template <int KIND, int WPR, bool VEC>
 struct LnFetch {
   static constexpr int AHEAD = WPR == 16 && KIND != LN_F32 ? 3 : 2;
   static constexpr int DY = KIND == LN_F32 ? 32 : 16, X = KIND == LN_F32 ? 32 : (KIND == LN_BF16 ? 16 : 8);
-  static constexpr int T = LnBwd<WPR, KIND>::THREADS, R = LnBwd<WPR, KIND>::ROWS;
+  static constexpr int T = LnBwd<WPR, KIND, VEC>::THREADS, R = LnBwd<WPR, KIND, VEC>::ROWS;
   static constexpr int ROW = T * (DY + X), ROW_RES = ROW + T * DY;                 // bytes of a row
 };
 template <int KIND, int WPR, bool VEC, bool RES>
-__global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::CTAS)
+__global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIND, VEC>::CTAS)
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
              const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int nb, int passes, const void* res,
-             void* dx, float* __restrict__ partial, int* __restrict__ tickets) {
+             void* dx, float* __restrict__ partial) {
   grid_dep();
-  constexpr bool BF = KIND != LN_F32, STAGED = VEC && LnBwd<WPR, KIND>::AHEAD_ROWS;
-  using S = LnBwd<WPR, KIND>;
-  using Fx = LnFetch<KIND, WPR>;
+  constexpr bool BF = KIND != LN_F32, STAGED = LnBwd<WPR, KIND, VEC>::AHEAD_ROWS;
+  using S = LnBwd<WPR, KIND, VEC>;
+  using Fx = LnFetch<KIND, WPR, VEC>;
   constexpr int R = S::ROWS, T = S::THREADS, BYTES = RES ? Fx::ROW_RES : Fx::ROW, AHEAD = Fx::AHEAD;
   extern __shared__ __align__(16) char smem[];            // the rows on their way, then the waiting nodes [levels][4][T]
   float4* waiting = reinterpret_cast<float4*>(smem + (STAGED ? AHEAD * R * BYTES : 0));
+  __shared__ __align__(16) float rooms[VEC ? 1 : T / 32][VEC ? 4 : 256];
+  float* room = rooms[VEC ? 0 : threadIdx.x >> 5];
   __shared__ __align__(16) float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
@@ -280,7 +308,6 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::C
   const int leaves = (D + 255) >> 8;
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
-  if (partial && blockIdx.x == 0 && (int)threadIdx.x < 2 * ((D + 255) / 256)) tickets[threadIdx.x] = 0;   // for the kernel that follows
   // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
   float mu_next[R], rs_next[R], step_next[R];
   struct { int base, p, slot; } ahead = {(int)blockIdx.x * block, 0, 0};        // the pass to fetch next
@@ -310,14 +337,23 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::C
       const bool there = row < rows;
       mu_next[a] = there ? mean[row] : 0.0f;
       rs_next[a] = there ? rstd[row] : 0.0f;
-      if (KIND == LN_ACT8) step_next[a] = there && n > 0 ? a8_step(e8[(size_t)row * groups8 + e0 / A8_GROUP]) : 0.0f;
+      if (KIND == LN_ACT8 && VEC) step_next[a] = there && n > 0 ? a8_step(e8[(size_t)row * groups8 + e0 / A8_GROUP]) : 0.0f;
     }
   };
 #pragma unroll
   for (int k = 0; k < AHEAD - 1; ++k) fetch();
   statistics(blockIdx.x * block + mine);
   float g[8];
-  if (gamma) load8n<BF, VEC>(gamma, e0, n, g);
+  const int w0 = warp * 256, left = D - w0;              // the warp's first column, how many are left from there
+  if (gamma) {
+    if (VEC) {
+      load8n<BF>(gamma, e0, n, g);
+    } else {
+      uint32_t raw[8];
+      load_any<BF ? 2 : 4>(gamma, w0, left, raw);
+      deal_out(room, raw, g);
+    }
+  }
   float node[16];                                         // of this group's rows so far: 8 columns of dgamma, 8 of dbeta
   int slot = 0;
   bool odd = false;                                       // which half of leaf_s the pass uses
@@ -335,27 +371,33 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::C
     if (STAGED) fetch_wait<AHEAD - 1>();
     const char* place = smem + slot * R * BYTES;
     slot = slot + 1 == AHEAD ? 0 : slot + 1;
+    if (!VEC) {   // all loads first, then dealt out
+      uint32_t raw_dy[R][8], raw_x[R][8];
+#pragma unroll
+      for (int a = 0; a < R; ++a) {
+        const int l = first + a < rows ? left : 0;
+        load_any<BF ? 2 : 4>(dy, row_at(first + a, D, w0), l, raw_dy[a]);
+        load_any<KIND == LN_F32 ? 4 : (KIND == LN_BF16 ? 2 : 1)>(x, row_at(first + a, D, w0), l, raw_x[a]);
+        if (KIND == LN_ACT8) {   // the columns lane + 32 k are of one group for each k
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            raw_x[a][t] = __float_as_uint(fmul(__uint_as_float(raw_x[a][t]), l > 32 * t ? a8_step(e8[(size_t)(first + a) * groups8 + warp * 8 + t]) : 0.0f));
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < R; ++a) {
+        deal_out(room, raw_dy[a], w[a]);
+        deal_out(room, raw_x[a], xh[a]);
+      }
+    }
 #pragma unroll
     for (int a = 0; a < R; ++a) {
       const int row = first + a, m = row < rows ? n : 0;
       if (STAGED) row_take<BF, T>(place + a * BYTES, w[a]);
-      else load8n<BF, VEC>(dy, row_at(row, D, e0), m, w[a]);
-      if (KIND == LN_ACT8) {
-        uint2 c = make_uint2(0, 0);
-        if (STAGED) {
-          c = reinterpret_cast<const uint2*>(place + a * BYTES + T * Fx::DY)[threadIdx.x];
-        } else {
-          const int8_t* q = reinterpret_cast<const int8_t*>(x) + row_at(row, D, e0);
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-            if (t < m) (t < 4 ? c.x : c.y) |= (uint32_t)(uint8_t)q[t] << (8 * (t & 3));
-        }
-        a8_values8(c, step[a], xh[a]);
-      } else if (STAGED) {
-        row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
-      } else {
-        load8n<BF, VEC>(x, row_at(row, D, e0), m, xh[a]);
-      }
+      else if (VEC) load8n<BF>(dy, row_at(row, D, e0), m, w[a]);
+      if (STAGED && KIND == LN_ACT8) a8_values8(reinterpret_cast<const uint2*>(place + a * BYTES + T * Fx::DY)[threadIdx.x], step[a], xh[a]);
+      else if (STAGED) row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
+      else if (VEC) load8n<BF>(x, row_at(row, D, e0), m, xh[a]);
 #pragma unroll
       for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu[a]), rs[a]);
     }
@@ -417,12 +459,18 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::C
       for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
       if (RES) {   // the gradient that bypasses the norm (res may be dx)
         float b[8];
-        if (STAGED) row_take<BF, T>(place + a * BYTES + T * (Fx::DY + Fx::X), b);
-        else load8n<BF, VEC>(res, at, m, b);
+        if (STAGED) {
+          row_take<BF, T>(place + a * BYTES + T * (Fx::DY + Fx::X), b);
+        } else {
+          uint32_t raw[8];
+          load_any<BF ? 2 : 4>(res, row_at(first + a, D, w0), first + a < rows ? left : 0, raw);
+          deal_out(room, raw, b);
+        }
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = fadd(b[t], o[t]);
       }
-      store8n<BF, VEC>(dx, at, m, o);
+      if (!VEC) store_any<BF>(dx, row_at(first + a, D, w0), first + a < rows ? left : 0, room, o);
+      else if (m > 0) store8<BF>(dx, at, o);
     }
   }
   if (!partial) continue;
@@ -445,53 +493,55 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND>::THREADS, LnBwd<WPR, KIND>::C
   }
   if (grp == 0) {
     float* dst = partial + (size_t)blk * D + e0;
-    store8n<false, VEC>(dst, 0, n, node);
-    store8n<false, VEC>(dst + (size_t)nb * D, 0, n, node + 8);
+    if (!VEC) {
+      store_any<false>(dst - lane * 8, 0, left, room, node);
+      store_any<false>(dst - lane * 8 + (size_t)nb * D, 0, left, room, node + 8);
+    } else if (n > 0) {
+      store8<false>(dst, 0, node);
+      store8<false>(dst + (size_t)nb * D, 0, node + 8);
+    }
   }
   }
 }
 
-// The trees over the nb row blocks of every column of dgamma (z = 0) and dbeta (z = 1), 32 nodes a thread; the CTA
-// that completes a block of 256 columns goes on to the levels above for those columns, as in the RMSNorm's gain gradient.
-__global__ void __launch_bounds__(256) k_ln_cols(const float* __restrict__ partial, int nb, int D, float* __restrict__ upper,
-                                                 int nu, int* __restrict__ tickets, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ int last_s;
-  const int col = blockIdx.x * 256 + threadIdx.x, z = blockIdx.z;
-  float* out = z ? dbeta : dgamma;
+// The trees over the nb row blocks of every column of dgamma (y = 0) and dbeta (y = 1): a CTA has 32 columns, a warp 32 of 1024 adjacent nodes at a time
+// (independent loads), the first warp the tree over the warps' nodes; nodes of finished thousands wait as the digits of a binary counter do.
+__global__ void __launch_bounds__(1024) k_ln_cols(const float* __restrict__ partial, int nb, int D, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float nodes[32][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane;
+  float* out = blockIdx.y ? dbeta : dgamma;
   grid_dep();
   if (!out) return;
-  partial += (size_t)z * nb * D;
-  upper += (size_t)z * nu * D;
-  if (col < D) {
-    float s[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int b = blockIdx.y * 32 + i;
-      s[i] = b < nb ? partial[(size_t)b * D + col] : 0.0f;
-    }
-    upper[(size_t)blockIdx.y * D + col] = node_tree<32>(s, nb - blockIdx.y * 32);
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    last_s = atomicAdd(&tickets[2 * blockIdx.x + z], 1) == nu - 1;
-    __threadfence();
-  }
-  __syncthreads();
-  if (!last_s || col >= D) return;
-  int n = nu;
-  while (n > 1) {
-    const int groups = (n + 31) / 32;
-    for (int gg = 0; gg < groups; ++gg) {
+  partial += (size_t)blockIdx.y * nb * D;
+  float waiting[22], r = 0.0f;
+  const int thousands = (nb + 1023) / 1024;
+  for (int c = 0; c < thousands; ++c) {
+    const int first = c * 1024 + warp * 32, have = nb - first;
+    if (have > 0 && col < D) {
       float s[32];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) s[i] = gg * 32 + i < n ? __ldcg(&upper[(size_t)(gg * 32 + i) * D + col]) : 0.0f;
-      upper[(size_t)gg * D + col] = node_tree<32>(s, n - gg * 32);
+      for (int i = 0; i < 32; ++i) s[i] = i < have ? partial[(size_t)(first + i) * D + col] : 0.0f;
+      nodes[warp][lane] = node_tree<32>(s, have);
     }
-    n = groups;
+    __syncthreads();
+    if (warp == 0) {
+      float s[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i] = nodes[i][lane];
+      r = node_tree<32>(s, (nb - c * 1024 + 31) / 32);
+      int level = 0;
+      for (; (c >> level) & 1; ++level) r = fadd(waiting[level], r);
+      waiting[level] = r;
+    }
+    __syncthreads();
   }
+  if (warp || col >= D) return;
+  // what waits beside the last thousand's node, from the lowest level up: the nodes to their left
+  int level = 0;
+  while (((thousands - 1) >> level) & 1) ++level;
+  for (++level; (thousands >> level) != 0; ++level)
+    if ((thousands >> level) & 1) r = fadd(waiting[level], r);
   // the sum of one row is that row, carried up without an addition: flushed like every value that enters or leaves an operation
-  const float r = __ldcg(&upper[col]);
   out[col] = (__float_as_uint(r) & 0x7f800000u) ? r : __uint_as_float(__float_as_uint(r) & 0x80000000u);
 }
 
@@ -523,14 +573,14 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
           constexpr int W = decltype(wpr)::value;
           constexpr bool BF = decltype(is_bf)::value, VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
           if constexpr (BF || !RES) {
-            using S = LnShape<W>;
-            const int per = S::GROUPS * S::ROWS;
-            const size_t smem = VEC ? (size_t)S::AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : 0;
+            using S = LnShape<W, BF, VEC>;
+            const long long per = S::GROUPS * S::ROWS, blocks = (rows + per - 1) / per;
+            const size_t smem = S::AHEAD_ROWS ? (size_t)S::AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : (VEC ? 0 : (size_t)S::THREADS * 32);
             auto kern = k_ln_fwd<BF, W, VEC, RES>;
             static DevOnce once;
             if (smem > 40 * 1024) rc = dev_ensure_smem(once, (const void*)kern, smem);
             if (rc != DET_OK) return;
-            launch_after(kern, ln_grid(((long long)rows + per - 1) / per, S::CTAS), S::THREADS, smem, st, x, res, gamma, beta, rows, D, eps,
+            launch_after(kern, S::AHEAD_ROWS ? ln_grid(blocks, S::CTAS) : dim3((unsigned)blocks), S::THREADS, smem, st, x, res, gamma, beta, rows, D, eps,
                          (float)(1.0 / (double)D), sum, y, mean, rstd, s_q, qy, q8, e8);
           }
         });
@@ -548,7 +598,13 @@ struct LnBlock { int passes, rows; };
 template <int KIND>
 static LnBlock ln_block(int rows, int D) {
   int per = 0, levels = 0;
-  with_wpr(D, [&](auto wpr) { using S = LnBwd<decltype(wpr)::value, KIND>; per = S::GROUPS * S::ROWS; levels = S::LEVELS; });
+  with_wpr(D, [&](auto wpr) {
+    with_bool(D % 8 == 0, [&](auto is_vec) {
+      using S = LnBwd<decltype(wpr)::value, KIND, decltype(is_vec)::value>;
+      per = S::GROUPS * S::ROWS;
+      levels = S::LEVELS;
+    });
+  });
   int passes = 1;
   while (passes < (1 << levels) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
   return {passes, passes * per};
@@ -558,10 +614,8 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
                   const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
   const bool cols = dgamma || dbeta;
   const LnBlock block = ln_block<KIND>(rows, D);
-  const int passes = block.passes, nb = (int)(((long long)rows + block.rows - 1) / block.rows), nu = (nb + 31) / 32;
+  const int passes = block.passes, nb = (int)(((long long)rows + block.rows - 1) / block.rows);
   float* partial = cols ? (float*)ws : nullptr;
-  float* upper = cols ? partial + 2 * (size_t)nb * D : nullptr;
-  int* tickets = cols ? reinterpret_cast<int*>(upper + 2 * (size_t)nu * D) : nullptr;
   int rc = DET_OK;
   with_wpr(D, [&](auto wpr) {
     with_bool(D % 8 == 0, [&](auto is_vec) {
@@ -569,25 +623,25 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
         constexpr int W = decltype(wpr)::value;
         constexpr bool VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
         if constexpr (!(RES && KIND == LN_F32)) {
-          using S = LnBwd<W, KIND>;
+          using S = LnBwd<W, KIND, VEC>;
           int levels = 0;
           while ((1 << levels) < passes) ++levels;
           if (S::GROUPS > 1 && levels == 0) levels = 1;
-          const size_t ahead = VEC && S::AHEAD_ROWS ? (size_t)LnFetch<KIND, W>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W>::ROW_RES : LnFetch<KIND, W>::ROW) : 0;
+          const size_t ahead = S::AHEAD_ROWS ? (size_t)LnFetch<KIND, W, VEC>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W, VEC>::ROW_RES : LnFetch<KIND, W, VEC>::ROW) : 0;
           const size_t level = (size_t)16 * S::THREADS * sizeof(float);
           auto kern = k_ln_bwd<KIND, W, VEC, RES>;
           static DevOnce once;
           rc = dev_ensure_smem(once, (const void*)kern, ahead + S::LEVELS * level);
           if (rc != DET_OK) return;
           launch_after(kern, ln_grid(nb, S::CTAS), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
-                       (float)(1.0 / (double)D), nb, passes, res, dx, partial, tickets);
+                       (float)(1.0 / (double)D), nb, passes, res, dx, partial);
         }
       });
     });
   });
   if (rc != DET_OK) return rc;
   if (cols)
-    launch_after(k_ln_cols, dim3((D + 255) / 256, nu, 2), 256, 0, st, (const float*)partial, nb, D, upper, nu, tickets, dgamma, dbeta);
+    launch_after(k_ln_cols, dim3((D + 31) / 32, 2), 1024, 0, st, (const float*)partial, nb, D, dgamma, dbeta);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -623,8 +677,7 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
 extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
   if (rows <= 0 || D <= 0 || D > 8192) return 256;
   const int least = min(ln_block<LN_F32>(rows, D).rows, min(ln_block<LN_BF16>(rows, D).rows, ln_block<LN_ACT8>(rows, D).rows));
-  const size_t nb = ((size_t)rows + least - 1) / least, nu = (nb + 31) / 32;
-  return align_up(2 * (nb + nu) * (size_t)D * sizeof(float), 256) + 256;
+  return align_up(2 * (((size_t)rows + least - 1) / least) * (size_t)D * sizeof(float), 256);
 }
 
 // what the three backward calls have in common: checks, nothing to do, launch

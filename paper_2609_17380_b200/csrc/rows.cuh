@@ -45,31 +45,54 @@ __device__ __forceinline__ void store8(void* p, size_t idx, const float v[8]) {
     q[1] = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
-// The same for rows of any length and address (VEC false: element by element): the first n of them, n may be beyond 8 or negative.
-template <bool BF, bool VEC>
+// The same where the row may end: n columns of it are left from the lane's first on, a multiple of 8 or none.
+template <bool BF>
 __device__ __forceinline__ void load8n(const void* p, size_t idx, int n, float v[8]) {
-  if (VEC) {
-    if (n > 0) { load8<BF>(p, idx, v); return; }
+  if (n > 0) { load8<BF>(p, idx, v); return; }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = 0.0f;
-  } else {
+  for (int t = 0; t < 8; ++t) v[t] = 0.0f;
+}
+// Rows of any length and address: a warp's 256 columns are read lane by lane (column lane + 32 k: 64 or 128 adjacent bytes an instruction, where eight
+// adjacent values a lane touch sixteen times as many sectors) and dealt out through `room`, 256 floats of the warp's own.  `left` columns of
+// the row are left from the warp's first on, `base` is that one's index.  BYTES 1: codes.
+template <int BYTES>
+__device__ __forceinline__ void load_any(const void* p, size_t base, int left, uint32_t raw[8]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      v[t] = t < n ? (BF ? bf2f(reinterpret_cast<const uint16_t*>(p)[idx + t]) : reinterpret_cast<const float*>(p)[idx + t]) : 0.0f;
+  for (int k = 0; k < 8; ++k) {
+    const int e = lane + 32 * k;
+    raw[k] = 0u;
+    if (e < left) {
+      if (BYTES == 4) raw[k] = reinterpret_cast<const uint32_t*>(p)[base + e];
+      else if (BYTES == 2) raw[k] = (uint32_t)reinterpret_cast<const uint16_t*>(p)[base + e] << 16;
+      else raw[k] = __float_as_uint((float)reinterpret_cast<const int8_t*>(p)[base + e]);
+    }
   }
 }
-template <bool BF, bool VEC>
-__device__ __forceinline__ void store8n(void* p, size_t idx, int n, const float v[8]) {
-  if (VEC) {
-    if (n > 0) store8<BF>(p, idx, v);
-  } else {
+__device__ __forceinline__ void deal_out(float* room, const uint32_t raw[8], float v[8]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      if (t < n) {
-        if (BF) reinterpret_cast<uint16_t*>(p)[idx + t] = f2bf(v[t]);
-        else reinterpret_cast<float*>(p)[idx + t] = v[t];
-      }
+  for (int k = 0; k < 8; ++k) room[lane + 32 * k] = __uint_as_float(raw[k]);
+  __syncwarp();
+  const float4 a = reinterpret_cast<const float4*>(room)[2 * lane], b = reinterpret_cast<const float4*>(room)[2 * lane + 1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  __syncwarp();
+}
+template <bool BF>
+__device__ __forceinline__ void store_any(void* p, size_t base, int left, float* room, const float v[8]) {
+  const int lane = threadIdx.x & 31;
+  reinterpret_cast<float4*>(room)[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(room)[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int e = lane + 32 * k;
+    if (e < left) {
+      if (BF) reinterpret_cast<uint16_t*>(p)[base + e] = f2bf(room[e]);
+      else reinterpret_cast<float*>(p)[base + e] = room[e];
+    }
   }
+  __syncwarp();
 }
 
 // ---- values on their way: asynchronous copies into a place of the thread's own, so that nothing but the thread waits for them -----------
