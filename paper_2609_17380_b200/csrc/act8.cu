@@ -7,120 +7,250 @@
 
 namespace det {
 
-// Rows of a multiple of 8 columns, 16-byte aligned: a lane has eight adjacent values, four lanes a group.
+// i / d for i below 2^31 by a multiplication
+struct Divider {
+  uint32_t d, m;
+  int s;
+  explicit Divider(uint32_t n) : d(n), s(0) {
+    while ((1ull << s) < n) ++s;
+    m = (uint32_t)((((1ull << s) - n) << 32) / n) + 1;
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t i) const { return (__umulhi(i, m) + i) >> s; }
+};
+
+// Rows of a multiple of 8 columns, 16-byte aligned: a lane has eight adjacent values, four lanes a group; A8_EACH such pieces a thread, 256 apart, their
+// loads ahead of the rest.
+constexpr int A8_EACH = 4;
 template <bool BF>
-__global__ void __launch_bounds__(256) k_a8_pack(const void* __restrict__ x, size_t ld, int rows, int D, int8_t* __restrict__ q,
+__global__ void __launch_bounds__(256) k_a8_pack(const void* __restrict__ x, size_t ld, Divider lanes, uint32_t pieces, int D, int8_t* __restrict__ q,
                                                  uint8_t* __restrict__ e) {
   grid_dep();
-  const size_t lanes = (size_t)((D + A8_GROUP - 1) / A8_GROUP) * 4;          // per row, the last group's whole four included
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const size_t r = i / lanes, c = (i % lanes) * 8;
-  const bool have = r < (size_t)rows && c < (size_t)D;
-  float v[8];
-  load8n<BF>(x, r * ld + c, have, v);
-  const uint32_t field = a8_field(a8_quad_max(a8_amax8(v)));
-  if (!have) return;
-  *reinterpret_cast<uint2*>(q + r * D + c) = a8_codes8(v, field);
-  if ((i & 3) == 0) e[i / 4] = (uint8_t)field;
+  // lanes: pieces of a row, the last group's whole four included
+  const uint32_t first = blockIdx.x * (256 * A8_EACH) + threadIdx.x;
+  float v[A8_EACH][8];
+  uint32_t r[A8_EACH], c[A8_EACH];
+  bool have[A8_EACH];
+#pragma unroll
+  for (int k = 0; k < A8_EACH; ++k) {
+    const uint32_t i = first + 256 * k;
+    r[k] = lanes(i);
+    c[k] = (i - r[k] * lanes.d) * 8;
+    have[k] = i < pieces && c[k] < (uint32_t)D;
+    load8n<BF>(x, (size_t)r[k] * ld + c[k], have[k], v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < A8_EACH; ++k) {
+    const uint32_t field = a8_field(a8_quad_max(a8_amax8(v[k])));
+    if (!have[k]) continue;
+    *reinterpret_cast<uint2*>(q + (size_t)r[k] * D + c[k]) = a8_codes8(v[k], field);
+    if ((threadIdx.x & 3) == 0) e[(first + 256 * k) / 4] = (uint8_t)field;
+  }
 }
 template <bool BF>
-__global__ void __launch_bounds__(256) k_a8_unpack(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int rows, int D,
+__global__ void __launch_bounds__(256) k_a8_unpack(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, Divider lanes, uint32_t pieces, int D,
                                                    void* __restrict__ y, size_t ld) {
   grid_dep();
-  const size_t lanes = (size_t)D / 8;
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const size_t r = i / lanes, c = (i % lanes) * 8;
-  if (r >= (size_t)rows) return;
-  float v[8];
-  a8_values8(*reinterpret_cast<const uint2*>(q + r * D + c), a8_step(e[r * ((D + A8_GROUP - 1) / A8_GROUP) + c / A8_GROUP]), v);
-  store8<BF>(y, r * ld + c, v);
+  const uint32_t first = blockIdx.x * (256 * A8_EACH) + threadIdx.x;
+  uint2 codes[A8_EACH];
+  uint32_t r[A8_EACH], c[A8_EACH], field[A8_EACH];
+  bool have[A8_EACH];
+#pragma unroll
+  for (int k = 0; k < A8_EACH; ++k) {
+    const uint32_t i = first + 256 * k;
+    r[k] = lanes(i);
+    c[k] = (i - r[k] * lanes.d) * 8;
+    have[k] = i < pieces && c[k] < (uint32_t)D;
+    if (!have[k]) continue;
+    codes[k] = *reinterpret_cast<const uint2*>(q + (size_t)r[k] * D + c[k]);
+    field[k] = e[i / 4];
+  }
+#pragma unroll
+  for (int k = 0; k < A8_EACH; ++k) {
+    if (!have[k]) continue;
+    float v[8];
+    a8_values8(codes[k], a8_step(field[k]), v);
+    store8<BF>(y, (size_t)r[k] * ld + c[k], v);
+  }
 }
-// Any width, stride and address: a warp per group, a lane per value.
+// Any width, stride and address: a lane per value, a warp per group, A8_GROUPS of them one after the other with their loads ahead of the rest.
+constexpr int A8_GROUPS = 8;
 template <bool BF>
-__global__ void __launch_bounds__(256) k_a8_pack_any(const void* __restrict__ x, size_t ld, int rows, int D, int8_t* __restrict__ q,
+__global__ void __launch_bounds__(256) k_a8_pack_any(const void* __restrict__ x, size_t ld, Divider ng, uint32_t groups, int D, int8_t* __restrict__ q,
                                                      uint8_t* __restrict__ e) {
   grid_dep();
-  const size_t ng = (D + A8_GROUP - 1) / A8_GROUP, w = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const uint32_t first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * A8_GROUPS;
   const int lane = threadIdx.x & 31;
-  const size_t r = w / ng, c = (w % ng) * A8_GROUP + lane;
-  if (r >= (size_t)rows) return;
-  const bool have = c < (size_t)D;
-  const float v = have ? (BF ? bf2f(reinterpret_cast<const uint16_t*>(x)[r * ld + c]) : reinterpret_cast<const float*>(x)[r * ld + c]) : 0.0f;
-  const uint32_t field = a8_field(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
-  if (have) q[r * D + c] = (int8_t)(field != 255u ? __float_as_uint(fadd(fmul(v, a8_inv(field)), 12582912.0f)) : a8_code_nonfinite(v));
-  if (lane == 0) e[w] = (uint8_t)field;
+  float v[A8_GROUPS];
+  size_t at[A8_GROUPS];
+  bool have[A8_GROUPS];
+#pragma unroll
+  for (int k = 0; k < A8_GROUPS; ++k) {
+    const uint32_t r = ng(first + k), c = (first + k - r * ng.d) * A8_GROUP + lane;
+    have[k] = first + k < groups && c < (uint32_t)D;
+    at[k] = (size_t)r * D + c;
+    const size_t from = (size_t)r * ld + c;
+    v[k] = have[k] ? (BF ? bf2f(reinterpret_cast<const uint16_t*>(x)[from]) : reinterpret_cast<const float*>(x)[from]) : 0.0f;
+  }
+  uint32_t mine = 0;                                     // lane k keeps the field of group k
+#pragma unroll
+  for (int k = 0; k < A8_GROUPS; ++k) {
+    const uint32_t field = a8_field(__reduce_max_sync(0xffffffffu, __float_as_uint(v[k]) & 0x7fffffffu));
+    if (have[k]) q[at[k]] = (int8_t)(field != 255u ? __float_as_uint(fadd(fmul(v[k], a8_inv(field)), 12582912.0f)) : a8_code_nonfinite(v[k]));
+    if (lane == k) mine = field;
+  }
+  if (lane < A8_GROUPS && first + lane < groups) e[first + lane] = (uint8_t)mine;
 }
 template <bool BF>
-__global__ void __launch_bounds__(256) k_a8_unpack_any(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, int rows, int D,
+__global__ void __launch_bounds__(256) k_a8_unpack_any(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, Divider ng, uint32_t groups, int D,
                                                        void* __restrict__ y, size_t ld) {
   grid_dep();
-  const size_t ng = (D + A8_GROUP - 1) / A8_GROUP, w = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const size_t r = w / ng, c = (w % ng) * A8_GROUP + (threadIdx.x & 31);
-  if (r >= (size_t)rows || c >= (size_t)D) return;
-  const float v = fmul((float)q[r * D + c], a8_step(e[w]));
-  if (BF) reinterpret_cast<uint16_t*>(y)[r * ld + c] = f2bf(v);
-  else reinterpret_cast<float*>(y)[r * ld + c] = v;
+  const uint32_t first = (blockIdx.x * 8 + (threadIdx.x >> 5)) * A8_GROUPS;
+  const int lane = threadIdx.x & 31;
+  float v[A8_GROUPS];
+  size_t to[A8_GROUPS];
+  bool have[A8_GROUPS];
+  const uint32_t mine = lane < A8_GROUPS && first + lane < groups ? e[first + lane] : 0u;
+#pragma unroll
+  for (int k = 0; k < A8_GROUPS; ++k) {
+    const uint32_t r = ng(first + k), c = (first + k - r * ng.d) * A8_GROUP + lane;
+    have[k] = first + k < groups && c < (uint32_t)D;
+    to[k] = (size_t)r * ld + c;
+    v[k] = have[k] ? (float)q[(size_t)r * D + c] : 0.0f;
+  }
+#pragma unroll
+  for (int k = 0; k < A8_GROUPS; ++k) {
+    const float step = a8_step(__shfl_sync(0xffffffffu, mine, k));
+    if (!have[k]) continue;
+    if (BF) reinterpret_cast<uint16_t*>(y)[to[k]] = f2bf(fmul(v[k], step));
+    else reinterpret_cast<float*>(y)[to[k]] = fmul(v[k], step);
+  }
 }
 
 // ---- SwiGLU: gu [rows, 2F] = (gate | up), F a multiple of 32, so no group holds both -----------------------
-__device__ __forceinline__ float sigmoid_a8(float g) { return fdiv(1.0f, fadd(1.0f, det_exp(-g))); }
+// The gate is a bf16 either way, so its sigmoid has few values: 33 exponents of magnitude (below 2^-26 it is 1/2, from 128 on 1 or 0) of 128 fractions and two
+// signs.  They are evaluated by the compiler, with the steps of the formula, and looked up in shared memory: with an exponential and a division for every
+// value the three kernels took 160, 133 and 152 us for 8192 x 8192, bound by the arithmetic.
+constexpr int SG_LOW = 0x3280, SG_TOP = 0x4300, SG_TAB = (SG_TOP - SG_LOW + 1 + 3) / 4 * 4;
+struct __align__(16) SgTable { float v[2 * SG_TAB]; };     // of positive gates, of negative ones
+constexpr float sg_at(int bits, bool negative) {
+  float x = 1.0f + (bits & 127) / 128.0f;
+  for (int e = bits >> 7; e > 127; --e) x *= 2.0f;
+  for (int e = bits >> 7; e < 127; ++e) x *= 0.5f;
+  if (!negative) x = -x;
+  float e = 0.0f;                                          // exp(-gate)
+  if (x > 0x1.62e42ep+6f) return 0.0f;
+  if (x >= -0x1.5d58a0p+6f) {
+    float t = x * 0x1.715476p+0f;
+    t = t + 12582912.0f;
+    const float kf = t - 12582912.0f;
+    t = kf * 0x1.62e400p-1f;
+    float r = x - t;
+    t = kf * 0x1.7f7d1cp-20f;
+    r = r - t;
+    const float c[7] = {0x1.6c16c2p-10f, 0x1.111112p-7f, 0x1.555556p-5f, 0x1.555556p-3f, 0.5f, 1.0f, 1.0f};
+    e = 0x1.a01a02p-13f;
+    for (int i = 0; i < 7; ++i) {
+      t = e * r;
+      e = t + c[i];
+    }
+    for (int k = (int)kf; k < 0; ++k) e *= 0.5f;
+    for (int k = (int)kf; k > 0; --k) e *= 2.0f;
+  }
+  const float d = 1.0f + e, q = 1.0f / d;
+  return q < 0x1p-126f ? 0.0f : q;
+}
+constexpr SgTable sg_make_table() {
+  SgTable t{};
+  for (int i = 0; i < SG_TAB; ++i) {
+    t.v[i] = sg_at(SG_LOW + i, false);
+    t.v[SG_TAB + i] = sg_at(SG_LOW + i, true);
+  }
+  return t;
+}
+__device__ constexpr SgTable sg_table_image = sg_make_table();
 
-// FROM: gate and up come from the checkpoint (gu absent), else they come from gu and the checkpoint is written
-template <bool FROM>
-__global__ void __launch_bounds__(256) k_swiglu_fwd_a8(const uint16_t* __restrict__ gu, int8_t* q, uint8_t* e, int rows, int F,
-                                                       uint16_t* __restrict__ h, const float* __restrict__ s_q, int8_t* __restrict__ qh) {
+// the sigmoid of a gate; by table a NaN has that of an infinity, and what it is multiplied with, the gate itself, is the NaN
+template <bool TAB>
+__device__ __forceinline__ float sigmoid_a8(float g, const float* tab) {
+  if (!TAB) return fdiv(1.0f, fadd(1.0f, det_exp(-g)));
+  const uint32_t u = __float_as_uint(g);
+  const int i = __vimin_s32_relu((int)((u >> 14) & 0x1fffcu) - 4 * SG_LOW, 4 * (SG_TOP - SG_LOW)) + (int)(u >> 31) * (4 * SG_TAB);
+  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tab) + i);
+}
+template <bool TAB>
+__device__ __forceinline__ void sg_copy_table(float* tab) {
+  if (!TAB) return;
+  for (int i = threadIdx.x; i < 2 * SG_TAB / 4; i += 256) reinterpret_cast<float4*>(tab)[i] = reinterpret_cast<const float4*>(sg_table_image.v)[i];
+  __syncthreads();
+}
+// FROM: gate and up come from the checkpoint (gu absent), else they come from gu and the checkpoint is written.  A thread has eight adjacent gates and
+// their ups at a time; `pieces` of them are walked over by CTAs that stay (TAB) or there is a thread for each.
+template <bool FROM, bool TAB>
+__global__ void __launch_bounds__(256, 4) k_swiglu_fwd_a8(const uint16_t* __restrict__ gu, int8_t* q, uint8_t* e, Divider lanes, uint32_t pieces, int F,
+                                                          uint16_t* __restrict__ h, const float* __restrict__ s_q, int8_t* __restrict__ qh) {
+  __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
+  sg_copy_table<TAB>(tab);
   grid_dep();
-  const size_t lanes = (size_t)F / 8, i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const bool have = i < lanes * rows;
-  const size_t r = have ? i / lanes : 0, c = have ? (i % lanes) * 8 : 0, at = r * 2 * F + c;
-  float g[8], u[8], o[8];
-  if (FROM) {
-    if (!have) return;
-    a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
-    a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
-  } else {
-    load8n<true>(gu, at, have, g);
-    load8n<true>(gu, at + F, have, u);
-    const uint32_t fg = a8_field(a8_quad_max(a8_amax8(g))), fu = a8_field(a8_quad_max(a8_amax8(u)));
-    if (!have) return;
-    *reinterpret_cast<uint2*>(q + at) = a8_codes8(g, fg);
-    *reinterpret_cast<uint2*>(q + at + F) = a8_codes8(u, fu);
-    if ((i & 3) == 0) {
-      e[at / A8_GROUP] = (uint8_t)fg;
-      e[(at + F) / A8_GROUP] = (uint8_t)fu;
+  const float inv_q = qh ? fdiv(1.0f, s_q[0]) : 0.0f;
+  for (uint32_t base = blockIdx.x * 256; base < pieces; base += gridDim.x * 256) {
+    const uint32_t i = base + threadIdx.x;
+    const bool have = i < pieces;
+    const uint32_t r = have ? lanes(i) : 0, c = have ? (i - r * lanes.d) * 8 : 0;
+    const size_t at = (size_t)r * 2 * F + c;
+    float g[8], u[8], o[8];
+    if (FROM) {
+      if (!have) continue;
+      a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
+      a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
+    } else {
+      load8n<true>(gu, at, have, g);
+      load8n<true>(gu, at + F, have, u);
+      const uint32_t fg = a8_field(a8_quad_max(a8_amax8(g))), fu = a8_field(a8_quad_max(a8_amax8(u)));
+      if (!have) continue;
+      *reinterpret_cast<uint2*>(q + at) = a8_codes8(g, fg);
+      *reinterpret_cast<uint2*>(q + at + F) = a8_codes8(u, fu);
+      if ((i & 3) == 0) {
+        e[at / A8_GROUP] = (uint8_t)fg;
+        e[(at + F) / A8_GROUP] = (uint8_t)fu;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[t] = fmul(fmul(g[t], sigmoid_a8<TAB>(g[t], tab)), u[t]);
+    store8<true>(h, (size_t)r * F + c, o);
+    if (qh) {   // the next linear's quantiser, applied to the bf16 values just stored
+      round8(o);
+      *reinterpret_cast<uint2*>(qh + (size_t)r * F + c) = quant8(o, inv_q);
     }
   }
-#pragma unroll
-  for (int t = 0; t < 8; ++t) o[t] = fmul(fmul(g[t], sigmoid_a8(g[t])), u[t]);
-  store8<true>(h, r * F + c, o);
-  if (qh) {   // the next linear's quantiser, applied to the bf16 values just stored
-    const float inv_q = fdiv(1.0f, s_q[0]);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) o[t] = bf2f(f2bf(o[t]));
-    *reinterpret_cast<uint2*>(qh + r * F + c) = quant8(o, inv_q);
-  }
 }
-__global__ void __launch_bounds__(256) k_swiglu_bwd_a8(const uint16_t* __restrict__ dh, const int8_t* __restrict__ q,
-                                                       const uint8_t* __restrict__ e, int rows, int F, uint16_t* __restrict__ dgu) {
+template <bool TAB>
+__global__ void __launch_bounds__(256, 4) k_swiglu_bwd_a8(const uint16_t* __restrict__ dh, const int8_t* __restrict__ q, const uint8_t* __restrict__ e,
+                                                          Divider lanes, uint32_t pieces, int F, uint16_t* __restrict__ dgu) {
+  __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
+  sg_copy_table<TAB>(tab);
   grid_dep();
-  const size_t lanes = (size_t)F / 8, i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= lanes * rows) return;
-  const size_t r = i / lanes, c = (i % lanes) * 8, at = r * 2 * F + c;
-  float g[8], u[8], d[8], dg[8], du[8];
-  a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
-  a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
-  load8<true>(dh, r * F + c, d);
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
+    const uint32_t r = lanes(i), c = (i - r * lanes.d) * 8;
+    const size_t at = (size_t)r * 2 * F + c;
+    float g[8], u[8], d[8], dg[8], du[8];
+    a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
+    a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
+    load8<true>(dh, (size_t)r * F + c, d);
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const float sg = sigmoid_a8(g[t]);
-    du[t] = fmul(d[t], fmul(g[t], sg));
-    dg[t] = fmul(fmul(d[t], u[t]), fmul(sg, fadd(1.0f, fmul(g[t], fsub(1.0f, sg)))));
+    for (int t = 0; t < 8; ++t) {
+      const float sg = sigmoid_a8<TAB>(g[t], tab);
+      du[t] = fmul(d[t], fmul(g[t], sg));
+      dg[t] = fmul(fmul(d[t], u[t]), fmul(sg, fadd(1.0f, fmul(g[t], fsub(1.0f, sg)))));
+    }
+    store8<true>(dgu, at, dg);
+    store8<true>(dgu, at + F, du);
   }
-  store8<true>(dgu, at, dg);
-  store8<true>(dgu, at + F, du);
 }
 
-static unsigned blocks_for(size_t threads) { return (unsigned)((threads + 255) / 256); }
+static unsigned blocks_for(size_t n, size_t each) { return (unsigned)((n + each - 1) / each); }
+// SwiGLU: by table where every one of the CTAs that the GPU holds, four on an SM, has several pieces a thread (the table is 34 KiB to each)
+constexpr int SG_CTAS = 4;
+static bool sg_by_table(size_t pieces) { return pieces >= (size_t)SG_CTAS * dev_sm_count() * 256 * 2; }
 
 }  // namespace det
 
@@ -132,7 +262,7 @@ extern "C" size_t det_act8_exp_bytes(int rows, int D) {
 
 static int a8_check(int io, const void* x, int ld, int rows, int D, const void* q, const void* e) {
   if (!x || !q || !e || rows < 0 || D <= 0 || ld < D || (io != DET_F32 && io != DET_BF16)) return DET_ERR_ARG;
-  if ((size_t)rows * (((size_t)D + 31) / 32) > ((size_t)1 << 33)) return DET_ERR_SHAPE;      // blocks of 8 warps in a grid
+  if ((size_t)rows * (((size_t)D + 31) / 32) >= ((size_t)1 << 28)) return DET_ERR_SHAPE;      // four pieces a group, numbered in 31 bits
   if ((uintptr_t)x % (io == DET_BF16 ? 2 : 4)) return DET_ERR_ALIGN;
   return DET_OK;
 }
@@ -144,11 +274,13 @@ extern "C" int det_act8_pack(int io, const void* x, int ld, int rows, int D, int
   const int rc = a8_check(io, x, ld, rows, D, q8, e8);
   if (rc != DET_OK || rows == 0) return rc;
   cudaStream_t st = (cudaStream_t)stream;
-  const size_t groups = det_act8_exp_bytes(rows, D);
+  const uint32_t groups = (uint32_t)det_act8_exp_bytes(rows, D), ng = groups / rows;
   if (a8_vec(io, x, ld, D, q8))
-    launch_after(io == DET_BF16 ? k_a8_pack<true> : k_a8_pack<false>, blocks_for(groups * 4), 256, 0, st, x, (size_t)ld, rows, D, q8, e8);
+    launch_after(io == DET_BF16 ? k_a8_pack<true> : k_a8_pack<false>, blocks_for(groups * 4, 256 * A8_EACH), 256, 0, st, x, (size_t)ld, Divider(ng * 4),
+                 groups * 4, D, q8, e8);
   else
-    launch_after(io == DET_BF16 ? k_a8_pack_any<true> : k_a8_pack_any<false>, blocks_for(groups * 32), 256, 0, st, x, (size_t)ld, rows, D, q8, e8);
+    launch_after(io == DET_BF16 ? k_a8_pack_any<true> : k_a8_pack_any<false>, blocks_for(groups, 8 * A8_GROUPS), 256, 0, st, x, (size_t)ld, Divider(ng),
+                 groups, D, q8, e8);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -157,19 +289,29 @@ extern "C" int det_act8_unpack(int io, const int8_t* q8, const uint8_t* e8, int 
   const int rc = a8_check(io, y, ld, rows, D, q8, e8);
   if (rc != DET_OK || rows == 0) return rc;
   cudaStream_t st = (cudaStream_t)stream;
+  const uint32_t groups = (uint32_t)det_act8_exp_bytes(rows, D), ng = groups / rows;
   if (a8_vec(io, y, ld, D, q8))
-    launch_after(io == DET_BF16 ? k_a8_unpack<true> : k_a8_unpack<false>, blocks_for((size_t)rows * (D / 8)), 256, 0, st, q8, e8, rows, D, y, (size_t)ld);
+    launch_after(io == DET_BF16 ? k_a8_unpack<true> : k_a8_unpack<false>, blocks_for(groups * 4, 256 * A8_EACH), 256, 0, st, q8, e8, Divider(ng * 4),
+                 groups * 4, D, y, (size_t)ld);
   else
-    launch_after(io == DET_BF16 ? k_a8_unpack_any<true> : k_a8_unpack_any<false>, blocks_for(det_act8_exp_bytes(rows, D) * 32), 256, 0, st, q8, e8, rows, D, y, (size_t)ld);
+    launch_after(io == DET_BF16 ? k_a8_unpack_any<true> : k_a8_unpack_any<false>, blocks_for(groups, 8 * A8_GROUPS), 256, 0, st, q8, e8, Divider(ng), groups,
+                 D, y, (size_t)ld);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
 
 static int swiglu_a8_check(const void* a, const void* b, const int8_t* q8, const uint8_t* e8, int rows, int F) {
   if (!a || !b || !q8 || !e8 || rows < 0 || F <= 0) return DET_ERR_ARG;
-  if (F % 32 || F > (1 << 29) || (size_t)rows * (F / 8) > ((size_t)1 << 38)) return DET_ERR_SHAPE;
+  if (F % 32 || F > (1 << 29) || (size_t)rows * (F / 8) >= ((size_t)1 << 30)) return DET_ERR_SHAPE;
   if (!aligned16(a) || !aligned16(b) || ((uintptr_t)q8 & 7u)) return DET_ERR_ALIGN;
   return DET_OK;
+}
+template <bool FROM>
+static void swiglu_a8_fwd(const det_bf16* gu, int8_t* q8, uint8_t* e8, int rows, int F, det_bf16* h, const float* s_q, int8_t* qh, cudaStream_t st) {
+  const uint32_t pieces = (uint32_t)rows * (F / 8);
+  const bool tab = sg_by_table(pieces);
+  launch_after(tab ? k_swiglu_fwd_a8<FROM, true> : k_swiglu_fwd_a8<FROM, false>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, st, gu, q8,
+               e8, Divider(F / 8), pieces, F, h, s_q, qh);
 }
 extern "C" int det_swiglu_fwd_act8(const det_bf16* gu, int rows, int F, det_bf16* h, int8_t* q8, uint8_t* e8, const float* s_q, int8_t* qh,
                                    void* stream) {
@@ -178,7 +320,7 @@ extern "C" int det_swiglu_fwd_act8(const det_bf16* gu, int rows, int F, det_bf16
   if (qh && !s_q) return DET_ERR_ARG;
   if ((uintptr_t)qh & 7u) return DET_ERR_ALIGN;
   if (rows == 0) return DET_OK;
-  launch_after(k_swiglu_fwd_a8<false>, blocks_for((size_t)rows * (F / 8)), 256, 0, (cudaStream_t)stream, gu, q8, e8, rows, F, h, s_q, qh);
+  swiglu_a8_fwd<false>(gu, q8, e8, rows, F, h, s_q, qh, (cudaStream_t)stream);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -188,15 +330,17 @@ extern "C" int det_swiglu_act8(const int8_t* q8, const uint8_t* e8, int rows, in
   if (qh && !s_q) return DET_ERR_ARG;
   if ((uintptr_t)qh & 7u) return DET_ERR_ALIGN;
   if (rows == 0) return DET_OK;
-  launch_after(k_swiglu_fwd_a8<true>, blocks_for((size_t)rows * (F / 8)), 256, 0, (cudaStream_t)stream, nullptr, const_cast<int8_t*>(q8),
-               const_cast<uint8_t*>(e8), rows, F, h, s_q, qh);
+  swiglu_a8_fwd<true>(nullptr, const_cast<int8_t*>(q8), const_cast<uint8_t*>(e8), rows, F, h, s_q, qh, (cudaStream_t)stream);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
 extern "C" int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8, int rows, int F, det_bf16* dgu, void* stream) {
   const int rc = swiglu_a8_check(dh, dgu, q8, e8, rows, F);
   if (rc != DET_OK || rows == 0) return rc;
-  launch_after(k_swiglu_bwd_a8, blocks_for((size_t)rows * (F / 8)), 256, 0, (cudaStream_t)stream, dh, q8, e8, rows, F, dgu);
+  const uint32_t pieces = (uint32_t)rows * (F / 8);
+  const bool tab = sg_by_table(pieces);
+  launch_after(tab ? k_swiglu_bwd_a8<true> : k_swiglu_bwd_a8<false>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, (cudaStream_t)stream, dh,
+               q8, e8, Divider(F / 8), pieces, F, dgu);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }

@@ -124,7 +124,7 @@ __device__ __forceinline__ void leaf_sums(const float (&v)[N], float* out, int w
 }
 // the sum of a lane's eight terms
 template <bool VEC>
-__device__ __forceinline__ float lane_sum(const float v[8], int e0, int D) { return VEC ? tree8_full(v) : tree8(v, e0, D); }
+__device__ __forceinline__ float lane_sum(const float v[8], int e0, int D) { return VEC || e0 + 8 <= D ? tree8_full(v) : tree8(v, e0, D); }
 
 // Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (AHEAD passes, each thread its own
 // columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
   float* room = reinterpret_cast<float*>(smem) + (threadIdx.x >> 5) * 256;            // VEC false: of the warp
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
-  const bool full = (D & 255) == 0;
+  const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
   const int stride = gridDim.x * S::GROUPS * R;
   auto fetch = [&](int first, int slot) {
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
   __shared__ __align__(16) float leaf_s[2][S::GROUPS][R][2][WPR];
   const int grp = (threadIdx.x >> 5) / WPR, warp = (threadIdx.x >> 5) % WPR, lane = threadIdx.x & 31;
   const int e0 = warp * 256 + lane * 8, n = D - e0;
-  const bool full = (D & 255) == 0;
+  const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
