@@ -1060,7 +1060,7 @@ void orc_act8_pack(int bf, const void *x, int rows, int D, int8_t *q, uint8_t *e
       float m = 0.0f;
       int finite = 1;
       for (int j = lo; j < hi; ++j) {
-        float v = ld(bf, x, (size_t)r * D + j);
+        float v = ftz(ld(bf, x, (size_t)r * D + j));
         if (isnan(v) || isinf(v)) finite = 0;
         else if (fabsf(v) > m) m = fabsf(v);
       }
@@ -1068,7 +1068,7 @@ void orc_act8_pack(int bf, const void *x, int rows, int D, int8_t *q, uint8_t *e
       while (ldexp(127.0, E) < (double)m) ++E;
       e[(size_t)r * ng + g] = finite ? (uint8_t)(E + 127) : 255;
       for (int j = lo; j < hi; ++j) {
-        float v = ld(bf, x, (size_t)r * D + j);
+        float v = ftz(ld(bf, x, (size_t)r * D + j));
         if (finite) q[(size_t)r * D + j] = (int8_t)rint(ldexp((double)v, -E));
         else q[(size_t)r * D + j] = isinf(v) ? (v > 0 ? 127 : -127) : 0;
       }

@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(256) k_a8_unpack_any(const int8_t* __restrict_
 // The gate is a bf16 either way, so its sigmoid has few values: 33 exponents of magnitude (below 2^-26 it is 1/2, from 128 on 1 or 0) of 128 fractions and two
 // signs.  They are evaluated by the compiler, with the steps of the formula, and looked up in shared memory: with an exponential and a division for every
 // value the three kernels took 160, 133 and 152 us for 8192 x 8192, bound by the arithmetic.
-constexpr int SG_LOW = 0x3280, SG_TOP = 0x4300, SG_TAB = (SG_TOP - SG_LOW + 1 + 3) / 4 * 4;
+constexpr int SG_LOW = 0x3280, SG_TOP = 0x4300, SG_TAB = (SG_TOP - SG_LOW + 1 + 255) / 256 * 256;
 struct __align__(16) SgTable { float v[2 * SG_TAB]; };     // of positive gates, of negative ones
 constexpr float sg_at(int bits, bool negative) {
   float x = 1.0f + (bits & 127) / 128.0f;
@@ -159,52 +159,95 @@ constexpr float sg_at(int bits, bool negative) {
   const float d = 1.0f + e, q = 1.0f / d;
   return q < 0x1p-126f ? 0.0f : q;
 }
+// Where entry i lies: a code below 64 has fractions that end in zeros, and in order of the magnitude they would meet in a few banks of shared memory.
+constexpr int sg_place(int i) { return i ^ ((i >> 3) & 31); }
 constexpr SgTable sg_make_table() {
   SgTable t{};
   for (int i = 0; i < SG_TAB; ++i) {
-    t.v[i] = sg_at(SG_LOW + i, false);
-    t.v[SG_TAB + i] = sg_at(SG_LOW + i, true);
+    t.v[sg_place(i)] = sg_at(SG_LOW + i, false);
+    t.v[SG_TAB + sg_place(i)] = sg_at(SG_LOW + i, true);
   }
   return t;
 }
 __device__ constexpr SgTable sg_table_image = sg_make_table();
 
 // the sigmoid of a gate; by table a NaN has that of an infinity, and what it is multiplied with, the gate itself, is the NaN
-template <bool TAB>
+// (TAB 0: by the formula, 1: by table in order, for gates with any fractions, 2: by table in its places)
+template <int TAB>
 __device__ __forceinline__ float sigmoid_a8(float g, const float* tab) {
   if (!TAB) return fdiv(1.0f, fadd(1.0f, det_exp(-g)));
   const uint32_t u = __float_as_uint(g);
-  const int i = __vimin_s32_relu((int)((u >> 14) & 0x1fffcu) - 4 * SG_LOW, 4 * (SG_TOP - SG_LOW)) + (int)(u >> 31) * (4 * SG_TAB);
-  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tab) + i);
+  int i = __vimin_s32_relu((int)((u >> 14) & 0x1fffcu) - 4 * SG_LOW, 4 * (SG_TOP - SG_LOW));           // in bytes
+  if (TAB == 2) i ^= (i >> 3) & 0x7c;
+  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tab) + i + (int)(u >> 31) * (4 * SG_TAB));
 }
-template <bool TAB>
+template <int TAB>
 __device__ __forceinline__ void sg_copy_table(float* tab) {
   if (!TAB) return;
-  for (int i = threadIdx.x; i < 2 * SG_TAB / 4; i += 256) reinterpret_cast<float4*>(tab)[i] = reinterpret_cast<const float4*>(sg_table_image.v)[i];
+  for (int i = threadIdx.x; i < 2 * SG_TAB / 4; i += 256) {
+    const float4 v = reinterpret_cast<const float4*>(sg_table_image.v)[i];
+    if (TAB == 2) {
+      reinterpret_cast<float4*>(tab)[i] = v;
+    } else {   // SG_TAB is a multiple of 256, so a place is undone in either half alike
+      const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        int at = 4 * i + k;
+        at ^= (at >> 3) & 28;                            // undoes the upper three of the five bits, which the lower two came from
+        at ^= (at >> 3) & 3;
+        tab[at] = w[k];
+      }
+    }
+  }
   __syncthreads();
 }
+// Eight adjacent gates and their ups on their way: of gu, or codes and fields of the checkpoint; dh beside them in the backward pass.
+struct SgRaw {
+  uint4 g, u, d;
+  uint32_t fg, fu;
+};
 // FROM: gate and up come from the checkpoint (gu absent), else they come from gu and the checkpoint is written.  A thread has eight adjacent gates and
-// their ups at a time; `pieces` of them are walked over by CTAs that stay (TAB) or there is a thread for each.
-template <bool FROM, bool TAB>
+// their ups at a time, the next ones on their way; `pieces` of them are walked over by CTAs that stay (TAB) or there is a thread for each.
+template <bool FROM, int TAB>
 __global__ void __launch_bounds__(256, 4) k_swiglu_fwd_a8(const uint16_t* __restrict__ gu, int8_t* q, uint8_t* e, Divider lanes, uint32_t pieces, int F,
                                                           uint16_t* __restrict__ h, const float* __restrict__ s_q, int8_t* __restrict__ qh) {
   __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
   sg_copy_table<TAB>(tab);
   grid_dep();
   const float inv_q = qh ? fdiv(1.0f, s_q[0]) : 0.0f;
-  for (uint32_t base = blockIdx.x * 256; base < pieces; base += gridDim.x * 256) {
+  const uint32_t step = gridDim.x * 256;
+  auto fetch = [&](uint32_t i) {
+    SgRaw w = {};
+    if (i >= pieces) return w;
+    const uint32_t r = lanes(i), c = (i - r * lanes.d) * 8;
+    const size_t at = (size_t)r * 2 * F + c;
+    if (FROM) {
+      const uint2 a = *reinterpret_cast<const uint2*>(q + at), b = *reinterpret_cast<const uint2*>(q + at + F);
+      w.g.x = a.x; w.g.y = a.y; w.u.x = b.x; w.u.y = b.y;
+      w.fg = e[at / A8_GROUP];
+      w.fu = e[(at + F) / A8_GROUP];
+    } else {
+      w.g = *reinterpret_cast<const uint4*>(gu + at);
+      w.u = *reinterpret_cast<const uint4*>(gu + at + F);
+    }
+    return w;
+  };
+  SgRaw next = fetch(blockIdx.x * 256 + threadIdx.x);
+  for (uint32_t base = blockIdx.x * 256; base < pieces; base += step) {
     const uint32_t i = base + threadIdx.x;
+    const SgRaw now = next;
+    if (TAB) next = fetch(i + step);
     const bool have = i < pieces;
     const uint32_t r = have ? lanes(i) : 0, c = have ? (i - r * lanes.d) * 8 : 0;
-    const size_t at = (size_t)r * 2 * F + c;
     float g[8], u[8], o[8];
     if (FROM) {
       if (!have) continue;
-      a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
-      a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
+      a8_values8(make_uint2(now.g.x, now.g.y), a8_step(now.fg), g);
+      a8_values8(make_uint2(now.u.x, now.u.y), a8_step(now.fu), u);
     } else {
-      load8n<true>(gu, at, have, g);
-      load8n<true>(gu, at + F, have, u);
+      const size_t at = (size_t)r * 2 * F + c;
+      unpack8(now.g, g);
+      unpack8(now.u, u);
       const uint32_t fg = a8_field(a8_quad_max(a8_amax8(g))), fu = a8_field(a8_quad_max(a8_amax8(u)));
       if (!have) continue;
       *reinterpret_cast<uint2*>(q + at) = a8_codes8(g, fg);
@@ -223,19 +266,36 @@ __global__ void __launch_bounds__(256, 4) k_swiglu_fwd_a8(const uint16_t* __rest
     }
   }
 }
-template <bool TAB>
+template <int TAB>
 __global__ void __launch_bounds__(256, 4) k_swiglu_bwd_a8(const uint16_t* __restrict__ dh, const int8_t* __restrict__ q, const uint8_t* __restrict__ e,
                                                           Divider lanes, uint32_t pieces, int F, uint16_t* __restrict__ dgu) {
   __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
   sg_copy_table<TAB>(tab);
   grid_dep();
-  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
+  const uint32_t step = gridDim.x * 256;
+  auto fetch = [&](uint32_t i) {
+    SgRaw w = {};
+    if (i >= pieces) return w;
+    const uint32_t r = lanes(i), c = (i - r * lanes.d) * 8;
+    const size_t at = (size_t)r * 2 * F + c;
+    const uint2 a = *reinterpret_cast<const uint2*>(q + at), b = *reinterpret_cast<const uint2*>(q + at + F);
+    w.g.x = a.x; w.g.y = a.y; w.u.x = b.x; w.u.y = b.y;
+    w.fg = e[at / A8_GROUP];
+    w.fu = e[(at + F) / A8_GROUP];
+    w.d = *reinterpret_cast<const uint4*>(dh + (size_t)r * F + c);
+    return w;
+  };
+  uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  SgRaw next = fetch(i);
+  for (; i < pieces; i += step) {
+    const SgRaw now = next;
+    if (TAB) next = fetch(i + step);
     const uint32_t r = lanes(i), c = (i - r * lanes.d) * 8;
     const size_t at = (size_t)r * 2 * F + c;
     float g[8], u[8], d[8], dg[8], du[8];
-    a8_values8(*reinterpret_cast<const uint2*>(q + at), a8_step(e[at / A8_GROUP]), g);
-    a8_values8(*reinterpret_cast<const uint2*>(q + at + F), a8_step(e[(at + F) / A8_GROUP]), u);
-    load8<true>(dh, (size_t)r * F + c, d);
+    a8_values8(make_uint2(now.g.x, now.g.y), a8_step(now.fg), g);
+    a8_values8(make_uint2(now.u.x, now.u.y), a8_step(now.fu), u);
+    unpack8(now.d, d);
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       const float sg = sigmoid_a8<TAB>(g[t], tab);
@@ -310,7 +370,7 @@ template <bool FROM>
 static void swiglu_a8_fwd(const det_bf16* gu, int8_t* q8, uint8_t* e8, int rows, int F, det_bf16* h, const float* s_q, int8_t* qh, cudaStream_t st) {
   const uint32_t pieces = (uint32_t)rows * (F / 8);
   const bool tab = sg_by_table(pieces);
-  launch_after(tab ? k_swiglu_fwd_a8<FROM, true> : k_swiglu_fwd_a8<FROM, false>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, st, gu, q8,
+  launch_after(tab ? k_swiglu_fwd_a8<FROM, FROM ? 2 : 1> : k_swiglu_fwd_a8<FROM, 0>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, st, gu, q8,
                e8, Divider(F / 8), pieces, F, h, s_q, qh);
 }
 extern "C" int det_swiglu_fwd_act8(const det_bf16* gu, int rows, int F, det_bf16* h, int8_t* q8, uint8_t* e8, const float* s_q, int8_t* qh,
@@ -339,7 +399,7 @@ extern "C" int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const u
   if (rc != DET_OK || rows == 0) return rc;
   const uint32_t pieces = (uint32_t)rows * (F / 8);
   const bool tab = sg_by_table(pieces);
-  launch_after(tab ? k_swiglu_bwd_a8<true> : k_swiglu_bwd_a8<false>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, (cudaStream_t)stream, dh,
+  launch_after(tab ? k_swiglu_bwd_a8<2> : k_swiglu_bwd_a8<0>, tab ? SG_CTAS * dev_sm_count() : blocks_for(pieces, 256), 256, 0, (cudaStream_t)stream, dh,
                q8, e8, Divider(F / 8), pieces, F, dgu);
   DET_CHECK_LAUNCH();
   return DET_OK;

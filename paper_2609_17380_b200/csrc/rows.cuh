@@ -19,6 +19,10 @@ __device__ __forceinline__ void round8(float v[8]) {
     v[t + 1] = bfhi(u);
   }
 }
+__device__ __forceinline__ void unpack8(const uint4& u, float v[8]) {
+  v[0] = bflo(u.x); v[1] = bfhi(u.x); v[2] = bflo(u.y); v[3] = bfhi(u.y);
+  v[4] = bflo(u.z); v[5] = bfhi(u.z); v[6] = bflo(u.w); v[7] = bfhi(u.w);
+}
 // element `col` of row `row` of rows of D
 __device__ __forceinline__ size_t row_at(int row, int D, int col) { return (size_t)((unsigned long long)(unsigned)row * (unsigned)D) + col; }
 template <bool BF>

@@ -217,7 +217,7 @@ def test_act8_at_odd_addresses(det):
         assert not got[:off].any() and not got[off + rows * D:].any()
 
 
-@pytest.mark.parametrize("rows,Fd", [(1, 32), (37, 1024), (5, 96), (129, 512), (1000, 64), (3, 8192), (2000, 1056)])
+@pytest.mark.parametrize("rows,Fd", [(1, 32), (37, 1024), (5, 96), (129, 512), (1000, 64), (3, 8192), (2000, 1056), (1300, 2112)])
 def test_swiglu_from_checkpoint(det, rows, Fd):
     gu = synth.normal_bf16((rows, 2 * Fd), 2.0, seed=71, tid=1)
     gu[0, :4] = synth.to_bf16(np.array([-200.0, 200.0, 90.0, -90.0], F))
@@ -256,6 +256,33 @@ def test_swiglu_from_checkpoint_every_gate(det):
     _sync()
     kept = oracle.act8_unpack(q, e)
     same(host(h, np.uint16), oracle.swiglu_fwd(kept), "h")
+    same(host(dgu, np.uint16), oracle.swiglu_bwd(dh, kept), "dgu")
+
+
+def test_swiglu_by_table_every_gate(det):
+    """Rows enough for the table: every bf16 as the gate of the forward pass, every code and step as that of the others."""
+    rows, Fd = 1300, 2112
+    g = np.arange(rows * Fd, dtype=np.uint32).astype(np.uint16).reshape(rows, Fd)
+    up, dh = synth.normal_bf16((rows, Fd), 1.0, seed=74, tid=1), synth.normal_bf16((rows, Fd), 1.0, seed=74, tid=2)
+    gu = np.concatenate([g, up], 1)
+    h, q, e = empty((rows, Fd), np.uint16), empty((rows, 2 * Fd), np.int8), empty((rows, 2 * Fd // 32), np.uint8)
+    det.det_swiglu_fwd_act8(dev(gu), rows, Fd, h, q, e)
+    _sync()
+    oq, oe = oracle.act8_pack(gu)
+    same(host(q), oq, "codes")
+    same(host(e), oe, "steps")
+    same(host(h, np.uint16), oracle.swiglu_fwd(gu), "h")
+    n = Fd // 32
+    codes = (np.arange(rows * Fd) % 255 - 127).astype(np.int8).reshape(rows, Fd)
+    steps = (np.arange(rows * n) % 250).astype(np.uint8).reshape(rows, n)
+    steps[steps == 0] = 255
+    q8, e8 = np.concatenate([codes, oq[:, Fd:]], 1), np.concatenate([steps, oe[:, n:]], 1)
+    again, dgu = empty((rows, Fd), np.uint16), empty((rows, 2 * Fd), np.uint16)
+    det.det_swiglu_act8(dev(q8), dev(e8), rows, Fd, again)
+    det.det_swiglu_bwd_act8(dev(dh), dev(q8), dev(e8), rows, Fd, dgu)
+    _sync()
+    kept = oracle.act8_unpack(q8, e8)
+    same(host(again, np.uint16), oracle.swiglu_fwd(kept), "h again")
     same(host(dgu, np.uint16), oracle.swiglu_bwd(dh, kept), "dgu")
 
 
