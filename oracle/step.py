@@ -27,48 +27,87 @@ def _window(cfg, l):
 def _specs(cfg):
     D, Fh, V, L = cfg["d_model"], cfg["ffn"], cfg["vocab"], cfg["n_layers"]
     nq = D + 2 * 128 * _kv(cfg)
+    shift = ("", "_shift") if _layer(cfg) else ("",)
+    norm = lambda name: [(name + part, (D,)) for part in shift]
     s = [("embed", (V, D))]
     if cfg.get("embed_norm"):
-        s += [("embed_norm", (D,))]
+        s += norm("embed_norm")
     for l in range(L):
-        s += [("l%d.attn_norm" % l, (D,)), ("l%d.w_qkv" % l, (nq, D)), ("l%d.w_o" % l, (D, D)),
-              ("l%d.ffn_norm" % l, (D,)), ("l%d.w_gu" % l, (2 * Fh, D)), ("l%d.w_down" % l, (D, Fh)),
-              ("l%d.s_x" % l, (4,))]
-    return s + [("final_norm", (D,)), ("lm_head", (V, D))]
+        s += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (2 * D if _recurrent(cfg, l) else nq, D)), ("l%d.w_o" % l, (D, D))]
+        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D)), ("l%d.w_down" % l, (D, Fh)), ("l%d.s_x" % l, (4,))]
+    return s + norm("final_norm") + [("lm_head", (V, D))]
+
+
+def _layer(cfg):
+    return cfg.get("norm", "rms") == "layer"
+
+
+def _recurrent(cfg, l):
+    return l in cfg.get("recurrent", ())
+
+
+def _norm(cfg, P, name, x):
+    """The norm's output and its statistics (mean, rstd; no mean for RMSNorm)."""
+    if _layer(cfg):
+        y, mean, rstd = O.layernorm_fwd(x, P[name], P[name + "_shift"], 1e-6, bf=True)
+        return y, (mean, rstd)
+    y, rstd = O.rmsnorm_fwd(x, P[name], 1e-6, bf=True)
+    return y, (None, rstd)
+
+
+def _norm_bwd(cfg, P, G, name, dy, x, stat, past=None):
+    """Gradient of the norm's input, with that of what bypasses it (past) added; gain's and shift's go to G."""
+    if _layer(cfg):
+        dx, G[name], G[name + "_shift"] = O.layernorm_bwd(dy, x, P[name], stat[0], stat[1], past, bf=True)
+        return dx
+    dx, G[name] = O.rmsnorm_bwd(dy, x, P[name], stat[1], bf=True)
+    return dx if past is None else O.residual_add(past, dx)
+
+
+def _kept(cfg, x):
+    """What the backward pass has of an activation: itself, or what its 8-bit checkpoint stands for."""
+    return O.act8_unpack(*O.act8_pack(x)) if cfg.get("act8") else x
+
+
+def _attention(cfg, l, a, rope):
+    H, S, B, D, Hkv = cfg["n_heads"], cfg["seq"], cfg["micro_batch"], cfg["d_model"], _kv(cfg)
+    # the paper's block: gain-free RMS norm of every query and key head, then the rotary embedding
+    qk = np.ascontiguousarray(a["qkv"][:, :D + 128 * Hkv]).reshape(-1, 128)
+    if cfg.get("qk_norm"):
+        a["qk_pre"] = qk
+        qk, a["rstd_qk"] = O.rmsnorm_fwd(qk, None, 1e-6, bf=True)
+    if rope is not None:
+        qk = O.rope(qk.reshape(B * S, H + Hkv, 128), S, rope[0], rope[1]).reshape(-1, 128)
+    a["qkr"] = np.ascontiguousarray(np.concatenate([qk.reshape(B * S, -1), a["qkv"][:, D + 128 * Hkv:]], 1))
+    a["att"], a["lse"] = O.attn_fwd(a["qkr"], B, H, S, Hkv=Hkv, window=_window(cfg, l), int8_pv=bool(cfg.get("pv_int8")))
 
 
 def forward(cfg, P, sw, tok, calibrate=False):
     """Returns (saved activations, loss pieces).  With calibrate, every activation step is set from its input."""
-    L, H, S, B = cfg["n_layers"], cfg["n_heads"], cfg["seq"], cfg["micro_batch"]
-    Hkv, D = _kv(cfg), cfg["d_model"]
+    L, S, B = cfg["n_layers"], cfg["seq"], cfg["micro_batch"]
     inp = tok[:, :-1].reshape(-1)
     x = O.embed_fwd(inp, P["embed"])
     saved = {"inp": inp, "layers": []}
     if cfg.get("embed_norm"):
         saved["x_emb"] = x
-        x, saved["rstd_emb"] = O.rmsnorm_fwd(x, P["embed_norm"], 1e-6, bf=True)
+        x, saved["stat_emb"] = _norm(cfg, P, "embed_norm", x)
     rope = cfg.get("rope_tables")
     for l in range(L):
         sx = P["l%d.s_x" % l]
         a = {"x": x}
-        a["n1"], a["rstd1"] = O.rmsnorm_fwd(x, P["l%d.attn_norm" % l], 1e-6, bf=True)
+        a["n1"], a["stat1"] = _norm(cfg, P, "l%d.attn_norm" % l, x)
         if calibrate:
             sx[0] = O.lsq_act_scale_init(a["n1"])[0]
         a["qkv"], _, _ = O.linear_fwd(a["n1"], P["l%d.w_qkv" % l], sx[0:1], sw["l%d.w_qkv" % l])
-        # the paper's block: gain-free RMS norm of every query and key head, then the rotary embedding
-        qk = np.ascontiguousarray(a["qkv"][:, :D + 128 * Hkv]).reshape(-1, 128)
-        if cfg.get("qk_norm"):
-            a["qk_pre"] = qk
-            qk, a["rstd_qk"] = O.rmsnorm_fwd(qk, None, 1e-6, bf=True)
-        if rope is not None:
-            qk = O.rope(qk.reshape(B * S, H + Hkv, 128), S, rope[0], rope[1]).reshape(-1, 128)
-        a["qkr"] = np.ascontiguousarray(np.concatenate([qk.reshape(B * S, -1), a["qkv"][:, D + 128 * Hkv:]], 1))
-        a["att"], a["lse"] = O.attn_fwd(a["qkr"], B, H, S, Hkv=Hkv, window=_window(cfg, l), int8_pv=bool(cfg.get("pv_int8")))
+        if _recurrent(cfg, l):
+            a["att"], _, a["states"] = O.linrec_fwd(a["qkv"], B, S)
+        else:
+            _attention(cfg, l, a, rope)
         if calibrate:
             sx[1] = O.lsq_act_scale_init(a["att"])[0]
         o, _, _ = O.linear_fwd(a["att"], P["l%d.w_o" % l], sx[1:2], sw["l%d.w_o" % l])
         a["h"] = O.residual_add(x, o)
-        a["n2"], a["rstd2"] = O.rmsnorm_fwd(a["h"], P["l%d.ffn_norm" % l], 1e-6, bf=True)
+        a["n2"], a["stat2"] = _norm(cfg, P, "l%d.ffn_norm" % l, a["h"])
         if calibrate:
             sx[2] = O.lsq_act_scale_init(a["n2"])[0]
         a["gu"], _, _ = O.linear_fwd(a["n2"], P["l%d.w_gu" % l], sx[2:3], sw["l%d.w_gu" % l])
@@ -79,17 +118,29 @@ def forward(cfg, P, sw, tok, calibrate=False):
         x = O.residual_add(a["h"], dn)
         saved["layers"].append(a)
     saved["xf"] = x
-    saved["nf"], saved["rstdf"] = O.rmsnorm_fwd(x, P["final_norm"], 1e-6, bf=True)
+    saved["nf"], saved["statf"] = _norm(cfg, P, "final_norm", x)
     # arithmetic version 2 (cfg["arith"] == 2) replaces the LM-head contractions by the order-free ones of oracle/v2
     saved["logits"] = (O2 if cfg.get("arith", 1) == 2 else O).lmhead_fwd(saved["nf"], P["lm_head"])
     return saved
 
 
+def _attention_bwd(cfg, l, a, d_att, rope):
+    H, S, B, D, Hkv = cfg["n_heads"], cfg["seq"], cfg["micro_batch"], cfg["d_model"], _kv(cfg)
+    d_qkv = O.attn_bwd(d_att, a["qkr"], a["att"], a["lse"], B, H, S, Hkv=Hkv, window=_window(cfg, l),
+                       fixq=bool(cfg.get("dq_fixed")))
+    dqk = np.ascontiguousarray(d_qkv[:, :D + 128 * Hkv]).reshape(-1, 128)
+    if rope is not None:
+        dqk = O.rope(dqk.reshape(B * S, H + Hkv, 128), S, rope[0], rope[1], inverse=True).reshape(-1, 128)
+    if cfg.get("qk_norm"):
+        dqk, _ = O.rmsnorm_bwd(dqk, a["qk_pre"], None, a["rstd_qk"], bf=True)
+    return np.ascontiguousarray(np.concatenate([dqk.reshape(B * S, -1), d_qkv[:, D + 128 * Hkv:]], 1))
+
+
 def microbatch_grad(cfg, P, sw, tok):
     """Forward + backward of one micro-batch; returns (flat f32 gradient in canonical order, mean loss)."""
-    L, H, S, B = cfg["n_layers"], cfg["n_heads"], cfg["seq"], cfg["micro_batch"]
+    L, S, B = cfg["n_layers"], cfg["seq"], cfg["micro_batch"]
     hb = cfg.get("hadamard_block", 128)
-    Hkv, D, rope = _kv(cfg), cfg["d_model"], cfg.get("rope_tables")
+    rope = cfg.get("rope_tables")
     sv = forward(cfg, P, sw, tok)
     labels = tok[:, 1:].reshape(-1).astype(np.int32)
     T = labels.size
@@ -97,32 +148,28 @@ def microbatch_grad(cfg, P, sw, tok):
     dlog = O.xent_bwd(sv["logits"], labels, lse, cfg.get("z_weight", 0.0), np.float32(1.0 / T))
     G = {}
     d_nf, G["lm_head"] = (O2 if cfg.get("arith", 1) == 2 else O).lmhead_bwd(dlog, sv["nf"], P["lm_head"])
-    dx, G["final_norm"] = O.rmsnorm_bwd(d_nf, sv["xf"], P["final_norm"], sv["rstdf"], bf=True)
+    dx = _norm_bwd(cfg, P, G, "final_norm", d_nf, sv["xf"], sv["statf"])
     for l in reversed(range(L)):
         a = sv["layers"][l]
         sx = P["l%d.s_x" % l]
         ds = np.zeros(4, np.float32)
-        d_act, G["l%d.w_down" % l], d3 = O.linear_bwd(dx, a["act"], P["l%d.w_down" % l], sx[3:4], sw["l%d.w_down" % l], hb)
-        d_gu = O.swiglu_bwd(d_act, a["gu"])
+        gu = _kept(cfg, a["gu"])
+        act = O.swiglu_fwd(gu) if cfg.get("act8") else a["act"]         # made again from what was kept
+        d_act, G["l%d.w_down" % l], d3 = O.linear_bwd(dx, act, P["l%d.w_down" % l], sx[3:4], sw["l%d.w_down" % l], hb)
+        d_gu = O.swiglu_bwd(d_act, gu)
         d_n2, G["l%d.w_gu" % l], d2 = O.linear_bwd(d_gu, a["n2"], P["l%d.w_gu" % l], sx[2:3], sw["l%d.w_gu" % l], hb)
-        d_h2, G["l%d.ffn_norm" % l] = O.rmsnorm_bwd(d_n2, a["h"], P["l%d.ffn_norm" % l], a["rstd2"], bf=True)
-        d_h = O.residual_add(dx, d_h2)
+        d_h = _norm_bwd(cfg, P, G, "l%d.ffn_norm" % l, d_n2, _kept(cfg, a["h"]), a["stat2"], dx)
         d_att, G["l%d.w_o" % l], d1 = O.linear_bwd(d_h, a["att"], P["l%d.w_o" % l], sx[1:2], sw["l%d.w_o" % l], hb)
-        d_qkv = O.attn_bwd(d_att, a["qkr"], a["att"], a["lse"], B, H, S, Hkv=Hkv, window=_window(cfg, l),
-                           fixq=bool(cfg.get("dq_fixed")))
-        dqk = np.ascontiguousarray(d_qkv[:, :D + 128 * Hkv]).reshape(-1, 128)
-        if rope is not None:
-            dqk = O.rope(dqk.reshape(B * S, H + Hkv, 128), S, rope[0], rope[1], inverse=True).reshape(-1, 128)
-        if cfg.get("qk_norm"):
-            dqk, _ = O.rmsnorm_bwd(dqk, a["qk_pre"], None, a["rstd_qk"], bf=True)
-        d_qkv = np.ascontiguousarray(np.concatenate([dqk.reshape(B * S, -1), d_qkv[:, D + 128 * Hkv:]], 1))
+        if _recurrent(cfg, l):
+            d_qkv, _ = O.linrec_bwd(d_att, _kept(cfg, a["qkv"]), a["states"], B, S)
+        else:
+            d_qkv = _attention_bwd(cfg, l, a, d_att, rope)
         d_n1, G["l%d.w_qkv" % l], d0 = O.linear_bwd(d_qkv, a["n1"], P["l%d.w_qkv" % l], sx[0:1], sw["l%d.w_qkv" % l], hb)
-        d_x1, G["l%d.attn_norm" % l] = O.rmsnorm_bwd(d_n1, a["x"], P["l%d.attn_norm" % l], a["rstd1"], bf=True)
-        dx = O.residual_add(d_h, d_x1)
+        dx = _norm_bwd(cfg, P, G, "l%d.attn_norm" % l, d_n1, _kept(cfg, a["x"]), a["stat1"], d_h)
         ds[0], ds[1], ds[2], ds[3] = d0[0], d1[0], d2[0], d3[0]
         G["l%d.s_x" % l] = ds
     if cfg.get("embed_norm"):
-        dx, G["embed_norm"] = O.rmsnorm_bwd(dx, sv["x_emb"], P["embed_norm"], sv["rstd_emb"], bf=True)
+        dx = _norm_bwd(cfg, P, G, "embed_norm", dx, sv["x_emb"], sv["stat_emb"])
     G["embed"] = O.embed_bwd(sv["inp"], dx, cfg["vocab"])
     flat = np.concatenate([np.asarray(G[name], np.float32).reshape(-1) for name, _ in _specs(cfg)])
     return flat, float(loss_mean[0])
@@ -131,7 +178,8 @@ def microbatch_grad(cfg, P, sw, tok):
 def run_step(cfg, params, tokens, opt=None, calibrate=True):
     """One optimizer step.  cfg: dict (n_layers, d_model, n_heads, ffn, vocab, seq, micro_batch, mesh=(accum,
     dp_shard, dp_replicate), optional hadamard_block, z_weight, lr, betas, eps, wd, clip, step; the paper's block:
-    n_kv_heads, qk_norm, rope_tables=(cos, sin) f32 [seq, 64], embed_norm, window, full_every).
+    n_kv_heads, qk_norm, rope_tables=(cos, sin) f32 [seq, 64], embed_norm, window, full_every; other blocks: norm = "layer", recurrent = layers
+    with the gated linear recurrence, act8 = activations in 8 bits for the backward pass).
     params: dict name -> numpy (uint16 bf16 bits / float32 steps).  tokens: [n_mb, micro_batch, seq+1]."""
     P = {k: np.array(v, copy=True) for k, v in params.items()}
     specs = _specs(cfg)

@@ -44,6 +44,10 @@ class ModelConfig:
     pv_int8: bool = False            # forward P.V of every block of 128 keys on the int8 tensor cores
     dq_fixed: bool = False           # query gradient accumulated over the key blocks in 64-bit fixed point
     arith: int = 1                   # 2: the LM-head contractions in arithmetic version 2 (order-free, int8 tensor cores)
+    # blocks that are not the paper's
+    norm: str = "rms"                # "layer": the norms subtract the mean and have a shift beside the gain
+    recurrent: tuple = ()            # layers whose mixer is the gated linear recurrence (w_qkv: gate and value, 2 d_model rows) in place of attention
+    act8: bool = False               # inputs of the norms, of SwiGLU and of the recurrence are kept in 8 bits for the backward pass
 
     def as_dict(self):
         return dict(self.__dict__)
@@ -64,6 +68,10 @@ class ModelConfig:
     def qkv_width(self):
         return (self.n_heads + 2 * self.kv_heads) * 128
 
+    def mixer_width(self, l):
+        """Rows of w_qkv: queries, keys and values, or gate and value."""
+        return 2 * self.d_model if l in self.recurrent else self.qkv_width
+
     def layer_window(self, l):
         if not self.window or l == self.n_layers - 1 or (l + 1) % self.full_every == 0:
             return 0
@@ -72,14 +80,17 @@ class ModelConfig:
 
 def param_specs(cfg):
     D, Fh, V, L = cfg.d_model, cfg.ffn, cfg.vocab, cfg.n_layers
+
+    def norm(name):
+        return [(name, (D,), "bf16")] + ([(name + "_shift", (D,), "bf16")] if cfg.norm == "layer" else [])
     s = [("embed", (V, D), "bf16")]
     if cfg.embed_norm:
-        s += [("embed_norm", (D,), "bf16")]
+        s += norm("embed_norm")
     for l in range(L):
-        s += [("l%d.attn_norm" % l, (D,), "bf16"), ("l%d.w_qkv" % l, (cfg.qkv_width, D), "bf16"), ("l%d.w_o" % l, (D, D), "bf16"),
-              ("l%d.ffn_norm" % l, (D,), "bf16"), ("l%d.w_gu" % l, (2 * Fh, D), "bf16"), ("l%d.w_down" % l, (D, Fh), "bf16"),
-              ("l%d.s_x" % l, (4,), "f32")]
-    return s + [("final_norm", (D,), "bf16"), ("lm_head", (V, D), "bf16")]
+        s += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (cfg.mixer_width(l), D), "bf16"), ("l%d.w_o" % l, (D, D), "bf16")]
+        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "bf16"), ("l%d.w_down" % l, (D, Fh), "bf16"),
+                                         ("l%d.s_x" % l, (4,), "f32")]
+    return s + norm("final_norm") + [("lm_head", (V, D), "bf16")]
 
 
 def _numel(shape):
@@ -113,6 +124,8 @@ class Replay:
         self.specs = param_specs(cfg)
         D, Fh, V, L, T = cfg.d_model, cfg.ffn, cfg.vocab, cfg.n_layers, cfg.tokens_per_microbatch
         assert D == cfg.n_heads * 128, "head_dim is 128"
+        assert cfg.norm in ("rms", "layer") and all(0 <= l < L for l in cfg.recurrent)
+        self.layer_norm = cfg.norm == "layer"
         self.goff, self.poff = {}, {}
         self.shape = dict((n, sh) for n, sh, _ in self.specs)
         g = p = 0
@@ -143,7 +156,7 @@ class Replay:
         self.abufs = z(self.nbufs * (accum_len or g), F32)
         self.lin = {}
         for l in range(L):
-            for w, (N, K) in zip(LINEARS, ((cfg.qkv_width, D), (D, D), (2 * Fh, D), (D, Fh))):
+            for w, (N, K) in zip(LINEARS, ((cfg.mixer_width(l), D), (D, D), (2 * Fh, D), (D, Fh))):
                 self.lin[(l, w)] = dict(name="l%d.%s" % (l, w), N=N, K=K, s_w=z(N, F32), qW=z(N * K, I8), qWt=z(N * K, I8), s_u=z(1, F32))
         e = lambda n, dt: torch.empty(n, dtype=dt, device=device)
         QW, Hkv = cfg.qkv_width, cfg.kv_heads
@@ -151,18 +164,18 @@ class Replay:
         if cfg.rope_tables is not None:
             self.rope_cos = torch.from_numpy(np.ascontiguousarray(cfg.rope_tables[0], dtype=np.float32)).to(device)
             self.rope_sin = torch.from_numpy(np.ascontiguousarray(cfg.rope_tables[1], dtype=np.float32)).to(device)
-        self.act = [dict(x=e(T * D, I16), rstd1=e(T, F32), n1=e(T * D, I16), qx_qkv=e(T * D, I8), qkv=e(T * QW, I16),
-                         qkr=e(T * QW if self.head_ops else 0, I16),
-                         rstd_qk=e(T * (cfg.n_heads + Hkv) if cfg.qk_norm else 0, F32),
-                         lse=e(T * cfg.n_heads, F32), att=e(T * D, I16), qx_o=e(T * D, I8), h=e(T * D, I16), rstd2=e(T, F32),
-                         n2=e(T * D, I16), qx_gu=e(T * D, I8), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16),
-                         qx_down=e(T * Fh, I8)) for _ in range(L)]
-        self.xf, self.rstdf, self.nf = e(T * D, I16), e(T, F32), e(T * D, I16)
-        self.x_emb, self.rstd_emb = (e(T * D, I16), e(T, F32)) if cfg.embed_norm else (None, None)
+        self.act = [self._activations(l, e) for l in range(L)]
+        self.xf, self.rstdf, self.nf, self.meanf = e(T * D, I16), e(T, F32), e(T * D, I16), e(T if self.layer_norm else 0, F32)
+        self.x_emb, self.rstd_emb, self.mean_emb = (e(T * D, I16), e(T, F32), e(T if self.layer_norm else 0, F32)) if cfg.embed_norm else (None, None, None)
         self.logits = e(T * V, F32)
         self.loss_row, self.lse_x = e(T, F32), e(T, F32)
         self.loss_mean, self.z_mean = e(1, F32), e(1, F32)
-        self.tmp = [e(T * max(QW, 2 * Fh), I16) for _ in range(3)]   # gradient scratch activations
+        wide = max([QW, 2 * Fh] + [cfg.mixer_width(l) for l in cfg.recurrent])
+        self.tmp = [e(T * wide, I16) for _ in range(3)]              # gradient scratch activations
+        # what the layers share where their own copies are in 8 bits: the residual stream at either norm, the inputs of SwiGLU and of the
+        # recurrence, the down projection's input, which the backward pass makes again
+        self.shared = dict(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * Fh, I8),
+                           gv=e(T * 2 * D if cfg.recurrent else 0, I16)) if cfg.act8 else None
         self.tok = e(T, I32)
         self.lab = e(T, I32)
         # what a step reports lies in one buffer and comes back in one copy: status, norm and clip coefficient, hash roots, losses
@@ -180,11 +193,31 @@ class Replay:
                     ([_numel(shape) * (2 if kind == "bf16" else 4) for _, shape, kind in self.specs], [2 * p, 16 * L])],
                   det.det_sum_ws_bytes(g), 1 << 20,
                   (max(det.det_lmhead_fwd_v2_ws_bytes(T, V, D), det.det_lmhead_bwd_v2_ws_bytes(T, V, D)) if cfg.arith == 2 else 0),
-                  *[det.det_linear_bwd_ws_bytes(T, N, K) for (N, K) in ((QW, D), (D, D), (2 * Fh, D), (D, Fh))])
+                  det.det_layernorm_bwd_ws_bytes(T, D) if self.layer_norm else 0,
+                  *[det.det_linear_bwd_ws_bytes(T, N, K) for (N, K) in ((QW, D), (D, D), (2 * Fh, D), (D, Fh), (2 * D, D))])
         self.ws = e(wsb + 4096, torch.uint8)
         self.losses = []
         self.prof = None
         self.fuse_quant = True       # producers write the linears' int8 inputs (False: separate quantiser pass per linear)
+
+    def _activations(self, l, e):
+        """What layer l keeps from its forward pass for its backward pass."""
+        cfg = self.cfg
+        D, Fh, T, QW, Hkv = cfg.d_model, cfg.ffn, cfg.tokens_per_microbatch, cfg.mixer_width(l), cfg.kv_heads
+        rec, stat = l in cfg.recurrent, T if self.layer_norm else 0
+        a = dict(rstd1=e(T, F32), mean1=e(stat, F32), n1=e(T * D, I16), qx_qkv=e(T * D, I8), att=e(T * D, I16), qx_o=e(T * D, I8), rstd2=e(T, F32),
+                 mean2=e(stat, F32), n2=e(T * D, I16), qx_gu=e(T * D, I8))
+        if rec:
+            a.update(states=e(det.det_linrec_state_floats(cfg.micro_batch, cfg.seq, D), F32))
+        else:
+            a.update(qkv=e(T * QW, I16), qkr=e(T * QW if self.head_ops else 0, I16), lse=e(T * cfg.n_heads, F32),
+                     rstd_qk=e(T * (cfg.n_heads + Hkv) if cfg.qk_norm else 0, F32))
+        if not cfg.act8:
+            a.update(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * Fh, I8))
+            return dict(a, gv=e(T * QW, I16)) if rec else a
+        for name, width in (("x", D), ("h", D), ("gu", 2 * Fh)) + ((("gv", 2 * D),) if rec else ()):
+            a[name + "8"], a[name + "_e"] = e(T * width, I8), e(det.det_act8_exp_bytes(T, width), torch.uint8)
+        return a
 
     # ---- optional per-call-site device timing (CUDA events on the launching stream) --------------------
     class _Span:
@@ -245,6 +278,8 @@ class Replay:
             dst = self.p(name)
             if name.endswith("norm"):
                 dst.fill_(0x3F80)
+            elif name.endswith("norm_shift"):
+                dst.zero_()
             else:
                 n = dst.numel()
                 for o in range(0, n, 1 << 26):
@@ -294,29 +329,57 @@ class Replay:
             else:
                 det.det_linear_fwd(X, d["qW"], sx, d["s_w"], M, d["N"], d["K"], Y, qx, self.status)
 
-    def _norm(self, a, b, x, gain, y, rstd, s_q=None, qy=None):
-        """y = RMSNorm of x, after x = a + b unless a is None; with s_q the next linear's int8 input too."""
+    def _norm(self, a, b, x, name, y, rstd, mean, s_q=None, qy=None, kept=None):
+        """y = norm of x, after x = a + b unless a is None; with s_q the next linear's int8 input too, with kept = (codes, steps) x in 8 bits."""
         T, D = self.cfg.tokens_per_microbatch, self.cfg.d_model
-        g = self._views["pbf"][gain]
+        P = self._views["pbf"]
+        g = P[name]
+        if self.layer_norm:
+            q8, e8 = kept or (None, None)
+            det.det_residual_layernorm_fwd(x if a is None else a, None if a is None else b, g, P[name + "_shift"], T, D, 1e-6, x, y, mean, rstd, s_q,
+                                           qy if s_q is not None else None, q8, e8)
+            return
         if a is not None and D <= 2048:
             det.det_residual_rmsnorm_fwd(a, b, g, T, D, 1e-6, x, y, rstd, s_q, qy if s_q is not None else None)
-            return
-        if a is not None:
-            det.det_residual_add(a, b, T * D, x)
-        if s_q is not None:
-            det.det_rmsnorm_fwd_q(x, g, T, D, 1e-6, y, rstd, s_q, qy)
         else:
-            det.det_rmsnorm_fwd(det.DET_BF16, x, g, T, D, 1e-6, y, rstd)
+            if a is not None:
+                det.det_residual_add(a, b, T * D, x)
+            if s_q is not None:
+                det.det_rmsnorm_fwd_q(x, g, T, D, 1e-6, y, rstd, s_q, qy)
+            else:
+                det.det_rmsnorm_fwd(det.DET_BF16, x, g, T, D, 1e-6, y, rstd)
+        if kept is not None:
+            det.det_act8_pack(det.DET_BF16, x, D, T, D, *kept)
 
-    def _norm_bwd(self, dy, x, gain, rstd, dx, tmp):
-        """dx += gradient through the norm (rounded on its own first); the gain's gradient goes to its place."""
+    def _norm_bwd(self, dy, x, name, rstd, mean, dx, tmp, kept=None):
+        """dx += gradient through the norm (rounded on its own first where the norm is RMSNorm); the gradients of gain and shift go to their places.
+        kept: x in 8 bits; x is then where it may be restored to."""
         T, D = self.cfg.tokens_per_microbatch, self.cfg.d_model
-        g, dg = self._views["pbf"][gain], self._views["gmb"][gain]
+        P, G = self._views["pbf"], self._views["gmb"]
+        g, dg = P[name], G[name]
+        if self.layer_norm:
+            db = G[name + "_shift"]
+            if kept is not None:
+                det.det_layernorm_bwd_act8(dy, *kept, g, mean, rstd, T, D, dx, dx, dg, db, self.ws)
+            else:
+                det.det_layernorm_bwd_residual(dy, x, g, mean, rstd, T, D, dx, dx, dg, db, self.ws)
+            return
+        if kept is not None:
+            det.det_act8_unpack(det.DET_BF16, *kept, T, D, x, D)
         if D <= 2048:
             det.det_rmsnorm_bwd_residual(dy, x, g, rstd, T, D, dx, dx, dg, self.ws)
             return
         det.det_rmsnorm_bwd(det.DET_BF16, dy, x, g, rstd, T, D, tmp, dg, self.ws)
         det.det_residual_add(dx, tmp, T * D, dx)
+
+    def _norm_bwd_alone(self, dy, x, name, rstd, mean, dx):
+        """dx = gradient through a norm that nothing bypasses."""
+        T, D = self.cfg.tokens_per_microbatch, self.cfg.d_model
+        g, G = self._views["pbf"][name], self._views["gmb"]
+        if self.layer_norm:
+            det.det_layernorm_bwd(det.DET_BF16, dy, x, g, mean, rstd, T, D, dx, G[name], G[name + "_shift"], self.ws)
+        else:
+            det.det_rmsnorm_bwd(det.DET_BF16, dy, x, g, rstd, T, D, dx, G[name], self.ws)
 
     def _set_tokens(self, dst, part):
         """dst <- the tokens of a micro-batch, row after row; rows of another length count as one sequence of tokens."""
@@ -324,6 +387,41 @@ class Replay:
             dst.view(part.shape).copy_(part)          # without a contiguous copy in between
         else:
             dst.copy_(part.reshape(-1))
+
+    def _recurrence(self, a, gv, kept):
+        """att = the gated linear recurrence over gate and value, the halves of gv's rows."""
+        cfg = self.cfg
+        D, p = cfg.d_model, gv.data_ptr()
+        with self.span("linrec_fwd"):
+            det.det_linrec_fwd(p, p + 2 * D, 2 * D, cfg.micro_batch, cfg.seq, D, a["att"], D, states=a["states"], status_dev=self.status)
+        if kept is not None:
+            det.det_act8_pack(det.DET_BF16, gv, 2 * D, cfg.tokens_per_microbatch, 2 * D, *kept)
+
+    def _attention(self, l, a, s_o):
+        """att = attention over qkv; with s_o the output projection's int8 input too (not beside the int8 P.V)."""
+        cfg = self.cfg
+        D, T, B, H, S, Hkv, QW = cfg.d_model, cfg.tokens_per_microbatch, cfg.micro_batch, cfg.n_heads, cfg.seq, cfg.kv_heads, cfg.qkv_width
+        qp = vp = a["qkv"].data_ptr()
+        if self.head_ops:
+            # queries and keys (the first H + Hkv heads of every row) are normalised and rotated into qkr; the
+            # values are read from qkv, which has the same row stride
+            src = a["qkv"]
+            if cfg.qk_norm:
+                det.det_headnorm_fwd(src, QW, T, H + Hkv, 1e-6, a["qkr"], QW, a["rstd_qk"])
+                src = a["qkr"]
+            if cfg.rope_tables is not None:
+                det.det_rope(src, QW, T, H + Hkv, S, self.rope_cos, self.rope_sin, 0, a["qkr"], QW)
+            qp = a["qkr"].data_ptr()
+        with self.span("attn_fwd"):
+            if cfg.pv_int8:
+                det.det_attn_fwd_int8pv(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"],
+                                        self.status, Hkv=Hkv, window=cfg.layer_window(l))
+            elif s_o is not None:
+                det.det_attn_fwd_q(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"], s_o,
+                                   a["qx_o"], Hkv=Hkv, window=cfg.layer_window(l))
+            else:
+                det.det_attn_fwd(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"], Hkv=Hkv,
+                                 window=cfg.layer_window(l))
 
     def forward(self, tokens_mb, calibrate=False):
         cfg = self.cfg
@@ -333,11 +431,12 @@ class Replay:
         P, X = views["pbf"], views["sx"]
         self._set_tokens(self.tok, tokens_mb[:, :-1])
         self._set_tokens(self.lab, tokens_mb[:, 1:])
-        Hkv, QW = cfg.kv_heads, cfg.qkv_width
-        x = self.act[0]["x"] if L else self.xf
+        own = (lambda a, name: self.shared[name]) if cfg.act8 else (lambda a, name: a[name])     # an activation, or the one the layers share
+        kept = (lambda a, name: (a[name + "8"], a[name + "_e"])) if cfg.act8 else (lambda a, name: None)
+        x = own(self.act[0], "x") if L else self.xf
         if cfg.embed_norm:
             det.det_embed_fwd(self.tok, T, P["embed"], V, D, self.x_emb)
-            det.det_rmsnorm_fwd(det.DET_BF16, self.x_emb, P["embed_norm"], T, D, 1e-6, x, self.rstd_emb)
+            self._norm(None, None, self.x_emb, "embed_norm", x, self.rstd_emb, self.mean_emb)
         else:
             det.det_embed_fwd(self.tok, T, P["embed"], V, D, x)
         # outside the calibration pass every activation step is known before its activation is produced, so the
@@ -347,40 +446,29 @@ class Replay:
         for l in range(L):
             a = self.act[l]
             sxl = [X[l, i] for i in range(4)] if fuse else None
-            self._norm(res, dn, a["x"], "l%d.attn_norm" % l, a["n1"], a["rstd1"], sxl[0] if fuse else None, a["qx_qkv"])
-            self._linear(l, "w_qkv", 0, a["n1"], T, a["qkv"], a["qx_qkv"], calibrate, fuse)
-            qp = vp = a["qkv"].data_ptr()
-            if self.head_ops:
-                # queries and keys (the first H + Hkv heads of every row) are normalised and rotated into qkr; the
-                # values are read from qkv, which has the same row stride
-                src = a["qkv"]
-                if cfg.qk_norm:
-                    det.det_headnorm_fwd(src, QW, T, H + Hkv, 1e-6, a["qkr"], QW, a["rstd_qk"])
-                    src = a["qkr"]
-                if cfg.rope_tables is not None:
-                    det.det_rope(src, QW, T, H + Hkv, S, self.rope_cos, self.rope_sin, 0, a["qkr"], QW)
-                qp = a["qkr"].data_ptr()
-            with self.span("attn_fwd"):
-                if cfg.pv_int8:
-                    det.det_attn_fwd_int8pv(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"],
-                                            self.status, Hkv=Hkv, window=cfg.layer_window(l))
-                elif fuse:
-                    det.det_attn_fwd_q(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"], sxl[1],
-                                       a["qx_o"], Hkv=Hkv, window=cfg.layer_window(l))
-                else:
-                    det.det_attn_fwd(qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), QW, B, H, S, a["att"], D, a["lse"], Hkv=Hkv,
-                                     window=cfg.layer_window(l))
-            o = self.tmp[1][:T * D]
-            self._linear(l, "w_o", 1, a["att"], T, o, a["qx_o"], calibrate, fuse and not cfg.pv_int8)
-            self._norm(a["x"], o, a["h"], "l%d.ffn_norm" % l, a["n2"], a["rstd2"], sxl[2] if fuse else None, a["qx_gu"])
-            self._linear(l, "w_gu", 2, a["n2"], T, a["gu"], a["qx_gu"], calibrate, fuse)
-            if fuse:
-                det.det_swiglu_fwd_q(a["gu"], T, Fh, a["a"], sxl[3], a["qx_down"])
+            ax, ah = own(a, "x"), own(a, "h")
+            self._norm(res, dn, ax, "l%d.attn_norm" % l, a["n1"], a["rstd1"], a["mean1"], sxl[0] if fuse else None, a["qx_qkv"], kept(a, "x"))
+            rec = l in cfg.recurrent
+            mix = own(a, "gv") if rec else a["qkv"]
+            self._linear(l, "w_qkv", 0, a["n1"], T, mix, a["qx_qkv"], calibrate, fuse)
+            if rec:
+                self._recurrence(a, mix, kept(a, "gv"))
             else:
-                det.det_swiglu_fwd(a["gu"], T, Fh, a["a"])
-            self._linear(l, "w_down", 3, a["a"], T, dn, a["qx_down"], calibrate, fuse)
-            res = a["h"]
-        self._norm(res, dn, self.xf, "final_norm", self.nf, self.rstdf)
+                self._attention(l, a, sxl[1] if fuse else None)
+            o = self.tmp[1][:T * D]
+            self._linear(l, "w_o", 1, a["att"], T, o, a["qx_o"], calibrate, fuse and not cfg.pv_int8 and not rec)
+            self._norm(ax, o, ah, "l%d.ffn_norm" % l, a["n2"], a["rstd2"], a["mean2"], sxl[2] if fuse else None, a["qx_gu"], kept(a, "h"))
+            gu, act, qx_down = own(a, "gu"), own(a, "a"), own(a, "qx_down")
+            self._linear(l, "w_gu", 2, a["n2"], T, gu, a["qx_gu"], calibrate, fuse)
+            if cfg.act8:
+                det.det_swiglu_fwd_act8(gu, T, Fh, act, *kept(a, "gu"), *((sxl[3], qx_down) if fuse else ()))
+            elif fuse:
+                det.det_swiglu_fwd_q(gu, T, Fh, act, sxl[3], qx_down)
+            else:
+                det.det_swiglu_fwd(gu, T, Fh, act)
+            self._linear(l, "w_down", 3, act, T, dn, qx_down, calibrate, fuse)
+            res = ah
+        self._norm(res, dn, self.xf, "final_norm", self.nf, self.rstdf, self.meanf)
         with self.span("lmhead_fwd"):
             if cfg.arith == 2:
                 det.det_lmhead_fwd_v2(self.nf, P["lm_head"], T, V, D, self.logits, self.ws, self.status)
@@ -396,6 +484,29 @@ class Replay:
         with self.span("linear_bwd"):
             det.det_linear_bwd(dY, X, qx, P[name], d["qWt"], self._views["sx"][l, idx], d["s_w"], d["s_u"], M, d["N"], d["K"],
                                self.cfg.hadamard_block, dX, G[name], G[l, idx], self.ws, self.status)
+
+    def _recurrence_bwd(self, d_att, a, gv, kept, d_gv):
+        cfg = self.cfg
+        D = cfg.d_model
+        if kept is not None:
+            det.det_act8_unpack(det.DET_BF16, *kept, cfg.tokens_per_microbatch, 2 * D, gv, 2 * D)
+        p, o = gv.data_ptr(), d_gv.data_ptr()
+        with self.span("linrec_bwd"):
+            det.det_linrec_bwd(d_att, D, p, p + 2 * D, 2 * D, cfg.micro_batch, cfg.seq, D, a["states"], o, o + 2 * D, 2 * D, status_dev=self.status)
+
+    def _attention_bwd(self, l, d_att, a, d_qkv):
+        cfg = self.cfg
+        D, T, B, H, S, Hkv, QW = cfg.d_model, cfg.tokens_per_microbatch, cfg.micro_batch, cfg.n_heads, cfg.seq, cfg.kv_heads, cfg.qkv_width
+        vp, dp = a["qkv"].data_ptr(), d_qkv.data_ptr()
+        qp = a["qkr"].data_ptr() if self.head_ops else vp
+        with self.span("attn_bwd"):
+            bwd = det.det_attn_bwd_fixq if cfg.dq_fixed else det.det_attn_bwd
+            bwd(d_att, qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), a["att"], a["lse"], QW, D, B, H, S, dp,
+                dp + 2 * D, dp + 2 * (D + 128 * Hkv), QW, self.ws, Hkv=Hkv, window=cfg.layer_window(l))
+        if cfg.rope_tables is not None:
+            det.det_rope(d_qkv, QW, T, H + Hkv, S, self.rope_cos, self.rope_sin, 1, d_qkv, QW)
+        if cfg.qk_norm:
+            det.det_headnorm_bwd(d_qkv, QW, a["qkv"], QW, a["rstd_qk"], T, H + Hkv, d_qkv, QW)
 
     def backward(self):
         cfg = self.cfg
@@ -414,38 +525,37 @@ class Replay:
             else:
                 det.det_lmhead_bwd(self.logits, self.nf, P["lm_head"], T, V, D, d_nf, G["lm_head"], 1)
         dx = t1[:T * D]
-        det.det_rmsnorm_bwd(det.DET_BF16, d_nf, self.xf, P["final_norm"], self.rstdf, T, D, dx,
-                            G["final_norm"], self.ws)
+        self._norm_bwd_alone(d_nf, self.xf, "final_norm", self.rstdf, self.meanf, dx)
+        own = (lambda a, name: self.shared[name]) if cfg.act8 else (lambda a, name: a[name])
+        kept = (lambda a, name: (a[name + "8"], a[name + "_e"])) if cfg.act8 else (lambda a, name: None)
         for l in reversed(range(L)):
             a = self.act[l]
             d_a = t0[:T * Fh]
-            self._linear_bwd(l, "w_down", 3, dx, a["a"], a["qx_down"], T, d_a)
+            act, qx_down = own(a, "a"), own(a, "qx_down")
+            if cfg.act8:
+                det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act, views["sx"][l, 3], qx_down)
+            self._linear_bwd(l, "w_down", 3, dx, act, qx_down, T, d_a)
             d_gu = t2[:T * 2 * Fh]
-            det.det_swiglu_bwd(d_a, a["gu"], T, Fh, d_gu)
+            if cfg.act8:
+                det.det_swiglu_bwd_act8(d_a, *kept(a, "gu"), T, Fh, d_gu)
+            else:
+                det.det_swiglu_bwd(d_a, a["gu"], T, Fh, d_gu)
             d_n2 = t0[:T * D]
             self._linear_bwd(l, "w_gu", 2, d_gu, a["n2"], a["qx_gu"], T, d_n2)
-            self._norm_bwd(d_n2, a["h"], "l%d.ffn_norm" % l, a["rstd2"], dx, t2[:T * D])      # dx: gradient of h from here on
+            self._norm_bwd(d_n2, own(a, "h"), "l%d.ffn_norm" % l, a["rstd2"], a["mean2"], dx, t2[:T * D], kept(a, "h"))    # dx: gradient of h from here on
             d_att = t0[:T * D]
             self._linear_bwd(l, "w_o", 1, dx, a["att"], a["qx_o"], T, d_att)
-            Hkv, QW = cfg.kv_heads, cfg.qkv_width
-            d_qkv = t2[:T * QW]
-            vp, dp = a["qkv"].data_ptr(), d_qkv.data_ptr()
-            qp = a["qkr"].data_ptr() if self.head_ops else vp
-            with self.span("attn_bwd"):
-                bwd = det.det_attn_bwd_fixq if cfg.dq_fixed else det.det_attn_bwd
-                bwd(d_att, qp, qp + 2 * D, vp + 2 * (D + 128 * Hkv), a["att"], a["lse"], QW, D, B, H, S, dp,
-                    dp + 2 * D, dp + 2 * (D + 128 * Hkv), QW, self.ws, Hkv=Hkv, window=cfg.layer_window(l))
-            if cfg.rope_tables is not None:
-                det.det_rope(d_qkv, QW, T, H + Hkv, S, self.rope_cos, self.rope_sin, 1, d_qkv, QW)
-            if cfg.qk_norm:
-                det.det_headnorm_bwd(d_qkv, QW, a["qkv"], QW, a["rstd_qk"], T, H + Hkv, d_qkv, QW)
+            d_mix = t2[:T * cfg.mixer_width(l)]
+            if l in cfg.recurrent:
+                self._recurrence_bwd(d_att, a, own(a, "gv"), kept(a, "gv"), d_mix)
+            else:
+                self._attention_bwd(l, d_att, a, d_mix)
             d_n1 = t0[:T * D]
-            self._linear_bwd(l, "w_qkv", 0, d_qkv, a["n1"], a["qx_qkv"], T, d_n1)
-            self._norm_bwd(d_n1, a["x"], "l%d.attn_norm" % l, a["rstd1"], dx, t2[:T * D])     # and of x
+            self._linear_bwd(l, "w_qkv", 0, d_mix, a["n1"], a["qx_qkv"], T, d_n1)
+            self._norm_bwd(d_n1, own(a, "x"), "l%d.attn_norm" % l, a["rstd1"], a["mean1"], dx, t2[:T * D], kept(a, "x"))   # and of x
         if cfg.embed_norm:
             d_emb = t0[:T * D]
-            det.det_rmsnorm_bwd(det.DET_BF16, dx, self.x_emb, P["embed_norm"], self.rstd_emb, T, D, d_emb,
-                                G["embed_norm"], self.ws)
+            self._norm_bwd_alone(dx, self.x_emb, "embed_norm", self.rstd_emb, self.mean_emb, d_emb)
             dx = d_emb
         det.det_embed_bwd(self.tok, T, dx, V, D, G["embed"])
 

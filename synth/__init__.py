@@ -79,29 +79,32 @@ def randint(shape, high, seed=0, tid=0):
 def model_param_specs(cfg):
     """Canonical parameter order: embedding; per layer attn-norm gain, W_qkv, W_o, ffn-norm gain, W_gate/up,
     W_down, the four activation steps; final-norm gain; LM head.  cfg: dict with n_layers, d_model, ffn, vocab and
-    optionally n_kv_heads (grouped queries: W_qkv has (n_heads + 2 n_kv_heads) * 128 rows) and embed_norm (a gain
-    after the embedding).  Returns a list of (name, shape, kind), kind in {"embed", "gain", "linear", "step", "head"}."""
+    optionally n_kv_heads (grouped queries: W_qkv has (n_heads + 2 n_kv_heads) * 128 rows), embed_norm (a gain
+    after the embedding), norm = "layer" (a shift behind every gain) and recurrent (layers whose W_qkv has 2 d_model rows, gate and
+    value).  Returns a list of (name, shape, kind), kind in {"embed", "gain", "shift", "linear", "step", "head"}."""
     D, Fh, V, L = cfg["d_model"], cfg["ffn"], cfg["vocab"], cfg["n_layers"]
     nq = D + 2 * 128 * (cfg.get("n_kv_heads") or cfg["n_heads"]) if "n_heads" in cfg else 3 * D
+    layer, rec = cfg.get("norm", "rms") == "layer", cfg.get("recurrent", ())
+    norm = lambda name: [(name, (D,), "gain")] + ([(name + "_shift", (D,), "shift")] if layer else [])
     specs = [("embed", (V, D), "embed")]
     if cfg.get("embed_norm"):
-        specs += [("embed_norm", (D,), "gain")]
+        specs += norm("embed_norm")
     for l in range(L):
-        specs += [("l%d.attn_norm" % l, (D,), "gain"), ("l%d.w_qkv" % l, (nq, D), "linear"),
-                  ("l%d.w_o" % l, (D, D), "linear"), ("l%d.ffn_norm" % l, (D,), "gain"),
-                  ("l%d.w_gu" % l, (2 * Fh, D), "linear"), ("l%d.w_down" % l, (D, Fh), "linear"),
-                  ("l%d.s_x" % l, (4,), "step")]
-    specs += [("final_norm", (D,), "gain"), ("lm_head", (V, D), "head")]
-    return specs
+        specs += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (2 * D if l in rec else nq, D), "linear"), ("l%d.w_o" % l, (D, D), "linear")]
+        specs += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "linear"), ("l%d.w_down" % l, (D, Fh), "linear"),
+                                             ("l%d.s_x" % l, (4,), "step")]
+    return specs + norm("final_norm") + [("lm_head", (V, D), "head")]
 
 
 def model_params(cfg, seed=0):
-    """Random-init parameters: weights ~ N(0, 0.02) as bf16 bit patterns, gains = 1 (bf16), activation steps
+    """Random-init parameters: weights ~ N(0, 0.02) as bf16 bit patterns, gains = 1 and shifts = 0 (bf16), activation steps
     filled later by a calibration forward (zeros here, float32)."""
     out = {}
     for tid, (name, shape, kind) in enumerate(model_param_specs(cfg)):
         if kind == "gain":
             out[name] = np.full(shape, 0x3F80, np.uint16)
+        elif kind == "shift":
+            out[name] = np.zeros(shape, np.uint16)
         elif kind == "step":
             out[name] = np.zeros(shape, np.float32)
         else:
