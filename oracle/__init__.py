@@ -231,18 +231,18 @@ def act8_unpack(q, e, bf=True):
 
 
 # ---- gated linear recurrence --------------------------------------------------
-LINREC_BLOCK = 64
+LINREC_CHUNK = 8            # rows between two saved states
 
 
 def linrec_fwd(gv, B, S, flags=None, h0=None):
-    """gv: uint16 [B*S, 2D] (gate | value).  Returns y [B*S, D], hT [B, D] and the states at the starts of the blocks."""
+    """gv: uint16 [B*S, 2D] (gate | value).  Returns y [B*S, D], hT [B, D] and the states in front of every 8 rows."""
     gv = _c(gv, np.uint16)
     D = gv.shape[1] // 2
     assert gv.shape[0] == B * S
     flags = _c(flags, np.uint8) if flags is not None else None
     h0 = _c(h0, np.float32) if h0 is not None else None
     y, hT = np.empty((B * S, D), np.uint16), np.empty((B, D), np.float32)
-    states = np.empty((B, (S + LINREC_BLOCK - 1) // LINREC_BLOCK, D), np.float32)
+    states = np.empty((B, (S + LINREC_CHUNK - 1) // LINREC_CHUNK, D), np.float32)
     base = gv.ctypes.data
     lib().orc_linrec_fwd(C.c_void_p(base), C.c_void_p(base + 2 * D), C.c_int(2 * D), C.c_int(B), C.c_int(S), C.c_int(D), _p(flags), _p(h0),
                          _p(y), C.c_int(D), _p(hT), _p(states))

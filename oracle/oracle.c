@@ -1084,8 +1084,10 @@ void orc_act8_unpack(int bf, const int8_t *q, const uint8_t *e, int rows, int D,
 /* ------------------------------------------------------------------ */
 /* gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) v_t           */
 /* ------------------------------------------------------------------ */
-#define LR_CHUNK 8   /* rows of a span that is walked row by row */
-#define LR_BLOCK 64  /* rows of a block of chunks */
+#define LR_CHUNK 8   /* rows of a chunk, walked row by row */
+#define LR_BLOCK 2   /* chunks of a block */
+#define LR_GROUP 8   /* chunks of a group: 4 blocks, composed one after the other */
+#define LR_SPAN 16   /* chunks of a span: 2 groups */
 
 /* the smaller of f and 1 - f is e / (1 + e), e = exp(-|g|); the larger its difference to 1 */
 static void lr_gate(float g, float *f, float *z) {
@@ -1095,97 +1097,114 @@ static void lr_gate(float g, float *f, float *z) {
   *f = f2u(g) >> 31 ? m : M;
   *z = f2u(g) >> 31 ? M : m;
 }
-/* the span (A, H) applied to what comes in; a span that forgets everything lets nothing in, not even a NaN */
-static float lr_apply(float A, float H, float s) { return A == 0.0f ? H : fadd(fmul(A, s), H); }
-
-/* One channel.  With chunk-wise composites (A, H) from zero, prefixes of them within a block and the states at the starts of
- * the blocks: h[t] is walked from the state at the start of its chunk. */
-static void lr_forward(const float *f, const float *z, const float *v, const uint8_t *flags, int S, float h0, float *hprev,
-                       float *h, float *states, float *hT) {
-  float s = h0;
-  for (int b0 = 0, b = 0; b0 < S; b0 += LR_BLOCK, ++b) {
-    int b1 = b0 + LR_BLOCK < S ? b0 + LR_BLOCK : S;
-    if (states) states[b] = s;
-    float PA = 1.0f, PH = 0.0f;
-    for (int c0 = b0; c0 < b1; c0 += LR_CHUNK) {
-      int c1 = c0 + LR_CHUNK < b1 ? c0 + LR_CHUNK : b1;
-      float x = c0 == b0 ? s : lr_apply(PA, PH, s), A = 1.0f, H = 0.0f;
-      for (int t = c0; t < c1; ++t) {
-        float u = fmul(z[t], v[t]);
-        int cut = flags && flags[t];
-        hprev[t] = cut ? 0.0f : x;
-        x = cut ? u : fadd(fmul(f[t], x), u);
-        h[t] = x;
-        if (t == c0) { A = cut ? 0.0f : f[t]; H = u; }
-        else { A = cut ? 0.0f : fmul(A, f[t]); H = cut ? u : fadd(fmul(f[t], H), u); }
+/* Some rows are the map s -> A s + H; one that forgets everything lets nothing in, not even a NaN. */
+typedef struct { float A, H; } lr_map;
+static float lr_apply(lr_map m, float s) { return m.A == 0.0f ? m.H : fadd(fmul(m.A, s), m.H); }
+static lr_map lr_then(lr_map first, lr_map then) { /* first, then `then` */
+  lr_map r = {then.A == 0.0f ? 0.0f : fmul(first.A, then.A), lr_apply(then, first.H)};
+  return r;
+}
+/* What comes into every chunk, in the order of the pass, from the maps of the n chunks and what comes into the first one; returns what
+ * comes out of the last. */
+static float lr_chain(const lr_map *m, int n, float s, float *in) {
+  for (int c0 = 0; c0 < n; c0 += LR_SPAN) {
+    lr_map span = {1.0f, 0.0f};
+    for (int g0 = c0; g0 < n && g0 < c0 + LR_SPAN; g0 += LR_GROUP) {
+      float in_group = g0 == c0 ? s : lr_apply(span, s);
+      lr_map group = {1.0f, 0.0f};
+      for (int b0 = g0; b0 < n && b0 < g0 + LR_GROUP; b0 += LR_BLOCK) {
+        in[b0] = b0 == g0 ? in_group : lr_apply(group, in_group);
+        lr_map block = m[b0];
+        if (b0 + 1 < n) {
+          in[b0 + 1] = lr_apply(block, in[b0]);
+          block = lr_then(block, m[b0 + 1]);
+        }
+        group = b0 == g0 ? block : lr_then(group, block);
       }
-      if (c0 == b0) { PA = A; PH = H; }
-      else { PH = lr_apply(A, H, PH); PA = A == 0.0f ? 0.0f : fmul(PA, A); }
+      span = g0 == c0 ? group : lr_then(span, group);
     }
-    s = lr_apply(PA, PH, s);
+    s = lr_apply(span, s);
   }
-  if (hT) *hT = s;
+  return s;
+}
+static void lr_load(const bf16_t *g, const bf16_t *v, int ldi, int b, int j, int S, float *f, float *z, float *u, float *vv) {
+  for (int t = 0; t < S; ++t) {
+    lr_gate(bf2f(g[((size_t)b * S + t) * ldi + j]), f + t, z + t);
+    vv[t] = bf2f(v[((size_t)b * S + t) * ldi + j]);
+    u[t] = fmul(z[t], vv[t]);
+  }
 }
 void orc_linrec_fwd(const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int D, const uint8_t *flags, const float *h0,
                     bf16_t *y, int ldy, float *hT, float *states) {
-  int nb = (S + LR_BLOCK - 1) / LR_BLOCK;
-#pragma omp parallel for
-  for (int i = 0; i < B * D; ++i) {
-    int b = i / D, j = i % D;
-    float *w = (float *)malloc((size_t)(5 * (size_t)S + nb + 1) * sizeof(float));
-    float *f = w, *z = w + S, *vv = w + 2 * (size_t)S, *hp = w + 3 * (size_t)S, *h = w + 4 * (size_t)S, *stt = w + 5 * (size_t)S;
-    for (int t = 0; t < S; ++t) {
-      lr_gate(bf2f(g[((size_t)b * S + t) * ldi + j]), f + t, z + t);
-      vv[t] = bf2f(v[((size_t)b * S + t) * ldi + j]);
-    }
-    lr_forward(f, z, vv, flags ? flags + (size_t)b * S : NULL, S, h0 ? h0[i] : 0.0f, hp, h, stt, hT ? hT + i : NULL);
-    for (int t = 0; t < S; ++t) y[((size_t)b * S + t) * ldy + j] = f2bf(h[t]);
-    if (states) for (int k = 0; k < nb; ++k) states[((size_t)b * nb + k) * D + j] = stt[k];
-    free(w);
-  }
-}
-/* dh_t = dy_t + f_{t+1} dh_{t+1}: the same composition from the end; carry = f_t dh_t is what row t hands to row t - 1 */
-void orc_linrec_bwd(const bf16_t *dy, int ldy, const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int D,
-                    const uint8_t *flags, const float *states, const float *dhT, bf16_t *dg, bf16_t *dv, int ldd, float *dh0) {
-  int nb = (S + LR_BLOCK - 1) / LR_BLOCK;
+  int n = (S + LR_CHUNK - 1) / LR_CHUNK;
 #pragma omp parallel for
   for (int i = 0; i < B * D; ++i) {
     int b = i / D, j = i % D;
     const uint8_t *fl = flags ? flags + (size_t)b * S : NULL;
-    float *w = (float *)malloc((6 * (size_t)S + 1) * sizeof(float));
-    float *f = w, *z = w + S, *vv = w + 2 * (size_t)S, *hp = w + 3 * (size_t)S, *h = w + 4 * (size_t)S, *d = w + 5 * (size_t)S;
-    for (int t = 0; t < S; ++t) {
-      lr_gate(bf2f(g[((size_t)b * S + t) * ldi + j]), f + t, z + t);
-      vv[t] = bf2f(v[((size_t)b * S + t) * ldi + j]);
-    }
-    float carry = dhT ? dhT[i] : 0.0f;
-    for (int b0 = (nb - 1) * LR_BLOCK; b0 >= 0; b0 -= LR_BLOCK) {
-      int b1 = b0 + LR_BLOCK < S ? b0 + LR_BLOCK : S, nc = (b1 - b0 + LR_CHUNK - 1) / LR_CHUNK;
-      /* the block again from its state, as in the forward pass */
-      lr_forward(f + b0, z + b0, vv + b0, fl ? fl + b0 : NULL, b1 - b0, states[((size_t)b * nb + b0 / LR_BLOCK) * D + j], hp + b0, h + b0,
-                 NULL, NULL);
-      float SA = 1.0f, SK = 0.0f;
-      for (int c = nc - 1; c >= 0; --c) {
-        int c0 = b0 + c * LR_CHUNK, c1 = c0 + LR_CHUNK < b1 ? c0 + LR_CHUNK : b1;
-        float x = c == nc - 1 ? carry : lr_apply(SA, SK, carry), A = 1.0f, K = 0.0f;
-        for (int t = c1 - 1; t >= c0; --t) {
-          int cut = fl && fl[t];
-          float dyt = bf2f(dy[((size_t)b * S + t) * ldy + j]);
-          d[t] = fadd(dyt, x);
-          x = cut ? 0.0f : fmul(f[t], d[t]);
-          if (t == c1 - 1) { A = cut ? 0.0f : f[t]; K = cut ? 0.0f : fmul(f[t], dyt); }
-          else { A = cut ? 0.0f : fmul(f[t], A); K = cut ? 0.0f : fmul(f[t], fadd(dyt, K)); }
-        }
-        if (c == nc - 1) { SA = A; SK = K; }
-        else { SK = lr_apply(A, K, SK); SA = A == 0.0f ? 0.0f : fmul(SA, A); }
+    float *w = (float *)malloc((4 * (size_t)S + 3 * (size_t)n + 1) * sizeof(float));
+    float *f = w, *z = w + S, *u = w + 2 * (size_t)S, *vv = w + 3 * (size_t)S, *in = w + 4 * (size_t)S;
+    lr_map *m = (lr_map *)(in + n);
+    lr_load(g, v, ldi, b, j, S, f, z, u, vv);
+    for (int c = 0; c < n; ++c)
+      for (int t = c * LR_CHUNK; t < S && t < (c + 1) * LR_CHUNK; ++t) {
+        int cut = fl && fl[t], first = t == c * LR_CHUNK;
+        m[c].H = cut || first ? u[t] : fadd(fmul(f[t], m[c].H), u[t]);
+        m[c].A = cut ? 0.0f : (first ? f[t] : fmul(m[c].A, f[t]));
       }
-      carry = lr_apply(SA, SK, carry);
+    float last = lr_chain(m, n, h0 ? h0[i] : 0.0f, in);
+    for (int c = 0; c < n; ++c) {
+      float h = in[c];
+      if (states) states[((size_t)b * n + c) * D + j] = h;
+      for (int t = c * LR_CHUNK; t < S && t < (c + 1) * LR_CHUNK; ++t) {
+        h = fl && fl[t] ? u[t] : fadd(fmul(f[t], h), u[t]);
+        y[((size_t)b * S + t) * ldy + j] = f2bf(h);
+      }
     }
-    for (int t = 0; t < S; ++t) {
-      dv[((size_t)b * S + t) * ldd + j] = f2bf(fmul(d[t], z[t]));
-      dg[((size_t)b * S + t) * ldd + j] = f2bf(fmul(fmul(d[t], fsub(hp[t], vv[t])), fmul(f[t], z[t])));
+    if (hT) hT[i] = last;
+    free(w);
+  }
+}
+/* dh_t = dy_t + f_{t+1} dh_{t+1}: the chunks from the last to the first, in each the rows from the last to the first; what row t hands to row
+ * t - 1 is f_t dh_t */
+void orc_linrec_bwd(const bf16_t *dy, int ldy, const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int D,
+                    const uint8_t *flags, const float *states, const float *dhT, bf16_t *dg, bf16_t *dv, int ldd, float *dh0) {
+  int n = (S + LR_CHUNK - 1) / LR_CHUNK;
+#pragma omp parallel for
+  for (int i = 0; i < B * D; ++i) {
+    int b = i / D, j = i % D;
+    const uint8_t *fl = flags ? flags + (size_t)b * S : NULL;
+    float *w = (float *)malloc((5 * (size_t)S + 3 * (size_t)n + 1) * sizeof(float));
+    float *f = w, *z = w + S, *u = w + 2 * (size_t)S, *vv = w + 3 * (size_t)S, *hp = w + 4 * (size_t)S, *in = w + 5 * (size_t)S;
+    lr_map *m = (lr_map *)(in + n);
+    lr_load(g, v, ldi, b, j, S, f, z, u, vv);
+    for (int c = 0; c < n; ++c) {                             /* h_{t-1}, walked from the states at the starts of the chunks */
+      float h = states[((size_t)b * n + c) * D + j];
+      for (int t = c * LR_CHUNK; t < S && t < (c + 1) * LR_CHUNK; ++t) {
+        hp[t] = fl && fl[t] ? 0.0f : h;
+        h = fl && fl[t] ? u[t] : fadd(fmul(f[t], h), u[t]);
+      }
     }
-    if (dh0) dh0[i] = carry;
+    for (int o = 0; o < n; ++o) {
+      int c = n - 1 - o, end = (c + 1) * LR_CHUNK < S ? (c + 1) * LR_CHUNK : S;
+      for (int t = end - 1; t >= c * LR_CHUNK; --t) {
+        int cut = fl && fl[t], first = t == end - 1;
+        float d = bf2f(dy[((size_t)b * S + t) * ldy + j]);
+        m[o].H = cut ? 0.0f : fmul(f[t], first ? d : fadd(d, m[o].H));
+        m[o].A = cut ? 0.0f : (first ? f[t] : fmul(f[t], m[o].A));
+      }
+    }
+    float last = lr_chain(m, n, dhT ? dhT[i] : 0.0f, in);
+    for (int o = 0; o < n; ++o) {
+      int c = n - 1 - o, end = (c + 1) * LR_CHUNK < S ? (c + 1) * LR_CHUNK : S;
+      float x = in[o];
+      for (int t = end - 1; t >= c * LR_CHUNK; --t) {
+        float d = fadd(bf2f(dy[((size_t)b * S + t) * ldy + j]), x);
+        x = fl && fl[t] ? 0.0f : fmul(f[t], d);
+        dv[((size_t)b * S + t) * ldd + j] = f2bf(fmul(d, z[t]));
+        dg[((size_t)b * S + t) * ldd + j] = f2bf(fmul(fmul(d, fsub(hp[t], vv[t])), fmul(f[t], z[t])));
+      }
+    }
+    if (dh0) dh0[i] = last;
     free(w);
   }
 }

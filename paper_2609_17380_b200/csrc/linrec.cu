@@ -4,25 +4,31 @@
 // f and z come from one exponential: with e = exp(-|g|) the smaller of them is m = e / (1 + e) and the larger 1 - m, so neither
 // loses digits where the gate saturates.
 //
-// Order of the sums.  A span of rows is the map s -> A s + H.  A sequence is cut into blocks of 64 rows, a block into chunks of 8.  Chunk maps are
-// composed row by row from the identity; the maps of the chunks before a chunk, from the block's start on, one after the other; the state at
-// a block's start is the block map applied to the state at the start of the block before; the state at a chunk's start is the map of the
-// chunks before it applied to that; inside a chunk the recurrence is walked row by row.  A map with A = 0 lets nothing in, not even
-// a NaN.  The backward pass is the same from the last row to the first.  None of it depends on how blocks are dealt out.
+// Order of the sums.  Some rows are the map s -> A s + H.  A sequence is cut into chunks of 8 rows, blocks of 2 chunks, groups of 4 blocks and spans of
+// 2 groups, from its first row on (backward from its last).  A chunk's map is composed row by row, a block's of its chunks, a group's of its blocks one after
+// the other, a span's of its groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came into that; what comes
+// into a block or a chunk is the map of all those before it, in its group or block, applied to what comes into that; inside a chunk the recurrence is
+// walked row by row.  A map with A = 0 lets nothing in, not even a NaN.
 //
-// A chunk is walked by a half or a whole warp, two channels a lane, so a CTA of eight warps has a strip of 64 channels and one block, or 32 channels
-// and two blocks, a round.  One warp composes the chunk maps of a round.  The CTAs of a cluster take adjacent blocks and hand each other their
-// block maps through distributed shared memory, by stores that complete a transaction barrier of the receiver (a fence and a cluster barrier a round
-// took 1300 cycles of 4800); every CTA applies the maps of the blocks before its own.
-// So every value is read once and written once however long a sequence is and however few there are, with no workspace.  The raw
-// values of the next round come in by asynchronous copies while this one is worked on.
+// A warp has a block of 32 channels: sixteen lanes a chunk, two channels a lane, so that a row's piece is 64 bytes (of 32 bytes the L1 cache was 64 % busy
+// with finding lines); the maps of its two chunks meet in a shuffle.  The eight warps of a CTA have the blocks of a span, and every warp composes the
+// block maps again from shared memory, a group in each half: one barrier a round.  Where there are too few strips the CTAs of a cluster take adjacent
+// spans and send each other the span maps by stores that complete a transaction barrier of the receiver.  So every value is read once and written once
+// however long a sequence is and however few there are, with no workspace.  A warp's raw values of the next round come in by asynchronous copies as soon as
+// those of this round are in registers.
+#include <algorithm>
+#include <mutex>
+#include <type_traits>
+
 #include "common.cuh"
 #include "internal.h"
+#include "rows.cuh"
 #include "tc05.cuh"
 
 namespace det {
 
-constexpr int LR_CHUNK = 8, LR_CHUNKS = 8, LR_BLOCK = LR_CHUNK * LR_CHUNKS, LR_T = 256, LR_MAXC = 16;
+constexpr int LR_CHUNK = 8, LR_BLOCK = 2, LR_GROUP = 4, LR_WARPS = 8, LR_T = 32 * LR_WARPS, LR_CH = 32, LR_MAXC = 16;
+constexpr int LR_ROWS = LR_WARPS * LR_BLOCK * LR_CHUNK;   // of a span
 
 __device__ __forceinline__ float lr_minor(float g) {
   const float e = det_exp_le0(-fabsf(g));
@@ -62,63 +68,67 @@ constexpr LrTable lr_make_table() {
 }
 __device__ constexpr LrTable lr_table_image = lr_make_table();
 
-__device__ __forceinline__ void lr_gate(float m, bool negative, float& f, float& z) {
-  const float M = fsub(1.0f, m);
-  f = negative ? m : M;
-  z = negative ? M : m;
-}
 // gates of the two channels in one word; by table a NaN is looked up as an infinity: lr_gates puts it right
 template <bool TAB>
-__device__ __forceinline__ void lr_gate2(uint32_t w, const float* tab, float f[2], float z[2]) {
+__device__ __forceinline__ void lr_gate2(uint32_t w, const float* tab, float2& f, float2& z) {
   const char* t = reinterpret_cast<const char*>(tab);
   constexpr int last = 4 * (LR_TOP - LR_LOW);
-  const float m0 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w << 2) & 0x1fffcu) - 4 * LR_LOW, last)) : lr_minor(bflo(w));
+  const float m0 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)(w & 0x7fffu) * 4 - 4 * LR_LOW, last)) : lr_minor(bflo(w));
   const float m1 = TAB ? *reinterpret_cast<const float*>(t + __vimin_s32_relu((int)((w >> 14) & 0x1fffcu) - 4 * LR_LOW, last)) : lr_minor(bfhi(w));
-  lr_gate(m0, w & 0x8000u, f[0], z[0]);
-  lr_gate(m1, (int)w < 0, f[1], z[1]);
+  const float2 M = fma2(make_float2(m0, m1), same2(-1.0f), same2(1.0f));             // 1 - m, rounded once either way
+  const bool n0 = w & 0x8000u, n1 = (int)w < 0;
+  f = make_float2(n0 ? m0 : M.x, n1 ? m1 : M.y);
+  z = make_float2(n0 ? M.x : m0, n1 ? M.y : m1);
 }
 struct LrMap { float2 a, h; };                           // s -> a s + h for two channels
-__device__ __forceinline__ float lr_apply1(float a, float h, float s) { return a == 0.0f ? h : fadd(fmul(a, s), h); }
-__device__ __forceinline__ float2 lr_apply(const LrMap& m, float2 s) { return make_float2(lr_apply1(m.a.x, m.h.x, s.x), lr_apply1(m.a.y, m.h.y, s.y)); }
+// Pairs of channels in packed arithmetic, no product fused with a sum: `one` is the factor 1 that add2 needs.
+__device__ __forceinline__ float2 lr_axpy(float2 a, float2 s, float2 h, float2 one) { return add2(mul2(a, s), h, one); }
+__device__ __forceinline__ float2 lr_sub(float2 a, float2 b) { return fma2(b, same2(-1.0f), a); }
+__device__ __forceinline__ float2 lr_apply(const LrMap& m, float2 s, float2 one) {
+  const float2 r = lr_axpy(m.a, s, m.h, one);
+  return make_float2(m.a.x == 0.0f ? m.h.x : r.x, m.a.y == 0.0f ? m.h.y : r.y);
+}
 // the map `first`, then `then`
-__device__ __forceinline__ LrMap lr_compose(const LrMap& first, const LrMap& then) {
-  LrMap r;
-  r.h = lr_apply(then, first.h);
-  r.a = make_float2(then.a.x == 0.0f ? 0.0f : fmul(first.a.x, then.a.x), then.a.y == 0.0f ? 0.0f : fmul(first.a.y, then.a.y));
-  return r;
+__device__ __forceinline__ LrMap lr_compose(const LrMap& first, const LrMap& then, float2 one) {
+  const float2 a = mul2(first.a, then.a), h = lr_axpy(then.a, first.h, then.h, one);
+  const bool x = then.a.x == 0.0f, y = then.a.y == 0.0f;
+  return LrMap{make_float2(x ? 0.0f : a.x, y ? 0.0f : a.y), make_float2(x ? then.h.x : h.x, y ? then.h.y : h.y)};
 }
 __device__ __forceinline__ float4 lr_pack(const LrMap& m) { return make_float4(m.a.x, m.a.y, m.h.x, m.h.y); }
 __device__ __forceinline__ LrMap lr_unpack(float4 v) { return LrMap{make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
-__device__ __forceinline__ float2 lr_step(const float f[2], const float2 u, float2 h, bool cut) {
-  return cut ? u : make_float2(fadd(fmul(f[0], h.x), u.x), fadd(fmul(f[1], h.y), u.y));
+__device__ __forceinline__ float2 lr_step(float2 f, float2 u, float2 h, bool cut, float2 one) {
+  const float2 r = lr_axpy(f, h, u, one);
+  return cut ? u : r;
 }
-// row i of a map that has come to `m` (i == 0: the map of the row alone); rows from the n-th on do not exist
-__device__ __forceinline__ void lr_extend(LrMap& m, int i, int n, const float f[2], const float2 u, bool cut) {
-  if (i >= n && i > 0) return;
-  const float2 a = i ? make_float2(fmul(m.a.x, f[0]), fmul(m.a.y, f[1])) : make_float2(f[0], f[1]);
-  m.h = i ? lr_step(f, u, m.h, cut) : u;
-  m.a = cut ? make_float2(0.0f, 0.0f) : a;
+// one more row of a chunk's map (first: the map of the row alone)
+__device__ __forceinline__ void lr_extend(LrMap& m, bool first, float2 f, float2 u, bool cut, float2 one) {
+  m.h = first ? u : lr_step(f, u, m.h, cut, one);
+  m.a = first ? f : mul2(m.a, f);
+  if (cut) m.a = same2(0.0f);
+}
+// the same from the last row to the first, of the gradient
+__device__ __forceinline__ void lr_extend_back(LrMap& m, bool first, float2 f, float2 d, bool cut, float2 one) {
+  m.h = mul2(f, first ? d : add2(m.h, d, one));
+  m.a = first ? f : mul2(m.a, f);
+  if (cut) m.a = m.h = same2(0.0f);
+}
+// dg of a row: (dh (h_{t-1} - v)) (f z)
+__device__ __forceinline__ uint32_t lr_dg(float2 d, float2 diff, float2 f, float2 z) {
+  const float2 r = mul2(mul2(d, diff), mul2(f, z));
+  return bf_pair(r.x, r.y);
 }
 
-// CH channels a CTA: LANES lanes a chunk, BLOCKS blocks a round.
-template <int CH>
-struct LrDim {
-  static constexpr int LANES = CH / 2, BLOCKS = 64 / CH, PAD = CH == 64 ? 0 : 16;     // PAD: so that the two halves of a warp read different banks
-  static constexpr int STRIDE = LR_CHUNK * LANES + PAD, RAW = BLOCKS * LR_CHUNKS * STRIDE;
-};
-// NS: tensors that come in by asynchronous copies.  The block maps of the cluster, two rounds of them, lie behind this.
-template <int CH, int NS>
+// NS: tensors that come in by asynchronous copies.  A chunk's raw values take 16 words more than they have, so that the two chunks of a warp read
+// different banks.
+constexpr int LR_RAW = LR_CHUNK * 16 + 16;
+template <int NS>
 struct __align__(16) LrShared {
-  uint32_t raw[NS == 3 ? 2 : 1][NS][LrDim<CH>::RAW];     // backward two rounds; [chunk of the CTA][row][lane]
+  uint32_t raw[LR_WARPS][NS][LR_BLOCK][LR_RAW];          // of each warp: [tensor][chunk][row, lane of 16]
   float tab[LR_TAB];
-  float4 chunk[LR_T];                                    // [block of the CTA][chunk][lane]: the chunk maps of this round, then the maps of those before
-  float4 ahead[NS == 3 ? LR_T : 1];                      // backward: the same of the recurrence itself
-  float2 start[32];                                      // [block of the CTA][lane]: what comes into the blocks
-  float2 state[NS == 3 ? 32 : 1];                        // backward: the states in front of the blocks
-  unsigned long long arrived[2];                         // transaction barriers of the block maps, two rounds
+  float4 block[2][LR_WARPS][16];                         // the block maps of this round; two rounds
+  float4 span[2][LR_MAXC][16];                           // the span maps of the cluster; two rounds
+  unsigned long long arrived[2];                         // transaction barriers of the span maps, two rounds
   int gone;                                              // a wait ran out
-  __device__ __forceinline__ float4* slots(int round, int cl) { return reinterpret_cast<float4*>(this + 1) + (round & 1) * 32 * cl; }
-  static size_t bytes(int cl) { return sizeof(LrShared) + (size_t)2 * cl * 32 * sizeof(float4); }
 };
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
@@ -137,150 +147,189 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool t
   if (WORDS == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
-__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 struct LrArgs {
   const uint16_t *g, *v, *dy;
   const uint8_t* flags;
-  const float *first, *states;                           // state before the first row, or gradient of the state behind the last one
+  const float *first, *states;                           // what comes into the first chunk; backward: the states in front of the chunks
   uint16_t *y, *dg, *dv;
-  float *last, *save;                                    // what comes out at the other end; states at the starts of the blocks
+  float *last, *save;                                    // what comes out of the last chunk; forward: the states for the backward pass
   size_t ld, ld_y, ld_d;
-  int S, D, strips, nb, cl;                              // cl: CTAs of a cluster
+  int S, D, n, cl;                                       // n chunks, cl CTAs of a cluster
+  int strips, items, step, rounds;                       // strips of a row and of all sequences (items); from a CTA's item to its next, rounds of one
   int* status;
 };
 
-// Where a thread is
-template <int CH>
+// Where a thread is: rank in its cluster, warp (of the span, in the order of the pass), chunk o of its block, lane of 16.
 struct LrPlace {
-  int b, c0, rank, blk, k, lane;                         // sequence, first channel of the strip; block of the CTA's, chunk of the block, lane of the chunk
-  bool have;                                             // the lane's channels exist
+  int rank, warp, o, lane;
   __device__ __forceinline__ LrPlace(const LrArgs& p) {
     rank = blockIdx.x % p.cl;
-    const int q = blockIdx.x / p.cl;
-    b = q / p.strips;
-    lane = threadIdx.x % LrDim<CH>::LANES;
-    const int chunk = threadIdx.x / LrDim<CH>::LANES;
-    blk = chunk / LR_CHUNKS;
-    k = chunk % LR_CHUNKS;
-    c0 = (q % p.strips) * CH;
-    have = c0 + 2 * lane < p.D;
+    warp = threadIdx.x >> 5;
+    o = (threadIdx.x >> 4) & 1;
+    lane = threadIdx.x & 15;
   }
 };
-// The rows of the CTA's blocks of one tensor on their way, in pieces of WORDS words: block j starts at row first + j * step (64 or -64), rows
-// outside the sequence and channels outside the tensor are zeros.
-template <int CH, int WORDS>
-__device__ __forceinline__ void lr_fetch(uint32_t* raw, const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace<CH>& at, int first, int step) {
-  constexpr int LANES = LrDim<CH>::LANES, PER = LANES / WORDS, COUNT = LrDim<CH>::BLOCKS * LR_BLOCK * PER / LR_T;
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(raw);
-  const int word = (threadIdx.x % PER) * WORDS, r0 = threadIdx.x / PER;
-  const bool have = at.c0 + 2 * word < p.D;
-  const uint16_t* base = x + (size_t)at.b * p.S * ld + at.c0 + 2 * word;
+// What a CTA does in a round: the span `span` (in the order of the pass) of sequence b and the 32 channels from ch0 on.  Round k of an item (a sequence's
+// strip); only a lone CTA has more than one item.
+template <bool BACK>
+struct LrRound {
+  int item, k, b, ch0, span;
+  __device__ __forceinline__ LrRound(const LrArgs& p, const LrPlace& at) : item(blockIdx.x / p.cl), k(0) { begin(p, at); }
+  __device__ __forceinline__ void begin(const LrArgs& p, const LrPlace& at) {
+    b = item / p.strips;
+    ch0 = (item - b * p.strips) * LR_CH;
+    span = at.rank;
+  }
+  __device__ __forceinline__ bool more(const LrArgs& p) const { return item < p.items; }
+  __device__ __forceinline__ bool last(const LrArgs& p) const { return k + 1 == p.rounds; }
+  __device__ __forceinline__ void next(const LrArgs& p, const LrPlace& at) {
+    ++k;
+    span += p.cl;
+    if (k < p.rounds) return;
+    k = 0;
+    item += p.step;
+    begin(p, at);
+  }
+  // the first row of a warp's chunk; below 0 or from S on there is none
+  __device__ __forceinline__ int row(const LrArgs& p, int warp, int o) const {
+    const int chunk = (span * LR_WARPS + warp) * LR_BLOCK + o;
+    return (BACK ? p.n - 1 - chunk : chunk) * LR_CHUNK;
+  }
+  // all rows and all channels exist
+  __device__ __forceinline__ bool full(const LrArgs& p) const {
+    return ch0 + LR_CH <= p.D && (span + 1) * LR_ROWS <= (BACK ? p.n * LR_CHUNK : p.S) && (!BACK || span > 0 || p.S % LR_CHUNK == 0);
+  }
+  __device__ __forceinline__ size_t state(const LrArgs& p, const LrPlace& at) const { return (size_t)b * p.D + ch0 + 2 * at.lane; }
+};
+
+// A thread's place in a tensor of the rows, in pieces of WORDS words: where it reads or writes for the first chunk of its warp's block (WORDS 0: of its own
+// chunk, its own channels).  Kept from round to round: worked out anew for every row the addresses were a tenth of the instructions.
+template <int WORDS>
+struct LrCursor {
+  static constexpr int PER = WORDS ? 16 / WORDS : 16, ROWS = 32 / PER;                // pieces of a row, rows of an instruction
+  const uint16_t* at;
+  template <bool BACK>
+  __device__ __forceinline__ void begin(const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace& w, const LrRound<BACK>& r) {
+    const int l = threadIdx.x & 31, row = WORDS ? l / PER : 0;
+    at = x + ((long long)r.b * p.S + r.row(p, w.warp, WORDS ? 0 : w.o) + row) * (long long)ld + r.ch0 + (WORDS ? 2 * (l % PER * WORDS) : 2 * w.lane);
+  }
+  template <bool BACK>
+  __device__ __forceinline__ void next(size_t ld, const LrArgs& p) {
+    const long long d = (long long)p.cl * LR_ROWS * (long long)ld;
+    at += BACK ? -d : d;
+  }
+};
+// The rows of a warp's block of one tensor on their way.  The address is only followed where the row exists.
+template <bool BACK, int WORDS, bool FULL>
+__device__ __forceinline__ void lr_fetch(uint32_t (*raw)[LR_RAW], const LrCursor<WORDS>& c, const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace& at,
+                                         const LrRound<BACK>& r) {
+  constexpr int PER = LrCursor<WORDS>::PER, ROWS = LrCursor<WORDS>::ROWS;
+  const int l = threadIdx.x & 31, word = l % PER * WORDS, row = l / PER;
+  const bool have = FULL || r.ch0 + 2 * word < p.D;
+  const uint32_t dst = smem_u32(raw) + 4 * (row * 16 + word);
+  const int t0 = r.row(p, at.warp, 0) + row;
 #pragma unroll
-  for (int j = 0; j < COUNT; ++j) {
-    const int row = r0 + j * (LR_T / PER), t = first + (row / LR_BLOCK) * step + row % LR_BLOCK;
-    const bool there = have && (unsigned)t < (unsigned)p.S;
-    copy_async<WORDS>(dst + 4 * ((row / LR_CHUNK) * LrDim<CH>::STRIDE + (row % LR_CHUNK) * LANES + word), there ? base + (size_t)t * ld : x, there);
+  for (int j = 0; j < LR_BLOCK * LR_CHUNK / ROWS; ++j) {
+    // chunk 1 lies behind chunk 0 forward and before it backward
+    const int o = j * ROWS / LR_CHUNK, i = j * ROWS % LR_CHUNK, off = (BACK ? -o : o) * LR_CHUNK + i;
+    const bool there = FULL || (have && (unsigned)(t0 + off) < (unsigned)p.S);
+    copy_async<WORDS>(dst + 4 * (o * LR_RAW + i * 16), there ? c.at + off * (long long)ld : x, there);
   }
 }
-// the flag of row (lane of the chunk) of a chunk of n rows, and from the flags of the warp the cuts of this thread's chunk
-template <int CH, bool FLAGS>
-__device__ __forceinline__ bool lr_flag(const LrArgs& p, const LrPlace<CH>& at, int t0, int n) {
-  return FLAGS && at.lane < min(n, LR_CHUNK) && p.flags[(size_t)at.b * p.S + t0 + at.lane] != 0;
+// the flag of the row `lane` of a chunk of n rows from t on
+template <bool FLAGS>
+__device__ __forceinline__ bool lr_flag(const LrArgs& p, int b, int lane, int t, int n) {
+  return FLAGS && lane < min(n, LR_CHUNK) && p.flags[(size_t)b * p.S + t + lane] != 0;
 }
-template <int CH, bool FLAGS>
+// the cuts of this thread's chunk, from the flags of the warp
+template <bool FLAGS>
 __device__ __forceinline__ uint32_t lr_cuts(bool flag) {
   if (!FLAGS) return 0;
-  return __ballot_sync(0xffffffffu, flag) >> ((threadIdx.x & 31) & ~(CH / 2 - 1));
+  return (__ballot_sync(0xffffffffu, flag) >> (threadIdx.x & 16)) & 0xffu;
 }
-// The gates of a chunk.  A NaN gate comes out of the table as one of an infinity: it makes its gate a NaN here.
-__device__ __forceinline__ void lr_gates(const uint32_t* raw, int lanes, const float* tab, float f[LR_CHUNK][2], float z[LR_CHUNK][2]) {
-  uint32_t top = 0;
+// The gates of a chunk.  A NaN comes out of the table as an infinity's gate and is put right here.  Whether there is one (or an infinity) shows the sum
+// of all words times zero.
+__device__ __forceinline__ void lr_gates(const uint32_t* raw, const float* tab, float2 f[LR_CHUNK], float2 z[LR_CHUNK]) {
+  __nv_bfloat162 odd = __float2bfloat162_rn(0.0f);
 #pragma unroll
   for (int i = 0; i < LR_CHUNK; ++i) {
-    const uint32_t w = raw[i * lanes];
+    const uint32_t w = raw[i * 16];
     lr_gate2<true>(w, tab, f[i], z[i]);
-    top = __vmaxu2(top, w & 0x7fff7fffu);
+    odd = __hfma2(reinterpret_cast<const __nv_bfloat162&>(w), __float2bfloat162_rn(0.0f), odd);
   }
-  if ((top & 0xffffu) > 0x7f80u || (top >> 16) > 0x7f80u) {
+  if (reinterpret_cast<uint32_t&>(odd) & 0x7fff7fffu) {
 #pragma unroll
     for (int i = 0; i < LR_CHUNK; ++i) {
-      const uint32_t w = raw[i * lanes];
-      if ((w & 0x7fffu) > 0x7f80u) f[i][0] = z[i][0] = __int_as_float(0x7fffffff);
-      if (((w >> 16) & 0x7fffu) > 0x7f80u) f[i][1] = z[i][1] = __int_as_float(0x7fffffff);
+      const uint32_t w = raw[i * 16];
+      if ((w & 0x7fffu) > 0x7f80u) f[i].x = z[i].x = __int_as_float(0x7fffffff);
+      if (((w >> 16) & 0x7fffu) > 0x7f80u) f[i].y = z[i].y = __int_as_float(0x7fffffff);
     }
   }
 }
-// The maps of the `chunks` chunks of a block, one after the other, by one thread: the map of those before chunk k takes chunk k's place, the map
-// of all comes back.
-template <int LANES>
-__device__ __forceinline__ LrMap lr_scan(float4* chunk, int chunks) {
-  LrMap m = lr_unpack(chunk[0]);
-  if (chunks == LR_CHUNKS) {
-    float4 next[LR_CHUNKS];
-#pragma unroll
-    for (int i = 1; i < LR_CHUNKS; ++i) next[i] = chunk[i * LANES];
-#pragma unroll
-    for (int i = 1; i < LR_CHUNKS; ++i) {
-      chunk[i * LANES] = lr_pack(m);
-      m = lr_compose(m, lr_unpack(next[i]));
-    }
-  } else {
-#pragma unroll 1
-    for (int i = 1; i < chunks; ++i) {
-      const LrMap here = lr_unpack(chunk[i * LANES]);
-      chunk[i * LANES] = lr_pack(m);
-      m = lr_compose(m, here);
-    }
-  }
-  return m;
+__device__ __forceinline__ LrMap lr_from(const LrMap& m, int lane) {
+  return LrMap{make_float2(__shfl_sync(0xffffffffu, m.a.x, lane), __shfl_sync(0xffffffffu, m.a.y, lane)),
+               make_float2(__shfl_sync(0xffffffffu, m.h.x, lane), __shfl_sync(0xffffffffu, m.h.y, lane))};
 }
-// The round's hand-over, by the first warp, a thread per block of the CTA and lane: block maps to the CTAs of the cluster, what comes into each block
-// of this CTA back.  `s`, what comes into the round, becomes what comes into the next one.  `chunks` of the thread's block exist, in the places from
-// `first` on; `blocks` of the round.
-// The maps of two rounds have places of their own: a CTA sends those of round r + 2 when it has all of round r + 1, this CTA's among them, which this CTA
-// sent after it had read round r's.
-template <int CH, int NS>
-__device__ __forceinline__ float2 lr_hand_over(LrShared<CH, NS>& sh, const LrArgs& p, const LrPlace<CH>& at, int round, int first, int chunks, int blocks,
-                                               float2& s) {
-  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS, BATCH = 8;
-  const int blk = threadIdx.x / LANES, own = at.rank * BLOCKS + blk;
-  float4* slots = sh.slots(round, p.cl);
-  uint64_t* bar = reinterpret_cast<uint64_t*>(&sh.arrived[round & 1]);
-  if (p.cl > 1 && threadIdx.x == 0) mbar_expect_tx(bar, p.cl * 32 * sizeof(float4));
-  const float4 whole = lr_pack(lr_scan<LANES>(sh.chunk + (blk * LR_CHUNKS + first) * LANES + at.lane, chunks));
-  if (p.cl == 1) {
-    slots[own * LANES + at.lane] = whole;
-    __syncwarp();
-  } else {
-#pragma unroll 4
-    for (int r = 0; r < p.cl; ++r) store_in_cluster(&slots[own * LANES + at.lane], bar, r, whole);
-    mbar_wait_warp(bar, (round >> 1) & 1, &sh.gone, p.status);
+// The hand-over of a round: the map of this thread's chunk in, what comes into the chunk out; `s`, what comes into the round, becomes what comes into
+// the next one.  `turn` counts the rounds of the CTA.
+// The maps of two rounds have places of their own: a warp writes its block's map of round r + 2 behind the barrier of round r + 1, which all warps pass
+// when they have read round r's; a CTA sends its span's map of round r + 2 when it has all of round r + 1, those of the receiver among them, which that
+// one sent behind the same barrier.
+template <bool FULL, bool BACK, int NS>
+__device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p, const LrPlace& at, const LrRound<BACK>& r, int turn, const LrMap& mine, float2& s,
+                                               float2 one) {
+  const int chunks = p.n - r.span * LR_WARPS * LR_BLOCK, blocks = (chunks + 1) / LR_BLOCK;               // from the CTA's first ones on
+  const LrMap other = lr_from(mine, threadIdx.x ^ 16), both = lr_compose(other, mine, one);              // `both`: in the lanes of chunk 1
+  const bool two = FULL || chunks > at.warp * LR_BLOCK + 1;
+  float4(*const maps)[16] = sh.block[turn & 1];
+  if (at.o == (two ? 1 : 0)) maps[at.warp][at.lane] = lr_pack(two ? both : mine);
+  if (p.cl > 1 && threadIdx.x == 0) mbar_expect_tx(reinterpret_cast<uint64_t*>(&sh.arrived[turn & 1]), p.cl * 16 * sizeof(float4));
+  __syncthreads();
+  // a group in each half of the warp
+  LrMap group = lr_unpack(maps[at.o * LR_GROUP][at.lane]), before = group;
+#pragma unroll
+  for (int i = 1; i < LR_GROUP; ++i) {
+    const LrMap m = lr_unpack(maps[at.o * LR_GROUP + i][at.lane]);
+    if (i == (at.warp & 3)) before = group;
+    if (FULL || at.o * LR_GROUP + i < blocks) group = lr_compose(group, m, one);
   }
+  const int half = at.warp / LR_GROUP;
+  before = lr_from(before, half * 16 + at.lane);
+  const LrMap g0 = lr_from(group, at.lane), g1 = lr_from(group, 16 + at.lane);
+  LrMap span = g0;
+  if (FULL || blocks > LR_GROUP) span = lr_compose(g0, g1, one);
   float2 start = s;
   if (p.cl == 1) {
-    for (int r = 0; r < blocks; ++r) {
-      if (r == own) start = s;
-      s = lr_apply(lr_unpack(slots[r * LANES + at.lane]), s);
-    }
-    return start;
-  }
-  for (int r0 = 0; r0 < blocks; r0 += BATCH) {
-    float4 m[BATCH];
+    s = lr_apply(span, s, one);
+  } else {
+    constexpr int BATCH = 4;
+    uint64_t* bar = reinterpret_cast<uint64_t*>(&sh.arrived[turn & 1]);
+    float4(*const place)[16] = sh.span[turn & 1];
+    const int to = at.warp + LR_WARPS * at.o;
+    if (to < p.cl) store_in_cluster(&place[at.rank][at.lane], bar, to, lr_pack(span));
+    mbar_wait_warp(bar, (turn >> 1) & 1, &sh.gone, p.status);
+    const int spans = min(p.cl, (p.n + LR_WARPS * LR_BLOCK - 1) / (LR_WARPS * LR_BLOCK) - (r.span - at.rank));
+    for (int r0 = 0; r0 < spans; r0 += BATCH) {
+      float4 m[BATCH];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) m[i] = slots[min(r0 + i, blocks - 1) * LANES + at.lane];
+      for (int i = 0; i < BATCH; ++i) m[i] = place[min(r0 + i, spans - 1)][at.lane];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      if (r0 + i == own) start = s;
-      if (r0 + i < blocks) s = lr_apply(lr_unpack(m[i]), s);
+      for (int i = 0; i < BATCH; ++i) {
+        if (r0 + i == at.rank) start = s;
+        if (r0 + i < spans) s = lr_apply(lr_unpack(m[i]), s, one);
+      }
     }
   }
-  return start;
+  if (half) start = lr_apply(g0, start, one);
+  if (at.warp & 3) start = lr_apply(before, start, one);
+  const float2 second = lr_apply(other, start, one);
+  return at.o ? second : start;
 }
-// before the first round: the barriers, known to the cluster before anyone sends
-template <int CH, int NS>
-__device__ __forceinline__ void lr_open(LrShared<CH, NS>& sh, const LrArgs& p) {
+// before the first round: the barriers, known to the cluster before anyone sends, and the table on its way
+template <int NS>
+__device__ __forceinline__ void lr_open(LrShared<NS>& sh, const LrArgs& p) {
   if (threadIdx.x == 0) {
     sh.gone = 0;
     mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[0]), 1);
@@ -289,6 +338,8 @@ __device__ __forceinline__ void lr_open(LrShared<CH, NS>& sh, const LrArgs& p) {
   }
   __syncthreads();
   if (p.cl > 1) cluster_arrive();
+  const uint32_t dst = smem_u32(sh.tab);
+  for (int i = threadIdx.x; i < LR_TAB / 4; i += LR_T) copy_async<4>(dst + 16 * i, lr_table_image.m + 4 * i, true);
 }
 // no CTA leaves while another one may still send to it (after a wait that ran out)
 __device__ __forceinline__ void lr_close(const LrArgs& p) {
@@ -296,182 +347,196 @@ __device__ __forceinline__ void lr_close(const LrArgs& p) {
   cluster_arrive();
   cluster_wait();
 }
-template <int CH, int NS>
-__device__ __forceinline__ void lr_copy_table(LrShared<CH, NS>& sh) {
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(sh.tab);
-  for (int i = threadIdx.x; i < LR_TAB / 4; i += LR_T) copy_async<4>(dst + 16 * i, lr_table_image.m + 4 * i, true);
-}
-
-template <int CH, int WORDS, bool FLAGS>
-__global__ void __launch_bounds__(LR_T, 4) k_linrec_fwd(const __grid_constant__ LrArgs p) {
+template <int WORDS, bool FLAGS>
+__global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<CH, 2>& sh = *reinterpret_cast<LrShared<CH, 2>*>(smem);
-  const LrPlace<CH> at(p);
-  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
+  LrShared<2>& sh = *reinterpret_cast<LrShared<2>*>(smem);
+  const LrPlace at(p);
+  const float2 one = same2(c_one);
   lr_open(sh, p);
-  lr_copy_table(sh);
   grid_dep();
-  const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per, step = per * LR_BLOCK;
-  int b0 = at.rank * BLOCKS * LR_BLOCK;                  // the CTA's first row of the round
-  const int ch = at.c0 + 2 * at.lane;
-  const bool lead = threadIdx.x < 32;
+  uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
+  LrRound<false> r(p, at), ahead = r;
   bool flag = false;
-  auto fetch = [&](int row) {
-    lr_fetch<CH, WORDS>(sh.raw[0][0], p.g, p.ld, p, at, row, LR_BLOCK);
-    lr_fetch<CH, WORDS>(sh.raw[0][1], p.v, p.ld, p, at, row, LR_BLOCK);
-    const int t = row + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK;
-    flag = lr_flag<CH, FLAGS>(p, at, t, p.S - t);
+  float2 s = make_float2(0.0f, 0.0f), first = s;
+  LrCursor<WORDS> cg, cv;
+  LrCursor<0> cy;
+  auto fetch = [&] {
+    const LrRound<false>& r = ahead;                       // of the round that is fetched
+    if (r.k == 0) {
+      cg.template begin<false>(p.g, p.ld, p, at, r);
+      cv.template begin<false>(p.v, p.ld, p, at, r);
+    } else {
+      cg.template next<false>(p.ld, p);
+      cv.template next<false>(p.ld, p);
+    }
+    if (r.full(p)) {
+      lr_fetch<false, WORDS, true>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<false, WORDS, true>(raw[1], cv, p.v, p.ld, p, at, r);
+    } else {
+      lr_fetch<false, WORDS, false>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<false, WORDS, false>(raw[1], cv, p.v, p.ld, p, at, r);
+    }
+    const int t = r.row(p, at.warp, at.o);
+    flag = lr_flag<FLAGS>(p, r.b, at.lane, t, p.S - t);
+    if (p.first && ahead.k == 0 && r.ch0 + 2 * at.lane < p.D) first = *reinterpret_cast<const float2*>(p.first + r.state(p, at));
+    ahead.next(p, at);
   };
-  fetch(b0);
-  float2 s = make_float2(0.0f, 0.0f);
-  if (lead && p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + ch);
+  fetch();
   copies_done();
-  __syncthreads();
+  __syncthreads();                                       // the table
   if (p.cl > 1) cluster_wait();
-  for (int k = 0; k < rounds; ++k, b0 += step) {
-    const int t0 = b0 + (at.blk * LR_CHUNKS + at.k) * LR_CHUNK, n = p.S - t0;          // n rows of the chunk exist
-    const uint32_t cuts = lr_cuts<CH, FLAGS>(flag);
-    const uint32_t* raw = sh.raw[0][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
-    float f[LR_CHUNK][2], u[LR_CHUNK][2];
-    lr_gates(raw, LANES, sh.tab, f, u);
-    raw += LrDim<CH>::RAW;
-    LrMap mine;
+  int turn = 0;
+  for (; r.more(p); r.next(p, at), ++turn) {
+    const int t0 = r.row(p, at.warp, at.o);
+    if (r.k == 0) {
+      s = first;
+      cy.template begin<false>(p.y, p.ld_y, p, at, r);
+    }
+    auto round = [&](auto whole) {
+      constexpr bool FULL = decltype(whole)::value;
+      const int n = FULL ? LR_CHUNK : p.S - t0;          // n rows of the chunk exist
+      const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
+      const uint32_t cuts = lr_cuts<FLAGS>(flag);
+      const uint32_t* q = raw[0][at.o] + at.lane;
+      float2 f[LR_CHUNK], u[LR_CHUNK];
+      lr_gates(q, sh.tab, f, u);
+      LrMap mine;
 #pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) {
-      const uint32_t w = raw[i * LANES];
-      u[i][0] = fmul(u[i][0], bflo(w));
-      u[i][1] = fmul(u[i][1], bfhi(w));
-      lr_extend(mine, i, n, f[i], make_float2(u[i][0], u[i][1]), (cuts >> i) & 1);
-    }
-    sh.chunk[threadIdx.x] = lr_pack(mine);               // [block][chunk][lane] is the thread's number
-    __syncthreads();
-    if (k + 1 < rounds) fetch(b0 + step);                // the raw values of this round are read
-    if (lead) {
-      const int row = b0 + (threadIdx.x / LANES) * LR_BLOCK, blk = row / LR_BLOCK;
-      const int chunks = max(0, min(LR_CHUNKS, (p.S - row + LR_CHUNK - 1) / LR_CHUNK));
-      const float2 start = lr_hand_over(sh, p, at, k, 0, chunks, min(per, p.nb - k * per), s);
-      sh.start[threadIdx.x] = start;
-      if (p.save && chunks > 0 && at.have) *reinterpret_cast<float2*>(p.save + ((size_t)at.b * p.nb + blk) * p.D + ch) = start;
-    }
+      for (int i = 0; i < LR_CHUNK; ++i) {
+        const uint32_t w = q[LR_BLOCK * LR_RAW + i * 16];
+        u[i] = mul2(u[i], make_float2(bflo(w), bfhi(w)));
+        if (i == 0 || i < n) lr_extend(mine, i == 0, f[i], u[i], (cuts >> i) & 1, one);
+      }
+      __syncwarp();
+      if (ahead.more(p)) fetch();
+      float2 h = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
+      if (p.save && n > 0 && have) *reinterpret_cast<float2*>(p.save + r.state(p, at) + ((size_t)r.b * (p.n - 1) + t0 / LR_CHUNK) * p.D) = h;
+      uint16_t* out = const_cast<uint16_t*>(cy.at);
+#pragma unroll
+      for (int i = 0; i < LR_CHUNK; ++i) {
+        h = lr_step(f[i], u[i], h, (cuts >> i) & 1, one);
+        if (i < n && have) *reinterpret_cast<uint32_t*>(out) = bf_pair(h.x, h.y);
+        out += p.ld_y;
+      }
+    };
+    if (r.full(p)) round(std::true_type{});
+    else round(std::false_type{});
+    cy.template next<false>(p.ld_y, p);
+    if (p.last && r.last(p) && threadIdx.x < 16 && at.rank == 0 && r.ch0 + 2 * at.lane < p.D) *reinterpret_cast<float2*>(p.last + r.state(p, at)) = s;
     copies_done();
-    __syncthreads();
-    if (sh.gone) break;
-    float2 h = sh.start[at.blk * LANES + at.lane];
-    if (at.k) h = lr_apply(lr_unpack(sh.chunk[threadIdx.x]), h);
-    uint16_t* out = p.y + ((size_t)at.b * p.S + t0) * p.ld_y + ch;
-#pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) {
-      h = lr_step(f[i], make_float2(u[i][0], u[i][1]), h, (cuts >> i) & 1);
-      if (i < n && at.have) *reinterpret_cast<uint32_t*>(out) = pack_bf2(h.x, h.y);
-      out += p.ld_y;
-    }
     __syncwarp();
+    if (p.cl > 1 && __any_sync(0xffffffffu, *static_cast<volatile int*>(&sh.gone))) break;
   }
-  copies_done();
   lr_close(p);
-  if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
-template <int CH, int WORDS, bool FLAGS>
+template <int WORDS, bool FLAGS>
 __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<CH, 3>& sh = *reinterpret_cast<LrShared<CH, 3>*>(smem);
-  const LrPlace<CH> at(p);
-  constexpr int LANES = LrDim<CH>::LANES, BLOCKS = LrDim<CH>::BLOCKS;
+  LrShared<3>& sh = *reinterpret_cast<LrShared<3>*>(smem);
+  const LrPlace at(p);
+  const float2 one = same2(c_one);
   lr_open(sh, p);
-  lr_copy_table(sh);
   grid_dep();
-  const int per = p.cl * BLOCKS, rounds = (p.nb + per - 1) / per;
-  const int ch = at.c0 + 2 * at.lane, warp = threadIdx.x >> 5, own = (threadIdx.x & 31) / LANES;
-  int top = p.nb - 1 - at.rank * BLOCKS;                 // the CTA's blocks of the round are top, top - 1; below 0: none
+  uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
+  LrRound<true> r(p, at), ahead = r;
   bool flag = false;
-  float2 state = make_float2(0.0f, 0.0f);
-  auto fetch = [&](int round, int first) {
-    const int row = first * LR_BLOCK;
-    lr_fetch<CH, WORDS>(sh.raw[round & 1][0], p.g, p.ld, p, at, row, -LR_BLOCK);
-    lr_fetch<CH, WORDS>(sh.raw[round & 1][1], p.v, p.ld, p, at, row, -LR_BLOCK);
-    lr_fetch<CH, WORDS>(sh.raw[round & 1][2], p.dy, p.ld_y, p, at, row, -LR_BLOCK);
-    const int t = (first - at.blk) * LR_BLOCK + at.k * LR_CHUNK;
-    flag = lr_flag<CH, FLAGS>(p, at, t, first - at.blk < 0 ? 0 : p.S - t);
-    if (warp == 1 && first - own >= 0 && at.have) state = *reinterpret_cast<const float2*>(p.states + ((size_t)at.b * p.nb + first - own) * p.D + ch);
+  float2 s = make_float2(0.0f, 0.0f), first = s, next = s;                            // next: the state in front of the thread's chunk
+  LrCursor<WORDS> cg, cv, cdy;
+  LrCursor<0> odv, odg;
+  auto fetch = [&] {
+    const LrRound<true>& r = ahead;                       // of the round that is fetched
+    if (r.k == 0) {
+      cg.template begin<true>(p.g, p.ld, p, at, r);
+      cv.template begin<true>(p.v, p.ld, p, at, r);
+      cdy.template begin<true>(p.dy, p.ld_y, p, at, r);
+    } else {
+      cg.template next<true>(p.ld, p);
+      cv.template next<true>(p.ld, p);
+      cdy.template next<true>(p.ld_y, p);
+    }
+    if (r.full(p)) {
+      lr_fetch<true, WORDS, true>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<true, WORDS, true>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<true, WORDS, true>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
+    } else {
+      lr_fetch<true, WORDS, false>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<true, WORDS, false>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<true, WORDS, false>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
+    }
+    const int t = r.row(p, at.warp, at.o);
+    const bool have = r.ch0 + 2 * at.lane < p.D;
+    flag = lr_flag<FLAGS>(p, r.b, at.lane, t, t < 0 ? 0 : p.S - t);
+    if (t >= 0 && have) next = *reinterpret_cast<const float2*>(p.states + r.state(p, at) + ((size_t)r.b * (p.n - 1) + t / LR_CHUNK) * p.D);
+    if (p.first && ahead.k == 0 && have) first = *reinterpret_cast<const float2*>(p.first + r.state(p, at));
+    ahead.next(p, at);
   };
-  fetch(0, top);
-  float2 s = make_float2(0.0f, 0.0f);
-  if (warp == 0 && p.first && at.have) s = *reinterpret_cast<const float2*>(p.first + (size_t)at.b * p.D + ch);
+  fetch();
   copies_done();
-  __syncthreads();
+  __syncthreads();                                       // the table
   if (p.cl > 1) cluster_wait();
-  for (int r = 0; r < rounds; ++r, top -= per) {
-    const int blk = top - at.blk, t0 = blk * LR_BLOCK + at.k * LR_CHUNK, n = blk < 0 ? 0 : p.S - t0;
-    const int chunks = blk < 0 ? 0 : min(LR_CHUNKS, (p.S - blk * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK);
-    const uint32_t cuts = lr_cuts<CH, FLAGS>(flag);
-    const float2 front = state;
-    if (r + 1 < rounds) fetch(r + 1, top - per);
-    const uint32_t* raw = sh.raw[r & 1][0] + (at.blk * LR_CHUNKS + at.k) * LrDim<CH>::STRIDE + at.lane;
-    float f[LR_CHUNK][2], z[LR_CHUNK][2];
-    uint32_t wv[LR_CHUNK], wd[LR_CHUNK];
-    lr_gates(raw, LANES, sh.tab, f, z);
-    LrMap mine, fore;                                    // of the gradient, of the state
+  int turn = 0;
+  for (; r.more(p); r.next(p, at), ++turn) {
+    const int t0 = r.row(p, at.warp, at.o);
+    if (r.k == 0) {
+      s = first;
+      odv.template begin<true>(p.dv, p.ld_d, p, at, r);
+      odg.template begin<true>(p.dg, p.ld_d, p, at, r);
+    }
+    auto round = [&](auto whole) {
+      constexpr bool FULL = decltype(whole)::value;
+      const int n = FULL ? LR_CHUNK : t0 < 0 ? 0 : p.S - t0;                          // n rows of the chunk exist
+      const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
+      const uint32_t cuts = lr_cuts<FLAGS>(flag);
+      float2 h = next;
+      const uint32_t* q = raw[0][at.o] + at.lane;
+      float2 f[LR_CHUNK], z[LR_CHUNK];
+      uint32_t wv[LR_CHUNK], wd[LR_CHUNK];
+      lr_gates(q, sh.tab, f, z);
 #pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) {
-      wv[i] = raw[LrDim<CH>::RAW + i * LANES];
-      wd[i] = raw[2 * LrDim<CH>::RAW + i * LANES];
-      lr_extend(fore, i, n, f[i], make_float2(fmul(z[i][0], bflo(wv[i])), fmul(z[i][1], bfhi(wv[i]))), (cuts >> i) & 1);
-    }
-    bool any = false;
-    mine.a = mine.h = make_float2(0.0f, 0.0f);
+      for (int i = 0; i < LR_CHUNK; ++i) {
+        wv[i] = q[LR_BLOCK * LR_RAW + i * 16];
+        wd[i] = q[2 * LR_BLOCK * LR_RAW + i * 16];
+      }
+      __syncwarp();
+      if (ahead.more(p)) fetch();
+      LrMap mine;
+      mine.a = mine.h = same2(0.0f);
 #pragma unroll
-    for (int i = LR_CHUNK - 1; i >= 0; --i) {
-      if (i >= n) continue;
-      const float2 d = make_float2(bflo(wd[i]), bfhi(wd[i]));
-      mine.h = any ? make_float2(fmul(f[i][0], fadd(d.x, mine.h.x)), fmul(f[i][1], fadd(d.y, mine.h.y))) : make_float2(fmul(f[i][0], d.x), fmul(f[i][1], d.y));
-      mine.a = any ? make_float2(fmul(f[i][0], mine.a.x), fmul(f[i][1], mine.a.y)) : make_float2(f[i][0], f[i][1]);
-      if ((cuts >> i) & 1) mine.a = mine.h = make_float2(0.0f, 0.0f);
-      any = true;
-    }
-    // in the order of the backward pass: the block's last chunk, which may not exist, has the first place
-    float4* place = sh.chunk + (at.blk * LR_CHUNKS + LR_CHUNKS - 1 - at.k) * LANES + at.lane;
-    *place = lr_pack(mine);
-    sh.ahead[threadIdx.x] = lr_pack(fore);
-    __syncthreads();
-    if (warp == 0) {
-      const int b = top - own, have = b < 0 ? 0 : min(LR_CHUNKS, (p.S - b * LR_BLOCK + LR_CHUNK - 1) / LR_CHUNK);
-      sh.start[threadIdx.x] = lr_hand_over(sh, p, at, r, have ? LR_CHUNKS - have : 0, have, min(per, p.nb - r * per), s);
-    } else if (warp == 1) {
-      lr_scan<LANES>(sh.ahead + own * LR_CHUNKS * LANES + at.lane, LR_CHUNKS);
-      sh.state[threadIdx.x & 31] = front;
-    }
+      for (int i = LR_CHUNK - 1; i >= 0; --i)
+        if (i < n) lr_extend_back(mine, i == (FULL ? LR_CHUNK : min(n, LR_CHUNK)) - 1, f[i], make_float2(bflo(wd[i]), bfhi(wd[i])), (cuts >> i) & 1, one);
+      float2 c = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
+      float2 diff[LR_CHUNK];                             // h_{t-1} - v
+#pragma unroll
+      for (int i = 0; i < LR_CHUNK; ++i) {
+        const bool cut = (cuts >> i) & 1;
+        const float2 v = make_float2(bflo(wv[i]), bfhi(wv[i]));
+        diff[i] = lr_sub(cut ? same2(0.0f) : h, v);
+        h = lr_step(f[i], mul2(z[i], v), h, cut, one);
+      }
+      uint16_t *dv = const_cast<uint16_t*>(odv.at) + (LR_CHUNK - 1) * p.ld_d, *dg = const_cast<uint16_t*>(odg.at) + (LR_CHUNK - 1) * p.ld_d;
+#pragma unroll
+      for (int i = LR_CHUNK - 1; i >= 0; --i, dv -= p.ld_d, dg -= p.ld_d) {
+        if (i >= n) continue;
+        const float2 d = add2(c, make_float2(bflo(wd[i]), bfhi(wd[i])), one), w = mul2(d, z[i]);
+        c = mul2(f[i], d);
+        if ((cuts >> i) & 1) c = same2(0.0f);
+        if (!have) continue;
+        *reinterpret_cast<uint32_t*>(dv) = bf_pair(w.x, w.y);
+        *reinterpret_cast<uint32_t*>(dg) = lr_dg(d, diff[i], f[i], z[i]);
+      }
+    };
+    if (r.full(p)) round(std::true_type{});
+    else round(std::false_type{});
+    odv.template next<true>(p.ld_d, p);
+    odg.template next<true>(p.ld_d, p);
+    if (p.last && r.last(p) && threadIdx.x < 16 && at.rank == 0 && r.ch0 + 2 * at.lane < p.D) *reinterpret_cast<float2*>(p.last + r.state(p, at)) = s;
     copies_done();
-    __syncthreads();
-    if (sh.gone) break;
-    float2 h = sh.state[at.blk * LANES + at.lane], c = sh.start[at.blk * LANES + at.lane];
-    if (at.k) h = lr_apply(lr_unpack(sh.ahead[threadIdx.x]), h);
-    if (at.k + 1 < chunks) c = lr_apply(lr_unpack(*place), c);
-    float2 diff[LR_CHUNK];                               // h_{t-1} - v
-#pragma unroll
-    for (int i = 0; i < LR_CHUNK; ++i) {
-      const bool cut = (cuts >> i) & 1;
-      const float2 v = make_float2(bflo(wv[i]), bfhi(wv[i]));
-      diff[i] = cut ? make_float2(fsub(0.0f, v.x), fsub(0.0f, v.y)) : make_float2(fsub(h.x, v.x), fsub(h.y, v.y));
-      h = lr_step(f[i], make_float2(fmul(z[i][0], v.x), fmul(z[i][1], v.y)), h, cut);
-    }
-    const size_t o = ((size_t)at.b * p.S + t0 + LR_CHUNK - 1) * p.ld_d + ch;           // only followed where the row exists
-    uint16_t *dv = p.dv + o, *dg = p.dg + o;
-#pragma unroll
-    for (int i = LR_CHUNK - 1; i >= 0; --i, dv -= p.ld_d, dg -= p.ld_d) {
-      if (i >= n) continue;
-      const float2 d = make_float2(fadd(bflo(wd[i]), c.x), fadd(bfhi(wd[i]), c.y));
-      c = (cuts >> i) & 1 ? make_float2(0.0f, 0.0f) : make_float2(fmul(f[i][0], d.x), fmul(f[i][1], d.y));
-      if (!at.have) continue;
-      *reinterpret_cast<uint32_t*>(dv) = pack_bf2(fmul(d.x, z[i][0]), fmul(d.y, z[i][1]));
-      *reinterpret_cast<uint32_t*>(dg) =
-          pack_bf2(fmul(fmul(d.x, diff[i].x), fmul(f[i][0], z[i][0])), fmul(fmul(d.y, diff[i].y), fmul(f[i][1], z[i][1])));
-    }
     __syncwarp();
+    if (p.cl > 1 && __any_sync(0xffffffffu, *static_cast<volatile int*>(&sh.gone))) break;
   }
-  copies_done();
   lr_close(p);
-  if (p.last && at.have && threadIdx.x < LANES && at.rank == 0) *reinterpret_cast<float2*>(p.last + (size_t)at.b * p.D + ch) = s;
 }
 
 // Sequences of one chunk (a token at a time among them): a thread walks two channels alone, with nothing to hand over.
@@ -494,20 +559,20 @@ __global__ void __launch_bounds__(128) k_linrec_chunk(const __grid_constant__ Lr
   float2 s = p.first ? *reinterpret_cast<const float2*>(p.first + at) : make_float2(0.0f, 0.0f);
   float2 h = BWD ? *reinterpret_cast<const float2*>(p.states + at) : s;
   if (p.save) *reinterpret_cast<float2*>(p.save + at) = s;
-  float f[LR_CHUNK][2], z[LR_CHUNK][2];
-  float2 prev[LR_CHUNK];
+  const float2 one = same2(c_one);
+  float2 f[LR_CHUNK], z[LR_CHUNK], diff[LR_CHUNK];
   LrMap m;
-  m.a = m.h = make_float2(0.0f, 0.0f);
+  m.a = m.h = same2(0.0f);
 #pragma unroll
   for (int t = 0; t < LR_CHUNK; ++t) {
     if (t >= n) continue;
     lr_gate2<false>(wg[t], nullptr, f[t], z[t]);
     const bool cut = (cuts >> t) & 1;
-    const float2 v = make_float2(bflo(wv[t]), bfhi(wv[t])), u = make_float2(fmul(z[t][0], v.x), fmul(z[t][1], v.y));
-    if (!BWD) lr_extend(m, t, n, f[t], u, cut);
-    prev[t] = cut ? make_float2(fsub(0.0f, v.x), fsub(0.0f, v.y)) : make_float2(fsub(h.x, v.x), fsub(h.y, v.y));
-    h = lr_step(f[t], u, h, cut);
-    if (!BWD) *reinterpret_cast<uint32_t*>(p.y + (row + t) * p.ld_y + c0) = pack_bf2(h.x, h.y);
+    const float2 v = make_float2(bflo(wv[t]), bfhi(wv[t])), u = mul2(z[t], v);
+    if (!BWD) lr_extend(m, t == 0, f[t], u, cut, one);
+    diff[t] = lr_sub(cut ? same2(0.0f) : h, v);
+    h = lr_step(f[t], u, h, cut, one);
+    if (!BWD) *reinterpret_cast<uint32_t*>(p.y + (row + t) * p.ld_y + c0) = bf_pair(h.x, h.y);
   }
   if (BWD) {
     float2 c = s;
@@ -515,88 +580,119 @@ __global__ void __launch_bounds__(128) k_linrec_chunk(const __grid_constant__ Lr
     for (int t = LR_CHUNK - 1; t >= 0; --t) {
       if (t >= n) continue;
       const bool cut = (cuts >> t) & 1;
-      const float2 dy = make_float2(bflo(wd[t]), bfhi(wd[t])), d = make_float2(fadd(dy.x, c.x), fadd(dy.y, c.y));
-      c = cut ? make_float2(0.0f, 0.0f) : make_float2(fmul(f[t][0], d.x), fmul(f[t][1], d.y));
-      m.h = t + 1 < n ? make_float2(fmul(f[t][0], fadd(dy.x, m.h.x)), fmul(f[t][1], fadd(dy.y, m.h.y))) : make_float2(fmul(f[t][0], dy.x), fmul(f[t][1], dy.y));
-      m.a = t + 1 < n ? make_float2(fmul(f[t][0], m.a.x), fmul(f[t][1], m.a.y)) : make_float2(f[t][0], f[t][1]);
-      if (cut) m.a = m.h = make_float2(0.0f, 0.0f);
-      *reinterpret_cast<uint32_t*>(p.dv + (row + t) * p.ld_d + c0) = pack_bf2(fmul(d.x, z[t][0]), fmul(d.y, z[t][1]));
-      *reinterpret_cast<uint32_t*>(p.dg + (row + t) * p.ld_d + c0) =
-          pack_bf2(fmul(fmul(d.x, prev[t].x), fmul(f[t][0], z[t][0])), fmul(fmul(d.y, prev[t].y), fmul(f[t][1], z[t][1])));
+      const float2 dy = make_float2(bflo(wd[t]), bfhi(wd[t])), d = add2(c, dy, one), w = mul2(d, z[t]);
+      c = cut ? same2(0.0f) : mul2(f[t], d);
+      lr_extend_back(m, t == n - 1, f[t], dy, cut, one);
+      *reinterpret_cast<uint32_t*>(p.dv + (row + t) * p.ld_d + c0) = bf_pair(w.x, w.y);
+      *reinterpret_cast<uint32_t*>(p.dg + (row + t) * p.ld_d + c0) = lr_dg(d, diff[t], f[t], z[t]);
     }
   }
-  if (p.last) *reinterpret_cast<float2*>(p.last + at) = lr_apply(m, s);
+  if (p.last) *reinterpret_cast<float2*>(p.last + at) = lr_apply(m, s, one);
 }
 
-// The strip and the cluster: narrow strips, then larger clusters, while their CTAs are all on the GPU at once (`per_sm` of them on an SM), no more CTAs
-// than there are blocks.  Clusters do not fill the GPU: of 444 CTAs, three on an SM, 416 fit in clusters of 4, 384 in clusters of 8, 336 in
-// clusters of 16, and a round of 65536 x 512 that needed 256 of 224 took twice as long.
-struct LrPlan { int ch, cl; };
-static LrPlan lr_plan(int B, int D, int nb, int per_sm) {
-  const long long slots = (long long)per_sm * dev_sm_count();
-  LrPlan q = {64, 1};
-  auto chains = [&](int ch) { return (long long)B * ((D + ch - 1) / ch); };
-  if (nb > 1 && chains(32) <= slots) q.ch = 32;
-  while (q.cl < LR_MAXC && 2 * q.cl * (64 / q.ch) <= nb && chains(q.ch) * 2 * q.cl <= (q.cl == 8 ? slots * 3 / 4 : (q.cl > 1 ? slots * 6 / 7 : slots))) q.cl *= 2;
-  return q;
-}
-static int lr_launch(void (*kern)(const LrArgs), const LrArgs& p, int B, size_t smem, size_t most, DevOnce& once, cudaStream_t st) {
-  int rc = dev_ensure_smem(once, (const void*)kern, most);
-  if (rc != DET_OK) return rc;
-  if (p.cl > 8 && cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    cudaGetLastError();
-    return DET_ERR_CUDA;
-  }
+// How a call is dealt out: more CTAs of a cluster while all are on the GPU at once and each has a span; where even lone CTAs are too many, each goes
+// through several strips, about as many as the others.
+// A cluster needs its CTAs on one part of the GPU, and they do not pack: of 444 CTAs, three on an SM, 416 fit in clusters of 4, 384 of 8 and 336 of 16; so the
+// runtime is asked once per device and kernel what fits.  And the CTAs of a grid are not spread evenly: 256 of them ran in 42 us where three fit on an SM
+// and in 31 where two did (4 x 2048 x 2048 forward).  So no more are let on an SM than are needed, by the shared memory that is asked for.
+using LrKernel = void (*)(const LrArgs);
+constexpr int LR_MAXR = 3;                               // CTAs on an SM
+struct LrFits {
+  std::mutex lock;
+  bool known[MAX_DEVICES] = {};
+  int ctas[MAX_DEVICES][LR_MAXR][5] = {};                // at once on the GPU, by CTAs on an SM and log2 of the cluster
+};
+struct LrLaunch {
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = p.cl;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((long long)B * p.strips * p.cl));
-  cfg.blockDim = dim3(LR_T);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = p.cl > 1 ? 2 : 1;
+  LrLaunch(unsigned grid, int cl, size_t smem, cudaStream_t st) {
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cl;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(LR_T);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+  }
+};
+// shared memory of a CTA of which r fit on an SM and r + 1 do not (an SM has 228 KB; each CTA takes 1 KB more than it asks for)
+static size_t lr_smem(size_t need, int r) {
+  const size_t least = (size_t)228 * 1024 / (r + 1);
+  return need > least ? need : least;
+}
+static const int (*lr_fits(LrKernel kern, size_t need, LrFits& f))[5] {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return nullptr;
+  std::lock_guard<std::mutex> hold(f.lock);
+  if (!f.known[dev]) {
+    if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lr_smem(need, 1)) != cudaSuccess ||
+        cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    for (int r = 1; r <= LR_MAXR; ++r)
+      for (int i = 0; i < 5; ++i) {
+        LrLaunch l(1u << i, 1 << i, lr_smem(need, r), nullptr);
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, kern, &l.cfg) != cudaSuccess) {
+          cudaGetLastError();
+          clusters = 0;
+        }
+        f.ctas[dev][r - 1][i] = clusters << i;
+      }
+    if (f.ctas[dev][0][0] <= 0) return nullptr;
+    f.known[dev] = true;
+  }
+  return f.ctas[dev];
+}
+template <bool BACK, int WORDS, bool FLAGS>
+static int lr_run(LrArgs& p, int B, cudaStream_t st) {
+  static LrFits fits;
+  LrKernel kern;
+  if constexpr (BACK) kern = k_linrec_bwd<WORDS, FLAGS>;
+  else kern = k_linrec_fwd<WORDS, FLAGS>;
+  constexpr size_t need = sizeof(LrShared<BACK ? 3 : 2>);
+  const int(*ctas)[5] = lr_fits(kern, need, fits);
+  if (!ctas) return DET_ERR_CUDA;
+  const auto most = [&](int i) { return std::max(ctas[0][i], std::max(ctas[1][i], ctas[2][i])); };
+  p.strips = (p.D + LR_CH - 1) / LR_CH;
+  p.items = B * p.strips;
+  int i = 0, r = 0;
+  while (i < 4 && p.S > (LR_ROWS << i) && (long long)p.items << (i + 1) <= most(i + 1)) ++i;
+  const int passes = (p.items + most(0) - 1) / most(0);
+  p.cl = 1 << i;
+  p.step = i ? p.items : (p.items + passes - 1) / passes;
+  p.rounds = (p.S + (LR_ROWS << i) - 1) / (LR_ROWS << i);
+  while (r < LR_MAXR - 1 && p.step << i > ctas[r][i]) ++r;
+  LrLaunch l((unsigned)p.step << i, p.cl, lr_smem(need, r + 1), st);
   note_launch();
-  cudaLaunchKernelEx(&cfg, kern, p);
+  cudaLaunchKernelEx(&l.cfg, kern, p);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
-template <int CH, int WORDS, bool FLAGS>
-static int lr_run(bool bwd, const LrArgs& p, int B, cudaStream_t st) {
-  static DevOnce fwd_once, bwd_once;
-  using Sf = LrShared<CH, 2>;
-  using Sb = LrShared<CH, 3>;
-  return bwd ? lr_launch(k_linrec_bwd<CH, WORDS, FLAGS>, p, B, Sb::bytes(p.cl), Sb::bytes(LR_MAXC), bwd_once, st)
-             : lr_launch(k_linrec_fwd<CH, WORDS, FLAGS>, p, B, Sf::bytes(p.cl), Sf::bytes(LR_MAXC), fwd_once, st);
-}
-template <int CH>
-static int lr_pick(bool bwd, const LrArgs& p, int B, bool wide, cudaStream_t st) {
-  return wide ? (p.flags ? lr_run<CH, 4, true>(bwd, p, B, st) : lr_run<CH, 4, false>(bwd, p, B, st))
-              : (p.flags ? lr_run<CH, 1, true>(bwd, p, B, st) : lr_run<CH, 1, false>(bwd, p, B, st));
-}
-static int lr_any(bool bwd, LrArgs& p, int B, cudaStream_t st) {
-  p.nb = (p.S + LR_BLOCK - 1) / LR_BLOCK;
+static int lr_any(bool back, LrArgs& p, int B, cudaStream_t st) {
+  p.n = (p.S + LR_CHUNK - 1) / LR_CHUNK;
   if (p.S <= LR_CHUNK) {
     const size_t threads = (size_t)B * (p.D / 2);
-    launch_after(bwd ? k_linrec_chunk<true> : k_linrec_chunk<false>, dim3((unsigned)((threads + 127) / 128)), 128, 0, st, p, threads);
+    launch_after(back ? k_linrec_chunk<true> : k_linrec_chunk<false>, dim3((unsigned)((threads + 127) / 128)), 128, 0, st, p, threads);
     DET_CHECK_LAUNCH();
     return DET_OK;
   }
-  const LrPlan q = lr_plan(B, p.D, p.nb, bwd ? 2 : 4);
-  p.cl = q.cl;
-  p.strips = (p.D + q.ch - 1) / q.ch;
   // whole pieces of 16 bytes where the tensors allow it
-  const bool wide = p.D % 8 == 0 && p.ld % 8 == 0 && aligned16(p.g) && aligned16(p.v) && (!bwd || (p.ld_y % 8 == 0 && aligned16(p.dy)));
-  return q.ch == 64 ? lr_pick<64>(bwd, p, B, wide, st) : lr_pick<32>(bwd, p, B, wide, st);
+  const bool wide = p.D % 8 == 0 && p.ld % 8 == 0 && aligned16(p.g) && aligned16(p.v) && (!back || (p.ld_y % 8 == 0 && aligned16(p.dy)));
+  if (back) return wide ? (p.flags ? lr_run<true, 4, true>(p, B, st) : lr_run<true, 4, false>(p, B, st))
+                        : (p.flags ? lr_run<true, 1, true>(p, B, st) : lr_run<true, 1, false>(p, B, st));
+  return wide ? (p.flags ? lr_run<false, 4, true>(p, B, st) : lr_run<false, 4, false>(p, B, st))
+              : (p.flags ? lr_run<false, 1, true>(p, B, st) : lr_run<false, 1, false>(p, B, st));
 }
 static int lr_check(const void* a, const void* b, int ld, int B, int S, int D) {
   if (!a || !b || B < 0 || S < 0 || D <= 0 || ld < D) return DET_ERR_ARG;
   if (D % 2 || ld % 2 || S > (1 << 30)) return DET_ERR_SHAPE;
-  if ((long long)B * ((D + 31) / 32) > (1 << 26)) return DET_ERR_SHAPE;
+  if ((long long)B * ((D + LR_CH - 1) / LR_CH) > (1 << 26)) return DET_ERR_SHAPE;
   if (((uintptr_t)a | (uintptr_t)b) & 3u) return DET_ERR_ALIGN;
   return DET_OK;
 }
@@ -612,7 +708,7 @@ static int lr_empty(const float* in, float* out, size_t n, cudaStream_t st) {
 using namespace det;
 
 extern "C" size_t det_linrec_state_floats(int B, int S, int D) {
-  return B > 0 && S > 0 && D > 0 ? (size_t)B * (((size_t)S + LR_BLOCK - 1) / LR_BLOCK) * (size_t)D : 0;
+  return B > 0 && S > 0 && D > 0 ? (size_t)B * (((size_t)S + LR_CHUNK - 1) / LR_CHUNK) * (size_t)D : 0;
 }
 
 extern "C" int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, det_bf16* y, int ld_y, const uint8_t* flags,

@@ -96,4 +96,4 @@ def test_linrec_refusals():
         refused(SHAPE, "det_linrec_bwd", b(**bad))
     for bad in (dict(dy=A + 2), dict(dg=A + 2), dict(dv=A + 2), dict(dhT=A + 4), dict(dh0=A + 4), dict(st=A + 4)):
         refused(ALIGN, "det_linrec_bwd", b(**bad))
-    assert det.det_linrec_state_floats(2, 65, 10) == 40 and det.det_linrec_state_floats(2, 0, 10) == 0
+    assert det.det_linrec_state_floats(2, 65, 10) == 180 and det.det_linrec_state_floats(2, 0, 10) == 0

@@ -309,7 +309,7 @@ def _linrec(det, gv, dy, B, S, fl, h0, dhT, pad=0):
     opt = lambda a: dev(a) if a is not None else None
     y, hT, dh0 = dev(np.zeros((T, D + pad), np.uint16)), empty((B, D), F), empty((B, D), F)
     n = det.det_linrec_state_floats(B, S, D)
-    assert n == B * ((S + 63) // 64) * D
+    assert n == B * ((S + 7) // 8) * D
     states, out = empty((n,), F), dev(np.zeros((T, ld), np.uint16))
     p = dgv_in.data_ptr()
     dfl, dh, ddhT = opt(fl), opt(h0), opt(dhT)
@@ -340,10 +340,11 @@ def _linrec_check(det, B, S, D, every=0, ends=True, pad=0, gv=None, dy=None, fl=
 @pytest.mark.parametrize("B,S,D,every,ends,pad", [
     (1, 1, 2, 0, True, 0), (3, 1, 64, 0, False, 0), (2, 7, 66, 0, True, 4), (1, 8, 128, 3, True, 0), (1, 9, 30, 0, False, 2), (2, 63, 130, 5, True, 0),
     (1, 64, 64, 0, True, 0), (3, 65, 34, 0, True, 0), (1, 128, 256, 0, True, 0), (2, 129, 70, 1, True, 2), (1, 500, 100, 40, True, 0),
-    (2, 513, 64, 0, True, 0), (1, 1000, 200, 0, False, 0), (1, 4096, 64, 100, True, 0), (4, 333, 512, 0, True, 0), (1, 5000, 30, 0, True, 6),
+    (2, 513, 64, 0, True, 0), (1, 1000, 200, 0, False, 0), (1, 4096, 64, 100, True, 0), (4, 333, 512, 0, True, 0), (1, 5000, 30, 0, True, 6), (2, 1025, 4, 0, True, 0), (1, 1024, 2, 0, True, 0), (1, 33000, 6, 300, True, 0), (2, 31, 18, 0, True, 0),
+    (1, 96, 32, 0, True, 0), (3, 127, 16, 4, True, 0), (1, 2177, 512, 0, True, 0), (1, 700, 1500, 0, True, 0),
     (40, 300, 128, 0, True, 0), (130, 260, 64, 9, True, 0), (1, 20000, 16, 0, True, 0), (500, 70, 64, 0, False, 0)])
 def test_linrec(det, B, S, D, every, ends, pad):
-    """Lengths around chunks and blocks, every number of CTAs in a cluster, with and without the table of gates, cuts, strides."""
+    """Lengths around chunks, blocks and spans, every number of CTAs in a cluster, either number of warps along a sequence, cuts, strides."""
     _linrec_check(det, B, S, D, every, ends, pad)
 
 

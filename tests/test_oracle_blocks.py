@@ -123,7 +123,7 @@ def test_linrec_against_64_bits(B, S, D, every, ends):
     R.close(y, w["h"], w["err_h"], True, "y")
     R.close(hT, w["hT"], w["err_hT"], what="hT")
     for k in range(1, states.shape[1]):
-        R.close(states[:, k], w["h"].reshape(B, S, D)[:, 64 * k - 1], w["err_h"].reshape(B, S, D)[:, 64 * k - 1], what="states")
+        R.close(states[:, k], w["h"].reshape(B, S, D)[:, 8 * k - 1], w["err_h"].reshape(B, S, D)[:, 8 * k - 1], what="states")
     dgv, dh0 = oracle.linrec_bwd(dy, gv, states, B, S, fl, dhT)
     w = R.linrec_bwd(dy, gv, B, S, fl, h0, dhT)
     R.close(np.ascontiguousarray(dgv[:, D:]), w["dv"], w["err_dv"], True, "dv")
@@ -164,17 +164,19 @@ def test_linrec_gradient_by_differences():
             assert abs(d - got.flat[i]) <= R.UBF * abs(d) + 1e-7       # bf16 gradients; the difference is good to 1e-9
 
 
-def test_linrec_in_pieces_of_whole_blocks_is_the_same():
-    """A sequence in pieces of whole blocks, each starting from what the one before left: every bit, forward and backward."""
-    S, D = 192, 6
+def test_linrec_in_pieces_of_whole_spans_is_the_same():
+    """A sequence in pieces of whole spans (128 rows), each starting from what the one before left: every bit.  Backward the spans are counted from the
+    end of the call."""
+    S, D, cut = 256 + 130, 4, 128
     gv, dy = _gv(1, S, D, 31), synth.normal_bf16((S, D), 1.0, seed=32, tid=1)
     y, hT, st = oracle.linrec_fwd(gv, 1, S)
-    dgv, dh0 = oracle.linrec_bwd(dy, gv, st, 1, S)
-    y0, s, st0 = oracle.linrec_fwd(gv[:64], 1, 64)
-    y1, s, st1 = oracle.linrec_fwd(gv[64:], 1, 128, h0=s)
+    y0, s, st0 = oracle.linrec_fwd(gv[:cut], 1, cut)
+    y1, s, st1 = oracle.linrec_fwd(gv[cut:], 1, S - cut, h0=s)
     assert np.array_equal(y, np.concatenate([y0, y1])) and np.array_equal(hT, s) and np.array_equal(st, np.concatenate([st0, st1], 1))
-    d1, c = oracle.linrec_bwd(dy[64:], gv[64:], st1, 1, 128)
-    d0, c = oracle.linrec_bwd(dy[:64], gv[:64], st0, 1, 64, dhT=c)
+    S = 256
+    dgv, dh0 = oracle.linrec_bwd(dy[:S], gv[:S], st[:, :S // 8], 1, S)
+    d1, c = oracle.linrec_bwd(dy[cut:S], gv[cut:S], st[:, cut // 8:S // 8], 1, S - cut)
+    d0, c = oracle.linrec_bwd(dy[:cut], gv[:cut], st[:, :cut // 8], 1, cut, dhT=c)
     assert np.array_equal(dgv, np.concatenate([d0, d1])) and np.array_equal(dh0, c)
 
 
