@@ -11,11 +11,11 @@
 // walked row by row.  A map with A = 0 lets nothing in, not even a NaN.
 //
 // A warp has a block of 32 channels: sixteen lanes a chunk, two channels a lane, so that a row's piece is 64 bytes (of 32 bytes the L1 cache was 64 % busy
-// with finding lines); the maps of its two chunks meet in a shuffle.  The eight warps of a CTA have the blocks of a span, and every warp composes the
-// block maps again from shared memory, a group in each half: one barrier a round.  Where there are too few strips the CTAs of a cluster take adjacent
-// spans and send each other the span maps by stores that complete a transaction barrier of the receiver.  So every value is read once and written once
-// however long a sequence is and however few there are, with no workspace.  A warp's raw values of the next round come in by asynchronous copies as soon as
-// those of this round are in registers.
+// with finding lines); the maps of its two chunks meet in a shuffle.  Eight warps have the blocks of a span, and every warp composes the block maps again
+// from shared memory, a group in each half.
+// Where there are few strips the CTAs of a cluster take adjacent spans: they send each other the span maps, by stores that complete a transaction
+// barrier of the receiver, and one warp of each applies them in turn.  So every value is read once and written once however long a sequence is and however
+// few there are, with no workspace.  A warp's raw values of the next round come in by asynchronous copies as soon as those of this round are in registers.
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
@@ -121,12 +121,13 @@ __device__ __forceinline__ uint32_t lr_dg(float2 d, float2 diff, float2 f, float
 // NS: tensors that come in by asynchronous copies.  A chunk's raw values take 16 words more than they have, so that the two chunks of a warp read
 // different banks.
 constexpr int LR_RAW = LR_CHUNK * 16 + 16;
-template <int NS>
+template <int NS, bool JOINED>
 struct __align__(16) LrShared {
-  uint32_t raw[LR_WARPS][NS][LR_BLOCK][LR_RAW];          // of each warp: [tensor][chunk][row, lane of 16]
+  uint32_t raw[LR_WARPS][NS][LR_BLOCK][LR_RAW];  // of each warp: [tensor][chunk][row, lane of 16]
   float tab[LR_TAB];
   float4 block[2][LR_WARPS][16];                         // the block maps of this round; two rounds
-  float4 span[2][LR_MAXC][16];                           // the span maps of the cluster; two rounds
+  float4 span[2][JOINED ? LR_MAXC : 1][16];             // the span maps of the cluster; two rounds
+  float2 start[2][16];                                   // what comes into the CTA's span, and into the next round
   unsigned long long arrived[2];                         // transaction barriers of the span maps, two rounds
   int gone;                                              // a wait ran out
 };
@@ -162,10 +163,11 @@ struct LrArgs {
 };
 
 // Where a thread is: rank in its cluster, warp (of the span, in the order of the pass), chunk o of its block, lane of 16.
+template <bool JOINED>
 struct LrPlace {
   int rank, warp, o, lane;
   __device__ __forceinline__ LrPlace(const LrArgs& p) {
-    rank = blockIdx.x % p.cl;
+    rank = JOINED ? blockIdx.x % p.cl : 0;
     warp = threadIdx.x >> 5;
     o = (threadIdx.x >> 4) & 1;
     lane = threadIdx.x & 15;
@@ -173,20 +175,20 @@ struct LrPlace {
 };
 // What a CTA does in a round: the span `span` (in the order of the pass) of sequence b and the 32 channels from ch0 on.  Round k of an item (a sequence's
 // strip); only a lone CTA has more than one item.
-template <bool BACK>
+template <bool BACK, bool JOINED>
 struct LrRound {
   int item, k, b, ch0, span;
-  __device__ __forceinline__ LrRound(const LrArgs& p, const LrPlace& at) : item(blockIdx.x / p.cl), k(0) { begin(p, at); }
-  __device__ __forceinline__ void begin(const LrArgs& p, const LrPlace& at) {
+  __device__ __forceinline__ LrRound(const LrArgs& p, const LrPlace<JOINED>& at) : item(JOINED ? blockIdx.x / p.cl : blockIdx.x), k(0) { begin(p, at); }
+  __device__ __forceinline__ void begin(const LrArgs& p, const LrPlace<JOINED>& at) {
     b = item / p.strips;
     ch0 = (item - b * p.strips) * LR_CH;
     span = at.rank;
   }
   __device__ __forceinline__ bool more(const LrArgs& p) const { return item < p.items; }
   __device__ __forceinline__ bool last(const LrArgs& p) const { return k + 1 == p.rounds; }
-  __device__ __forceinline__ void next(const LrArgs& p, const LrPlace& at) {
+  __device__ __forceinline__ void next(const LrArgs& p, const LrPlace<JOINED>& at) {
     ++k;
-    span += p.cl;
+    span += JOINED ? p.cl : 1;
     if (k < p.rounds) return;
     k = 0;
     item += p.step;
@@ -201,7 +203,7 @@ struct LrRound {
   __device__ __forceinline__ bool full(const LrArgs& p) const {
     return ch0 + LR_CH <= p.D && (span + 1) * LR_ROWS <= (BACK ? p.n * LR_CHUNK : p.S) && (!BACK || span > 0 || p.S % LR_CHUNK == 0);
   }
-  __device__ __forceinline__ size_t state(const LrArgs& p, const LrPlace& at) const { return (size_t)b * p.D + ch0 + 2 * at.lane; }
+  __device__ __forceinline__ size_t state(const LrArgs& p, const LrPlace<JOINED>& at) const { return (size_t)b * p.D + ch0 + 2 * at.lane; }
 };
 
 // A thread's place in a tensor of the rows, in pieces of WORDS words: where it reads or writes for the first chunk of its warp's block (WORDS 0: of its own
@@ -210,8 +212,8 @@ template <int WORDS>
 struct LrCursor {
   static constexpr int PER = WORDS ? 16 / WORDS : 16, ROWS = 32 / PER;                // pieces of a row, rows of an instruction
   const uint16_t* at;
-  template <bool BACK>
-  __device__ __forceinline__ void begin(const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace& w, const LrRound<BACK>& r) {
+  template <bool BACK, bool JOINED>
+  __device__ __forceinline__ void begin(const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace<JOINED>& w, const LrRound<BACK, JOINED>& r) {
     const int l = threadIdx.x & 31, row = WORDS ? l / PER : 0;
     at = x + ((long long)r.b * p.S + r.row(p, w.warp, WORDS ? 0 : w.o) + row) * (long long)ld + r.ch0 + (WORDS ? 2 * (l % PER * WORDS) : 2 * w.lane);
   }
@@ -222,9 +224,9 @@ struct LrCursor {
   }
 };
 // The rows of a warp's block of one tensor on their way.  The address is only followed where the row exists.
-template <bool BACK, int WORDS, bool FULL>
-__device__ __forceinline__ void lr_fetch(uint32_t (*raw)[LR_RAW], const LrCursor<WORDS>& c, const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace& at,
-                                         const LrRound<BACK>& r) {
+template <bool FULL, int WORDS, bool BACK, bool JOINED>
+__device__ __forceinline__ void lr_fetch(uint32_t (*raw)[LR_RAW], const LrCursor<WORDS>& c, const uint16_t* x, size_t ld, const LrArgs& p, const LrPlace<JOINED>& at,
+                                         const LrRound<BACK, JOINED>& r) {
   constexpr int PER = LrCursor<WORDS>::PER, ROWS = LrCursor<WORDS>::ROWS;
   const int l = threadIdx.x & 31, word = l % PER * WORDS, row = l / PER;
   const bool have = FULL || r.ch0 + 2 * word < p.D;
@@ -243,11 +245,12 @@ template <bool FLAGS>
 __device__ __forceinline__ bool lr_flag(const LrArgs& p, int b, int lane, int t, int n) {
   return FLAGS && lane < min(n, LR_CHUNK) && p.flags[(size_t)b * p.S + t + lane] != 0;
 }
-// the cuts of this thread's chunk, from the flags of the warp
-template <bool FLAGS>
-__device__ __forceinline__ uint32_t lr_cuts(bool flag) {
-  if (!FLAGS) return 0;
-  return (__ballot_sync(0xffffffffu, flag) >> (threadIdx.x & 16)) & 0xffu;
+// work(std::true_type) with cuts of a warp's rows, work(std::false_type) without: rows without a cut need no selection, and cuts are few (65536 rows of 512
+// channels with a cut every 700: 121 -> 110 us forward, 164 -> 159 backward)
+template <bool FLAGS, typename W>
+__device__ __forceinline__ void lr_with_cuts(uint32_t cuts, W&& work) {
+  if (FLAGS && cuts) work(std::true_type{});
+  else work(std::false_type{});
 }
 // The gates of a chunk.  A NaN comes out of the table as an infinity's gate and is put right here.  Whether there is one (or an infinity) shows the sum
 // of all words times zero.
@@ -274,18 +277,19 @@ __device__ __forceinline__ LrMap lr_from(const LrMap& m, int lane) {
 }
 // The hand-over of a round: the map of this thread's chunk in, what comes into the chunk out; `s`, what comes into the round, becomes what comes into
 // the next one.  `turn` counts the rounds of the CTA.
-// The maps of two rounds have places of their own: a warp writes its block's map of round r + 2 behind the barrier of round r + 1, which all warps pass
-// when they have read round r's; a CTA sends its span's map of round r + 2 when it has all of round r + 1, those of the receiver among them, which that
-// one sent behind the same barrier.
-template <bool FULL, bool BACK, int NS>
-__device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p, const LrPlace& at, const LrRound<BACK>& r, int turn, const LrMap& mine, float2& s,
-                                               float2 one) {
+// The maps of two rounds have places of their own: a warp writes its block's map of round r + 2 behind a barrier of round r + 1, which all warps pass
+// when they have read round r's; a CTA sends its span's map of round r + 2 when it has all of round r + 1, that of the receiver among them, which was
+// sent behind the barrier that the receiver's reader of round r has passed too.
+template <bool FULL, bool BACK, int NS, bool JOINED>
+__device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const LrArgs& p, const LrPlace<JOINED>& at, const LrRound<BACK, JOINED>& r, int turn,
+                                               const LrMap& mine, float2& s, float2 one) {
   const int chunks = p.n - r.span * LR_WARPS * LR_BLOCK, blocks = (chunks + 1) / LR_BLOCK;               // from the CTA's first ones on
   const LrMap other = lr_from(mine, threadIdx.x ^ 16), both = lr_compose(other, mine, one);              // `both`: in the lanes of chunk 1
   const bool two = FULL || chunks > at.warp * LR_BLOCK + 1;
   float4(*const maps)[16] = sh.block[turn & 1];
+  uint64_t* bar = reinterpret_cast<uint64_t*>(&sh.arrived[turn & 1]);
   if (at.o == (two ? 1 : 0)) maps[at.warp][at.lane] = lr_pack(two ? both : mine);
-  if (p.cl > 1 && threadIdx.x == 0) mbar_expect_tx(reinterpret_cast<uint64_t*>(&sh.arrived[turn & 1]), p.cl * 16 * sizeof(float4));
+  if (JOINED && threadIdx.x == 0) mbar_expect_tx(bar, p.cl * 16 * sizeof(float4));
   __syncthreads();
   // a group in each half of the warp
   LrMap group = lr_unpack(maps[at.o * LR_GROUP][at.lane]), before = group;
@@ -301,26 +305,34 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p
   LrMap span = g0;
   if (FULL || blocks > LR_GROUP) span = lr_compose(g0, g1, one);
   float2 start = s;
-  if (p.cl == 1) {
+  if (!JOINED) {
     s = lr_apply(span, s, one);
   } else {
-    constexpr int BATCH = 4;
-    uint64_t* bar = reinterpret_cast<uint64_t*>(&sh.arrived[turn & 1]);
     float4(*const place)[16] = sh.span[turn & 1];
     const int to = at.warp + LR_WARPS * at.o;
     if (to < p.cl) store_in_cluster(&place[at.rank][at.lane], bar, to, lr_pack(span));
-    mbar_wait_warp(bar, (turn >> 1) & 1, &sh.gone, p.status);
-    const int spans = min(p.cl, (p.n + LR_WARPS * LR_BLOCK - 1) / (LR_WARPS * LR_BLOCK) - (r.span - at.rank));
-    for (int r0 = 0; r0 < spans; r0 += BATCH) {
-      float4 m[BATCH];
+    if (at.warp == turn % LR_WARPS) {
+      constexpr int BATCH = 4;
+      mbar_wait_warp(bar, (turn >> 1) & 1, &sh.gone, p.status);
+      const int spans = min(p.cl, (p.n + LR_WARPS * LR_BLOCK - 1) / (LR_WARPS * LR_BLOCK) - (r.span - at.rank));
+      for (int r0 = 0; r0 < spans; r0 += BATCH) {
+        float4 m[BATCH];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) m[i] = place[min(r0 + i, spans - 1)][at.lane];
+        for (int i = 0; i < BATCH; ++i) m[i] = place[min(r0 + i, spans - 1)][at.lane];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        if (r0 + i == at.rank) start = s;
-        if (r0 + i < spans) s = lr_apply(lr_unpack(m[i]), s, one);
+        for (int i = 0; i < BATCH; ++i) {
+          if (r0 + i == at.rank) start = s;
+          if (r0 + i < spans) s = lr_apply(lr_unpack(m[i]), s, one);
+        }
+      }
+      if (at.o == 0) {
+        sh.start[0][at.lane] = start;
+        sh.start[1][at.lane] = s;
       }
     }
+    __syncthreads();
+    start = sh.start[0][at.lane];
+    s = sh.start[1][at.lane];
   }
   if (half) start = lr_apply(g0, start, one);
   if (at.warp & 3) start = lr_apply(before, start, one);
@@ -328,54 +340,60 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS>& sh, const LrArgs& p
   return at.o ? second : start;
 }
 // before the first round: the barriers, known to the cluster before anyone sends, and the table on its way
-template <int NS>
-__device__ __forceinline__ void lr_open(LrShared<NS>& sh, const LrArgs& p) {
-  if (threadIdx.x == 0) {
-    sh.gone = 0;
-    mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[0]), 1);
-    mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[1]), 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+template <int NS, bool JOINED>
+__device__ __forceinline__ void lr_open(LrShared<NS, JOINED>& sh, const LrArgs& p) {
+  if (JOINED) {
+    if (threadIdx.x == 0) {
+      sh.gone = 0;
+      mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[0]), 1);
+      mbar_init(reinterpret_cast<uint64_t*>(&sh.arrived[1]), 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cluster_arrive();
   }
-  __syncthreads();
-  if (p.cl > 1) cluster_arrive();
   const uint32_t dst = smem_u32(sh.tab);
   for (int i = threadIdx.x; i < LR_TAB / 4; i += LR_T) copy_async<4>(dst + 16 * i, lr_table_image.m + 4 * i, true);
 }
 // no CTA leaves while another one may still send to it (after a wait that ran out)
-__device__ __forceinline__ void lr_close(const LrArgs& p) {
-  if (p.cl == 1) return;
+__device__ __forceinline__ void lr_close() {
   cluster_arrive();
   cluster_wait();
 }
-template <int WORDS, bool FLAGS>
-__global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
+
+// Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 30 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
+// 110 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 25 and 37 of 8 and 14; 1 x 65536 x 512 with cuts 110 and 159 of 31 and 51.  The first
+// three are bound by instructions (some 500 a round of 8 rows a warp forward, 130 of them the hand-over), the last by the steps that a round of a
+// cluster has to wait for one after the other.
+template <int WORDS, bool FLAGS, bool JOINED>
+__global__ void __launch_bounds__(LR_T, JOINED ? 2 : 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<2>& sh = *reinterpret_cast<LrShared<2>*>(smem);
-  const LrPlace at(p);
+  LrShared<2, JOINED>& sh = *reinterpret_cast<LrShared<2, JOINED>*>(smem);
+  const LrPlace<JOINED> at(p);
   const float2 one = same2(c_one);
   lr_open(sh, p);
   grid_dep();
   uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
-  LrRound<false> r(p, at), ahead = r;
+  LrRound<false, JOINED> r(p, at), ahead = r;
   bool flag = false;
   float2 s = make_float2(0.0f, 0.0f), first = s;
   LrCursor<WORDS> cg, cv;
   LrCursor<0> cy;
   auto fetch = [&] {
-    const LrRound<false>& r = ahead;                       // of the round that is fetched
+    const LrRound<false, JOINED>& r = ahead;                       // of the round that is fetched
     if (r.k == 0) {
-      cg.template begin<false>(p.g, p.ld, p, at, r);
-      cv.template begin<false>(p.v, p.ld, p, at, r);
+      cg.begin(p.g, p.ld, p, at, r);
+      cv.begin(p.v, p.ld, p, at, r);
     } else {
       cg.template next<false>(p.ld, p);
       cv.template next<false>(p.ld, p);
     }
     if (r.full(p)) {
-      lr_fetch<false, WORDS, true>(raw[0], cg, p.g, p.ld, p, at, r);
-      lr_fetch<false, WORDS, true>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<true>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<true>(raw[1], cv, p.v, p.ld, p, at, r);
     } else {
-      lr_fetch<false, WORDS, false>(raw[0], cg, p.g, p.ld, p, at, r);
-      lr_fetch<false, WORDS, false>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<false>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<false>(raw[1], cv, p.v, p.ld, p, at, r);
     }
     const int t = r.row(p, at.warp, at.o);
     flag = lr_flag<FLAGS>(p, r.b, at.lane, t, p.S - t);
@@ -385,40 +403,44 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
   fetch();
   copies_done();
   __syncthreads();                                       // the table
-  if (p.cl > 1) cluster_wait();
+  if (JOINED) cluster_wait();
   int turn = 0;
   for (; r.more(p); r.next(p, at), ++turn) {
     const int t0 = r.row(p, at.warp, at.o);
     if (r.k == 0) {
       s = first;
-      cy.template begin<false>(p.y, p.ld_y, p, at, r);
+      cy.begin(p.y, p.ld_y, p, at, r);
     }
     auto round = [&](auto whole) {
       constexpr bool FULL = decltype(whole)::value;
       const int n = FULL ? LR_CHUNK : p.S - t0;          // n rows of the chunk exist
       const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
-      const uint32_t cuts = lr_cuts<FLAGS>(flag);
+      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
       const uint32_t* q = raw[0][at.o] + at.lane;
       float2 f[LR_CHUNK], u[LR_CHUNK];
       lr_gates(q, sh.tab, f, u);
       LrMap mine;
+      lr_with_cuts<FLAGS>(all, [&](auto some) {
 #pragma unroll
-      for (int i = 0; i < LR_CHUNK; ++i) {
-        const uint32_t w = q[LR_BLOCK * LR_RAW + i * 16];
-        u[i] = mul2(u[i], make_float2(bflo(w), bfhi(w)));
-        if (i == 0 || i < n) lr_extend(mine, i == 0, f[i], u[i], (cuts >> i) & 1, one);
-      }
+        for (int i = 0; i < LR_CHUNK; ++i) {
+          const uint32_t w = q[LR_BLOCK * LR_RAW + i * 16];
+          u[i] = mul2(u[i], make_float2(bflo(w), bfhi(w)));
+          if (i == 0 || i < n) lr_extend(mine, i == 0, f[i], u[i], decltype(some)::value && ((cuts >> i) & 1), one);
+        }
+      });
       __syncwarp();
       if (ahead.more(p)) fetch();
       float2 h = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
       if (p.save && n > 0 && have) *reinterpret_cast<float2*>(p.save + r.state(p, at) + ((size_t)r.b * (p.n - 1) + t0 / LR_CHUNK) * p.D) = h;
       uint16_t* out = const_cast<uint16_t*>(cy.at);
+      lr_with_cuts<FLAGS>(all, [&](auto some) {
 #pragma unroll
-      for (int i = 0; i < LR_CHUNK; ++i) {
-        h = lr_step(f[i], u[i], h, (cuts >> i) & 1, one);
-        if (i < n && have) *reinterpret_cast<uint32_t*>(out) = bf_pair(h.x, h.y);
-        out += p.ld_y;
-      }
+        for (int i = 0; i < LR_CHUNK; ++i) {
+          h = lr_step(f[i], u[i], h, decltype(some)::value && ((cuts >> i) & 1), one);
+          if (i < n && have) *reinterpret_cast<uint32_t*>(out) = bf_pair(h.x, h.y);
+          out += p.ld_y;
+        }
+      });
     };
     if (r.full(p)) round(std::true_type{});
     else round(std::false_type{});
@@ -426,44 +448,44 @@ __global__ void __launch_bounds__(LR_T, 3) k_linrec_fwd(const __grid_constant__ 
     if (p.last && r.last(p) && threadIdx.x < 16 && at.rank == 0 && r.ch0 + 2 * at.lane < p.D) *reinterpret_cast<float2*>(p.last + r.state(p, at)) = s;
     copies_done();
     __syncwarp();
-    if (p.cl > 1 && __any_sync(0xffffffffu, *static_cast<volatile int*>(&sh.gone))) break;
+    if (JOINED && *static_cast<volatile int*>(&sh.gone)) break;                    // set before the round's second barrier: all see the same
   }
-  lr_close(p);
+  if (JOINED) lr_close();
 }
 
-template <int WORDS, bool FLAGS>
+template <int WORDS, bool FLAGS, bool JOINED>
 __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
-  LrShared<3>& sh = *reinterpret_cast<LrShared<3>*>(smem);
-  const LrPlace at(p);
+  LrShared<3, JOINED>& sh = *reinterpret_cast<LrShared<3, JOINED>*>(smem);
+  const LrPlace<JOINED> at(p);
   const float2 one = same2(c_one);
   lr_open(sh, p);
   grid_dep();
   uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
-  LrRound<true> r(p, at), ahead = r;
+  LrRound<true, JOINED> r(p, at), ahead = r;
   bool flag = false;
   float2 s = make_float2(0.0f, 0.0f), first = s, next = s;                            // next: the state in front of the thread's chunk
   LrCursor<WORDS> cg, cv, cdy;
   LrCursor<0> odv, odg;
   auto fetch = [&] {
-    const LrRound<true>& r = ahead;                       // of the round that is fetched
+    const LrRound<true, JOINED>& r = ahead;                       // of the round that is fetched
     if (r.k == 0) {
-      cg.template begin<true>(p.g, p.ld, p, at, r);
-      cv.template begin<true>(p.v, p.ld, p, at, r);
-      cdy.template begin<true>(p.dy, p.ld_y, p, at, r);
+      cg.begin(p.g, p.ld, p, at, r);
+      cv.begin(p.v, p.ld, p, at, r);
+      cdy.begin(p.dy, p.ld_y, p, at, r);
     } else {
       cg.template next<true>(p.ld, p);
       cv.template next<true>(p.ld, p);
       cdy.template next<true>(p.ld_y, p);
     }
     if (r.full(p)) {
-      lr_fetch<true, WORDS, true>(raw[0], cg, p.g, p.ld, p, at, r);
-      lr_fetch<true, WORDS, true>(raw[1], cv, p.v, p.ld, p, at, r);
-      lr_fetch<true, WORDS, true>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
+      lr_fetch<true>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<true>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<true>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
     } else {
-      lr_fetch<true, WORDS, false>(raw[0], cg, p.g, p.ld, p, at, r);
-      lr_fetch<true, WORDS, false>(raw[1], cv, p.v, p.ld, p, at, r);
-      lr_fetch<true, WORDS, false>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
+      lr_fetch<false>(raw[0], cg, p.g, p.ld, p, at, r);
+      lr_fetch<false>(raw[1], cv, p.v, p.ld, p, at, r);
+      lr_fetch<false>(raw[2], cdy, p.dy, p.ld_y, p, at, r);
     }
     const int t = r.row(p, at.warp, at.o);
     const bool have = r.ch0 + 2 * at.lane < p.D;
@@ -475,20 +497,20 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
   fetch();
   copies_done();
   __syncthreads();                                       // the table
-  if (p.cl > 1) cluster_wait();
+  if (JOINED) cluster_wait();
   int turn = 0;
   for (; r.more(p); r.next(p, at), ++turn) {
     const int t0 = r.row(p, at.warp, at.o);
     if (r.k == 0) {
       s = first;
-      odv.template begin<true>(p.dv, p.ld_d, p, at, r);
-      odg.template begin<true>(p.dg, p.ld_d, p, at, r);
+      odv.begin(p.dv, p.ld_d, p, at, r);
+      odg.begin(p.dg, p.ld_d, p, at, r);
     }
     auto round = [&](auto whole) {
       constexpr bool FULL = decltype(whole)::value;
       const int n = FULL ? LR_CHUNK : t0 < 0 ? 0 : p.S - t0;                          // n rows of the chunk exist
       const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
-      const uint32_t cuts = lr_cuts<FLAGS>(flag);
+      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
       float2 h = next;
       const uint32_t* q = raw[0][at.o] + at.lane;
       float2 f[LR_CHUNK], z[LR_CHUNK];
@@ -503,29 +525,33 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
       if (ahead.more(p)) fetch();
       LrMap mine;
       mine.a = mine.h = same2(0.0f);
+      lr_with_cuts<FLAGS>(all, [&](auto some) {
 #pragma unroll
-      for (int i = LR_CHUNK - 1; i >= 0; --i)
-        if (i < n) lr_extend_back(mine, i == (FULL ? LR_CHUNK : min(n, LR_CHUNK)) - 1, f[i], make_float2(bflo(wd[i]), bfhi(wd[i])), (cuts >> i) & 1, one);
+        for (int i = LR_CHUNK - 1; i >= 0; --i)
+          if (i < n) lr_extend_back(mine, i == (FULL ? LR_CHUNK : min(n, LR_CHUNK)) - 1, f[i], make_float2(bflo(wd[i]), bfhi(wd[i])), decltype(some)::value && ((cuts >> i) & 1), one);
+      });
       float2 c = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
-      float2 diff[LR_CHUNK];                             // h_{t-1} - v
-#pragma unroll
-      for (int i = 0; i < LR_CHUNK; ++i) {
-        const bool cut = (cuts >> i) & 1;
-        const float2 v = make_float2(bflo(wv[i]), bfhi(wv[i]));
-        diff[i] = lr_sub(cut ? same2(0.0f) : h, v);
-        h = lr_step(f[i], mul2(z[i], v), h, cut, one);
-      }
       uint16_t *dv = const_cast<uint16_t*>(odv.at) + (LR_CHUNK - 1) * p.ld_d, *dg = const_cast<uint16_t*>(odg.at) + (LR_CHUNK - 1) * p.ld_d;
+      lr_with_cuts<FLAGS>(all, [&](auto some) {
+        float2 diff[LR_CHUNK];                             // h_{t-1} - v
 #pragma unroll
-      for (int i = LR_CHUNK - 1; i >= 0; --i, dv -= p.ld_d, dg -= p.ld_d) {
-        if (i >= n) continue;
-        const float2 d = add2(c, make_float2(bflo(wd[i]), bfhi(wd[i])), one), w = mul2(d, z[i]);
-        c = mul2(f[i], d);
-        if ((cuts >> i) & 1) c = same2(0.0f);
-        if (!have) continue;
-        *reinterpret_cast<uint32_t*>(dv) = bf_pair(w.x, w.y);
-        *reinterpret_cast<uint32_t*>(dg) = lr_dg(d, diff[i], f[i], z[i]);
-      }
+        for (int i = 0; i < LR_CHUNK; ++i) {
+          const bool cut = decltype(some)::value && ((cuts >> i) & 1);
+          const float2 v = make_float2(bflo(wv[i]), bfhi(wv[i]));
+          diff[i] = lr_sub(cut ? same2(0.0f) : h, v);
+          h = lr_step(f[i], mul2(z[i], v), h, cut, one);
+        }
+#pragma unroll
+        for (int i = LR_CHUNK - 1; i >= 0; --i, dv -= p.ld_d, dg -= p.ld_d) {
+          if (i >= n) continue;
+          const float2 d = add2(c, make_float2(bflo(wd[i]), bfhi(wd[i])), one), w = mul2(d, z[i]);
+          c = mul2(f[i], d);
+          if (decltype(some)::value && ((cuts >> i) & 1)) c = same2(0.0f);
+          if (!have) continue;
+          *reinterpret_cast<uint32_t*>(dv) = bf_pair(w.x, w.y);
+          *reinterpret_cast<uint32_t*>(dg) = lr_dg(d, diff[i], f[i], z[i]);
+        }
+      });
     };
     if (r.full(p)) round(std::true_type{});
     else round(std::false_type{});
@@ -534,9 +560,9 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
     if (p.last && r.last(p) && threadIdx.x < 16 && at.rank == 0 && r.ch0 + 2 * at.lane < p.D) *reinterpret_cast<float2*>(p.last + r.state(p, at)) = s;
     copies_done();
     __syncwarp();
-    if (p.cl > 1 && __any_sync(0xffffffffu, *static_cast<volatile int*>(&sh.gone))) break;
+    if (JOINED && *static_cast<volatile int*>(&sh.gone)) break;                    // set before the round's second barrier: all see the same
   }
-  lr_close(p);
+  if (JOINED) lr_close();
 }
 
 // Sequences of one chunk (a token at a time among them): a thread walks two channels alone, with nothing to hand over.
@@ -590,17 +616,20 @@ __global__ void __launch_bounds__(128) k_linrec_chunk(const __grid_constant__ Lr
   if (p.last) *reinterpret_cast<float2*>(p.last + at) = lr_apply(m, s, one);
 }
 
-// How a call is dealt out: more CTAs of a cluster while all are on the GPU at once and each has a span; where even lone CTAs are too many, each goes
-// through several strips, about as many as the others.
-// A cluster needs its CTAs on one part of the GPU, and they do not pack: of 444 CTAs, three on an SM, 416 fit in clusters of 4, 384 of 8 and 336 of 16; so the
-// runtime is asked once per device and kernel what fits.  And the CTAs of a grid are not spread evenly: 256 of them ran in 42 us where three fit on an SM
-// and in 31 where two did (4 x 2048 x 2048 forward).  So no more are let on an SM than are needed, by the shared memory that is asked for.
+// How a call is dealt out.  More CTAs of a cluster, of any number, while two on an SM have room for all of them.  A cluster needs its CTAs on one part of the
+// GPU, and they do not pack: of 296 CTAs, two on an SM, 264 fit in clusters of 4, 240 of 8 and 224 of 16, and a pass that needed 256 where 224 fit took
+// twice as long; so the runtime is asked once per device and kernel what fits.
+// Where there are strips enough, lone CTAs go through several, about as many as the others.  The CTAs of a grid are not spread evenly: 256 of them ran in
+// 42 us where three fit on an SM and in 31 where two did (4 x 2048 x 2048 forward).  So no more are let on an SM than are needed, by the shared memory that
+// is asked for.
 using LrKernel = void (*)(const LrArgs);
-constexpr int LR_MAXR = 3;                               // CTAs on an SM
+constexpr int LR_MAXR = 3;                               // lone CTAs on an SM
 struct LrFits {
   std::mutex lock;
   bool known[MAX_DEVICES] = {};
-  int ctas[MAX_DEVICES][LR_MAXR][5] = {};                // at once on the GPU, by CTAs on an SM and log2 of the cluster
+  struct {
+    int lone[LR_MAXR], joined[LR_MAXC - 1];              // CTAs at once on the GPU: lone, 1 .. on an SM; in clusters of 2 ..
+  } dev[MAX_DEVICES] = {};
 };
 struct LrLaunch {
   cudaLaunchAttribute attr[2];
@@ -624,53 +653,67 @@ static size_t lr_smem(size_t need, int r) {
   const size_t least = (size_t)228 * 1024 / (r + 1);
   return need > least ? need : least;
 }
-static const int (*lr_fits(LrKernel kern, size_t need, LrFits& f))[5] {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return nullptr;
-  std::lock_guard<std::mutex> hold(f.lock);
-  if (!f.known[dev]) {
-    if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lr_smem(need, 1)) != cudaSuccess ||
-        cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-      cudaGetLastError();
-      return nullptr;
-    }
-    for (int r = 1; r <= LR_MAXR; ++r)
-      for (int i = 0; i < 5; ++i) {
-        LrLaunch l(1u << i, 1 << i, lr_smem(need, r), nullptr);
-        int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, kern, &l.cfg) != cudaSuccess) {
-          cudaGetLastError();
-          clusters = 0;
-        }
-        f.ctas[dev][r - 1][i] = clusters << i;
-      }
-    if (f.ctas[dev][0][0] <= 0) return nullptr;
-    f.known[dev] = true;
-  }
-  return f.ctas[dev];
+struct LrVariant {
+  LrKernel kern;
+  size_t smem;
+};
+// the CTAs that run at once, 0 if they do not run at all
+static int lr_at_once(const LrVariant& v, size_t smem, int cl) {
+  LrLaunch l((unsigned)cl, cl, smem, nullptr);
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, v.kern, &l.cfg) == cudaSuccess) return clusters * cl;
+  cudaGetLastError();
+  return 0;
 }
 template <bool BACK, int WORDS, bool FLAGS>
 static int lr_run(LrArgs& p, int B, cudaStream_t st) {
   static LrFits fits;
-  LrKernel kern;
-  if constexpr (BACK) kern = k_linrec_bwd<WORDS, FLAGS>;
-  else kern = k_linrec_fwd<WORDS, FLAGS>;
-  constexpr size_t need = sizeof(LrShared<BACK ? 3 : 2>);
-  const int(*ctas)[5] = lr_fits(kern, need, fits);
-  if (!ctas) return DET_ERR_CUDA;
-  const auto most = [&](int i) { return std::max(ctas[0][i], std::max(ctas[1][i], ctas[2][i])); };
+  constexpr int NS = BACK ? 3 : 2;
+  LrVariant lone{nullptr, sizeof(LrShared<NS, false>)}, joined{nullptr, sizeof(LrShared<NS, true>)};
+  if constexpr (BACK) lone.kern = k_linrec_bwd<WORDS, FLAGS, false>, joined.kern = k_linrec_bwd<WORDS, FLAGS, true>;
+  else lone.kern = k_linrec_fwd<WORDS, FLAGS, false>, joined.kern = k_linrec_fwd<WORDS, FLAGS, true>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return DET_ERR_CUDA;
+  auto& fit = fits.dev[dev];
+  {
+    std::lock_guard<std::mutex> hold(fits.lock);
+    if (!fits.known[dev]) {
+      const auto allow = [](const LrVariant& v, size_t smem) {
+        return cudaFuncSetAttribute((const void*)v.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess;
+      };
+      if (!allow(lone, lr_smem(lone.smem, 1)) || !allow(joined, lr_smem(joined.smem, 2)) ||
+          cudaFuncSetAttribute((const void*)joined.kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+        cudaGetLastError();
+        return DET_ERR_CUDA;
+      }
+      for (int r = 1; r <= LR_MAXR; ++r) fit.lone[r - 1] = lr_at_once(lone, lr_smem(lone.smem, r), 1);
+      for (int cl = 2; cl <= LR_MAXC; ++cl) fit.joined[cl - 2] = lr_at_once(joined, lr_smem(joined.smem, 2), cl);
+      fits.known[dev] = true;
+    }
+  }
   p.strips = (p.D + LR_CH - 1) / LR_CH;
   p.items = B * p.strips;
-  int i = 0, r = 0;
-  while (i < 4 && p.S > (LR_ROWS << i) && (long long)p.items << (i + 1) <= most(i + 1)) ++i;
-  const int passes = (p.items + most(0) - 1) / most(0);
-  p.cl = 1 << i;
-  p.step = i ? p.items : (p.items + passes - 1) / passes;
-  p.rounds = (p.S + (LR_ROWS << i) - 1) / (LR_ROWS << i);
-  while (r < LR_MAXR - 1 && p.step << i > ctas[r][i]) ++r;
-  LrLaunch l((unsigned)p.step << i, p.cl, lr_smem(need, r + 1), st);
+  const int spans = (p.S + LR_ROWS - 1) / LR_ROWS;
+  p.cl = 1;
+  for (int cl = 2; cl <= LR_MAXC && cl <= spans; ++cl)
+    if ((long long)p.items * cl <= fit.joined[cl - 2]) p.cl = cl;
+  p.rounds = (spans + p.cl - 1) / p.cl;
+  p.cl = (spans + p.rounds - 1) / p.rounds;              // as many as have work in every round
+  p.step = p.items;
   note_launch();
-  cudaLaunchKernelEx(&l.cfg, kern, p);
+  if (p.cl > 1) {
+    LrLaunch l((unsigned)(p.items * p.cl), p.cl, lr_smem(joined.smem, 2), st);
+    cudaLaunchKernelEx(&l.cfg, joined.kern, p);
+  } else {
+    const int most = *std::max_element(fit.lone, fit.lone + LR_MAXR);
+    if (most <= 0) return DET_ERR_CUDA;
+    const int passes = (p.items + most - 1) / most;
+    p.step = (p.items + passes - 1) / passes;
+    int r = 0;
+    while (r < LR_MAXR - 1 && p.step > fit.lone[r]) ++r;
+    LrLaunch l((unsigned)p.step, 1, lr_smem(lone.smem, r + 1), st);
+    cudaLaunchKernelEx(&l.cfg, lone.kern, p);
+  }
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
