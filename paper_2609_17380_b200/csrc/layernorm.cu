@@ -7,6 +7,8 @@
 // of the backward one.
 #include <type_traits>
 
+#include <algorithm>
+
 #include "common.cuh"
 #include "internal.h"
 #include "rows.cuh"
@@ -43,6 +45,25 @@ __device__ __forceinline__ float node_tree(float (&v)[N], int have) {
     for (int w = 1; w < N; w <<= 1)
 #pragma unroll
       for (int j = 0; j < N; j += 2 * w) v[j] = j + w < have ? fadd(v[j], v[j + w]) : v[j];
+  }
+  return v[0];
+}
+// Two neighbours of a lane's columns in packed arithmetic, no product fused with a sum (8192 x 2048 backward with the residual stream 37.7 -> 36.3 us, 15.9 -> 13.5 million instructions).
+__device__ __forceinline__ float2 two(const float* v) { return make_float2(v[0], v[1]); }
+__device__ __forceinline__ void two(float* v, float2 x) { v[0] = x.x; v[1] = x.y; }
+template <int N>
+__device__ __forceinline__ float2 node_tree2(float2 (&v)[N], int have, float2 one) {
+  if (have >= N) {
+#pragma unroll
+    for (int w = 1; w < N; w <<= 1)
+#pragma unroll
+      for (int j = 0; j < N; j += 2 * w) v[j] = add2(v[j], v[j + w], one);
+  } else {
+#pragma unroll
+    for (int w = 1; w < N; w <<= 1)
+#pragma unroll
+      for (int j = 0; j < N; j += 2 * w)
+        if (j + w < have) v[j] = add2(v[j], v[j + w], one);
   }
   return v[0];
 }
@@ -125,6 +146,16 @@ __device__ __forceinline__ void leaf_sums(const float (&v)[N], float* out, int w
 // the sum of a lane's eight terms
 template <bool VEC>
 __device__ __forceinline__ float lane_sum(const float v[8], int e0, int D) { return VEC || e0 + 8 <= D ? tree8_full(v) : tree8(v, e0, D); }
+
+// of two sets of terms
+template <bool VEC>
+__device__ __forceinline__ float2 lane_sums(const float a[8], const float b[8], int e0, int D, float2 one) {
+  if (!VEC && e0 + 8 > D) return make_float2(tree8(a, e0, D), tree8(b, e0, D));
+  float2 s[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s[j] = make_float2(fadd(a[2 * j], a[2 * j + 1]), fadd(b[2 * j], b[2 * j + 1]));
+  return add2(add2(s[0], s[1], one), add2(s[2], s[3], one), one);
+}
 
 // Rows are walked over by as many CTAs as the GPU holds; what the next passes need is on its way (AHEAD passes, each thread its own
 // columns) while one is worked on: with a CTA for every few rows the loads of 8192 x 2048 stood still at the barriers (21 us, 32 with the residual
@@ -291,7 +322,7 @@ template <int KIND, int WPR, bool VEC, bool RES>
 __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIND, VEC>::CTAS)
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
              const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int nb, int passes, const void* res,
-             void* dx, float* __restrict__ partial) {
+             void* dx, float* __restrict__ partial, float4* __restrict__ upper, int upper_levels) {
   grid_dep();
   constexpr bool BF = KIND != LN_F32, STAGED = LnBwd<WPR, KIND, VEC>::AHEAD_ROWS;
   using S = LnBwd<WPR, KIND, VEC>;
@@ -306,6 +337,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
+  const float2 one = same2(c_one), minus = same2(-c_one);
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
   // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
@@ -399,41 +431,48 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
       else if (STAGED) row_take<BF, T>(place + a * BYTES + T * Fx::DY, xh[a]);
       else if (VEC) load8n<BF>(x, row_at(row, D, e0), m, xh[a]);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) xh[a][t] = fmul(fsub(xh[a][t], mu[a]), rs[a]);
+      for (int t = 0; t < 8; t += 2) two(xh[a] + t, mul2(fma2(same2(mu[a]), same2(-1.0f), two(xh[a] + t)), same2(rs[a])));
     }
     if (partial) {   // rows in pairs, pairs in pairs; a right node exists iff its first row does, else the left one is carried up unchanged
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        float c[R], d[R];
+      for (int t = 0; t < 8; t += 2) {
+        float2 c[R], d[R];
 #pragma unroll
-        for (int a = 0; a < R; ++a) { c[a] = fmul(w[a][t], xh[a][t]); d[a] = w[a][t]; }
-        node[t] = node_tree<R>(c, rows - first);
-        node[8 + t] = node_tree<R>(d, rows - first);
+        for (int a = 0; a < R; ++a) { d[a] = two(w[a] + t); c[a] = mul2(d[a], two(xh[a] + t)); }
+        two(node + t, node_tree2<R>(c, rows - first, one));
+        two(node + 8 + t, node_tree2<R>(d, rows - first, one));
       }
-      int level = 0;
-      for (; (p >> level) & 1; ++level) {
-        const bool have = r0 + ((p >> level) << level) * R < rows;
-        const float4* l = waiting + level * 4 * T + threadIdx.x;
+      // the lowest levels in shared memory, the others, which are met rarely, in the CTA's place in the workspace
+      float4* far = upper + (size_t)blockIdx.x * upper_levels * 4 * T + threadIdx.x;
+      const auto join = [&](const float4* l, bool have) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float4 q = l[t * T];
-          node[4 * t] = have ? fadd(q.x, node[4 * t]) : q.x;
-          node[4 * t + 1] = have ? fadd(q.y, node[4 * t + 1]) : q.y;
-          node[4 * t + 2] = have ? fadd(q.z, node[4 * t + 2]) : q.z;
-          node[4 * t + 3] = have ? fadd(q.w, node[4 * t + 3]) : q.w;
+          const float2 a = make_float2(q.x, q.y), b = make_float2(q.z, q.w);
+          two(node + 4 * t, have ? add2(a, two(node + 4 * t), one) : a);
+          two(node + 4 * t + 2, have ? add2(b, two(node + 4 * t + 2), one) : b);
         }
-      }
-      if (p + 1 < passes) {
-        float4* l = waiting + level * 4 * T + threadIdx.x;
+      };
+      const auto wait = [&](float4* l) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) l[t * T] = make_float4(node[4 * t], node[4 * t + 1], node[4 * t + 2], node[4 * t + 3]);
+      };
+      int level = 0;
+      for (; (p >> level) & 1; ++level) {
+        const bool have = r0 + ((p >> level) << level) * R < rows;
+        if (level < S::LEVELS) join(waiting + level * 4 * T + threadIdx.x, have);
+        else join(far + (level - S::LEVELS) * 4 * T, have);
+      }
+      if (p + 1 < passes) {
+        if (level < S::LEVELS) wait(waiting + level * 4 * T + threadIdx.x);
+        else wait(far + (level - S::LEVELS) * 4 * T);
       }
     }
     if (gamma) {
 #pragma unroll
       for (int a = 0; a < R; ++a)
 #pragma unroll
-        for (int t = 0; t < 8; ++t) w[a][t] = fmul(w[a][t], g[t]);
+        for (int t = 0; t < 8; t += 2) two(w[a] + t, mul2(two(w[a] + t), two(g + t)));
     }
     float (*leaf)[2][WPR] = leaf_s[odd][grp];
     odd = !odd;
@@ -442,9 +481,8 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
     for (int a = 0; a < R; ++a) {
       float pr[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) pr[t] = fmul(w[a][t], xh[a][t]);
-      part[2 * a] = lane_sum<VEC>(w[a], e0, D);
-      part[2 * a + 1] = lane_sum<VEC>(pr, e0, D);
+      for (int t = 0; t < 8; t += 2) two(pr + t, mul2(two(w[a] + t), two(xh[a] + t)));
+      two(part + 2 * a, lane_sums<VEC>(w[a], pr, e0, D, one));
     }
     leaf_sums<2 * R, WPR>(part, leaf[0][0], warp, D, full);
     __syncthreads();
@@ -456,7 +494,8 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
       const size_t at = row_at(first + a, D, e0);
       float o[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = fmul(rs[a], fsub(fsub(w[a][t], c1), fmul(xh[a][t], c2)));
+      for (int t = 0; t < 8; t += 2)
+        two(o + t, mul2(same2(rs[a]), fma2(mul2(two(xh[a] + t), same2(c2)), minus, add2(two(w[a] + t), same2(-c1), one))));
       if (RES) {   // the gradient that bypasses the norm (res may be dx)
         float b[8];
         if (STAGED) {
@@ -467,7 +506,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
           deal_out(room, raw, b);
         }
 #pragma unroll
-        for (int t = 0; t < 8; ++t) o[t] = fadd(b[t], o[t]);
+        for (int t = 0; t < 8; t += 2) two(o + t, add2(two(o + t), two(b + t), one));
       }
       if (!VEC) store_any<BF>(dx, row_at(first + a, D, w0), first + a < rows ? left : 0, room, o);
       else if (m > 0) store8<BF>(dx, at, o);
@@ -592,30 +631,54 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
   return DET_OK;
 }
 
-// Rows of a block of the backward pass, whose node goes to memory: a multiple of what a CTA works on at a time, more of it while there are two blocks for
-// every CTA on the GPU (each halving of the nodes saves the second kernel half its reading), as many as shared memory has room for waiting nodes.
-struct LnBlock { int passes, rows; };
+// Rows of a block of the backward pass, whose nodes go to memory for the second kernel: more of them while the CTA with the most has not much more to do (all
+// that are on the GPU at once share the blocks).  Fewer nodes are less to write and to read: 8192 x 2048 with blocks of 8 and 32 rows 36.1
+// and 35.3 us, 4096 x 4096 with 2 and 16 passes 42.9 and 37.7.
+constexpr int LN_PASSES = 16, LN_SLACK = 6;                // passes of a block at most; of the busiest CTA, to those with blocks of one, times 4
+struct LnBlock {
+  int passes, rows, levels, upper, ctas;                 // passes of a block, its rows; levels of waiting nodes, how many in the workspace; CTAs at once
+  size_t level;                                          // bytes of a CTA's waiting nodes of a level
+  int blocks(int n) const { return (int)(((long long)n + rows - 1) / rows); }
+  int grid(int n) const { return std::min(blocks(n), ctas); }
+};
 template <int KIND>
 static LnBlock ln_block(int rows, int D) {
-  int per = 0, levels = 0;
+  LnBlock r{};
+  int per = 0, own = 0;
   with_wpr(D, [&](auto wpr) {
     with_bool(D % 8 == 0, [&](auto is_vec) {
       using S = LnBwd<decltype(wpr)::value, KIND, decltype(is_vec)::value>;
       per = S::GROUPS * S::ROWS;
-      levels = S::LEVELS;
+      own = S::LEVELS;
+      r.ctas = S::CTAS * 148;
+      r.level = (size_t)16 * S::THREADS * sizeof(float);
     });
   });
-  int passes = 1;
-  while (passes < (1 << levels) && (long long)rows >= (long long)passes * 4 * per * 296) passes *= 2;
-  return {passes, passes * per};
+  const auto most = [&](int passes) {                    // passes of the CTA with the most
+    const long long blocks = ((long long)rows + (long long)passes * per - 1) / ((long long)passes * per);
+    return (blocks + r.ctas - 1) / r.ctas * passes;
+  };
+  r.passes = 1;
+  for (int p = 2; p <= LN_PASSES; p *= 2)
+    if (4 * most(p) <= LN_SLACK * most(1)) {
+      r.passes = p;
+      ++r.levels;
+    } else {
+      break;
+    }
+  r.rows = r.passes * per;
+  r.upper = std::max(0, r.levels - own);
+  return r;
 }
+static size_t ln_nodes(int nb, int D) { return ((size_t)2 * nb * D * sizeof(float) + 15) / 16 * 16; }
 template <int KIND>
 static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* gamma, const float* mean, const float* rstd, int rows, int D,
                   const void* res, void* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
   const bool cols = dgamma || dbeta;
   const LnBlock block = ln_block<KIND>(rows, D);
-  const int passes = block.passes, nb = (int)(((long long)rows + block.rows - 1) / block.rows);
+  const int nb = block.blocks(rows);
   float* partial = cols ? (float*)ws : nullptr;
+  float4* upper = cols ? (float4*)((char*)ws + ln_nodes(nb, D)) : nullptr;
   int rc = DET_OK;
   with_wpr(D, [&](auto wpr) {
     with_bool(D % 8 == 0, [&](auto is_vec) {
@@ -624,17 +687,14 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
         constexpr bool VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
         if constexpr (!(RES && KIND == LN_F32)) {
           using S = LnBwd<W, KIND, VEC>;
-          int levels = 0;
-          while ((1 << levels) < passes) ++levels;
-          if (S::GROUPS > 1 && levels == 0) levels = 1;
+          const int levels = std::max(std::min(block.levels, (int)S::LEVELS), S::GROUPS > 1 ? 1 : 0);      // in shared memory; the groups meet in the first
           const size_t ahead = S::AHEAD_ROWS ? (size_t)LnFetch<KIND, W, VEC>::AHEAD * S::ROWS * (RES ? LnFetch<KIND, W, VEC>::ROW_RES : LnFetch<KIND, W, VEC>::ROW) : 0;
-          const size_t level = (size_t)16 * S::THREADS * sizeof(float);
           auto kern = k_ln_bwd<KIND, W, VEC, RES>;
           static DevOnce once;
-          rc = dev_ensure_smem(once, (const void*)kern, ahead + S::LEVELS * level);
+          rc = dev_ensure_smem(once, (const void*)kern, ahead + S::LEVELS * block.level);
           if (rc != DET_OK) return;
-          launch_after(kern, ln_grid(nb, S::CTAS), S::THREADS, ahead + (cols ? levels * level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
-                       (float)(1.0 / (double)D), nb, passes, res, dx, partial);
+          launch_after(kern, dim3((unsigned)block.grid(rows)), S::THREADS, ahead + (cols ? levels * block.level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
+                       (float)(1.0 / (double)D), nb, block.passes, res, dx, partial, upper, block.upper);
         }
       });
     });
@@ -676,8 +736,10 @@ extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, 
 
 extern "C" size_t det_layernorm_bwd_ws_bytes(int rows, int D) {
   if (rows <= 0 || D <= 0 || D > 8192) return 256;
-  const int least = min(ln_block<LN_F32>(rows, D).rows, min(ln_block<LN_BF16>(rows, D).rows, ln_block<LN_ACT8>(rows, D).rows));
-  return align_up(2 * (((size_t)rows + least - 1) / least) * (size_t)D * sizeof(float), 256);
+  size_t most = 0;
+  for (const LnBlock& b : {ln_block<LN_F32>(rows, D), ln_block<LN_BF16>(rows, D), ln_block<LN_ACT8>(rows, D)})
+    most = std::max(most, ln_nodes(b.blocks(rows), D) + b.level * b.upper * b.grid(rows));
+  return align_up(most, 256);
 }
 
 // what the three backward calls have in common: checks, nothing to do, launch
