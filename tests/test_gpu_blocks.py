@@ -79,7 +79,7 @@ def test_layernorm(det, bf, rows, D):
             same(host(db), odb, "dbeta")
 
 
-@pytest.mark.parametrize("rows,D", [(30000, 64), (15001, 256), (9000, 768), (29000, 512), (7300, 2048), (3700, 4096), (2000, 8192), (8001, 2041)])
+@pytest.mark.parametrize("rows,D", [(30000, 64), (15001, 256), (9000, 768), (29000, 512), (7300, 2048), (3700, 4096), (2000, 8192), (8001, 2041), (150001, 8)])
 def test_layernorm_many_rows(det, rows, D):
     """Rows enough for every number of passes a group of warps makes."""
     x, dy, g = _rows((rows, D), 13, True), _rows((rows, D), 16, True), _rows(D, 14, True, 1.0, 0.1)
@@ -89,6 +89,19 @@ def test_layernorm_many_rows(det, rows, D):
     _sync()
     odx, odg, odb = oracle.layernorm_bwd(dy, x, g, mean, rstd, bf=True)
     same(host(dx, np.uint16), odx, "dx")
+    same(host(dg), odg, "dgamma")
+    same(host(db), odb, "dbeta")
+
+
+@pytest.mark.parametrize("rows,D", [(113001, 8), (15001, 200), (5001, 1024), (2399, 2056)])
+def test_layernorm_many_rows_binary32(det, rows, D):
+    x, dy, g = _rows((rows, D), 23, False), _rows((rows, D), 26, False), _rows(D, 24, False, 1.0, 0.1)
+    mean, rstd = synth.normal_f32(rows, 0.1, seed=27, tid=1), np.abs(synth.normal_f32(rows, 1.0, seed=27, tid=2)) + F(0.5)
+    dx, dg, db = empty((rows, D), F), empty((D,), F), empty((D,), F)
+    det.det_layernorm_bwd(det.DET_F32, dev(dy), dev(x), dev(g), dev(mean), dev(rstd), rows, D, dx, dg, db, ws(det.det_layernorm_bwd_ws_bytes(rows, D)))
+    _sync()
+    odx, odg, odb = oracle.layernorm_bwd(dy, x, g, mean, rstd, bf=False)
+    same(host(dx), odx, "dx")
     same(host(dg), odg, "dgamma")
     same(host(db), odb, "dbeta")
 
