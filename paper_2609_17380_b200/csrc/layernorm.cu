@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
   // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
-  float mu_next[R], rs_next[R], step_next[R];
+  float mu_next[R], rs_next[R];
+  uint32_t step_next[R];                                  // the field: a step worked out here would wait for the load
   struct { int base, p, slot; } ahead = {(int)blockIdx.x * block, 0, 0};        // the pass to fetch next
   auto fetch = [&]() {
     if (STAGED) {
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
       const bool there = row < rows;
       mu_next[a] = there ? mean[row] : 0.0f;
       rs_next[a] = there ? rstd[row] : 0.0f;
-      if (KIND == LN_ACT8 && VEC) step_next[a] = there && n > 0 ? a8_step(e8[(size_t)row * groups8 + e0 / A8_GROUP]) : 0.0f;
+      if (KIND == LN_ACT8 && VEC) step_next[a] = there && n > 0 ? e8[(size_t)row * groups8 + e0 / A8_GROUP] : 0u;
     }
   };
 #pragma unroll
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
     const int first = r0 + p * R;
     float w[R][8], xh[R][8], rs[R], mu[R], step[R];
 #pragma unroll
-    for (int a = 0; a < R; ++a) { mu[a] = mu_next[a]; rs[a] = rs_next[a]; step[a] = KIND == LN_ACT8 ? step_next[a] : 0.0f; }
+    for (int a = 0; a < R; ++a) { mu[a] = mu_next[a]; rs[a] = rs_next[a]; step[a] = KIND == LN_ACT8 && VEC ? a8_step(step_next[a]) : 0.0f; }
     fetch();
     statistics(p + 1 < passes ? first + R : r0 + stride);
     if (STAGED) fetch_wait<AHEAD - 1>();

@@ -127,7 +127,7 @@ struct __align__(16) LrShared {
   float tab[LR_TAB];
   float4 block[2][LR_WARPS][16];                         // the block maps of this round; two rounds
   float4 span[2][JOINED ? LR_MAXC : 1][16];             // the span maps of the cluster; two rounds
-  float2 start[2][16];                                   // what comes into the CTA's span, and into the next round
+  float2 start[LR_MAXC + 1][16];                         // what comes into the spans of the cluster, and into the next round
   unsigned long long arrived[2];                         // transaction barriers of the span maps, two rounds
   int gone;                                              // a wait ran out
 };
@@ -242,8 +242,8 @@ __device__ __forceinline__ void lr_fetch(uint32_t (*raw)[LR_RAW], const LrCursor
 }
 // the flag of the row `lane` of a chunk of n rows from t on
 template <bool FLAGS>
-__device__ __forceinline__ bool lr_flag(const LrArgs& p, int b, int lane, int t, int n) {
-  return FLAGS && lane < min(n, LR_CHUNK) && p.flags[(size_t)b * p.S + t + lane] != 0;
+__device__ __forceinline__ uint32_t lr_flag(const LrArgs& p, int b, int lane, int t, int n) {
+  return FLAGS && lane < min(n, LR_CHUNK) ? p.flags[(size_t)b * p.S + t + lane] : 0u;
 }
 // work(std::true_type) with cuts of a warp's rows, work(std::false_type) without: rows without a cut need no selection, and cuts are few (65536 rows of 512
 // channels with a cut every 700: 121 -> 110 us forward, 164 -> 159 backward)
@@ -311,28 +311,30 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
     float4(*const place)[16] = sh.span[turn & 1];
     const int to = at.warp + LR_WARPS * at.o;
     if (to < p.cl) store_in_cluster(&place[at.rank][at.lane], bar, to, lr_pack(span));
-    if (at.warp == turn % LR_WARPS) {
+    if (at.warp == 0) {
       constexpr int BATCH = 4;
       mbar_wait_warp(bar, (turn >> 1) & 1, &sh.gone, p.status);
       const int spans = min(p.cl, (p.n + LR_WARPS * LR_BLOCK - 1) / (LR_WARPS * LR_BLOCK) - (r.span - at.rank));
-      for (int r0 = 0; r0 < spans; r0 += BATCH) {
-        float4 m[BATCH];
+      int i = 0;
+      for (; i + BATCH <= spans; i += BATCH) {
+        LrMap m[BATCH];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) m[i] = place[min(r0 + i, spans - 1)][at.lane];
+        for (int j = 0; j < BATCH; ++j) m[j] = lr_unpack(place[i + j][at.lane]);
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-          if (r0 + i == at.rank) start = s;
-          if (r0 + i < spans) s = lr_apply(lr_unpack(m[i]), s, one);
+        for (int j = 0; j < BATCH; ++j) {
+          sh.start[i + j][at.lane] = s;
+          s = lr_apply(m[j], s, one);
         }
       }
-      if (at.o == 0) {
-        sh.start[0][at.lane] = start;
-        sh.start[1][at.lane] = s;
+      for (; i < spans; ++i) {
+        sh.start[i][at.lane] = s;
+        s = lr_apply(lr_unpack(place[i][at.lane]), s, one);
       }
+      sh.start[LR_MAXC][at.lane] = s;
     }
     __syncthreads();
-    start = sh.start[0][at.lane];
-    s = sh.start[1][at.lane];
+    start = sh.start[at.rank][at.lane];
+    s = sh.start[LR_MAXC][at.lane];
   }
   if (half) start = lr_apply(g0, start, one);
   if (at.warp & 3) start = lr_apply(before, start, one);
@@ -361,12 +363,12 @@ __device__ __forceinline__ void lr_close() {
   cluster_wait();
 }
 
-// Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 30 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
-// 110 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 25 and 37 of 8 and 14; 1 x 65536 x 512 with cuts 110 and 159 of 31 and 51.  The first
+// Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 29 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
+// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 25 and 38 of 8 and 14; 1 x 65536 x 512 with cuts 102 and 144 of 31 and 51.  The first
 // three are bound by instructions (some 500 a round of 8 rows a warp forward, 130 of them the hand-over), the last by the steps that a round of a
 // cluster has to wait for one after the other.
 template <int WORDS, bool FLAGS, bool JOINED>
-__global__ void __launch_bounds__(LR_T, JOINED ? 2 : 3) k_linrec_fwd(const __grid_constant__ LrArgs p) {
+__global__ void __launch_bounds__(LR_T, 2) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];
   LrShared<2, JOINED>& sh = *reinterpret_cast<LrShared<2, JOINED>*>(smem);
   const LrPlace<JOINED> at(p);
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(LR_T, JOINED ? 2 : 3) k_linrec_fwd(const __gri
   grid_dep();
   uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
   LrRound<false, JOINED> r(p, at), ahead = r;
-  bool flag = false;
+  uint32_t flag = 0;                                     // compared in the round that uses it: a comparison here waits for the load
   float2 s = make_float2(0.0f, 0.0f), first = s;
   LrCursor<WORDS> cg, cv;
   LrCursor<0> cy;
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(LR_T, JOINED ? 2 : 3) k_linrec_fwd(const __gri
       constexpr bool FULL = decltype(whole)::value;
       const int n = FULL ? LR_CHUNK : p.S - t0;          // n rows of the chunk exist
       const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
-      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
+      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag != 0) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
       const uint32_t* q = raw[0][at.o] + at.lane;
       float2 f[LR_CHUNK], u[LR_CHUNK];
       lr_gates(q, sh.tab, f, u);
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
   grid_dep();
   uint32_t(*raw)[LR_BLOCK][LR_RAW] = sh.raw[at.warp];
   LrRound<true, JOINED> r(p, at), ahead = r;
-  bool flag = false;
+  uint32_t flag = 0;                                     // compared in the round that uses it: a comparison here waits for the load
   float2 s = make_float2(0.0f, 0.0f), first = s, next = s;                            // next: the state in front of the thread's chunk
   LrCursor<WORDS> cg, cv, cdy;
   LrCursor<0> odv, odg;
@@ -510,7 +512,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
       constexpr bool FULL = decltype(whole)::value;
       const int n = FULL ? LR_CHUNK : t0 < 0 ? 0 : p.S - t0;                          // n rows of the chunk exist
       const bool have = FULL || r.ch0 + 2 * at.lane < p.D;
-      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
+      const uint32_t all = FLAGS ? __ballot_sync(0xffffffffu, flag != 0) : 0u, cuts = (all >> (threadIdx.x & 16)) & 0xffu;
       float2 h = next;
       const uint32_t* q = raw[0][at.o] + at.lane;
       float2 f[LR_CHUNK], z[LR_CHUNK];
@@ -620,10 +622,10 @@ __global__ void __launch_bounds__(128) k_linrec_chunk(const __grid_constant__ Lr
 // GPU, and they do not pack: of 296 CTAs, two on an SM, 264 fit in clusters of 4, 240 of 8 and 224 of 16, and a pass that needed 256 where 224 fit took
 // twice as long; so the runtime is asked once per device and kernel what fits.
 // Where there are strips enough, lone CTAs go through several, about as many as the others.  The CTAs of a grid are not spread evenly: 256 of them ran in
-// 42 us where three fit on an SM and in 31 where two did (4 x 2048 x 2048 forward).  So no more are let on an SM than are needed, by the shared memory that
-// is asked for.
+// 42 us where three fitted on an SM and in 31 where two did (4 x 2048 x 2048 forward).  So no more are let on an SM than are needed, by the shared memory
+// that is asked for.
 using LrKernel = void (*)(const LrArgs);
-constexpr int LR_MAXR = 3;                               // lone CTAs on an SM
+constexpr int LR_MAXR = 2;                               // lone CTAs on an SM (three, with 80 registers a thread, took 30.2 us where two take 29.0)
 struct LrFits {
   std::mutex lock;
   bool known[MAX_DEVICES] = {};
