@@ -311,26 +311,30 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
     float4(*const place)[16] = sh.span[turn & 1];
     const int to = at.warp + LR_WARPS * at.o;
     if (to < p.cl) store_in_cluster(&place[at.rank][at.lane], bar, to, lr_pack(span));
-    if (at.warp == 0) {
+    if (at.warp == 0) {   // a lane a channel: the packed instructions take longer one after the other (1 x 65536 x 64 58.7 -> 55.9 us)
       constexpr int BATCH = 4;
+      const int l = threadIdx.x & 31;
       mbar_wait_warp(bar, (turn >> 1) & 1, &sh.gone, p.status);
       const int spans = min(p.cl, (p.n + LR_WARPS * LR_BLOCK - 1) / (LR_WARPS * LR_BLOCK) - (r.span - at.rank));
+      const float* maps = reinterpret_cast<const float*>(place) + l / 2 * 4 + l % 2;
+      float* in = reinterpret_cast<float*>(sh.start) + l;
+      float c = in[LR_MAXC * LR_CH];
       int i = 0;
       for (; i + BATCH <= spans; i += BATCH) {
-        LrMap m[BATCH];
+        float m[BATCH][2];
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j) m[j] = lr_unpack(place[i + j][at.lane]);
+        for (int j = 0; j < BATCH; ++j) m[j][0] = maps[(i + j) * 64], m[j][1] = maps[(i + j) * 64 + 2];
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
-          sh.start[i + j][at.lane] = s;
-          s = lr_apply(m[j], s, one);
+          in[(i + j) * LR_CH] = c;
+          c = m[j][0] == 0.0f ? m[j][1] : fadd(fmul(m[j][0], c), m[j][1]);
         }
       }
       for (; i < spans; ++i) {
-        sh.start[i][at.lane] = s;
-        s = lr_apply(lr_unpack(place[i][at.lane]), s, one);
+        in[i * LR_CH] = c;
+        c = maps[i * 64] == 0.0f ? maps[i * 64 + 2] : fadd(fmul(maps[i * 64], c), maps[i * 64 + 2]);
       }
-      sh.start[LR_MAXC][at.lane] = s;
+      in[LR_MAXC * LR_CH] = c;
     }
     __syncthreads();
     start = sh.start[at.rank][at.lane];
@@ -364,7 +368,7 @@ __device__ __forceinline__ void lr_close() {
 }
 
 // Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 29 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
-// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 25 and 38 of 8 and 14; 1 x 65536 x 512 with cuts 102 and 144 of 31 and 51.  The first
+// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 26 and 37 of 8 and 14; 1 x 65536 x 512 with cuts 97 and 138 of 31 and 51.  The first
 // three are bound by instructions (some 500 a round of 8 rows a warp forward, 130 of them the hand-over), the last by the steps that a round of a
 // cluster has to wait for one after the other.
 template <int WORDS, bool FLAGS, bool JOINED>
@@ -411,6 +415,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_fwd(const __grid_constant__ 
     const int t0 = r.row(p, at.warp, at.o);
     if (r.k == 0) {
       s = first;
+      if (JOINED && threadIdx.x < 16) sh.start[LR_MAXC][at.lane] = s;                 // read behind the barrier of the hand-over
       cy.begin(p.y, p.ld_y, p, at, r);
     }
     auto round = [&](auto whole) {
@@ -505,6 +510,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
     const int t0 = r.row(p, at.warp, at.o);
     if (r.k == 0) {
       s = first;
+      if (JOINED && threadIdx.x < 16) sh.start[LR_MAXC][at.lane] = s;                 // read behind the barrier of the hand-over
       odv.begin(p.dv, p.ld_d, p, at, r);
       odg.begin(p.dg, p.ld_d, p, at, r);
     }
