@@ -276,13 +276,13 @@ __device__ __forceinline__ LrMap lr_from(const LrMap& m, int lane) {
                make_float2(__shfl_sync(0xffffffffu, m.h.x, lane), __shfl_sync(0xffffffffu, m.h.y, lane))};
 }
 // The hand-over of a round: the map of this thread's chunk in, what comes into the chunk out; `s`, what comes into the round, becomes what comes into
-// the next one.  `turn` counts the rounds of the CTA.
+// the next one.  `turn` counts the rounds of the CTA; `meanwhile` is done while the maps of the others are on their way.
 // The maps of two rounds have places of their own: a warp writes its block's map of round r + 2 behind a barrier of round r + 1, which all warps pass
 // when they have read round r's; a CTA sends its span's map of round r + 2 when it has all of round r + 1, that of the receiver among them, which was
 // sent behind the barrier that the receiver's reader of round r has passed too.
-template <bool FULL, bool BACK, int NS, bool JOINED>
+template <bool FULL, bool BACK, int NS, bool JOINED, typename M>
 __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const LrArgs& p, const LrPlace<JOINED>& at, const LrRound<BACK, JOINED>& r, int turn,
-                                               const LrMap& mine, float2& s, float2 one) {
+                                               const LrMap& mine, float2& s, float2 one, M&& meanwhile) {
   const int chunks = p.n - r.span * LR_WARPS * LR_BLOCK, blocks = (chunks + 1) / LR_BLOCK;               // from the CTA's first ones on
   const LrMap other = lr_from(mine, threadIdx.x ^ 16), both = lr_compose(other, mine, one);              // `both`: in the lanes of chunk 1
   const bool two = FULL || chunks > at.warp * LR_BLOCK + 1;
@@ -300,7 +300,6 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
     if (FULL || at.o * LR_GROUP + i < blocks) group = lr_compose(group, m, one);
   }
   const int half = at.warp / LR_GROUP;
-  before = lr_from(before, half * 16 + at.lane);
   const LrMap g0 = lr_from(group, at.lane), g1 = lr_from(group, 16 + at.lane);
   LrMap span = g0;
   if (FULL || blocks > LR_GROUP) span = lr_compose(g0, g1, one);
@@ -311,6 +310,7 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
     float4(*const place)[16] = sh.span[turn & 1];
     const int to = at.warp + LR_WARPS * at.o;
     if (to < p.cl) store_in_cluster(&place[at.rank][at.lane], bar, to, lr_pack(span));
+    meanwhile();
     if (at.warp == 0) {   // a lane a channel: the packed instructions take longer one after the other (1 x 65536 x 64 58.7 -> 55.9 us)
       constexpr int BATCH = 4;
       const int l = threadIdx.x & 31;
@@ -340,6 +340,7 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
     start = sh.start[at.rank][at.lane];
     s = sh.start[LR_MAXC][at.lane];
   }
+  before = lr_from(before, half * 16 + at.lane);
   if (half) start = lr_apply(g0, start, one);
   if (at.warp & 3) start = lr_apply(before, start, one);
   const float2 second = lr_apply(other, start, one);
@@ -368,7 +369,7 @@ __device__ __forceinline__ void lr_close() {
 }
 
 // Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 29 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
-// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 26 and 37 of 8 and 14; 1 x 65536 x 512 with cuts 97 and 138 of 31 and 51.  The first
+// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 24 and 35 of 8 and 14; 1 x 65536 x 512 with cuts 93 and 131 of 31 and 51.  The first
 // three are bound by instructions (some 500 a round of 8 rows a warp forward, 130 of them the hand-over), the last by the steps that a round of a
 // cluster has to wait for one after the other.
 template <int WORDS, bool FLAGS, bool JOINED>
@@ -436,8 +437,9 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_fwd(const __grid_constant__ 
         }
       });
       __syncwarp();
-      if (ahead.more(p)) fetch();
-      float2 h = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
+      const auto next_round = [&] { if (ahead.more(p)) fetch(); };
+      if (!JOINED) next_round();
+      float2 h = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one, next_round);
       if (p.save && n > 0 && have) *reinterpret_cast<float2*>(p.save + r.state(p, at) + ((size_t)r.b * (p.n - 1) + t0 / LR_CHUNK) * p.D) = h;
       uint16_t* out = const_cast<uint16_t*>(cy.at);
       lr_with_cuts<FLAGS>(all, [&](auto some) {
@@ -530,7 +532,8 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
         wd[i] = q[2 * LR_BLOCK * LR_RAW + i * 16];
       }
       __syncwarp();
-      if (ahead.more(p)) fetch();
+      const auto next_round = [&] { if (ahead.more(p)) fetch(); };
+      if (!JOINED) next_round();
       LrMap mine;
       mine.a = mine.h = same2(0.0f);
       lr_with_cuts<FLAGS>(all, [&](auto some) {
@@ -538,7 +541,7 @@ __global__ void __launch_bounds__(LR_T, 2) k_linrec_bwd(const __grid_constant__ 
         for (int i = LR_CHUNK - 1; i >= 0; --i)
           if (i < n) lr_extend_back(mine, i == (FULL ? LR_CHUNK : min(n, LR_CHUNK)) - 1, f[i], make_float2(bflo(wd[i]), bfhi(wd[i])), decltype(some)::value && ((cuts >> i) & 1), one);
       });
-      float2 c = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one);
+      float2 c = lr_hand_over<FULL>(sh, p, at, r, turn, mine, s, one, next_round);
       uint16_t *dv = const_cast<uint16_t*>(odv.at) + (LR_CHUNK - 1) * p.ld_d, *dg = const_cast<uint16_t*>(odg.at) + (LR_CHUNK - 1) * p.ld_d;
       lr_with_cuts<FLAGS>(all, [&](auto some) {
         float2 diff[LR_CHUNK];                             // h_{t-1} - v
