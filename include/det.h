@@ -167,7 +167,7 @@ int det_rmsnorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf
                              const det_bf16* res, det_bf16* dx, float* dgamma, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- layer norm -------------------------------------------------------------------------------------------
- * The norm that subtracts the mean; not in the paper's block, for replays of models that use it.  Any rows and 1 <= D <= 8192;
+ * The norm that subtracts the mean; not in the paper's block, for replays of models that use it.  Up to 2e9 rows and 1 <= D <= 8192;
  * pointers 16-byte aligned where D % 8 == 0, aligned to their element otherwise; io: dtype of x, y, gamma, beta, dy, dx.
  *   mean = det_sum(x) * (1/D), d = x - mean, rstd = 1 / sqrt(det_sum(d^2) * (1/D) + eps), y = (d * rstd) * gamma + beta;
  * gamma or beta NULL: without that step.  mean, rstd f32 [rows]. */
@@ -199,13 +199,14 @@ int det_layernorm_bwd_act8(const det_bf16* dy, const int8_t* q8, const uint8_t* 
  * 2^-126: code = rne(v * 2^-E) in [-127, 127], value = code * 2^E.  Every product is exact, so a value is off by at most half a step and comes
  * back exactly in bf16 as in f32.  q8 int8 [rows, D], e8 uint8 [rows, ceil(D/32)] = E + 127; a group with an infinity or a NaN has
  * e8 = 255 and comes back as infinities (code +-127) and NaNs (code 0).
- * io: dtype of x and y; their rows are ld elements apart (ld >= D); any D, any alignment to the element. */
+ * io: dtype of x and y; their rows are ld elements apart (ld >= D); any D, any alignment to the element; fewer than 2^28 groups. */
 size_t det_act8_exp_bytes(int rows, int D); /* bytes of e8 */
 int det_act8_pack(int io, const void* x, int ld, int rows, int D, int8_t* q8, uint8_t* e8, void* stream);
 int det_act8_unpack(int io, const int8_t* q8, const uint8_t* e8, int rows, int D, void* y, int ld, void* stream);
 /* SwiGLU (see det_swiglu_fwd) with gu kept in 8 bits: det_swiglu_fwd_act8 is the forward pass that also packs gu; det_swiglu_act8 and
  * det_swiglu_bwd_act8 are det_swiglu_fwd and det_swiglu_bwd of the unpacked gu, bit for bit.  With qh also det_swiglu_fwd_q's codes of the h
- * they write (qh, s_q may be NULL).  q8 int8 [rows, 2F], e8 [rows, 2F/32]; F % 32 == 0; q8, qh 8-byte aligned. */
+ * they write (qh, s_q may be NULL).  q8 int8 [rows, 2F], e8 [rows, 2F/32]; F % 32 == 0, rows * F < 2^33; q8, qh
+ * 8-byte aligned. */
 int det_swiglu_fwd_act8(const det_bf16* gu, int rows, int F, det_bf16* h, int8_t* q8, uint8_t* e8, const float* s_q, int8_t* qh, void* stream);
 int det_swiglu_act8(const int8_t* q8, const uint8_t* e8, int rows, int F, det_bf16* h, const float* s_q, int8_t* qh, void* stream);
 int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8, int rows, int F, det_bf16* dgu, void* stream);
@@ -223,7 +224,7 @@ int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8,
  * groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came into that; what comes into a block or a chunk
  * the map of all those before it, in its group or block, applied to what comes into that; h is walked row by row from there.  A = 0 lets nothing in.
  * states f32 [B, ceil(S/8), D] (det_linrec_state_floats; NULL: not kept) are the states in front of the chunks, for the backward pass.
- * D, ld, ld_y, ld_d even, S <= 2^30; bf16 pointers 4-byte, f32 pointers 8-byte aligned.  S = 0: hT = h0, dh0 = dhT.  Outputs overlap no
+ * D, ld, ld_y, ld_d even, S <= 2^30, B * ceil(D/32) <= 2^26; bf16 pointers 4-byte, f32 pointers 8-byte aligned.  S = 0: hT = h0, dh0 = dhT.  Outputs overlap no
  * input but as said.  status_dev (may be NULL) receives DET_DEV_TIMEOUT if a bounded wait of one CTA for another runs out. */
 size_t det_linrec_state_floats(int B, int S, int D);
 int det_linrec_fwd(const det_bf16* g, const det_bf16* v, int ld, int B, int S, int D, det_bf16* y, int ld_y, const uint8_t* flags,

@@ -711,9 +711,9 @@ static int lr_run(LrArgs& p, int B, cudaStream_t st) {
   p.rounds = (spans + p.cl - 1) / p.cl;
   p.cl = (spans + p.rounds - 1) / p.rounds;              // as many as have work in every round
   p.step = p.items;
-  note_launch();
   if (p.cl > 1) {
     LrLaunch l((unsigned)(p.items * p.cl), p.cl, lr_smem(joined.smem, 2), st);
+    note_launch();
     cudaLaunchKernelEx(&l.cfg, joined.kern, p);
   } else {
     const int most = *std::max_element(fit.lone, fit.lone + LR_MAXR);
@@ -723,6 +723,7 @@ static int lr_run(LrArgs& p, int B, cudaStream_t st) {
     int r = 0;
     while (r < LR_MAXR - 1 && p.step > fit.lone[r]) ++r;
     LrLaunch l((unsigned)p.step, 1, lr_smem(lone.smem, r + 1), st);
+    note_launch();
     cudaLaunchKernelEx(&l.cfg, lone.kern, p);
   }
   DET_CHECK_LAUNCH();

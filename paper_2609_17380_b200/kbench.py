@@ -4,7 +4,8 @@
 
 Cases follow the benchmark configurations: the order-fixed reductions (RMSNorm 16384x2048 f32, cross-entropy
 4096x50304, sum of squares over 1.2e9 f32), the 1B-shaped linear set at 8192 tokens per micro-batch, attention
-(4 x 16 heads x 2048), the LM head, accumulation, AdamW and the hash.  `--small` shrinks every case to a few hundred
+(4 x 16 heads x 2048), the LM head, accumulation, AdamW and the hash; then the operators of other blocks: layer norm at the residual
+stream (16384 x 2048 bf16), activations in 8 bits, SwiGLU on them, the linear recurrence (8 x 4096 x 2048).  `--small` shrinks every case to a few hundred
 MB for profiler captures.  Rates are algorithmic bytes (or integer / floating-point operations) per second.
 """
 import argparse
@@ -85,6 +86,59 @@ def case_rmsnorm(small, bwd):
     if bwd:
         return (lambda: det.det_rmsnorm_bwd(det.DET_F32, dy, x, g, rstd, rows, D, y, dg, w)), 12.0 * rows * D, "B"
     return (lambda: det.det_rmsnorm_fwd(det.DET_F32, x, g, rows, D, 1e-6, y, rstd)), 8.0 * rows * D, "B"
+
+
+def _bf16(*shape):
+    return torch.randn(*shape, device="cuda").bfloat16()
+
+
+def case_layernorm(small, what):
+    """The norm at the residual stream, as the step driver calls it."""
+    rows, D = 16384, 2048
+    x, o, dy = _bf16(rows, D), _bf16(rows, D), _bf16(rows, D)
+    g, b = 1 + 0.02 * _bf16(D), 0.02 * _bf16(D)
+    y, s = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, dg, db = (torch.empty(n, device="cuda") for n in (rows, rows, D, D))
+    q, e = torch.empty(rows, D, dtype=I8, device="cuda"), torch.empty(det.det_act8_exp_bytes(rows, D), dtype=torch.uint8, device="cuda")
+    w = ws(det.det_layernorm_bwd_ws_bytes(rows, D))
+    fwd = lambda: det.det_residual_layernorm_fwd(x, o, g, b, rows, D, 1e-6, s, y, mean, rstd, q8=q, e8=e)
+    fwd()
+    if what == "fwd":
+        return (lambda: det.det_residual_layernorm_fwd(x, o, g, b, rows, D, 1e-6, s, y, mean, rstd)), 8.0 * rows * D, "B"
+    if what == "bwd":
+        return (lambda: det.det_layernorm_bwd_residual(dy, s, g, mean, rstd, rows, D, o, y, dg, db, w)), 8.0 * rows * D, "B"
+    return (lambda: det.det_layernorm_bwd_act8(dy, q, e, g, mean, rstd, rows, D, o, y, dg, db, w)), (7.0 + 1 / 32) * rows * D, "B"
+
+
+def case_act8(small, back):
+    rows, D = (8192 if small else 16384), 16384
+    x, q, e = _bf16(rows, D), torch.empty(rows, D, dtype=I8, device="cuda"), torch.empty(det.det_act8_exp_bytes(rows, D), dtype=torch.uint8, device="cuda")
+    det.det_act8_pack(det.DET_BF16, x, D, rows, D, q, e)
+    fn = (lambda: det.det_act8_unpack(det.DET_BF16, q, e, rows, D, x, D)) if back else (lambda: det.det_act8_pack(det.DET_BF16, x, D, rows, D, q, e))
+    return fn, (3.0 + 1 / 32) * rows * D, "B"
+
+
+def case_swiglu_act8(small, what):
+    rows, Fh = (8192 if small else 16384), 8192
+    gu, h = _bf16(rows, 2 * Fh), torch.empty(rows, Fh, dtype=torch.bfloat16, device="cuda")
+    q, e = torch.empty(rows, 2 * Fh, dtype=I8, device="cuda"), torch.empty(rows, 2 * Fh // 32, dtype=torch.uint8, device="cuda")
+    det.det_swiglu_fwd_act8(gu, rows, Fh, h, q, e)
+    n = rows * Fh
+    return {"fwd": ((lambda: det.det_swiglu_fwd_act8(gu, rows, Fh, h, q, e)), (8.0 + 1 / 16) * n, "B"),
+            "again": ((lambda: det.det_swiglu_act8(q, e, rows, Fh, h)), (4.0 + 1 / 16) * n, "B"),
+            "bwd": ((lambda: det.det_swiglu_bwd_act8(h, q, e, rows, Fh, gu)), (8.0 + 1 / 16) * n, "B")}[what]
+
+
+def case_linrec(small, bwd):
+    B, S, D = 8, 4096, 2048
+    T = B * S
+    gv, dy, y, dgv = _bf16(T, 2 * D), _bf16(T, D), _bf16(T, D), _bf16(T, 2 * D)
+    st, p, o = torch.empty(det.det_linrec_state_floats(B, S, D), device="cuda"), gv.data_ptr(), dgv.data_ptr()
+    fwd = lambda: det.det_linrec_fwd(p, p + 2 * D, 2 * D, B, S, D, y, D, states=st)
+    fwd()
+    if bwd:   # gv and dgv are held by the call
+        return (lambda gv=gv, dgv=dgv: det.det_linrec_bwd(dy, D, p, p + 2 * D, 2 * D, B, S, D, st, o, o + 2 * D, 2 * D)), 10.5 * T * D, "B"
+    return (lambda gv=gv: fwd()), 6.5 * T * D, "B"
 
 
 def case_xent(small, bwd):
@@ -243,7 +297,13 @@ def build_cases():
          "attn_fwd_int8pv": lambda s: case_attn(s, False, True), "attn_fwd_v2": case_attn_v2,
          "attn_bwd_fixq": lambda s: case_attn(s, True, False, True),
          "lmhead_fwd": lambda s: case_lmhead(s, False), "lmhead_fwd_v2": case_lmhead_v2, "lmhead_bwd_v2": case_lmhead_bwd_v2, "lmhead_bwd": lambda s: case_lmhead(s, True),
-         "accum": case_accum, "adamw": case_adamw, "hash": case_hash}
+         "accum": case_accum, "adamw": case_adamw, "hash": case_hash,
+         "act8_pack": lambda s: case_act8(s, False), "act8_unpack": lambda s: case_act8(s, True),
+         "linrec_fwd": lambda s: case_linrec(s, False), "linrec_bwd": lambda s: case_linrec(s, True)}
+    for k in ("fwd", "bwd", "bwd_act8"):
+        c["layernorm_" + k] = (lambda s, k=k: case_layernorm(s, k))
+    for k in ("fwd", "again", "bwd"):
+        c["swiglu_act8_" + k] = (lambda s, k=k: case_swiglu_act8(s, k))
     for k in LINEAR_SHAPES:
         c["igemm_" + k] = (lambda s, k=k: case_igemm(s, k))
         c["linear_fwd_" + k] = (lambda s, k=k: case_linear(s, k, False))
