@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
   const int e0 = warp * 256 + lane * 8, n = D - e0;
   const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
+  const float2 one = same2(c_one);
   const int stride = gridDim.x * S::GROUPS * R;
   auto fetch = [&](int first, int slot) {
     if (S::AHEAD_ROWS) {
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
         if (S::AHEAD_ROWS) row_take<BF, T>(place + a * BYTES + T * 8 * EL, c);
         else deal_out(room, raw_res[a], c);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[a][t] = fadd(v[a][t], c[t]);
+        for (int t = 0; t < 8; t += 2) two(v[a] + t, add2(two(v[a] + t), two(c + t), one));
         if (!VEC) store_any<BF>(sum, row_at(first + a, D, w0), first + a < rows ? left : 0, room, v[a]);
         else if (m > 0) store8<BF>(sum, at, v[a]);
         if (BF) {
@@ -267,9 +268,10 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
       const float mu = __shfl_sync(0xffffffffu, mu_mine, a);
       float sq[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        v[a][t] = fsub(v[a][t], mu);
-        sq[t] = fmul(v[a][t], v[a][t]);
+      for (int t = 0; t < 8; t += 2) {
+        const float2 d = fma2(same2(mu), same2(-1.0f), two(v[a] + t));
+        two(v[a] + t, d);
+        two(sq + t, mul2(d, d));
       }
       part[a] = lane_sum<VEC>(sq, e0, D);
     }
@@ -286,14 +288,14 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
       if (first + a >= rows) continue;
       float o[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = fmul(v[a][t], rs);
+      for (int t = 0; t < 8; t += 2) two(o + t, mul2(two(v[a] + t), same2(rs)));
       if (gamma) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) o[t] = fmul(o[t], g[t]);
+        for (int t = 0; t < 8; t += 2) two(o + t, mul2(two(o + t), two(g + t)));
       }
       if (beta) {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) o[t] = fadd(o[t], b[t]);
+        for (int t = 0; t < 8; t += 2) two(o + t, add2(two(o + t), two(b + t), one));
       }
       const size_t at = row_at(first + a, D, e0);
       if (!VEC) store_any<BF>(y, row_at(first + a, D, w0), left, room, o);
