@@ -48,6 +48,8 @@ __device__ __forceinline__ float node_tree(float (&v)[N], int have) {
   }
   return v[0];
 }
+// The sum of one row is that row, carried up without an addition: flushed like every value that enters or leaves an operation.
+__device__ __forceinline__ float ln_flush(float r) { return (__float_as_uint(r) & 0x7f800000u) ? r : __uint_as_float(__float_as_uint(r) & 0x80000000u); }
 // Two neighbours of a lane's columns in packed arithmetic, no product fused with a sum (8192 x 2048 backward with the residual stream 37.7 -> 36.3 us, 15.9 -> 13.5 million instructions).
 __device__ __forceinline__ float2 two(const float* v) { return make_float2(v[0], v[1]); }
 __device__ __forceinline__ void two(float* v, float2 x) { v[0] = x.x; v[1] = x.y; }
@@ -310,7 +312,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
 
 // Backward.  Each group of warps takes `passes` x ROWS adjacent rows (passes a power of two), ROWS at a time; a lane sees the same eight columns of
 // all of them, so the trees of dgamma and dbeta over the group's rows run in its own registers, the nodes of finished passes waiting
-// in shared memory as the digits of a binary counter do.  The nodes of a CTA go to partial[0 (dgamma), 1 (dbeta)][CTA][D], for k_ln_cols.
+// in shared memory as the digits of a binary counter do.  The node of a block goes to out_g, out_b [block][D], for k_ln_cols; with one block they are dgamma and dbeta.
 // What is fetched ahead of a pass: dy, x (or its codes) and the bypassing gradient of its rows, AHEAD passes of them.  As many CTAs as the GPU holds walk
 // over the blocks of rows, so the loads go on across the blocks.
 template <int KIND, int WPR, bool VEC>
@@ -324,7 +326,7 @@ template <int KIND, int WPR, bool VEC, bool RES>
 __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIND, VEC>::CTAS)
     k_ln_bwd(const void* __restrict__ dy, const void* __restrict__ x, const uint8_t* __restrict__ e8, const void* __restrict__ gamma,
              const float* __restrict__ mean, const float* __restrict__ rstd, int rows, int D, float invD, int nb, int passes, const void* res,
-             void* dx, float* __restrict__ partial, float4* __restrict__ upper, int upper_levels) {
+             void* dx, float* __restrict__ out_g, float* __restrict__ out_b, float4* __restrict__ upper, int upper_levels) {
   grid_dep();
   constexpr bool BF = KIND != LN_F32, STAGED = LnBwd<WPR, KIND, VEC>::AHEAD_ROWS;
   using S = LnBwd<WPR, KIND, VEC>;
@@ -340,6 +342,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
   const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
   const float2 one = same2(c_one), minus = same2(-c_one);
+  const bool cols = out_g || out_b;
   const int groups8 = (D + A8_GROUP - 1) / A8_GROUP;
   const int block = S::GROUPS * R * passes, stride = gridDim.x * block, mine = grp * R * passes;   // rows: of a block, to this CTA's next one, of the groups before
   // the row's statistics and, of a checkpoint, the step travel in registers, a pass ahead
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
 #pragma unroll
       for (int t = 0; t < 8; t += 2) two(xh[a] + t, mul2(fma2(same2(mu[a]), same2(-1.0f), two(xh[a] + t)), same2(rs[a])));
     }
-    if (partial) {   // rows in pairs, pairs in pairs; a right node exists iff its first row does, else the left one is carried up unchanged
+    if (cols) {   // rows in pairs, pairs in pairs; a right node exists iff its first row does, else the left one is carried up unchanged
 #pragma unroll
       for (int t = 0; t < 8; t += 2) {
         float2 c[R], d[R];
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
       else if (m > 0) store8<BF>(dx, at, o);
     }
   }
-  if (!partial) continue;
+  if (!cols) continue;
   if (S::GROUPS > 1) {   // the tree over the groups' nodes
     __syncthreads();
     float* meet = reinterpret_cast<float*>(waiting) + threadIdx.x;
@@ -534,13 +537,15 @@ __global__ void __launch_bounds__(LnBwd<WPR, KIND, VEC>::THREADS, LnBwd<WPR, KIN
     __syncthreads();
   }
   if (grp == 0) {
-    float* dst = partial + (size_t)blk * D + e0;
-    if (!VEC) {
-      store_any<false>(dst - lane * 8, 0, left, room, node);
-      store_any<false>(dst - lane * 8 + (size_t)nb * D, 0, left, room, node + 8);
-    } else if (n > 0) {
-      store8<false>(dst, 0, node);
-      store8<false>(dst + (size_t)nb * D, 0, node + 8);
+#pragma unroll
+    for (int t = 0; t < 16; ++t) node[t] = ln_flush(node[t]);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      float* dst = w ? out_b : out_g;
+      if (!dst) continue;
+      dst += (size_t)blk * D + e0;
+      if (!VEC) store_any<false>(dst - lane * 8, 0, left, room, node + 8 * w);
+      else if (n > 0) store8<false>(dst, 0, node + 8 * w);
     }
   }
   }
@@ -583,8 +588,7 @@ __global__ void __launch_bounds__(1024) k_ln_cols(const float* __restrict__ part
   while (((thousands - 1) >> level) & 1) ++level;
   for (++level; (thousands >> level) != 0; ++level)
     if ((thousands >> level) & 1) r = fadd(waiting[level], r);
-  // the sum of one row is that row, carried up without an addition: flushed like every value that enters or leaves an operation
-  out[col] = (__float_as_uint(r) & 0x7f800000u) ? r : __uint_as_float(__float_as_uint(r) & 0x80000000u);
+  out[col] = r;
 }
 
 // ---- host side -------------------------------------------------------------------------------------------
@@ -680,7 +684,9 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
   const bool cols = dgamma || dbeta;
   const LnBlock block = ln_block<KIND>(rows, D);
   const int nb = block.blocks(rows);
-  float* partial = cols ? (float*)ws : nullptr;
+  const bool direct = nb == 1 && (D % 8 != 0 || (aligned16(dgamma) && aligned16(dbeta)));     // few rows: no second launch
+  float* partial = (float*)ws;
+  float *out_g = direct ? dgamma : cols ? partial : nullptr, *out_b = direct ? dbeta : cols ? partial + (size_t)nb * D : nullptr;
   float4* upper = cols ? (float4*)((char*)ws + ln_nodes(nb, D)) : nullptr;
   int rc = DET_OK;
   with_wpr(D, [&](auto wpr) {
@@ -697,13 +703,13 @@ static int ln_bwd(const void* dy, const void* x, const uint8_t* e8, const void* 
           rc = dev_ensure_smem(once, (const void*)kern, ahead + S::LEVELS * block.level);
           if (rc != DET_OK) return;
           launch_after(kern, dim3((unsigned)block.grid(rows)), S::THREADS, ahead + (cols ? levels * block.level : 0), st, dy, x, e8, gamma, mean, rstd, rows, D,
-                       (float)(1.0 / (double)D), nb, block.passes, res, dx, partial, upper, block.upper);
+                       (float)(1.0 / (double)D), nb, block.passes, res, dx, out_g, out_b, upper, block.upper);
         }
       });
     });
   });
   if (rc != DET_OK) return rc;
-  if (cols)
+  if (cols && !direct)
     launch_after(k_ln_cols, dim3((D + 31) / 32, 2), 1024, 0, st, (const float*)partial, nb, D, dgamma, dbeta);
   DET_CHECK_LAUNCH();
   return DET_OK;

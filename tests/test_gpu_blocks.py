@@ -93,6 +93,26 @@ def test_layernorm_many_rows(det, rows, D):
     same(host(db), odb, "dbeta")
 
 
+@pytest.mark.parametrize("rows,D", [(1, 64), (4, 2048), (3, 1003), (2, 4096), (1, 8192)])
+def test_layernorm_few_rows(det, rows, D):
+    """One block of rows: gain and shift come from the first kernel, or from the second where their place is not aligned; a row alone is flushed."""
+    x, dy, g = _rows((rows, D), 33, True), _rows((rows, D), 36, True), _rows(D, 34, True, 1.0, 0.1)
+    dy[0, :D // 2] = 0x0003                                         # subnormal
+    mean, rstd = synth.normal_f32(rows, 0.1, seed=37, tid=1), np.abs(synth.normal_f32(rows, 1.0, seed=37, tid=2)) + F(0.5)
+    odx, odg, odb = oracle.layernorm_bwd(dy, x, g, mean, rstd, bf=True)
+    for off in (0, 1):
+        for which in ((1, 1), (1, 0), (0, 1)):
+            dx, buf = empty((rows, D), np.uint16), [dev(np.full(D + 2, 7.0, F)) for _ in range(2)]
+            dg, db = (b[off:off + D] if w else None for b, w in zip(buf, which))
+            det.det_layernorm_bwd(det.DET_BF16, dev(dy), dev(x), dev(g), dev(mean), dev(rstd), rows, D, dx, dg, db, ws(det.det_layernorm_bwd_ws_bytes(rows, D)))
+            _sync()
+            same(host(dx, np.uint16), odx, "dx")
+            for b, w, want, what in zip(buf, which, (odg, odb), ("dgamma", "dbeta")):
+                if w:
+                    same(host(b[off:off + D]), want, what)
+                assert (b[:off] == 7).all() and (b[off + D * w:] == 7).all()
+
+
 @pytest.mark.parametrize("rows,D", [(113001, 8), (15001, 200), (5001, 1024), (2399, 2056)])
 def test_layernorm_many_rows_binary32(det, rows, D):
     x, dy, g = _rows((rows, D), 23, False), _rows((rows, D), 26, False), _rows(D, 24, False, 1.0, 0.1)
