@@ -639,9 +639,9 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
 }
 
 // Rows of a block of the backward pass, whose nodes go to memory for the second kernel: more of them while the CTA with the most has not much more to do (all
-// that are on the GPU at once share the blocks).  Fewer nodes are less to write and to read: 8192 x 2048 with blocks of 8 and 32 rows 36.1
-// and 35.3 us, 4096 x 4096 with 2 and 16 passes 42.9 and 37.7.
-constexpr int LN_PASSES = 16, LN_SLACK = 6;                // passes of a block at most; of the busiest CTA, to those with blocks of one, times 4
+// that are on the GPU at once share the blocks).  Fewer nodes are less to write and to read: 8192 x 2048 with blocks of 8 and 32 rows 36.5
+// and 34.0 us, 8192 x 4096 with 2 and 16 passes 82 and 68; but 12000 x 2048 with 4 passes 49 and with 8, where the busiest CTA has half as much again, 59.
+constexpr int LN_PASSES = 16, LN_SLACK = 5;                // passes of a block at most; of the busiest CTA, to those with blocks of one, times 4
 struct LnBlock {
   int passes, rows, levels, upper, ctas;                 // passes of a block, its rows; levels of waiting nodes, how many in the workspace; CTAs at once
   size_t level;                                          // bytes of a CTA's waiting nodes of a level
