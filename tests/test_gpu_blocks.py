@@ -375,7 +375,8 @@ def _linrec_check(det, B, S, D, every=0, ends=True, pad=0, gv=None, dy=None, fl=
     (1, 64, 64, 0, True, 0), (3, 65, 34, 0, True, 0), (1, 128, 256, 0, True, 0), (2, 129, 70, 1, True, 2), (1, 500, 100, 40, True, 0),
     (2, 513, 64, 0, True, 0), (1, 1000, 200, 0, False, 0), (1, 4096, 64, 100, True, 0), (4, 333, 512, 0, True, 0), (1, 5000, 30, 0, True, 6), (2, 1025, 4, 0, True, 0), (1, 1024, 2, 0, True, 0), (1, 33000, 6, 300, True, 0), (2, 31, 18, 0, True, 0),
     (1, 96, 32, 0, True, 0), (3, 127, 16, 4, True, 0), (1, 2177, 512, 0, True, 0), (1, 700, 1500, 0, True, 0),
-    (40, 300, 128, 0, True, 0), (130, 260, 64, 9, True, 0), (1, 20000, 16, 0, True, 0), (500, 70, 64, 0, False, 0)])
+    (40, 300, 128, 0, True, 0), (130, 260, 64, 9, True, 0), (1, 20000, 16, 0, True, 0), (500, 70, 64, 0, False, 0),
+    (400, 260, 32, 9, True, 0), (300, 140, 34, 5, True, 2), (310, 136, 40, 0, True, 0)])
 def test_linrec(det, B, S, D, every, ends, pad):
     """Lengths around chunks, blocks and spans, every number of CTAs in a cluster, either number of warps along a sequence, cuts, strides."""
     _linrec_check(det, B, S, D, every, ends, pad)
