@@ -15,7 +15,8 @@
 // from shared memory, a group in each half.
 // Where there are few strips the CTAs of a cluster take adjacent spans: they send each other the span maps, by stores that complete a transaction
 // barrier of the receiver, and one warp of each applies them in turn.  So every value is read once and written once however long a sequence is and however
-// few there are, with no workspace.  A warp's raw values of the next round come in by asynchronous copies as soon as those of this round are in registers.
+// few there are, with no workspace.  A warp's raw values of the next round come in by asynchronous copies as soon as those of this round are in registers
+// (in a cluster, as soon as its maps are sent).
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
