@@ -48,6 +48,10 @@ int det_test_attn_fwd(int rows, const det_bf16* q, const det_bf16* k, const det_
 /* The form that det_attn_fwd takes on this device for that many heads (of all sequences together); 0 for sizes that it refuses. */
 int det_test_attn_rows(int heads, int S, int window);
 
+/* How the CTAs of det_layernorm_fwd walk over the rows on a GPU of `sms` SMs, worked out on the host with the kernel's own steps: seen[0] passes of
+ * all CTAs, seen[1] of the one with the most, seen[2] and seen[3] the lowest and the highest row that a pass starts at. */
+int det_test_layernorm_walk(int io, int rows, int D, int sms, long long seen[4]);
+
 #ifdef __cplusplus
 }
 #endif

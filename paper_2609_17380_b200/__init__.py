@@ -68,7 +68,7 @@ _SIGNATURES = {
     "det_tensor_hash_batch_ws_bytes": "zpi", "det_tensor_hash_batch": "ippippzp", "det_test_prim": "iipppzp",
     "det_residual_rmsnorm_fwd": "ipppiifpppppp", "det_rmsnorm_bwd_residual": "ippppiippppzp", "det_test_igemm_tn": "ippiiipipp", "det_test_lmhead_tile": "iiippiiipip",
     "det_test_wait_timeout": "iplp", "det_test_wait_warp": "iplp", "det_test_attn_fwd": "iipppiiiiiipipppp",
-    "det_test_attn_rows": "iiii", "det_test_lmhead_pick": "iiii",
+    "det_test_attn_rows": "iiii", "det_test_lmhead_pick": "iiii", "det_test_layernorm_walk": "iiiiip",
     "det_layernorm_fwd": "iipppiifpppp", "det_residual_layernorm_fwd": "ippppiifppppppppp", "det_layernorm_bwd_ws_bytes": "zii",
     "det_layernorm_bwd": "iipppppiippppzp", "det_layernorm_bwd_residual": "ipppppiipppppzp", "det_layernorm_bwd_act8": "ippppppiipppppzp",
     "det_act8_exp_bytes": "zii", "det_act8_pack": "iipiiippp", "det_act8_unpack": "iippiipip",
@@ -467,6 +467,13 @@ def det_test_attn_rows(heads, S, window=0):
 
 def det_test_lmhead_pick(M, V, K):
     return load().det_test_lmhead_pick(M, V, K)
+
+
+def det_test_layernorm_walk(io, rows, D, sms):
+    """Passes of all CTAs, passes of the one with the most, lowest and highest row that a pass starts at."""
+    seen = (C.c_longlong * 4)()
+    _check("det_test_layernorm_walk", load().det_test_layernorm_walk(io, rows, D, sms, seen))
+    return tuple(seen)
 
 
 # ---- gradient accumulation, AdamW, hash ---------------------------------------------------------------------------

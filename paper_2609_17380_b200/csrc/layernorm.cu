@@ -9,6 +9,7 @@
 
 #include <algorithm>
 
+#include "../../include/det_test.h"
 #include "common.cuh"
 #include "internal.h"
 #include "rows.cuh"
@@ -23,6 +24,15 @@ struct LnShape {
   static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = BF && VEC && WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
   static constexpr bool AHEAD_ROWS = BF && VEC;          // binary32 rows: a CTA for every two rows and loads in place (27 us for 8192 x 2048, 36 ahead)
   static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
+};
+// The rows that a CTA of the forward pass works on: GROUPS * ROWS of them from `base` on, then, with rows on their way ahead, those `stride` behind.  That
+// stays below LN_ROWS and a few thousand.  Without, there is a CTA for every such piece: the next would be `rows` behind, past 2^31 where there are more than 2^30.
+template <class S>
+struct LnWalk {
+  static constexpr int PIECE = S::GROUPS * S::ROWS;
+  int base, stride;
+  __host__ __device__ __forceinline__ LnWalk(unsigned cta, unsigned ctas) : base((int)cta * PIECE), stride(S::AHEAD_ROWS ? (int)ctas * PIECE : 0) {}
+  __host__ __device__ __forceinline__ void next(int rows) { base = S::AHEAD_ROWS ? base + stride : rows; }
 };
 enum { LN_F32 = 0, LN_BF16 = 1, LN_ACT8 = 2 };   // what x is backward: as dy, or the 8-bit checkpoint (dy bf16)
 template <int WPR, int KIND, bool VEC>
@@ -180,7 +190,7 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
   const bool full = D - warp * 256 >= 256 || D <= warp * 256;     // the warp's leaf is whole, or there is none
   const int leaves = (D + 255) >> 8;
   const float2 one = same2(c_one);
-  const int stride = gridDim.x * S::GROUPS * R;
+  LnWalk<S> walk(blockIdx.x, gridDim.x);
   auto fetch = [&](int first, int slot) {
     if (S::AHEAD_ROWS) {
       if (first < rows) {
@@ -196,9 +206,9 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
       fetch_close();
     }
   };
-  int first = (blockIdx.x * S::GROUPS + grp) * R;
+  int first = walk.base + grp * R;
 #pragma unroll
-  for (int k = 0; k < S::AHEAD - 1; ++k) fetch(first + k * stride, k);
+  for (int k = 0; k < S::AHEAD - 1; ++k) fetch(first + k * walk.stride, k);
   float g[8], b[8];
   const int w0 = warp * 256, left = D - w0;              // the warp's first column, how many are left from there
   auto take = [&](const void* p, float v[8]) {
@@ -214,11 +224,11 @@ __global__ void __launch_bounds__(LnShape<WPR, BF, VEC>::THREADS, LnShape<WPR, B
   if (beta) take(beta, b);
   const float inv_q = (BF && VEC && qy) ? fdiv(1.0f, s_q[0]) : 0.0f;
   // all groups of the CTA make the same passes
-  for (int base = blockIdx.x * S::GROUPS * R, slot = 0; base < rows; base += stride, first += stride) {
+  for (int slot = 0; walk.base < rows; walk.next(rows), first += walk.stride) {
     float v[R][8];
     if (S::AHEAD_ROWS) {
       const int next = slot == 0 ? S::AHEAD - 1 : slot - 1;
-      fetch(first + (S::AHEAD - 1) * stride, next);
+      fetch(first + (S::AHEAD - 1) * walk.stride, next);
       fetch_wait<S::AHEAD - 1>();
     }
     const char* place = smem + slot * R * BYTES;
@@ -604,10 +614,11 @@ static void with_wpr(int D, F f) {
 template <class F>
 static void with_bool(bool b, F f) { if (b) f(std::true_type()); else f(std::false_type()); }
 
-// CTAs for `blocks` pieces of work: all that are on the GPU at once, `per_sm` on an SM
-static dim3 ln_grid(long long blocks, int per_sm) {
-  const long long most = (long long)per_sm * dev_sm_count();
-  return dim3((unsigned)(blocks < most || most <= 0 ? blocks : most));
+// CTAs of the forward pass: with rows on their way ahead all that are on a GPU of `sms` SMs at once, else one for every piece of rows
+template <class S>
+static unsigned ln_ctas(int rows, int sms) {
+  const long long pieces = ((long long)rows + LnWalk<S>::PIECE - 1) / LnWalk<S>::PIECE, most = (long long)S::CTAS * std::max(sms, 1);
+  return (unsigned)(S::AHEAD_ROWS ? std::min(pieces, most) : pieces);
 }
 static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, const void* beta, int rows, int D, float eps, void* sum,
                   void* y, float* mean, float* rstd, const float* s_q, int8_t* qy, int8_t* q8, uint8_t* e8, cudaStream_t st) {
@@ -620,14 +631,13 @@ static int ln_fwd(bool bf, const void* x, const void* res, const void* gamma, co
           constexpr bool BF = decltype(is_bf)::value, VEC = decltype(is_vec)::value, RES = decltype(is_res)::value;
           if constexpr (BF || !RES) {
             using S = LnShape<W, BF, VEC>;
-            const long long per = S::GROUPS * S::ROWS, blocks = (rows + per - 1) / per;
             const size_t smem = S::AHEAD_ROWS ? (size_t)S::AHEAD * S::ROWS * S::THREADS * 8 * (BF ? 2 : 4) * (RES ? 2 : 1) : (VEC ? 0 : (size_t)S::THREADS * 32);
             auto kern = k_ln_fwd<BF, W, VEC, RES>;
             static DevOnce once;
             if (smem > 40 * 1024) rc = dev_ensure_smem(once, (const void*)kern, smem);
             if (rc != DET_OK) return;
-            launch_after(kern, S::AHEAD_ROWS ? ln_grid(blocks, S::CTAS) : dim3((unsigned)blocks), S::THREADS, smem, st, x, res, gamma, beta, rows, D, eps,
-                         (float)(1.0 / (double)D), sum, y, mean, rstd, s_q, qy, q8, e8);
+            launch_after(kern, dim3(ln_ctas<S>(rows, dev_sm_count())), S::THREADS, smem, st, x, res, gamma, beta, rows, D, eps, (float)(1.0 / (double)D), sum, y, mean,
+                         rstd, s_q, qy, q8, e8);
           }
         });
       });
@@ -729,6 +739,31 @@ extern "C" int det_layernorm_fwd(int io, const void* x, const void* gamma, const
   if (!elem_aligned(x, D, el) || !elem_aligned(y, D, el) || !elem_aligned(gamma, D, el) || !elem_aligned(beta, D, el)) return DET_ERR_ALIGN;
   if (rows == 0) return DET_OK;
   return ln_fwd(io == DET_BF16, x, nullptr, gamma, beta, rows, D, eps, nullptr, y, mean, rstd, nullptr, nullptr, nullptr, nullptr, (cudaStream_t)stream);
+}
+
+extern "C" int det_test_layernorm_walk(int io, int rows, int D, int sms, long long seen[4]) {
+  if (rows <= 0 || rows > LN_ROWS || D <= 0 || D > 8192 || sms <= 0 || !seen || (io != DET_F32 && io != DET_BF16)) return DET_ERR_ARG;
+  with_wpr(D, [&](auto wpr) {
+    with_bool(io == DET_BF16, [&](auto is_bf) {
+      with_bool(D % 8 == 0, [&](auto is_vec) {
+        using S = LnShape<decltype(wpr)::value, decltype(is_bf)::value, decltype(is_vec)::value>;
+        const unsigned ctas = ln_ctas<S>(rows, sms);
+        seen[0] = seen[1] = 0;
+        seen[2] = rows;
+        seen[3] = -1;
+        for (unsigned cta = 0; cta < ctas; ++cta) {
+          long long passes = 0;
+          for (LnWalk<S> w(cta, ctas); w.base < rows; w.next(rows), ++passes) {
+            seen[2] = std::min<long long>(seen[2], w.base);
+            seen[3] = std::max<long long>(seen[3], w.base);
+          }
+          seen[0] += passes;
+          seen[1] = std::max(seen[1], passes);
+        }
+      });
+    });
+  });
+  return DET_OK;
 }
 
 extern "C" int det_residual_layernorm_fwd(const det_bf16* a, const det_bf16* b, const det_bf16* gamma, const det_bf16* beta, int rows, int D,
