@@ -1,11 +1,11 @@
-"""Layer norm of more than 2^30 rows on the GPU."""
+"""Layer norm of many rows on the GPU: more than 2^30 of them, and forward passes in which every CTA walks over several pieces of rows."""
 import numpy as np
 import pytest
 
 import oracle
 import synth
 from gpu_util import dev, empty, host, ws
-from test_gpu_blocks import _rows, _sync
+from test_gpu_blocks import _rows, _sync, same
 
 pytestmark = pytest.mark.gpu
 F = np.float32
@@ -79,3 +79,52 @@ def test_backward_of_more_rows_than_two_to_the_thirty(det):
             total = F(2.0 ** k) if total is None else F(2.0 ** k) + total
     assert host(db).tolist() == [total, total]
     assert np.isfinite(host(dg)).all()
+
+
+# rows for more passes of a CTA than are on their way ahead, the last one ragged, for every number of warps a row
+WALK = [(60001, 256), (60003, 40), (29001, 512), (15001, 1000), (8191, 2048), (3001, 4096), (1501, 8192), (1499, 8184)]
+
+
+def _walks(det, rows, D):
+    passes, most, _, _ = det.det_test_layernorm_walk(det.DET_BF16, rows, D, det.det_device_sm_count())
+    return passes > 4 and most >= 5
+
+
+@pytest.mark.parametrize("rows,D", WALK)
+def test_forward_walk(det, rows, D):
+    assert _walks(det, rows, D)
+    x, g, b = _rows((rows, D), 3, True, 0.5), _rows(D, 4, True, 1.0, 0.1), _rows(D, 5, True, 0.0, 0.3)
+    y, mean, rstd = dev(np.full((rows + 2, D), 0x7ABC, np.uint16)), dev(np.full(rows + 2, 7.0, F)), dev(np.full(rows + 2, 7.0, F))
+    det.det_layernorm_fwd(det.DET_BF16, dev(x), dev(g), dev(b), rows, D, 1e-6, y, mean, rstd)
+    _sync()
+    oy, om, ors = oracle.layernorm_fwd(x, g, b, 1e-6, bf=True)
+    same(host(mean)[:rows], om, "mean")
+    same(host(rstd)[:rows], ors, "rstd")
+    got = host(y, np.uint16)
+    same(got[:rows], oy, "y")
+    assert (got[rows:] == 0x7ABC).all() and (host(mean)[rows:] == 7).all() and (host(rstd)[rows:] == 7).all()      # behind the last row
+
+
+@pytest.mark.parametrize("rows,D", WALK)
+def test_forward_walk_with_the_residual_stream(det, rows, D):
+    """The sum, the codes of the next linear and the checkpoint, with the sum and without a second summand."""
+    assert _walks(det, rows, D)
+    a, b = _rows((rows, D), 43, True), _rows((rows, D), 44, True)
+    g, s = _rows(D, 45, True, 1.0, 0.1), _rows(D, 46, True, 0.0, 0.2)
+    sq = np.array([0.021], F)
+    for other in (b, None):
+        osum = a if other is None else oracle.residual_add(a, other)
+        oy, om, ors = oracle.layernorm_fwd(osum, g, s, 1e-6, bf=True)
+        oq, oe = oracle.act8_pack(osum)
+        total, y, mean, rstd = empty((rows, D), np.uint16), empty((rows, D), np.uint16), empty((rows,), F), empty((rows,), F)
+        qy, q8, e8 = empty((rows, D), np.int8), empty((rows, D), np.int8), empty((rows, (D + 31) // 32), np.uint8)
+        det.det_residual_layernorm_fwd(dev(a), None if other is None else dev(other), dev(g), dev(s), rows, D, 1e-6, total, y, mean, rstd, dev(sq), qy, q8, e8)
+        _sync()
+        if other is not None:
+            same(host(total, np.uint16), osum, "sum")
+        same(host(y, np.uint16), oy, "y")
+        same(host(mean), om, "mean")
+        same(host(rstd), ors, "rstd")
+        same(host(qy), oracle.lsq_quantize(oy, sq, False), "codes of y")
+        same(host(q8), oq, "checkpoint codes")
+        same(host(e8), oe, "checkpoint steps")
