@@ -1097,11 +1097,13 @@ static void lr_gate(float g, float *f, float *z) {
   *f = f2u(g) >> 31 ? m : M;
   *z = f2u(g) >> 31 ? M : m;
 }
-/* Some rows are the map s -> A s + H; one that forgets everything lets nothing in, not even a NaN. */
+/* Some rows are the map s -> A s + H.  Gates are never below +0; a row with a cut has A = -0, a sign that every product keeps, and lets nothing in, not
+ * even a NaN.  A product of gates that underflowed is +0: an infinity or a NaN goes on through it as it does through the rows one by one. */
 typedef struct { float A, H; } lr_map;
-static float lr_apply(lr_map m, float s) { return m.A == 0.0f ? m.H : fadd(fmul(m.A, s), m.H); }
+static int lr_cut(lr_map m) { return f2u(m.A) == 0x80000000u; }
+static float lr_apply(lr_map m, float s) { return lr_cut(m) ? m.H : fadd(fmul(m.A, s), m.H); }
 static lr_map lr_then(lr_map first, lr_map then) { /* first, then `then` */
-  lr_map r = {then.A == 0.0f ? 0.0f : fmul(first.A, then.A), lr_apply(then, first.H)};
+  lr_map r = {lr_cut(then) ? -0.0f : fmul(first.A, then.A), lr_apply(then, first.H)};
   return r;
 }
 /* What comes into every chunk, in the order of the pass, from the maps of the n chunks and what comes into the first one; returns what
@@ -1149,7 +1151,7 @@ void orc_linrec_fwd(const bf16_t *g, const bf16_t *v, int ldi, int B, int S, int
       for (int t = c * LR_CHUNK; t < S && t < (c + 1) * LR_CHUNK; ++t) {
         int cut = fl && fl[t], first = t == c * LR_CHUNK;
         m[c].H = cut || first ? u[t] : fadd(fmul(f[t], m[c].H), u[t]);
-        m[c].A = cut ? 0.0f : (first ? f[t] : fmul(m[c].A, f[t]));
+        m[c].A = cut ? -0.0f : (first ? f[t] : fmul(m[c].A, f[t]));
       }
     float last = lr_chain(m, n, h0 ? h0[i] : 0.0f, in);
     for (int c = 0; c < n; ++c) {
@@ -1190,7 +1192,7 @@ void orc_linrec_bwd(const bf16_t *dy, int ldy, const bf16_t *g, const bf16_t *v,
         int cut = fl && fl[t], first = t == end - 1;
         float d = bf2f(dy[((size_t)b * S + t) * ldy + j]);
         m[o].H = cut ? 0.0f : fmul(f[t], first ? d : fadd(d, m[o].H));
-        m[o].A = cut ? 0.0f : (first ? f[t] : fmul(f[t], m[o].A));
+        m[o].A = cut ? -0.0f : (first ? f[t] : fmul(f[t], m[o].A));
       }
     }
     float last = lr_chain(m, n, dhT ? dhT[i] : 0.0f, in);

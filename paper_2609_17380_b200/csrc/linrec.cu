@@ -8,7 +8,8 @@
 // 2 groups, from its first row on (backward from its last).  A chunk's map is composed row by row, a block's of its chunks, a group's of its blocks one after
 // the other, a span's of its groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came into that; what comes
 // into a block or a chunk is the map of all those before it, in its group or block, applied to what comes into that; inside a chunk the recurrence is
-// walked row by row.  A map with A = 0 lets nothing in, not even a NaN.
+// walked row by row.  Gates are never below +0.  A row with a cut has A = -0, a sign that every product keeps: such a map lets nothing in, not even a NaN.  A
+// product of gates that underflowed is +0, and what is not finite goes on through it as it does through the rows one by one.
 //
 // A warp has a block of 32 channels: sixteen lanes a chunk, two channels a lane, so that a row's piece is 64 bytes (of 32 bytes the L1 cache was 64 % busy
 // with finding lines); the maps of its two chunks meet in a shuffle.  Eight warps have the blocks of a span, and every warp composes the block maps again
@@ -85,15 +86,17 @@ struct LrMap { float2 a, h; };                           // s -> a s + h for two
 // Pairs of channels in packed arithmetic, no product fused with a sum: `one` is the factor 1 that add2 needs.
 __device__ __forceinline__ float2 lr_axpy(float2 a, float2 s, float2 h, float2 one) { return add2(mul2(a, s), h, one); }
 __device__ __forceinline__ float2 lr_sub(float2 a, float2 b) { return fma2(b, same2(-1.0f), a); }
+// a map with a cut among its rows
+__device__ __forceinline__ bool lr_closed(float a) { return __float_as_uint(a) == 0x80000000u; }
 __device__ __forceinline__ float2 lr_apply(const LrMap& m, float2 s, float2 one) {
   const float2 r = lr_axpy(m.a, s, m.h, one);
-  return make_float2(m.a.x == 0.0f ? m.h.x : r.x, m.a.y == 0.0f ? m.h.y : r.y);
+  return make_float2(lr_closed(m.a.x) ? m.h.x : r.x, lr_closed(m.a.y) ? m.h.y : r.y);
 }
 // the map `first`, then `then`
 __device__ __forceinline__ LrMap lr_compose(const LrMap& first, const LrMap& then, float2 one) {
   const float2 a = mul2(first.a, then.a), h = lr_axpy(then.a, first.h, then.h, one);
-  const bool x = then.a.x == 0.0f, y = then.a.y == 0.0f;
-  return LrMap{make_float2(x ? 0.0f : a.x, y ? 0.0f : a.y), make_float2(x ? then.h.x : h.x, y ? then.h.y : h.y)};
+  const bool x = lr_closed(then.a.x), y = lr_closed(then.a.y);
+  return LrMap{make_float2(x ? -0.0f : a.x, y ? -0.0f : a.y), make_float2(x ? then.h.x : h.x, y ? then.h.y : h.y)};
 }
 __device__ __forceinline__ float4 lr_pack(const LrMap& m) { return make_float4(m.a.x, m.a.y, m.h.x, m.h.y); }
 __device__ __forceinline__ LrMap lr_unpack(float4 v) { return LrMap{make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
@@ -105,13 +108,16 @@ __device__ __forceinline__ float2 lr_step(float2 f, float2 u, float2 h, bool cut
 __device__ __forceinline__ void lr_extend(LrMap& m, bool first, float2 f, float2 u, bool cut, float2 one) {
   m.h = first ? u : lr_step(f, u, m.h, cut, one);
   m.a = first ? f : mul2(m.a, f);
-  if (cut) m.a = same2(0.0f);
+  if (cut) m.a = same2(-0.0f);
 }
 // the same from the last row to the first, of the gradient
 __device__ __forceinline__ void lr_extend_back(LrMap& m, bool first, float2 f, float2 d, bool cut, float2 one) {
   m.h = mul2(f, first ? d : add2(m.h, d, one));
   m.a = first ? f : mul2(m.a, f);
-  if (cut) m.a = m.h = same2(0.0f);
+  if (cut) {
+    m.a = same2(-0.0f);
+    m.h = same2(0.0f);
+  }
 }
 // dg of a row: (dh (h_{t-1} - v)) (f z)
 __device__ __forceinline__ uint32_t lr_dg(float2 d, float2 diff, float2 f, float2 z) {
@@ -328,12 +334,12 @@ __device__ __forceinline__ float2 lr_hand_over(LrShared<NS, JOINED>& sh, const L
 #pragma unroll
         for (int j = 0; j < BATCH; ++j) {
           in[(i + j) * LR_CH] = c;
-          c = m[j][0] == 0.0f ? m[j][1] : fadd(fmul(m[j][0], c), m[j][1]);
+          c = lr_closed(m[j][0]) ? m[j][1] : fadd(fmul(m[j][0], c), m[j][1]);
         }
       }
       for (; i < spans; ++i) {
         in[i * LR_CH] = c;
-        c = maps[i * 64] == 0.0f ? maps[i * 64 + 2] : fadd(fmul(maps[i * 64], c), maps[i * 64 + 2]);
+        c = lr_closed(maps[i * 64]) ? maps[i * 64 + 2] : fadd(fmul(maps[i * 64], c), maps[i * 64 + 2]);
       }
       in[LR_MAXC * LR_CH] = c;
     }
