@@ -4,6 +4,7 @@ forward/backward in mesh order, gradients folded in the cluster's order, clip, A
 This module only owns device memory (torch tensors) and the order of the calls; every arithmetic step runs
 inside libdet.  It never imports the oracle.
 """
+import json
 import math
 from dataclasses import dataclass, field
 
@@ -287,13 +288,27 @@ class Replay:
                     dst[o:o + c] = (torch.randn(c, generator=gen, device=self.dev) * 0.02).to(torch.bfloat16).view(I16)
 
     # ---- state dump: everything a later step depends on (Appendix B: replay from a saved state) ------------------
+    def _layout(self):
+        """What the numbers of the flat buffers mean: the parameters in their order, the kind of norm, the layers whose w_qkv is gate and value (which may
+        have the shape of an attention layer's).  How activations are kept between the passes is no part of it."""
+        cfg = self.cfg
+        return json.dumps(dict(params=[(name, [int(n) for n in shape], kind) for name, shape, kind in self.specs], norm=cfg.norm,
+                               recurrent=sorted({int(l) for l in cfg.recurrent})))
+
     def save_state(self, path):
-        """Parameters (bf16 bits), activation steps, both Adam moments and the step counter, as one .npz file."""
+        """Parameters (bf16 bits), activation steps, both Adam moments and the step counter, as one .npz file, with what lies where."""
         np.savez(path, pbf=self.pbf.cpu().numpy(), sx=self.sx.cpu().numpy(), m=self.m.cpu().numpy(), v=self.v.cpu().numpy(),
-                 step=np.array([self.cfg.step], np.int64))
+                 step=np.array([self.cfg.step], np.int64), layout=np.array(self._layout()))
 
     def load_state(self, path):
+        """Takes the files of save_state of a configuration with the same parameters, else ValueError.  A file that does not say what lies where is taken
+        for blocks without recurrent layers, by the lengths alone."""
         z = np.load(path)
+        if "layout" in z.files:
+            if str(z["layout"]) != self._layout():
+                raise ValueError("state file does not match this configuration: other parameters, norm or recurrent layers")
+        elif self.cfg.recurrent:
+            raise ValueError("state file does not say which layers are recurrent")
         for name, dst in (("pbf", self.pbf), ("sx", self.sx), ("m", self.m), ("v", self.v)):
             a = z[name]
             if a.shape != tuple(dst.shape):
