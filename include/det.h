@@ -219,11 +219,12 @@ int det_swiglu_bwd_act8(const det_bf16* dh, const int8_t* q8, const uint8_t* e8,
  * a time included).  flags uint8 [B, S] (may be NULL): a row whose flag is set starts from zero instead of h_{t-1}; nothing before it, a NaN
  * included, reaches it, and no gradient goes back across it.  g, v bf16 (row b*S + t at ld*(b*S + t); gate and value may be the two halves of one
  * projection), y with ld_y.
- * Some rows are the map s -> A s + H.  Chunks of 8 rows, blocks of 2 chunks, groups of 4 blocks and spans of 2 groups are counted from the first row
- * (backward from the last).  A chunk's map is composed row by row, a block's of its chunks, a group's of its blocks one after the other, a span's of its
- * groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came into that; what comes into a block or a chunk
- * the map of all those before it, in its group or block, applied to what comes into that; h is walked row by row from there.  A row with a cut
- * has A = -0, which stays so in every product, and that lets nothing in; a product of gates that underflowed is +0, and lets an infinity or a NaN go on.
+ * Some rows are the map s -> A s + H.  Chunks are 8 rows, from the first row on (the last one may be shorter); blocks of 2 chunks, groups of 4 blocks and
+ * spans of 2 groups are counted from the first chunk (backward from the last).  A chunk's map is composed row by row, a block's of its chunks, a group's of
+ * its blocks one after the other, a span's of its groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came
+ * into that; what comes into a block or a chunk the map of all those before it, in its group or block, applied to what comes into that; h is walked row by
+ * row from there.  A row with a cut has A = -0, which stays so in every product, and that lets nothing in; a product of gates that underflowed is +0, and
+ * lets an infinity or a NaN go on.
  * states f32 [B, ceil(S/8), D] (det_linrec_state_floats; NULL: not kept) are the states in front of the chunks, for the backward pass.
  * D, ld, ld_y, ld_d even, S <= 2^30, B * ceil(D/32) <= 2^26; bf16 pointers 4-byte, f32 pointers 8-byte aligned.  S = 0: hT = h0, dh0 = dhT.  Outputs overlap no
  * input but as said.  status_dev (may be NULL) receives DET_DEV_TIMEOUT if a bounded wait of one CTA for another runs out. */

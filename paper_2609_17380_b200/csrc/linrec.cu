@@ -4,8 +4,8 @@
 // f and z come from one exponential: with e = exp(-|g|) the smaller of them is m = e / (1 + e) and the larger 1 - m, so neither
 // loses digits where the gate saturates.
 //
-// Order of the sums.  Some rows are the map s -> A s + H.  A sequence is cut into chunks of 8 rows, blocks of 2 chunks, groups of 4 blocks and spans of
-// 2 groups, from its first row on (backward from its last).  A chunk's map is composed row by row, a block's of its chunks, a group's of its blocks one after
+// Order of the sums.  Some rows are the map s -> A s + H.  A sequence is cut into chunks of 8 rows, from its first row on; blocks of 2 chunks, groups of
+// 4 blocks and spans of 2 groups are counted from its first chunk on (backward from its last).  A chunk's map is composed row by row, a block's of its chunks, a group's of its blocks one after
 // the other, a span's of its groups.  What comes into a span or a group is the map of the one before, in its span, applied to what came into that; what comes
 // into a block or a chunk is the map of all those before it, in its group or block, applied to what comes into that; inside a chunk the recurrence is
 // walked row by row.  Gates are never below +0.  A row with a cut has A = -0, a sign that every product keeps: such a map lets nothing in, not even a NaN.  A
