@@ -194,11 +194,11 @@ int det_layernorm_bwd_act8(const det_bf16* dy, const int8_t* q8, const uint8_t* 
                            size_t ws_bytes, void* stream);
 
 /* ---- activations in 8 bits between the forward and the backward pass ------------------------------------------
- * The replay runs every virtual rank on one GPU, so what a micro-batch keeps for its backward pass bounds its size.  32 adjacent values of
- * a row (the last group of a row may be shorter) share a step 2^E, the smallest power of two with max|v| <= 127 * 2^E, at least
- * 2^-126: code = rne(v * 2^-E) in [-127, 127], value = code * 2^E.  Every product is exact, so a value is off by at most half a step and comes
- * back exactly in bf16 as in f32.  q8 int8 [rows, D], e8 uint8 [rows, ceil(D/32)] = E + 127; a group with an infinity or a NaN has
- * e8 = 255 and comes back as infinities (code +-127) and NaNs (code 0).
+ * What a micro-batch keeps for its backward pass takes half the bytes of bf16, and the gradients are those of the kept values: for runs that were
+ * trained so, with larger micro-batches for it; a run trained on whole activations is not replayed with them.  32 adjacent values of a row (the last
+ * group of a row may be shorter) share a step 2^E, the smallest power of two with max|v| <= 127 * 2^E, at least 2^-126: code = rne(v * 2^-E) in [-127,
+ * 127], value = code * 2^E.  Every product is exact, so a value is off by at most half a step and comes back exactly in bf16 as in f32.  q8 int8 [rows,
+ * D], e8 uint8 [rows, ceil(D/32)] = E + 127; a group with an infinity or a NaN has e8 = 255 and comes back as infinities (code +-127) and NaNs (code 0).
  * io: dtype of x and y; their rows are ld elements apart (ld >= D); any D, any alignment to the element; fewer than 2^28 groups. */
 size_t det_act8_exp_bytes(int rows, int D); /* bytes of e8 */
 int det_act8_pack(int io, const void* x, int ld, int rows, int D, int8_t* q8, uint8_t* e8, void* stream);

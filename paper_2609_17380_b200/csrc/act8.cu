@@ -129,8 +129,8 @@ __global__ void __launch_bounds__(256) k_a8_unpack_any(const int8_t* __restrict_
 // ---- SwiGLU: gu [rows, 2F] = (gate | up), F a multiple of 32, so no group holds both -----------------------
 // The gate is a bf16 either way, so its sigmoid has few values: 33 exponents of magnitude (below 2^-26 it is 1/2, from 128 on 1 or 0) of 128 fractions and two
 // signs.  They are evaluated by the compiler, with the steps of the formula, and looked up in shared memory: with an exponential and a division for every
-// value the three kernels took 160, 133 and 152 us for 8192 x 8192, bound by the arithmetic; now 92, 76 and 92, where the bytes alone would take 83, 42 and
-// 83 at the measured copy's rate.
+// value the three kernels took 160, 133 and 152 us for 8192 x 8192, bound by the arithmetic; now 92, 76 and 92 (each over and over; the three in turn on the same tensors 284), where the
+// bytes alone would take 83, 42 and 83 at the measured copy's rate.
 constexpr int SG_LOW = 0x3280, SG_TOP = 0x4300, SG_TAB = (SG_TOP - SG_LOW + 1 + 255) / 256 * 256;
 struct __align__(16) SgTable { float v[2 * SG_TAB]; };     // of positive gates, of negative ones
 constexpr float sg_at(int bits, bool negative) {

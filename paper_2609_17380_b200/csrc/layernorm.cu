@@ -22,7 +22,7 @@ namespace det {
 template <int WPR, bool BF, bool VEC>
 struct LnShape {
   static constexpr int GROUPS = WPR < 8 ? 8 / WPR : 1, THREADS = 32 * WPR * GROUPS, ROWS = BF && VEC && WPR <= 8 ? 4 : 2, AHEAD = ROWS == 4 ? 2 : 3;
-  static constexpr bool AHEAD_ROWS = BF && VEC;          // binary32 rows: a CTA for every two rows and loads in place (27 us for 8192 x 2048, 36 ahead)
+  static constexpr bool AHEAD_ROWS = BF && VEC;          // binary32 rows: a CTA for every two rows and loads in place (25.5 us for 8192 x 2048, 36 ahead)
   static constexpr int CTAS = WPR == 32 ? 1 : (WPR == 16 ? 2 : (ROWS == 4 ? 3 : 4));
 };
 // The rows that a CTA of the forward pass works on: GROUPS * ROWS of them from `base` on, then, with rows on their way ahead, those `stride` behind.  That

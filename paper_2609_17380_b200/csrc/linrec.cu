@@ -375,10 +375,11 @@ __device__ __forceinline__ void lr_close() {
   cluster_wait();
 }
 
-// Measured on a B200 (its copy moves 6.53 TB/s): 4 x 2048 x 2048 29 us forward and 41 backward, where the bytes alone would take 15 and 26; 8 x 4096 x 2048
-// 105 and 152 of 62 and 103; 3 x 1999 x 1502, pieces of 4 bytes, 24 and 35 of 8 and 14; 1 x 65536 x 512 with cuts 93 and 131 of 31 and 51.  The first
-// three are bound by instructions (some 500 a round of 8 rows a warp forward, 130 of them the hand-over), the last by the steps that a round of a
-// cluster has to wait for one after the other.
+// Measured on a B200 (its copy moves 6.53 TB/s), calls one behind the other on inputs that change: 4 x 2048 x 2048 29 us forward and 41 backward, where
+// the bytes alone would take 15 and 26; 8 x 4096 x 2048 106 and 152 of 62 and 103 (with the L2 cache flushed in front of every call 113 and 158); 3 x 1999 x
+// 1502, pieces of 4 bytes, 24 and 35 of 8 and 14; 1 x 65536 x 512 with cuts 93 and 132 of 31 and 51.  The lone CTAs of the first two are bound by what a round
+// waits for, lookups and the hand-over's barrier with 16 warps on an SM (issue slots 54 %, L1 60 %, no arithmetic pipe above 50 %, some 500 instructions a
+// round of 8 rows a warp forward), on 256 of 296 places; the last by the steps that a round of a cluster has to wait for one after the other.
 template <int WORDS, bool FLAGS, bool JOINED>
 __global__ void __launch_bounds__(LR_T, 2) k_linrec_fwd(const __grid_constant__ LrArgs p) {
   extern __shared__ __align__(16) char smem[];

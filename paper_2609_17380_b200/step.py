@@ -47,7 +47,7 @@ class ModelConfig:
     arith: int = 1                   # 2: the LM-head contractions in arithmetic version 2 (order-free, int8 tensor cores)
     # blocks that are not the paper's
     norm: str = "rms"                # "layer": the norms subtract the mean and have a shift beside the gain
-    recurrent: tuple = ()            # layers whose mixer is the gated linear recurrence (w_qkv: gate and value, 2 d_model rows) in place of attention
+    recurrent: tuple = ()            # layers whose mixer is the gated linear recurrence (w_qkv: gate and value, 2 d_model rows) in place of attention; every sequence from zero, without cuts
     act8: bool = False               # inputs of the norms, of SwiGLU and of the recurrence are kept in 8 bits for the backward pass
 
     def as_dict(self):
