@@ -138,26 +138,8 @@ constexpr float sg_at(int bits, bool negative) {
   for (int e = bits >> 7; e > 127; --e) x *= 2.0f;
   for (int e = bits >> 7; e < 127; ++e) x *= 0.5f;
   if (!negative) x = -x;
-  float e = 0.0f;                                          // exp(-gate)
-  if (x > 0x1.62e42ep+6f) return 0.0f;
-  if (x >= -0x1.5d58a0p+6f) {
-    float t = x * 0x1.715476p+0f;
-    t = t + 12582912.0f;
-    const float kf = t - 12582912.0f;
-    t = kf * 0x1.62e400p-1f;
-    float r = x - t;
-    t = kf * 0x1.7f7d1cp-20f;
-    r = r - t;
-    const float c[7] = {0x1.6c16c2p-10f, 0x1.111112p-7f, 0x1.555556p-5f, 0x1.555556p-3f, 0.5f, 1.0f, 1.0f};
-    e = 0x1.a01a02p-13f;
-    for (int i = 0; i < 7; ++i) {
-      t = e * r;
-      e = t + c[i];
-    }
-    for (int k = (int)kf; k < 0; ++k) e *= 0.5f;
-    for (int k = (int)kf; k > 0; --k) e *= 2.0f;
-  }
-  const float d = 1.0f + e, q = 1.0f / d;
+  if (x > 0x1.62e42ep+6f) return 0.0f;                     // x: -gate
+  const float d = 1.0f + det_exp_at(x), q = 1.0f / d;
   return q < 0x1p-126f ? 0.0f : q;
 }
 // Where entry i lies: a code below 64 has fractions that end in zeros, and in order of the magnitude they would meet in a few banks of shared memory.

@@ -79,6 +79,27 @@ __device__ __forceinline__ float det_exp(float x) {
   return v;
 }
 
+// The same function for the compiler to evaluate, in tables of its values: x at most 0x1.62e42ep+6.  A statement for every rounding.
+constexpr float det_exp_at(float x) {
+  if (x < -0x1.5d58a0p+6f) return 0.0f;
+  float t = x * 0x1.715476p+0f;
+  t = t + 12582912.0f;
+  const float kf = t - 12582912.0f;
+  t = kf * 0x1.62e400p-1f;
+  float r = x - t;
+  t = kf * 0x1.7f7d1cp-20f;
+  r = r - t;
+  const float c[7] = {0x1.6c16c2p-10f, 0x1.111112p-7f, 0x1.555556p-5f, 0x1.555556p-3f, 0.5f, 1.0f, 1.0f};
+  float p = 0x1.a01a02p-13f;
+  for (int i = 0; i < 7; ++i) {
+    t = p * r;
+    p = t + c[i];
+  }
+  for (int k = (int)kf; k < 0; ++k) p *= 0.5f;
+  for (int k = (int)kf; k > 0; --k) p *= 2.0f;
+  return p;
+}
+
 // The same function for arguments that are never positive (x <= 0, or NaN): a softmax argument z - max.  There k <= 0, so
 // neither the k = 128 product nor the overflow select can be chosen and the upper clamp of k never binds; what is left
 // is the same sequence, so every result has the bits det_exp gives.  For x > 0 the value is unspecified (no trap).

@@ -45,22 +45,7 @@ constexpr float lr_minor_at(int bits) {
   float x = -(1.0f + (bits & 127) / 128.0f);
   for (int e = bits >> 7; e > 127; --e) x *= 2.0f;
   for (int e = bits >> 7; e < 127; ++e) x *= 0.5f;
-  if (x < -0x1.5d58a0p+6f) return 0.0f;
-  float t = x * 0x1.715476p+0f;
-  t = t + 12582912.0f;
-  const float kf = t - 12582912.0f;
-  t = kf * 0x1.62e400p-1f;
-  float r = x - t;
-  t = kf * 0x1.7f7d1cp-20f;
-  r = r - t;
-  const float c[7] = {0x1.6c16c2p-10f, 0x1.111112p-7f, 0x1.555556p-5f, 0x1.555556p-3f, 0.5f, 1.0f, 1.0f};
-  float q = 0x1.a01a02p-13f;
-  for (int i = 0; i < 7; ++i) {
-    t = q * r;
-    q = t + c[i];
-  }
-  for (int k = (int)kf; k < 0; ++k) q *= 0.5f;
-  const float d = 1.0f + q;
+  const float q = det_exp_at(x), d = 1.0f + q;
   return q / d;
 }
 constexpr LrTable lr_make_table() {

@@ -28,9 +28,7 @@ __device__ __forceinline__ size_t row_at(int row, int D, int col) { return (size
 template <bool BF>
 __device__ __forceinline__ void load8(const void* p, size_t idx, float v[8]) {
   if (BF) {
-    uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + idx);
-    v[0] = bflo(u.x); v[1] = bfhi(u.x); v[2] = bflo(u.y); v[3] = bfhi(u.y);
-    v[4] = bflo(u.z); v[5] = bfhi(u.z); v[6] = bflo(u.w); v[7] = bfhi(u.w);
+    unpack8(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + idx), v);
   } else {
     const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + idx);
     float4 a = q[0], b = q[1];
@@ -123,8 +121,7 @@ __device__ __forceinline__ void row_take(const char* place, float v[8]) {
   const uint4* q = reinterpret_cast<const uint4*>(place) + threadIdx.x;
   const uint4 a = q[0];
   if (BF) {
-    v[0] = bflo(a.x); v[1] = bfhi(a.x); v[2] = bflo(a.y); v[3] = bfhi(a.y);
-    v[4] = bflo(a.z); v[5] = bfhi(a.z); v[6] = bflo(a.w); v[7] = bfhi(a.w);
+    unpack8(a, v);
   } else {
     const uint4 b = q[T];
     v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
