@@ -166,6 +166,43 @@ int det_residual_rmsnorm_fwd(const det_bf16* a, const det_bf16* b, const det_bf1
 int det_rmsnorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf16* gamma, const float* rstd, int rows, int D,
                              const det_bf16* res, det_bf16* dx, float* dgamma, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- 8-bit products with a scale for each token and each output channel -------------------------------------------
+ * Linears of runs that are not the paper's: the scales follow the values, by token and by channel, where det_linear_fwd has one learned step for all tokens.
+ * Codes of a row v of values: a = max|v|, s = fdiv(a, 127), inv = fdiv(1, s) (0 where s is 0), code = rne(v * inv) in [-127, 127]; a row with an infinity
+ * or a NaN has s = NaN and codes 0, and everything that is made from it is NaN.  Rows of K codes are det_tok8_ld(K) bytes apart (K rounded up to 16),
+ * 16-byte aligned, with ZEROS behind the last code, which the calls that write codes put there.
+ *   det_tok8_quant: qX, s_x [M] of the rows of X; of a weight [N, K] those are its channels (the forward pass wants qW, s_w [N]).
+ *   det_tok8_transpose: codes [M, K] -> [K, M] (the backward pass wants the weight's, qWt [K, det_tok8_ld(N)]).
+ * Any M >= 0 (up to 2^28), any N, K >= 1; bf16 matrices have rows ld elements apart (ld >= the width), any alignment to the element; scales f32.  Whole
+ * rows in 16-byte pieces are faster.  K < 2^17 (DET_ERR_RANGE), in the backward pass M and N too.  M = 0: no rows, and a dW of zeros.
+ * Outputs overlap no input.  Two tokens' results never depend on each other; nor does a token's on how many there are. */
+int det_tok8_ld(int K);
+int det_tok8_quant(const det_bf16* X, int ld, int M, int K, int8_t* qX, float* s_x, void* stream);
+int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, void* stream);
+/* Y[m,n] = bf16(float(sum_k qX qW) * (s_x[m] * s_w[n])), the sum exact in int32.  det_tok8_linear_fwd = det_tok8_quant, then _fwd_q; qX, s_x are its
+ * outputs, kept for the backward pass. */
+int det_tok8_linear_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int N, int K, det_bf16* Y, int ld_y, int8_t* qX, float* s_x,
+                        void* stream, int* status_dev);
+int det_tok8_linear_fwd_q(const int8_t* qX, const float* s_x, const int8_t* qW, const float* s_w, int M, int N, int K, det_bf16* Y, int ld_y, void* stream,
+                          int* status_dev);
+/* Straight through the codes.  A scale cannot leave a sum over its own index, so it goes into the gradient before that is put into codes:
+ *   A = dY * s_w[n] by token (s_a):    dX[m,k] = bf16(float(sum_n qA qW) * s_a[m])
+ *   G = dY * s_x[m] by channel (s_g):  dW[n,k] = float(sum_m qG qX) * s_g[n]   (f32 [N, K], overwritten)
+ * dX or dW may be NULL (not both).  ws: 256-byte aligned. */
+size_t det_tok8_linear_bwd_ws_bytes(int M, int N, int K);
+int det_tok8_linear_bwd(const det_bf16* dY, int ld_dy, const int8_t* qX, const float* s_x, const int8_t* qWt, const float* s_w, int M, int N, int K,
+                        det_bf16* dX, int ld_dx, float* dW, void* ws, size_t ws_bytes, void* stream, int* status_dev);
+/* The gated feed-forward block: both projections, the activation and the product in one kernel.  qW: codes of the gates' F channels, then of the ups' (the
+ * fused weight of the step), s_w [2F].  gu = det_tok8_linear_fwd's Y (bf16 [M, 2F], rows ld_gu apart; NULL: not kept), h = det_swiglu_fwd of it, bit for bit.
+ * det_tok8_glu_bwd: dgu = det_swiglu_bwd of dh and gu, then det_tok8_linear_bwd of dgu, bit for bit; qWt [K, det_tok8_ld(2F)], dW [2F, K]. */
+int det_tok8_glu_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int F, int K, det_bf16* h, int ld_h, det_bf16* gu, int ld_gu,
+                     int8_t* qX, float* s_x, void* stream, int* status_dev);
+int det_tok8_glu_fwd_q(const int8_t* qX, const float* s_x, const int8_t* qW, const float* s_w, int M, int F, int K, det_bf16* h, int ld_h, det_bf16* gu,
+                       int ld_gu, void* stream, int* status_dev);
+size_t det_tok8_glu_bwd_ws_bytes(int M, int F, int K);
+int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* gu, int ld_gu, const int8_t* qX, const float* s_x, const int8_t* qWt, const float* s_w,
+                     int M, int F, int K, det_bf16* dX, int ld_dx, float* dW, void* ws, size_t ws_bytes, void* stream, int* status_dev);
+
 /* ---- layer norm -------------------------------------------------------------------------------------------
  * The norm that subtracts the mean; not in the paper's block, for replays of models that use it.  Up to 2e9 rows and 1 <= D <= 8192;
  * pointers 16-byte aligned where D % 8 == 0, aligned to their element otherwise; io: dtype of x, y, gamma, beta, dy, dx.
@@ -396,6 +433,26 @@ int det_adamw_step(const det_adamw_desc* h, int pdtype, void* p, const float* g,
  * scalar, may be NULL) every g[t][i] is first multiplied by *coef_dev and stored, exactly as det_scale_inplace does. */
 int det_adamw_batch(const det_adamw_desc* descs, const int* pdtypes, void* const* p, float* const* g, float* const* m,
                     float* const* v, const size_t* n, int ntensors, const float* coef_dev, void* stream);
+
+/* The same with moments in 8 bits: for runs that were trained so.  256 adjacent values of a tensor (its last block may be shorter) share two scales,
+ * sm = max|m| and sr = max sqrt(v), kept as s[2b], s[2b+1] of block b (det_adamw8_scale_floats(n) floats, 8-byte aligned).  The codes count the root of a
+ * value's share of its scale: with t = code * (1/127), m = sm * (t |t|); with t = code * (1/255), r = sr * (t t), v = r r.  m8 int8, v8 uint8 [n].
+ * The update of m and v as in det_adamw_step, p moved by the new moments in binary32; then r = fsqrt(v), new scales, and the codes
+ * rne(fsqrt(|m| * fdiv(1, sm)) * 127) with the sign of m, rne(fsqrt(r * fdiv(1, sr)) * 255), at least 1 where r > 0; all zero is scale 0, codes 0.  A block
+ * with an infinity or a NaN has the scale NaN and codes 0.  A new state is zeros.
+ * Tensor by tensor: s[t] NULL has m[t], v[t] in f32 as for det_adamw_batch (s_out[t] NULL too).  The new state goes to p_out, m_out, v_out, s_out; each
+ * tensor there is the same as the input (in place) or overlaps none.  p, g (16-byte aligned, bf16 parameters 8), n, coef_dev as for det_adamw_batch: with
+ * coef_dev every g[t][i] is multiplied by it and stored.  Codes 4-byte aligned.  A call that changes inputs beyond recall (in place, or a coefficient other
+ * than 1) is not for repeating. */
+size_t det_adamw8_scale_floats(size_t n);
+int det_adamw8_batch(const det_adamw_desc* descs, const int* pdtypes, const void* const* p, float* const* g, const void* const* m, const void* const* v,
+                     const float* const* s, void* const* p_out, void* const* m_out, void* const* v_out, float* const* s_out, const size_t* n, int ntensors,
+                     const float* coef_dev, void* stream);
+/* Moments into codes and back (f32 m, v 16-byte aligned), many tensors at once: a state of 32 bits taken over, one of 8 bits looked at. */
+int det_adamw8_pack(const float* const* m, const float* const* v, int8_t* const* m8, uint8_t* const* v8, float* const* s, const size_t* n, int ntensors,
+                    void* stream);
+int det_adamw8_unpack(const int8_t* const* m8, const uint8_t* const* v8, const float* const* s, float* const* m, float* const* v, const size_t* n,
+                      int ntensors, void* stream);
 
 /* ---- tensor hash (Appendix B: per-step state hash, here on the device) --------------------------------
  * Level 1: SHA-256 of every 4 KiB chunk of the raw bytes (last chunk may be shorter).  While more than 128

@@ -152,6 +152,39 @@ def linear_bwd(dY, X, W, s_x, s_w, hb=128, debug=False):
     return (dX, dW, ds, dbg) if debug else (dX, dW, ds)
 
 
+# ---- 8-bit products with a scale for each token and output channel -------------
+def tok8_quant(X, row_factor=None, col_factor=None, by_col=False):
+    """Codes (rows of X, or its columns as rows where by_col) and scales of X times a factor for every row and column."""
+    X = _c(X, np.uint16)
+    R, n = X.shape
+    fr = _c(row_factor, np.float32) if row_factor is not None else None
+    fc = _c(col_factor, np.float32) if col_factor is not None else None
+    q, s = np.empty((n, R) if by_col else (R, n), np.int8), np.empty(n if by_col else R, np.float32)
+    lib().orc_tok8_quant(_p(X), C.c_int(R), C.c_int(n), _p(fr), _p(fc), C.c_int(int(by_col)), _p(q), _p(s))
+    return q, s
+
+
+def tok8_product(A, B, si, sj=None, bf=True):
+    A, B, si = _c(A, np.int8), _c(B, np.int8), _c(si, np.float32)
+    sj = _c(sj, np.float32) if sj is not None else None
+    out = np.empty((A.shape[0], B.shape[0]), np.uint16 if bf else np.float32)
+    lib().orc_tok8_product(_p(A), _p(B), C.c_int(A.shape[0]), C.c_int(B.shape[0]), C.c_int(A.shape[1]), _p(si), _p(sj), C.c_int(int(bf)), _p(out))
+    return out
+
+
+def tok8_linear_fwd(X, W):
+    """Y, codes and scales of the tokens, codes and scales of the channels."""
+    (qX, sX), (qW, sW) = tok8_quant(X), tok8_quant(W)
+    return tok8_product(qX, qW, sX, sW), qX, sX, qW, sW
+
+
+def tok8_linear_bwd(dY, X, W):
+    (qX, sX), (qW, sW) = tok8_quant(X), tok8_quant(W)
+    qA, sA = tok8_quant(dY, col_factor=sW)
+    qG, sG = tok8_quant(dY, row_factor=sX, by_col=True)
+    return tok8_product(qA, np.ascontiguousarray(qW.T), sA), tok8_product(qG, np.ascontiguousarray(qX.T), sG, bf=False)
+
+
 def wht128_f(v):
     v = _c(v, np.float32).copy()
     lib().orc_wht128_f(_p(v))
@@ -496,6 +529,34 @@ def adamw(p, g, m, v, lr, beta1, beta2, eps, wd, step):
     lib().orc_adamw(C.c_double(lr), C.c_double(beta1), C.c_double(beta2), C.c_double(eps), C.c_double(wd), C.c_int(step),
                     C.c_int(int(bf)), _p(p), _p(g), _p(m), _p(v), C.c_size_t(p.size))
     return p, m, v
+
+
+# ---- AdamW with moments in 8 bits --------------------------------------------
+ADAMW8_BLOCK = 256
+
+
+def adamw8_pack(m, v):
+    """Codes m8 (int8), v8 (uint8) and scales [blocks, 2] of the moments of one tensor."""
+    m, v = _c(m, np.float32).reshape(-1), _c(v, np.float32).reshape(-1)
+    m8, v8, s = np.empty(m.size, np.int8), np.empty(m.size, np.uint8), np.empty(((m.size + 255) // 256, 2), np.float32)
+    lib().orc_adamw8_pack(_p(m), _p(v), _p(m8), _p(v8), _p(s), C.c_size_t(m.size))
+    return m8, v8, s
+
+
+def adamw8_unpack(m8, v8, s):
+    m8, v8, s = _c(m8, np.int8), _c(v8, np.uint8), _c(s, np.float32)
+    m, v = np.empty(m8.size, np.float32), np.empty(m8.size, np.float32)
+    lib().orc_adamw8_unpack(_p(m8), _p(v8), _p(s), _p(m), _p(v), C.c_size_t(m8.size))
+    return m, v
+
+
+def adamw8(p, g, m8, v8, s, lr, beta1, beta2, eps, wd, step):
+    """adamw with the moments kept in 8 bits: updated copies of p, m8, v8 and the scales."""
+    p, m8, v8, s = np.ascontiguousarray(p).copy(), _c(m8, np.int8).copy(), _c(v8, np.uint8).copy(), _c(s, np.float32).copy()
+    g = _c(g, np.float32)
+    lib().orc_adamw8(C.c_double(lr), C.c_double(beta1), C.c_double(beta2), C.c_double(eps), C.c_double(wd), C.c_int(step),
+                     C.c_int(int(p.dtype == np.uint16)), _p(p), _p(g), _p(m8), _p(v8), _p(s), C.c_size_t(p.size))
+    return p, m8, v8, s
 
 
 def sha256(data):

@@ -1210,3 +1210,122 @@ void orc_linrec_bwd(const bf16_t *dy, int ldy, const bf16_t *g, const bf16_t *v,
     free(w);
   }
 }
+
+/* ------------------------------------------------------------------ */
+/* 8-bit products with a scale for each token and output channel       */
+/* ------------------------------------------------------------------ */
+/* Codes of the rows of X (of its columns where by_col), after a factor for every row (fr) and column (fc), each NULL for none: the group's
+ * largest magnitude a gives s = a / 127, code = rne(v * (1/s)), 0 where s is 0; a group with an infinity or a NaN has s = NaN and codes 0.
+ * q: [R, C], or [C, R] where by_col; s: one for each group. */
+void orc_tok8_quant(const bf16_t *X, int R, int C, const float *fr, const float *fc, int by_col, int8_t *q, float *s) {
+  int groups = by_col ? C : R, len = by_col ? R : C;
+#pragma omp parallel for
+  for (int g = 0; g < groups; ++g) {
+    float *v = (float *)malloc((size_t)(len ? len : 1) * sizeof(float)), a = 0.0f;
+    int finite = 1;
+    for (int i = 0; i < len; ++i) {
+      int r = by_col ? i : g, c = by_col ? g : i;
+      float t = ftz(bf2f(X[(size_t)r * C + c]));
+      if (fc) t = fmul(t, fc[c]);
+      if (fr) t = fmul(t, fr[r]);
+      v[i] = t;
+      if (isnan(t) || isinf(t)) finite = 0;
+      else if (fabsf(t) > a) a = fabsf(t);
+    }
+    float step = fdiv(a, 127.0f), inv = step > 0.0f ? fdiv(1.0f, step) : 0.0f;
+    s[g] = finite ? step : NAN;
+    for (int i = 0; i < len; ++i) {
+      float t = finite ? frne(fmul(v[i], inv)) : 0.0f;
+      q[(size_t)g * len + i] = (int8_t)(t > 127.0f ? 127.0f : t < -127.0f ? -127.0f : t);
+    }
+    free(v);
+  }
+}
+/* C[i,j] = float(sum_k A[i,k] B[j,k]) * (si[i] * sj[j]), or * si[i] where sj is NULL; rounded to bf16 or left in binary32 */
+void orc_tok8_product(const int8_t *A, const int8_t *B, int I, int J, int K, const float *si, const float *sj, int bf, void *C) {
+  int32_t *acc = (int32_t *)malloc((size_t)I * J * sizeof(int32_t) + 4);
+  igemm_tn(A, B, I, J, K, acc);
+#pragma omp parallel for
+  for (int i = 0; i < I; ++i)
+    for (int j = 0; j < J; ++j) {
+      float f = fmul(i2f(acc[(size_t)i * J + j]), sj ? fmul(si[i], sj[j]) : si[i]);
+      if (bf) ((bf16_t *)C)[(size_t)i * J + j] = f2bf(f);
+      else ((float *)C)[(size_t)i * J + j] = f;
+    }
+  free(acc);
+}
+
+/* ------------------------------------------------------------------ */
+/* AdamW with moments in 8 bits: 256 adjacent values of a tensor share */
+/* the largest first moment and the largest root of the second         */
+/* ------------------------------------------------------------------ */
+#define A8B 256
+#define A8_127 0x1.020408p-7f /* 1/127 */
+#define A8_255 0x1.010102p-8f /* 1/255 */
+static float a8_first(int8_t c, float s) { float t = fmul((float)c, A8_127); return fmul(s, fmul(t, fabs1(t))); }
+static float a8_root(uint8_t c, float s) { float t = fmul((float)c, A8_255); return fmul(s, fmul(t, t)); }
+/* codes of a block: the root of a value's share of the largest, in 127 or 255 parts; a block with a value that is not finite: scale NaN, codes 0 */
+static float a8_block(const float *x, int n, int top, int *c) {
+  float a = 0.0f;
+  int finite = 1;
+  for (int i = 0; i < n; ++i) {
+    if (isnan(x[i]) || isinf(x[i])) finite = 0;
+    else if (fabs1(x[i]) > a) a = fabs1(x[i]);
+  }
+  float inv = a > 0.0f ? fdiv(1.0f, a) : 0.0f;
+  for (int i = 0; i < n; ++i) {
+    float t = finite ? frne(fmul(fsqrt(fmul(fabs1(x[i]), inv)), (float)top)) : 0.0f;
+    c[i] = t > (float)top ? top : (int)t;
+    if (top == 255 && finite && x[i] > 0.0f && c[i] < 1) c[i] = 1; /* a root that is not zero is not kept as zero */
+    if (top == 127 && x[i] < 0.0f) c[i] = -c[i];
+  }
+  return finite ? a : NAN;
+}
+static void a8_put(const float *m, const float *r, int n, int8_t *m8, uint8_t *v8, float *s) {
+  int c[A8B];
+  s[0] = a8_block(m, n, 127, c);
+  for (int i = 0; i < n; ++i) m8[i] = (int8_t)c[i];
+  s[1] = a8_block(r, n, 255, c);
+  for (int i = 0; i < n; ++i) v8[i] = (uint8_t)c[i];
+}
+void orc_adamw8_pack(const float *m, const float *v, int8_t *m8, uint8_t *v8, float *s, size_t n) {
+#pragma omp parallel for
+  for (size_t b = 0; b < (n + A8B - 1) / A8B; ++b) {
+    size_t lo = b * A8B;
+    int k = (int)(n - lo < A8B ? n - lo : A8B);
+    float mi[A8B], ri[A8B];
+    for (int i = 0; i < k; ++i) { mi[i] = ftz(m[lo + i]); ri[i] = fsqrt(v[lo + i]); }
+    a8_put(mi, ri, k, m8 + lo, v8 + lo, s + 2 * b);
+  }
+}
+void orc_adamw8_unpack(const int8_t *m8, const uint8_t *v8, const float *s, float *m, float *v, size_t n) {
+#pragma omp parallel for
+  for (size_t i = 0; i < n; ++i) {
+    float r = a8_root(v8[i], s[2 * (i / A8B) + 1]);
+    m[i] = a8_first(m8[i], s[2 * (i / A8B)]);
+    v[i] = fmul(r, r);
+  }
+}
+void orc_adamw8(double lr, double beta1, double beta2, double eps, double wd, int step, int p_is_bf16, void *p, const float *g, int8_t *m8, uint8_t *v8,
+                float *s, size_t n) {
+  double bc1 = 1.0 - ipow(beta1, step), bc2 = 1.0 - ipow(beta2, step);
+  float stepsz = (float)(lr / bc1), isb2 = (float)(1.0 / sqrt(bc2)), decay = (float)(1.0 - lr * wd);
+  float b1 = (float)beta1, b2 = (float)beta2, epsf = (float)eps;
+  float omb1 = fsub(1.0f, b1), omb2 = fsub(1.0f, b2);
+#pragma omp parallel for
+  for (size_t b = 0; b < (n + A8B - 1) / A8B; ++b) {
+    size_t lo = b * A8B;
+    int k = (int)(n - lo < A8B ? n - lo : A8B);
+    float mi[A8B], ri[A8B];
+    for (int j = 0; j < k; ++j) {
+      size_t i = lo + j;
+      float pv = p_is_bf16 ? bf2f(((bf16_t *)p)[i]) : ftz(((float *)p)[i]), gi = g[i];
+      float r0 = a8_root(v8[i], s[2 * b + 1]), v0 = fmul(r0, r0), m0 = a8_first(m8[i], s[2 * b]);
+      mi[j] = fadd(fmul(b1, m0), fmul(omb1, gi));
+      ri[j] = fsqrt(fadd(fmul(b2, v0), fmul(omb2, fmul(gi, gi))));
+      pv = fsub(fmul(pv, decay), fmul(stepsz, fdiv(mi[j], fadd(fmul(ri[j], isb2), epsf))));
+      if (p_is_bf16) ((bf16_t *)p)[i] = f2bf(pv); else ((float *)p)[i] = pv;
+    }
+    a8_put(mi, ri, k, m8 + lo, v8 + lo, s + 2 * b);
+  }
+}

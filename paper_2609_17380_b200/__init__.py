@@ -73,6 +73,11 @@ _SIGNATURES = {
     "det_layernorm_bwd": "iipppppiippppzp", "det_layernorm_bwd_residual": "ipppppiipppppzp", "det_layernorm_bwd_act8": "ippppppiipppppzp",
     "det_act8_exp_bytes": "zii", "det_act8_pack": "iipiiippp", "det_act8_unpack": "iippiipip",
     "det_swiglu_fwd_act8": "ipiipppppp", "det_swiglu_act8": "ippiipppp", "det_swiglu_bwd_act8": "ipppiipp",
+    "det_tok8_ld": "ii", "det_tok8_quant": "ipiiippp", "det_tok8_transpose": "ipiipp", "det_tok8_linear_fwd": "ipippiiipipppp",
+    "det_tok8_linear_fwd_q": "ippppiiipipp", "det_tok8_linear_bwd_ws_bytes": "ziii", "det_tok8_linear_bwd": "ipippppiiipippzpp",
+    "det_tok8_glu_fwd": "ipippiiipipipppp", "det_tok8_glu_fwd_q": "ippppiiipipipp", "det_tok8_glu_bwd_ws_bytes": "ziii",
+    "det_tok8_glu_bwd": "ipipippppiiipippzpp", "det_adamw8_scale_floats": "zz", "det_adamw8_batch": "ippppppppppppipp",
+    "det_adamw8_pack": "ippppppip", "det_adamw8_unpack": "ippppppip",
     "det_linrec_state_floats": "ziii", "det_linrec_fwd": "ippiiiipipppppp", "det_linrec_bwd": "ipippiiiipppippppp",
 }
 
@@ -93,6 +98,9 @@ _PATTERNS = {
     "det_layernorm_fwd": "ipppiifppps", "det_residual_layernorm_fwd": "ppppiifpppppppps", "det_layernorm_bwd": "ipppppiipppws",
     "det_layernorm_bwd_residual": "pppppiippppws", "det_layernorm_bwd_act8": "ppppppiippppws", "det_act8_pack": "ipiiipps",
     "det_act8_unpack": "ippiipis", "det_swiglu_fwd_act8": "piippppps", "det_swiglu_act8": "ppiippps",
+    "det_tok8_quant": "piiipps", "det_tok8_transpose": "piips", "det_tok8_linear_fwd": "pippiiipippsp", "det_tok8_linear_fwd_q": "ppppiiipisp",
+    "det_tok8_linear_bwd": "pippppiiipipwsp", "det_tok8_glu_fwd": "pippiiipipippsp", "det_tok8_glu_fwd_q": "ppppiiipipisp",
+    "det_tok8_glu_bwd": "pipippppiiipipwsp",
     "det_swiglu_bwd_act8": "pppiips", "det_linrec_fwd": "ppiiiipippppsp", "det_linrec_bwd": "pippiiiipppipppsp",
 }
 
@@ -366,6 +374,52 @@ def det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags=None
     _c.det_linrec_bwd(dy, ld_y, g, v, ld, B, S, D, states, dg, dv, ld_d, flags, dhT, dh0, status_dev)
 
 
+# ---- 8-bit products with a scale for each token and output channel -----------------------------------------------
+def det_tok8_ld(K):
+    """Bytes from a row of K codes to the next."""
+    return load().det_tok8_ld(K)
+
+
+def det_tok8_quant(X, ld, M, K, qX, s_x):
+    _c.det_tok8_quant(X, ld, M, K, qX, s_x)
+
+
+def det_tok8_transpose(q, M, K, qT):
+    _c.det_tok8_transpose(q, M, K, qT)
+
+
+def det_tok8_linear_fwd(X, ld, qW, s_w, M, N, K, Y, ld_y, qX, s_x, status_dev=None):
+    _c.det_tok8_linear_fwd(X, ld, qW, s_w, M, N, K, Y, ld_y, qX, s_x, status_dev)
+
+
+def det_tok8_linear_fwd_q(qX, s_x, qW, s_w, M, N, K, Y, ld_y, status_dev=None):
+    _c.det_tok8_linear_fwd_q(qX, s_x, qW, s_w, M, N, K, Y, ld_y, status_dev)
+
+
+def det_tok8_linear_bwd_ws_bytes(M, N, K):
+    return load().det_tok8_linear_bwd_ws_bytes(M, N, K)
+
+
+def det_tok8_linear_bwd(dY, ld_dy, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, status_dev=None):
+    _c.det_tok8_linear_bwd(dY, ld_dy, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, status_dev)
+
+
+def det_tok8_glu_fwd(X, ld, qW, s_w, M, F, K, h, ld_h, gu, ld_gu, qX, s_x, status_dev=None):
+    _c.det_tok8_glu_fwd(X, ld, qW, s_w, M, F, K, h, ld_h, gu, ld_gu, qX, s_x, status_dev)
+
+
+def det_tok8_glu_fwd_q(qX, s_x, qW, s_w, M, F, K, h, ld_h, gu=None, ld_gu=0, status_dev=None):
+    _c.det_tok8_glu_fwd_q(qX, s_x, qW, s_w, M, F, K, h, ld_h, gu, ld_gu, status_dev)
+
+
+def det_tok8_glu_bwd_ws_bytes(M, F, K):
+    return load().det_tok8_glu_bwd_ws_bytes(M, F, K)
+
+
+def det_tok8_glu_bwd(dh, ld_dh, gu, ld_gu, qX, s_x, qWt, s_w, M, F, K, dX, ld_dx, dW, ws, status_dev=None):
+    _c.det_tok8_glu_bwd(dh, ld_dh, gu, ld_gu, qX, s_x, qWt, s_w, M, F, K, dX, ld_dx, dW, ws, status_dev)
+
+
 # ---- attention ------------------------------------------------------------------------------------------------
 def det_attn_fwd(q, k, v, ld, B, H, S, out, ld_out, lse, Hkv=None, window=0):
     _c.det_attn_fwd(q, k, v, ld, B, H, H if Hkv is None else Hkv, S, window, out, ld_out, lse)
@@ -509,6 +563,52 @@ def det_adamw_batch(descs, pdtypes, ps, gs, ms, vs, coef_dev=None):
         "one entry per tensor in every list; parameter, gradient and moments of a tensor have the same number of elements"
     _check("det_adamw_batch", load().det_adamw_batch((det_adamw_desc * k)(*descs), (C.c_int * k)(*pdtypes), table(ps), table(gs),
                                                      table(ms), table(vs), (C.c_size_t * k)(*counts), k, _ptr(coef_dev), _stream()))
+
+
+def det_adamw8_scale_floats(n):
+    return load().det_adamw8_scale_floats(n)
+
+
+def _scales_fit(n, s):
+    return s is None or (s.dtype == torch.float32 and s.numel() == det_adamw8_scale_floats(n))
+
+
+def det_adamw8_batch(descs, pdtypes, ps, gs, ms, vs, ss, coef_dev=None, outs=None):
+    """One launch for many tensors; ss: the scales of a tensor's moments in 8 bits, or None where they are f32.  outs = (ps, ms, vs, ss): where the new
+    state goes, None: in place.  coef_dev: as for det_adamw_batch."""
+    k, numel, size = len(ps), torch.Tensor.numel, torch.Tensor.element_size
+    counts = list(map(numel, ps))
+    ins = (ps, ms, vs, ss)
+    outs = ins if outs is None else outs
+    each = [2 if kind == DET_BF16 else 4 for kind in pdtypes]
+    moment = [4 if s is None else 1 for s in ss]
+    assert k == len(descs) == len(pdtypes) and list(map(numel, gs)) == counts and list(map(size, gs)) == [4] * k and all(
+        list(map(numel, ts)) == counts for side in (ins, outs) for ts in side[:3]) and all(
+        list(map(size, side[0])) == each and list(map(size, side[1])) == moment and list(map(size, side[2])) == moment and len(side[3]) == k and
+        all(map(_scales_fit, counts, side[3])) for side in (ins, outs)) and [s is None for s in ss] == [s is None for s in outs[3]], \
+        "one entry per tensor in every list; parameter, gradient and moments of a tensor have the same number of elements, two scales for every 256"
+    table = lambda ts: (C.c_void_p * k)(*map(_ptr, ts))
+    _check("det_adamw8_batch", load().det_adamw8_batch((det_adamw_desc * k)(*descs), (C.c_int * k)(*pdtypes), table(ps), table(gs), table(ms), table(vs),
+                                                       table(ss), *map(table, outs), (C.c_size_t * k)(*counts), k, _ptr(coef_dev), _stream()))
+
+
+def _adamw8_numbers(name, m8s, v8s, ss, ms, vs, order):
+    k, numel, size = len(m8s), torch.Tensor.numel, torch.Tensor.element_size
+    counts = list(map(numel, m8s))
+    assert all(list(map(numel, ts)) == counts and list(map(size, ts)) == [width] * k for ts, width in ((m8s, 1), (v8s, 1), (ms, 4), (vs, 4))) and \
+        len(ss) == k and all(s is not None and _scales_fit(n, s) for n, s in zip(counts, ss)), \
+        "one entry per tensor in every list; codes and moments of a tensor have the same number of elements, two scales for every 256"
+    _check(name, getattr(load(), name)(*((C.c_void_p * k)(*map(_ptr, ts)) for ts in order), (C.c_size_t * k)(*counts), k, _stream()))
+
+
+def det_adamw8_pack(ms, vs, m8s, v8s, ss):
+    """Moments of many tensors into codes and scales."""
+    _adamw8_numbers("det_adamw8_pack", m8s, v8s, ss, ms, vs, (ms, vs, m8s, v8s, ss))
+
+
+def det_adamw8_unpack(m8s, v8s, ss, ms, vs):
+    """The moments that codes and scales of many tensors stand for."""
+    _adamw8_numbers("det_adamw8_unpack", m8s, v8s, ss, ms, vs, (m8s, v8s, ss, ms, vs))
 
 
 def det_tensor_hash_ws_bytes(nbytes):

@@ -509,11 +509,12 @@ static EncodeTiledFn get_encode() {
   }
   return fn;
 }
-bool make_map(CUtensorMap* tm, const int8_t* base, int rows, int K, int box_rows) {
+bool make_map(CUtensorMap* tm, const int8_t* base, int rows, int K, int box_rows) { return make_map_ld(tm, base, rows, K, K, box_rows); }
+bool make_map_ld(CUtensorMap* tm, const int8_t* base, int rows, int K, int ld, int box_rows) {
   EncodeTiledFn enc = get_encode();
   if (!enc) return false;
   cuuint64_t gdim[2] = {(cuuint64_t)K, (cuuint64_t)rows};
-  cuuint64_t gstr[1] = {(cuuint64_t)K};
+  cuuint64_t gstr[1] = {(cuuint64_t)ld};
   cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
   return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,

@@ -28,6 +28,25 @@ inline void launch_after(void (*kern)(P...), dim3 grid, int threads, size_t smem
   note_launch();
   cudaLaunchKernelEx(&cfg, kern, args...);   // an error stays for the caller's check of the launch
 }
+// The same for clusters of `cluster` CTAs in a row (1: none).
+template <class... P, class... A>
+inline void launch_after_cluster(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const A&... args) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  note_launch();
+  cudaLaunchKernelEx(&cfg, kern, args...);
+}
 // floats of scratch the multi-level tree sum needs for n elements
 size_t sum_ws_floats(size_t n);
 // out[0] = det_sum(x[0..n)) (squares: of x^2); launches on st, scratch in ws (sum_ws_floats(n) floats)

@@ -168,6 +168,7 @@ __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t (&r)[1
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // host: tensor map of a row-major int8 matrix [rows, K] with boxes of box_rows x 128 bytes, 128-byte swizzle (igemm.cu)
 bool make_map(CUtensorMap* tm, const int8_t* base, int rows, int K, int box_rows);
+bool make_map_ld(CUtensorMap* tm, const int8_t* base, int rows, int K, int ld, int box_rows);   // rows ld bytes apart, a multiple of 16; zeros behind K
 
 // A warp's 32 rows x 32 columns of output, held one row per lane (`w`: NW sixteen-byte words), go through a 32 x NW*16
 // byte staging tile in shared memory (sixteen-byte pieces XOR-swizzled, conflict-free both ways) so that every store
