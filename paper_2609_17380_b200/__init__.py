@@ -569,46 +569,26 @@ def det_adamw8_scale_floats(n):
     return load().det_adamw8_scale_floats(n)
 
 
-def _scales_fit(n, s):
-    return s is None or (s.dtype == torch.float32 and s.numel() == det_adamw8_scale_floats(n))
+def _native(name):
+    load()
+    from . import _binding
+    return getattr(_binding, name)
 
 
 def det_adamw8_batch(descs, pdtypes, ps, gs, ms, vs, ss, coef_dev=None, outs=None):
     """One launch for many tensors; ss: the scales of a tensor's moments in 8 bits, or None where they are f32.  outs = (ps, ms, vs, ss): where the new
     state goes, None: in place.  coef_dev: as for det_adamw_batch."""
-    k, numel, size = len(ps), torch.Tensor.numel, torch.Tensor.element_size
-    counts = list(map(numel, ps))
-    ins = (ps, ms, vs, ss)
-    outs = ins if outs is None else outs
-    each = [2 if kind == DET_BF16 else 4 for kind in pdtypes]
-    moment = [4 if s is None else 1 for s in ss]
-    assert k == len(descs) == len(pdtypes) and list(map(numel, gs)) == counts and list(map(size, gs)) == [4] * k and all(
-        list(map(numel, ts)) == counts for side in (ins, outs) for ts in side[:3]) and all(
-        list(map(size, side[0])) == each and list(map(size, side[1])) == moment and list(map(size, side[2])) == moment and len(side[3]) == k and
-        all(map(_scales_fit, counts, side[3])) for side in (ins, outs)) and [s is None for s in ss] == [s is None for s in outs[3]], \
-        "one entry per tensor in every list; parameter, gradient and moments of a tensor have the same number of elements, two scales for every 256"
-    table = lambda ts: (C.c_void_p * k)(*map(_ptr, ts))
-    _check("det_adamw8_batch", load().det_adamw8_batch((det_adamw_desc * k)(*descs), (C.c_int * k)(*pdtypes), table(ps), table(gs), table(ms), table(vs),
-                                                       table(ss), *map(table, outs), (C.c_size_t * k)(*counts), k, _ptr(coef_dev), _stream()))
-
-
-def _adamw8_numbers(name, m8s, v8s, ss, ms, vs, order):
-    k, numel, size = len(m8s), torch.Tensor.numel, torch.Tensor.element_size
-    counts = list(map(numel, m8s))
-    assert all(list(map(numel, ts)) == counts and list(map(size, ts)) == [width] * k for ts, width in ((m8s, 1), (v8s, 1), (ms, 4), (vs, 4))) and \
-        len(ss) == k and all(s is not None and _scales_fit(n, s) for n, s in zip(counts, ss)), \
-        "one entry per tensor in every list; codes and moments of a tensor have the same number of elements, two scales for every 256"
-    _check(name, getattr(load(), name)(*((C.c_void_p * k)(*map(_ptr, ts)) for ts in order), (C.c_size_t * k)(*counts), k, _stream()))
+    _check("det_adamw8_batch", _native("adamw8_batch")(descs, pdtypes, ps, gs, ms, vs, ss, coef_dev, outs))
 
 
 def det_adamw8_pack(ms, vs, m8s, v8s, ss):
     """Moments of many tensors into codes and scales."""
-    _adamw8_numbers("det_adamw8_pack", m8s, v8s, ss, ms, vs, (ms, vs, m8s, v8s, ss))
+    _check("det_adamw8_pack", _native("adamw8_numbers")(True, m8s, v8s, ss, ms, vs))
 
 
 def det_adamw8_unpack(m8s, v8s, ss, ms, vs):
     """The moments that codes and scales of many tensors stand for."""
-    _adamw8_numbers("det_adamw8_unpack", m8s, v8s, ss, ms, vs, (m8s, v8s, ss, ms, vs))
+    _check("det_adamw8_unpack", _native("adamw8_numbers")(False, m8s, v8s, ss, ms, vs))
 
 
 def det_tensor_hash_ws_bytes(nbytes):

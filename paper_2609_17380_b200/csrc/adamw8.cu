@@ -6,6 +6,7 @@
 // The update itself is det_adamw_batch's; the parameter moves by the moments before they are put into codes.
 #include "common.cuh"
 #include "internal.h"
+#include "rows.cuh"
 
 namespace det {
 
@@ -14,9 +15,10 @@ constexpr int ADAM8_JOBS = 128;           // tensors per launch
 constexpr float A8_127 = 0x1.020408p-7f, A8_255 = 0x1.010102p-8f;     // 1/127, 1/255
 
 struct Adam8Scalars { float b1, b2, omb1, omb2, eps, stepsz, isb2, decay; };
-// Job j: warps first[j] .. first[j + 1] - 1 of the launch, each with 256 of its len[j] values.  s NULL: moments in 32 bits.
+// Job j: CTAs first[j] .. first[j + 1] - 1 of the launch, each with `rounds` times 2048 of its len[j] values, 256 a warp and round.  A job belongs to whole
+// CTAs, and its entries, constants at an index, are read once for all rounds.  s NULL: moments in 32 bits.
 struct Adam8Jobs {
-  int n;
+  int n, rounds;
   uint32_t first[ADAM8_JOBS + 1];
   const void *p[ADAM8_JOBS], *m[ADAM8_JOBS], *v[ADAM8_JOBS];
   const float* s[ADAM8_JOBS];
@@ -36,19 +38,27 @@ __device__ __forceinline__ float a8_root(int c, float s) {
   const float t = fmul(__int2float_rn(c), A8_255);
   return fmul(s, fmul(t, t));
 }
+// fsqrt and fdiv; a zero, which sends a whole warp through the compiler's path for special operands, is answered beside them.  A value in fifty that is
+// zero (weights that have had no gradient) is in every second warp.
+__device__ __forceinline__ float a8_sqrt(float x) { return x > 0.0f ? fsqrt(x > 0.0f ? x : 1.0f) : fmul(x, x); }         // x is never negative, but may be a NaN
+__device__ __forceinline__ float a8_div(float a, float b) {
+  const bool plain = a == 0.0f && b > 0.0f;                               // 0 / b is that zero
+  const float q = fdiv(plain ? 1.0f : a, plain ? 1.0f : b);
+  return plain ? a : q;
+}
 // the scale of a block from its largest magnitude's bits: NaN where a value is not finite
 __device__ __forceinline__ float a8_scale(uint32_t amax) { return amax >= 0x7f800000u ? __int_as_float(0x7fffffff) : __uint_as_float(amax); }
 __device__ __forceinline__ float a8_inverse(float s) { return s > 0.0f ? fdiv(1.0f, s) : 0.0f; }
 // a share of at most 1 (1 + 2^-23), so the code needs no clamp
-__device__ __forceinline__ int a8_code(float x, float inv, float top) { return __float2int_rn(fmul(fsqrt(fmul(x, inv)), top)); }
-__device__ __forceinline__ uint32_t a8_bytes(int a, int b, int c, int d) {
-  return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
+__device__ __forceinline__ int a8_code(float x, float inv, float top) { return __float2int_rn(fmul(a8_sqrt(fmul(x, inv)), top)); }
+__device__ __forceinline__ uint32_t t4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {      // four low bytes
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 
-// Four adjacent values from i on, `n` of them there.
-template <bool BF>
+// Four adjacent values from i on, `n` of them there; FULL: all four, in the block of a tensor that has all its 256.
+template <bool FULL, bool BF>
 __device__ __forceinline__ void a8_load_p(const void* p, size_t i, int n, float v[4]) {
-  if (n >= 4) {
+  if (FULL || n >= 4) {
     if (BF) {
       const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
       v[0] = bflo(u.x); v[1] = bfhi(u.x); v[2] = bflo(u.y); v[3] = bfhi(u.y);
@@ -61,79 +71,132 @@ __device__ __forceinline__ void a8_load_p(const void* p, size_t i, int n, float 
 #pragma unroll
   for (int k = 0; k < 4; ++k) v[k] = k < n ? (BF ? bf2f(static_cast<const uint16_t*>(p)[i + k]) : static_cast<const float*>(p)[i + k]) : 0.0f;
 }
-template <bool BF>
-__device__ __forceinline__ void a8_store_p(void* p, size_t i, int n, const float v[4]) {
-  if (n >= 4) {
-    if (BF) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]));
-    else *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
-    return;
-  }
+template <bool FULL>
+__device__ __forceinline__ void a8_store_f(void* p, size_t i, int n, const float v[4]) {
+  if (FULL || n >= 4) { *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]); return; }
 #pragma unroll
   for (int k = 0; k < 4; ++k)
-    if (k < n) {
-      if (BF) static_cast<uint16_t*>(p)[i + k] = f2bf(v[k]);
-      else static_cast<float*>(p)[i + k] = v[k];
-    }
+    if (k < n) static_cast<float*>(p)[i + k] = v[k];
 }
+template <bool FULL>
+__device__ __forceinline__ void a8_store_bf(void* p, size_t i, int n, uint32_t a, uint32_t b) {
+  if (FULL || n >= 4) { *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(a, b); return; }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (k < n) static_cast<uint16_t*>(p)[i + k] = (uint16_t)((k < 2 ? a : b) >> (16 * (k & 1)));
+}
+template <bool FULL>
 __device__ __forceinline__ uint32_t a8_load_codes(const void* p, size_t i, int n) {
-  if (n >= 4) return *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i);
+  if (FULL || n >= 4) return *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i);
   uint32_t u = 0;
   for (int k = 0; k < n; ++k) u |= (uint32_t)static_cast<const uint8_t*>(p)[i + k] << (8 * k);
   return u;
 }
+template <bool FULL>
 __device__ __forceinline__ void a8_store_codes(void* p, size_t i, int n, uint32_t u) {
-  if (n >= 4) { *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = u; return; }
+  if (FULL || n >= 4) { *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = u; return; }
   for (int k = 0; k < n; ++k) static_cast<uint8_t*>(p)[i + k] = (uint8_t)(u >> (8 * k));
 }
-// moments of a warp's 256 values into codes
-__device__ __forceinline__ void a8_put(const float (&m)[8], const float (&r)[8], int lane, size_t i0, const int (&n)[2], int8_t* m8, uint8_t* v8, float2* s) {
-  uint32_t am = 0, ar = 0;
+// Square roots and a quotient of two or three roundings for every value hold the issue slots longer than the memory takes, and a code needs none of
+// them: it is the same for every t nearer to the exact one than t is to a border between codes.  So t is made from the hardware's approximation
+// (sqrt.approx and rcp.approx: 2^-23 of the value at most), which can be off by `off` in all, and where a border is nearer than that, some value in
+// four thousand, the exact steps are taken.
+__device__ __forceinline__ float a8_sqrt_near(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float a8_rcp_near(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// the code of t in the low byte; far: how far t is from it, at most
+__device__ __forceinline__ uint32_t a8_rounded(float t, float& far) {
+  const float k = fadd(t, 12582912.0f);
+  far = fmaxf(far, fabsf(fsub(t, fsub(k, 12582912.0f))));
+  return __float_as_uint(k);
+}
+// Off by: sqrt.approx for fsqrt 1.5 * 2^-23, the product with 127 another 2^-23: 127 * 2.5 * 2^-23 < 2^-14.  Of r: r itself 1.5 and its share 1 more, halved by
+// the root, whose own 1.5, the product's 1: 255 * 3.75 * 2^-23 < 1.5 * 2^-13.
+constexpr float A8_OFF_M = 0x1p-14f, A8_OFF_R = 0x1.8p-13f;
+// The moments of a warp's 256 values into codes: m, v = r r in binary32 (r near by: a8_sqrt_near(v)).
+template <bool FULL>
+__device__ __forceinline__ void a8_put(const float (&m)[8], const float (&v)[8], const float (&near)[8], int lane, size_t i0, const int (&n)[2], int8_t* m8,
+                                       uint8_t* v8, float2* s) {
+  uint32_t am = 0, av = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     am = max(am, __float_as_uint(m[k]) & 0x7fffffffu);
-    ar = max(ar, __float_as_uint(r[k]) & 0x7fffffffu);
+    av = max(av, __float_as_uint(v[k]));                                  // a negative v counts as not finite, as its root is
   }
   am = __reduce_max_sync(0xffffffffu, am);
-  ar = __reduce_max_sync(0xffffffffu, ar);
-  const float sm = a8_scale(am), sr = a8_scale(ar), im = a8_inverse(sm), ir = a8_inverse(sr);
-  const bool fm = am < 0x7f800000u, fr = ar < 0x7f800000u;
+  av = __reduce_max_sync(0xffffffffu, av);
+  // the largest root is the root of the largest
+  const float sm = a8_scale(am), sr = av >= 0x7f800000u ? __int_as_float(0x7fffffff) : a8_sqrt(__uint_as_float(av)), im = a8_inverse(sm), ir = a8_inverse(sr);
+  const uint32_t fm = am < 0x7f800000u ? ~0u : 0u, fr = av < 0x7f800000u ? ~0u : 0u;
   if (lane == 0) *s = make_float2(sm, sr);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    int a[4], b[4];
+    uint32_t a[4], b[4];
+    float far_m = 0.0f, far_r = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float mv = m[4 * h + k], rv = r[4 * h + k];
-      const int c = a8_code(fabsf(mv), im, 127.0f), d = a8_code(rv, ir, 255.0f);
-      a[k] = fm ? (mv < 0.0f ? -c : c) : 0;
-      b[k] = fr ? (rv > 0.0f ? max(d, 1) : d) : 0;
+      const float mv = m[4 * h + k], w = near[4 * h + k];
+      const float tm = fmul(a8_sqrt_near(fmul(fabsf(mv), im)), 127.0f), tr = fmul(a8_sqrt_near(fmul(w, ir)), 255.0f);
+      a[k] = a8_rounded(copysignf(tm, mv), far_m);
+      b[k] = a8_rounded(fmaxf(tr, __saturatef(fmul(w, 0x1p100f))), far_r);      // at least 1 where r > 0, which is 2^-63 or more
     }
-    a8_store_codes(m8, i0 + 128 * h, n[h], a8_bytes(a[0], a[1], a[2], a[3]));
-    a8_store_codes(v8, i0 + 128 * h, n[h], a8_bytes(b[0], b[1], b[2], b[3]));
+    if (far_m > 0.5f - A8_OFF_M || far_r > 0.5f - A8_OFF_R) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float mv = m[4 * h + k], vv = v[4 * h + k];
+        const int c = a8_code(fabsf(mv), im, 127.0f);
+        a[k] = (uint32_t)(mv < 0.0f ? -c : c);
+        b[k] = (uint32_t)max(a8_code(a8_sqrt(vv), ir, 255.0f), vv > 0.0f ? 1 : 0);
+      }
+    }
+    a8_store_codes<FULL>(m8, i0 + 128 * h, n[h], t4(a[0], a[1], a[2], a[3]) & fm);
+    a8_store_codes<FULL>(v8, i0 + 128 * h, n[h], t4(b[0], b[1], b[2], b[3]) & fr);
   }
 }
 
-template <bool BF, bool EIGHT>
-__device__ __forceinline__ void adam8_block(const Adam8Jobs& jobs, int j, float coef, bool clip, size_t base, int lane) {
-  const Adam8Scalars h = jobs.h[j];
-  const size_t len = jobs.len[j], i0 = base + lane * 4;
+// p moved by the moments, exactly as det_adamw_step
+__device__ __forceinline__ float a8_moved(const Adam8Scalars& h, float p, float m, float root) {
+  return fsub(fmul(p, h.decay), fmul(h.stepsz, a8_div(m, fadd(fmul(root, h.isb2), h.eps))));
+}
+// A job's entries
+struct Adam8Job {
+  const void *p, *m, *v;
+  const float* s;
+  float* g;
+  void *po, *mo, *vo;
+  float* so;
+  size_t len;
+  Adam8Scalars h;
+};
+// a warp's 256 values from `base` on
+template <bool FULL, bool BF, bool EIGHT>
+__device__ __forceinline__ void adam8_block(const Adam8Job& job, float coef, bool clip, size_t base, int lane) {
+  const Adam8Scalars& h = job.h;
+  const size_t i0 = base + lane * 4;
   int n[2];
-  float p[8], g[8], m[8], r[8];
-  uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
-  float2 s = make_float2(0.0f, 0.0f);
-  if (EIGHT) s = reinterpret_cast<const float2*>(jobs.s[j])[base / A8_VALUES];
+  float p[8], g[8], m[8], v[8], near[8];
+  uint32_t cm[2], cv[2];
+  float2 s;
+  if (EIGHT) s = reinterpret_cast<const float2*>(job.s)[base / A8_VALUES];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const size_t i = i0 + 128 * q;
-    n[q] = i + 4 <= len ? 4 : i < len ? (int)(len - i) : 0;
-    a8_load_p<BF>(jobs.p[j], i, n[q], p + 4 * q);
-    a8_load_p<false>(jobs.g[j], i, n[q], g + 4 * q);
+    n[q] = FULL || i + 4 <= job.len ? 4 : i < job.len ? (int)(job.len - i) : 0;
+    a8_load_p<FULL, BF>(job.p, i, n[q], p + 4 * q);
+    a8_load_p<FULL, false>(job.g, i, n[q], g + 4 * q);
     if (EIGHT) {
-      cm[q] = a8_load_codes(jobs.m[j], i, n[q]);
-      cv[q] = a8_load_codes(jobs.v[j], i, n[q]);
+      cm[q] = a8_load_codes<FULL>(job.m, i, n[q]);
+      cv[q] = a8_load_codes<FULL>(job.v, i, n[q]);
     } else {
-      a8_load_p<false>(jobs.m[j], i, n[q], m + 4 * q);
-      a8_load_p<false>(jobs.v[j], i, n[q], r + 4 * q);
+      a8_load_p<FULL, false>(job.m, i, n[q], m + 4 * q);
+      a8_load_p<FULL, false>(job.v, i, n[q], v + 4 * q);
     }
   }
 #pragma unroll
@@ -141,108 +204,159 @@ __device__ __forceinline__ void adam8_block(const Adam8Jobs& jobs, int j, float 
     if (EIGHT) {
       m[k] = a8_first((int)(int8_t)(cm[k >> 2] >> (8 * (k & 3))), s.x);
       const float w = a8_root((int)(uint8_t)(cv[k >> 2] >> (8 * (k & 3))), s.y);
-      r[k] = fmul(w, w);
+      v[k] = fmul(w, w);
     }
     if (clip) g[k] = fmul(g[k], coef);
     m[k] = fadd(fmul(h.b1, m[k]), fmul(h.omb1, g[k]));
-    const float v = fadd(fmul(h.b2, r[k]), fmul(h.omb2, fmul(g[k], g[k]))), root = fsqrt(v);
-    p[k] = fsub(fmul(p[k], h.decay), fmul(h.stepsz, fdiv(m[k], fadd(fmul(root, h.isb2), h.eps))));
-    r[k] = EIGHT ? root : v;
+    v[k] = fadd(fmul(h.b2, v[k]), fmul(h.omb2, fmul(g[k], g[k])));
+    if (EIGHT) near[k] = a8_sqrt_near(v[k]);
+  }
+  if (clip) {
+    a8_store_f<FULL>(job.g, i0, n[0], g);
+    a8_store_f<FULL>(job.g, i0 + 128, n[1], g + 4);
   }
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    const size_t i = i0 + 128 * q;
-    a8_store_p<BF>(jobs.po[j], i, n[q], p + 4 * q);
-    if (clip) a8_store_p<false>(jobs.g[j], i, n[q], g + 4 * q);
     if (!EIGHT) {
-      a8_store_p<false>(jobs.mo[j], i, n[q], m + 4 * q);
-      a8_store_p<false>(jobs.vo[j], i, n[q], r + 4 * q);
+      a8_store_f<FULL>(job.mo, i0 + 128 * q, n[q], m + 4 * q);
+      a8_store_f<FULL>(job.vo, i0 + 128 * q, n[q], v + 4 * q);
     }
+    float to[4];
+    bool exact = !(BF && EIGHT);
+    if (BF && EIGHT) {
+      // The bf16 that the moved parameter is rounded to is nearly always that of every number near it.  With the approximations for root and quotient the
+      // step is off by 6.5 * 2^-23 of itself, the difference's own rounding comes on top, and what is flushed on the way.  Where the ends of that interval
+      // are rounded to two numbers, some value in eight thousand, or where eps is no small positive number, the exact steps are taken.
+      exact = !(h.eps >= 0.0f && h.eps < 0x1p90f);
+      uint32_t ends[2][2];
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        float lo[2], hi[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = 4 * q + k + e;
+          const float step = fmul(h.stepsz, fmul(m[i], a8_rcp_near(fadd(fmul(near[i], h.isb2), h.eps))));
+          const float x = fsub(fmul(p[i], h.decay), step), off = __fmaf_rn(fabsf(x), 0x1p-22f, __fmaf_rn(fabsf(step), 0x1p-20f, 0x1p-100f));
+          to[k + e] = x;
+          lo[e] = fsub(x, off);
+          hi[e] = fadd(x, off);
+        }
+        ends[k / 2][0] = bf_pair(lo[0], lo[1]);
+        ends[k / 2][1] = bf_pair(hi[0], hi[1]);
+      }
+      exact = exact || ends[0][0] != ends[0][1] || ends[1][0] != ends[1][1];
+    }
+    if (exact) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) to[k] = a8_moved(h, p[4 * q + k], m[4 * q + k], a8_sqrt(v[4 * q + k]));
+    }
+    if (BF) a8_store_bf<FULL>(job.po, i0 + 128 * q, n[q], bf_pair(to[0], to[1]), bf_pair(to[2], to[3]));
+    else a8_store_f<FULL>(job.po, i0 + 128 * q, n[q], to);
   }
   if (EIGHT) {
+    if (!FULL) {                                                          // the end of the tensor: nothing behind it counts
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if ((k & 3) >= n[k >> 2]) m[k] = r[k] = 0.0f;                       // behind the last value
-    a8_put(m, r, lane, i0, n, static_cast<int8_t*>(jobs.mo[j]), static_cast<uint8_t*>(jobs.vo[j]), reinterpret_cast<float2*>(jobs.so[j]) + base / A8_VALUES);
+      for (int k = 0; k < 8; ++k)
+        if ((k & 3) >= n[k >> 2]) m[k] = v[k] = near[k] = 0.0f;
+    }
+    a8_put<FULL>(m, v, near, lane, i0, n, static_cast<int8_t*>(job.mo), static_cast<uint8_t*>(job.vo), reinterpret_cast<float2*>(job.so) + base / A8_VALUES);
   }
 }
-__device__ __forceinline__ int a8_job(const uint32_t* first, int n, uint32_t w) {      // the last job whose first warp is <= w
+template <bool BF, bool EIGHT>
+__device__ __forceinline__ void adam8_rounds(const Adam8Job& job, float coef, bool clip, size_t base, int rounds, int lane) {
+#pragma unroll 1
+  for (int r = 0; r < rounds && base < job.len; ++r, base += 8 * A8_VALUES) {
+    if (base + A8_VALUES <= job.len) adam8_block<true, BF, EIGHT>(job, coef, clip, base, lane);
+    else adam8_block<false, BF, EIGHT>(job, coef, clip, base, lane);
+  }
+}
+__device__ __forceinline__ int a8_job(const uint32_t* first, int n) {      // the last job whose first CTA is <= this one
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= w) lo = mid; else hi = mid - 1;
+    if (first[mid] <= blockIdx.x) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
 __global__ void __launch_bounds__(256) k_adamw8(const __grid_constant__ Adam8Jobs jobs, const float* __restrict__ coef) {
   grid_dep();
-  const uint32_t w = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (w >= jobs.first[jobs.n]) return;
-  const int j = a8_job(jobs.first, jobs.n, w), lane = threadIdx.x & 31;
-  const size_t base = (size_t)(w - jobs.first[j]) * A8_VALUES;
+  const int j = a8_job(jobs.first, jobs.n), lane = threadIdx.x & 31;
+  const size_t base = ((size_t)(blockIdx.x - jobs.first[j]) * (8 * jobs.rounds) + (threadIdx.x >> 5)) * A8_VALUES;
+  const Adam8Job job = {jobs.p[j], jobs.m[j], jobs.v[j], jobs.s[j], jobs.g[j], jobs.po[j], jobs.mo[j], jobs.vo[j], jobs.so[j], jobs.len[j], jobs.h[j]};
+  if (base >= job.len) return;
   const bool clip = coef != nullptr;
   const float c = clip ? coef[0] : 1.0f;
-  if (jobs.s[j]) {
-    if (jobs.bf[j]) adam8_block<true, true>(jobs, j, c, clip, base, lane);
-    else adam8_block<false, true>(jobs, j, c, clip, base, lane);
+  if (job.s) {
+    if (jobs.bf[j]) adam8_rounds<true, true>(job, c, clip, base, jobs.rounds, lane);
+    else adam8_rounds<false, true>(job, c, clip, base, jobs.rounds, lane);
   } else {
-    if (jobs.bf[j]) adam8_block<true, false>(jobs, j, c, clip, base, lane);
-    else adam8_block<false, false>(jobs, j, c, clip, base, lane);
+    if (jobs.bf[j]) adam8_rounds<true, false>(job, c, clip, base, jobs.rounds, lane);
+    else adam8_rounds<false, false>(job, c, clip, base, jobs.rounds, lane);
   }
 }
 
 // Codes to numbers and back, many tensors at once.
 struct Adam8Numbers {
-  int n;
+  int n, rounds;
   uint32_t first[ADAM8_JOBS + 1];
   int8_t* m8[ADAM8_JOBS];
   uint8_t* v8[ADAM8_JOBS];
   float *s[ADAM8_JOBS], *m[ADAM8_JOBS], *v[ADAM8_JOBS];
   size_t len[ADAM8_JOBS];
 };
-template <bool PACK>
-__global__ void __launch_bounds__(256) k_adamw8_numbers(const __grid_constant__ Adam8Numbers jobs) {
-  grid_dep();
-  const uint32_t w = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (w >= jobs.first[jobs.n]) return;
-  const int j = a8_job(jobs.first, jobs.n, w), lane = threadIdx.x & 31;
-  const size_t base = (size_t)(w - jobs.first[j]) * A8_VALUES, len = jobs.len[j], i0 = base + lane * 4;
+template <bool PACK, bool FULL>
+__device__ __forceinline__ void adam8_numbers(const Adam8Numbers& jobs, int j, size_t base, size_t len, int lane) {
+  const size_t i0 = base + lane * 4;
   float2* s = reinterpret_cast<float2*>(jobs.s[j]) + base / A8_VALUES;
   int n[2];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) n[q] = i0 + 128 * q + 4 <= len ? 4 : i0 + 128 * q < len ? (int)(len - i0 - 128 * q) : 0;
-  float m[8], r[8];
+  for (int q = 0; q < 2; ++q) n[q] = FULL || i0 + 128 * q + 4 <= len ? 4 : i0 + 128 * q < len ? (int)(len - i0 - 128 * q) : 0;
+  float m[8], v[8];
   if (PACK) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      a8_load_p<false>(jobs.m[j], i0 + 128 * q, n[q], m + 4 * q);
-      a8_load_p<false>(jobs.v[j], i0 + 128 * q, n[q], r + 4 * q);
+      a8_load_p<FULL, false>(jobs.m[j], i0 + 128 * q, n[q], m + 4 * q);
+      a8_load_p<FULL, false>(jobs.v[j], i0 + 128 * q, n[q], v + 4 * q);
     }
+    float near[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       m[k] = fmul(m[k], 1.0f);                                            // a subnormal number counts as zero
-      r[k] = fsqrt(r[k]);
+      v[k] = fadd(v[k], 0.0f);                                            // and -0 as +0
+      near[k] = a8_sqrt_near(v[k]);
     }
-    a8_put(m, r, lane, i0, n, jobs.m8[j], jobs.v8[j], s);
+    a8_put<FULL>(m, v, near, lane, i0, n, jobs.m8[j], jobs.v8[j], s);
   } else {
     const float2 sc = *s;
     uint32_t cm[2], cv[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      cm[q] = a8_load_codes(jobs.m8[j], i0 + 128 * q, n[q]);
-      cv[q] = a8_load_codes(jobs.v8[j], i0 + 128 * q, n[q]);
+      cm[q] = a8_load_codes<FULL>(jobs.m8[j], i0 + 128 * q, n[q]);
+      cv[q] = a8_load_codes<FULL>(jobs.v8[j], i0 + 128 * q, n[q]);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       m[k] = a8_first((int)(int8_t)(cm[k >> 2] >> (8 * (k & 3))), sc.x);
-      const float w2 = a8_root((int)(uint8_t)(cv[k >> 2] >> (8 * (k & 3))), sc.y);
-      r[k] = fmul(w2, w2);
+      const float r = a8_root((int)(uint8_t)(cv[k >> 2] >> (8 * (k & 3))), sc.y);
+      v[k] = fmul(r, r);
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      a8_store_p<false>(jobs.m[j], i0 + 128 * q, n[q], m + 4 * q);
-      a8_store_p<false>(jobs.v[j], i0 + 128 * q, n[q], r + 4 * q);
+      a8_store_f<FULL>(jobs.m[j], i0 + 128 * q, n[q], m + 4 * q);
+      a8_store_f<FULL>(jobs.v[j], i0 + 128 * q, n[q], v + 4 * q);
     }
+  }
+}
+template <bool PACK>
+__global__ void __launch_bounds__(256) k_adamw8_numbers(const __grid_constant__ Adam8Numbers jobs) {
+  grid_dep();
+  const int j = a8_job(jobs.first, jobs.n), lane = threadIdx.x & 31;
+  const size_t len = jobs.len[j];
+  size_t base = ((size_t)(blockIdx.x - jobs.first[j]) * (8 * jobs.rounds) + (threadIdx.x >> 5)) * A8_VALUES;
+#pragma unroll 1
+  for (int round = 0; round < jobs.rounds && base < len; ++round, base += 8 * A8_VALUES) {
+    if (base + A8_VALUES <= len) adam8_numbers<PACK, true>(jobs, j, base, len, lane);
+    else adam8_numbers<PACK, false>(jobs, j, base, len, lane);
   }
 }
 
@@ -269,19 +383,23 @@ static bool a8_moments_at(const void* m, const void* v, const void* s) {
 // the tensors t, t + 1, ... as jobs of one launch: fill(job, tensor) for each that has values
 template <class Jobs, class Fill>
 static int a8_take(Jobs& jobs, int& t, int ntensors, const size_t* n, Fill fill) {
-  size_t w = 0;
+  // four rounds a CTA where the CTAs fill the GPU some times over all the same
+  size_t ctas = 0, total = 0;
+  for (int i = t; i < ntensors; ++i) total += n[i] / (8 * A8_VALUES);
   jobs.n = 0;
+  jobs.rounds = total >= 16384 ? 4 : 1;
+  const size_t per = (size_t)8 * A8_VALUES * jobs.rounds;
   for (; t < ntensors && jobs.n < ADAM8_JOBS; ++t) {
     if (!n[t]) continue;
-    const size_t warps = (n[t] + A8_VALUES - 1) / A8_VALUES;
-    if (w + warps > 0x7fffffffull) break;                                  // its own is checked before
-    jobs.first[jobs.n] = (uint32_t)w;
+    const size_t each = (n[t] + per - 1) / per;
+    if (ctas + each > 0x7fffffffull) break;                                // one tensor alone is within that, see the callers
+    jobs.first[jobs.n] = (uint32_t)ctas;
     jobs.len[jobs.n] = n[t];
     fill(jobs.n++, t);
-    w += warps;
+    ctas += each;
   }
-  jobs.first[jobs.n] = (uint32_t)w;
-  return (int)((w + 7) / 8);
+  jobs.first[jobs.n] = (uint32_t)ctas;
+  return (int)ctas;
 }
 }  // namespace det
 
