@@ -12,7 +12,7 @@ CSRC = os.path.join(_DIR, "csrc")
 OUT = os.path.join(_DIR, "libdet.so")
 BINDING = os.path.join(_DIR, "_binding.so")
 SOURCES = ["reduce.cu", "norm_loss.cu", "glue_optim.cu", "hash.cu", "igemm.cu", "lsq.cu", "ogemm.cu", "attn.cu", "attn_pv8.cu", "headops.cu", "sum_static.cu", "lmhead_v2.cu", "attn_v2.cu", "layernorm.cu", "act8.cu", "linrec.cu", "tok8.cu", "adamw8.cu"]
-HEADERS = ["common.cuh", "internal.h", "rows.cuh", "ogemm_core.cuh", "attn_core.cuh", "tc05.cuh", "v2_slice.cuh", os.path.join("..", "..", "include", "det.h"),
+HEADERS = ["common.cuh", "internal.h", "rows.cuh", "sigmoid.cuh", "ogemm_core.cuh", "attn_core.cuh", "tc05.cuh", "v2_slice.cuh", os.path.join("..", "..", "include", "det.h"),
            os.path.join("..", "..", "include", "det_test.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-fmad=false",
               "-ftz=true", "-prec-div=true", "-prec-sqrt=true", "-Xcompiler", "-fPIC"]

@@ -4,6 +4,7 @@
 #include "common.cuh"
 #include "internal.h"
 #include "rows.cuh"
+#include "sigmoid.cuh"
 
 namespace det {
 
@@ -131,59 +132,6 @@ __global__ void __launch_bounds__(256) k_a8_unpack_any(const int8_t* __restrict_
 // signs.  They are evaluated by the compiler, with the steps of the formula, and looked up in shared memory: with an exponential and a division for every
 // value the three kernels took 160, 133 and 152 us for 8192 x 8192, bound by the arithmetic; now 92, 76 and 92 (each over and over; the three in turn on the same tensors 284), where the
 // bytes alone would take 83, 42 and 83 at the measured copy's rate.
-constexpr int SG_LOW = 0x3280, SG_TOP = 0x4300, SG_TAB = (SG_TOP - SG_LOW + 1 + 255) / 256 * 256;
-struct __align__(16) SgTable { float v[2 * SG_TAB]; };     // of positive gates, of negative ones
-constexpr float sg_at(int bits, bool negative) {
-  float x = 1.0f + (bits & 127) / 128.0f;
-  for (int e = bits >> 7; e > 127; --e) x *= 2.0f;
-  for (int e = bits >> 7; e < 127; ++e) x *= 0.5f;
-  if (!negative) x = -x;
-  if (x > 0x1.62e42ep+6f) return 0.0f;                     // x: -gate
-  const float d = 1.0f + det_exp_at(x), q = 1.0f / d;
-  return q < 0x1p-126f ? 0.0f : q;
-}
-// Where entry i lies: a code below 64 has fractions that end in zeros, and in order of the magnitude they would meet in a few banks of shared memory.
-constexpr int sg_place(int i) { return i ^ ((i >> 3) & 31); }
-constexpr SgTable sg_make_table() {
-  SgTable t{};
-  for (int i = 0; i < SG_TAB; ++i) {
-    t.v[sg_place(i)] = sg_at(SG_LOW + i, false);
-    t.v[SG_TAB + sg_place(i)] = sg_at(SG_LOW + i, true);
-  }
-  return t;
-}
-__device__ constexpr SgTable sg_table_image = sg_make_table();
-
-// the sigmoid of a gate; by table a NaN has that of an infinity, and what it is multiplied with, the gate itself, is the NaN
-// (TAB 0: by the formula, 1: by table in order, for gates with any fractions, 2: by table in its places)
-template <int TAB>
-__device__ __forceinline__ float sigmoid_a8(float g, const float* tab) {
-  if (!TAB) return fdiv(1.0f, fadd(1.0f, det_exp(-g)));
-  const uint32_t u = __float_as_uint(g);
-  int i = __vimin_s32_relu((int)((u >> 14) & 0x1fffcu) - 4 * SG_LOW, 4 * (SG_TOP - SG_LOW));           // in bytes
-  if (TAB == 2) i ^= (i >> 3) & 0x7c;
-  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tab) + i + (int)(u >> 31) * (4 * SG_TAB));
-}
-template <int TAB>
-__device__ __forceinline__ void sg_copy_table(float* tab) {
-  if (!TAB) return;
-  for (int i = threadIdx.x; i < 2 * SG_TAB / 4; i += 256) {
-    const float4 v = reinterpret_cast<const float4*>(sg_table_image.v)[i];
-    if (TAB == 2) {
-      reinterpret_cast<float4*>(tab)[i] = v;
-    } else {   // SG_TAB is a multiple of 256, so a place is undone in either half alike
-      const float w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        int at = 4 * i + k;
-        at ^= (at >> 3) & 28;                            // undoes the upper three of the five bits, which the lower two came from
-        at ^= (at >> 3) & 3;
-        tab[at] = w[k];
-      }
-    }
-  }
-  __syncthreads();
-}
 // Eight adjacent gates and their ups on their way: of gu, or codes and fields of the checkpoint; dh beside them in the backward pass.
 struct SgRaw {
   uint4 g, u, d;

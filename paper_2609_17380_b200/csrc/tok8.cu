@@ -10,6 +10,7 @@
 #include "tc05.cuh"
 #include "internal.h"
 #include "rows.cuh"
+#include "sigmoid.cuh"
 
 namespace det {
 
@@ -124,106 +125,237 @@ __global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__
 }
 
 // ---- operands of the backward products ---------------------------------------------------------------------
-// dY [M, N] with the scales of the channels (A) and of the tokens (G).  Largest magnitudes first: a warp reads 256 columns of a row, a CTA 128 rows.
-__device__ __forceinline__ void t8_load8(const uint16_t* p, size_t at, int n, bool vec, float v[8]) {
-  if (vec && n >= 8) { load8<true>(p, at, v); return; }
+// The gradient of the product's output, [M, N], with the scales of the channels (A) and of the tokens (G).  It is dY itself, or (GLU) what the activation
+// makes of dh [M, F] and the kept gu [M, 2F], N = 2F, rounded to bf16.  The pass over the largest magnitudes stores that one for the pass over the codes:
+// worked out again there it would cost 2 bytes a pair less, but both passes are then bound by their instructions (8192 x 8192: 124 + 168 us).
+struct T8Grad {
+  const uint16_t *d, *gu;
+  size_t ld, ld_gu;
+  const float *s_x, *s_w;
+  uint16_t* dgu;                          // GLU: the gradient, rows ld_dgu apart
+  size_t ld_dgu;
+  int M, N, W;                            // W: columns of d, N or N / 2
+  int vec;                                // rows in whole pieces of four
+};
+// Four adjacent values from `at` on, n of them there; FULL: all, in one piece.
+template <bool FULL>
+__device__ __forceinline__ uint2 t8_load4(const uint16_t* p, size_t at, int n, int vec) {
+  if (FULL || (vec && n >= 4)) return __ldg(reinterpret_cast<const uint2*>(p + at));
+  uint32_t w[4];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) v[t] = t < n ? bf2f(p[at + t]) : 0.0f;
+  for (int t = 0; t < 4; ++t) w[t] = t < n ? p[at + t] : 0u;
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
-constexpr int T8_GR = 128;
-__global__ void __launch_bounds__(256) k_t8_grad_max(const uint16_t* __restrict__ dy, size_t ld, int M, int N, const float* __restrict__ s_x,
-                                                     const float* __restrict__ s_w, uint32_t* __restrict__ rowmax, uint32_t* __restrict__ colmax, int vec) {
-  grid_dep();
-  __shared__ uint32_t cols[8][256];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 256 + lane * 8, r0 = blockIdx.y * T8_GR;
-  const int left = N - c;
-  float sw[8];
-  uint32_t cm[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    sw[t] = t < left ? s_w[c + t] : 0.0f;
-    cm[t] = 0;
+// Four columns of both halves of a row of the gradient (GLU: gates' and ups', else columns 64 apart), on their way and as bf16 pairs.
+template <bool GLU>
+struct T8Raw { uint2 d, e, u; };         // GLU: dh, gate, up; else both halves of dY
+template <bool FULL, bool GLU>
+__device__ __forceinline__ void t8_fetch(const T8Grad& x, size_t r, const int (&at)[2], const int (&left)[2], T8Raw<GLU>& w) {
+  w.d = t8_load4<FULL>(x.d, r * x.ld + at[0], left[0], x.vec);
+  if (GLU) {
+    w.e = t8_load4<FULL>(x.gu, r * x.ld_gu + at[0], left[0], x.vec);
+    w.u = t8_load4<FULL>(x.gu, r * x.ld_gu + x.W + at[0], left[0], x.vec);
+  } else {
+    w.e = t8_load4<FULL>(x.d, r * x.ld + at[1], left[1], x.vec);
   }
-#pragma unroll 4
-  for (int i = 0; i < T8_GR / 8; ++i) {
-    const int r = r0 + i * 8 + warp;
-    if (r >= M) break;
-    float v[8];
-    t8_load8(dy, (size_t)r * ld + c, left, vec, v);
-    const float sx = s_x[r];
-    uint32_t rm = 0;
+}
+template <bool GLU, int TAB>
+__device__ __forceinline__ void t8_grad4(const T8Raw<GLU>& w, const float* tab, uint2 (&v)[2]) {
+  if (!GLU) { v[0] = w.d; v[1] = w.e; return; }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      if (t >= left) break;
-      rm = max(rm, __float_as_uint(fmul(v[t], sw[t])) & 0x7fffffffu);
-      cm[t] = max(cm[t], __float_as_uint(fmul(v[t], sx)) & 0x7fffffffu);
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t dd = k ? w.d.y : w.d.x, gg = k ? w.e.y : w.e.x, uu = k ? w.u.y : w.u.x;
+    float dg[2], du[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float d = t ? bfhi(dd) : bflo(dd), g = t ? bfhi(gg) : bflo(gg), u = t ? bfhi(uu) : bflo(uu), sg = sigmoid_a8<TAB>(g, tab);
+      du[t] = fmul(d, fmul(g, sg));
+      dg[t] = fmul(fmul(d, u), fmul(sg, fadd(1.0f, fmul(g, fsub(1.0f, sg)))));
     }
-    rm = __reduce_max_sync(0xffffffffu, rm);
-    if (lane == 0) atomicMax(rowmax + r, rm);
+    (k ? v[0].y : v[0].x) = bf_pair(dg[0], dg[1]);
+    (k ? v[1].y : v[1].x) = bf_pair(du[0], du[1]);
   }
-#pragma unroll
-  for (int t = 0; t < 8; ++t) cols[warp][lane * 8 + t] = cm[t];
-  __syncthreads();
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  uint32_t m = 0;
-#pragma unroll
-  for (int w = 0; w < 8; ++w) m = max(m, cols[w][threadIdx.x]);
-  if (j < N) atomicMax(colmax + j, m);
 }
-// Then the codes: A as it lies, G transposed.  A thread has 8 rows of 8 columns of a tile of 128 x 128; eight codes of a column are a piece of 8 bytes
-// whose place in shared memory is swizzled by the group of columns, so that the sixteen of a warp meet in no bank.
-__global__ void __launch_bounds__(256) k_t8_grad_codes(const uint16_t* __restrict__ dy, size_t ld, int M, int N, const float* __restrict__ s_x,
-                                                       const float* __restrict__ s_w, const uint32_t* __restrict__ rowmax,
-                                                       const uint32_t* __restrict__ colmax, int8_t* __restrict__ qa, float* __restrict__ s_a,
-                                                       int8_t* __restrict__ qgt, float* __restrict__ s_g, int vec) {
-  grid_dep();
-  __shared__ __align__(16) uint8_t tile[128 * 128];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, r0 = blockIdx.y * 128, c0 = blockIdx.x * 128, c = c0 + tx * 8;
-  const int left = N - c, ldn = t8_ld(N), ldm = t8_ld(M);
-  float sw[8], ig[8];
-  bool dead_c[8];
+__device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? bfhi(t & 2 ? v.y : v.x) : bflo(t & 2 ? v.y : v.x); }
+
+// Largest magnitudes first.  A tile is 128 rows of 128 columns of either half (GLU), or of 256 columns; a warp has every eighth row, a lane four columns of
+// each half; four rows are on their way together.
+constexpr int T8_ROWS = 128;
+template <bool FULL, bool GLU, int TAB>
+__device__ __forceinline__ void t8_max_rows(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4], uint32_t (&cm)[2][4],
+                                            uint32_t* __restrict__ rowmax, const float* tab) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int i = 0; i < T8_ROWS / 8; i += 4) {
+    T8Raw<GLU> w[4];
+    float sx[4];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const uint32_t m = t < left ? colmax[c + t] : 0u;
-    const float sg = t8_scale(m);
-    sw[t] = t < left ? s_w[c + t] : 0.0f;
-    ig[t] = t8_inverse(sg);
-    dead_c[t] = m >= 0x7f800000u;
-    if (blockIdx.y == 0 && ty == 0 && t < left) s_g[c + t] = sg;
-  }
-  uint32_t piece[8][2];
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + (i + k) * 8 + warp;
+      if (!FULL && r >= x.M) { w[k].d = w[k].e = w[k].u = make_uint2(0u, 0u); sx[k] = 0.0f; continue; }
+      t8_fetch<FULL, GLU>(x, r, at, left, w[k]);
+      sx[k] = fabsf(__ldg(x.s_x + r));
+    }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t g[4][8];
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + (i + k) * 8 + warp;
+      uint2 v[2];
+      t8_grad4<GLU, TAB>(w[k], tab, v);
+      if (GLU && (FULL || r < x.M)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + ty * 8 + h * 4 + i;
-      const bool there = r < M;
-      float v[8];
-      t8_load8(dy, (size_t)r * ld + c, there ? left : 0, vec, v);
-      const uint32_t m = there ? rowmax[r] : 0u;
-      const float sa = t8_scale(m), ia = t8_inverse(sa), sx = there ? s_x[r] : 0.0f;
-      if (there && blockIdx.x == 0 && tx == 0) s_a[r] = sa;
-      float a[8];
+        for (int h = 0; h < 2; ++h) {
+          uint16_t* to = x.dgu + r * x.ld_dgu + h * x.W + at[0];
+          if (FULL) {
+            *reinterpret_cast<uint2*>(to) = v[h];
+          } else {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        a[t] = fmul(v[t], sw[t]);
-        g[i][t] = dead_c[t] || !there ? 0u : t8_code(fmul(v[t], sx), ig[t]);
+            for (int t = 0; t < 4; ++t)
+              if (t < left[0]) to[t] = (uint16_t)((t & 2 ? v[h].y : v[h].x) >> (16 * (t & 1)));
+          }
+        }
       }
-      if (there && c < ldn) *reinterpret_cast<uint2*>(qa + (size_t)r * ldn + c) = t8_codes8(a, ia, m >= 0x7f800000u);
+      uint32_t rm = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t a[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float m = fabsf(t8_at(v[h], t));                          // no factor is negative, and a NaN's bits are the largest
+          a[t] = __float_as_uint(fmul(m, sw[h][t]));
+          cm[h][t] = max(cm[h][t], __float_as_uint(fmul(m, sx[k])));
+        }
+        rm = __vimax3_u32(__vimax3_u32(rm, a[0], a[1]), a[2], a[3]);
+      }
+      rm = __reduce_max_sync(0xffffffffu, rm);
+      if (lane == 0 && (FULL || r < x.M)) atomicMax(rowmax + r, rm);
+    }
+  }
+}
+template <bool GLU, int TAB>
+__global__ void __launch_bounds__(256) k_t8_grad_max(const __grid_constant__ T8Grad x, uint32_t* __restrict__ rowmax, uint32_t* __restrict__ colmax) {
+  __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
+  __shared__ __align__(16) uint32_t cols[8][256];
+  sg_copy_table<TAB>(tab);
+  grid_dep();
+  constexpr int FW = GLU ? 128 : 256;                                     // columns of d in a tile
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int across = (x.W + FW - 1) / FW, tiles = across * ((x.M + T8_ROWS - 1) / T8_ROWS);
+#pragma unroll 1
+  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int c0 = tile % across * FW, r0 = tile / across * T8_ROWS;
+    const int at[2] = {c0 + lane * 4, c0 + lane * 4 + (GLU ? 0 : 128)}, left[2] = {x.W - at[0], x.W - at[1]};
+    float sw[2][4];
+    uint32_t cm[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        sw[h][t] = t < left[h] ? fabsf(x.s_w[(GLU ? h * x.W : 0) + at[h] + t]) : 0.0f;
+        cm[h][t] = 0;
+      }
+    if (x.vec && c0 + FW <= x.W && r0 + T8_ROWS <= x.M) t8_max_rows<true, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
+    else t8_max_rows<false, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
+    if (tile != blockIdx.x) __syncthreads();                              // the columns before have been read
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(&cols[warp][h * 128 + lane * 4]) = make_uint4(cm[h][0], cm[h][1], cm[h][2], cm[h][3]);
+    __syncthreads();
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) m = max(m, cols[w][threadIdx.x]);
+    const int c = c0 + (GLU ? threadIdx.x & 127 : threadIdx.x);
+    if (c < x.W) atomicMax(colmax + (GLU ? (threadIdx.x >> 7) * x.W : 0) + c, m);
+  }
+}
+// The scales and their inverses, once for every row and column; a scale that is a NaN has the inverse -1.
+__global__ void __launch_bounds__(256) k_t8_scales(const uint32_t* __restrict__ rowmax, const uint32_t* __restrict__ colmax, int M, int N, float* __restrict__ s_a,
+                                                   float* __restrict__ i_a, float* __restrict__ s_g, float* __restrict__ i_g) {
+  const int i = blockIdx.x * 256 + threadIdx.x + grid_dep();
+  if (i >= M + N) return;
+  const uint32_t m = i < M ? rowmax[i] : colmax[i - M];
+  const float s = t8_scale(m), inv = m >= 0x7f800000u ? -1.0f : t8_inverse(s);
+  if (i < M) { s_a[i] = s; i_a[i] = inv; }
+  else { s_g[i - M] = s; i_g[i - M] = inv; }
+}
+// Then the codes: A as it lies, G transposed.  A tile is 128 rows of 128 columns, in two halves of 64; a thread has 8 rows of 4
+// columns of each, four rows on their way together.  Eight codes of a column are a piece of 8 bytes, whose place in its row of the transposed tile is
+// swizzled by the columns' four, so that a warp's pieces meet in no bank.
+template <bool FULL>
+__device__ __forceinline__ void t8_code_rows(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4],
+                                             const float (&ig)[2][4], const float* __restrict__ i_a, int8_t* __restrict__ qa, uint32_t (&g)[2][2][4]) {
+  const int ldn = t8_ld(x.N);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    T8Raw<false> w[4];
+    float sx[4], ia[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + half * 4 + k;
+      if (!FULL && r >= x.M) { w[k].d = w[k].e = make_uint2(0u, 0u); sx[k] = 0.0f; continue; }
+      t8_fetch<FULL, false>(x, r, at, left, w[k]);
+      sx[k] = __ldg(x.s_x + r);
+      ia[k] = __ldg(i_a + r);
     }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) piece[t][h] = t8_pack4(g[0][t], g[1][t], g[2][t], g[3][t]);
-  }
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + half * 4 + k;
+      const uint2 v[2] = {w[k].d, w[k].e};
 #pragma unroll
-  for (int t = 0; t < 8; ++t) *reinterpret_cast<uint2*>(tile + (tx * 8 + t) * 128 + ((ty ^ tx) << 3)) = make_uint2(piece[t][0], piece[t][1]);
+      for (int h = 0; h < 2; ++h) {
+        uint32_t a[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float y = t8_at(v[h], t);
+          const uint32_t code = t8_code(fmul(y, sx[k]), ig[h][t]);
+          a[t] = t8_code(fmul(y, sw[h][t]), ia[k]);
+          g[h][half][t] = k == 0 ? code : __byte_perm(g[h][half][t], code, k == 1 ? 0x3240 : k == 2 ? 0x3410 : 0x4210);
+        }
+        if (!FULL && r >= x.M) continue;
+        const uint32_t q = ia[k] < 0.0f ? 0u : t8_pack4(a[0], a[1], a[2], a[3]);
+        int8_t* row = qa + (size_t)r * ldn;
+        if (FULL) {
+          *reinterpret_cast<uint32_t*>(row + at[h]) = q;
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            if (t < left[h]) row[at[h] + t] = (int8_t)(q >> (8 * t));
+          if (left[h] > 0 && left[h] <= 4)                                // the row's end, and the zeros behind it
+            for (int c = x.N; c < ldn; ++c) row[c] = 0;
+        }
+      }
+    }
+  }
+}
+__global__ void __launch_bounds__(256, 3) k_t8_grad_codes(const __grid_constant__ T8Grad x, const float* __restrict__ i_a, const float* __restrict__ i_g,
+                                                          int8_t* __restrict__ qa, int8_t* __restrict__ qgt) {
+  grid_dep();
+  __shared__ __align__(16) uint8_t out[128 * 128];
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, ldm = t8_ld(x.M), c0 = blockIdx.x * 128, r0 = blockIdx.y * 128;
+  const int at[2] = {c0 + tx * 4, c0 + tx * 4 + 64}, left[2] = {x.N - at[0], x.N - at[1]};
+  float sw[2][4], ig[2][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      sw[h][t] = t < left[h] ? x.s_w[at[h] + t] : 0.0f;
+      ig[h][t] = t < left[h] ? i_g[at[h] + t] : 0.0f;
+    }
+  uint32_t g[2][2][4];                                                    // [half of the columns][four rows][column], a byte a row
+  if (x.vec && c0 + 128 <= x.N && r0 + 128 <= x.M) t8_code_rows<true>(x, r0 + ty * 8, at, left, sw, ig, i_a, qa, g);
+  else t8_code_rows<false>(x, r0 + ty * 8, at, left, sw, ig, i_a, qa, g);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool dead = ig[h][t] < 0.0f;
+      *reinterpret_cast<uint2*>(out + (h * 64 + tx * 4 + t) * 128 + ((ty ^ tx) << 3)) = make_uint2(dead ? 0u : g[h][0][t], dead ? 0u : g[h][1][t]);
+    }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int col = i * 32 + (threadIdx.x >> 3), ch = threadIdx.x & 7, f = (col >> 3) & 15;
-    uint4 w = *reinterpret_cast<const uint4*>(tile + col * 128 + (((2 * ch) ^ (f & 14)) << 3));
+    const int k = i * 32 + (threadIdx.x >> 3), ch = threadIdx.x & 7, f = (k >> 2) & 15;
+    uint4 w = *reinterpret_cast<const uint4*>(out + k * 128 + (((2 * ch) ^ (f & 14)) << 3));
     if (f & 1) w = make_uint4(w.z, w.w, w.x, w.y);
-    if (c0 + col < N && r0 + ch * 16 < ldm) *reinterpret_cast<uint4*>(qgt + (size_t)(c0 + col) * ldm + r0 + ch * 16) = w;
+    if (c0 + k < x.N && r0 + ch * 16 < ldm) *reinterpret_cast<uint4*>(qgt + (size_t)(c0 + k) * ldm + r0 + ch * 16) = w;
   }
 }
 
@@ -278,16 +410,15 @@ __device__ __forceinline__ void t8_scaled(const uint32_t (&r)[32], float rs, con
     reinterpret_cast<uint32_t*>(o)[2 * v + 1] = bf_pair(b.x, b.y);
   }
 }
-__device__ __forceinline__ float t8_sigmoid(float g) { return fdiv(1.0f, fadd(1.0f, det_exp(-g))); }
-__device__ __forceinline__ uint32_t t8_glu2(uint32_t g, uint32_t u) {
-  const float2 sg = make_float2(t8_sigmoid(bflo(g)), t8_sigmoid(bfhi(g)));
+__device__ __forceinline__ uint32_t t8_glu2(uint32_t g, uint32_t u, const float* tab) {
+  const float2 sg = make_float2(sigmoid_a8<1>(bflo(g), tab), sigmoid_a8<1>(bfhi(g), tab));
   const float2 h = mul2(mul2(make_float2(bflo(g), bfhi(g)), sg), make_float2(bflo(u), bfhi(u)));
   return bf_pair(h.x, h.y);
 }
 // Columns j0 .. j0 + CW of the warp's 32 rows (row0 the first); GLU: the ups' accumulators lie UP columns behind the gates'.  stage: the
-// warp's own 4 KiB in shared memory, whose upper half holds the columns' scales (bf16 rows take the lower one alone).
+// warp's own staging tile in shared memory, with the columns' scales behind it.
 template <int EPI, int CW, int UP>
-__device__ __forceinline__ void t8_epilogue(const T8Out& o, uint32_t taddr, int row0, int j0, uint8_t* stage) {
+__device__ __forceinline__ void t8_epilogue(const T8Out& o, uint32_t taddr, int row0, int j0, uint8_t* stage, const float* tab) {
   float* cs = reinterpret_cast<float*>(stage + 2048);
   const int lane = threadIdx.x & 31, rows = o.I - row0;
   if (rows <= 0) return;
@@ -331,7 +462,7 @@ __device__ __forceinline__ void t8_epilogue(const T8Out& o, uint32_t taddr, int 
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       uint32_t* gp = reinterpret_cast<uint32_t*>(g) + v;
-      *gp = t8_glu2(*gp, reinterpret_cast<const uint32_t*>(u)[v]);
+      *gp = t8_glu2(*gp, reinterpret_cast<const uint32_t*>(u)[v], tab);
     }
     t8_store<4, 2>(stage, reinterpret_cast<uint8_t*>(reinterpret_cast<uint16_t*>(o.out) + row0 * o.ld + j), o.ld * 2, rows, cols, o.vec, g);
   }
@@ -339,18 +470,19 @@ __device__ __forceinline__ void t8_epilogue(const T8Out& o, uint32_t taddr, int 
 
 // Tiles of 128 x BN by one CTA, or of 256 x 256 by the two of a cluster (PAIR; each has 128 rows and stages half of the columns' operand).  The
 // columns of a GLU tile are BN / 2 gates and the ups that belong to them.  Roles, ring and waits as in igemm.cu.
-template <bool PAIR, int BN>
+template <bool PAIR, int BN, int EPI>
 struct T8Tile {
   static constexpr int BM = PAIR ? 256 : 128, BROWS = PAIR ? BN / 2 : BN;         // BROWS: rows of the columns' operand that a CTA stages
   static constexpr int STAGE_A = 128 * T8_K, STAGE_B = BROWS * T8_K, STAGE = STAGE_A + STAGE_B;
-  static constexpr int STAGES = PAIR ? 6 : (BN == 128 ? 6 : 8), EW = BN == 64 ? 4 : 8;
+  static constexpr int STAGES = (PAIR || BN == 128 ? 6 : 8) - (EPI == T8_GLU ? 1 : 0), EW = BN == 64 ? 4 : 8;    // GLU: room for the sigmoids
+  static constexpr int WARP = EPI == T8_F32 ? 4096 : 2048 + 256;                    // staging tile of a warp, and the scales of its columns
   static constexpr int THREADS = 64 + 32 * EW, TCOLS = 2 * BN;
-  static constexpr size_t SMEM = (size_t)STAGES * STAGE + EW * 4096 + 1024;
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE + EW * WARP + (EPI == T8_GLU ? 2 * SG_TAB * 4 : 0) + 1024;
 };
 template <bool PAIR, int BN, int EPI>
-__global__ void __launch_bounds__(T8Tile<PAIR, BN>::THREADS, 1)
+__global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
     k_t8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ T8Out o, int* status) {
-  typedef T8Tile<PAIR, BN> T;
+  typedef T8Tile<PAIR, BN, EPI> T;
   constexpr int STAGES = T::STAGES, EW = T::EW, BH = EPI == T8_GLU ? BN / 2 : BN;    // BH: columns of the output in a tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -452,7 +584,12 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN>::THREADS, 1)
   } else {
     const int q = warp & 3, part = (warp - 2) >> 2;      // TMEM lane quarter this warp may read; its share of the columns
     constexpr int CW = BH / (EW / 4);
-    uint8_t* stage = smem + STAGES * T::STAGE + (warp - 2) * 4096;
+    uint8_t* stage = smem + STAGES * T::STAGE + (warp - 2) * T::WARP;
+    float* tab = reinterpret_cast<float*>(smem + STAGES * T::STAGE + EW * T::WARP);
+    if (EPI == T8_GLU) {                                 // while the first tile's operands are on their way
+      sg_fill_table<1>(tab, threadIdx.x - 64, EW * 32);
+      asm volatile("bar.sync 1, %0;" ::"n"(EW * 32) : "memory");
+    }
     const uint32_t free0 = PAIR ? mapa_u32(smem_u32(&bar_tempty[0]), 0) : 0, free1 = PAIR ? mapa_u32(smem_u32(&bar_tempty[1]), 0) : 0;
     int it = 0;
     for (int tile = unit; tile < tiles; tile += units, ++it) {
@@ -462,7 +599,7 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN>::THREADS, 1)
       mbar_wait(&bar_tfull[acc], (uint32_t)(it >> 1) & 1u, abort_flag, status);      // passed over when it ran out: the lanes stay together
       tc_fence_after();
       t8_epilogue<EPI, CW, BN / 2>(o, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part * CW), i0 + (int)rank * 128 + q * 32,
-                                   j0 + part * CW, stage);
+                                   j0 + part * CW, stage, tab);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -489,7 +626,7 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN>::THREADS, 1)
 
 template <bool PAIR, int BN, int EPI>
 static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
-  typedef T8Tile<PAIR, BN> T;
+  typedef T8Tile<PAIR, BN, EPI> T;
   constexpr int BH = EPI == T8_GLU ? BN / 2 : BN;
   static DevOnce once = {};
   if (dev_ensure_smem(once, (const void*)k_t8_gemm<PAIR, BN, EPI>, T::SMEM) != DET_OK) return DET_ERR_CUDA;
@@ -544,8 +681,11 @@ static int t8_sizes(long long M, long long N, long long K) {
 }
 static int t8_vec(const void* p, size_t ld, int size) { return aligned16(p) && ld * size % 16 == 0; }
 
+static int t8_vec4(const void* p, size_t ld) { return aligned_to(p, 8) && ld % 4 == 0; }
+
 // gradient operands into the workspace, then both products
-struct T8Ws { size_t qa, qgt, qxt, s_a, s_g, rowmax, colmax, dgu, bytes; };
+struct T8Ws { size_t qa, qgt, qxt, s_a, s_g, i_a, i_g, rowmax, colmax, dgu, bytes; };
+static size_t t8_ld_dgu(int N) { return ((size_t)N + 3) / 4 * 4; }
 static T8Ws t8_ws(int M, int N, int K, bool glu) {
   T8Ws w;
   size_t at = 0;
@@ -555,21 +695,37 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
   w.qxt = take((size_t)K * t8_ld(M));
   w.s_a = take((size_t)M * 4);
   w.s_g = take((size_t)N * 4);
+  w.i_a = take((size_t)M * 4);
+  w.i_g = take((size_t)N * 4);
   w.rowmax = take((size_t)M * 4);
   w.colmax = take((size_t)N * 4);
-  w.dgu = take(glu ? (size_t)M * N * 2 : 0);
+  w.dgu = take(glu ? (size_t)M * t8_ld_dgu(N) * 2 : 0);
   w.bytes = at;
   return w;
 }
-static int t8_backward(const uint16_t* dY, int ld_dy, const int8_t* qX, const float* s_x, const int8_t* qWt, const float* s_w, int M, int N, int K,
-                       uint16_t* dX, int ld_dx, float* dW, const T8Ws& w, char* ws, int* status, cudaStream_t st) {
+struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *i_a, *s_g, *i_g; int8_t *qa, *qgt; };
+template <bool GLU, int TAB>
+static void t8_largest(const T8Grad& x, const T8Operands& o, int sms, cudaStream_t st) {
+  const long long tiles = (long long)((x.W + (GLU ? 127 : 255)) / (GLU ? 128 : 256)) * ((x.M + T8_ROWS - 1) / T8_ROWS);
+  const long long most = TAB ? 3LL * sms : 0x7fffffffLL;                   // with a table CTAs stay and walk over the tiles
+  launch_after(k_t8_grad_max<GLU, TAB>, (unsigned)(tiles < most ? tiles : most), 256, 0, st, x, o.rowmax, o.colmax);
+}
+static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int K, uint16_t* dX, int ld_dx, float* dW, char* ws, int* status,
+                       cudaStream_t st) {
+  const int M = x.M, N = x.N, sms = dev_sm_count();
+  if (sms <= 0) return DET_ERR_CUDA;
+  const T8Ws w = t8_ws(M, N, K, x.gu != nullptr);
   int8_t *qa = (int8_t*)(ws + w.qa), *qgt = (int8_t*)(ws + w.qgt), *qxt = (int8_t*)(ws + w.qxt);
   float *s_a = (float*)(ws + w.s_a), *s_g = (float*)(ws + w.s_g);
-  uint32_t *rowmax = (uint32_t*)(ws + w.rowmax), *colmax = (uint32_t*)(ws + w.colmax);
-  if (cudaMemsetAsync(rowmax, 0, w.dgu - w.rowmax, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
-  const int vec = t8_vec(dY, ld_dy, 2);
-  launch_after(k_t8_grad_max, dim3((N + 255) / 256, (M + T8_GR - 1) / T8_GR), 256, 0, st, dY, (size_t)ld_dy, M, N, s_x, s_w, rowmax, colmax, vec);
-  launch_after(k_t8_grad_codes, dim3((N + 127) / 128, (M + 127) / 128), 256, 0, st, dY, (size_t)ld_dy, M, N, s_x, s_w, rowmax, colmax, qa, s_a, qgt, s_g, vec);
+  const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), s_a, (float*)(ws + w.i_a), s_g, (float*)(ws + w.i_g), qa, qgt};
+  if (cudaMemsetAsync(op.rowmax, 0, w.dgu - w.rowmax, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
+  if (!x.gu) t8_largest<false, 0>(x, op, sms, st);
+  else if ((long long)M * x.W >= 8LL * sms * 128 * 64) t8_largest<true, 1>(x, op, sms, st);      // some tiles for every CTA
+  else t8_largest<true, 0>(x, op, sms, st);
+  launch_after(k_t8_scales, (unsigned)((M + N + 255) / 256), 256, 0, st, op.rowmax, op.colmax, M, N, op.s_a, op.i_a, op.s_g, op.i_g);
+  T8Grad y = x;                                                            // as the codes are made of it
+  if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
+  launch_after(k_t8_grad_codes, dim3((N + 127) / 128, (M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, qa, qgt);
   DET_CHECK_LAUNCH();
   if (dX) {
     T8Out o = {};
@@ -660,7 +816,8 @@ extern "C" int det_tok8_linear_bwd(const det_bf16* dY, int ld_dy, const int8_t* 
   const int rc = t8_bwd_check(dY, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, det_tok8_linear_bwd_ws_bytes(M, N, K), ws_bytes);
   if (rc != DET_OK) return rc;
   if (!M) return t8_no_rows(dW, N, K, (cudaStream_t)stream);
-  return t8_backward(dY, ld_dy, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, t8_ws(M, N, K, false), (char*)ws, status_dev, (cudaStream_t)stream);
+  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec4(dY, ld_dy) && N % 4 == 0};
+  return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
 
 extern "C" int det_tok8_glu_fwd_q(const int8_t* qX, const float* s_x, const int8_t* qW, const float* s_w, int M, int F, int K, det_bf16* h, int ld_h,
@@ -689,16 +846,6 @@ extern "C" int det_tok8_glu_fwd(const det_bf16* X, int ld, const int8_t* qW, con
   return rc != DET_OK ? rc : det_tok8_glu_fwd_q(qX, s_x, qW, s_w, M, F, K, h, ld_h, gu, ld_gu, stream, status_dev);
 }
 
-// dgu as det_swiglu_bwd gives it, any width and stride: a thread a value
-__global__ void __launch_bounds__(256) k_t8_dgu(const uint16_t* __restrict__ dh, size_t ld_dh, const uint16_t* __restrict__ gu, size_t ld_gu, int F,
-                                                uint16_t* __restrict__ dgu) {
-  const int j = blockIdx.x * 256 + threadIdx.x + grid_dep();
-  const size_t r = blockIdx.y;
-  if (j >= F) return;
-  const float d = bf2f(dh[r * ld_dh + j]), g = bf2f(gu[r * ld_gu + j]), u = bf2f(gu[r * ld_gu + F + j]), sg = t8_sigmoid(g);
-  dgu[r * 2 * F + j] = f2bf(fmul(fmul(d, u), fmul(sg, fadd(1.0f, fmul(g, fsub(1.0f, sg))))));
-  dgu[r * 2 * F + F + j] = f2bf(fmul(d, fmul(g, sg)));
-}
 extern "C" size_t det_tok8_glu_bwd_ws_bytes(int M, int F, int K) {
   return M > 0 && F > 0 && F <= (1 << 27) && K > 0 ? t8_ws(M, 2 * F, K, true).bytes : 0;
 }
@@ -711,13 +858,6 @@ extern "C" int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* g
   if (rc != DET_OK) return rc;
   if (!aligned_to(gu, 2)) return DET_ERR_ALIGN;
   if (!M) return t8_no_rows(dW, 2 * F, K, (cudaStream_t)stream);
-  const T8Ws w = t8_ws(M, 2 * F, K, true);
-  uint16_t* dgu = (uint16_t*)((char*)ws + w.dgu);
-  for (int r = 0; r < M; r += 32768) {
-    const int rows = M - r < 32768 ? M - r : 32768;
-    launch_after(k_t8_dgu, dim3((F + 255) / 256, rows), 256, 0, (cudaStream_t)stream, dh + (size_t)r * ld_dh, (size_t)ld_dh, gu + (size_t)r * ld_gu,
-                 (size_t)ld_gu, F, dgu + (size_t)r * 2 * F);
-  }
-  DET_CHECK_LAUNCH();
-  return t8_backward(dgu, 2 * F, qX, s_x, qWt, s_w, M, 2 * F, K, dX, ld_dx, dW, w, (char*)ws, status_dev, (cudaStream_t)stream);
+  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec4(dh, ld_dh) && t8_vec4(gu, ld_gu) && F % 4 == 0};
+  return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
