@@ -15,6 +15,7 @@
 namespace det {
 
 constexpr int T8_K = 128;                                // bytes (= codes) a stage along the contraction
+constexpr size_t T8_FEW_SMEM = 64 * 1024;                // codes of few tokens in a CTA
 __host__ __device__ __forceinline__ int t8_ld(int K) { return (K + 15) / 16 * 16; }   // bytes from a row of codes to the next
 
 // ---- codes -------------------------------------------------------------------------------------------------
@@ -624,6 +625,182 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
   }
 }
 
+// ---- few tokens ----------------------------------------------------------------------------------------------
+// Up to eight tokens: the weights are read once, a warp R channels (GLU: R / 2 gates and their ups) at a time in pieces of 16 bytes a lane, against the
+// tokens' codes in shared memory.  A CTA makes the codes itself (QUANT) or fetches them: made by a launch of its own they cost more than all of this for one
+// token.  Bound by memory, and by the two launches' worth of latency where the weights are small.
+struct T8Few {
+  const uint16_t* x;     // QUANT: the tokens, rows ld apart; their codes and scales go to q and s
+  size_t ld;
+  int8_t* q;
+  float* s;
+  const int8_t* w;
+  T8Out o;
+};
+template <int MT, int R, bool GLU, bool QUANT>
+__global__ void __launch_bounds__(256) k_t8_few(const __grid_constant__ T8Few f) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];                     // the tokens' codes
+  __shared__ float s_x[MT];
+  __shared__ uint32_t part[MT][8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, K = f.o.K, M = f.o.I, ldk = t8_ld(K), pieces = ldk / 16;
+  grid_dep();
+  if (QUANT) {
+    uint32_t m[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      m[t] = 0;
+      if (t < M)
+        for (int c = threadIdx.x; c < K; c += 256) {
+          const uint32_t u = f.x[t * f.ld + c];
+          m[t] = max(m[t], u << 16 & 0x7fffffffu);
+          reinterpret_cast<uint16_t*>(smem_raw)[t * ldk + c] = (uint16_t)u;   // the values for now, twice the codes' room
+        }
+      m[t] = __reduce_max_sync(0xffffffffu, m[t]);
+      if (lane == 0) part[t][warp] = m[t];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      m[t] = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) m[t] = max(m[t], part[t][w]);
+      const float sc = t8_scale(m[t]), inv = t8_inverse(sc);
+      if (threadIdx.x == 0) {
+        s_x[t] = sc;
+        if (blockIdx.x == 0 && t < M) f.s[t] = sc;
+      }
+      // sixteen values into a piece of codes: a token's codes lie where its values lay, so all of them are read before any is written
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(smem_raw) + t * ldk;
+      for (int p0 = 0; p0 < pieces; p0 += 256) {
+        const int p = p0 + threadIdx.x;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (p < pieces && m[t] < 0x7f800000u) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            if (p * 16 + k < K) w[k >> 2] |= (t8_code(bf2f(v[p * 16 + k]), inv) & 255u) << (8 * (k & 3));
+        }
+        __syncthreads();
+        if (p < pieces) {
+          const uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(smem_raw + (size_t)t * ldk * 2 + p * 16) = c;
+          if (blockIdx.x == 0 && t < M) *reinterpret_cast<uint4*>(f.q + (size_t)t * ldk + p * 16) = c;
+        }
+      }
+    }
+  } else {
+    for (int i = threadIdx.x; i < MT * pieces; i += 256) {
+      const int t = i / pieces;
+      reinterpret_cast<uint4*>(smem_raw)[i] = t < M ? reinterpret_cast<const uint4*>(f.q)[i] : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (threadIdx.x < MT) s_x[threadIdx.x] = threadIdx.x < M ? f.s[threadIdx.x] : 0.0f;
+  }
+  __syncthreads();
+  constexpr int PITCH = QUANT ? 2 : 1;                                    // of a token's codes, in rows of codes
+  constexpr int OUT = GLU ? R / 2 : R;                                    // channels of the output a warp has at a time
+  const int J = f.o.J, tasks = (J + OUT - 1) / OUT;
+#pragma unroll 1
+  for (int task = blockIdx.x * 8 + warp; task < tasks; task += gridDim.x * 8) {
+    const int j0 = task * OUT;
+    const int8_t* row[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int j = min(j0 + (GLU ? r >> 1 : r), J - 1) + (GLU && (r & 1) ? J : 0);
+      row[r] = f.w + (size_t)j * ldk;
+    }
+    int acc[R][MT];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[r][t] = 0;
+    constexpr int U = R >= 4 ? 2 : 4;                                     // pieces of a row on their way together
+    for (int p0 = lane; p0 < pieces; p0 += 32 * U) {
+      uint4 w[U][R];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          w[u][r] = p0 + 32 * u < pieces ? __ldg(reinterpret_cast<const uint4*>(row[r]) + p0 + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p0 + 32 * u >= pieces) break;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const uint4 x = *reinterpret_cast<const uint4*>(smem_raw + (size_t)t * PITCH * ldk + (p0 + 32 * u) * 16);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            int a = acc[r][t];
+            a = __dp4a((int)w[u][r].x, (int)x.x, a);
+            a = __dp4a((int)w[u][r].y, (int)x.y, a);
+            a = __dp4a((int)w[u][r].z, (int)x.z, a);
+            acc[r][t] = __dp4a((int)w[u][r].w, (int)x.w, a);
+          }
+        }
+      }
+    }
+    // lane k takes output k / MT of the warp's and token k % MT
+    int mine = 0, up = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const int sum = __reduce_add_sync(0xffffffffu, acc[r][t]);
+        if (lane == (GLU ? r >> 1 : r) * MT + t) {
+          if (GLU && (r & 1)) up = sum;
+          else mine = sum;
+        }
+      }
+    const int j = j0 + lane / MT, t = lane % MT;
+    if (lane < OUT * MT && j < J && t < M) {
+      const float sx = s_x[t];
+      const uint16_t y = f2bf(fmul(__int2float_rn(mine), fmul(sx, f.o.cs[j])));
+      uint16_t* out = reinterpret_cast<uint16_t*>(f.o.out) + t * f.o.ld + j;
+      if (!GLU) {
+        *out = y;
+      } else {
+        const uint16_t z = f2bf(fmul(__int2float_rn(up), fmul(sx, f.o.cs[J + j])));
+        if (f.o.gu) {
+          f.o.gu[t * f.o.ld_gu + j] = y;
+          f.o.gu[t * f.o.ld_gu + J + j] = z;
+        }
+        *out = f2bf(fmul(fmul(bf2f(y), sigmoid_a8<0>(bf2f(y), nullptr)), bf2f(z)));
+      }
+    }
+  }
+}
+template <int MT, int R, bool GLU, bool QUANT>
+static int t8_few_launch(const T8Few& f, int sms, cudaStream_t st) {
+  const size_t smem = (size_t)MT * t8_ld(f.o.K) * (QUANT ? 2 : 1);
+  static DevOnce once = {};
+  if (smem > 40 * 1024 && dev_ensure_smem(once, (const void*)k_t8_few<MT, R, GLU, QUANT>, T8_FEW_SMEM) != DET_OK) return DET_ERR_CUDA;
+  const long long ctas = ((long long)(f.o.J + (GLU ? R / 2 : R) - 1) / (GLU ? R / 2 : R) + 7) / 8;
+  launch_after(k_t8_few<MT, R, GLU, QUANT>, (unsigned)(ctas < 2 * sms ? ctas : 2 * sms), 256, smem, st, f);
+  DET_CHECK_LAUNCH();
+  return DET_OK;
+}
+// Four channels at a time where there are enough of them for every warp, else fewer: more warps, each with less to wait for
+template <int MT, bool GLU, bool QUANT>
+static int t8_few_rows(const T8Few& f, int sms, cudaStream_t st) {
+  const long long rows = (long long)f.o.J * (GLU ? 2 : 1), warps = 16LL * sms;
+  if (rows >= 4 * warps) return t8_few_launch<MT, 4, GLU, QUANT>(f, sms, st);
+  if (GLU || rows >= 2 * warps) return t8_few_launch<MT, 2, GLU, QUANT>(f, sms, st);
+  return t8_few_launch<MT, GLU ? 2 : 1, GLU, QUANT>(f, sms, st);
+}
+// Whether a call is for this: few tokens, whose codes fit into a CTA's share of shared memory; more than four only where the tensor cores' tiles would not
+// have the SMs to themselves (8 tokens, 16384 channels of 2048: 12.6 here, 13.1 there, gates and ups 11.5 and 14.8; 2048 channels of 8192 12.0 and 8.0).
+// quant: the codes are made here too.
+static bool t8_few_fits(int M, int rows, int K, bool quant) {
+  return (M <= (quant ? 2 : 4) || (!quant && M <= 8 && rows >= 12288)) && (size_t)(M > 4 ? 8 : M > 2 ? 4 : M) * t8_ld(K) * (quant ? 2 : 1) <= T8_FEW_SMEM;
+}
+template <bool GLU, bool QUANT>
+static int t8_few(const T8Few& f, cudaStream_t st) {
+  const int sms = dev_sm_count();
+  if (sms <= 0) return DET_ERR_CUDA;
+  if (f.o.I == 1) return t8_few_rows<1, GLU, QUANT>(f, sms, st);
+  if (f.o.I == 2) return t8_few_rows<2, GLU, QUANT>(f, sms, st);
+  if constexpr (!QUANT) return f.o.I <= 4 ? t8_few_rows<4, GLU, false>(f, sms, st) : t8_few_rows<8, GLU, false>(f, sms, st);
+  return DET_ERR_SHAPE;
+}
+
 template <bool PAIR, int BN, int EPI>
 static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
   typedef T8Tile<PAIR, BN, EPI> T;
@@ -641,21 +818,224 @@ static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& 
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
-// The tile by whole rounds of tiles over the SMs, each the longer of its multiply loop and its epilogue (microseconds, the figures of igemm.cu).
+// ---- few tiles -----------------------------------------------------------------------------------------------
+// Where the output has fewer tiles of 128 x 64 than the GPU has SMs and the contraction is long, the CTAs of a cluster share a tile: each sums its part of the
+// contraction in its tensor memory, puts the sums where the others can read them, and takes the columns that are its own from all of them.  The sums are
+// exact, so nothing shows of how many there were.  BM: rows of the tokens' operand that are staged (the tensor core takes 128, of which the others are never
+// looked at).
+template <int BM>
+struct T8Split {
+  static constexpr int STAGE_A = BM * T8_K, STAGE_B = 64 * T8_K, STAGE = STAGE_A + STAGE_B, STAGES = 6;
+  static constexpr int PITCH = 68;                                        // ints from a row of sums to the next: eight rows' sixteen bytes meet in no bank
+  // the tensor core reads 128 rows from where an operand begins: behind the last stage there has to be room
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE + (128 * T8_K - STAGE > 0 ? 128 * T8_K - STAGE : 0) + 1024;
+  static_assert((size_t)BM * PITCH * 4 <= (size_t)STAGES * STAGE, "the sums lie where the stages lay");
+};
+__device__ __forceinline__ uint4 ld_cluster16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// four adjacent values of a row, `left` of them in it
+template <class T>
+__device__ __forceinline__ void t8_put4(T* to, int left, int vec, const T (&v)[4]) {
+  if (vec && left >= 4) {
+    if (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2((uint32_t)v[0] | (uint32_t)v[1] << 16, (uint32_t)v[2] | (uint32_t)v[3] << 16);
+    else *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (t < left) to[t] = v[t];
+}
+template <int BM, int EPI>
+__global__ void __launch_bounds__(192) k_t8_split(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                                                  const __grid_constant__ T8Out o, int parts, int* status) {
+  typedef T8Split<BM> T;
+  constexpr int BH = EPI == T8_GLU ? 32 : 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ __align__(8) uint64_t bar_full[T::STAGES], bar_empty[T::STAGES], bar_done;
+  __shared__ uint32_t tmem_base_s;
+  __shared__ int abort_s;
+  volatile int* abort_flag = &abort_s;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < T::STAGES; ++s) { mbar_init(&bar_full[s], 1); mbar_init(&bar_empty[s], 1); }
+    mbar_init(&bar_done, 1);
+    abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmA)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmB)) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(64u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_s;
+  grid_dep();
+
+  const int tile = blockIdx.x / parts, tiles_i = (o.I + 127) / 128, i0 = tile % tiles_i * 128, j0 = tile / tiles_i * BH;
+  const int kblocks = (o.K + T8_K - 1) / T8_K, kb0 = (int)((long long)kblocks * rank / parts), kb1 = (int)((long long)kblocks * (rank + 1) / parts);
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&bar_empty[stage], phase ^ 1u, abort_flag, status)) break;
+        uint8_t *sa = smem + stage * T::STAGE, *sb = sa + T::STAGE_A;
+        mbar_expect_tx(&bar_full[stage], T::STAGE);
+        tma_load_2d(sa, &tmA, kb * T8_K, i0, &bar_full[stage]);
+        tma_load_2d(sb, &tmB, kb * T8_K, j0, &bar_full[stage]);
+        if (EPI == T8_GLU) tma_load_2d(sb + T::STAGE_B / 2, &tmB, kb * T8_K, o.J + j0, &bar_full[stage]);
+        if (++stage == T::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(64 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&bar_full[stage], phase, abort_flag, status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sa = smem_u32(smem + stage * T::STAGE);
+        const uint64_t da = make_smem_desc(sa), db = make_smem_desc(sa + T::STAGE_A);
+#pragma unroll
+        for (int k4 = 0; k4 < T8_K / 32; ++k4) umma_i8(tmem_base, da + (uint64_t)(k4 * 2), db + (uint64_t)(k4 * 2), idesc, (kb > kb0 || k4) ? 1u : 0u);
+        umma_commit(&bar_empty[stage]);
+        if (++stage == T::STAGES) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) umma_commit(&bar_done);
+    }
+  }
+  const int q = warp & 3, row = q * 32 + lane, rows = o.I - i0 < BM ? o.I - i0 : BM;
+  int* sums = reinterpret_cast<int*>(smem);
+  if (warp >= 2) {
+    mbar_wait(&bar_done, 0, abort_flag, status);         // passed over when it ran out; all operands have been read when it has not
+    tc_fence_after();
+    if (q * 32 < rows) {
+#pragma unroll
+      for (int c = 0; c < 64; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c, r);
+        if (row < rows) {
+#pragma unroll
+          for (int v = 0; v < 8; ++v) *reinterpret_cast<uint4*>(sums + row * T::PITCH + c + 4 * v) = make_uint4(r[4 * v], r[4 * v + 1], r[4 * v + 2], r[4 * v + 3]);
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  __syncthreads();
+  if (abort_s) {                                         // copies in flight get time to land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000ll) { }
+    __syncthreads();
+  }
+  cluster_sync_all();
+  if (warp >= 2) {
+    // this CTA's columns, four of a row a thread and adjacent ones in adjacent threads; parts divides BH / 4
+    const int groups = BH / 4 / parts, items = rows * groups;
+    for (int i = threadIdx.x - 64; i < items; i += 128) {
+      const int r = i / groups, c = (rank * groups + i % groups) * 4, j = j0 + c, left = o.J - j;
+      if (left <= 0) continue;
+      const uint32_t mine = smem_u32(sums + r * T::PITCH + c);
+      int a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
+      for (int p = 0; p < parts; ++p) {
+        const uint32_t there = mapa_u32(mine, (uint32_t)p);
+        const uint4 x = ld_cluster16(there);
+        a[0] += (int)x.x; a[1] += (int)x.y; a[2] += (int)x.z; a[3] += (int)x.w;
+        if (EPI == T8_GLU) {
+          const uint4 y = ld_cluster16(there + 32 * 4);
+          b[0] += (int)y.x; b[1] += (int)y.y; b[2] += (int)y.z; b[3] += (int)y.w;
+        }
+      }
+      const float rs = __ldg(o.rs + i0 + r);
+      float f[4], h[4];
+      uint16_t y[4], z[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bool there = t < left;
+        f[t] = fmul(__int2float_rn(a[t]), o.cs ? fmul(rs, there ? __ldg(o.cs + j + t) : 0.0f) : rs);
+        y[t] = f2bf(f[t]);
+        if (EPI != T8_GLU) continue;
+        z[t] = f2bf(fmul(__int2float_rn(b[t]), fmul(rs, there ? __ldg(o.cs + o.J + j + t) : 0.0f)));
+        h[t] = fmul(fmul(bf2f(y[t]), sigmoid_a8<0>(bf2f(y[t]), nullptr)), bf2f(z[t]));
+      }
+      if (EPI == T8_F32) {
+        t8_put4(reinterpret_cast<float*>(o.out) + (i0 + r) * o.ld + j, left, o.vec, f);
+      } else if (EPI == T8_BF16) {
+        t8_put4(reinterpret_cast<uint16_t*>(o.out) + (i0 + r) * o.ld + j, left, o.vec, y);
+      } else {
+        if (o.gu) {
+          uint16_t* g = o.gu + (i0 + r) * o.ld_gu + j;
+          t8_put4(g, left, o.vec_gu, y);
+          t8_put4(g + o.J, left, o.vec_gu, z);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) y[t] = f2bf(h[t]);
+        t8_put4(reinterpret_cast<uint16_t*>(o.out) + (i0 + r) * o.ld + j, left, o.vec, y);
+      }
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();                                    // nobody leaves while the others read
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(64u) : "memory");
+  }
+}
+template <int BM, int EPI>
+static int t8_split_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int* status, cudaStream_t st) {
+  static DevOnce once = {};
+  if (dev_ensure_smem(once, (const void*)k_t8_split<BM, EPI>, T8Split<BM>::SMEM) != DET_OK) return DET_ERR_CUDA;
+  CUtensorMap ta, tb;
+  if (!make_map_ld(&ta, A, o.I, o.K, t8_ld(o.K), BM) || !make_map_ld(&tb, B, rows_b, o.K, t8_ld(o.K), EPI == T8_GLU ? 32 : 64)) return DET_ERR_CUDA;
+  const int bh = EPI == T8_GLU ? 32 : 64, tiles = ((o.I + 127) / 128) * ((o.J + bh - 1) / bh);
+  launch_after_cluster(k_t8_split<BM, EPI>, tiles * parts, 192, T8Split<BM>::SMEM, parts, st, ta, tb, o, parts, status);
+  DET_CHECK_LAUNCH();
+  return DET_OK;
+}
+template <int EPI>
+static int t8_split(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int* status, cudaStream_t st) {
+  if (o.I <= 32) return t8_split_launch<32, EPI>(A, B, rows_b, o, parts, status, st);
+  return t8_split_launch<128, EPI>(A, B, rows_b, o, parts, status, st);
+}
+
+// The tile by whole rounds of tiles over the SMs, each the longer of its multiply loop and its epilogue, once the other of the two and what a launch takes
+// (microseconds; steps and turns of igemm.cu).  Tiles that the CTAs of a cluster share: as many CTAs as the SMs have room for, at least two steps of the
+// contraction for each; their exchange takes longer the more rows there are.  Measured over 32 shapes, the rule within 14 % of the best of all: 24 x 2048 x 8192
+// with 8 CTAs to a tile 8.7, alone 23.9; 128 x 2048 x 8192 with 4 12.4, alone 24.3; 256 x 2048 x 2048 with 2 11.6, alone 8.9 (64 columns), 9.5 (128), 12.0 (pair);
+// 2738 x 520 x 1003 9.4, 7.6, 10.2; 8192 x 2048 x 2048 78, 43, 30.
 template <int EPI>
 static int t8_product(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
   const int sms = dev_sm_count();
   if (sms < 2) return DET_ERR_CUDA;
   static const struct { int bn, bi; double step, turn, epi[3]; } C[3] = {
-      {256, 256, 0.365, 0.9, {4.2, 6.6, 9.0}}, {128, 128, 0.30, 0.5, {1.7, 3.8, 5.0}}, {64, 128, 0.30, 0.5, {1.7, 1.8, 4.0}}};
+      {256, 256, 0.365, 0.9, {4.2, 6.6, 6.0}}, {128, 128, 0.30, 0.5, {1.7, 3.8, 3.0}}, {64, 128, 0.30, 0.5, {1.2, 1.5, 2.0}}};
+  const int steps = (o.K + T8_K - 1) / T8_K;
   int pick = 0;
   double best = 0.0;
   for (int i = 0; i < 3; ++i) {
     const int bh = EPI == T8_GLU ? C[i].bn / 2 : C[i].bn, units = i == 0 ? sms / 2 : sms;
     const double tiles = (double)((o.I + C[i].bi - 1) / C[i].bi) * ((o.J + bh - 1) / bh), rounds = (double)(long long)((tiles + units - 1) / units);
-    const double loop = ((o.K + T8_K - 1) / T8_K) * C[i].step, e = C[i].epi[EPI], t = rounds * ((loop > e ? loop : e) + C[i].turn) + (loop > e ? e : loop);
+    const double loop = steps * C[i].step, e = C[i].epi[EPI], t = 2.0 + rounds * ((loop > e ? loop : e) + C[i].turn) + (loop > e ? e : loop);
     if (i == 0 || t < best) { best = t; pick = i; }
   }
+  const int bh = EPI == T8_GLU ? 32 : 64, room = o.I <= 32 ? 2 * sms : sms;
+  const long long tiles = (long long)((o.I + 127) / 128) * ((o.J + bh - 1) / bh);
+  // clusters of eight large CTAs find their SMs in few places: half of the GPU
+  int parts = 1;
+  while (parts < 8 && tiles * parts * 2 <= (parts == 4 && o.I > 32 ? room / 2 : room) && steps >= parts * 4) parts *= 2;
+  if (parts > 1 && 5.2 + 0.025 * (o.I < 128 ? o.I : 168) + steps * 0.27 / parts < best) return t8_split<EPI>(A, B, rows_b, o, parts, status, st);
   if (pick == 0) return t8_launch<true, 256, EPI>(A, B, rows_b, o, status, st);
   if (pick == 1) return t8_launch<false, 128, EPI>(A, B, rows_b, o, status, st);
   return t8_launch<false, 64, EPI>(A, B, rows_b, o, status, st);
@@ -781,6 +1161,8 @@ extern "C" int det_tok8_linear_fwd_q(const int8_t* qX, const float* s_x, const i
   if (rc != DET_OK || !M) return rc;
   T8Out o = {};
   o.out = Y; o.ld = ld_y; o.rs = s_x; o.cs = s_w; o.I = M; o.J = N; o.K = K; o.vec = t8_vec(Y, ld_y, 2);
+  if (t8_few_fits(M, N, K, false))
+    return t8_few<false, false>(T8Few{nullptr, 0, const_cast<int8_t*>(qX), const_cast<float*>(s_x), qW, o}, (cudaStream_t)stream);
   return t8_product<T8_BF16>(qX, qW, N, o, status_dev, (cudaStream_t)stream);
 }
 extern "C" int det_tok8_linear_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int N, int K, det_bf16* Y, int ld_y, int8_t* qX,
@@ -790,6 +1172,11 @@ extern "C" int det_tok8_linear_fwd(const det_bf16* X, int ld, const int8_t* qW, 
   if (rc != DET_OK) return rc;
   if (!aligned_to(X, 2)) return DET_ERR_ALIGN;
   if (!M) return DET_OK;
+  if (t8_few_fits(M, N, K, true)) {
+    T8Out o = {};
+    o.out = Y; o.ld = ld_y; o.cs = s_w; o.I = M; o.J = N; o.K = K;
+    return t8_few<false, true>(T8Few{X, (size_t)ld, qX, s_x, qW, o}, (cudaStream_t)stream);
+  }
   rc = t8_quant(X, ld, M, K, qX, s_x, (cudaStream_t)stream);
   return rc != DET_OK ? rc : det_tok8_linear_fwd_q(qX, s_x, qW, s_w, M, N, K, Y, ld_y, stream, status_dev);
 }
@@ -831,6 +1218,8 @@ extern "C" int det_tok8_glu_fwd_q(const int8_t* qX, const float* s_x, const int8
   T8Out o = {};
   o.out = h; o.ld = ld_h; o.rs = s_x; o.cs = s_w; o.gu = gu; o.ld_gu = ld_gu; o.I = M; o.J = F; o.K = K; o.vec = t8_vec(h, ld_h, 2);
   o.vec_gu = t8_vec(gu, ld_gu, 2) && F % 8 == 0;
+  if (t8_few_fits(M, 2 * F, K, false))
+    return t8_few<true, false>(T8Few{nullptr, 0, const_cast<int8_t*>(qX), const_cast<float*>(s_x), qW, o}, (cudaStream_t)stream);
   return t8_product<T8_GLU>(qX, qW, 2 * F, o, status_dev, (cudaStream_t)stream);
 }
 extern "C" int det_tok8_glu_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int F, int K, det_bf16* h, int ld_h, det_bf16* gu,
@@ -842,6 +1231,11 @@ extern "C" int det_tok8_glu_fwd(const det_bf16* X, int ld, const int8_t* qW, con
   if (gu && ld_gu < 2 * F) return DET_ERR_ARG;
   if (!aligned_to(X, 2) || !aligned_to(gu, 2)) return DET_ERR_ALIGN;
   if (!M) return DET_OK;
+  if (t8_few_fits(M, 2 * F, K, true)) {
+    T8Out o = {};
+    o.out = h; o.ld = ld_h; o.cs = s_w; o.gu = gu; o.ld_gu = ld_gu; o.I = M; o.J = F; o.K = K;
+    return t8_few<true, true>(T8Few{X, (size_t)ld, qX, s_x, qW, o}, (cudaStream_t)stream);
+  }
   rc = t8_quant(X, ld, M, K, qX, s_x, (cudaStream_t)stream);
   return rc != DET_OK ? rc : det_tok8_glu_fwd_q(qX, s_x, qW, s_w, M, F, K, h, ld_h, gu, ld_gu, stream, status_dev);
 }

@@ -59,7 +59,10 @@ def strided(a, ld, fill=0xABAB):
 
 # one token, some, ragged tiles of every kind, odd widths and whole ones; contractions shorter than a stage, of one stage and of several
 SIZES = [(1, 1, 1), (1, 64, 128), (2, 33, 7), (7, 130, 65), (16, 256, 256), (31, 100, 1000), (64, 257, 384), (129, 65, 129), (128, 128, 128), (130, 520, 264),
-         (257, 200, 515), (300, 1003, 777), (256, 768, 256), (515, 384, 2056), (1000, 1040, 96), (9, 4104, 2048), (4, 40, 9000), (3, 24, 17000)]
+         (257, 200, 515), (300, 1003, 777), (256, 768, 256), (515, 384, 2056), (1000, 1040, 96), (9, 4104, 2048), (4, 40, 9000), (3, 24, 17000),
+         # up to eight tokens by every number of channels a warp has at a time; tiles that two, four and eight CTAs share, ragged ones among them
+         (1, 9500, 40), (2, 4800, 300), (1, 2048, 2048), (2, 130, 9000), (5, 9480, 72), (8, 4800, 528), (3, 9999, 17), (8, 500, 1000),
+         (24, 136, 8192), (9, 70, 1024), (32, 4100, 600), (33, 257, 2050), (100, 90, 4096), (128, 500, 2000), (150, 40, 3000), (20, 9000, 520)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
