@@ -96,7 +96,8 @@ struct AuxScope {
 // kernel's opt-in for large dynamic shared memory has been made there.  Both helpers act on the CURRENT device.
 constexpr int MAX_DEVICES = 64;
 struct DevOnce { bool done[MAX_DEVICES]; };
-int dev_ensure_smem(DevOnce& once, const void* fn, size_t bytes);  // DET_OK or DET_ERR_CUDA
+// DET_OK or DET_ERR_CUDA; whole: the SM is set up for as much shared memory as it has, so that what this kernel leaves is there for another's CTAs
+int dev_ensure_smem(DevOnce& once, const void* fn, size_t bytes, bool whole = false);
 int dev_sm_count();                                                 // SMs of the current device (0 on error)
 
 // C[i,j] = sum_k A[i,k] B[j,k] on the tensor cores with the chosen epilogue; host-side checks included

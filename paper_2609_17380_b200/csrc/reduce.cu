@@ -63,12 +63,16 @@ bool aux_join(cudaStream_t st, AuxStreams* a) {
   return ok;
 }
 
-int dev_ensure_smem(DevOnce& once, const void* fn, size_t bytes) {
+int dev_ensure_smem(DevOnce& once, const void* fn, size_t bytes, bool whole) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return DET_ERR_CUDA;
   std::lock_guard<std::mutex> lock(g_dev_mutex);
   if (!once.done[dev]) {
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+      cudaGetLastError();
+      return DET_ERR_CUDA;
+    }
+    if (whole && cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) {
       cudaGetLastError();
       return DET_ERR_CUDA;
     }

@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t t8_max8(const float v[8], uint32_t m) {
   return m;
 }
 
-// Rows of a multiple of 8 columns, 16-byte aligned: WPR warps a row, up to 64 values a lane, which stay in registers.
+// Rows of a multiple of 8 columns, 16-byte aligned: WPR warps a row, up to 64 values a lane, which stay in registers as they came.
 template <int WPR>
 __global__ void __launch_bounds__(256) k_t8_rows(const uint16_t* __restrict__ x, size_t ld, int M, int K, int8_t* __restrict__ q, float* __restrict__ s) {
   grid_dep();
@@ -49,16 +49,17 @@ __global__ void __launch_bounds__(256) k_t8_rows(const uint16_t* __restrict__ x,
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = blockIdx.x * (8 / WPR) + warp / WPR, first = ((warp % WPR) * 32 + lane) * 8, ldq = t8_ld(K);
   const bool there = row < M;
-  float v[8][8];
-  uint32_t m = 0;
+  uint4 v[8];
+  uint32_t pair = 0;                      // the largest of the lower halves and of the upper ones
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int c = first + k * (WPR * 256);
-    load8n<true>(x, (size_t)row * ld + c, there && c < K, v[k]);
+    v[k] = there && c < K ? __ldg(reinterpret_cast<const uint4*>(x + (size_t)row * ld + c)) : make_uint4(0u, 0u, 0u, 0u);
   }
 #pragma unroll
-  for (int k = 0; k < 8; ++k) m = t8_max8(v[k], m);
-  m = __reduce_max_sync(0xffffffffu, m);
+  for (int k = 0; k < 8; ++k)
+    pair = __vmaxu2(pair, __vmaxu2(__vmaxu2(v[k].x & 0x7fff7fffu, v[k].y & 0x7fff7fffu), __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu)));
+  uint32_t m = __reduce_max_sync(0xffffffffu, max(pair << 16, pair & 0xffff0000u));
   if (WPR > 1) {
     if (lane == 0) part[warp] = m;
     __syncthreads();
@@ -72,33 +73,46 @@ __global__ void __launch_bounds__(256) k_t8_rows(const uint16_t* __restrict__ x,
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int c = first + k * (WPR * 256);
-    if (c < ldq) *reinterpret_cast<uint2*>(q + (size_t)row * ldq + c) = c < K ? t8_codes8(v[k], inv, dead) : make_uint2(0u, 0u);
+    if (c >= ldq) break;
+    float f[8];
+    unpack8(v[k], f);                     // zeros behind the row's end
+    *reinterpret_cast<uint2*>(q + (size_t)row * ldq + c) = t8_codes8(f, inv, dead);
   }
 }
-// Any width, stride and address: a CTA a row, which is read twice.
-__global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict__ x, size_t ld, int K, int8_t* __restrict__ q, float* __restrict__ s) {
+// Any width, stride and address: a warp a row (WIDE: a CTA), which is read twice, an element a lane.
+template <bool WIDE>
+__global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict__ x, size_t ld, int M, int K, int8_t* __restrict__ q, float* __restrict__ s) {
   grid_dep();
   __shared__ uint32_t part[8];
-  const int row = blockIdx.x, ldq = t8_ld(K);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = WIDE ? blockIdx.x : blockIdx.x * 8 + warp, ldq = t8_ld(K);
+  const int at = WIDE ? threadIdx.x : lane, step = WIDE ? 256 : 32;
+  if (row >= M) return;
   const uint16_t* p = x + (size_t)row * ld;
   uint32_t m = 0;
-  for (int c = threadIdx.x; c < K; c += 256) m = max(m, ((uint32_t)p[c] << 16) & 0x7fffffffu);
-  m = __reduce_max_sync(0xffffffffu, m);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
-  __syncthreads();
+#pragma unroll 8
+  for (int c = at; c < K; c += step) m = max(m, (uint32_t)__ldg(p + c) & 0x7fffu);
+  m = __reduce_max_sync(0xffffffffu, m) << 16;
+  if (WIDE) {
+    if (lane == 0) part[warp] = m;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 8; ++w) m = max(m, part[w]);
+    for (int w = 0; w < 8; ++w) m = max(m, part[w]);
+  }
   const float sc = t8_scale(m), inv = t8_inverse(sc);
-  if (threadIdx.x == 0) s[row] = sc;
-  for (int c = threadIdx.x; c < ldq; c += 256)
-    q[(size_t)row * ldq + c] = c < K && m < 0x7f800000u ? (int8_t)t8_code(bf2f(p[c]), inv) : (int8_t)0;
+  if (at == 0) s[row] = sc;
+#pragma unroll 8
+  for (int c = at; c < ldq; c += step)
+    q[(size_t)row * ldq + c] = c < K && m < 0x7f800000u ? (int8_t)t8_code(bf2f(__ldg(p + c)), inv) : (int8_t)0;
 }
 
 // Codes [R, ld(C)] -> [C, ld(R)], through shared memory, whole 128-byte lines on both sides but at the edges.  What lies behind column C of the
 // input is zero; so is what is written behind column R.
-__global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__ in, int R, int C, int8_t* __restrict__ out) {
+// fill: the kernel before has nothing to do with it (common.cuh).
+__global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__ in, int R, int C, int8_t* __restrict__ out, int fill) {
   __shared__ __align__(16) uint8_t tile[128 * 128];
-  const int t = threadIdx.x, c0 = blockIdx.x * 128 + grid_dep(), r0 = blockIdx.y * 128, ldi = t8_ld(C), ldo = t8_ld(R);
+  if (fill) grid_fill_begin();
+  else grid_dep();
+  const int t = threadIdx.x, c0 = blockIdx.x * 128, r0 = blockIdx.y * 128, ldi = t8_ld(C), ldo = t8_ld(R);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = i * 16 + (t >> 3), ch = (t & 7) * 16;
@@ -123,6 +137,7 @@ __global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__
     if (c0 + r < C && r0 + ch * 16 < ldo)
       *reinterpret_cast<uint4*>(out + (size_t)(c0 + r) * ldo + r0 + ch * 16) = *reinterpret_cast<const uint4*>(tile + r * 128 + ((ch ^ (r & 7)) << 4));
   }
+  if (fill) grid_fill_end();
 }
 
 // ---- operands of the backward products ---------------------------------------------------------------------
@@ -137,6 +152,7 @@ struct T8Grad {
   size_t ld_dgu;
   int M, N, W;                            // W: columns of d, N or N / 2
   int vec;                                // rows in whole pieces of four
+  int tile;                               // rows of a tile of the first pass, 32 or 128
 };
 // Four adjacent values from `at` on, n of them there; FULL: all, in one piece.
 template <bool FULL>
@@ -179,15 +195,14 @@ __device__ __forceinline__ void t8_grad4(const T8Raw<GLU>& w, const float* tab, 
 }
 __device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? bfhi(t & 2 ? v.y : v.x) : bflo(t & 2 ? v.y : v.x); }
 
-// Largest magnitudes first.  A tile is 128 rows of 128 columns of either half (GLU), or of 256 columns; a warp has every eighth row, a lane four columns of
-// each half; four rows are on their way together.
-constexpr int T8_ROWS = 128;
+// Largest magnitudes first.  A tile is 128 rows (32 where those would leave SMs without one) of 128 columns of either half (GLU), or of 256 columns; a
+// warp has every eighth row, a lane four columns of each half; four rows are on their way together.
 template <bool FULL, bool GLU, int TAB>
 __device__ __forceinline__ void t8_max_rows(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4], uint32_t (&cm)[2][4],
                                             uint32_t* __restrict__ rowmax, const float* tab) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int i = 0; i < T8_ROWS / 8; i += 4) {
+  for (int i = 0; i < x.tile / 8; i += 4) {
     T8Raw<GLU> w[4];
     float sx[4];
 #pragma unroll
@@ -240,10 +255,10 @@ __global__ void __launch_bounds__(256) k_t8_grad_max(const __grid_constant__ T8G
   grid_dep();
   constexpr int FW = GLU ? 128 : 256;                                     // columns of d in a tile
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int across = (x.W + FW - 1) / FW, tiles = across * ((x.M + T8_ROWS - 1) / T8_ROWS);
+  const int across = (x.W + FW - 1) / FW, tiles = across * ((x.M + x.tile - 1) / x.tile);
 #pragma unroll 1
   for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int c0 = tile % across * FW, r0 = tile / across * T8_ROWS;
+    const int c0 = tile % across * FW, r0 = tile / across * x.tile;
     const int at[2] = {c0 + lane * 4, c0 + lane * 4 + (GLU ? 0 : 128)}, left[2] = {x.W - at[0], x.W - at[1]};
     float sw[2][4];
     uint32_t cm[2][4];
@@ -254,7 +269,7 @@ __global__ void __launch_bounds__(256) k_t8_grad_max(const __grid_constant__ T8G
         sw[h][t] = t < left[h] ? fabsf(x.s_w[(GLU ? h * x.W : 0) + at[h] + t]) : 0.0f;
         cm[h][t] = 0;
       }
-    if (x.vec && c0 + FW <= x.W && r0 + T8_ROWS <= x.M) t8_max_rows<true, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
+    if (x.vec && c0 + FW <= x.W && r0 + x.tile <= x.M) t8_max_rows<true, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
     else t8_max_rows<false, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
     if (tile != blockIdx.x) __syncthreads();                              // the columns before have been read
 #pragma unroll
@@ -475,7 +490,7 @@ template <bool PAIR, int BN, int EPI>
 struct T8Tile {
   static constexpr int BM = PAIR ? 256 : 128, BROWS = PAIR ? BN / 2 : BN;         // BROWS: rows of the columns' operand that a CTA stages
   static constexpr int STAGE_A = 128 * T8_K, STAGE_B = BROWS * T8_K, STAGE = STAGE_A + STAGE_B;
-  static constexpr int STAGES = (PAIR || BN == 128 ? 6 : 8) - (EPI == T8_GLU ? 1 : 0), EW = BN == 64 ? 4 : 8;    // GLU: room for the sigmoids
+  static constexpr int STAGES = (PAIR || BN == 128 ? 6 : 8) - (EPI == T8_F32 ? 0 : 1), EW = BN == 64 ? 4 : 8;    // one less where the sigmoids, or CTAs of the transposition beside, want the room
   static constexpr int WARP = EPI == T8_F32 ? 4096 : 2048 + 256;                    // staging tile of a warp, and the scales of its columns
   static constexpr int THREADS = 64 + 32 * EW, TCOLS = 2 * BN;
   static constexpr size_t SMEM = (size_t)STAGES * STAGE + EW * WARP + (EPI == T8_GLU ? 2 * SG_TAB * 4 : 0) + 1024;
@@ -806,7 +821,7 @@ static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& 
   typedef T8Tile<PAIR, BN, EPI> T;
   constexpr int BH = EPI == T8_GLU ? BN / 2 : BN;
   static DevOnce once = {};
-  if (dev_ensure_smem(once, (const void*)k_t8_gemm<PAIR, BN, EPI>, T::SMEM) != DET_OK) return DET_ERR_CUDA;
+  if (dev_ensure_smem(once, (const void*)k_t8_gemm<PAIR, BN, EPI>, T::SMEM, EPI == T8_BF16) != DET_OK) return DET_ERR_CUDA;
   const int sms = dev_sm_count();
   if (sms < 2) return DET_ERR_CUDA;
   CUtensorMap ta, tb;
@@ -1047,7 +1062,8 @@ static int t8_quant(const uint16_t* X, int ld, int M, int K, int8_t* q, float* s
     else if (K <= 8192) launch_after(k_t8_rows<4>, (unsigned)((M + 1) / 2), 256, 0, st, X, (size_t)ld, M, K, q, s);
     else launch_after(k_t8_rows<8>, (unsigned)M, 256, 0, st, X, (size_t)ld, M, K, q, s);
   } else {
-    launch_after(k_t8_rows_any, (unsigned)M, 256, 0, st, X, (size_t)ld, K, q, s);
+    if (K <= 2048) launch_after(k_t8_rows_any<false>, (unsigned)((M + 7) / 8), 256, 0, st, X, (size_t)ld, M, K, q, s);
+    else launch_after(k_t8_rows_any<true>, (unsigned)M, 256, 0, st, X, (size_t)ld, M, K, q, s);
   }
   DET_CHECK_LAUNCH();
   return DET_OK;
@@ -1085,9 +1101,10 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
 }
 struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *i_a, *s_g, *i_g; int8_t *qa, *qgt; };
 template <bool GLU, int TAB>
-static void t8_largest(const T8Grad& x, const T8Operands& o, int sms, cudaStream_t st) {
-  const long long tiles = (long long)((x.W + (GLU ? 127 : 255)) / (GLU ? 128 : 256)) * ((x.M + T8_ROWS - 1) / T8_ROWS);
-  const long long most = TAB ? 3LL * sms : 0x7fffffffLL;                   // with a table CTAs stay and walk over the tiles
+static void t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
+  const long long across = (x.W + (GLU ? 127 : 255)) / (GLU ? 128 : 256);
+  x.tile = across * ((x.M + 127) / 128) < 2 * sms ? 32 : 128;
+  const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = TAB ? 3LL * sms : 0x7fffffffLL;    // with a table CTAs stay and walk over the tiles
   launch_after(k_t8_grad_max<GLU, TAB>, (unsigned)(tiles < most ? tiles : most), 256, 0, st, x, o.rowmax, o.colmax);
 }
 static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int K, uint16_t* dX, int ld_dx, float* dW, char* ws, int* status,
@@ -1114,7 +1131,8 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
     if (rc != DET_OK) return rc;
   }
   if (dW) {
-    launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, st, qX, M, K, qxt);
+    // beside the other product, which leaves the memory idle and room on every SM for two CTAs of this
+    launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, st, qX, M, K, qxt, dX ? 1 : 0);
     T8Out o = {};
     o.out = dW; o.ld = K; o.rs = s_g; o.I = N; o.J = K; o.K = M; o.vec = t8_vec(dW, K, 4);
     const int rc = t8_product<T8_F32>(qgt, qxt, K, o, status, st);
@@ -1143,7 +1161,7 @@ extern "C" int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, voi
   if ((M + 127) / 128 > 65535) return DET_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(qT)) return DET_ERR_ALIGN;
   if (!M) return DET_OK;
-  launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, (cudaStream_t)stream, q, M, K, qT);
+  launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, (cudaStream_t)stream, q, M, K, qT, 0);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -1203,7 +1221,7 @@ extern "C" int det_tok8_linear_bwd(const det_bf16* dY, int ld_dy, const int8_t* 
   const int rc = t8_bwd_check(dY, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, det_tok8_linear_bwd_ws_bytes(M, N, K), ws_bytes);
   if (rc != DET_OK) return rc;
   if (!M) return t8_no_rows(dW, N, K, (cudaStream_t)stream);
-  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec4(dY, ld_dy) && N % 4 == 0};
+  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec4(dY, ld_dy) && N % 4 == 0, 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
 
@@ -1252,6 +1270,6 @@ extern "C" int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* g
   if (rc != DET_OK) return rc;
   if (!aligned_to(gu, 2)) return DET_ERR_ALIGN;
   if (!M) return t8_no_rows(dW, 2 * F, K, (cudaStream_t)stream);
-  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec4(dh, ld_dh) && t8_vec4(gu, ld_gu) && F % 4 == 0};
+  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec4(dh, ld_dh) && t8_vec4(gu, ld_gu) && F % 4 == 0, 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
