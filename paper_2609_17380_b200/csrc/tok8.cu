@@ -431,45 +431,67 @@ __device__ __forceinline__ uint32_t t8_glu2(uint32_t g, uint32_t u, const float*
   const float2 h = mul2(mul2(make_float2(bflo(g), bfhi(g)), sg), make_float2(bflo(u), bfhi(u)));
   return bf_pair(h.x, h.y);
 }
+// The scales that a warp needs for a tile: its rows' a lane, its columns' in steps of 32.  They are fetched while the tile before is worked on.
+template <int EPI, int CW>
+struct T8Scales {
+  float row, col[EPI == T8_F32 ? 1 : CW / 32], up[EPI == T8_GLU ? CW / 32 : 1];
+  __device__ __forceinline__ void fetch(const T8Out& o, int row0, int j0) {
+    const int lane = threadIdx.x & 31;
+    row = row0 + lane < o.I ? __ldg(o.rs + row0 + lane) : 0.0f;
+    if (EPI == T8_F32) return;
+#pragma unroll
+    for (int c = 0; c < CW / 32; ++c) {
+      const int j = j0 + c * 32 + lane;
+      col[c] = j < o.J && o.cs ? __ldg(o.cs + j) : 0.0f;
+      if (EPI == T8_GLU) up[c] = j < o.J ? __ldg(o.cs + o.J + j) : 0.0f;
+    }
+  }
+};
 // Columns j0 .. j0 + CW of the warp's 32 rows (row0 the first); GLU: the ups' accumulators lie UP columns behind the gates'.  stage: the
-// warp's own staging tile in shared memory, with the columns' scales behind it.
-template <int EPI, int CW, int UP>
-__device__ __forceinline__ void t8_epilogue(const T8Out& o, uint32_t taddr, int row0, int j0, uint8_t* stage, const float* tab) {
+// warp's own staging tile in shared memory, with room for the columns' scales behind it.  read_all: called once, when the last accumulator is in registers.
+template <int EPI, int CW, int UP, class F>
+__device__ __forceinline__ void t8_epilogue(const T8Out& o, const T8Scales<EPI, CW>& sc, uint32_t taddr, int row0, int j0, uint8_t* stage, const float* tab,
+                                            F read_all) {
   float* cs = reinterpret_cast<float*>(stage + 2048);
   const int lane = threadIdx.x & 31, rows = o.I - row0;
-  if (rows <= 0) return;
-  const float rs = lane < rows ? o.rs[row0 + lane] : 0.0f;
-#pragma unroll 1
+  if (rows <= 0 || o.J <= j0) { read_all(); return; }
+#pragma unroll
   for (int c = 0; c < CW; c += 32) {
     const int j = j0 + c, cols = o.J - j;
-    if (cols <= 0) break;
+    if (c && cols <= 0) break;
+    const bool last = c + 32 == CW || cols <= 32;
     uint32_t r[32];
-    tmem_ld32(taddr + (uint32_t)c, r);
     if (EPI == T8_F32) {
+      tmem_ld32(taddr + (uint32_t)c, r);
+      if (last) read_all();
       uint4 w[8];
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const float2 f = mul2(make_float2(__int2float_rn((int)r[2 * v]), __int2float_rn((int)r[2 * v + 1])), same2(rs));
+        const float2 f = mul2(make_float2(__int2float_rn((int)r[2 * v]), __int2float_rn((int)r[2 * v + 1])), same2(sc.row));
         reinterpret_cast<float2*>(w)[v] = f;
       }
       t8_store<8, 4>(stage, reinterpret_cast<uint8_t*>(reinterpret_cast<float*>(o.out) + row0 * o.ld + j), o.ld * 4, rows, cols, o.vec, w);
       continue;
     }
+    tmem_ld32_nowait(taddr + (uint32_t)c, r);
+    uint32_t r2[32];
+    if (EPI == T8_GLU) tmem_ld32_nowait(taddr + (uint32_t)(UP + c), r2);
     if (o.cs) {
       __syncwarp();
-      cs[lane] = lane < cols ? o.cs[j + lane] : 0.0f;
-      if (EPI == T8_GLU) cs[32 + lane] = lane < cols ? o.cs[o.J + j + lane] : 0.0f;
+      cs[lane] = sc.col[c / 32];
+      if (EPI == T8_GLU) cs[32 + lane] = sc.up[c / 32];
       __syncwarp();
     }
+    tmem_wait_ld();
+    if (last) read_all();
     uint4 g[4];
-    t8_scaled(r, rs, cs, o.cs != nullptr, g);
+    t8_scaled(r, sc.row, cs, o.cs != nullptr, g);
     if (EPI == T8_BF16) {
       t8_store<4, 2>(stage, reinterpret_cast<uint8_t*>(reinterpret_cast<uint16_t*>(o.out) + row0 * o.ld + j), o.ld * 2, rows, cols, o.vec, g);
       continue;
     }
     uint4 u[4];
-    tmem_ld32(taddr + (uint32_t)(UP + c), r);
-    t8_scaled(r, rs, cs + 32, true, u);
+    t8_scaled(r2, sc.row, cs + 32, true, u);
     if (o.gu) {
       uint8_t* p = reinterpret_cast<uint8_t*>(o.gu + row0 * o.ld_gu + j);
       t8_store<4, 2>(stage, p, o.ld_gu * 2, rows, cols, o.vec_gu, g);
@@ -495,6 +517,11 @@ struct T8Tile {
   static constexpr int THREADS = 64 + 32 * EW, TCOLS = 2 * BN;
   static constexpr size_t SMEM = (size_t)STAGES * STAGE + EW * WARP + (EPI == T8_GLU ? 2 * SG_TAB * 4 : 0) + 1024;
 };
+// An accumulator is free again, on the barrier of the pair's leader.  What this orders is tensor memory's (tcgen05.wait::ld and the fence before it), no
+// other memory: with release semantics it would wait for the tile's stores as well.
+__device__ __forceinline__ void t8_arrive_leader(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 template <bool PAIR, int BN, int EPI>
 __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
     k_t8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ T8Out o, int* status) {
@@ -607,21 +634,29 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
       asm volatile("bar.sync 1, %0;" ::"n"(EW * 32) : "memory");
     }
     const uint32_t free0 = PAIR ? mapa_u32(smem_u32(&bar_tempty[0]), 0) : 0, free1 = PAIR ? mapa_u32(smem_u32(&bar_tempty[1]), 0) : 0;
-    int it = 0;
+    int it = 0, i0 = 0, j0 = 0;
+    T8Scales<EPI, CW> next = {};
+    if (unit < tiles) {
+      origin(unit, i0, j0);
+      next.fetch(o, i0 + (int)rank * 128 + q * 32, j0 + part * CW);
+    }
     for (int tile = unit; tile < tiles; tile += units, ++it) {
-      const int acc = it & 1;
-      int i0, j0;
-      origin(tile, i0, j0);
+      const int acc = it & 1, row0 = i0 + (int)rank * 128 + q * 32, col0 = j0 + part * CW;
+      const T8Scales<EPI, CW> now = next;
+      if (tile + units < tiles) {
+        origin(tile + units, i0, j0);
+        next.fetch(o, i0 + (int)rank * 128 + q * 32, j0 + part * CW);
+      }
       mbar_wait(&bar_tfull[acc], (uint32_t)(it >> 1) & 1u, abort_flag, status);      // passed over when it ran out: the lanes stay together
       tc_fence_after();
-      t8_epilogue<EPI, CW, BN / 2>(o, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part * CW), i0 + (int)rank * 128 + q * 32,
-                                   j0 + part * CW, stage, tab);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) mbar_arrive_remote(acc ? free1 : free0);
-        else mbar_arrive(&bar_tempty[acc]);
-      }
+      t8_epilogue<EPI, CW, BN / 2>(o, now, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * BN + part * CW), row0, col0, stage, tab, [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) t8_arrive_leader(acc ? free1 : free0);
+          else mbar_arrive(&bar_tempty[acc]);
+        }
+      });
     }
   }
 
