@@ -151,8 +151,8 @@ struct T8Grad {
   uint16_t* dgu;                          // GLU: the gradient, rows ld_dgu apart
   size_t ld_dgu;
   int M, N, W;                            // W: columns of d, N or N / 2
-  int vec;                                // rows in whole pieces of four
-  int tile;                               // rows of a tile of the first pass, 32 or 128
+  int vec;                                // rows in whole sixteen-byte pieces
+  int tile;                               // rows of a tile of the first pass, 16 to 128
 };
 // Four adjacent values from `at` on, n of them there; FULL: all, in one piece.
 template <bool FULL>
@@ -163,123 +163,191 @@ __device__ __forceinline__ uint2 t8_load4(const uint16_t* p, size_t at, int n, i
   for (int t = 0; t < 4; ++t) w[t] = t < n ? p[at + t] : 0u;
   return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
-// Four columns of both halves of a row of the gradient (GLU: gates' and ups', else columns 64 apart), on their way and as bf16 pairs.
+__device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? bfhi(t & 2 ? v.y : v.x) : bflo(t & 2 ? v.y : v.x); }
+
+// Largest magnitudes first.  A tile is up to 128 rows of 256 columns (GLU: of either half); a warp has every eighth
+// row, a lane eight of its columns.  Of a whole tile the rows come in by asynchronous copies, each lane's into places of its own, T8_AHEAD of them on their way, the
+// next tile's first ones with this one's last.
+constexpr int T8_AHEAD = 4;
+// eight columns' values of a row: GLU dh, gate and up, else dY
 template <bool GLU>
-struct T8Raw { uint2 d, e, u; };         // GLU: dh, gate, up; else both halves of dY
-template <bool FULL, bool GLU>
-__device__ __forceinline__ void t8_fetch(const T8Grad& x, size_t r, const int (&at)[2], const int (&left)[2], T8Raw<GLU>& w) {
-  w.d = t8_load4<FULL>(x.d, r * x.ld + at[0], left[0], x.vec);
-  if (GLU) {
-    w.e = t8_load4<FULL>(x.gu, r * x.ld_gu + at[0], left[0], x.vec);
-    w.u = t8_load4<FULL>(x.gu, r * x.ld_gu + x.W + at[0], left[0], x.vec);
-  } else {
-    w.e = t8_load4<FULL>(x.d, r * x.ld + at[1], left[1], x.vec);
-  }
-}
-template <bool GLU, int TAB>
-__device__ __forceinline__ void t8_grad4(const T8Raw<GLU>& w, const float* tab, uint2 (&v)[2]) {
-  if (!GLU) { v[0] = w.d; v[1] = w.e; return; }
+struct T8Row { uint4 d, e, u; };
+// a row's part of the maxima, and (GLU) its gradient stored
+template <bool FULL, bool GLU, int TAB>
+__device__ __forceinline__ void t8_max_row(const T8Grad& x, int r, const T8Row<GLU>& w, float sx, int left, uint16_t* to, const float (&sw)[2][8],
+                                           uint32_t (&cm)[2][8], uint32_t* __restrict__ rowmax, const float* tab) {
+  constexpr int H = GLU ? 2 : 1;
+  const bool there = FULL || r < x.M;
+  const uint32_t d4[4] = {w.d.x, w.d.y, w.d.z, w.d.w}, e4[4] = {w.e.x, w.e.y, w.e.z, w.e.w}, u4[4] = {w.u.x, w.u.y, w.u.z, w.u.w};
+  uint32_t v[2][4];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint32_t dd = k ? w.d.y : w.d.x, gg = k ? w.e.y : w.e.x, uu = k ? w.u.y : w.u.x;
+  for (int k = 0; k < 4; ++k) {
+    if (!GLU) { v[0][k] = d4[k]; continue; }
     float dg[2], du[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const float d = t ? bfhi(dd) : bflo(dd), g = t ? bfhi(gg) : bflo(gg), u = t ? bfhi(uu) : bflo(uu), sg = sigmoid_a8<TAB>(g, tab);
+      const float d = t ? bfhi(d4[k]) : bflo(d4[k]), g = t ? bfhi(e4[k]) : bflo(e4[k]), u = t ? bfhi(u4[k]) : bflo(u4[k]), sg = sigmoid_a8<TAB>(g, tab);
       du[t] = fmul(d, fmul(g, sg));
       dg[t] = fmul(fmul(d, u), fmul(sg, fadd(1.0f, fmul(g, fsub(1.0f, sg)))));
     }
-    (k ? v[0].y : v[0].x) = bf_pair(dg[0], dg[1]);
-    (k ? v[1].y : v[1].x) = bf_pair(du[0], du[1]);
+    v[0][k] = bf_pair(dg[0], dg[1]);
+    v[1][k] = bf_pair(du[0], du[1]);
   }
+  if (GLU && there) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (FULL) {
+        *reinterpret_cast<uint4*>(to + h * x.W) = make_uint4(v[h][0], v[h][1], v[h][2], v[h][3]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (32 * t < left) to[h * x.W + 32 * t] = (uint16_t)(v[h][t >> 1] >> (16 * (t & 1)));
+      }
+    }
+  }
+  uint32_t rm = 0;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // no factor is negative, and a NaN's bits are the largest
+      const float lo = fabsf(bflo(v[h][k])), hi = fabsf(bfhi(v[h][k]));
+      rm = __vimax3_u32(rm, __float_as_uint(fmul(lo, sw[h][2 * k])), __float_as_uint(fmul(hi, sw[h][2 * k + 1])));
+      cm[h][2 * k] = max(cm[h][2 * k], __float_as_uint(fmul(lo, sx)));
+      cm[h][2 * k + 1] = max(cm[h][2 * k + 1], __float_as_uint(fmul(hi, sx)));
+    }
+  rm = __reduce_max_sync(0xffffffffu, rm);
+  if ((threadIdx.x & 31) == 0 && there) atomicMax(rowmax + r, rm);
 }
-__device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? bfhi(t & 2 ? v.y : v.x) : bflo(t & 2 ? v.y : v.x); }
-
-// Largest magnitudes first.  A tile is 128 rows (32 where those would leave SMs without one) of 128 columns of either half (GLU), or of 256 columns; a
-// warp has every eighth row, a lane four columns of each half; four rows are on their way together.
-template <bool FULL, bool GLU, int TAB>
-__device__ __forceinline__ void t8_max_rows(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4], uint32_t (&cm)[2][4],
-                                            uint32_t* __restrict__ rowmax, const float* tab) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll 1
-  for (int i = 0; i < x.tile / 8; i += 4) {
-    T8Raw<GLU> w[4];
-    float sx[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + (i + k) * 8 + warp;
-      if (!FULL && r >= x.M) { w[k].d = w[k].e = w[k].u = make_uint2(0u, 0u); sx[k] = 0.0f; continue; }
-      t8_fetch<FULL, GLU>(x, r, at, left, w[k]);
-      sx[k] = fabsf(__ldg(x.s_x + r));
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + (i + k) * 8 + warp;
-      uint2 v[2];
-      t8_grad4<GLU, TAB>(w[k], tab, v);
-      if (GLU && (FULL || r < x.M)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint16_t* to = x.dgu + r * x.ld_dgu + h * x.W + at[0];
-          if (FULL) {
-            *reinterpret_cast<uint2*>(to) = v[h];
-          } else {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-              if (t < left[0]) to[t] = (uint16_t)((t & 2 ? v[h].y : v[h].x) >> (16 * (t & 1)));
-          }
-        }
-      }
-      uint32_t rm = 0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t a[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float m = fabsf(t8_at(v[h], t));                          // no factor is negative, and a NaN's bits are the largest
-          a[t] = __float_as_uint(fmul(m, sw[h][t]));
-          cm[h][t] = max(cm[h][t], __float_as_uint(fmul(m, sx[k])));
-        }
-        rm = __vimax3_u32(__vimax3_u32(rm, a[0], a[1]), a[2], a[3]);
-      }
-      rm = __reduce_max_sync(0xffffffffu, rm);
-      if (lane == 0 && (FULL || r < x.M)) atomicMax(rowmax + r, rm);
-    }
-  }
+__device__ __forceinline__ void t8_copy16(uint32_t place, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place), "l"(src) : "memory");
 }
 template <bool GLU, int TAB>
-__global__ void __launch_bounds__(256) k_t8_grad_max(const __grid_constant__ T8Grad x, uint32_t* __restrict__ rowmax, uint32_t* __restrict__ colmax) {
-  __shared__ __align__(16) float tab[TAB ? 2 * SG_TAB : 4];
-  __shared__ __align__(16) uint32_t cols[8][256];
+struct T8MaxRoom {                        // of a CTA, in shared memory
+  static constexpr int SLOT = (GLU ? 3 : 1) * 256 * 16, TABLE = TAB ? 2 * SG_TAB * 4 : 0;
+  static constexpr size_t BYTES = TABLE + 8 * 256 * 4 + T8_AHEAD * SLOT;
+};
+__device__ __forceinline__ uint4 t8_load8_any(const uint16_t* p, int n) {
+  uint32_t w[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) w[t] = 32 * t < n ? p[32 * t] : 0u;
+  return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+template <bool GLU, int TAB>
+__global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ T8Grad x, uint32_t* __restrict__ rowmax, uint32_t* __restrict__ colmax) {
+  typedef T8MaxRoom<GLU, TAB> Room;
+  constexpr int H = GLU ? 2 : 1;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  float* tab = reinterpret_cast<float*>(smem_raw);
+  uint32_t* cols = reinterpret_cast<uint32_t*>(smem_raw + Room::TABLE);   // [8][256]
+  const uint8_t* place = smem_raw + Room::TABLE + 8 * 256 * 4 + threadIdx.x * 16;
+  const uint32_t place_u = (uint32_t)__cvta_generic_to_shared(place);
   sg_copy_table<TAB>(tab);
   grid_dep();
-  constexpr int FW = GLU ? 128 : 256;                                     // columns of d in a tile
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int across = (x.W + FW - 1) / FW, tiles = across * ((x.M + x.tile - 1) / x.tile);
+  const int across = (x.W + 255) / 256, tiles = across * ((x.M + x.tile - 1) / x.tile), rows = x.tile / 8;
+  auto whole = [&](int tile) { return x.vec && tile % across * 256 + 256 <= x.W && tile / across * x.tile + x.tile <= x.M; };
+  // where the next row to fetch lies, and how many of its tile's rows have been fetched
+  const uint16_t *fd = nullptr, *fg = nullptr;
+  auto begin = [&](int tile) {
+    const size_t r = tile / across * x.tile + warp;
+    const int c = tile % across * 256 + lane * 8;
+    fd = x.d + r * x.ld + c;
+    if (GLU) fg = x.gu + r * x.ld_gu + c;
+  };
+  auto fetch = [&](int slot) {
+    const uint32_t to = place_u + slot * Room::SLOT;
+    t8_copy16(to, fd);
+    fd += 8 * x.ld;
+    if (GLU) {
+      t8_copy16(to + 4096, fg);
+      t8_copy16(to + 8192, fg + x.W);
+      fg += 8 * x.ld_gu;
+    }
+  };
+  bool ahead = false;                                                     // the first rows are on their way
 #pragma unroll 1
   for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int c0 = tile % across * FW, r0 = tile / across * x.tile;
-    const int at[2] = {c0 + lane * 4, c0 + lane * 4 + (GLU ? 0 : 128)}, left[2] = {x.W - at[0], x.W - at[1]};
-    float sw[2][4];
-    uint32_t cm[2][4];
+    // a lane's eight columns are adjacent in a whole tile, else 32 apart, so that values that are read one by one lie side by side over the lanes
+    const bool full = whole(tile);
+    const int step = full ? 1 : 32, c = tile % across * 256 + (full ? lane * 8 : lane), r0 = tile / across * x.tile + warp, left = x.W - c;
+    float sw[2][8];
+    uint32_t cm[2][8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        sw[h][t] = t < left[h] ? fabsf(x.s_w[(GLU ? h * x.W : 0) + at[h] + t]) : 0.0f;
+      for (int t = 0; t < 8; ++t) {
+        sw[h][t] = step * t < left ? fabsf(x.s_w[h * x.W + c + step * t]) : 0.0f;
         cm[h][t] = 0;
       }
-    if (x.vec && c0 + FW <= x.W && r0 + x.tile <= x.M) t8_max_rows<true, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
-    else t8_max_rows<false, GLU, TAB>(x, r0, at, left, sw, cm, rowmax, tab);
-    if (tile != blockIdx.x) __syncthreads();                              // the columns before have been read
+    const float sx_all = lane < rows && r0 + lane * 8 < x.M ? fabsf(__ldg(x.s_x + r0 + lane * 8)) : 0.0f;     // row i's with lane i
+    uint16_t* to = GLU ? x.dgu + r0 * x.ld_dgu + c : nullptr;
+    if (full) {
+      const int then = tile + gridDim.x;
+      const bool more = then < tiles && whole(then);
+      if (!ahead) {
+        begin(tile);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) *reinterpret_cast<uint4*>(&cols[warp][h * 128 + lane * 4]) = make_uint4(cm[h][0], cm[h][1], cm[h][2], cm[h][3]);
-    __syncthreads();
-    uint32_t m = 0;
+        for (int i = 0; i < T8_AHEAD; ++i) {
+          fetch(i);
+          fetch_close();
+        }
+      }
+#pragma unroll 1
+      for (int i0 = 0; i0 < rows; i0 += T8_AHEAD) {
+        const bool end = i0 + T8_AHEAD == rows;                           // this tile's rows are all on their way
+        if (end && more) begin(then);
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, cols[w][threadIdx.x]);
-    const int c = c0 + (GLU ? threadIdx.x & 127 : threadIdx.x);
-    if (c < x.W) atomicMax(colmax + (GLU ? (threadIdx.x >> 7) * x.W : 0) + c, m);
+        for (int k = 0; k < T8_AHEAD; ++k) {
+          const float sx = __shfl_sync(0xffffffffu, sx_all, i0 + k);
+          fetch_wait<T8_AHEAD - 1>();
+          const uint8_t* from = place + k * Room::SLOT;
+          T8Row<GLU> w;
+          w.d = *reinterpret_cast<const uint4*>(from);
+          if (GLU) {
+            w.e = *reinterpret_cast<const uint4*>(from + 4096);
+            w.u = *reinterpret_cast<const uint4*>(from + 8192);
+          }
+          if (!end || more) fetch(k);
+          fetch_close();                                                  // of nothing at the very end, so that the count stays
+          t8_max_row<true, GLU, TAB>(x, r0 + (i0 + k) * 8, w, sx, left, to, sw, cm, rowmax, tab);
+          if (GLU) to += 8 * x.ld_dgu;
+        }
+      }
+      ahead = more;
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < rows; i += 2) {                                 // two rows' values, read one by one, on their way together
+        T8Row<GLU> w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const size_t r = r0 + (i + k) * 8;
+          const int n = r < (size_t)x.M ? left : 0;
+          w[k].d = t8_load8_any(x.d + r * x.ld + c, n);
+          if (GLU) {
+            w[k].e = t8_load8_any(x.gu + r * x.ld_gu + c, n);
+            w[k].u = t8_load8_any(x.gu + r * x.ld_gu + x.W + c, n);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          t8_max_row<false, GLU, TAB>(x, r0 + (i + k) * 8, w[k], __shfl_sync(0xffffffffu, sx_all, i + k), left, to, sw, cm, rowmax, tab);
+          if (GLU) to += 8 * x.ld_dgu;
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      if (tile != blockIdx.x || h) __syncthreads();                       // the columns before have been read
+#pragma unroll
+      for (int t = 0; t < 8; ++t) cols[warp * 256 + (full ? lane * 8 : lane) + step * t] = cm[h][t];
+      __syncthreads();
+      uint32_t m = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) m = max(m, cols[w * 256 + threadIdx.x]);
+      const int j = tile % across * 256 + threadIdx.x;
+      if (j < x.W) atomicMax(colmax + h * x.W + j, m);
+    }
   }
 }
 // The scales and their inverses, once for every row and column; a scale that is a NaN has the inverse -1.
@@ -301,26 +369,26 @@ __device__ __forceinline__ void t8_code_rows(const T8Grad& x, int r0, const int 
   const int ldn = t8_ld(x.N);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    T8Raw<false> w[4];
+    uint2 w[4][2];
     float sx[4], ia[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = r0 + half * 4 + k;
-      if (!FULL && r >= x.M) { w[k].d = w[k].e = make_uint2(0u, 0u); sx[k] = 0.0f; continue; }
-      t8_fetch<FULL, false>(x, r, at, left, w[k]);
+      if (!FULL && r >= x.M) { w[k][0] = w[k][1] = make_uint2(0u, 0u); sx[k] = ia[k] = 0.0f; continue; }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) w[k][h] = t8_load4<FULL>(x.d, r * x.ld + at[h], left[h], x.vec);
       sx[k] = __ldg(x.s_x + r);
       ia[k] = __ldg(i_a + r);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = r0 + half * 4 + k;
-      const uint2 v[2] = {w[k].d, w[k].e};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t a[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const float y = t8_at(v[h], t);
+          const float y = t8_at(w[k][h], t);
           const uint32_t code = t8_code(fmul(y, sx[k]), ig[h][t]);
           a[t] = t8_code(fmul(y, sw[h][t]), ia[k]);
           g[h][half][t] = k == 0 ? code : __byte_perm(g[h][half][t], code, k == 1 ? 0x3240 : k == 2 ? 0x3410 : 0x4210);
@@ -345,7 +413,10 @@ __global__ void __launch_bounds__(256, 3) k_t8_grad_codes(const __grid_constant_
                                                           int8_t* __restrict__ qa, int8_t* __restrict__ qgt) {
   grid_dep();
   __shared__ __align__(16) uint8_t out[128 * 128];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, ldm = t8_ld(x.M), c0 = blockIdx.x * 128, r0 = blockIdx.y * 128;
+  // eight tiles of rows under one another, then the next columns: what runs at a time reads long pieces of rows and writes long pieces of columns
+  const int across = (x.N + 127) / 128, down = (x.M + 127) / 128, panel = blockIdx.x / (8 * across), in = blockIdx.x - panel * 8 * across;
+  const int high = min(8, down - panel * 8), c0 = in / high * 128, r0 = (panel * 8 + in % high) * 128;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, ldm = t8_ld(x.M);
   const int at[2] = {c0 + tx * 4, c0 + tx * 4 + 64}, left[2] = {x.N - at[0], x.N - at[1]};
   float sw[2][4], ig[2][4];
 #pragma unroll
@@ -1112,11 +1183,9 @@ static int t8_sizes(long long M, long long N, long long K) {
 }
 static int t8_vec(const void* p, size_t ld, int size) { return aligned16(p) && ld * size % 16 == 0; }
 
-static int t8_vec4(const void* p, size_t ld) { return aligned_to(p, 8) && ld % 4 == 0; }
-
 // gradient operands into the workspace, then both products
 struct T8Ws { size_t qa, qgt, qxt, s_a, s_g, i_a, i_g, rowmax, colmax, dgu, bytes; };
-static size_t t8_ld_dgu(int N) { return ((size_t)N + 3) / 4 * 4; }
+static size_t t8_ld_dgu(int N) { return ((size_t)N + 7) / 8 * 8; }
 static T8Ws t8_ws(int M, int N, int K, bool glu) {
   T8Ws w;
   size_t at = 0;
@@ -1136,11 +1205,18 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
 }
 struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *i_a, *s_g, *i_g; int8_t *qa, *qgt; };
 template <bool GLU, int TAB>
-static void t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
-  const long long across = (x.W + (GLU ? 127 : 255)) / (GLU ? 128 : 256);
-  x.tile = across * ((x.M + 127) / 128) < 2 * sms ? 32 : 128;
-  const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = TAB ? 3LL * sms : 0x7fffffffLL;    // with a table CTAs stay and walk over the tiles
-  launch_after(k_t8_grad_max<GLU, TAB>, (unsigned)(tiles < most ? tiles : most), 256, 0, st, x, o.rowmax, o.colmax);
+static int t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
+  const size_t smem = T8MaxRoom<GLU, TAB>::BYTES;
+  static DevOnce once = {};
+  if (smem > 48 * 1024 && dev_ensure_smem(once, (const void*)k_t8_grad_max<GLU, TAB>, smem) != DET_OK) return DET_ERR_CUDA;
+  const long long across = (x.W + 255) / 256;
+  // the most rows with which there are still some tiles for every place of a CTA; rows without a common alignment, whose loads wait one by one, fewer
+  x.tile = 128;
+  while (x.tile > (x.vec ? 32 : 16) && across * ((x.M + x.tile - 1) / x.tile) < 6 * sms) x.tile /= 2;
+  const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = (GLU ? 2LL : 3LL) * sms;    // CTAs stay and walk over the tiles
+  launch_after(k_t8_grad_max<GLU, TAB>, (unsigned)(tiles < most ? tiles : most), 256, smem, st, x, o.rowmax, o.colmax);
+  DET_CHECK_LAUNCH();
+  return DET_OK;
 }
 static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int K, uint16_t* dX, int ld_dx, float* dW, char* ws, int* status,
                        cudaStream_t st) {
@@ -1151,13 +1227,13 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
   float *s_a = (float*)(ws + w.s_a), *s_g = (float*)(ws + w.s_g);
   const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), s_a, (float*)(ws + w.i_a), s_g, (float*)(ws + w.i_g), qa, qgt};
   if (cudaMemsetAsync(op.rowmax, 0, w.dgu - w.rowmax, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
-  if (!x.gu) t8_largest<false, 0>(x, op, sms, st);
-  else if ((long long)M * x.W >= 8LL * sms * 128 * 64) t8_largest<true, 1>(x, op, sms, st);      // some tiles for every CTA
-  else t8_largest<true, 0>(x, op, sms, st);
+  const bool table = (long long)M * x.W >= 8LL * sms * 128 * 64;           // some tiles for every CTA
+  const int rc0 = !x.gu ? t8_largest<false, 0>(x, op, sms, st) : table ? t8_largest<true, 1>(x, op, sms, st) : t8_largest<true, 0>(x, op, sms, st);
+  if (rc0 != DET_OK) return rc0;
   launch_after(k_t8_scales, (unsigned)((M + N + 255) / 256), 256, 0, st, op.rowmax, op.colmax, M, N, op.s_a, op.i_a, op.s_g, op.i_g);
   T8Grad y = x;                                                            // as the codes are made of it
   if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
-  launch_after(k_t8_grad_codes, dim3((N + 127) / 128, (M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, qa, qgt);
+  launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, qa, qgt);
   DET_CHECK_LAUNCH();
   if (dX) {
     T8Out o = {};
@@ -1256,7 +1332,7 @@ extern "C" int det_tok8_linear_bwd(const det_bf16* dY, int ld_dy, const int8_t* 
   const int rc = t8_bwd_check(dY, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, det_tok8_linear_bwd_ws_bytes(M, N, K), ws_bytes);
   if (rc != DET_OK) return rc;
   if (!M) return t8_no_rows(dW, N, K, (cudaStream_t)stream);
-  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec4(dY, ld_dy) && N % 4 == 0, 0};
+  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec(dY, ld_dy, 2), 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
 
@@ -1305,6 +1381,6 @@ extern "C" int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* g
   if (rc != DET_OK) return rc;
   if (!aligned_to(gu, 2)) return DET_ERR_ALIGN;
   if (!M) return t8_no_rows(dW, 2 * F, K, (cudaStream_t)stream);
-  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec4(dh, ld_dh) && t8_vec4(gu, ld_gu) && F % 4 == 0, 0};
+  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec(dh, ld_dh, 2) && t8_vec(gu, ld_gu, 2) && F % 8 == 0, 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
