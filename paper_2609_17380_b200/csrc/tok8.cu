@@ -595,7 +595,7 @@ __device__ __forceinline__ void t8_arrive_leader(uint32_t cluster_addr) {
 }
 template <bool PAIR, int BN, int EPI>
 __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
-    k_t8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ T8Out o, int* status) {
+    k_t8_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ T8Out o, int* status, int fill) {
   typedef T8Tile<PAIR, BN, EPI> T;
   constexpr int STAGES = T::STAGES, EW = T::EW, BH = EPI == T8_GLU ? BN / 2 : BN;    // BH: columns of the output in a tile
   extern __shared__ uint8_t smem_raw[];
@@ -629,7 +629,8 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
   if (PAIR) cluster_sync_all();          // the peer's barriers are initialised before anything can signal them
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_s;
-  grid_dep();
+  if (fill) grid_fill_begin();           // nothing of the kernel before is needed (common.cuh)
+  else grid_dep();
 
   const int tiles_i = (o.I + T::BM - 1) / T::BM, tiles_j = (o.J + BH - 1) / BH, tiles = tiles_i * tiles_j, kblocks = (o.K + T8_K - 1) / T8_K;
   const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
@@ -744,6 +745,7 @@ __global__ void __launch_bounds__(T8Tile<PAIR, BN, EPI>::THREADS, 1)
     if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)T::TCOLS) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)T::TCOLS) : "memory");
   }
+  if (fill) grid_fill_end();
 }
 
 // ---- few tokens ----------------------------------------------------------------------------------------------
@@ -923,7 +925,7 @@ static int t8_few(const T8Few& f, cudaStream_t st) {
 }
 
 template <bool PAIR, int BN, int EPI>
-static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
+static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int fill, int* status, cudaStream_t st) {
   typedef T8Tile<PAIR, BN, EPI> T;
   constexpr int BH = EPI == T8_GLU ? BN / 2 : BN;
   static DevOnce once = {};
@@ -935,7 +937,7 @@ static int t8_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& 
     return DET_ERR_CUDA;
   const long long tiles = (long long)((o.I + T::BM - 1) / T::BM) * ((o.J + BH - 1) / BH);
   const int units = PAIR ? sms / 2 : sms, grid = (int)(tiles < units ? tiles : units) * (PAIR ? 2 : 1);
-  launch_after_cluster(k_t8_gemm<PAIR, BN, EPI>, grid, T::THREADS, T::SMEM, PAIR ? 2 : 1, st, ta, tb, o, status);
+  launch_after_cluster(k_t8_gemm<PAIR, BN, EPI>, grid, T::THREADS, T::SMEM, PAIR ? 2 : 1, st, ta, tb, o, status, fill);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -971,7 +973,7 @@ __device__ __forceinline__ void t8_put4(T* to, int left, int vec, const T (&v)[4
 }
 template <int BM, int EPI>
 __global__ void __launch_bounds__(192) k_t8_split(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                                                  const __grid_constant__ T8Out o, int parts, int* status) {
+                                                  const __grid_constant__ T8Out o, int parts, int* status, int fill) {
   typedef T8Split<BM> T;
   constexpr int BH = EPI == T8_GLU ? 32 : 64;
   extern __shared__ uint8_t smem_raw[];
@@ -999,7 +1001,8 @@ __global__ void __launch_bounds__(192) k_t8_split(const __grid_constant__ CUtens
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_s;
-  grid_dep();
+  if (fill) grid_fill_begin();
+  else grid_dep();
 
   const int tile = blockIdx.x / parts, tiles_i = (o.I + 127) / 128, i0 = tile % tiles_i * 128, j0 = tile / tiles_i * BH;
   const int kblocks = (o.K + T8_K - 1) / T8_K, kb0 = (int)((long long)kblocks * rank / parts), kb1 = (int)((long long)kblocks * (rank + 1) / parts);
@@ -1113,22 +1116,23 @@ __global__ void __launch_bounds__(192) k_t8_split(const __grid_constant__ CUtens
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(64u) : "memory");
   }
+  if (fill) grid_fill_end();
 }
 template <int BM, int EPI>
-static int t8_split_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int* status, cudaStream_t st) {
+static int t8_split_launch(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int fill, int* status, cudaStream_t st) {
   static DevOnce once = {};
   if (dev_ensure_smem(once, (const void*)k_t8_split<BM, EPI>, T8Split<BM>::SMEM) != DET_OK) return DET_ERR_CUDA;
   CUtensorMap ta, tb;
   if (!make_map_ld(&ta, A, o.I, o.K, t8_ld(o.K), BM) || !make_map_ld(&tb, B, rows_b, o.K, t8_ld(o.K), EPI == T8_GLU ? 32 : 64)) return DET_ERR_CUDA;
   const int bh = EPI == T8_GLU ? 32 : 64, tiles = ((o.I + 127) / 128) * ((o.J + bh - 1) / bh);
-  launch_after_cluster(k_t8_split<BM, EPI>, tiles * parts, 192, T8Split<BM>::SMEM, parts, st, ta, tb, o, parts, status);
+  launch_after_cluster(k_t8_split<BM, EPI>, tiles * parts, 192, T8Split<BM>::SMEM, parts, st, ta, tb, o, parts, status, fill);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
 template <int EPI>
-static int t8_split(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int* status, cudaStream_t st) {
-  if (o.I <= 32) return t8_split_launch<32, EPI>(A, B, rows_b, o, parts, status, st);
-  return t8_split_launch<128, EPI>(A, B, rows_b, o, parts, status, st);
+static int t8_split(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int parts, int fill, int* status, cudaStream_t st) {
+  if (o.I <= 32) return t8_split_launch<32, EPI>(A, B, rows_b, o, parts, fill, status, st);
+  return t8_split_launch<128, EPI>(A, B, rows_b, o, parts, fill, status, st);
 }
 
 // The tile by whole rounds of tiles over the SMs, each the longer of its multiply loop and its epilogue, once the other of the two and what a launch takes
@@ -1136,30 +1140,45 @@ static int t8_split(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o
 // contraction for each; their exchange takes longer the more rows there are.  Measured over 32 shapes, the rule within 14 % of the best of all: 24 x 2048 x 8192
 // with 8 CTAs to a tile 8.7, alone 23.9; 128 x 2048 x 8192 with 4 12.4, alone 24.3; 256 x 2048 x 2048 with 2 11.6, alone 8.9 (64 columns), 9.5 (128), 12.0 (pair);
 // 2738 x 520 x 1003 9.4, 7.6, 10.2; 8192 x 2048 x 2048 78, 43, 30.
-template <int EPI>
-static int t8_product(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
-  const int sms = dev_sm_count();
-  if (sms < 2) return DET_ERR_CUDA;
+struct T8Plan { int pick, parts; long long ctas; };      // pick: pair, 128 or 64 columns; parts > 1: CTAs to a tile
+static T8Plan t8_plan(int epi, const T8Out& o, int sms) {
   static const struct { int bn, bi; double step, turn, epi[3]; } C[3] = {
       {256, 256, 0.365, 0.9, {4.2, 6.6, 6.0}}, {128, 128, 0.30, 0.5, {1.7, 3.8, 3.0}}, {64, 128, 0.30, 0.5, {1.2, 1.5, 2.0}}};
   const int steps = (o.K + T8_K - 1) / T8_K;
-  int pick = 0;
+  T8Plan plan = {0, 1, 0};
   double best = 0.0;
   for (int i = 0; i < 3; ++i) {
-    const int bh = EPI == T8_GLU ? C[i].bn / 2 : C[i].bn, units = i == 0 ? sms / 2 : sms;
+    const int bh = epi == T8_GLU ? C[i].bn / 2 : C[i].bn, units = i == 0 ? sms / 2 : sms;
     const double tiles = (double)((o.I + C[i].bi - 1) / C[i].bi) * ((o.J + bh - 1) / bh), rounds = (double)(long long)((tiles + units - 1) / units);
-    const double loop = steps * C[i].step, e = C[i].epi[EPI], t = 2.0 + rounds * ((loop > e ? loop : e) + C[i].turn) + (loop > e ? e : loop);
-    if (i == 0 || t < best) { best = t; pick = i; }
+    const double loop = steps * C[i].step, e = C[i].epi[epi], t = 2.0 + rounds * ((loop > e ? loop : e) + C[i].turn) + (loop > e ? e : loop);
+    if (i == 0 || t < best) {
+      best = t;
+      plan.pick = i;
+      plan.ctas = (long long)(tiles < units ? tiles : units) * (i == 0 ? 2 : 1);
+    }
   }
-  const int bh = EPI == T8_GLU ? 32 : 64, room = o.I <= 32 ? 2 * sms : sms;
+  const int bh = epi == T8_GLU ? 32 : 64, room = o.I <= 32 ? 2 * sms : sms;
   const long long tiles = (long long)((o.I + 127) / 128) * ((o.J + bh - 1) / bh);
   // clusters of eight large CTAs find their SMs in few places: half of the GPU
   int parts = 1;
   while (parts < 8 && tiles * parts * 2 <= (parts == 4 && o.I > 32 ? room / 2 : room) && steps >= parts * 4) parts *= 2;
-  if (parts > 1 && 5.2 + 0.025 * (o.I < 128 ? o.I : 168) + steps * 0.27 / parts < best) return t8_split<EPI>(A, B, rows_b, o, parts, status, st);
-  if (pick == 0) return t8_launch<true, 256, EPI>(A, B, rows_b, o, status, st);
-  if (pick == 1) return t8_launch<false, 128, EPI>(A, B, rows_b, o, status, st);
-  return t8_launch<false, 64, EPI>(A, B, rows_b, o, status, st);
+  if (parts > 1 && 5.2 + 0.025 * (o.I < 128 ? o.I : 168) + steps * 0.27 / parts < best) {
+    plan.parts = parts;
+    plan.ctas = tiles * parts;
+  }
+  return plan;
+}
+template <int EPI>
+static int t8_product(const T8Plan& plan, const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int fill, int* status, cudaStream_t st) {
+  if (plan.parts > 1) return t8_split<EPI>(A, B, rows_b, o, plan.parts, fill, status, st);
+  if (plan.pick == 0) return t8_launch<true, 256, EPI>(A, B, rows_b, o, fill, status, st);
+  if (plan.pick == 1) return t8_launch<false, 128, EPI>(A, B, rows_b, o, fill, status, st);
+  return t8_launch<false, 64, EPI>(A, B, rows_b, o, fill, status, st);
+}
+template <int EPI>
+static int t8_product(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o, int* status, cudaStream_t st) {
+  const int sms = dev_sm_count();
+  return sms < 2 ? DET_ERR_CUDA : t8_product<EPI>(t8_plan(EPI, o, sms), A, B, rows_b, o, 0, status, st);
 }
 
 static int t8_quant(const uint16_t* X, int ld, int M, int K, int8_t* q, float* s, cudaStream_t st) {
@@ -1223,9 +1242,9 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
   const int M = x.M, N = x.N, sms = dev_sm_count();
   if (sms <= 0) return DET_ERR_CUDA;
   const T8Ws w = t8_ws(M, N, K, x.gu != nullptr);
-  int8_t *qa = (int8_t*)(ws + w.qa), *qgt = (int8_t*)(ws + w.qgt), *qxt = (int8_t*)(ws + w.qxt);
-  float *s_a = (float*)(ws + w.s_a), *s_g = (float*)(ws + w.s_g);
-  const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), s_a, (float*)(ws + w.i_a), s_g, (float*)(ws + w.i_g), qa, qgt};
+  int8_t* qxt = (int8_t*)(ws + w.qxt);
+  const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), (float*)(ws + w.s_a), (float*)(ws + w.i_a), (float*)(ws + w.s_g),
+                         (float*)(ws + w.i_g), (int8_t*)(ws + w.qa), (int8_t*)(ws + w.qgt)};
   if (cudaMemsetAsync(op.rowmax, 0, w.dgu - w.rowmax, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
   const bool table = (long long)M * x.W >= 8LL * sms * 128 * 64;           // some tiles for every CTA
   const int rc0 = !x.gu ? t8_largest<false, 0>(x, op, sms, st) : table ? t8_largest<true, 1>(x, op, sms, st) : t8_largest<true, 0>(x, op, sms, st);
@@ -1233,22 +1252,24 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
   launch_after(k_t8_scales, (unsigned)((M + N + 255) / 256), 256, 0, st, op.rowmax, op.colmax, M, N, op.s_a, op.i_a, op.s_g, op.i_g);
   T8Grad y = x;                                                            // as the codes are made of it
   if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
-  launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, qa, qgt);
+  launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, op.qa, op.qgt);
   DET_CHECK_LAUNCH();
-  if (dX) {
-    T8Out o = {};
-    o.out = dX; o.ld = ld_dx; o.rs = s_a; o.I = M; o.J = K; o.K = N; o.vec = t8_vec(dX, ld_dx, 2);
-    const int rc = t8_product<T8_BF16>(qa, qWt, K, o, status, st);
-    if (rc != DET_OK) return rc;
+  T8Out ox = {}, ow = {};
+  ox.out = dX; ox.ld = ld_dx; ox.rs = op.s_a; ox.I = M; ox.J = K; ox.K = N; ox.vec = t8_vec(dX, ld_dx, 2);
+  ow.out = dW; ow.ld = K; ow.rs = op.s_g; ow.I = N; ow.J = K; ow.K = M; ow.vec = t8_vec(dW, K, 4);
+  const T8Plan px = t8_plan(T8_BF16, ox, sms), pw = t8_plan(T8_F32, ow, sms);
+  const dim3 tgrid((K + 127) / 128, (M + 127) / 128);
+  // Where the first product leaves SMs without a CTA the second comes in beside it, and the transposition has to be done before; else the transposition runs
+  // beside the first product, which leaves the memory idle and room on every SM for two CTAs of it (8192 x 2048 x 8192: 248 -> 229 us).
+  const bool beside = dX && dW && px.ctas < sms;
+  if (beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, 1);
+  int rc = DET_OK;
+  if (dX) rc = t8_product<T8_BF16>(px, op.qa, qWt, K, ox, 0, status, st);
+  if (dW && rc == DET_OK) {
+    if (!beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, dX ? 1 : 0);
+    rc = t8_product<T8_F32>(pw, op.qgt, qxt, K, ow, beside ? 1 : 0, status, st);
   }
-  if (dW) {
-    // beside the other product, which leaves the memory idle and room on every SM for two CTAs of this
-    launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, st, qX, M, K, qxt, dX ? 1 : 0);
-    T8Out o = {};
-    o.out = dW; o.ld = K; o.rs = s_g; o.I = N; o.J = K; o.K = M; o.vec = t8_vec(dW, K, 4);
-    const int rc = t8_product<T8_F32>(qgt, qxt, K, o, status, st);
-    if (rc != DET_OK) return rc;
-  }
+  if (rc != DET_OK) return rc;
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
