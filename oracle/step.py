@@ -34,12 +34,36 @@ def _specs(cfg):
         s += norm("embed_norm")
     for l in range(L):
         s += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (2 * D if _recurrent(cfg, l) else nq, D)), ("l%d.w_o" % l, (D, D))]
-        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D)), ("l%d.w_down" % l, (D, Fh)), ("l%d.s_x" % l, (4,))]
+        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D)), ("l%d.w_down" % l, (D, Fh))]
+        s += [] if _by_token(cfg) else [("l%d.s_x" % l, (4,))]
     return s + norm("final_norm") + [("lm_head", (V, D))]
 
 
 def _layer(cfg):
     return cfg.get("norm", "rms") == "layer"
+
+
+def _by_token(cfg):
+    """Linears whose scales follow the values, by token and output channel, in place of the learned steps."""
+    return cfg.get("linear", "lsq") == "token"
+
+
+def _linear(cfg, P, sw, l, w, i, x):
+    name = "l%d.%s" % (l, w)
+    if _by_token(cfg):
+        return O.tok8_linear_fwd(x, P[name])[0]
+    return O.linear_fwd(x, P[name], P["l%d.s_x" % l][i:i + 1], sw[name])[0]
+
+
+def _linear_bwd(cfg, P, G, ds, sw, l, w, i, dy, x):
+    """The gradient of the linear's input; the weights' goes to G, the step's to ds."""
+    name = "l%d.%s" % (l, w)
+    if _by_token(cfg):
+        dx, G[name] = O.tok8_linear_bwd(dy, x, P[name])
+        return dx
+    dx, G[name], d = O.linear_bwd(dy, x, P[name], P["l%d.s_x" % l][i:i + 1], sw[name], cfg.get("hadamard_block", 128))
+    ds[i] = d[0]
+    return dx
 
 
 def _recurrent(cfg, l):
@@ -93,28 +117,28 @@ def forward(cfg, P, sw, tok, calibrate=False):
         x, saved["stat_emb"] = _norm(cfg, P, "embed_norm", x)
     rope = cfg.get("rope_tables")
     for l in range(L):
-        sx = P["l%d.s_x" % l]
+        sx = P.get("l%d.s_x" % l)
         a = {"x": x}
         a["n1"], a["stat1"] = _norm(cfg, P, "l%d.attn_norm" % l, x)
         if calibrate:
             sx[0] = O.lsq_act_scale_init(a["n1"])[0]
-        a["qkv"], _, _ = O.linear_fwd(a["n1"], P["l%d.w_qkv" % l], sx[0:1], sw["l%d.w_qkv" % l])
+        a["qkv"] = _linear(cfg, P, sw, l, "w_qkv", 0, a["n1"])
         if _recurrent(cfg, l):
             a["att"], _, a["states"] = O.linrec_fwd(a["qkv"], B, S)
         else:
             _attention(cfg, l, a, rope)
         if calibrate:
             sx[1] = O.lsq_act_scale_init(a["att"])[0]
-        o, _, _ = O.linear_fwd(a["att"], P["l%d.w_o" % l], sx[1:2], sw["l%d.w_o" % l])
+        o = _linear(cfg, P, sw, l, "w_o", 1, a["att"])
         a["h"] = O.residual_add(x, o)
         a["n2"], a["stat2"] = _norm(cfg, P, "l%d.ffn_norm" % l, a["h"])
         if calibrate:
             sx[2] = O.lsq_act_scale_init(a["n2"])[0]
-        a["gu"], _, _ = O.linear_fwd(a["n2"], P["l%d.w_gu" % l], sx[2:3], sw["l%d.w_gu" % l])
+        a["gu"] = _linear(cfg, P, sw, l, "w_gu", 2, a["n2"])
         a["act"] = O.swiglu_fwd(a["gu"])
         if calibrate:
             sx[3] = O.lsq_act_scale_init(a["act"])[0]
-        dn, _, _ = O.linear_fwd(a["act"], P["l%d.w_down" % l], sx[3:4], sw["l%d.w_down" % l])
+        dn = _linear(cfg, P, sw, l, "w_down", 3, a["act"])
         x = O.residual_add(a["h"], dn)
         saved["layers"].append(a)
     saved["xf"] = x
@@ -139,7 +163,6 @@ def _attention_bwd(cfg, l, a, d_att, rope):
 def microbatch_grad(cfg, P, sw, tok):
     """Forward + backward of one micro-batch; returns (flat f32 gradient in canonical order, mean loss)."""
     L, S, B = cfg["n_layers"], cfg["seq"], cfg["micro_batch"]
-    hb = cfg.get("hadamard_block", 128)
     rope = cfg.get("rope_tables")
     sv = forward(cfg, P, sw, tok)
     labels = tok[:, 1:].reshape(-1).astype(np.int32)
@@ -151,23 +174,22 @@ def microbatch_grad(cfg, P, sw, tok):
     dx = _norm_bwd(cfg, P, G, "final_norm", d_nf, sv["xf"], sv["statf"])
     for l in reversed(range(L)):
         a = sv["layers"][l]
-        sx = P["l%d.s_x" % l]
         ds = np.zeros(4, np.float32)
         gu = _kept(cfg, a["gu"])
         act = O.swiglu_fwd(gu) if cfg.get("act8") else a["act"]         # made again from what was kept
-        d_act, G["l%d.w_down" % l], d3 = O.linear_bwd(dx, act, P["l%d.w_down" % l], sx[3:4], sw["l%d.w_down" % l], hb)
+        d_act = _linear_bwd(cfg, P, G, ds, sw, l, "w_down", 3, dx, act)
         d_gu = O.swiglu_bwd(d_act, gu)
-        d_n2, G["l%d.w_gu" % l], d2 = O.linear_bwd(d_gu, a["n2"], P["l%d.w_gu" % l], sx[2:3], sw["l%d.w_gu" % l], hb)
+        d_n2 = _linear_bwd(cfg, P, G, ds, sw, l, "w_gu", 2, d_gu, a["n2"])
         d_h = _norm_bwd(cfg, P, G, "l%d.ffn_norm" % l, d_n2, _kept(cfg, a["h"]), a["stat2"], dx)
-        d_att, G["l%d.w_o" % l], d1 = O.linear_bwd(d_h, a["att"], P["l%d.w_o" % l], sx[1:2], sw["l%d.w_o" % l], hb)
+        d_att = _linear_bwd(cfg, P, G, ds, sw, l, "w_o", 1, d_h, a["att"])
         if _recurrent(cfg, l):
             d_qkv, _ = O.linrec_bwd(d_att, _kept(cfg, a["qkv"]), a["states"], B, S)
         else:
             d_qkv = _attention_bwd(cfg, l, a, d_att, rope)
-        d_n1, G["l%d.w_qkv" % l], d0 = O.linear_bwd(d_qkv, a["n1"], P["l%d.w_qkv" % l], sx[0:1], sw["l%d.w_qkv" % l], hb)
+        d_n1 = _linear_bwd(cfg, P, G, ds, sw, l, "w_qkv", 0, d_qkv, a["n1"])
         dx = _norm_bwd(cfg, P, G, "l%d.attn_norm" % l, d_n1, _kept(cfg, a["x"]), a["stat1"], d_h)
-        ds[0], ds[1], ds[2], ds[3] = d0[0], d1[0], d2[0], d3[0]
-        G["l%d.s_x" % l] = ds
+        if not _by_token(cfg):
+            G["l%d.s_x" % l] = ds
     if cfg.get("embed_norm"):
         dx = _norm_bwd(cfg, P, G, "embed_norm", dx, sv["x_emb"], sv["stat_emb"])
     G["embed"] = O.embed_bwd(sv["inp"], dx, cfg["vocab"])
@@ -179,17 +201,18 @@ def run_step(cfg, params, tokens, opt=None, calibrate=True):
     """One optimizer step.  cfg: dict (n_layers, d_model, n_heads, ffn, vocab, seq, micro_batch, mesh=(accum,
     dp_shard, dp_replicate), optional hadamard_block, z_weight, lr, betas, eps, wd, clip, step; the paper's block:
     n_kv_heads, qk_norm, rope_tables=(cos, sin) f32 [seq, 64], embed_norm, window, full_every; other blocks: norm = "layer", recurrent = layers
-    with the gated linear recurrence, act8 = activations in 8 bits for the backward pass).
+    with the gated linear recurrence, act8 = activations in 8 bits for the backward pass, linear = "token" = linears with token and channel scales, state8 =
+    moments of the matrices in 8 bits).
     params: dict name -> numpy (uint16 bf16 bits / float32 steps).  tokens: [n_mb, micro_batch, seq+1]."""
     P = {k: np.array(v, copy=True) for k, v in params.items()}
     specs = _specs(cfg)
     accum, shard, rep = cfg["mesh"]
     assert tokens.shape[0] == accum * shard * rep
     sw = {}
-    for l in range(cfg["n_layers"]):
+    for l in range(cfg["n_layers"] if not _by_token(cfg) else 0):
         for w in LINEARS:
             sw["l%d.%s" % (l, w)] = O.lsq_weight_scale(P["l%d.%s" % (l, w)])
-    if calibrate:
+    if calibrate and not _by_token(cfg):
         forward(cfg, P, sw, tokens[0], calibrate=True)
     n = sum(int(np.prod(s)) for _, s in specs)
     acc = O.Accum(accum, shard, rep, n)
@@ -203,19 +226,32 @@ def run_step(cfg, params, tokens, opt=None, calibrate=True):
     views = [g[offs[i]:offs[i + 1]] for i in range(len(specs))]
     norm, coef = O.grad_norm(views, cfg.get("clip", 1.0))
     g = O.scale(g, coef)
+    # with state8 the moments of the matrices are codes and scales, one tensor's behind the other's; the others' are in 32 bits, likewise
+    eight = [bool(cfg.get("state8")) and len(shape) > 1 for _, shape in specs]
+    size = [int(np.prod(shape)) for _, shape in specs]
     if opt is None:
-        opt = {"m": np.zeros(n, np.float32), "v": np.zeros(n, np.float32)}
-    m, v = opt["m"].copy(), opt["v"].copy()
+        n32, n8 = sum(k for k, e in zip(size, eight) if not e), [k for k, e in zip(size, eight) if e]
+        opt = {"m": np.zeros(n32, np.float32), "v": np.zeros(n32, np.float32), "m8": np.zeros(sum(n8), np.int8), "v8": np.zeros(sum(n8), np.uint8),
+               "s": np.zeros((sum(-(-k // O.ADAMW8_BLOCK) for k in n8), 2), np.float32)}
+    st = {k: x.copy() for k, x in opt.items()}
     lr, (b1, b2), eps, wd, t = cfg.get("lr", 3e-4), cfg.get("betas", (0.9, 0.95)), cfg.get("eps", 1e-8), cfg.get("wd", 0.1), cfg.get("step", 1)
-    hashes = {}
+    hashes, at32, at8, ats = {}, 0, 0, 0
     for i, (name, shape) in enumerate(specs):
-        sl = slice(offs[i], offs[i + 1])
+        sl, k = slice(offs[i], offs[i + 1]), size[i]
         decay = wd if (name == "lm_head" or name.split(".")[-1] in LINEARS) else 0.0
-        p, m[sl], v[sl] = O.adamw(P[name].reshape(-1), g[sl], m[sl], v[sl], lr, b1, b2, eps, decay, t)
+        if eight[i]:
+            c, b = slice(at8, at8 + k), slice(ats, ats + -(-k // O.ADAMW8_BLOCK))
+            p, st["m8"][c], st["v8"][c], st["s"][b] = O.adamw8(P[name].reshape(-1), g[sl], st["m8"][c], st["v8"][c], st["s"][b], lr, b1, b2, eps, decay, t)
+            at8, ats = c.stop, b.stop
+        else:
+            c = slice(at32, at32 + k)
+            p, st["m"][c], st["v"][c] = O.adamw(P[name].reshape(-1), g[sl], st["m"][c], st["v"][c], lr, b1, b2, eps, decay, t)
+            at32 = c.stop
         P[name] = p.reshape(shape)
         hashes[name] = O.tensor_hash(P[name])
     hashes["grad"] = O.tensor_hash(g)
-    hashes["adam_m"] = O.tensor_hash(m)
-    hashes["adam_v"] = O.tensor_hash(v)
-    return {"params": P, "m": m, "v": v, "grad": g, "loss": float(np.mean(losses)), "losses": losses,
+    hashes["adam_m"], hashes["adam_v"] = O.tensor_hash(st["m"]), O.tensor_hash(st["v"])
+    if cfg.get("state8"):
+        hashes.update(adam_m8=O.tensor_hash(st["m8"]), adam_v8=O.tensor_hash(st["v8"]), adam_scales=O.tensor_hash(st["s"]))
+    return {"params": P, "m": st["m"], "v": st["v"], "opt": st, "grad": g, "loss": float(np.mean(losses)), "losses": losses,
             "grad_norm": float(norm), "coef": float(coef), "hashes": hashes}

@@ -49,6 +49,8 @@ class ModelConfig:
     norm: str = "rms"                # "layer": the norms subtract the mean and have a shift beside the gain
     recurrent: tuple = ()            # layers whose mixer is the gated linear recurrence (w_qkv: gate and value, 2 d_model rows) in place of attention; every sequence from zero, without cuts
     act8: bool = False               # inputs of the norms, of SwiGLU and of the recurrence are kept in 8 bits for the backward pass
+    linear: str = "lsq"              # "token": 8-bit linears whose scales follow the values, by token and output channel; no learned steps, no calibration, no rotation
+    state8: bool = False             # AdamW keeps the moments of the matrices in 8 bits (those of gains, shifts and steps in 32)
 
     def as_dict(self):
         return dict(self.__dict__)
@@ -89,8 +91,8 @@ def param_specs(cfg):
         s += norm("embed_norm")
     for l in range(L):
         s += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (cfg.mixer_width(l), D), "bf16"), ("l%d.w_o" % l, (D, D), "bf16")]
-        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "bf16"), ("l%d.w_down" % l, (D, Fh), "bf16"),
-                                         ("l%d.s_x" % l, (4,), "f32")]
+        s += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "bf16"), ("l%d.w_down" % l, (D, Fh), "bf16")]
+        s += [("l%d.s_x" % l, (4,), "f32")] if cfg.linear == "lsq" else []
     return s + norm("final_norm") + [("lm_head", (V, D), "bf16")]
 
 
@@ -125,8 +127,8 @@ class Replay:
         self.specs = param_specs(cfg)
         D, Fh, V, L, T = cfg.d_model, cfg.ffn, cfg.vocab, cfg.n_layers, cfg.tokens_per_microbatch
         assert D == cfg.n_heads * 128, "head_dim is 128"
-        assert cfg.norm in ("rms", "layer") and all(0 <= l < L for l in cfg.recurrent)
-        self.layer_norm = cfg.norm == "layer"
+        assert cfg.norm in ("rms", "layer") and cfg.linear in ("lsq", "token") and all(0 <= l < L for l in cfg.recurrent)
+        self.layer_norm, self.by_token = cfg.norm == "layer", cfg.linear == "token"
         self.goff, self.poff = {}, {}
         self.shape = dict((n, sh) for n, sh, _ in self.specs)
         g = p = 0
@@ -139,17 +141,29 @@ class Replay:
         self.n_grad = g
         # where a parameter lies in the flat buffers, and by (layer, linear) a single activation step and its gradient
         grads = {n: (lo, _numel(self.shape[n])) for n, lo in self.goff.items()}
-        steps = {"l%d.s_x" % l: (4 * l, 4) for l in range(L)}
-        for l in range(L):
+        steps = {"l%d.s_x" % l: (4 * l, 4) for l in range(L)} if not self.by_token else {}
+        for l in range(L if not self.by_token else 0):
             steps.update({(l, i): (4 * l + i, 1) for i in range(4)})
             grads.update({(l, i): (self.goff["l%d.s_x" % l] + i, 1) for i in range(4)})
+        # moments: in the gradient's layout, or those of the matrices in 8 bits with their scales, one behind the other, and the others' in 32 behind one another
+        codes, scales, moments, n8, ns, n32 = {}, {}, {}, 0, 0, 0
+        for name, shape, _ in self.specs:
+            n = _numel(shape)
+            if cfg.state8 and len(shape) > 1:
+                codes[name], scales[name] = (n8, n), (ns, det.det_adamw8_scale_floats(n))
+                n8, ns = n8 + n, ns + scales[name][1]
+            else:
+                moments[name] = (n32, n)
+                n32 += n
+        moments = moments if cfg.state8 else grads
         self._views = {}
-        self._parts = dict(pbf={n: (lo, _numel(self.shape[n])) for n, lo in self.poff.items()}, sx=steps, gmb=grads, gout=grads, m=grads,
-                           v=grads)
+        self._parts = dict(pbf={n: (lo, _numel(self.shape[n])) for n, lo in self.poff.items()}, sx=steps, gmb=grads, gout=grads, m=moments,
+                           v=moments, m8=codes, v8=codes, ms=scales)
         z = lambda n, dt: torch.zeros(n, dtype=dt, device=device)
         self.pbf = z(p, I16)                       # bf16 parameters (bit patterns), canonical order
         self.sx = z(L * 4, F32)                    # LSQ activation steps, [layer, (qkv, o, gu, down)]
-        self.m, self.v = z(g, F32), z(g, F32)      # Adam moments, gradient layout
+        self.m, self.v = z(n32, F32), z(n32, F32)  # Adam moments, gradient layout, or those that stay in 32 bits
+        self.m8, self.v8, self.ms = z(n8, I8), z(n8, torch.uint8), z(ns, F32)
         self.gmb = z(g, F32)                       # gradient of the current micro-batch
         self.gout_padded = z(max(g, gout_len or 0), F32)
         self.gout = self.gout_padded[:g]           # reduced gradient
@@ -158,7 +172,8 @@ class Replay:
         self.lin = {}
         for l in range(L):
             for w, (N, K) in zip(LINEARS, ((cfg.mixer_width(l), D), (D, D), (2 * Fh, D), (D, Fh))):
-                self.lin[(l, w)] = dict(name="l%d.%s" % (l, w), N=N, K=K, s_w=z(N, F32), qW=z(N * K, I8), qWt=z(N * K, I8), s_u=z(1, F32))
+                ld, ld_t = (det.det_tok8_ld(K), det.det_tok8_ld(N)) if self.by_token else (K, N)
+                self.lin[(l, w)] = dict(name="l%d.%s" % (l, w), N=N, K=K, s_w=z(N, F32), qW=z(N * ld, I8), qWt=z(K * ld_t, I8), s_u=z(1, F32))
         e = lambda n, dt: torch.empty(n, dtype=dt, device=device)
         QW, Hkv = cfg.qkv_width, cfg.kv_heads
         self.head_ops = cfg.qk_norm or cfg.rope_tables is not None
@@ -180,7 +195,7 @@ class Replay:
         self.tok = e(T, I32)
         self.lab = e(T, I32)
         # what a step reports lies in one buffer and comes back in one copy: status, norm and clip coefficient, hash roots, losses
-        nr, n_mb = 32 * (max(len(self.specs), 2) + 3), cfg.mesh[0] * cfg.mesh[1] * cfg.mesh[2]
+        nr, n_mb = 32 * (max(len(self.specs), 2) + 6), cfg.mesh[0] * cfg.mesh[1] * cfg.mesh[2]
         self._out = z(16 + nr + 4 * n_mb, torch.uint8)
         self.status = self._out[0:4].view(I32)
         self.norm, self.coef = self._out[4:8].view(F32), self._out[8:12].view(F32)
@@ -195,7 +210,9 @@ class Replay:
                   det.det_sum_ws_bytes(g), 1 << 20,
                   (max(det.det_lmhead_fwd_v2_ws_bytes(T, V, D), det.det_lmhead_bwd_v2_ws_bytes(T, V, D)) if cfg.arith == 2 else 0),
                   det.det_layernorm_bwd_ws_bytes(T, D) if self.layer_norm else 0,
-                  *[det.det_linear_bwd_ws_bytes(T, N, K) for (N, K) in ((QW, D), (D, D), (2 * Fh, D), (D, Fh), (2 * D, D))])
+                  *([det.det_tok8_linear_bwd_ws_bytes(T, N, K) for (N, K) in ((QW, D), (D, D), (D, Fh), (2 * D, D))] +
+                    [det.det_tok8_glu_bwd_ws_bytes(T, Fh, D)] if self.by_token else
+                    [det.det_linear_bwd_ws_bytes(T, N, K) for (N, K) in ((QW, D), (D, D), (2 * Fh, D), (D, Fh), (2 * D, D))]))
         self.ws = e(wsb + 4096, torch.uint8)
         self.losses = []
         self.prof = None
@@ -205,8 +222,8 @@ class Replay:
         """What layer l keeps from its forward pass for its backward pass."""
         cfg = self.cfg
         D, Fh, T, QW, Hkv = cfg.d_model, cfg.ffn, cfg.tokens_per_microbatch, cfg.mixer_width(l), cfg.kv_heads
-        rec, stat = l in cfg.recurrent, T if self.layer_norm else 0
-        a = dict(rstd1=e(T, F32), mean1=e(stat, F32), n1=e(T * D, I16), qx_qkv=e(T * D, I8), att=e(T * D, I16), qx_o=e(T * D, I8), rstd2=e(T, F32),
+        rec, stat, tok = l in cfg.recurrent, T if self.layer_norm else 0, T if self.by_token else 0
+        a = dict(sx_qkv=e(tok, F32), sx_o=e(tok, F32), sx_gu=e(tok, F32), sx_down=e(tok, F32), rstd1=e(T, F32), mean1=e(stat, F32), n1=e(T * D, I16), qx_qkv=e(T * D, I8), att=e(T * D, I16), qx_o=e(T * D, I8), rstd2=e(T, F32),
                  mean2=e(stat, F32), n2=e(T * D, I16), qx_gu=e(T * D, I8))
         if rec:
             a.update(states=e(det.det_linrec_state_floats(cfg.micro_batch, cfg.seq, D), F32))
@@ -293,11 +310,14 @@ class Replay:
         have the shape of an attention layer's).  How activations are kept between the passes is no part of it."""
         cfg = self.cfg
         return json.dumps(dict(params=[(name, [int(n) for n in shape], kind) for name, shape, kind in self.specs], norm=cfg.norm,
-                               recurrent=sorted({int(l) for l in cfg.recurrent})))
+                               recurrent=sorted({int(l) for l in cfg.recurrent}), **(dict(state8=True) if cfg.state8 else {})))
+
+    def _state(self):
+        return ("pbf", "sx", "m", "v") + (("m8", "v8", "ms") if self.cfg.state8 else ())
 
     def save_state(self, path):
-        """Parameters (bf16 bits), activation steps, both Adam moments and the step counter, as one .npz file, with what lies where."""
-        np.savez(path, pbf=self.pbf.cpu().numpy(), sx=self.sx.cpu().numpy(), m=self.m.cpu().numpy(), v=self.v.cpu().numpy(),
+        """Parameters (bf16 bits), activation steps, both Adam moments (with state8 codes and scales too) and the step counter, as one .npz file, with what lies where."""
+        np.savez(path, **{name: getattr(self, name).cpu().numpy() for name in self._state()},
                  step=np.array([self.cfg.step], np.int64), layout=np.array(self._layout()))
 
     def load_state(self, path):
@@ -307,10 +327,10 @@ class Replay:
         if "layout" in z.files:
             if str(z["layout"]) != self._layout():
                 raise ValueError("state file does not match this configuration: other parameters, norm or recurrent layers")
-        elif self.cfg.recurrent:
-            raise ValueError("state file does not say which layers are recurrent")
-        for name, dst in (("pbf", self.pbf), ("sx", self.sx), ("m", self.m), ("v", self.v)):
-            a = z[name]
+        elif self.cfg.recurrent or self.cfg.state8:
+            raise ValueError("state file does not say which layers are recurrent, or what it keeps in 8 bits")
+        for name in self._state():
+            a, dst = z[name], getattr(self, name)
             if a.shape != tuple(dst.shape):
                 raise ValueError("state file does not match this configuration: %s %s vs %s" % (name, a.shape, tuple(dst.shape)))
             dst.copy_(torch.from_numpy(a).to(self.dev))
@@ -329,12 +349,20 @@ class Replay:
         hb, P = self.cfg.hadamard_block, self._fresh()["pbf"]
         for d in self.lin.values():
             W = P[d["name"]]
+            if self.by_token:
+                det.det_tok8_quant(W, d["K"], d["N"], d["K"], d["qW"], d["s_w"])
+                det.det_tok8_transpose(d["qW"], d["N"], d["K"], d["qWt"])
+                continue
             det.det_lsq_weight_scale(W, d["N"], d["K"], 0, d["s_w"], self.ws)
             det.det_lsq_quantize_weight(W, d["s_w"], d["N"], d["K"], hb, d["qW"], d["qWt"], d["s_u"], self.ws)
 
     def _linear(self, l, w, idx, X, M, Y, qx, calibrate, prequantised=False):
         """prequantised: the kernel that produced X already wrote its int8 codes into qx."""
         d = self.lin[(l, w)]
+        if self.by_token:
+            with self.span("linear_fwd"):
+                det.det_tok8_linear_fwd(X, d["K"], d["qW"], d["s_w"], M, d["N"], d["K"], Y, d["N"], qx, self.act[l]["sx" + w[1:]], self.status)
+            return
         sx = self._views["sx"][l, idx]
         if calibrate:
             det.det_lsq_act_scale_init(X, M * d["K"], sx, self.ws)
@@ -456,7 +484,7 @@ class Replay:
             det.det_embed_fwd(self.tok, T, P["embed"], V, D, x)
         # outside the calibration pass every activation step is known before its activation is produced, so the
         # producers write the next linear's int8 input themselves (same bits as the separate quantiser pass)
-        fuse = self.fuse_quant and not calibrate and D <= 2048
+        fuse = self.fuse_quant and not calibrate and D <= 2048 and not self.by_token
         dn, res = self.tmp[1][:T * D], None           # the residual sum that ends a layer runs with the norm that starts the next
         for l in range(L):
             a = self.act[l]
@@ -474,13 +502,20 @@ class Replay:
             self._linear(l, "w_o", 1, a["att"], T, o, a["qx_o"], calibrate, fuse and not cfg.pv_int8 and not rec)
             self._norm(ax, o, ah, "l%d.ffn_norm" % l, a["n2"], a["rstd2"], a["mean2"], sxl[2] if fuse else None, a["qx_gu"], kept(a, "h"))
             gu, act, qx_down = own(a, "gu"), own(a, "a"), own(a, "qx_down")
-            self._linear(l, "w_gu", 2, a["n2"], T, gu, a["qx_gu"], calibrate, fuse)
-            if cfg.act8:
-                det.det_swiglu_fwd_act8(gu, T, Fh, act, *kept(a, "gu"), *((sxl[3], qx_down) if fuse else ()))
-            elif fuse:
-                det.det_swiglu_fwd_q(gu, T, Fh, act, sxl[3], qx_down)
+            if self.by_token:
+                d = self.lin[(l, "w_gu")]
+                with self.span("linear_fwd"):
+                    det.det_tok8_glu_fwd(a["n2"], D, d["qW"], d["s_w"], T, Fh, D, act, Fh, gu, 2 * Fh, a["qx_gu"], a["sx_gu"], self.status)
+                if cfg.act8:
+                    det.det_act8_pack(det.DET_BF16, gu, 2 * Fh, T, 2 * Fh, *kept(a, "gu"))
             else:
-                det.det_swiglu_fwd(gu, T, Fh, act)
+                self._linear(l, "w_gu", 2, a["n2"], T, gu, a["qx_gu"], calibrate, fuse)
+                if cfg.act8:
+                    det.det_swiglu_fwd_act8(gu, T, Fh, act, *kept(a, "gu"), *((sxl[3], qx_down) if fuse else ()))
+                elif fuse:
+                    det.det_swiglu_fwd_q(gu, T, Fh, act, sxl[3], qx_down)
+                else:
+                    det.det_swiglu_fwd(gu, T, Fh, act)
             self._linear(l, "w_down", 3, act, T, dn, qx_down, calibrate, fuse)
             res = ah
         self._norm(res, dn, self.xf, "final_norm", self.nf, self.rstdf, self.meanf)
@@ -496,6 +531,11 @@ class Replay:
     def _linear_bwd(self, l, w, idx, dY, X, qx, M, dX):
         d = self.lin[(l, w)]
         P, G, name = self._views["pbf"], self._views["gmb"], d["name"]
+        if self.by_token:
+            with self.span("linear_bwd"):
+                det.det_tok8_linear_bwd(dY, d["N"], qx, self.act[l]["sx" + w[1:]], d["qWt"], d["s_w"], M, d["N"], d["K"], dX, d["K"], G[name], self.ws,
+                                        self.status)
+            return
         with self.span("linear_bwd"):
             det.det_linear_bwd(dY, X, qx, P[name], d["qWt"], self._views["sx"][l, idx], d["s_w"], d["s_u"], M, d["N"], d["K"],
                                self.cfg.hadamard_block, dX, G[name], G[l, idx], self.ws, self.status)
@@ -547,16 +587,27 @@ class Replay:
             a = self.act[l]
             d_a = t0[:T * Fh]
             act, qx_down = own(a, "a"), own(a, "qx_down")
-            if cfg.act8:
+            if cfg.act8 and self.by_token:
+                det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act)
+                det.det_tok8_quant(act, Fh, T, Fh, qx_down, a["sx_down"])
+            elif cfg.act8:
                 det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act, views["sx"][l, 3], qx_down)
             self._linear_bwd(l, "w_down", 3, dx, act, qx_down, T, d_a)
-            d_gu = t2[:T * 2 * Fh]
-            if cfg.act8:
-                det.det_swiglu_bwd_act8(d_a, *kept(a, "gu"), T, Fh, d_gu)
+            if self.by_token:
+                d, gu, d_n2 = self.lin[(l, "w_gu")], own(a, "gu"), t2[:T * D]
+                if cfg.act8:
+                    det.det_act8_unpack(det.DET_BF16, *kept(a, "gu"), T, 2 * Fh, gu, 2 * Fh)
+                with self.span("linear_bwd"):
+                    det.det_tok8_glu_bwd(d_a, Fh, gu, 2 * Fh, a["qx_gu"], a["sx_gu"], d["qWt"], d["s_w"], T, Fh, D, d_n2, D, G[d["name"]], self.ws, self.status)
+                t0, t2 = t2, t0                                            # the input's gradient lies in the other buffer
             else:
-                det.det_swiglu_bwd(d_a, a["gu"], T, Fh, d_gu)
-            d_n2 = t0[:T * D]
-            self._linear_bwd(l, "w_gu", 2, d_gu, a["n2"], a["qx_gu"], T, d_n2)
+                d_gu = t2[:T * 2 * Fh]
+                if cfg.act8:
+                    det.det_swiglu_bwd_act8(d_a, *kept(a, "gu"), T, Fh, d_gu)
+                else:
+                    det.det_swiglu_bwd(d_a, a["gu"], T, Fh, d_gu)
+                d_n2 = t0[:T * D]
+                self._linear_bwd(l, "w_gu", 2, d_gu, a["n2"], a["qx_gu"], T, d_n2)
             self._norm_bwd(d_n2, own(a, "h"), "l%d.ffn_norm" % l, a["rstd2"], a["mean2"], dx, t2[:T * D], kept(a, "h"))    # dx: gradient of h from here on
             d_att = t0[:T * D]
             self._linear_bwd(l, "w_o", 1, dx, a["att"], a["qx_o"], T, d_att)
@@ -587,15 +638,22 @@ class Replay:
             kinds.append(det.DET_BF16 if kind == "bf16" else det.DET_F32)
         # the clip coefficient is applied to the gradient in the same pass (every element of gout belongs to one tensor)
         params = [views["sx" if kind == "f32" else "pbf"][name] for name, _, kind in self.specs]
-        det.det_adamw_batch(descs, kinds, params, grads, part("m"), part("v"), self.coef)
+        if cfg.state8:
+            eight = [name in self._parts["m8"] for name in names]
+            of = lambda a, b: [views[a if e else b][name] for e, name in zip(eight, names)]
+            det.det_adamw8_batch(descs, kinds, params, grads, of("m8", "m"), of("v8", "v"), [views["ms"][name] if e else None for e, name in zip(eight, names)],
+                                 self.coef)
+        else:
+            det.det_adamw_batch(descs, kinds, params, grads, part("m"), part("v"), self.coef)
 
     def _hash_jobs(self, per_tensor):
         if per_tensor:
             views = self._fresh()
             jobs = [(name, views["sx" if kind == "f32" else "pbf"][name]) for name, _, kind in self.specs]
         else:
-            jobs = [("params_bf16", self.pbf), ("steps_f32", self.sx)]
-        return jobs + [("grad", self.gout), ("adam_m", self.m), ("adam_v", self.v)]
+            jobs = [("params_bf16", self.pbf)] + ([("steps_f32", self.sx)] if not self.by_token else [])
+        jobs += [("grad", self.gout), ("adam_m", self.m), ("adam_v", self.v)]
+        return jobs + ([("adam_m8", self.m8), ("adam_v8", self.v8), ("adam_scales", self.ms)] if self.cfg.state8 else [])
 
     def _queue_hashes(self, per_tensor):
         jobs = self._hash_jobs(per_tensor)
@@ -613,7 +671,9 @@ class Replay:
         return self._hex(names, self.roots.cpu().numpy().tobytes())
 
     def calibrate(self, tokens_mb):
-        """Untimed: set every activation step from the first micro-batch (LSQ initialisation rule)."""
+        """Untimed: set every activation step from the first micro-batch (LSQ initialisation rule); without steps there is nothing to set."""
+        if self.by_token:
+            return
         self.prepare_weights()
         self.forward(tokens_mb, calibrate=True)
 

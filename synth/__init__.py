@@ -80,8 +80,8 @@ def model_param_specs(cfg):
     """Canonical parameter order: embedding; per layer attn-norm gain, W_qkv, W_o, ffn-norm gain, W_gate/up,
     W_down, the four activation steps; final-norm gain; LM head.  cfg: dict with n_layers, d_model, ffn, vocab and
     optionally n_kv_heads (grouped queries: W_qkv has (n_heads + 2 n_kv_heads) * 128 rows), embed_norm (a gain
-    after the embedding), norm = "layer" (a shift behind every gain) and recurrent (layers whose W_qkv has 2 d_model rows, gate and
-    value).  Returns a list of (name, shape, kind), kind in {"embed", "gain", "shift", "linear", "step", "head"}."""
+    after the embedding), norm = "layer" (a shift behind every gain) recurrent (layers whose W_qkv has 2 d_model rows, gate and
+    value) and linear = "token" (no activation steps).  Returns a list of (name, shape, kind), kind in {"embed", "gain", "shift", "linear", "step", "head"}."""
     D, Fh, V, L = cfg["d_model"], cfg["ffn"], cfg["vocab"], cfg["n_layers"]
     nq = D + 2 * 128 * (cfg.get("n_kv_heads") or cfg["n_heads"]) if "n_heads" in cfg else 3 * D
     layer, rec = cfg.get("norm", "rms") == "layer", cfg.get("recurrent", ())
@@ -91,8 +91,8 @@ def model_param_specs(cfg):
         specs += norm("embed_norm")
     for l in range(L):
         specs += norm("l%d.attn_norm" % l) + [("l%d.w_qkv" % l, (2 * D if l in rec else nq, D), "linear"), ("l%d.w_o" % l, (D, D), "linear")]
-        specs += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "linear"), ("l%d.w_down" % l, (D, Fh), "linear"),
-                                             ("l%d.s_x" % l, (4,), "step")]
+        specs += norm("l%d.ffn_norm" % l) + [("l%d.w_gu" % l, (2 * Fh, D), "linear"), ("l%d.w_down" % l, (D, Fh), "linear")]
+        specs += [("l%d.s_x" % l, (4,), "step")] if cfg.get("linear", "lsq") == "lsq" else []
     return specs + norm("final_norm") + [("lm_head", (V, D), "head")]
 
 
