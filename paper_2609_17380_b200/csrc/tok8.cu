@@ -79,30 +79,45 @@ __global__ void __launch_bounds__(256) k_t8_rows(const uint16_t* __restrict__ x,
     *reinterpret_cast<uint2*>(q + (size_t)row * ldq + c) = t8_codes8(f, inv, dead);
   }
 }
-// Any width, stride and address: a warp a row (WIDE: a CTA), which is read twice, an element a lane.
-template <bool WIDE>
-__global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict__ x, size_t ld, int M, int K, int8_t* __restrict__ q, float* __restrict__ s) {
+// Any width, stride and address: a CTA a row, an element a thread at a time, up to 2048 of them kept in registers (LONG: read twice).
+template <bool LONG>
+__global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict__ x, size_t ld, int K, int8_t* __restrict__ q, float* __restrict__ s) {
   grid_dep();
   __shared__ uint32_t part[8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = WIDE ? blockIdx.x : blockIdx.x * 8 + warp, ldq = t8_ld(K);
-  const int at = WIDE ? threadIdx.x : lane, step = WIDE ? 256 : 32;
-  if (row >= M) return;
+  const int row = blockIdx.x, ldq = t8_ld(K);
   const uint16_t* p = x + (size_t)row * ld;
-  uint32_t m = 0;
+  uint32_t v[8], m = 0;
+  if (LONG) {
 #pragma unroll 8
-  for (int c = at; c < K; c += step) m = max(m, (uint32_t)__ldg(p + c) & 0x7fffu);
-  m = __reduce_max_sync(0xffffffffu, m) << 16;
-  if (WIDE) {
-    if (lane == 0) part[warp] = m;
-    __syncthreads();
+    for (int c = threadIdx.x; c < K; c += 256) m = max(m, (uint32_t)__ldg(p + c) & 0x7fffu);
+  } else {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, part[w]);
+    for (int k = 0; k < 8; ++k) {
+      const int c = threadIdx.x + k * 256;
+      v[k] = c < K ? __ldg(p + c) : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = max(m, v[k] & 0x7fffu);
   }
-  const float sc = t8_scale(m), inv = t8_inverse(sc);
-  if (at == 0) s[row] = sc;
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = max(m, part[w]);
+  const float sc = t8_scale(m << 16), inv = t8_inverse(sc);
+  const bool dead = m >= 0x7f80u;
+  if (threadIdx.x == 0) s[row] = sc;
+  int8_t* to = q + (size_t)row * ldq;
+  if (LONG) {
 #pragma unroll 8
-  for (int c = at; c < ldq; c += step)
-    q[(size_t)row * ldq + c] = c < K && m < 0x7f800000u ? (int8_t)t8_code(bf2f(__ldg(p + c)), inv) : (int8_t)0;
+    for (int c = threadIdx.x; c < ldq; c += 256) to[c] = c < K && !dead ? (int8_t)t8_code(bf2f(__ldg(p + c)), inv) : (int8_t)0;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int c = threadIdx.x + k * 256;
+      if (c < ldq) to[c] = dead ? (int8_t)0 : (int8_t)t8_code(__uint_as_float(v[k] << 16), inv);
+    }
+  }
 }
 
 // Codes [R, ld(C)] -> [C, ld(R)], through shared memory, whole 128-byte lines on both sides but at the edges.  What lies behind column C of the
@@ -478,10 +493,19 @@ __device__ __forceinline__ void t8_store(uint8_t* stage, uint8_t* base, size_t p
     }
   } else if (lane < cols) {
     const int piece = lane * ES / 16, at = lane * ES % 16;
-    for (int r = 0; r < 32 && r < rows; ++r) {
-      const uint8_t* p = stage + r * (NW * 16) + ((piece ^ ((r >> SH) & (NW - 1))) << 4) + at;
-      if (ES == 2) *reinterpret_cast<uint16_t*>(base + r * pitch + lane * 2) = *reinterpret_cast<const uint16_t*>(p);
-      else *reinterpret_cast<uint32_t*>(base + r * pitch + lane * 4) = *reinterpret_cast<const uint32_t*>(p);
+    uint8_t* to = base + lane * ES;
+#pragma unroll 2
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = r0 + k;
+        const uint8_t* p = stage + r * (NW * 16) + ((piece ^ ((r >> SH) & (NW - 1))) << 4) + at;
+        if (r < rows) {
+          if (ES == 2) *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(p);
+          else *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(p);
+        }
+        to += pitch;
+      }
     }
   }
 }
@@ -761,12 +785,33 @@ struct T8Few {
   T8Out o;
 };
 template <int MT, int R, bool GLU, bool QUANT>
-__global__ void __launch_bounds__(256) k_t8_few(const __grid_constant__ T8Few f) {
+__global__ void __launch_bounds__(256, MT <= 2 ? 4 : 2) k_t8_few(const __grid_constant__ T8Few f) {
   extern __shared__ __align__(16) uint8_t smem_raw[];                     // the tokens' codes
   __shared__ float s_x[MT];
   __shared__ uint32_t part[MT][8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, K = f.o.K, M = f.o.I, ldk = t8_ld(K), pieces = ldk / 16;
+  constexpr int PITCH = QUANT ? 2 : 1;                                    // of a token's codes, in rows of codes
+  constexpr int OUT = GLU ? R / 2 : R;                                    // channels of the output a warp has at a time
+  constexpr int U = R >= 4 ? 2 : 4;                                       // pieces of a row on their way together
+  const int J = f.o.J, tasks = (J + OUT - 1) / OUT;
+  auto row = [&](int task, int r) {                                       // r-th of a task's rows of the weights
+    const int j = min(task * OUT + (GLU ? r >> 1 : r), J - 1) + (GLU && (r & 1) ? J : 0);
+    return reinterpret_cast<const uint4*>(f.w + (size_t)j * ldk);
+  };
+  auto fetch = [&](uint4 (&w)[U][R], const uint4* const (&rows)[R], int p0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < R; ++r) w[u][r] = p0 + 32 * u < pieces ? __ldg(rows[r] + p0 + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+  };
   grid_dep();
+  // the first weights are on their way while the codes are made
+  int task = blockIdx.x * 8 + warp;
+  const uint4* rows[R];
+  uint4 w[U][R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) rows[r] = row(min(task, tasks - 1), r);
+  fetch(w, rows, lane);
   if (QUANT) {
     uint32_t m[MT];
 #pragma unroll
@@ -786,7 +831,7 @@ __global__ void __launch_bounds__(256) k_t8_few(const __grid_constant__ T8Few f)
     for (int t = 0; t < MT; ++t) {
       m[t] = 0;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) m[t] = max(m[t], part[t][w]);
+      for (int i = 0; i < 8; ++i) m[t] = max(m[t], part[t][i]);
       const float sc = t8_scale(m[t]), inv = t8_inverse(sc);
       if (threadIdx.x == 0) {
         s_x[t] = sc;
@@ -796,15 +841,15 @@ __global__ void __launch_bounds__(256) k_t8_few(const __grid_constant__ T8Few f)
       const uint16_t* v = reinterpret_cast<const uint16_t*>(smem_raw) + t * ldk;
       for (int p0 = 0; p0 < pieces; p0 += 256) {
         const int p = p0 + threadIdx.x;
-        uint32_t w[4] = {0, 0, 0, 0};
+        uint32_t b[4] = {0, 0, 0, 0};
         if (p < pieces && m[t] < 0x7f800000u) {
 #pragma unroll
           for (int k = 0; k < 16; ++k)
-            if (p * 16 + k < K) w[k >> 2] |= (t8_code(bf2f(v[p * 16 + k]), inv) & 255u) << (8 * (k & 3));
+            if (p * 16 + k < K) b[k >> 2] |= (t8_code(bf2f(v[p * 16 + k]), inv) & 255u) << (8 * (k & 3));
         }
         __syncthreads();
         if (p < pieces) {
-          const uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
+          const uint4 c = make_uint4(b[0], b[1], b[2], b[3]);
           *reinterpret_cast<uint4*>(smem_raw + (size_t)t * ldk * 2 + p * 16) = c;
           if (blockIdx.x == 0 && t < M) *reinterpret_cast<uint4*>(f.q + (size_t)t * ldk + p * 16) = c;
         }
@@ -818,31 +863,20 @@ __global__ void __launch_bounds__(256) k_t8_few(const __grid_constant__ T8Few f)
     if (threadIdx.x < MT) s_x[threadIdx.x] = threadIdx.x < M ? f.s[threadIdx.x] : 0.0f;
   }
   __syncthreads();
-  constexpr int PITCH = QUANT ? 2 : 1;                                    // of a token's codes, in rows of codes
-  constexpr int OUT = GLU ? R / 2 : R;                                    // channels of the output a warp has at a time
-  const int J = f.o.J, tasks = (J + OUT - 1) / OUT;
 #pragma unroll 1
-  for (int task = blockIdx.x * 8 + warp; task < tasks; task += gridDim.x * 8) {
+  for (bool first = true; task < tasks; task += gridDim.x * 8, first = false) {
     const int j0 = task * OUT;
-    const int8_t* row[R];
+    if (!first) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int j = min(j0 + (GLU ? r >> 1 : r), J - 1) + (GLU && (r & 1) ? J : 0);
-      row[r] = f.w + (size_t)j * ldk;
+      for (int r = 0; r < R; ++r) rows[r] = row(task, r);
     }
     int acc[R][MT];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int t = 0; t < MT; ++t) acc[r][t] = 0;
-    constexpr int U = R >= 4 ? 2 : 4;                                     // pieces of a row on their way together
     for (int p0 = lane; p0 < pieces; p0 += 32 * U) {
-      uint4 w[U][R];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-          w[u][r] = p0 + 32 * u < pieces ? __ldg(reinterpret_cast<const uint4*>(row[r]) + p0 + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+      if (!first || p0 >= 32) fetch(w, rows, p0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (p0 + 32 * u >= pieces) break;
@@ -896,7 +930,8 @@ static int t8_few_launch(const T8Few& f, int sms, cudaStream_t st) {
   static DevOnce once = {};
   if (smem > 40 * 1024 && dev_ensure_smem(once, (const void*)k_t8_few<MT, R, GLU, QUANT>, T8_FEW_SMEM) != DET_OK) return DET_ERR_CUDA;
   const long long ctas = ((long long)(f.o.J + (GLU ? R / 2 : R) - 1) / (GLU ? R / 2 : R) + 7) / 8;
-  launch_after(k_t8_few<MT, R, GLU, QUANT>, (unsigned)(ctas < 2 * sms ? ctas : 2 * sms), 256, smem, st, f);
+  const int most = (MT <= 2 ? 4 : 2) * sms;
+  launch_after(k_t8_few<MT, R, GLU, QUANT>, (unsigned)(ctas < most ? ctas : most), 256, smem, st, f);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -1187,8 +1222,7 @@ static int t8_quant(const uint16_t* X, int ld, int M, int K, int8_t* q, float* s
     else if (K <= 8192) launch_after(k_t8_rows<4>, (unsigned)((M + 1) / 2), 256, 0, st, X, (size_t)ld, M, K, q, s);
     else launch_after(k_t8_rows<8>, (unsigned)M, 256, 0, st, X, (size_t)ld, M, K, q, s);
   } else {
-    if (K <= 2048) launch_after(k_t8_rows_any<false>, (unsigned)((M + 7) / 8), 256, 0, st, X, (size_t)ld, M, K, q, s);
-    else launch_after(k_t8_rows_any<true>, (unsigned)M, 256, 0, st, X, (size_t)ld, M, K, q, s);
+    launch_after(K <= 2048 ? k_t8_rows_any<false> : k_t8_rows_any<true>, (unsigned)M, 256, 0, st, X, (size_t)ld, K, q, s);
   }
   DET_CHECK_LAUNCH();
   return DET_OK;
