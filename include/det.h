@@ -175,7 +175,8 @@ int det_rmsnorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf
  *   det_tok8_transpose: codes [M, K] -> [K, M] (the backward pass wants the weight's, qWt [K, det_tok8_ld(N)]).
  * Any M >= 0 (up to 2^28), any N, K >= 1; bf16 matrices have rows ld elements apart (ld >= the width), any alignment to the element; scales f32.  Whole
  * rows in 16-byte pieces are faster.  K < 2^17 (DET_ERR_RANGE), in the backward pass M and N too.  M = 0: no rows, and a dW of zeros.
- * Outputs overlap no input.  Two tokens' results never depend on each other; nor does a token's on how many there are. */
+ * Outputs overlap no input.  Two tokens' results never depend on each other; nor does a token's on how many there are.  status_dev (may be NULL) receives
+ * DET_DEV_TIMEOUT if a bounded wait of the tensor-core kernels expires; the outputs of that call are undefined then. */
 int det_tok8_ld(int K);
 int det_tok8_quant(const det_bf16* X, int ld, int M, int K, int8_t* qX, float* s_x, void* stream);
 int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, void* stream);

@@ -6,6 +6,7 @@
 #include <Python.h>
 #include <dlfcn.h>
 
+#include <cstring>
 #include <memory>
 #include <string>
 #include <type_traits>
@@ -37,6 +38,15 @@ static bool address_of(PyObject* t, unsigned long long& out) {
   }
   PyErr_Format(PyExc_TypeError, "expected a CUDA tensor, an address or None, got %s", Py_TYPE(t)->tp_name);
   return false;
+}
+// the same for calls that refuse a tensor on another device than the current one, where the kernels run: 8-bit linears, AdamW with moments in 8 bits
+static bool address_here(PyObject* t, unsigned long long& out) {
+  if (!address_of(t, out)) return false;
+  if (THPVariable_Check(t) && THPVariable_Unpack(t).get_device() != c10::cuda::current_device()) {
+    PyErr_SetString(PyExc_AssertionError, "tensors must be on the current CUDA device");
+    return false;
+  }
+  return true;
 }
 static unsigned long long current_stream() {
   at::globalContext().lazyInitDevice(c10::DeviceType::CUDA);
@@ -123,6 +133,7 @@ struct Callable {
   const Entry* entry;
   void* fn;
   std::string pattern;                         // per Python argument: p i z f, or w a workspace (its address and size); s the current stream
+  bool here = false;                           // tensors have to be on the current device
   PyObject* general = nullptr;                 // the entry point with its C types declared (ctypes)
   PyObject* raise_status = nullptr;            // raise_status(name, status)
   ~Callable() { Py_XDECREF(general); Py_XDECREF(raise_status); }
@@ -155,6 +166,7 @@ static PyObject* entry_call(PyObject* self, PyObject* const* args, Py_ssize_t na
   const Callable* e = static_cast<const Callable*>(PyCapsule_GetPointer(self, nullptr));
   if (!e) return nullptr;
   const char* name = e->entry->name;
+  const auto address = e->here ? address_here : address_of;
   Slot s[MAX_ARGS];
   int n = 0, rc;
   Py_ssize_t a = 0;
@@ -165,10 +177,10 @@ static PyObject* entry_call(PyObject* self, PyObject* const* args, Py_ssize_t na
     PyObject* x = args[a++];
     switch (c) {
       case 'p':
-        if (!address_of(x, s[n++].u)) return nullptr;
+        if (!address(x, s[n++].u)) return nullptr;
         break;
       case 'w':                                // the size comes from the tensor, so an address alone is no workspace
-        if (!address_of(x, s[n].u)) return nullptr;
+        if (!address(x, s[n].u)) return nullptr;
         if (x == Py_None) s[n + 1].u = 0;
         else if (THPVariable_Check(x)) s[n + 1].u = THPVariable_Unpack(x).nbytes();
         else { PyErr_Format(PyExc_AttributeError, "%s: a workspace is a tensor or None", name); return nullptr; }
@@ -225,7 +237,7 @@ struct Table {                                 // a list or tuple of tensors
       unsigned long long a = 0;
       if (t == Py_None && may_be_none) { p[i] = nullptr; n[i] = 0; width[i] = 0; continue; }
       if (!THPVariable_Check(t)) { PyErr_SetString(PyExc_AssertionError, "a table holds tensors"); return false; }
-      if (!address_of(t, a)) return false;
+      if (!address_here(t, a)) return false;
       const at::Tensor& x = THPVariable_Unpack(t);
       p[i] = reinterpret_cast<void*>(a);
       n[i] = (size_t)x.numel();
@@ -289,7 +301,7 @@ static PyObject* adamw8_batch(PyObject*, PyObject* args) {
     return nullptr;
   }
   unsigned long long c = 0;
-  if (!address_of(coef, c)) return nullptr;
+  if (!address_here(coef, c)) return nullptr;
   void* st = reinterpret_cast<void*>(current_stream());
   int rc;
   Py_BEGIN_ALLOW_THREADS
@@ -360,6 +372,7 @@ static PyObject* bind(PyObject*, PyObject* args) {
       return nullptr;
     }
     own->pattern = p;
+    own->here = std::strncmp(e.name, "det_tok8_", 9) == 0;
     own->general = PyObject_GetAttrString(declared, e.name);
     own->raise_status = Py_NewRef(raise);
     PyObject* self = own->general ? PyCapsule_New(own.get(), nullptr, callable_free) : nullptr;

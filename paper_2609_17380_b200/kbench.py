@@ -5,7 +5,8 @@
 Cases follow the benchmark configurations: the order-fixed reductions (RMSNorm 16384x2048 f32, cross-entropy
 4096x50304, sum of squares over 1.2e9 f32), the 1B-shaped linear set at 8192 tokens per micro-batch, attention
 (4 x 16 heads x 2048), the LM head, accumulation, AdamW and the hash; then the operators of other blocks: layer norm at the residual
-stream (16384 x 2048 bf16), activations in 8 bits, SwiGLU on them, the linear recurrence (8 x 4096 x 2048).  `--small` shrinks every case to a few hundred
+stream (16384 x 2048 bf16), activations in 8 bits, SwiGLU on them, the linear recurrence (8 x 4096 x 2048), the linears with token and
+channel scales and the gated block on them, AdamW with moments in 8 bits.  `--small` shrinks every case to a few hundred
 MB for profiler captures.  Rates are algorithmic bytes (or integer / floating-point operations) per second.
 """
 import argparse
@@ -139,6 +140,32 @@ def case_linrec(small, bwd):
     if bwd:   # gv and dgv are held by the call
         return (lambda gv=gv, dgv=dgv: det.det_linrec_bwd(dy, D, p, p + 2 * D, 2 * D, B, S, D, st, o, o + 2 * D, 2 * D)), 10.5 * T * D, "B"
     return (lambda gv=gv: fwd()), 6.5 * T * D, "B"
+
+
+def _tok8(x):
+    """Codes and scales of rows of x."""
+    q, s = torch.empty(x.shape[0], det.det_tok8_ld(x.shape[1]), dtype=I8, device="cuda"), torch.empty(x.shape[0], device="cuda")
+    det.det_tok8_quant(x, x.shape[1], *x.shape, q, s)
+    return q, s
+
+
+def case_tok8(small, what):
+    """Linears with token and channel scales: the down projection of the 1B-shaped decoder, backward with its operands' preparation; the gated block."""
+    M, D, Fh = (2048 if small else 8192), 2048, 8192
+    glu = what.startswith("glu")
+    N, K = (2 * Fh, D) if glu else (D, Fh)
+    x, w = _bf16(M, K), 0.02 * _bf16(N, K)
+    (qx, sx), (qw, sw) = _tok8(x), _tok8(w)
+    qwt = torch.empty(K, det.det_tok8_ld(N), dtype=I8, device="cuda")
+    det.det_tok8_transpose(qw, N, K, qwt)
+    y, h, d, dx, dw = _bf16(M, N), _bf16(M, Fh), _bf16(M, Fh if glu else N), _bf16(M, K), torch.empty(N, K, device="cuda")
+    wk = ws((det.det_tok8_glu_bwd_ws_bytes(M, Fh, K) if glu else det.det_tok8_linear_bwd_ws_bytes(M, N, K)) + 256)[:-256]
+    ops = 2.0 * M * N * K
+    return {"linear_fwd": ((lambda: det.det_tok8_linear_fwd(x, K, qw, sw, M, N, K, y, N, qx, sx)), ops, "op"),
+            "linear_bwd": ((lambda: det.det_tok8_linear_bwd(d, N, qx, sx, qwt, sw, M, N, K, dx, K, dw, wk)), 2 * ops, "op"),
+            "glu_fwd": ((lambda: det.det_tok8_glu_fwd(x, K, qw, sw, M, Fh, K, h, Fh, y, N, qx, sx)), ops, "op"),
+            "glu_bwd": ((lambda: det.det_tok8_glu_bwd(d, Fh, y, N, qx, sx, qwt, sw, M, Fh, K, dx, K, dw, wk)), 2 * ops, "op"),
+            "quant": ((lambda: det.det_tok8_quant(x, K, M, K, qx, sx)), 3.0 * M * K, "B")}[what]
 
 
 def case_xent(small, bwd):
@@ -283,6 +310,13 @@ def case_adamw(small):
     return (lambda: det.det_adamw_step(desc, det.DET_BF16, p, g, m, v, n)), 24.0 * n, "B"
 
 
+def case_adamw8(small):
+    n = (1 << 26) if small else (1 << 28)
+    p, g, m, v = randn_bf16(n, 0.02), torch.randn(n, device="cuda") * 1e-3, torch.zeros(n, dtype=I8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    s, desc = torch.zeros(det.det_adamw8_scale_floats(n), device="cuda"), det.det_adamw_desc(3e-4, 0.9, 0.95, 1e-8, 0.1, 1)
+    return (lambda: det.det_adamw8_batch([desc], [det.DET_BF16], [p], [g], [m], [v], [s])), (12.0 + 1 / 16) * n, "B"
+
+
 def case_hash(small):
     n = (1 << 28) if small else (1 << 30)
     b = torch.randint(0, 255, (n,), dtype=torch.uint8, device="cuda")
@@ -297,13 +331,15 @@ def build_cases():
          "attn_fwd_int8pv": lambda s: case_attn(s, False, True), "attn_fwd_v2": case_attn_v2,
          "attn_bwd_fixq": lambda s: case_attn(s, True, False, True),
          "lmhead_fwd": lambda s: case_lmhead(s, False), "lmhead_fwd_v2": case_lmhead_v2, "lmhead_bwd_v2": case_lmhead_bwd_v2, "lmhead_bwd": lambda s: case_lmhead(s, True),
-         "accum": case_accum, "adamw": case_adamw, "hash": case_hash,
+         "accum": case_accum, "adamw": case_adamw, "adamw8": case_adamw8, "hash": case_hash,
          "act8_pack": lambda s: case_act8(s, False), "act8_unpack": lambda s: case_act8(s, True),
          "linrec_fwd": lambda s: case_linrec(s, False), "linrec_bwd": lambda s: case_linrec(s, True)}
     for k in ("fwd", "bwd", "bwd_act8"):
         c["layernorm_" + k] = (lambda s, k=k: case_layernorm(s, k))
     for k in ("fwd", "again", "bwd"):
         c["swiglu_act8_" + k] = (lambda s, k=k: case_swiglu_act8(s, k))
+    for k in ("quant", "linear_fwd", "linear_bwd", "glu_fwd", "glu_bwd"):
+        c["tok8_" + k] = (lambda s, k=k: case_tok8(s, k))
     for k in LINEAR_SHAPES:
         c["igemm_" + k] = (lambda s, k=k: case_igemm(s, k))
         c["linear_fwd_" + k] = (lambda s, k=k: case_linear(s, k, False))
