@@ -133,7 +133,8 @@ __device__ __forceinline__ void a8_put(const float (&m)[8], const float (&v)[8],
   am = __reduce_max_sync(0xffffffffu, am);
   av = __reduce_max_sync(0xffffffffu, av);
   // the largest root is the root of the largest
-  const float sm = a8_scale(am), sr = av >= 0x7f800000u ? __int_as_float(0x7fffffff) : a8_sqrt(__uint_as_float(av)), im = a8_inverse(sm), ir = a8_inverse(sr);
+  const float sm = a8_scale(am), sr = av >= 0x7f800000u ? __int_as_float(0x7fffffff) : a8_sqrt(__uint_as_float(av));
+  const float inv = a8_inverse(lane & 1 ? sr : sm), im = __shfl_sync(0xffffffffu, inv, 0), ir = __shfl_sync(0xffffffffu, inv, 1);   // one division for both
   const uint32_t fm = am < 0x7f800000u ? ~0u : 0u, fr = av < 0x7f800000u ? ~0u : 0u;
   if (lane == 0) *s = make_float2(sm, sr);
 #pragma unroll

@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Exceptions.h>
 #include <ATen/Context.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include "../../include/det.h"
@@ -40,13 +41,18 @@ static bool address_of(PyObject* t, unsigned long long& out) {
   return false;
 }
 // the same for calls that refuse a tensor on another device than the current one, where the kernels run: 8-bit linears, AdamW with moments in 8 bits
-static bool address_here(PyObject* t, unsigned long long& out) {
+static bool address_on(PyObject* t, unsigned long long& out, int device) {
   if (!address_of(t, out)) return false;
-  if (THPVariable_Check(t) && THPVariable_Unpack(t).get_device() != c10::cuda::current_device()) {
+  if (THPVariable_Check(t) && THPVariable_Unpack(t).get_device() != device) {
     PyErr_SetString(PyExc_AssertionError, "tensors must be on the current CUDA device");
     return false;
   }
   return true;
+}
+// the current device, none where there is no GPU (a tensor on one is refused then as any is that is on the host)
+static int current_device() {
+  c10::DeviceIndex d = -1;
+  return c10::cuda::GetDevice(&d) == cudaSuccess ? d : -1;
 }
 static unsigned long long current_stream() {
   at::globalContext().lazyInitDevice(c10::DeviceType::CUDA);
@@ -166,7 +172,8 @@ static PyObject* entry_call(PyObject* self, PyObject* const* args, Py_ssize_t na
   const Callable* e = static_cast<const Callable*>(PyCapsule_GetPointer(self, nullptr));
   if (!e) return nullptr;
   const char* name = e->entry->name;
-  const auto address = e->here ? address_here : address_of;
+  const int device = e->here ? current_device() : -1;
+  const auto address = [&](PyObject* x, unsigned long long& out) { return e->here ? address_on(x, out, device) : address_of(x, out); };
   Slot s[MAX_ARGS];
   int n = 0, rc;
   Py_ssize_t a = 0;
@@ -227,7 +234,7 @@ struct Table {                                 // a list or tuple of tensors
   std::vector<size_t> n;
   std::vector<int> width;                      // bytes of an element, 0 for None
   ~Table() { Py_XDECREF(seq); }
-  bool take(PyObject* list, bool may_be_none) {
+  bool take(PyObject* list, bool may_be_none, int device) {
     seq = PySequence_Fast(list, "a table is a list of tensors");
     if (!seq) return false;
     const Py_ssize_t k = PySequence_Fast_GET_SIZE(seq);
@@ -237,7 +244,7 @@ struct Table {                                 // a list or tuple of tensors
       unsigned long long a = 0;
       if (t == Py_None && may_be_none) { p[i] = nullptr; n[i] = 0; width[i] = 0; continue; }
       if (!THPVariable_Check(t)) { PyErr_SetString(PyExc_AssertionError, "a table holds tensors"); return false; }
-      if (!address_here(t, a)) return false;
+      if (!address_on(t, a, device)) return false;
       const at::Tensor& x = THPVariable_Unpack(t);
       p[i] = reinterpret_cast<void*>(a);
       n[i] = (size_t)x.numel();
@@ -254,15 +261,16 @@ static PyObject* adamw8_batch(PyObject*, PyObject* args) {
   HANDLE_TH_ERRORS
   PyObject *descs, *kinds, *lists[5], *coef, *outs;
   if (!PyArg_ParseTuple(args, "OOOOOOOOO", &descs, &kinds, &lists[0], &lists[1], &lists[2], &lists[3], &lists[4], &coef, &outs)) return nullptr;
+  const int device = current_device();
   Table in[5], out[4];
   const int of_out[4] = {0, 2, 3, 4};
   for (int i = 0; i < 5; ++i)
-    if (!in[i].take(lists[i], i == 4)) return nullptr;
+    if (!in[i].take(lists[i], i == 4, device)) return nullptr;
   if (outs != Py_None) {
     PyObject* four[4];
     if (!PyArg_ParseTuple(outs, "OOOO", &four[0], &four[1], &four[2], &four[3])) return nullptr;
     for (int i = 0; i < 4; ++i)
-      if (!out[i].take(four[i], i == 3)) return nullptr;
+      if (!out[i].take(four[i], i == 3, device)) return nullptr;
   }
   Table* to[4];
   for (int i = 0; i < 4; ++i) to[i] = outs == Py_None ? &in[of_out[i]] : &out[i];
@@ -301,7 +309,7 @@ static PyObject* adamw8_batch(PyObject*, PyObject* args) {
     return nullptr;
   }
   unsigned long long c = 0;
-  if (!address_here(coef, c)) return nullptr;
+  if (!address_on(coef, c, device)) return nullptr;
   void* st = reinterpret_cast<void*>(current_stream());
   int rc;
   Py_BEGIN_ALLOW_THREADS
@@ -318,9 +326,10 @@ static PyObject* adamw8_numbers(PyObject*, PyObject* args) {
   int pack;
   PyObject* lists[5];
   if (!PyArg_ParseTuple(args, "pOOOOO", &pack, &lists[0], &lists[1], &lists[2], &lists[3], &lists[4])) return nullptr;
+  const int device = current_device();
   Table t[5];
   for (int i = 0; i < 5; ++i)
-    if (!t[i].take(lists[i], false)) return nullptr;
+    if (!t[i].take(lists[i], false, device)) return nullptr;
   const size_t k = t[0].p.size();
   bool fit = true;
   for (const Table& x : t) fit = fit && x.p.size() == k;
