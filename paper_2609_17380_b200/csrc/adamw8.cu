@@ -11,23 +11,24 @@
 namespace det {
 
 constexpr int A8_VALUES = 256;            // values that share scales: a warp's, eight a lane
-constexpr int ADAM8_JOBS = 128;           // tensors per launch
+constexpr int ADAM8_JOBS = 128, ADAM8_FEW = 16;     // tensors per launch; a launch of few has a shorter table to hand over
 constexpr float A8_127 = 0x1.020408p-7f, A8_255 = 0x1.010102p-8f;     // 1/127, 1/255
 
 struct Adam8Scalars { float b1, b2, omb1, omb2, eps, stepsz, isb2, decay; };
 // Job j: CTAs first[j] .. first[j + 1] - 1 of the launch, each with `rounds` times 2048 of its len[j] values, 256 a warp and round.  A job belongs to whole
 // CTAs, and its entries, constants at an index, are read once for all rounds.  s NULL: moments in 32 bits.
+template <int CAP>
 struct Adam8Jobs {
   int n, rounds;
-  uint32_t first[ADAM8_JOBS + 1];
-  const void *p[ADAM8_JOBS], *m[ADAM8_JOBS], *v[ADAM8_JOBS];
-  const float* s[ADAM8_JOBS];
-  float* g[ADAM8_JOBS];
-  void *po[ADAM8_JOBS], *mo[ADAM8_JOBS], *vo[ADAM8_JOBS];
-  float* so[ADAM8_JOBS];
-  size_t len[ADAM8_JOBS];
-  Adam8Scalars h[ADAM8_JOBS];
-  uint8_t bf[ADAM8_JOBS];
+  uint32_t first[CAP + 1];
+  const void *p[CAP], *m[CAP], *v[CAP];
+  const float* s[CAP];
+  float* g[CAP];
+  void *po[CAP], *mo[CAP], *vo[CAP];
+  float* so[CAP];
+  size_t len[CAP];
+  Adam8Scalars h[CAP];
+  uint8_t bf[CAP];
 };
 
 __device__ __forceinline__ float a8_first(int c, float s) {
@@ -279,7 +280,8 @@ __device__ __forceinline__ int a8_job(const uint32_t* first, int n) {      // th
   }
   return lo;
 }
-__global__ void __launch_bounds__(256) k_adamw8(const __grid_constant__ Adam8Jobs jobs, const float* __restrict__ coef) {
+template <int CAP>
+__global__ void __launch_bounds__(256) k_adamw8(const __grid_constant__ Adam8Jobs<CAP> jobs, const float* __restrict__ coef) {
   grid_dep();
   const int j = a8_job(jobs.first, jobs.n), lane = threadIdx.x & 31;
   const size_t base = ((size_t)(blockIdx.x - jobs.first[j]) * (8 * jobs.rounds) + (threadIdx.x >> 5)) * A8_VALUES;
@@ -297,16 +299,17 @@ __global__ void __launch_bounds__(256) k_adamw8(const __grid_constant__ Adam8Job
 }
 
 // Codes to numbers and back, many tensors at once.
+template <int CAP>
 struct Adam8Numbers {
   int n, rounds;
-  uint32_t first[ADAM8_JOBS + 1];
-  int8_t* m8[ADAM8_JOBS];
-  uint8_t* v8[ADAM8_JOBS];
-  float *s[ADAM8_JOBS], *m[ADAM8_JOBS], *v[ADAM8_JOBS];
-  size_t len[ADAM8_JOBS];
+  uint32_t first[CAP + 1];
+  int8_t* m8[CAP];
+  uint8_t* v8[CAP];
+  float *s[CAP], *m[CAP], *v[CAP];
+  size_t len[CAP];
 };
-template <bool PACK, bool FULL>
-__device__ __forceinline__ void adam8_numbers(const Adam8Numbers& jobs, int j, size_t base, size_t len, int lane) {
+template <bool PACK, bool FULL, int CAP>
+__device__ __forceinline__ void adam8_numbers(const Adam8Numbers<CAP>& jobs, int j, size_t base, size_t len, int lane) {
   const size_t i0 = base + lane * 4;
   float2* s = reinterpret_cast<float2*>(jobs.s[j]) + base / A8_VALUES;
   int n[2];
@@ -348,8 +351,8 @@ __device__ __forceinline__ void adam8_numbers(const Adam8Numbers& jobs, int j, s
     }
   }
 }
-template <bool PACK>
-__global__ void __launch_bounds__(256) k_adamw8_numbers(const __grid_constant__ Adam8Numbers jobs) {
+template <bool PACK, int CAP>
+__global__ void __launch_bounds__(256) k_adamw8_numbers(const __grid_constant__ Adam8Numbers<CAP> jobs) {
   grid_dep();
   const int j = a8_job(jobs.first, jobs.n), lane = threadIdx.x & 31;
   const size_t len = jobs.len[j];
@@ -382,15 +385,16 @@ static bool a8_moments_at(const void* m, const void* v, const void* s) {
   return s ? a8_at(m, 4) && a8_at(v, 4) && a8_at(s, 8) : a8_at(m, 16) && a8_at(v, 16);
 }
 // the tensors t, t + 1, ... as jobs of one launch: fill(job, tensor) for each that has values
-template <class Jobs, class Fill>
+template <int CAP, class Jobs, class Fill>
 static int a8_take(Jobs& jobs, int& t, int ntensors, const size_t* n, Fill fill) {
-  // four rounds a CTA where the CTAs fill the GPU some times over all the same
+  // as many rounds a CTA, up to four, as the GPU would otherwise be filled times over: what a CTA does first (finding its job) takes as long as a round
   size_t ctas = 0, total = 0;
-  for (int i = t; i < ntensors; ++i) total += n[i] / (8 * A8_VALUES);
+  const size_t places = (size_t)4 * (dev_sm_count() > 0 ? dev_sm_count() : 1);
+  for (int i = t; i < ntensors; ++i) total += (n[i] + 8 * A8_VALUES - 1) / (8 * A8_VALUES);
   jobs.n = 0;
-  jobs.rounds = total >= 16384 ? 4 : 1;
+  jobs.rounds = (int)(total > 4 * places ? 4 : total > places ? (total + places - 1) / places : 1);
   const size_t per = (size_t)8 * A8_VALUES * jobs.rounds;
-  for (; t < ntensors && jobs.n < ADAM8_JOBS; ++t) {
+  for (; t < ntensors && jobs.n < CAP; ++t) {
     if (!n[t]) continue;
     const size_t each = (n[t] + per - 1) / per;
     if (ctas + each > 0x7fffffffull) break;                                // one tensor alone is within that, see the callers
@@ -401,6 +405,41 @@ static int a8_take(Jobs& jobs, int& t, int ntensors, const size_t* n, Fill fill)
   }
   jobs.first[jobs.n] = (uint32_t)ctas;
   return (int)ctas;
+}
+template <int CAP>
+static int a8_update(const det_adamw_desc* descs, const int* pdtypes, const void* const* p, float* const* g, const void* const* m, const void* const* v,
+                     const float* const* s, void* const* p_out, void* const* m_out, void* const* v_out, float* const* s_out, const size_t* n, int ntensors,
+                     const float* coef_dev, cudaStream_t st) {
+  for (int t = 0; t < ntensors;) {
+    Adam8Jobs<CAP> jobs;
+    int last = -1;
+    const int ctas = a8_take<CAP>(jobs, t, ntensors, n, [&](int j, int i) {
+      jobs.p[j] = p[i]; jobs.m[j] = m[i]; jobs.v[j] = v[i]; jobs.s[j] = s[i]; jobs.g[j] = g[i];
+      jobs.po[j] = p_out[i]; jobs.mo[j] = m_out[i]; jobs.vo[j] = v_out[i]; jobs.so[j] = s_out[i];
+      const det_adamw_desc &d = descs[i], &e = descs[last < 0 ? i : last];  // tensors in a row mostly share theirs
+      const bool same = last >= 0 && d.lr == e.lr && d.beta1 == e.beta1 && d.beta2 == e.beta2 && d.eps == e.eps && d.weight_decay == e.weight_decay &&
+                        d.step == e.step;
+      if (same) jobs.h[j] = jobs.h[j - 1];
+      else jobs.h[j] = a8_scalars(&d);
+      last = i;
+      jobs.bf[j] = pdtypes[i] == DET_BF16;
+    });
+    if (!jobs.n) break;
+    launch_after(k_adamw8<CAP>, ctas, 256, 0, st, jobs, coef_dev);
+    DET_CHECK_LAUNCH();
+  }
+  return DET_OK;
+}
+template <bool PACK, int CAP>
+static int a8_convert(int8_t* const* m8, uint8_t* const* v8, float* const* s, float* const* m, float* const* v, const size_t* n, int ntensors, cudaStream_t st) {
+  for (int t = 0; t < ntensors;) {
+    Adam8Numbers<CAP> jobs;
+    const int ctas = a8_take<CAP>(jobs, t, ntensors, n, [&](int j, int i) { jobs.m8[j] = m8[i]; jobs.v8[j] = v8[i]; jobs.s[j] = s[i]; jobs.m[j] = m[i]; jobs.v[j] = v[i]; });
+    if (!jobs.n) break;
+    launch_after(k_adamw8_numbers<PACK, CAP>, ctas, 256, 0, st, jobs);
+    DET_CHECK_LAUNCH();
+  }
+  return DET_OK;
 }
 }  // namespace det
 
@@ -422,19 +461,8 @@ extern "C" int det_adamw8_batch(const det_adamw_desc* descs, const int* pdtypes,
     if (!a8_at(p[t], ap) || !a8_at(p_out[t], ap) || !aligned16(g[t]) || !a8_moments_at(m[t], v[t], s[t]) || !a8_moments_at(m_out[t], v_out[t], s_out[t]))
       return DET_ERR_ALIGN;
   }
-  for (int t = 0; t < ntensors;) {
-    Adam8Jobs jobs;
-    const int ctas = a8_take(jobs, t, ntensors, n, [&](int j, int i) {
-      jobs.p[j] = p[i]; jobs.g[j] = g[i]; jobs.m[j] = m[i]; jobs.v[j] = v[i]; jobs.s[j] = s[i];
-      jobs.po[j] = p_out[i]; jobs.mo[j] = m_out[i]; jobs.vo[j] = v_out[i]; jobs.so[j] = s_out[i];
-      jobs.h[j] = a8_scalars(&descs[i]);
-      jobs.bf[j] = pdtypes[i] == DET_BF16;
-    });
-    if (!jobs.n) break;
-    launch_after(k_adamw8, ctas, 256, 0, (cudaStream_t)stream, jobs, coef_dev);
-    DET_CHECK_LAUNCH();
-  }
-  return DET_OK;
+  const auto few = a8_update<ADAM8_FEW>, many = a8_update<ADAM8_JOBS>;
+  return (ntensors <= ADAM8_FEW ? few : many)(descs, pdtypes, p, g, m, v, s, p_out, m_out, v_out, s_out, n, ntensors, coef_dev, (cudaStream_t)stream);
 }
 
 template <bool PACK>
@@ -446,14 +474,8 @@ static int a8_numbers(int8_t* const* m8, uint8_t* const* v8, float* const* s, fl
     if (n[t] > (size_t)0x7fffffff * A8_VALUES) return DET_ERR_SHAPE;
     if (!a8_moments_at(m8[t], v8[t], s[t]) || !aligned16(m[t]) || !aligned16(v[t])) return DET_ERR_ALIGN;
   }
-  for (int t = 0; t < ntensors;) {
-    Adam8Numbers jobs;
-    const int ctas = a8_take(jobs, t, ntensors, n, [&](int j, int i) { jobs.m8[j] = m8[i]; jobs.v8[j] = v8[i]; jobs.s[j] = s[i]; jobs.m[j] = m[i]; jobs.v[j] = v[i]; });
-    if (!jobs.n) break;
-    launch_after(k_adamw8_numbers<PACK>, ctas, 256, 0, (cudaStream_t)stream, jobs);
-    DET_CHECK_LAUNCH();
-  }
-  return DET_OK;
+  const auto few = a8_convert<PACK, ADAM8_FEW>, many = a8_convert<PACK, ADAM8_JOBS>;
+  return (ntensors <= ADAM8_FEW ? few : many)(m8, v8, s, m, v, n, ntensors, (cudaStream_t)stream);
 }
 extern "C" int det_adamw8_pack(const float* const* m, const float* const* v, int8_t* const* m8, uint8_t* const* v8, float* const* s, const size_t* n,
                                int ntensors, void* stream) {
