@@ -122,11 +122,13 @@ __global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict_
 
 // Codes [R, ld(C)] -> [C, ld(R)], through shared memory, whole 128-byte lines on both sides but at the edges.  What lies behind column C of the
 // input is zero; so is what is written behind column R.
-// fill: the kernel before has nothing to do with it (common.cuh).
-__global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__ in, int R, int C, int8_t* __restrict__ out, int fill) {
+// fill: the kernel before has nothing to do with it (common.cuh).  zero: words that are set to 0 besides.
+__global__ void __launch_bounds__(128) k_t8_transpose(const int8_t* __restrict__ in, int R, int C, int8_t* __restrict__ out, int fill, uint32_t* __restrict__ zero,
+                                                      int nzero) {
   __shared__ __align__(16) uint8_t tile[128 * 128];
   if (fill) grid_fill_begin();
   else grid_dep();
+  for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * 128 + threadIdx.x; i < nzero; i += gridDim.x * gridDim.y * 128) zero[i] = 0u;
   const int t = threadIdx.x, c0 = blockIdx.x * 128, r0 = blockIdx.y * 128, ldi = t8_ld(C), ldo = t8_ld(R);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -365,36 +367,32 @@ __global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ 
     }
   }
 }
-// The scales and their inverses, once for every row and column; a scale that is a NaN has the inverse -1.
-__global__ void __launch_bounds__(256) k_t8_scales(const uint32_t* __restrict__ rowmax, const uint32_t* __restrict__ colmax, int M, int N, float* __restrict__ s_a,
-                                                   float* __restrict__ i_a, float* __restrict__ s_g, float* __restrict__ i_g) {
-  const int i = blockIdx.x * 256 + threadIdx.x + grid_dep();
-  if (i >= M + N) return;
-  const uint32_t m = i < M ? rowmax[i] : colmax[i - M];
-  const float s = t8_scale(m), inv = m >= 0x7f800000u ? -1.0f : t8_inverse(s);
-  if (i < M) { s_a[i] = s; i_a[i] = inv; }
-  else { s_g[i - M] = s; i_g[i - M] = inv; }
-}
 // Then the codes: A as it lies, G transposed.  A tile is 128 rows of 128 columns, in two halves of 64; a thread has 8 rows of 4
-// columns of each, four rows on their way together.  Eight codes of a column are a piece of 8 bytes, whose place in its row of the transposed tile is
-// swizzled by the columns' four, so that a warp's pieces meet in no bank.
+// columns of each, four rows on their way together.  A CTA works out the scales and inverses of its rows and columns once, a thread each.  Eight codes of a
+// column are a piece of 8 bytes, whose place in its row of the transposed tile is swizzled by the columns' four, so that a warp's pieces meet in no bank.
+struct T8CodeRoom {
+  uint8_t out[128 * 128];
+  float sx[128], ia[128], sw[128], ig[128];                               // an inverse of -1: the scale is a NaN, the codes are 0
+};
 template <bool FULL>
-__device__ __forceinline__ void t8_code_rows(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4],
-                                             const float (&ig)[2][4], const float* __restrict__ i_a, int8_t* __restrict__ qa, uint32_t (&g)[2][2][4]) {
+__device__ __forceinline__ void t8_code_fetch(const T8Grad& x, int r0, const int (&at)[2], const int (&left)[2], uint2 (&w)[4][2]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (!FULL && r0 + k >= x.M) { w[k][0] = w[k][1] = make_uint2(0u, 0u); continue; }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[k][h] = t8_load4<FULL>(x.d, (r0 + k) * x.ld + at[h], left[h], x.vec);
+  }
+}
+// w: the first four rows, which were fetched before the scales were there
+template <bool FULL>
+__device__ __forceinline__ void t8_code_rows(const T8Grad& x, uint2 (&w)[4][2], int r0, int at0, const int (&at)[2], const int (&left)[2], const float (&sw)[2][4],
+                                             const float (&ig)[2][4], const T8CodeRoom& room, int8_t* __restrict__ qa, uint32_t (&g)[2][2][4]) {
   const int ldn = t8_ld(x.N);
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    uint2 w[4][2];
-    float sx[4], ia[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + half * 4 + k;
-      if (!FULL && r >= x.M) { w[k][0] = w[k][1] = make_uint2(0u, 0u); sx[k] = ia[k] = 0.0f; continue; }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) w[k][h] = t8_load4<FULL>(x.d, r * x.ld + at[h], left[h], x.vec);
-      sx[k] = __ldg(x.s_x + r);
-      ia[k] = __ldg(i_a + r);
-    }
+    if (half) t8_code_fetch<FULL>(x, r0 + 4, at, left, w);
+    const float4 sx4 = *reinterpret_cast<const float4*>(room.sx + at0 + half * 4), ia4 = *reinterpret_cast<const float4*>(room.ia + at0 + half * 4);
+    const float sx[4] = {sx4.x, sx4.y, sx4.z, sx4.w}, ia[4] = {ia4.x, ia4.y, ia4.z, ia4.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = r0 + half * 4 + k;
@@ -424,38 +422,53 @@ __device__ __forceinline__ void t8_code_rows(const T8Grad& x, int r0, const int 
     }
   }
 }
-__global__ void __launch_bounds__(256, 3) k_t8_grad_codes(const __grid_constant__ T8Grad x, const float* __restrict__ i_a, const float* __restrict__ i_g,
+__global__ void __launch_bounds__(256, 3) k_t8_grad_codes(const __grid_constant__ T8Grad x, const uint32_t* __restrict__ rowmax,
+                                                          const uint32_t* __restrict__ colmax, float* __restrict__ s_a, float* __restrict__ s_g,
                                                           int8_t* __restrict__ qa, int8_t* __restrict__ qgt) {
   grid_dep();
-  __shared__ __align__(16) uint8_t out[128 * 128];
+  __shared__ __align__(16) T8CodeRoom room;
   // eight tiles of rows under one another, then the next columns: what runs at a time reads long pieces of rows and writes long pieces of columns
   const int across = (x.N + 127) / 128, down = (x.M + 127) / 128, panel = blockIdx.x / (8 * across), in = blockIdx.x - panel * 8 * across;
   const int high = min(8, down - panel * 8), c0 = in / high * 128, r0 = (panel * 8 + in % high) * 128;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, ldm = t8_ld(x.M);
   const int at[2] = {c0 + tx * 4, c0 + tx * 4 + 64}, left[2] = {x.N - at[0], x.N - at[1]};
+  const bool full = x.vec && c0 + 128 <= x.N && r0 + 128 <= x.M;
+  uint2 w[4][2];
+  if (full) t8_code_fetch<true>(x, r0 + ty * 8, at, left, w);
+  else t8_code_fetch<false>(x, r0 + ty * 8, at, left, w);
+  {
+    const int k = threadIdx.x & 127;
+    const bool row = threadIdx.x < 128, there = row ? r0 + k < x.M : c0 + k < x.N;
+    const uint32_t m = !there ? 0u : row ? rowmax[r0 + k] : colmax[c0 + k];
+    const float factor = !there ? 0.0f : row ? x.s_x[r0 + k] : x.s_w[c0 + k], s = t8_scale(m), inv = m >= 0x7f800000u ? -1.0f : t8_inverse(s);
+    (row ? room.sx : room.sw)[k] = factor;
+    (row ? room.ia : room.ig)[k] = inv;
+    if (there && row && c0 == 0) s_a[r0 + k] = s;
+    if (there && !row && r0 == 0) s_g[c0 + k] = s;
+  }
+  __syncthreads();
   float sw[2][4], ig[2][4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      sw[h][t] = t < left[h] ? x.s_w[at[h] + t] : 0.0f;
-      ig[h][t] = t < left[h] ? i_g[at[h] + t] : 0.0f;
-    }
+  for (int h = 0; h < 2; ++h) {
+    const float4 a = *reinterpret_cast<const float4*>(room.sw + h * 64 + tx * 4), b = *reinterpret_cast<const float4*>(room.ig + h * 64 + tx * 4);
+    sw[h][0] = a.x; sw[h][1] = a.y; sw[h][2] = a.z; sw[h][3] = a.w;
+    ig[h][0] = b.x; ig[h][1] = b.y; ig[h][2] = b.z; ig[h][3] = b.w;
+  }
   uint32_t g[2][2][4];                                                    // [half of the columns][four rows][column], a byte a row
-  if (x.vec && c0 + 128 <= x.N && r0 + 128 <= x.M) t8_code_rows<true>(x, r0 + ty * 8, at, left, sw, ig, i_a, qa, g);
-  else t8_code_rows<false>(x, r0 + ty * 8, at, left, sw, ig, i_a, qa, g);
+  if (full) t8_code_rows<true>(x, w, r0 + ty * 8, ty * 8, at, left, sw, ig, room, qa, g);
+  else t8_code_rows<false>(x, w, r0 + ty * 8, ty * 8, at, left, sw, ig, room, qa, g);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const bool dead = ig[h][t] < 0.0f;
-      *reinterpret_cast<uint2*>(out + (h * 64 + tx * 4 + t) * 128 + ((ty ^ tx) << 3)) = make_uint2(dead ? 0u : g[h][0][t], dead ? 0u : g[h][1][t]);
+      *reinterpret_cast<uint2*>(room.out + (h * 64 + tx * 4 + t) * 128 + ((ty ^ tx) << 3)) = make_uint2(dead ? 0u : g[h][0][t], dead ? 0u : g[h][1][t]);
     }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int k = i * 32 + (threadIdx.x >> 3), ch = threadIdx.x & 7, f = (k >> 2) & 15;
-    uint4 w = *reinterpret_cast<const uint4*>(out + k * 128 + (((2 * ch) ^ (f & 14)) << 3));
+    uint4 w = *reinterpret_cast<const uint4*>(room.out + k * 128 + (((2 * ch) ^ (f & 14)) << 3));
     if (f & 1) w = make_uint4(w.z, w.w, w.x, w.y);
     if (c0 + k < x.N && r0 + ch * 16 < ldm) *reinterpret_cast<uint4*>(qgt + (size_t)(c0 + k) * ldm + r0 + ch * 16) = w;
   }
@@ -1237,7 +1250,7 @@ static int t8_sizes(long long M, long long N, long long K) {
 static int t8_vec(const void* p, size_t ld, int size) { return aligned16(p) && ld * size % 16 == 0; }
 
 // gradient operands into the workspace, then both products
-struct T8Ws { size_t qa, qgt, qxt, s_a, s_g, i_a, i_g, rowmax, colmax, dgu, bytes; };
+struct T8Ws { size_t qa, qgt, qxt, s_a, s_g, rowmax, colmax, dgu, bytes; };
 static size_t t8_ld_dgu(int N) { return ((size_t)N + 7) / 8 * 8; }
 static T8Ws t8_ws(int M, int N, int K, bool glu) {
   T8Ws w;
@@ -1248,15 +1261,13 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
   w.qxt = take((size_t)K * t8_ld(M));
   w.s_a = take((size_t)M * 4);
   w.s_g = take((size_t)N * 4);
-  w.i_a = take((size_t)M * 4);
-  w.i_g = take((size_t)N * 4);
   w.rowmax = take((size_t)M * 4);
   w.colmax = take((size_t)N * 4);
   w.dgu = take(glu ? (size_t)M * t8_ld_dgu(N) * 2 : 0);
   w.bytes = at;
   return w;
 }
-struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *i_a, *s_g, *i_g; int8_t *qa, *qgt; };
+struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *s_g; int8_t *qa, *qgt; };
 template <bool GLU, int TAB>
 static int t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
   const size_t smem = T8MaxRoom<GLU, TAB>::BYTES;
@@ -1277,30 +1288,29 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
   if (sms <= 0) return DET_ERR_CUDA;
   const T8Ws w = t8_ws(M, N, K, x.gu != nullptr);
   int8_t* qxt = (int8_t*)(ws + w.qxt);
-  const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), (float*)(ws + w.s_a), (float*)(ws + w.i_a), (float*)(ws + w.s_g),
-                         (float*)(ws + w.i_g), (int8_t*)(ws + w.qa), (int8_t*)(ws + w.qgt)};
-  if (cudaMemsetAsync(op.rowmax, 0, w.dgu - w.rowmax, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
-  const bool table = (long long)M * x.W >= 8LL * sms * 128 * 64;           // some tiles for every CTA
-  const int rc0 = !x.gu ? t8_largest<false, 0>(x, op, sms, st) : table ? t8_largest<true, 1>(x, op, sms, st) : t8_largest<true, 0>(x, op, sms, st);
-  if (rc0 != DET_OK) return rc0;
-  launch_after(k_t8_scales, (unsigned)((M + N + 255) / 256), 256, 0, st, op.rowmax, op.colmax, M, N, op.s_a, op.i_a, op.s_g, op.i_g);
-  T8Grad y = x;                                                            // as the codes are made of it
-  if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
-  launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.i_a, op.i_g, op.qa, op.qgt);
-  DET_CHECK_LAUNCH();
+  const T8Operands op = {(uint32_t*)(ws + w.rowmax), (uint32_t*)(ws + w.colmax), (float*)(ws + w.s_a), (float*)(ws + w.s_g), (int8_t*)(ws + w.qa), (int8_t*)(ws + w.qgt)};
   T8Out ox = {}, ow = {};
   ox.out = dX; ox.ld = ld_dx; ox.rs = op.s_a; ox.I = M; ox.J = K; ox.K = N; ox.vec = t8_vec(dX, ld_dx, 2);
   ow.out = dW; ow.ld = K; ow.rs = op.s_g; ow.I = N; ow.J = K; ow.K = M; ow.vec = t8_vec(dW, K, 4);
   const T8Plan px = t8_plan(T8_BF16, ox, sms), pw = t8_plan(T8_F32, ow, sms);
   const dim3 tgrid((K + 127) / 128, (M + 127) / 128);
-  // Where the first product leaves SMs without a CTA the second comes in beside it, and the transposition has to be done before; else the transposition runs
-  // beside the first product, which leaves the memory idle and room on every SM for two CTAs of it (8192 x 2048 x 8192: 248 -> 229 us).
+  // Where the first product leaves SMs without a CTA the second comes in beside it, and the transposition is done first, which sets the maxima to 0 as well; else
+  // it runs beside the first product, which leaves the memory idle and room on every SM for two CTAs of it (8192 x 2048 x 8192: 248 -> 229 us).
   const bool beside = dX && dW && px.ctas < sms;
-  if (beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, 1);
+  const int words = (int)((w.dgu - w.rowmax) / 4);
+  if (beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, 0, op.rowmax, words);
+  else if (cudaMemsetAsync(op.rowmax, 0, (size_t)words * 4, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
+  const bool table = (long long)M * x.W >= 8LL * sms * 128 * 64;           // some tiles for every CTA
+  const int rc0 = !x.gu ? t8_largest<false, 0>(x, op, sms, st) : table ? t8_largest<true, 1>(x, op, sms, st) : t8_largest<true, 0>(x, op, sms, st);
+  if (rc0 != DET_OK) return rc0;
+  T8Grad y = x;                                                            // as the codes are made of it
+  if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
+  launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.rowmax, op.colmax, op.s_a, op.s_g, op.qa, op.qgt);
+  DET_CHECK_LAUNCH();
   int rc = DET_OK;
   if (dX) rc = t8_product<T8_BF16>(px, op.qa, qWt, K, ox, 0, status, st);
   if (dW && rc == DET_OK) {
-    if (!beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, dX ? 1 : 0);
+    if (!beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, dX ? 1 : 0, (uint32_t*)nullptr, 0);
     rc = t8_product<T8_F32>(pw, op.qgt, qxt, K, ow, beside ? 1 : 0, status, st);
   }
   if (rc != DET_OK) return rc;
@@ -1327,7 +1337,7 @@ extern "C" int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, voi
   if ((M + 127) / 128 > 65535) return DET_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(qT)) return DET_ERR_ALIGN;
   if (!M) return DET_OK;
-  launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, (cudaStream_t)stream, q, M, K, qT, 0);
+  launch_after(k_t8_transpose, dim3((K + 127) / 128, (M + 127) / 128), 128, 0, (cudaStream_t)stream, q, M, K, qT, 0, (uint32_t*)nullptr, 0);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
