@@ -4,6 +4,9 @@
 // scale, in 127 (m, with the sign of m) or 255 (r) parts: small values keep digits that equal steps would lose, and a code c of r is off by 2/c of v
 // at most.  A root that is not zero has a code of 1 at least, so that no update divides by eps where the first moment has outlived the second.
 // The update itself is det_adamw_batch's; the parameter moves by the moments before they are put into codes.
+//
+// 67 M values with bf16 parameters and the clip stored (16 bytes each) 198 us, 5.4 TB/s, bound by its 78 instructions a value (81 % of the issue slots); the
+// moments as numbers 115 us, 5.8 TB/s.
 #include "common.cuh"
 #include "internal.h"
 #include "rows.cuh"
