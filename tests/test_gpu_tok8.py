@@ -237,3 +237,116 @@ def test_graph_and_streams(det):
             same(host(b["h"], np.uint16), h, "h")
             same(host(b["dx"], np.uint16), dX, "dx")
             same(host(b["dw"]), dW, "dw")
+
+
+# contractions near the limit, forward and backward
+@pytest.mark.parametrize("M,N,K", [(2, 24, 131071), (1, 16, 40000), (70001, 24, 40), (24, 70001, 40)])
+def test_long_contractions(det, M, N, K):
+    x, w, dy = rows(M, K, 1), synth.normal_bf16((N, K), 0.02, seed=2), rows(M, N, 3, 0.01)
+    Y, qX, sX, qW, sW = oracle.tok8_linear_fwd(x, w)
+    y, q, s = empty((M, N), np.uint16), empty((M, det.det_tok8_ld(K)), np.int8), empty((M,), F)
+    det.det_tok8_linear_fwd(dev(x), K, dev(codes(qW)), dev(sW), M, N, K, y, N, q, s)
+    dx, dw = empty((M, K), np.uint16), empty((N, K), F)
+    det.det_tok8_linear_bwd(dev(dy), N, q, s, dev(codes(np.ascontiguousarray(qW.T))), dev(sW), M, N, K, dx, K, dw, ws(det.det_tok8_linear_bwd_ws_bytes(M, N, K)))
+    _sync()
+    dX, dW = oracle.tok8_linear_bwd(dy, x, w)
+    same(host(y, np.uint16), Y, "y")
+    same(host(dx, np.uint16), dX, "dx")
+    same(host(dw), dW, "dw")
+
+
+def test_extreme_codes(det):
+    """The largest sum there is: 131071 products of 127 and -127."""
+    K = 131071
+    x = np.full((9, K), 0x3F80, np.uint16)
+    w = np.full((70, K), 0xBF80, np.uint16)
+    for M in (1, 9):
+        Y, _, _, qW, sW = oracle.tok8_linear_fwd(x[:M], w)
+        y = empty((M, 70), np.uint16)
+        det.det_tok8_linear_fwd(dev(x[:M]), K, dev(codes(qW)), dev(sW), M, 70, K, y, 70, empty((M, det.det_tok8_ld(K)), np.int8), empty((M,), F))
+        _sync()
+        same(host(y, np.uint16), Y, "y")
+        assert (synth.from_bf16(host(y, np.uint16)) == synth.from_bf16(synth.to_bf16(np.array([-K], F)))).all()
+
+
+@pytest.mark.parametrize("M,Fh,K", [(1, 40, 48), (2, 33, 65), (5, 24, 40), (40, 72, 264), (130, 65, 129)])
+def test_any_address(det, M, Fh, K):
+    """Every matrix one element off an aligned address, and rows in front of and behind the outputs that stay."""
+    import torch
+    N = 2 * Fh
+    x, w, dh = rows(M, K, 4), synth.normal_bf16((N, K), 0.02, seed=5), rows(M, Fh, 6, 0.01)
+    gu, qX, sX, qW, sW = oracle.tok8_linear_fwd(x, w)
+    hold = []
+
+    def off(a, fill=0):
+        """An array one element off, with room in front and behind; its address and how to read it back."""
+        t = torch.full((a.size + 64,), fill, dtype={2: torch.int16, 4: torch.float32}[a.itemsize], device="cuda")
+        t[1:1 + a.size] = dev(a).reshape(-1)
+        hold.append(t)
+        return t.data_ptr() + a.itemsize, t
+    wc, wt = dev(codes(qW)), dev(codes(np.ascontiguousarray(qW.T)))
+    px, ps = off(x)[0], off(sW)[0]
+    ph, th = off(np.zeros((M, Fh), np.uint16), 77)
+    pg, tg = off(np.zeros((M, N), np.uint16), 77)
+    psx, tsx = off(np.zeros(M, F), 77)
+    q = empty((M, det.det_tok8_ld(K)), np.int8)
+    det.det_tok8_glu_fwd(px, K, wc, ps, M, Fh, K, ph, Fh, pg, N, q, psx)
+    _sync()
+    back = lambda t, a, dt: host(t, dt)[1:1 + a.size].reshape(a.shape)
+    same(back(th, np.zeros((M, Fh)), np.uint16), oracle.swiglu_fwd(gu), "h")
+    same(back(tg, gu, np.uint16), gu, "gu")
+    same(back(tsx, sX, F), sX, "scales")
+    pd = off(dh)[0]
+    pdx, tdx = off(np.zeros((M, K), np.uint16), 77)
+    pdw, tdw = off(np.zeros((N, K), F), 77)
+    det.det_tok8_glu_bwd(pd, Fh, pg, N, q, psx, wt, ps, M, Fh, K, pdx, K, pdw, ws(det.det_tok8_glu_bwd_ws_bytes(M, Fh, K)))
+    _sync()
+    dX, dW = oracle.tok8_linear_bwd(oracle.swiglu_bwd(dh, gu), x, w)
+    same(back(tdx, dX, np.uint16), dX, "dx")
+    same(back(tdw, dW, F), dW, "dw")
+    for t, n in ((th, M * Fh), (tg, M * N), (tsx, M), (tdx, M * K), (tdw, N * K)):
+        assert t[0] == 77 and (t[1 + n:] == 77).all()
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 12])
+def test_few_tokens_that_are_zero_or_not_finite(det, M):
+    N, K = 70, 264
+    w = synth.normal_bf16((N, K), 0.02, seed=2)
+    qW, sW = oracle.tok8_quant(w)
+    for value in (0x0000, 0x8000, 0x7F80, 0x7FC1, 0x0001, 0x0080):                # zeros, an infinity, a NaN, a subnormal, the smallest normal
+        x = rows(M, K, 1)
+        x[M - 1] = value if value in (0x0000, 0x8000, 0x0001, 0x0080) else x[M - 1]
+        x[M - 1, 5] = value
+        Y, qX, sX, _, _ = oracle.tok8_linear_fwd(x, w)
+        y, q, s = empty((M, N), np.uint16), empty((M, det.det_tok8_ld(K)), np.int8), empty((M,), F)
+        det.det_tok8_linear_fwd(dev(x), K, dev(codes(qW)), dev(sW), M, N, K, y, N, q, s)
+        _sync()
+        same(host(y, np.uint16), Y, "y")
+        same(host(q), codes(qX), "codes")
+        same(host(s), sX, "scales")
+
+
+def test_two_calls_at_once(det):
+    """Two streams with workspaces of their own, over and over, give what each gives alone."""
+    import torch
+    M, N, K = 700, 520, 392
+    x, w, dy = rows(M, K, 1), synth.normal_bf16((N, K), 0.02, seed=2), rows(M, N, 3, 0.01)
+    Y, qX, sX, qW, sW = oracle.tok8_linear_fwd(x, w)
+    dX, dW = oracle.tok8_linear_bwd(dy, x, w)
+    wc, wt, sw, gx, gy = dev(codes(qW)), dev(codes(np.ascontiguousarray(qW.T))), dev(sW), dev(x), dev(dy)
+    torch.cuda.synchronize()
+    sides = []
+    for _ in range(2):
+        sides.append(dict(st=torch.cuda.Stream(), y=empty((M, N), np.uint16), q=empty((M, det.det_tok8_ld(K)), np.int8), s=empty((M,), F),
+                          dx=empty((M, K), np.uint16), dw=empty((N, K), F), ws=ws(det.det_tok8_linear_bwd_ws_bytes(M, N, K))))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b in sides:
+            with torch.cuda.stream(b["st"]):
+                det.det_tok8_linear_fwd(gx, K, wc, sw, M, N, K, b["y"], N, b["q"], b["s"])
+                det.det_tok8_linear_bwd(gy, N, b["q"], b["s"], wt, sw, M, N, K, b["dx"], K, b["dw"], b["ws"])
+    _sync()
+    for b in sides:
+        same(host(b["y"], np.uint16), Y, "y")
+        same(host(b["dx"], np.uint16), dX, "dx")
+        same(host(b["dw"]), dW, "dw")
