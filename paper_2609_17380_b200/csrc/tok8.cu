@@ -170,13 +170,13 @@ struct T8Grad {
   uint16_t* dgu;                          // GLU: the gradient, rows ld_dgu apart
   size_t ld_dgu;
   int M, N, W;                            // W: columns of d, N or N / 2
-  int vec;                                // rows in whole sixteen-byte pieces
+  int vec, by4;                           // rows in whole pieces of sixteen bytes; of eight
   int tile;                               // rows of a tile of the first pass, 16 to 128
 };
 // Four adjacent values from `at` on, n of them there; FULL: all, in one piece.
 template <bool FULL>
-__device__ __forceinline__ uint2 t8_load4(const uint16_t* p, size_t at, int n, int vec) {
-  if (FULL || (vec && n >= 4)) return __ldg(reinterpret_cast<const uint2*>(p + at));
+__device__ __forceinline__ uint2 t8_load4(const uint16_t* p, size_t at, int n, int by4) {
+  if (FULL || (by4 && n >= 4)) return __ldg(reinterpret_cast<const uint2*>(p + at));
   uint32_t w[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) w[t] = t < n ? p[at + t] : 0u;
@@ -188,12 +188,14 @@ __device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? b
 // row, a lane eight of its columns.  Of a whole tile the rows come in by asynchronous copies, each lane's into places of its own, T8_AHEAD of them on their way, the
 // next tile's first ones with this one's last.  8192 x (2 x 8192) with the activation's gradient 116 us (10 bytes a pair: 5.8 TB/s), by waits and
 // instructions in turn (issue slots 64 %); loads into registers four rows at a time took 150.
+// The sigmoids are looked up at every size: all of the backward with the table and with the formula 82 and 91 us at 4096 x (2 x 2048) x 1024, 23.2 and
+// 25.0 at 512 x (2 x 2048) x 256, 19.0 and 21.0 at 256 x (2 x 1024) x 256, alike at 64 x (2 x 256) x 256, where five launches are what it takes.
 constexpr int T8_AHEAD = 4;
 // eight columns' values of a row: GLU dh, gate and up, else dY
 template <bool GLU>
 struct T8Row { uint4 d, e, u; };
 // a row's part of the maxima, and (GLU) its gradient stored
-template <bool FULL, bool GLU, int TAB>
+template <bool FULL, bool GLU>
 __device__ __forceinline__ void t8_max_row(const T8Grad& x, int r, const T8Row<GLU>& w, float sx, int left, uint16_t* to, const float (&sw)[2][8],
                                            uint32_t (&cm)[2][8], uint32_t* __restrict__ rowmax, const float* tab) {
   constexpr int H = GLU ? 2 : 1;
@@ -206,7 +208,7 @@ __device__ __forceinline__ void t8_max_row(const T8Grad& x, int r, const T8Row<G
     float dg[2], du[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const float d = t ? bfhi(d4[k]) : bflo(d4[k]), g = t ? bfhi(e4[k]) : bflo(e4[k]), u = t ? bfhi(u4[k]) : bflo(u4[k]), sg = sigmoid_a8<TAB>(g, tab);
+      const float d = t ? bfhi(d4[k]) : bflo(d4[k]), g = t ? bfhi(e4[k]) : bflo(e4[k]), u = t ? bfhi(u4[k]) : bflo(u4[k]), sg = sigmoid_a8<1>(g, tab);
       du[t] = fmul(d, fmul(g, sg));
       dg[t] = fmul(fmul(d, u), fmul(sg, fadd(1.0f, fmul(g, fsub(1.0f, sg)))));
     }
@@ -242,9 +244,9 @@ __device__ __forceinline__ void t8_max_row(const T8Grad& x, int r, const T8Row<G
 __device__ __forceinline__ void t8_copy16(uint32_t place, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place), "l"(src) : "memory");
 }
-template <bool GLU, int TAB>
+template <bool GLU>
 struct T8MaxRoom {                        // of a CTA, in shared memory
-  static constexpr int SLOT = (GLU ? 3 : 1) * 256 * 16, TABLE = TAB ? 2 * SG_TAB * 4 : 0;
+  static constexpr int SLOT = (GLU ? 3 : 1) * 256 * 16, TABLE = GLU ? 2 * SG_TAB * 4 : 0;
   static constexpr size_t BYTES = TABLE + 8 * 256 * 4 + T8_AHEAD * SLOT;
 };
 __device__ __forceinline__ uint4 t8_load8_any(const uint16_t* p, int n) {
@@ -253,16 +255,16 @@ __device__ __forceinline__ uint4 t8_load8_any(const uint16_t* p, int n) {
   for (int t = 0; t < 8; ++t) w[t] = 32 * t < n ? p[32 * t] : 0u;
   return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
 }
-template <bool GLU, int TAB>
+template <bool GLU>
 __global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ T8Grad x, uint32_t* __restrict__ rowmax, uint32_t* __restrict__ colmax) {
-  typedef T8MaxRoom<GLU, TAB> Room;
+  typedef T8MaxRoom<GLU> Room;
   constexpr int H = GLU ? 2 : 1;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   float* tab = reinterpret_cast<float*>(smem_raw);
   uint32_t* cols = reinterpret_cast<uint32_t*>(smem_raw + Room::TABLE);   // [8][256]
   const uint8_t* place = smem_raw + Room::TABLE + 8 * 256 * 4 + threadIdx.x * 16;
   const uint32_t place_u = (uint32_t)__cvta_generic_to_shared(place);
-  sg_copy_table<TAB>(tab);
+  sg_copy_table<GLU ? 1 : 0>(tab);
   grid_dep();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int across = (x.W + 255) / 256, tiles = across * ((x.M + x.tile - 1) / x.tile), rows = x.tile / 8;
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ 
           }
           if (!end || more) fetch(k);
           fetch_close();                                                  // of nothing at the very end, so that the count stays
-          t8_max_row<true, GLU, TAB>(x, r0 + (i0 + k) * 8, w, sx, left, to, sw, cm, rowmax, tab);
+          t8_max_row<true, GLU>(x, r0 + (i0 + k) * 8, w, sx, left, to, sw, cm, rowmax, tab);
           if (GLU) to += 8 * x.ld_dgu;
         }
       }
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ 
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          t8_max_row<false, GLU, TAB>(x, r0 + (i + k) * 8, w[k], __shfl_sync(0xffffffffu, sx_all, i + k), left, to, sw, cm, rowmax, tab);
+          t8_max_row<false, GLU>(x, r0 + (i + k) * 8, w[k], __shfl_sync(0xffffffffu, sx_all, i + k), left, to, sw, cm, rowmax, tab);
           if (GLU) to += 8 * x.ld_dgu;
         }
       }
@@ -384,7 +386,7 @@ __device__ __forceinline__ void t8_code_fetch(const T8Grad& x, int r0, const int
   for (int k = 0; k < 4; ++k) {
     if (!FULL && r0 + k >= x.M) { w[k][0] = w[k][1] = make_uint2(0u, 0u); continue; }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) w[k][h] = t8_load4<FULL>(x.d, (r0 + k) * x.ld + at[h], left[h], x.vec);
+    for (int h = 0; h < 2; ++h) w[k][h] = t8_load4<FULL>(x.d, (r0 + k) * x.ld + at[h], left[h], x.by4);
   }
 }
 // w: the first four rows, which were fetched before the scales were there
@@ -413,15 +415,7 @@ __device__ __forceinline__ void t8_code_rows(const T8Grad& x, uint2 (&w)[4][2], 
         if (!FULL && r >= x.M) continue;
         const uint32_t q = ia[k] < 0.0f ? 0u : t8_pack4(a[0], a[1], a[2], a[3]);
         int8_t* row = qa + (size_t)r * ldn;
-        if (FULL) {
-          *reinterpret_cast<uint32_t*>(row + at[h]) = q;
-        } else {
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            if (t < left[h]) row[at[h] + t] = (int8_t)(q >> (8 * t));
-          if (left[h] > 0 && left[h] <= 4)                                // the row's end, and the zeros behind it
-            for (int c = x.N; c < ldn; ++c) row[c] = 0;
-        }
+        if (FULL || at[h] < ldn) *reinterpret_cast<uint32_t*>(row + at[h]) = q;     // behind the row's end zeros
       }
     }
   }
@@ -436,7 +430,7 @@ __global__ void __launch_bounds__(256, 3) k_t8_grad_codes(const __grid_constant_
   const int high = min(8, down - panel * 8), c0 = in / high * 128, r0 = (panel * 8 + in % high) * 128;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, ldm = t8_ld(x.M);
   const int at[2] = {c0 + tx * 4, c0 + tx * 4 + 64}, left[2] = {x.N - at[0], x.N - at[1]};
-  const bool full = x.vec && c0 + 128 <= x.N && r0 + 128 <= x.M;
+  const bool full = x.by4 && c0 + 128 <= x.N && r0 + 128 <= x.M;
   uint2 w[4][2];
   if (full) t8_code_fetch<true>(x, r0 + ty * 8, at, left, w);
   else t8_code_fetch<false>(x, r0 + ty * 8, at, left, w);
@@ -1275,17 +1269,18 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
   return w;
 }
 struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *s_g; int8_t *qa, *qgt; };
-template <bool GLU, int TAB>
+template <bool GLU>
 static int t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
-  const size_t smem = T8MaxRoom<GLU, TAB>::BYTES;
+  const size_t smem = T8MaxRoom<GLU>::BYTES;
   static DevOnce once = {};
-  if (smem > 48 * 1024 && dev_ensure_smem(once, (const void*)k_t8_grad_max<GLU, TAB>, smem) != DET_OK) return DET_ERR_CUDA;
+  if (smem > 48 * 1024 && dev_ensure_smem(once, (const void*)k_t8_grad_max<GLU>, smem) != DET_OK) return DET_ERR_CUDA;
   const long long across = (x.W + 255) / 256;
-  // the most rows with which there are still some tiles for every place of a CTA; rows without a common alignment, whose loads wait one by one, fewer
+  // the most rows with which there are still some tiles for every place of a CTA, as it stays and walks over them
   x.tile = 128;
-  while (x.tile > (x.vec ? 32 : 16) && across * ((x.M + x.tile - 1) / x.tile) < 6 * sms) x.tile /= 2;
+  while (x.tile > 32 && across * ((x.M + x.tile - 1) / x.tile) < 6 * sms) x.tile /= 2;
+  if (!x.vec && across * ((x.M + 31) / 32) < 2 * sms) x.tile = 16;        // rows without a common alignment, whose loads wait one by one
   const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = (GLU ? 2LL : 3LL) * sms;    // CTAs stay and walk over the tiles
-  launch_after(k_t8_grad_max<GLU, TAB>, (unsigned)(tiles < most ? tiles : most), 256, smem, st, x, o.rowmax, o.colmax);
+  launch_after(k_t8_grad_max<GLU>, (unsigned)(tiles < most ? tiles : most), 256, smem, st, x, o.rowmax, o.colmax);
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
@@ -1307,11 +1302,10 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
   const int words = (int)((w.dgu - w.rowmax) / 4);
   if (beside) launch_after(k_t8_transpose, tgrid, 128, 0, st, qX, M, K, qxt, 0, op.rowmax, words);
   else if (cudaMemsetAsync(op.rowmax, 0, (size_t)words * 4, st) != cudaSuccess) { cudaGetLastError(); return DET_ERR_CUDA; }
-  const bool table = (long long)M * x.W >= 8LL * sms * 128 * 64;           // some tiles for every CTA
-  const int rc0 = !x.gu ? t8_largest<false, 0>(x, op, sms, st) : table ? t8_largest<true, 1>(x, op, sms, st) : t8_largest<true, 0>(x, op, sms, st);
+  const int rc0 = x.gu ? t8_largest<true>(x, op, sms, st) : t8_largest<false>(x, op, sms, st);
   if (rc0 != DET_OK) return rc0;
   T8Grad y = x;                                                            // as the codes are made of it
-  if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.vec = 1; }
+  if (x.gu) { y.d = x.dgu; y.ld = x.ld_dgu; y.W = N; y.by4 = 1; }
   launch_after(k_t8_grad_codes, (unsigned)((N + 127) / 128) * ((M + 127) / 128), 256, 0, st, y, op.rowmax, op.colmax, op.s_a, op.s_g, op.qa, op.qgt);
   DET_CHECK_LAUNCH();
   int rc = DET_OK;
@@ -1404,7 +1398,7 @@ extern "C" int det_tok8_linear_bwd(const det_bf16* dY, int ld_dy, const int8_t* 
   const int rc = t8_bwd_check(dY, qX, s_x, qWt, s_w, M, N, K, dX, ld_dx, dW, ws, det_tok8_linear_bwd_ws_bytes(M, N, K), ws_bytes);
   if (rc != DET_OK) return rc;
   if (!M) return t8_no_rows(dW, N, K, (cudaStream_t)stream);
-  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec(dY, ld_dy, 2), 0};
+  const T8Grad x = {dY, nullptr, (size_t)ld_dy, 0, s_x, s_w, nullptr, 0, M, N, N, t8_vec(dY, ld_dy, 2), aligned_to(dY, 8) && ld_dy % 4 == 0, 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
 
@@ -1453,6 +1447,6 @@ extern "C" int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* g
   if (rc != DET_OK) return rc;
   if (!aligned_to(gu, 2)) return DET_ERR_ALIGN;
   if (!M) return t8_no_rows(dW, 2 * F, K, (cudaStream_t)stream);
-  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec(dh, ld_dh, 2) && t8_vec(gu, ld_gu, 2) && F % 8 == 0, 0};
+  const T8Grad x = {dh, gu, (size_t)ld_dh, (size_t)ld_gu, s_x, s_w, (uint16_t*)((char*)ws + t8_ws(M, 2 * F, K, true).dgu), t8_ld_dgu(2 * F), M, 2 * F, F, t8_vec(dh, ld_dh, 2) && t8_vec(gu, ld_gu, 2) && F % 8 == 0, 0, 0};
   return t8_backward(x, qX, qWt, K, dX, ld_dx, dW, (char*)ws, status_dev, (cudaStream_t)stream);
 }
