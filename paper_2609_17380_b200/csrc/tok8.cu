@@ -1278,7 +1278,9 @@ static int t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
   // the most rows with which there are still some tiles for every place of a CTA, as it stays and walks over them
   x.tile = 128;
   while (x.tile > 32 && across * ((x.M + x.tile - 1) / x.tile) < 6 * sms) x.tile /= 2;
-  if (!x.vec && across * ((x.M + 31) / 32) < 2 * sms) x.tile = 16;        // rows without a common alignment, whose loads wait one by one
+  // Rows without a common alignment, whose loads wait one by one: with too few tiles of 32 for the SMs, 16 (all of the backward with 16 and 32, gated block: 64
+  // tiles of 32, 500 x 1003, 22.3 and 23.6 us; 192, 1003 x 1369, 33.9 and 33.6; 756, 2000 x 3001, 97.8 and 94.3; linear: 18.7 and 19.9, 26.6 and 25.8, 47.8 and 46.3).
+  if (!x.vec && across * ((x.M + 31) / 32) < sms) x.tile = 16;
   const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = (GLU ? 2LL : 3LL) * sms;    // CTAs stay and walk over the tiles
   launch_after(k_t8_grad_max<GLU>, (unsigned)(tiles < most ? tiles : most), 256, smem, st, x, o.rowmax, o.colmax);
   DET_CHECK_LAUNCH();
