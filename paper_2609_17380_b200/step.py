@@ -172,8 +172,8 @@ class Replay:
         self.lin = {}
         for l in range(L):
             for w, (N, K) in zip(LINEARS, ((cfg.mixer_width(l), D), (D, D), (2 * Fh, D), (D, Fh))):
-                ld, ld_t = (det.det_tok8_ld(K), det.det_tok8_ld(N)) if self.by_token else (K, N)
-                self.lin[(l, w)] = dict(name="l%d.%s" % (l, w), N=N, K=K, s_w=z(N, F32), qW=z(N * ld, I8), qWt=z(K * ld_t, I8), s_u=z(1, F32))
+                self.lin[(l, w)] = dict(name="l%d.%s" % (l, w), N=N, K=K, s_w=z(N, F32), qW=z(N * self._code_ld(K), I8), qWt=z(K * self._code_ld(N), I8),
+                                        s_u=z(1, F32))
         e = lambda n, dt: torch.empty(n, dtype=dt, device=device)
         QW, Hkv = cfg.qkv_width, cfg.kv_heads
         self.head_ops = cfg.qk_norm or cfg.rope_tables is not None
@@ -190,7 +190,7 @@ class Replay:
         self.tmp = [e(T * wide, I16) for _ in range(3)]              # gradient scratch activations
         # what the layers share where their own copies are in 8 bits: the residual stream at either norm, the inputs of SwiGLU and of the
         # recurrence, the down projection's input, which the backward pass makes again
-        self.shared = dict(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * Fh, I8),
+        self.shared = dict(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * self._code_ld(Fh), I8),
                            gv=e(T * 2 * D if cfg.recurrent else 0, I16)) if cfg.act8 else None
         self.tok = e(T, I32)
         self.lab = e(T, I32)
@@ -218,20 +218,25 @@ class Replay:
         self.prof = None
         self.fuse_quant = True       # producers write the linears' int8 inputs (False: separate quantiser pass per linear)
 
+    def _code_ld(self, width):
+        """Bytes from a row of codes to the next, of activations and weights alike: with scales by token the rows are padded."""
+        return det.det_tok8_ld(width) if self.by_token else width
+
     def _activations(self, l, e):
         """What layer l keeps from its forward pass for its backward pass."""
         cfg = self.cfg
         D, Fh, T, QW, Hkv = cfg.d_model, cfg.ffn, cfg.tokens_per_microbatch, cfg.mixer_width(l), cfg.kv_heads
         rec, stat, tok = l in cfg.recurrent, T if self.layer_norm else 0, T if self.by_token else 0
-        a = dict(sx_qkv=e(tok, F32), sx_o=e(tok, F32), sx_gu=e(tok, F32), sx_down=e(tok, F32), rstd1=e(T, F32), mean1=e(stat, F32), n1=e(T * D, I16), qx_qkv=e(T * D, I8), att=e(T * D, I16), qx_o=e(T * D, I8), rstd2=e(T, F32),
-                 mean2=e(stat, F32), n2=e(T * D, I16), qx_gu=e(T * D, I8))
+        codes = T * self._code_ld(D)
+        a = dict(sx_qkv=e(tok, F32), sx_o=e(tok, F32), sx_gu=e(tok, F32), sx_down=e(tok, F32), rstd1=e(T, F32), mean1=e(stat, F32), n1=e(T * D, I16),
+                 qx_qkv=e(codes, I8), att=e(T * D, I16), qx_o=e(codes, I8), rstd2=e(T, F32), mean2=e(stat, F32), n2=e(T * D, I16), qx_gu=e(codes, I8))
         if rec:
             a.update(states=e(det.det_linrec_state_floats(cfg.micro_batch, cfg.seq, D), F32))
         else:
             a.update(qkv=e(T * QW, I16), qkr=e(T * QW if self.head_ops else 0, I16), lse=e(T * cfg.n_heads, F32),
                      rstd_qk=e(T * (cfg.n_heads + Hkv) if cfg.qk_norm else 0, F32))
         if not cfg.act8:
-            a.update(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * Fh, I8))
+            a.update(x=e(T * D, I16), h=e(T * D, I16), gu=e(T * 2 * Fh, I16), a=e(T * Fh, I16), qx_down=e(T * self._code_ld(Fh), I8))
             return dict(a, gv=e(T * QW, I16)) if rec else a
         for name, width in (("x", D), ("h", D), ("gu", 2 * Fh)) + ((("gv", 2 * D),) if rec else ()):
             a[name + "8"], a[name + "_e"] = e(T * width, I8), e(det.det_act8_exp_bytes(T, width), torch.uint8)
