@@ -345,7 +345,8 @@ int det_attn_bwd_fixq(const det_bf16* dout, const det_bf16* q, const det_bf16* k
                       det_bf16* dk, det_bf16* dv, int ld_d, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- elementwise glue (Sec. 3.1: SwiGLU with fused gate/up projection, pre-norm residuals, embedding) */
-/* gu bf16 [rows, 2F] (gate | up), h bf16 [rows, F] = silu(gate) * up;  F % 8 == 0 */
+/* gu bf16 [rows, 2F] (gate | up), h bf16 [rows, F] = silu(gate) * up;  F % 8 == 0 but for det_swiglu_fwd, which takes any F (pointers
+ * aligned to the element where F % 8 != 0) */
 int det_swiglu_fwd(const det_bf16* gu, int rows, int F, det_bf16* h, void* stream);
 /* det_swiglu_fwd that also writes the down projection's int8 input qh [rows, F] (see det_linear_fwd_q) */
 int det_swiglu_fwd_q(const det_bf16* gu, int rows, int F, det_bf16* h, const float* s_q, int8_t* qh, void* stream);

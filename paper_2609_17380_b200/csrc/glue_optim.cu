@@ -42,6 +42,16 @@ __global__ void __launch_bounds__(256) k_swiglu_fwd(const uint16_t* __restrict__
   }
 }
 
+// Rows of any width and address: a value a thread, adjacent ones in adjacent threads.
+__global__ void __launch_bounds__(256) k_swiglu_fwd_any(const uint16_t* __restrict__ gu, size_t n, int F, uint16_t* __restrict__ h) {
+  grid_dep();
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const size_t at = i + i / F * F;
+  const float g = bf2f(gu[at]);
+  h[i] = f2bf(fmul(fmul(g, sigmoid_det(g)), bf2f(gu[at + F])));
+}
+
 __global__ void __launch_bounds__(256) k_swiglu_bwd(const uint16_t* __restrict__ dh, const uint16_t* __restrict__ gu,
                                                     int rows, int F, uint16_t* __restrict__ dgu) {
   grid_dep();
@@ -301,10 +311,15 @@ using namespace det;
 
 extern "C" int det_swiglu_fwd(const det_bf16* gu, int rows, int F, det_bf16* h, void* stream) {
   if (!gu || !h || rows < 0 || F <= 0) return DET_ERR_ARG;
-  if (F % 8) return DET_ERR_SHAPE;
-  if (!aligned16(gu) || !aligned16(h)) return DET_ERR_ALIGN;
-  size_t n = (size_t)rows * (F / 8);
+  if (F % 8 ? ((uintptr_t)gu | (uintptr_t)h) & 1u : !aligned16(gu) || !aligned16(h)) return DET_ERR_ALIGN;
+  size_t n = F % 8 ? (size_t)rows * F : (size_t)rows * (F / 8);
   if (!n) return DET_OK;
+  if (F % 8) {
+    if ((n + 255) / 256 > 0x7fffffffu) return DET_ERR_SHAPE;
+    launch_after(k_swiglu_fwd_any, (unsigned)((n + 255) / 256), 256, 0, (cudaStream_t)stream, gu, n, F, h);
+    DET_CHECK_LAUNCH();
+    return DET_OK;
+  }
   launch_after(k_swiglu_fwd, (unsigned)((n + 255) / 256), 256, 0, (cudaStream_t)stream, gu, rows, F, h, nullptr, nullptr);
   DET_CHECK_LAUNCH();
   return DET_OK;

@@ -593,14 +593,19 @@ class Replay:
             d_a = t0[:T * Fh]
             act, qx_down = own(a, "a"), own(a, "qx_down")
             if cfg.act8 and self.by_token:
-                det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act)
+                if Fh % 32 == 0:
+                    det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act)
+                else:                                                      # a group of the checkpoint lies across gates and ups
+                    gu = own(a, "gu")
+                    det.det_act8_unpack(det.DET_BF16, *kept(a, "gu"), T, 2 * Fh, gu, 2 * Fh)
+                    det.det_swiglu_fwd(gu, T, Fh, act)
                 det.det_tok8_quant(act, Fh, T, Fh, qx_down, a["sx_down"])
             elif cfg.act8:
                 det.det_swiglu_act8(*kept(a, "gu"), T, Fh, act, views["sx"][l, 3], qx_down)
             self._linear_bwd(l, "w_down", 3, dx, act, qx_down, T, d_a)
             if self.by_token:
                 d, gu, d_n2 = self.lin[(l, "w_gu")], own(a, "gu"), t2[:T * D]
-                if cfg.act8:
+                if cfg.act8 and Fh % 32 == 0:                              # else it is there already
                     det.det_act8_unpack(det.DET_BF16, *kept(a, "gu"), T, 2 * Fh, gu, 2 * Fh)
                 with self.span("linear_bwd"):
                     det.det_tok8_glu_bwd(d_a, Fh, gu, 2 * Fh, a["qx_gu"], a["sx_gu"], d["qWt"], d["s_w"], T, Fh, D, d_n2, D, G[d["name"]], self.ws, self.status)
