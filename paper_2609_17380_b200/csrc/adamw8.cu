@@ -44,7 +44,11 @@ __device__ __forceinline__ float a8_root(int c, float s) {
 }
 // fsqrt and fdiv; a zero, which sends a whole warp through the compiler's path for special operands, is answered beside them.  A value in fifty that is
 // zero (weights that have had no gradient) is in every second warp.
-__device__ __forceinline__ float a8_sqrt(float x) { return x > 0.0f ? fsqrt(x > 0.0f ? x : 1.0f) : fmul(x, x); }         // x is never negative, but may be a NaN
+__device__ __forceinline__ float a8_sqrt(float x) {
+  const bool zero = x == 0.0f;
+  const float r = fsqrt(zero ? 1.0f : x);                                 // of a negative v, which 32 bits may hold, a NaN
+  return zero ? x : r;
+}
 __device__ __forceinline__ float a8_div(float a, float b) {
   const bool plain = a == 0.0f && b > 0.0f;                               // 0 / b is that zero
   const float q = fdiv(plain ? 1.0f : a, plain ? 1.0f : b);
