@@ -305,6 +305,10 @@ __global__ void __launch_bounds__(256) k_adamw8(const __grid_constant__ Adam8Job
   }
 }
 
+// A moment as the definition takes it: subnormals and either zero are +0.  On the bits, as the scale of a block is taken from the bits too (a product with 1
+// or a sum with 0 is what a compiler may leave out).
+__device__ __forceinline__ float a8_flushed(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x00800000u ? 0.0f : x; }
+
 // Codes to numbers and back, many tensors at once.
 template <int CAP>
 struct Adam8Numbers {
@@ -332,8 +336,8 @@ __device__ __forceinline__ void adam8_numbers(const Adam8Numbers<CAP>& jobs, int
     float near[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      m[k] = fmul(m[k], 1.0f);                                            // a subnormal number counts as zero
-      v[k] = fadd(v[k], 0.0f);                                            // and -0 as +0
+      m[k] = a8_flushed(m[k]);
+      v[k] = a8_flushed(v[k]);
       near[k] = a8_sqrt_near(v[k]);
     }
     a8_put<FULL>(m, v, near, lane, i0, n, jobs.m8[j], jobs.v8[j], s);
