@@ -279,7 +279,7 @@ class Replay:
         return self._fresh()["sx" if name.endswith("s_x") else "pbf"][name]
 
     def g(self, buf, name):
-        for which in ("gmb", "gout", "m", "v"):
+        for which in ("gmb", "gout", "m", "v", "m8", "v8", "ms"):
             if buf is getattr(self, which):
                 return self._fresh()[which][name]
         return buf[self.goff[name]:self.goff[name] + _numel(self.shape[name])]

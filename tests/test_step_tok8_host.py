@@ -29,3 +29,21 @@ def test_rows_of_codes_have_room(ffn, act8):
 def test_rows_of_codes_with_a_learned_step_are_not_padded():
     r = dstep.Replay(dstep.ModelConfig(**BLOCK, ffn=384), device="cpu")
     assert [r.act[0][n].numel() for n in ("qx_qkv", "qx_o", "qx_gu", "qx_down")] == [128 * 256] * 3 + [128 * 384]
+
+
+def test_parts_of_the_state_by_name():
+    """Codes, scales and moments of a parameter lie where the update takes them from, whatever buffer they are asked of; together they are the whole buffers."""
+    r = dstep.Replay(dstep.ModelConfig(**BLOCK, ffn=100, linear="token", state8=True), device="cpu")
+    for buf, matrices in ((r.m8, True), (r.v8, True), (r.ms, True), (r.m, False), (r.v, False)):
+        at = 0
+        for name, shape, _ in r.specs:
+            n = shape[0] * (shape[1] if len(shape) > 1 else 1)
+            if (len(shape) > 1) != matrices:
+                with pytest.raises(KeyError):
+                    r.g(buf, name)
+                continue
+            n = det.det_adamw8_scale_floats(n) if buf is r.ms else n
+            part = r.g(buf, name)
+            assert part.numel() == n and part.data_ptr() == buf.data_ptr() + at * buf.element_size(), name
+            at += n
+        assert at == buf.numel()
