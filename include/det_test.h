@@ -52,6 +52,12 @@ int det_test_attn_rows(int heads, int S, int window);
  * all CTAs, seen[1] of the one with the most, seen[2] and seen[3] the lowest and the highest row that a pass starts at. */
 int det_test_layernorm_walk(int io, int rows, int D, int sms, long long seen[4]);
 
+/* How a product of the 8-bit linears [I, K] x [J, K] is cut on a GPU of `sms` SMs: plan[0] the tile (0: 256 x 256 by two CTAs, 1: 128 columns, 2: 64), plan[1]
+ * CTAs that share a tile of 64 columns (1: the tile of plan[0]).  epi: output bf16 (0), f32 (1), the gated block's (2, J its columns). */
+int det_test_tok8_plan(int epi, int I, int J, int K, int sms, int plan[2]);
+/* Rows of a tile in the backward passes' search for the largest magnitudes of a gradient [M, W] (gated block: of dh); vec: rows in whole sixteen-byte pieces. */
+int det_test_tok8_tile_rows(int M, int W, int vec, int sms);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@
 #include "internal.h"
 #include "rows.cuh"
 #include "sigmoid.cuh"
+#include "../../include/det_test.h"
 
 namespace det {
 
@@ -1269,18 +1270,22 @@ static T8Ws t8_ws(int M, int N, int K, bool glu) {
   return w;
 }
 struct T8Operands { uint32_t *rowmax, *colmax; float *s_a, *s_g; int8_t *qa, *qgt; };
+// Rows of a tile of the pass over the largest magnitudes: the most with which there are still some tiles for every place of a CTA, as it stays and walks over
+// them.  Rows without a common alignment, whose loads wait one by one: with too few tiles of 32 for the SMs, 16 (all of the backward with 16 and 32, gated block: 64
+// tiles of 32, 500 x 1003, 22.3 and 23.6 us; 192, 1003 x 1369, 33.9 and 33.6; 756, 2000 x 3001, 97.8 and 94.3; linear: 18.7 and 19.9, 26.6 and 25.8, 47.8 and 46.3).
+static int t8_tile_rows(int M, int W, int vec, int sms) {
+  const long long across = (W + 255) / 256;
+  int tile = 128;
+  while (tile > 32 && across * ((M + tile - 1) / tile) < 6 * sms) tile /= 2;
+  return !vec && across * ((M + 31) / 32) < sms ? 16 : tile;
+}
 template <bool GLU>
 static int t8_largest(T8Grad x, const T8Operands& o, int sms, cudaStream_t st) {
   const size_t smem = T8MaxRoom<GLU>::BYTES;
   static DevOnce once = {};
   if (smem > 48 * 1024 && dev_ensure_smem(once, (const void*)k_t8_grad_max<GLU>, smem) != DET_OK) return DET_ERR_CUDA;
   const long long across = (x.W + 255) / 256;
-  // the most rows with which there are still some tiles for every place of a CTA, as it stays and walks over them
-  x.tile = 128;
-  while (x.tile > 32 && across * ((x.M + x.tile - 1) / x.tile) < 6 * sms) x.tile /= 2;
-  // Rows without a common alignment, whose loads wait one by one: with too few tiles of 32 for the SMs, 16 (all of the backward with 16 and 32, gated block: 64
-  // tiles of 32, 500 x 1003, 22.3 and 23.6 us; 192, 1003 x 1369, 33.9 and 33.6; 756, 2000 x 3001, 97.8 and 94.3; linear: 18.7 and 19.9, 26.6 and 25.8, 47.8 and 46.3).
-  if (!x.vec && across * ((x.M + 31) / 32) < sms) x.tile = 16;
+  x.tile = t8_tile_rows(x.M, x.W, x.vec, sms);
   const long long tiles = across * ((x.M + x.tile - 1) / x.tile), most = (GLU ? 2LL : 3LL) * sms;    // CTAs stay and walk over the tiles
   launch_after(k_t8_grad_max<GLU>, (unsigned)(tiles < most ? tiles : most), 256, smem, st, x, o.rowmax, o.colmax);
   DET_CHECK_LAUNCH();
@@ -1323,6 +1328,17 @@ static int t8_backward(const T8Grad& x, const int8_t* qX, const int8_t* qWt, int
 }  // namespace det
 
 using namespace det;
+
+extern "C" int det_test_tok8_plan(int epi, int I, int J, int K, int sms, int plan[2]) {
+  if (epi < 0 || epi > 2 || I <= 0 || J <= 0 || K <= 0 || sms < 2 || !plan) return DET_ERR_ARG;
+  T8Out o = {};
+  o.I = I; o.J = J; o.K = K;
+  const T8Plan p = t8_plan(epi, o, sms);
+  plan[0] = p.pick;
+  plan[1] = p.parts;
+  return DET_OK;
+}
+extern "C" int det_test_tok8_tile_rows(int M, int W, int vec, int sms) { return M > 0 && W > 0 && sms > 0 ? t8_tile_rows(M, W, vec, sms) : DET_ERR_ARG; }
 
 extern "C" int det_tok8_ld(int K) { return K > 0 && K < (1 << 30) ? t8_ld(K) : 0; }
 
