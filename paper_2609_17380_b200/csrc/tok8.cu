@@ -36,11 +36,6 @@ __device__ __forceinline__ uint2 t8_codes8(const float v[8], float inv, bool dea
   for (int t = 0; t < 8; ++t) c[t] = t8_code(v[t], inv);
   return dead ? make_uint2(0u, 0u) : make_uint2(t8_pack4(c[0], c[1], c[2], c[3]), t8_pack4(c[4], c[5], c[6], c[7]));
 }
-__device__ __forceinline__ uint32_t t8_max8(const float v[8], uint32_t m) {
-#pragma unroll
-  for (int t = 0; t < 8; ++t) m = max(m, __float_as_uint(v[t]) & 0x7fffffffu);
-  return m;
-}
 
 // Rows of a multiple of 8 columns, 16-byte aligned: WPR warps a row, up to 64 values a lane, which stay in registers as they came, so that a row is read
 // once.  Bound by memory: 8192 x 2048 10 us, 0.8 of the copy's rate, 8192 x 8192 37 us.
