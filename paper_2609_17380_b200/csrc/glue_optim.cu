@@ -42,7 +42,8 @@ __global__ void __launch_bounds__(256) k_swiglu_fwd(const uint16_t* __restrict__
   }
 }
 
-// Rows of any width and address: a value a thread, adjacent ones in adjacent threads.
+// Rows of any width and address: a value a thread, adjacent ones in adjacent threads.  8192 x 1001 40 us, where 1000 columns take 16 (bound by its instructions,
+// a quotient of 64 bits among them): for widths that only a step with scales by token and activations in 8 bits has.
 __global__ void __launch_bounds__(256) k_swiglu_fwd_any(const uint16_t* __restrict__ gu, size_t n, int F, uint16_t* __restrict__ h) {
   grid_dep();
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) k_t8_rows(const uint16_t* __restrict__ x,
   }
 }
 // Any width, stride and address: a CTA a row, an element a thread at a time, up to 2048 of them kept in registers (LONG: read twice); 1531 x 1003 4 us, where a
-// warp a row took 6.8.
+// warp a row took 6.8; 8192 x 2041 16 us and 8192 x 8191 52, where k_t8_rows takes 8 for 2048 columns and 30 for 8192.
 template <bool LONG>
 __global__ void __launch_bounds__(256) k_t8_rows_any(const uint16_t* __restrict__ x, size_t ld, int K, int8_t* __restrict__ q, float* __restrict__ s) {
   grid_dep();
@@ -182,8 +182,8 @@ __device__ __forceinline__ float t8_at(const uint2& v, int t) { return t & 1 ? b
 
 // Largest magnitudes first.  A tile is up to 128 rows of 256 columns (GLU: of either half); a warp has every eighth
 // row, a lane eight of its columns.  Of a whole tile the rows come in by asynchronous copies, each lane's into places of its own, T8_AHEAD of them on their way, the
-// next tile's first ones with this one's last.  8192 x (2 x 8192) with the activation's gradient 116 us (10 bytes a pair: 5.8 TB/s), by waits and
-// instructions in turn (issue slots 64 %); loads into registers four rows at a time took 150.
+// next tile's first ones with this one's last.  8192 x (2 x 8192) with the activation's gradient 118 us (10 bytes a pair: 5.7 TB/s; 129 in a
+// long run), by waits and instructions in turn (issue slots 54 % at 2048 rows); loads into registers four rows at a time took 150.
 // The sigmoids are looked up at every size: all of the backward with the table and with the formula 82 and 91 us at 4096 x (2 x 2048) x 1024, 23.2 and
 // 25.0 at 512 x (2 x 2048) x 256, 19.0 and 21.0 at 256 x (2 x 1024) x 256, alike at 64 x (2 x 256) x 256, where five launches are what it takes.
 constexpr int T8_AHEAD = 4;
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(256, 2) k_t8_grad_max(const __grid_constant__ 
 // Then the codes: A as it lies, G transposed.  A tile is 128 rows of 128 columns, in two halves of 64; a thread has 8 rows of 4
 // columns of each, four rows on their way together.  A CTA works out the scales and inverses of its rows and columns once, a thread each.  Eight codes of a
 // column are a piece of 8 bytes, whose place in its row of the transposed tile is swizzled by the columns' four, so that a warp's pieces meet in no bank.
-// 8192 x 16384 113 us (4 bytes a value: 4.7 TB/s), issue slots 58 %; thread by thread the scales alone were a fifth of the instructions (484 us).
+// 8192 x 16384 111 us (4 bytes a value: 4.8 TB/s; 121 in a long run), issue slots 61 % at 2048 rows; thread by thread the scales alone were a fifth of the instructions (484 us).
 struct T8CodeRoom {
   uint8_t out[128 * 128];
   float sx[128], ia[128], sw[128], ig[128];                               // an inverse of -1: the scale is a NaN, the codes are 0
@@ -609,9 +609,10 @@ __device__ __forceinline__ void t8_epilogue(const T8Out& o, const T8Scales<EPI, 
 }
 
 // Tiles of 128 x BN by one CTA, or of 256 x 256 by the two of a cluster (PAIR; each has 128 rows and stages half of the columns' operand).  The
-// columns of a GLU tile are BN / 2 gates and the ups that belong to them.  Roles, ring and waits as in igemm.cu.  8192 x 6144 x 2048 78 us (2.6 POP/s),
-// 8192 x 2048 x 8192 94, the gated block 8192 x (2 x 8192) x 2048 with three outputs 235 (2.3): the tensor pipe is 67 % and 58 % active in a launch of its
-// own at 1.7 GHz, and a run of them is held by the power limit.
+// columns of a GLU tile are BN / 2 gates and the ups that belong to them.  Roles, ring and waits as in igemm.cu.  8192 x 6144 x 2048 75 us
+// (2.8 POP/s) in a short run and 86 in a long one, 8192 x 8192 x 2048 99 and 113, 8192 x 2048 x 16384 180 and 206, the gated block 8192 x (2 x 8192) x 2048 with
+// three outputs 224 (2.5) and 253: a long run draws 985 W, the power limit, and the clock falls from 1965 MHz to 1500 to 1650.  In a launch of its own over 2048
+// rows the tensor pipe is 65 % active, 76 % with a contraction of 16384 and 57 % in the gated block: few rounds of tiles, the last one part full.
 template <bool PAIR, int BN, int EPI>
 struct T8Tile {
   static constexpr int BM = PAIR ? 256 : 128, BROWS = PAIR ? BN / 2 : BN;         // BROWS: rows of the columns' operand that a CTA stages
@@ -1182,9 +1183,11 @@ static int t8_split(const int8_t* A, const int8_t* B, int rows_b, const T8Out& o
 
 // The tile by whole rounds of tiles over the SMs, each the longer of its multiply loop and its epilogue, once the other of the two and what a launch takes
 // (microseconds; steps and turns of igemm.cu).  Tiles that the CTAs of a cluster share: as many CTAs as the SMs have room for, at least two steps of the
-// contraction for each; their exchange takes longer the more rows there are.  Measured over 32 shapes, the rule within 14 % of the best of all: 24 x 2048 x 8192
-// with 8 CTAs to a tile 8.7, alone 23.9; 128 x 2048 x 8192 with 4 12.4, alone 24.3; 256 x 2048 x 2048 with 2 11.6, alone 8.9 (64 columns), 9.5 (128), 12.0 (pair);
-// 2738 x 520 x 1003 9.4, 7.6, 10.2; 8192 x 2048 x 2048 78, 43, 30.
+// contraction for each; their exchange takes longer the more rows there are.  Measured with every tile and number of CTAs
+// over 52 shapes, 18 of them weights' gradients: the rule takes at most 1.05 of the best time but for 24 x 2048 x 2048 (1.14: eight CTAs to a tile where four are
+// best), the gated 30 x 1000 x 4000 (1.13, likewise) and the gradient 2048 x 2048 x 512 (1.10: the pair where 128 columns are best).  24 x 2048 x 8192 with 8
+// CTAs to a tile 8.5, alone 21.1; 128 x 2048 x 8192 with 4 12.2, alone 21.4; 256 x 2048 x 2048 with 2 11.3, alone 7.7 (64 columns), 8.4 (128), 10.8 (pair);
+// 2738 x 520 x 1003 8.5, 6.9, 8.7; 8192 x 2048 x 2048 70, 38, 29; gradients 520 x 264 x 1030 5.7, 7.2, 9.3 and 2048 x 8192 x 8192 274, 136, 97.
 struct T8Plan { int pick, parts; long long ctas; };      // pick: pair, 128 or 64 columns; parts > 1: CTAs to a tile
 static T8Plan t8_plan(int epi, const T8Out& o, int sms) {
   static const struct { int bn, bi; double step, turn, epi[3]; } C[3] = {
