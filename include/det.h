@@ -174,7 +174,7 @@ int det_rmsnorm_bwd_residual(const det_bf16* dy, const det_bf16* x, const det_bf
  *   det_tok8_quant: qX, s_x [M] of the rows of X; of a weight [N, K] those are its channels (the forward pass wants qW, s_w [N]).
  *   det_tok8_transpose: codes [M, K] -> [K, M] (the backward pass wants the weight's, qWt [K, det_tok8_ld(N)]); at most 65535 * 128 rows.
  * Any M >= 0 (up to 2^28), any N, K >= 1; bf16 matrices have rows ld elements apart (ld >= the width), any alignment to the element; scales f32.  Whole
- * rows in 16-byte pieces are faster.  K < 2^17 (DET_ERR_RANGE), in the backward pass M and N too.  M = 0: no rows, and a dW of zeros.
+ * rows in 16-byte pieces are faster.  K < 2^17 (DET_ERR_RANGE), in the backward pass M and N too.  M = 0: no rows (what has one for every token may be NULL), and a dW of zeros.
  * Outputs overlap no input.  Two tokens' results never depend on each other; nor does a token's on how many there are.  status_dev (may be NULL) receives
  * DET_DEV_TIMEOUT if a bounded wait of the tensor-core kernels expires; the outputs of that call are undefined then. */
 int det_tok8_ld(int K);

@@ -1341,14 +1341,14 @@ extern "C" int det_test_tok8_tile_rows(int M, int W, int vec, int sms) { return 
 extern "C" int det_tok8_ld(int K) { return K > 0 && K < (1 << 30) ? t8_ld(K) : 0; }
 
 extern "C" int det_tok8_quant(const det_bf16* X, int ld, int M, int K, int8_t* qX, float* s_x, void* stream) {
-  if (!X || !qX || !s_x || ld < K) return DET_ERR_ARG;
+  if ((M && (!X || !qX || !s_x)) || ld < K) return DET_ERR_ARG;
   const int rc = t8_sizes(M, 1, K);
   if (rc != DET_OK) return rc;
   if (!aligned_to(X, 2) || !aligned16(qX) || !aligned_to(s_x, 4)) return DET_ERR_ALIGN;
   return M ? t8_quant(X, ld, M, K, qX, s_x, (cudaStream_t)stream) : DET_OK;
 }
 extern "C" int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, void* stream) {
-  if (!q || !qT) return DET_ERR_ARG;
+  if (M && (!q || !qT)) return DET_ERR_ARG;
   const int rc = t8_sizes(M, 1, K);
   if (rc != DET_OK) return rc;
   if ((M + 127) / 128 > 65535) return DET_ERR_SHAPE;
@@ -1359,8 +1359,9 @@ extern "C" int det_tok8_transpose(const int8_t* q, int M, int K, int8_t* qT, voi
   return DET_OK;
 }
 
+// what has a row for every token may be NULL where there are none, as an empty tensor's address is
 static int t8_fwd_check(const void* q, const float* s_x, const int8_t* qW, const float* s_w, int M, int N, int K, const void* Y, int ld_y) {
-  if (!q || !s_x || !qW || !s_w || !Y || ld_y < N) return DET_ERR_ARG;
+  if ((M && (!q || !s_x || !Y)) || !qW || !s_w || ld_y < N) return DET_ERR_ARG;
   const int rc = t8_sizes(M, N, K);
   if (rc != DET_OK) return rc;
   if (!aligned16(q) || !aligned16(qW) || !aligned_to(s_x, 4) || !aligned_to(s_w, 4) || !aligned_to(Y, 2)) return DET_ERR_ALIGN;
@@ -1378,7 +1379,7 @@ extern "C" int det_tok8_linear_fwd_q(const int8_t* qX, const float* s_x, const i
 }
 extern "C" int det_tok8_linear_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int N, int K, det_bf16* Y, int ld_y, int8_t* qX,
                                    float* s_x, void* stream, int* status_dev) {
-  if (!X || ld < K) return DET_ERR_ARG;
+  if ((M && !X) || ld < K) return DET_ERR_ARG;
   int rc = t8_fwd_check(qX, s_x, qW, s_w, M, N, K, Y, ld_y);
   if (rc != DET_OK) return rc;
   if (!aligned_to(X, 2)) return DET_ERR_ALIGN;
@@ -1395,7 +1396,7 @@ extern "C" int det_tok8_linear_fwd(const det_bf16* X, int ld, const int8_t* qW, 
 extern "C" size_t det_tok8_linear_bwd_ws_bytes(int M, int N, int K) { return M > 0 && N > 0 && K > 0 ? t8_ws(M, N, K, false).bytes : 0; }
 static int t8_bwd_check(const void* d, const int8_t* qX, const float* s_x, const int8_t* qWt, const float* s_w, int M, int N, int K, const void* dX, int ld_dx,
                         const float* dW, const void* ws, size_t need, size_t ws_bytes) {
-  if (!d || !qX || !s_x || !qWt || !s_w || (!dX && !dW) || (dX && ld_dx < K)) return DET_ERR_ARG;
+  if ((M && (!d || !qX || !s_x || (!dX && !dW))) || !qWt || !s_w || (dX && ld_dx < K)) return DET_ERR_ARG;
   int rc = t8_sizes(M, N, K);
   if (rc != DET_OK) return rc;
   if (M >= (1 << 17) || N >= (1 << 17)) return DET_ERR_RANGE;          // contracted over as well
@@ -1435,7 +1436,7 @@ extern "C" int det_tok8_glu_fwd_q(const int8_t* qX, const float* s_x, const int8
 }
 extern "C" int det_tok8_glu_fwd(const det_bf16* X, int ld, const int8_t* qW, const float* s_w, int M, int F, int K, det_bf16* h, int ld_h, det_bf16* gu,
                                 int ld_gu, int8_t* qX, float* s_x, void* stream, int* status_dev) {
-  if (!X || ld < K) return DET_ERR_ARG;
+  if ((M && !X) || ld < K) return DET_ERR_ARG;
   if (F > (1 << 27)) return DET_ERR_SHAPE;
   int rc = t8_fwd_check(qX, s_x, qW, s_w, M, F, K, h, ld_h);
   if (rc != DET_OK) return rc;
@@ -1458,7 +1459,7 @@ extern "C" int det_tok8_glu_bwd(const det_bf16* dh, int ld_dh, const det_bf16* g
                                 const float* s_w, int M, int F, int K, det_bf16* dX, int ld_dx, float* dW, void* ws, size_t ws_bytes, void* stream,
                                 int* status_dev) {
   if (F > (1 << 27)) return DET_ERR_SHAPE;
-  if (!gu || ld_dh < F || ld_gu < 2 * F) return DET_ERR_ARG;
+  if ((M && !gu) || ld_dh < F || ld_gu < 2 * F) return DET_ERR_ARG;
   const int rc = t8_bwd_check(dh, qX, s_x, qWt, s_w, M, 2 * F, K, dX, ld_dx, dW, ws, det_tok8_glu_bwd_ws_bytes(M, F, K), ws_bytes);
   if (rc != DET_OK) return rc;
   if (!aligned_to(gu, 2)) return DET_ERR_ALIGN;
