@@ -17,7 +17,6 @@ constexpr int A8_VALUES = 256;            // values that share scales: a warp's,
 constexpr int ADAM8_JOBS = 128, ADAM8_FEW = 16;     // tensors per launch; a launch of few has a shorter table to hand over
 constexpr float A8_127 = 0x1.020408p-7f, A8_255 = 0x1.010102p-8f;     // 1/127, 1/255
 
-struct Adam8Scalars { float b1, b2, omb1, omb2, eps, stepsz, isb2, decay; };
 // Job j: CTAs first[j] .. first[j + 1] - 1 of the launch, each with `rounds` times 2048 of its len[j] values, 256 a warp and round.  A job belongs to whole
 // CTAs, and its entries, constants at an index, are read once for all rounds.  s NULL: moments in 32 bits.
 template <int CAP>
@@ -30,7 +29,7 @@ struct Adam8Jobs {
   void *po[CAP], *mo[CAP], *vo[CAP];
   float* so[CAP];
   size_t len[CAP];
-  Adam8Scalars h[CAP];
+  AdamScalars h[CAP];
   uint8_t bf[CAP];
 };
 
@@ -59,9 +58,6 @@ __device__ __forceinline__ float a8_scale(uint32_t amax) { return amax >= 0x7f80
 __device__ __forceinline__ float a8_inverse(float s) { return s > 0.0f ? fdiv(1.0f, s) : 0.0f; }
 // a share of at most 1 (1 + 2^-23), so the code needs no clamp
 __device__ __forceinline__ int a8_code(float x, float inv, float top) { return __float2int_rn(fmul(a8_sqrt(fmul(x, inv)), top)); }
-__device__ __forceinline__ uint32_t t4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {      // four low bytes
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
-}
 
 // Four adjacent values from i on, `n` of them there; FULL: all four, in the block of a tensor that has all its 256.
 template <bool FULL, bool BF>
@@ -165,13 +161,13 @@ __device__ __forceinline__ void a8_put(const float (&m)[8], const float (&v)[8],
         b[k] = (uint32_t)max(a8_code(a8_sqrt(vv), ir, 255.0f), vv > 0.0f ? 1 : 0);
       }
     }
-    a8_store_codes<FULL>(m8, i0 + 128 * h, n[h], t4(a[0], a[1], a[2], a[3]) & fm);
-    a8_store_codes<FULL>(v8, i0 + 128 * h, n[h], t4(b[0], b[1], b[2], b[3]) & fr);
+    a8_store_codes<FULL>(m8, i0 + 128 * h, n[h], low_bytes(a[0], a[1], a[2], a[3]) & fm);
+    a8_store_codes<FULL>(v8, i0 + 128 * h, n[h], low_bytes(b[0], b[1], b[2], b[3]) & fr);
   }
 }
 
 // p moved by the moments, exactly as det_adamw_step
-__device__ __forceinline__ float a8_moved(const Adam8Scalars& h, float p, float m, float root) {
+__device__ __forceinline__ float a8_moved(const AdamScalars& h, float p, float m, float root) {
   return fsub(fmul(p, h.decay), fmul(h.stepsz, a8_div(m, fadd(fmul(root, h.isb2), h.eps))));
 }
 // A job's entries
@@ -182,12 +178,12 @@ struct Adam8Job {
   void *po, *mo, *vo;
   float* so;
   size_t len;
-  Adam8Scalars h;
+  AdamScalars h;
 };
 // a warp's 256 values from `base` on
 template <bool FULL, bool BF, bool EIGHT>
 __device__ __forceinline__ void adam8_block(const Adam8Job& job, float coef, bool clip, size_t base, int lane) {
-  const Adam8Scalars& h = job.h;
+  const AdamScalars& h = job.h;
   const size_t i0 = base + lane * 4;
   int n[2];
   float p[8], g[8], m[8], v[8], near[8];
@@ -375,25 +371,8 @@ __global__ void __launch_bounds__(256) k_adamw8_numbers(const __grid_constant__ 
   }
 }
 
-static double a8_ipow(double b, int e) {
-  double r = 1.0;
-  while (e > 0) { if (e & 1) r *= b; b *= b; e >>= 1; }
-  return r;
-}
-static Adam8Scalars a8_scalars(const det_adamw_desc* d) {
-  const double bc1 = 1.0 - a8_ipow(d->beta1, d->step), bc2 = 1.0 - a8_ipow(d->beta2, d->step);
-  Adam8Scalars h;
-  h.b1 = (float)d->beta1; h.b2 = (float)d->beta2;
-  h.omb1 = 1.0f - h.b1; h.omb2 = 1.0f - h.b2;
-  h.eps = (float)d->eps;
-  h.stepsz = (float)(d->lr / bc1);
-  h.isb2 = (float)(1.0 / sqrt(bc2));
-  h.decay = (float)(1.0 - d->lr * d->weight_decay);
-  return h;
-}
-static bool a8_at(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 static bool a8_moments_at(const void* m, const void* v, const void* s) {
-  return s ? a8_at(m, 4) && a8_at(v, 4) && a8_at(s, 8) : a8_at(m, 16) && a8_at(v, 16);
+  return s ? aligned_to(m, 4) && aligned_to(v, 4) && aligned_to(s, 8) : aligned_to(m, 16) && aligned_to(v, 16);
 }
 // the tensors t, t + 1, ... as jobs of one launch: fill(job, tensor) for each that has values
 template <int CAP, class Jobs, class Fill>
@@ -431,7 +410,7 @@ static int a8_update(const det_adamw_desc* descs, const int* pdtypes, const void
       const bool same = last >= 0 && d.lr == e.lr && d.beta1 == e.beta1 && d.beta2 == e.beta2 && d.eps == e.eps && d.weight_decay == e.weight_decay &&
                         d.step == e.step;
       if (same) jobs.h[j] = jobs.h[j - 1];
-      else jobs.h[j] = a8_scalars(&d);
+      else jobs.h[j] = adamw_scalars(&d);
       last = i;
       jobs.bf[j] = pdtypes[i] == DET_BF16;
     });
@@ -469,7 +448,7 @@ extern "C" int det_adamw8_batch(const det_adamw_desc* descs, const int* pdtypes,
       return DET_ERR_ARG;
     if (n[t] > (size_t)0x7fffffff * A8_VALUES) return DET_ERR_SHAPE;
     const size_t ap = pdtypes[t] == DET_BF16 ? 8 : 16;
-    if (!a8_at(p[t], ap) || !a8_at(p_out[t], ap) || !aligned16(g[t]) || !a8_moments_at(m[t], v[t], s[t]) || !a8_moments_at(m_out[t], v_out[t], s_out[t]))
+    if (!aligned_to(p[t], ap) || !aligned_to(p_out[t], ap) || !aligned16(g[t]) || !a8_moments_at(m[t], v[t], s[t]) || !a8_moments_at(m_out[t], v_out[t], s_out[t]))
       return DET_ERR_ALIGN;
   }
   const auto few = a8_update<ADAM8_FEW>, many = a8_update<ADAM8_JOBS>;

@@ -370,6 +370,7 @@ __device__ __forceinline__ void or_status(int* status, int bit) {
 }
 
 static inline bool aligned16(const void* p) { return (((uintptr_t)p) & 15u) == 0; }
+static inline bool aligned_to(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace det

@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
+#include "../../include/det.h"
 
 namespace det {
 // every kernel launch of the library passes its grid through DET_L, which counts it
@@ -99,6 +100,10 @@ struct DevOnce { bool done[MAX_DEVICES]; };
 // DET_OK or DET_ERR_CUDA; whole: the SM is set up for as much shared memory as it has, so that what this kernel leaves is there for another's CTAs
 int dev_ensure_smem(DevOnce& once, const void* fn, size_t bytes, bool whole = false);
 int dev_sm_count();                                                 // SMs of the current device (0 on error)
+
+// AdamW's constants of a tensor, in binary32 (glue_optim.cu)
+struct AdamScalars { float b1, b2, omb1, omb2, eps, stepsz, isb2, decay; };
+AdamScalars adamw_scalars(const det_adamw_desc* d);
 
 // C[i,j] = sum_k A[i,k] B[j,k] on the tensor cores with the chosen epilogue; host-side checks included
 // fill != 0: this product does not depend on the kernel before it on the stream and takes the SMs that one leaves (common.cuh)

@@ -10,6 +10,10 @@ __device__ __forceinline__ uint32_t bf_pair(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// four low bytes
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
 // eight values rounded to bf16 and back
 __device__ __forceinline__ void round8(float v[8]) {
 #pragma unroll
@@ -162,8 +166,8 @@ __device__ __forceinline__ uint2 a8_codes8(const float v[8], uint32_t field) {
     for (int t = 0; t < 8; ++t) c[t] = a8_code_nonfinite(v[t]);
   }
   uint2 o;
-  o.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
-  o.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+  o.x = low_bytes(c[0], c[1], c[2], c[3]);
+  o.y = low_bytes(c[4], c[5], c[6], c[7]);
   return o;
 }
 // values of eight codes: a byte, its sign flipped, in the low bits of 2^23 is 2^23 + 128 + code.  In pairs, but for the SwiGLU backward pass, for which the

@@ -27,14 +27,11 @@ __device__ __forceinline__ float t8_scale(uint32_t amax) {
 __device__ __forceinline__ float t8_inverse(float s) { return s > 0.0f ? fdiv(1.0f, s) : 0.0f; }     // 0 for a scale that is 0 or NaN
 // rne(v * inv) in the low byte of the result; |v * inv| is at most 127 (1 + 2^-22), so nothing has to be clamped.  dead: the group has the scale NaN.
 __device__ __forceinline__ uint32_t t8_code(float v, float inv) { return __float_as_uint(fadd(fmul(v, inv), 12582912.0f)); }
-__device__ __forceinline__ uint32_t t8_pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
-}
 __device__ __forceinline__ uint2 t8_codes8(const float v[8], float inv, bool dead) {
   uint32_t c[8];
 #pragma unroll
   for (int t = 0; t < 8; ++t) c[t] = t8_code(v[t], inv);
-  return dead ? make_uint2(0u, 0u) : make_uint2(t8_pack4(c[0], c[1], c[2], c[3]), t8_pack4(c[4], c[5], c[6], c[7]));
+  return dead ? make_uint2(0u, 0u) : make_uint2(low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7]));
 }
 
 // Rows of a multiple of 8 columns, 16-byte aligned: WPR warps a row, up to 64 values a lane, which stay in registers as they came, so that a row is read
@@ -409,7 +406,7 @@ __device__ __forceinline__ void t8_code_rows(const T8Grad& x, uint2 (&w)[4][2], 
           g[h][half][t] = k == 0 ? code : __byte_perm(g[h][half][t], code, k == 1 ? 0x3240 : k == 2 ? 0x3410 : 0x4210);
         }
         if (!FULL && r >= x.M) continue;
-        const uint32_t q = ia[k] < 0.0f ? 0u : t8_pack4(a[0], a[1], a[2], a[3]);
+        const uint32_t q = ia[k] < 0.0f ? 0u : low_bytes(a[0], a[1], a[2], a[3]);
         int8_t* row = qa + (size_t)r * ldn;
         if (FULL || at[h] < ldn) *reinterpret_cast<uint32_t*>(row + at[h]) = q;     // behind the row's end zeros
       }
@@ -1240,7 +1237,6 @@ static int t8_quant(const uint16_t* X, int ld, int M, int K, int8_t* q, float* s
   DET_CHECK_LAUNCH();
   return DET_OK;
 }
-static bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 // sizes that every call shares: contractions below 2^17 (int32), rows and columns that tensor maps and tiles can number
 static int t8_sizes(long long M, long long N, long long K) {
   if (M < 0 || N <= 0 || K <= 0) return DET_ERR_ARG;
